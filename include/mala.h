@@ -273,6 +273,63 @@ int mala_decode_paged(mala_tin q, mala_tin kpages, mala_tin vpages, const int32_
                       int Hkv, int num_pages, int page_size, int max_pages_per_seq, int Sq, int d, float scale,
                       float tau, int num_splits, void* ws, size_t ws_bytes, void* cuda_stream);
 
+/* ---- Attention with a learned relative position bias ------------------------------------------------------------
+ * The calls above with one more term in the scores: x = scale * q.k + table[bucket(delta)][h] for query head h and
+ * delta = key position - query position, where the queries are the last Nq of the Nk positions (query row q sits at
+ * q + Nk - Nq, also when not causal).  Everything that the calls above say of scores holds for x: the skip test, lse
+ * (in nats), the retained sets.
+ *   Buckets.  bidirectional != 0: half of the buckets, h = num_buckets / 2 (num_buckets even), belong to each side; the
+ *   keys after the query take the upper half, and n = |delta|.  bidirectional == 0: all h = num_buckets are for the keys
+ *   before the query, n = max(-delta, 0).  With e = h / 2 (rounded down): n < e lies in bucket n of its side, n >= e in
+ *   bucket e + floor((h - e) ln(n / e) / ln(max_distance / e)), at most h - 1; a distance that lies exactly on a border
+ *   belongs to the bucket that begins there.  2 <= num_buckets <= 128 (4 <= when bidirectional), e < max_distance <= 65536.
+ *   table: bf16, entry of bucket b and query head h at [b * sb + h].  Finite values, or -inf: keys of such a bucket are
+ *   masked, and a row that sees no other key gets o = 0, lse = -inf and no gradient.
+ * Head sizes: multiples of 8 up to 128 in all of these calls.  Not causal: any Nq and Nk.
+ * ws: mala_bias_workspace_bytes() bytes, 256-byte aligned (the forward calls need it too: the table laid out by distance). */
+typedef struct {
+  const void* table;                 /* bf16 [num_buckets, Hq] */
+  int64_t sb;                        /* elements from one bucket to the next */
+  int num_buckets, max_distance, bidirectional;
+} mala_rel_bias;
+
+/* mala_fwd_chunk / mala_bwd_chunk with a bias (HOST pointer, read during the call; its table is a device pointer).
+ * dtable: bf16, overwritten, entry of bucket b and head h at [b * dtable_sb + h] (dtable_sb >= Hq): the sum of
+ * dS = P o (dP - D) over batch entries and all retained query-key pairs with that bucket, kept in fp32 and added up in a
+ * fixed order.  With tau > 0 the backward tests and works tile by tile in one pass. */
+int mala_fwd_bias(mala_tin q, mala_tin k, mala_tin v, const mala_rel_bias* bias, mala_tout o, float* lse,
+                  const mala_stats* st, int B, int Hq, int Hkv, int Nq, int Nk, int d, int causal, float scale, float tau,
+                  void* ws, size_t ws_bytes, void* cuda_stream);
+int mala_bwd_bias(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dout, const float* lse,
+                  const mala_rel_bias* bias, mala_tout dq, mala_tout dk, mala_tout dv, void* dtable, int64_t dtable_sb,
+                  const mala_stats* st, int B, int Hq, int Hkv, int Nq, int Nk, int d, int causal, float scale, float tau,
+                  void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* mala_fwd_varlen_prefix / mala_bwd_varlen_prefix with a bias (pass the same offsets twice for self attention).  A sequence
+ * without keys (or, causal != 0, with more queries than keys) gets o = 0, lse = -inf and zero gradients. */
+int mala_fwd_varlen_bias(mala_tin q, mala_tin k, mala_tin v, const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k,
+                         const mala_rel_bias* bias, mala_tout o, float* lse, const mala_stats* st, int B, int Hq, int Hkv,
+                         int total_q, int total_k, int max_seqlen_q, int max_seqlen_k, int d, int causal, float scale,
+                         float tau, void* ws, size_t ws_bytes, void* cuda_stream);
+int mala_bwd_varlen_bias(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dout, const float* lse,
+                         const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, const mala_rel_bias* bias, mala_tout dq,
+                         mala_tout dk, mala_tout dv, void* dtable, int64_t dtable_sb, const mala_stats* st, int B, int Hq,
+                         int Hkv, int total_q, int total_k, int max_seqlen_q, int max_seqlen_k, int d, int causal,
+                         float scale, float tau, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* mala_decode_paged with a bias; a new token's position is that of its own key. */
+int mala_decode_paged_bias(mala_tin q, mala_tin kpages, mala_tin vpages, const int32_t* block_table,
+                           const int32_t* seqlens, const mala_rel_bias* bias, mala_tout o, float* lse_opt,
+                           const mala_stats* st, int B, int Hq, int Hkv, int num_pages, int page_size,
+                           int max_pages_per_seq, int Sq, int d, float scale, float tau, int num_splits, void* ws,
+                           size_t ws_bytes, void* cuda_stream);
+
+/* Scratch of the calls with a bias: op MALA_OP_FWD, MALA_OP_BWD or MALA_OP_DECODE; B sequences of up to Nq queries (decode: Sq)
+ * and Nk keys; total_q: all query rows of packed sequences, 0 for the calls that are not packed; num_splits for
+ * decode only.  Returns 0 for unsupported arguments. */
+size_t mala_bias_workspace_bytes(int op, int B, int Hq, int Hkv, int Nq, int Nk, int total_q, int d, int num_splits,
+                                 int num_buckets, int max_distance);
+
 /* Decode for callers that cannot allocate device memory.  (The paper has no counterpart: this entry point
  * exists for integration reasons only and computes exactly what mala_decode computes.)
  *

@@ -3,9 +3,10 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(HERE, "csrc", "mala_api.cu")
+SRCS = [os.path.join(HERE, "csrc", n) for n in ("mala_api.cu", "mala_bias.cu")]
 LIB = os.path.join(HERE, "libmala.so")
 
 
@@ -20,11 +21,17 @@ def _newest_source_mtime() -> float:
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source_mtime():
         return LIB
-    cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo", "-shared",
-           "-Xcompiler", "-fPIC", "-o", LIB, SRC, "-ldl"]
+    # (one nvcc per source, side by side; the objects go to a folder that does not outlive the call)
+    nvcc = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC"]
     if verbose:
-        cmd.insert(1, "-Xptxas=-v")
-    subprocess.check_call(cmd)
+        nvcc.append("-Xptxas=-v")
+    with tempfile.TemporaryDirectory() as tmp:
+        objs = [os.path.join(tmp, os.path.basename(s) + ".o") for s in SRCS]
+        jobs = [subprocess.Popen(nvcc + ["-c", "-o", o, s]) for o, s in zip(objs, SRCS)]
+        codes = [j.wait() for j in jobs]
+        if any(codes):
+            raise RuntimeError(f"nvcc failed: {[os.path.basename(s) for s, c in zip(SRCS, codes) if c]}")
+        subprocess.check_call(nvcc[:3] + ["-shared", "-o", LIB] + objs + ["-ldl"])
     return LIB
 
 

@@ -14,6 +14,7 @@
 #include "mala_decode.cuh"
 #include "mala_fwd.cuh"
 #include "mala_fwd_one.cuh"
+#include "mala_internal.h"
 #include "tensor_map.h"
 
 namespace mala {
@@ -53,7 +54,7 @@ static int static_scratch_address(int dev, unsigned char** out) {
   return MALA_OK;
 }
 
-static int current_device_checked(int* dev_out) {
+int current_device_checked(int* dev_out) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return MALA_ERR_CUDA;
   if (dev < 0 || dev >= 64) return MALA_ERR_UNSUPPORTED;
@@ -87,7 +88,7 @@ static bool set_smem_one() {
 }
 
 // SMs of a device, asked for once.
-static int sm_count(int dev) {
+int sm_count(int dev) {
   static std::atomic<int> known[64];
   int n = known[dev].load(std::memory_order_relaxed);
   if (n == 0 && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess)
@@ -96,7 +97,7 @@ static int sm_count(int dev) {
 }
 
 // One-time per-device set-up: status word address and dynamic shared memory limits.
-static int device_setup(int dev, int** status_out) {
+int device_setup(int dev, int** status_out) {
   std::lock_guard<std::mutex> lock(g_mu);
   if (!g_status_ptr[dev]) {
     void* ptr = nullptr;
@@ -116,6 +117,7 @@ static int device_setup(int dev, int** status_out) {
     ok = ok && set_smem_one<64>() && set_smem_one<128>() && set_smem_one<256>();
     ok = ok && bwd_set_attributes();
     ok = ok && decode_set_attributes();
+    ok = ok && bias_set_attributes();
     if (!ok) return MALA_ERR_CUDA;
     g_attr_done[dev] = true;
   }
@@ -158,37 +160,26 @@ static int env_flag(const char* name) {
 static int nvtx_on() { static const int v = env_flag("MALA_NVTX"); return v; }
 static int debug_on() { static const int v = env_flag("MALA_DEBUG"); return v; }
 
-struct ApiScope {
-  const char* name;
-  cudaStream_t stream;
-  bool pushed;
-  ApiScope(const char* n, void* s) : name(n), stream((cudaStream_t)s), pushed(false) {
-    if (nvtx_on()) { nvtxRangePushA(name); pushed = true; }
+ApiScope::ApiScope(const char* n, void* s) : name(n), stream((cudaStream_t)s), pushed(false) {
+  if (nvtx_on()) { nvtxRangePushA(name); pushed = true; }
+}
+ApiScope::~ApiScope() { if (pushed) nvtxRangePop(); }
+int ApiScope::finish(int rc) const {
+  if (rc != MALA_OK || !debug_on()) return rc;
+  cudaError_t e = cudaStreamSynchronize(stream);
+  if (e == cudaSuccess) e = cudaGetLastError();
+  if (e != cudaSuccess) {
+    fprintf(stderr, "[mala debug] %s: CUDA error %d (%s)\n", name, (int)e, cudaGetErrorString(e));
+    return MALA_ERR_CUDA;
   }
-  ~ApiScope() { if (pushed) nvtxRangePop(); }
-  int finish(int rc) const {
-    if (rc != MALA_OK || !debug_on()) return rc;
-    cudaError_t e = cudaStreamSynchronize(stream);
-    if (e == cudaSuccess) e = cudaGetLastError();
-    if (e != cudaSuccess) {
-      fprintf(stderr, "[mala debug] %s: CUDA error %d (%s)\n", name, (int)e, cudaGetErrorString(e));
-      return MALA_ERR_CUDA;
-    }
-    int code = 0;
-    if (mala_device_status(&code, 0) != MALA_OK) return MALA_ERR_CUDA;
-    if (code != 0) {
-      fprintf(stderr, "[mala debug] %s: device status %d (a bounded wait expired)\n", name, code);
-      return MALA_ERR_DEVICE_TIMEOUT;
-    }
-    return MALA_OK;
+  int code = 0;
+  if (mala_device_status(&code, 0) != MALA_OK) return MALA_ERR_CUDA;
+  if (code != 0) {
+    fprintf(stderr, "[mala debug] %s: device status %d (a bounded wait expired)\n", name, code);
+    return MALA_ERR_DEVICE_TIMEOUT;
   }
-};
-
-#define MALA_TRY(expr)              \
-  do {                              \
-    const int rc_ = (expr);         \
-    if (rc_ != MALA_OK) return rc_; \
-  } while (0)
+  return MALA_OK;
+}
 
 static const float kLog2e = 1.4426950408889634f;
 
@@ -317,12 +308,23 @@ struct FwdPaging {
   int num_pages, page_size, max_pages_per_seq;
 };
 
+// A relative position bias, and the scratch of its layout by distance (the last bytes of a call's workspace).
+static int check_bias(const mala_rel_bias* bias, int Hq, const void* ws, size_t ws_bytes) {
+  if (!bias || !bias->table || !ws) return MALA_ERR_INVALID_ARG;
+  BiasStarts s;
+  if (!bias_starts(bias->num_buckets, bias->max_distance, bias->bidirectional, &s)) return MALA_ERR_UNSUPPORTED;
+  if ((((uintptr_t)bias->table) & 1) != 0 || (((uintptr_t)ws) & 255) != 0) return MALA_ERR_MISALIGNED;
+  if (bias->sb < 0) return MALA_ERR_INVALID_ARG;
+  if (ws_bytes < bias_expand_bytes(Hq, bias->max_distance)) return MALA_ERR_WORKSPACE_TOO_SMALL;
+  return MALA_OK;
+}
+
 // cu != null: B packed sequences in [1, total, H, d] tensors, N = Nk = the longest one.
 static int fwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse, const mala_stats* st, int B, int Hq,
                     int Hkv, int N, int Nk, int d, int causal, float scale, float tau, void* cuda_stream,
                     const int32_t* cu = nullptr, int total = 0, int num_splits = 1, void* ws = nullptr,
                     size_t ws_bytes = 0, const int32_t* cu_k = nullptr, int total_k = 0,
-                    const FwdPaging* pg = nullptr) {
+                    const FwdPaging* pg = nullptr, const mala_rel_bias* bias = nullptr) {
   if (num_splits < 1) return MALA_ERR_INVALID_ARG;
   if (num_splits > 1) {
     if (cu || num_splits > 65535 || (long long)B * num_splits > 65535) return MALA_ERR_UNSUPPORTED;
@@ -332,8 +334,9 @@ static int fwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse,
         ws_bytes < fwd_split_workspace_bytes(B, Hq, N, padded_head_size(d), num_splits))
       return MALA_ERR_WORKSPACE_TOO_SMALL;
   }
-  MALA_TRY(check_common(B, Hq, Hkv, N, d, scale, tau, 256));
+  MALA_TRY(check_common(B, Hq, Hkv, N, d, scale, tau, bias ? 128 : 256));
   MALA_TRY(check_lengths(N, Nk, causal));
+  if (bias) MALA_TRY(check_bias(bias, Hq, ws, ws_bytes));
   if (!lse) return MALA_ERR_INVALID_ARG;
   const int Bt = cu ? 1 : B, Nt = cu ? total : N, Nkt = cu ? (cu_k ? total_k : total) : Nk;   // extents of the tensors
   MALA_TRY(check_view(q.p, q.sb, q.sn, q.sh, Bt, Nt, Hq));
@@ -408,6 +411,10 @@ static int fwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse,
     return MALA_ERR_CUDA;
   const bool dense = (tau == 0.f);
   int rc;
+  if (bias) {
+    MALA_TRY(bias_expand(bias, Hq, ws, &p.rb, stream));
+    return bias_launch_fwd(D, dense, one, tq, tk, tv, p, stream);
+  }
   if (D == 256) rc = launch_fwd<256>(dense, one, tq, tk, tv, p, stream);
   else if (D == 128) rc = launch_fwd<128>(dense, one, tq, tk, tv, p, stream);
   else rc = launch_fwd<64>(dense, one, tq, tk, tv, p, stream);
@@ -438,7 +445,8 @@ int mala_fwd_chunk(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse, 
 static int bwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dout, const float* lse, mala_tout dq,
                     mala_tout dk, mala_tout dv, const mala_stats* st, int B0, int Hq, int Hkv, int N0, int Nk0, int d,
                     int causal, float scale, float tau, void* ws, size_t ws_bytes, void* cuda_stream,
-                    const int32_t* cu = nullptr, int total = 0, const int32_t* cu_k = nullptr, int total_k = 0) {
+                    const int32_t* cu = nullptr, int total = 0, const int32_t* cu_k = nullptr, int total_k = 0,
+                    const mala_rel_bias* bias = nullptr, void* dtable = nullptr, int64_t dtable_sb = 0) {
   MALA_TRY(check_common(B0, Hq, Hkv, N0, d, scale, tau));
   MALA_TRY(check_lengths(N0, Nk0, causal));
   if (!lse || !ws) return MALA_ERR_INVALID_ARG;
@@ -457,12 +465,29 @@ static int bwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dou
   const int pad_rows = (causal && !cu) ? (Nk0 - N0) % 128 : 0;
   if (ws_bytes < bwd_base_workspace_bytes(B, Hq, cu ? total + (cu_k ? 384 : 128) * B0 : N + pad_rows, padded_head_size(d)))
     return MALA_ERR_WORKSPACE_TOO_SMALL;
+  BwdBias bb;
+  size_t base = 0;
+  if (bias) {   // behind the base scratch: the bias by distance, and the partial sums of the table's gradient
+    if (!dtable) return MALA_ERR_INVALID_ARG;
+    if ((((uintptr_t)dtable) & 1) != 0) return MALA_ERR_MISALIGNED;
+    if (dtable_sb < Hq) return MALA_ERR_INVALID_ARG;
+    base = bwd_base_workspace_bytes(B, Hq, cu ? total + 384 * B0 : N + pad_rows, padded_head_size(d));
+    MALA_TRY(check_bias(bias, Hq, ws, ws_bytes > base ? ws_bytes - base : 0));
+    if (ws_bytes < base + bias_expand_bytes(Hq, bias->max_distance) + bias_part_bytes(B0, Hq, (Nk0 + 127) / 128, bias->num_buckets))
+      return MALA_ERR_WORKSPACE_TOO_SMALL;
+  }
   int dev = 0;
   MALA_TRY(current_device_checked(&dev));
   int* status = nullptr;
   MALA_TRY(device_setup(dev, &status));
+  if (bias) {
+    MALA_TRY(bias_expand(bias, Hq, (uint8_t*)ws + base, &bb.v, (cudaStream_t)cuda_stream));
+    bb.v.part = (float*)((uint8_t*)ws + base + bias_expand_bytes(Hq, bias->max_distance));
+    bb.dtable = dtable;
+    bb.sb = dtable_sb;
+  }
   return bwd_launch(q, k, v, o, dout, lse, dq, dk, dv, st, B0, Hq, Hkv, N0, Nk0, d, causal ? 1 : 0, scale, tau, ws,
-                    ws_bytes, status, sm_count(dev), (cudaStream_t)cuda_stream, cu, total, cu_k, total_k);
+                    ws_bytes, status, sm_count(dev), (cudaStream_t)cuda_stream, cu, total, cu_k, total_k, bias ? &bb : nullptr);
 }
 
 int mala_fwd_chunk_split(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse, const mala_stats* st, int B,
@@ -705,17 +730,16 @@ int mala_decode_multi(mala_tin q, mala_tin kcache, mala_tin vcache, mala_tout o,
                        (cudaStream_t)cuda_stream, nullptr, Sq));
 }
 
-int mala_decode_paged(mala_tin q, mala_tin kpages, mala_tin vpages, const int32_t* block_table,
+static int decode_paged_impl(const ApiScope& scope, const mala_rel_bias* bias, mala_tin q, mala_tin kpages, mala_tin vpages, const int32_t* block_table,
                       const int32_t* seqlens, mala_tout o, float* lse_opt, const mala_stats* st, int B, int Hq,
                       int Hkv, int num_pages, int page_size, int max_pages_per_seq, int Sq, int d, float scale,
                       float tau, int num_splits, void* ws, size_t ws_bytes, void* cuda_stream) {
-  ApiScope scope("mala_decode_paged", cuda_stream);
   if (num_pages <= 0 || page_size <= 0 || max_pages_per_seq <= 0 || Sq <= 0 || !block_table) return MALA_ERR_INVALID_ARG;
   if (page_size < 8 || (page_size % 128 != 0 && 128 % page_size != 0) ||
       (long long)max_pages_per_seq * page_size > 0x7fffffffLL)
     return MALA_ERR_UNSUPPORTED;
   const int Nk = max_pages_per_seq * page_size;   // the longest cache a sequence can hold
-  MALA_TRY(check_common(B, Hq, Hkv, Nk, d, scale, tau, 256));
+  MALA_TRY(check_common(B, Hq, Hkv, Nk, d, scale, tau, bias ? 128 : 256));
   if (num_splits <= 0 || !ws) return MALA_ERR_INVALID_ARG;
   if ((Hq / Hkv) * Sq > 16 || num_splits > 65535) return MALA_ERR_UNSUPPORTED;
   if ((((uintptr_t)block_table) & 3) != 0 || (((uintptr_t)seqlens) & 3) != 0) return MALA_ERR_MISALIGNED;
@@ -725,6 +749,8 @@ int mala_decode_paged(mala_tin q, mala_tin kpages, mala_tin vpages, const int32_
   MALA_TRY(check_view(o.p, o.sb, Sq > 1 ? o.sn : 8, o.sh, B, Sq, Hq));
   if ((((uintptr_t)ws) & 255) != 0) return MALA_ERR_MISALIGNED;
   if (ws_bytes < decode_workspace_bytes(B * Sq, Hq, padded_head_size(d), num_splits)) return MALA_ERR_WORKSPACE_TOO_SMALL;
+  const size_t base = decode_workspace_bytes(B * Sq, Hq, padded_head_size(d), num_splits);   // (the bias by distance lies behind it)
+  if (bias) MALA_TRY(check_bias(bias, Hq, ws, ws_bytes - base));
   int dev = 0;
   MALA_TRY(current_device_checked(&dev));
   int* status = nullptr;
@@ -732,8 +758,95 @@ int mala_decode_paged(mala_tin q, mala_tin kpages, mala_tin vpages, const int32_
   DecPaging pg;
   pg.block_table = block_table; pg.seqlens = seqlens; pg.bt_stride = max_pages_per_seq; pg.page_size = page_size;
   pg.num_pages = num_pages;
+  RelBiasView view;
+  if (bias) MALA_TRY(bias_expand(bias, Hq, (uint8_t*)ws + base, &view, (cudaStream_t)cuda_stream));
   return scope.finish(decode_launch(q, kpages, vpages, o, lse_opt, st, B, Hq, Hkv, Nk, d, scale, tau, num_splits, ws, status,
-                       (cudaStream_t)cuda_stream, &pg, Sq));
+                       (cudaStream_t)cuda_stream, &pg, Sq, bias ? &view : nullptr));
+}
+
+int mala_decode_paged(mala_tin q, mala_tin kpages, mala_tin vpages, const int32_t* block_table,
+                      const int32_t* seqlens, mala_tout o, float* lse_opt, const mala_stats* st, int B, int Hq,
+                      int Hkv, int num_pages, int page_size, int max_pages_per_seq, int Sq, int d, float scale,
+                      float tau, int num_splits, void* ws, size_t ws_bytes, void* cuda_stream) {
+  ApiScope scope("mala_decode_paged", cuda_stream);
+  return decode_paged_impl(scope, nullptr, q, kpages, vpages, block_table, seqlens, o, lse_opt, st, B, Hq, Hkv, num_pages, page_size,
+                           max_pages_per_seq, Sq, d, scale, tau, num_splits, ws, ws_bytes, cuda_stream);
+}
+
+// ---- attention with a learned relative position bias
+
+int mala_decode_paged_bias(mala_tin q, mala_tin kpages, mala_tin vpages, const int32_t* block_table,
+                           const int32_t* seqlens, const mala_rel_bias* bias, mala_tout o, float* lse_opt,
+                           const mala_stats* st, int B, int Hq, int Hkv, int num_pages, int page_size,
+                           int max_pages_per_seq, int Sq, int d, float scale, float tau, int num_splits, void* ws,
+                           size_t ws_bytes, void* cuda_stream) {
+  ApiScope scope("mala_decode_paged_bias", cuda_stream);
+  if (!bias) return MALA_ERR_INVALID_ARG;
+  return decode_paged_impl(scope, bias, q, kpages, vpages, block_table, seqlens, o, lse_opt, st, B, Hq, Hkv, num_pages, page_size,
+                           max_pages_per_seq, Sq, d, scale, tau, num_splits, ws, ws_bytes, cuda_stream);
+}
+
+size_t mala_bias_workspace_bytes(int op, int B, int Hq, int Hkv, int Nq, int Nk, int total_q, int d, int num_splits,
+                                 int num_buckets, int max_distance) {
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Nq <= 0 || Nk <= 0 || total_q < 0 || !head_size_ok(d, 128) || num_buckets < 2 ||
+      num_buckets > kBiasMaxBuckets || max_distance < 1 || max_distance > kBiasMaxDistance)
+    return 0;
+  const size_t table = bias_expand_bytes(Hq, max_distance);
+  const int D = padded_head_size(d);
+  if (op == MALA_OP_FWD) return table;
+  // (a causal chunk that starts inside a tile has up to 127 more padded rows)
+  if (op == MALA_OP_BWD)
+    return (total_q ? bwd_base_workspace_bytes(1, Hq, total_q + 384 * B, D) : bwd_base_workspace_bytes(B, Hq, Nq + 127, D)) + table +
+           bias_part_bytes(B, Hq, (Nk + 127) / 128, num_buckets);
+  if (op == MALA_OP_DECODE) return num_splits > 0 ? decode_workspace_bytes(B * Nq, Hq, D, num_splits) + table : 0;
+  return 0;
+}
+
+int mala_fwd_bias(mala_tin q, mala_tin k, mala_tin v, const mala_rel_bias* bias, mala_tout o, float* lse, const mala_stats* st,
+                  int B, int Hq, int Hkv, int Nq, int Nk, int d, int causal, float scale, float tau, void* ws,
+                  size_t ws_bytes, void* cuda_stream) {
+  ApiScope scope("mala_fwd_bias", cuda_stream);
+  if (!bias) return MALA_ERR_INVALID_ARG;
+  return scope.finish(fwd_impl(q, k, v, o, lse, st, B, Hq, Hkv, Nq, Nk, d, causal, scale, tau, cuda_stream, nullptr, 0, 1, ws,
+                  ws_bytes, nullptr, 0, nullptr, bias));
+}
+
+int mala_bwd_bias(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dout, const float* lse, const mala_rel_bias* bias,
+                  mala_tout dq, mala_tout dk, mala_tout dv, void* dtable, int64_t dtable_sb, const mala_stats* st, int B,
+                  int Hq, int Hkv, int Nq, int Nk, int d, int causal, float scale, float tau, void* ws, size_t ws_bytes,
+                  void* cuda_stream) {
+  ApiScope scope("mala_bwd_bias", cuda_stream);
+  if (!bias) return MALA_ERR_INVALID_ARG;
+  return scope.finish(bwd_impl(q, k, v, o, dout, lse, dq, dk, dv, st, B, Hq, Hkv, Nq, Nk, d, causal, scale, tau, ws, ws_bytes,
+                  cuda_stream, nullptr, 0, nullptr, 0, bias, dtable, dtable_sb));
+}
+
+int mala_fwd_varlen_bias(mala_tin q, mala_tin k, mala_tin v, const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k,
+                         const mala_rel_bias* bias, mala_tout o, float* lse, const mala_stats* st, int B, int Hq, int Hkv,
+                         int total_q, int total_k, int max_seqlen_q, int max_seqlen_k, int d, int causal, float scale,
+                         float tau, void* ws, size_t ws_bytes, void* cuda_stream) {
+  ApiScope scope("mala_fwd_varlen_bias", cuda_stream);
+  if (!bias) return MALA_ERR_INVALID_ARG;
+  MALA_TRY(check_packed(cu_seqlens_q, B, total_q, max_seqlen_q));
+  MALA_TRY(check_packed(cu_seqlens_k, B, total_k, max_seqlen_k));
+  if (causal && max_seqlen_k < max_seqlen_q) return MALA_ERR_UNSUPPORTED;
+  return scope.finish(fwd_impl(q, k, v, o, lse, st, B, Hq, Hkv, max_seqlen_q, max_seqlen_k, d, causal, scale, tau, cuda_stream,
+                  cu_seqlens_q, total_q, 1, ws, ws_bytes, cu_seqlens_k, total_k, nullptr, bias));
+}
+
+int mala_bwd_varlen_bias(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dout, const float* lse,
+                         const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, const mala_rel_bias* bias, mala_tout dq,
+                         mala_tout dk, mala_tout dv, void* dtable, int64_t dtable_sb, const mala_stats* st, int B, int Hq,
+                         int Hkv, int total_q, int total_k, int max_seqlen_q, int max_seqlen_k, int d, int causal,
+                         float scale, float tau, void* ws, size_t ws_bytes, void* cuda_stream) {
+  ApiScope scope("mala_bwd_varlen_bias", cuda_stream);
+  if (!bias) return MALA_ERR_INVALID_ARG;
+  MALA_TRY(check_packed(cu_seqlens_q, B, total_q, max_seqlen_q));
+  MALA_TRY(check_packed(cu_seqlens_k, B, total_k, max_seqlen_k));
+  if ((long long)total_q + 384LL * B > 0x7fffffffLL) return MALA_ERR_UNSUPPORTED;
+  if (causal && max_seqlen_k < max_seqlen_q) return MALA_ERR_UNSUPPORTED;
+  return scope.finish(bwd_impl(q, k, v, o, dout, lse, dq, dk, dv, st, B, Hq, Hkv, max_seqlen_q, max_seqlen_k, d, causal, scale, tau,
+                  ws, ws_bytes, cuda_stream, cu_seqlens_q, total_q, cu_seqlens_k, total_k, bias, dtable, dtable_sb));
 }
 
 int mala_decode_static(mala_tin q, mala_tin kcache, mala_tin vcache, mala_tout o, float* lse_opt, int B, int Hq,

@@ -38,6 +38,7 @@
 #include <cuda_runtime.h>
 
 #include "../../include/mala.h"
+#include "mala_bias.cuh"
 #include "sm100_ptx.cuh"
 #include "tensor_map.h"
 
@@ -90,6 +91,7 @@ struct BwdParams {
   // Launched as a dependent (0: no) of the preprocess kernel, whose vectors the score group reads, or of the list mode, to whose
   // dK and dV it adds: it starts while the last blocks of that kernel run
   int behind;
+  RelBiasView rb;       // relative position bias (kernels with kBias)
 };
 constexpr int kBehindPre = 1, kBehindList = 2;
 
@@ -131,7 +133,10 @@ constexpr int kBwdListHeads = 16;     // query heads of a group in the two-pass 
 
 // kList (with kDense): the tiles are those of the mask rows in p.list_mask, all of them retained: no test, no votes,
 // the dense tile pipeline on a sparse tile sequence.
-template <int D, bool kDense, bool kList = false>
+// kBias: the scores carry a relative position bias (mala_bias.cuh), whose gradient, the sums of dS over the tiles' diagonals,
+// the score group takes beside dS^T: a flat tile's sum goes to one bucket, another tile's diagonals to theirs, and every warp
+// keeps its own sums, per query head, which bias_reduce_kernel adds up in a fixed order.
+template <int D, bool kDense, bool kList = false, bool kBias = false>
 __global__ void __launch_bounds__(768, 1)
 mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                 const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmDO,
@@ -188,6 +193,10 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     return;
   }
   static_assert(!kList || kDense, "the list mode runs the dense tile pipeline");
+  static_assert(!kList || !kBias, "the first pass knows no bias");
+  __shared__ float bsum[kBias ? kBiasWarps : 1][kBias ? kBiasMaxBuckets : 1];   // this head's sums of the table's gradient
+  if constexpr (kBias)
+    for (int x = threadIdx.x; x < kBiasWarps * kBiasMaxBuckets; x += blockDim.x) (&bsum[0][0])[x] = 0.f;
   __shared__ uint32_t lmask[kList ? kBwdListWords : 1];
   __shared__ int list_total;
   const int i0 = p.causal ? max(j - koff, 0) : 0;      // first query block that sees key block j
@@ -456,12 +465,38 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     int h_nx = 0, i_nx = i0;
     bool have_nx = true;
     if (kList) { it.init(lmask, p.wpad, G); have_nx = it.next(h_nx, i_nx); }
+    // Bias of tile i of query head hq_local: one number (true), which is folded into the tile's per-query vectors, or one per
+    // distance.  A tile's first key lies bias_d0(i) after its first query.
+    [[maybe_unused]] const int qoff = p.causal ? koff * 128 : Nkeys - Nq;
+    auto bias_row = [&](int hq_local) -> const float* {
+      return p.rb.b2 + (size_t)(hkv * G + hq_local) * (2 * p.rb.half + 1) + p.rb.half;
+    };
+    auto bias_d0 = [&](int i_) -> int { return bias_within(p.rb, j * 128 - i_ * 128 - qoff); };
+    auto bias_of_tile = [&](int hq_local, int i_) -> float {
+      float b_ = 0.f;
+      return bias_flat(p.rb, bias_row(hq_local), bias_d0(i_), b_) ? b_ : 0.f;
+    };
+    // the table's gradient: sum of the flat tiles since the bucket changed (per thread), and where the head's sums go
+    [[maybe_unused]] float fsum = 0.f;
+    [[maybe_unused]] int fbucket = -1;
+    [[maybe_unused]] float* const wsum = bsum[kBias ? warp - 4 : 0];
+    auto flush_flat = [&]() {
+      if (fbucket >= 0) {
+#pragma unroll
+        for (int m = 16; m > 0; m >>= 1) fsum += __shfl_xor_sync(0xffffffffu, fsum, m);
+        if (lane == 0) wsum[fbucket] += fsum;
+        __syncwarp();
+      }
+      fsum = 0.f;
+    };
     // per-query vectors of tile 0 into slot 0 (published by the first column quarter), then a group sync
     if (qt == 0) {
       if (!kDense && p.behind == kBehindPre) wait_for_primary();
       const size_t x = vec_index(kList ? h_nx : head(0), kList ? i_nx : i0);
-      vec[0][0][rl] = p.lse2[x];
-      vec[0][1][rl] = p.bq[x];
+      float b0 = 0.f;
+      if constexpr (kBias) b0 = bias_of_tile(head(0), i0);
+      vec[0][0][rl] = kBias ? p.lse2[x] - b0 : p.lse2[x];
+      vec[0][1][rl] = kBias ? p.bq[x] - b0 : p.bq[x];
       vec[0][2][rl] = p.Dq[x];
     }
     __syncwarp();
@@ -479,6 +514,10 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       if (qt == 0 && n + 1 < n_tot) {
         const size_t x = kList ? vec_index(h_nx, i_nx) : (last_of_head ? vec_index(head(hq_n + 1), i0) : vec_index(head(hq_n), i + 1));
         nx0 = p.lse2[x]; nx1 = p.bq[x]; nx2 = p.Dq[x];
+        if constexpr (kBias) {
+          const float b1 = bias_of_tile(head(last_of_head ? hq_n + 1 : hq_n), last_of_head ? i0 : i + 1);
+          nx0 -= b1; nx1 -= b1;
+        }
       }
       ok = mbar_wait_warp(&s_full, n & 1, status);
       if (!ok) break;
@@ -486,7 +525,23 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       uint32_t sc[32];
       tmem_ld_x32(tmem_addr(tb, lane_base, Cfg::kColS + qt * 32), sc);
       tmem_wait_ld();
-      if (p.cu && !valid_key) {   // packed sequences: a row past this sequence's end holds the next one's key
+      float cs = c2;                  // the tile's scores in the log2 domain are sc * cs (+ the flat tile's bias, see above)
+      bool flat = true;
+      if constexpr (kBias) {
+        float b_;
+        const float* brow = bias_row(head(hq_n));
+        const int d0 = bias_d0(i);
+        flat = bias_flat(p.rb, brow, d0, b_);
+        if (!flat) {
+          const float* bp = brow + d0 + rl - qt * 32;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) sc[e] = __float_as_uint(fmaf(__uint_as_float(sc[e]), c2, __ldg(bp - e)));
+          cs = 1.f;
+        }
+      }
+      // packed sequences: a row past this sequence's end holds the next one's key (and with a bias a row past the last key must
+      // not reach the sums along the diagonals)
+      if ((kBias || p.cu) && !valid_key) {
         const uint32_t ninf = 0xff800000u;
 #pragma unroll
         for (int e = 0; e < 32; ++e) sc[e] = ninf;
@@ -505,8 +560,8 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float4 x0 = bb[e];
-          crit = fmaxf(crit, fmaxf(fmaxf(fmaf(__uint_as_float(sc[4 * e + 0]), c2, -x0.x), fmaf(__uint_as_float(sc[4 * e + 1]), c2, -x0.y)),
-                                   fmaxf(fmaf(__uint_as_float(sc[4 * e + 2]), c2, -x0.z), fmaf(__uint_as_float(sc[4 * e + 3]), c2, -x0.w))));
+          crit = fmaxf(crit, fmaxf(fmaxf(fmaf(__uint_as_float(sc[4 * e + 0]), cs, -x0.x), fmaf(__uint_as_float(sc[4 * e + 1]), cs, -x0.y)),
+                                   fmaxf(fmaf(__uint_as_float(sc[4 * e + 2]), cs, -x0.z), fmaf(__uint_as_float(sc[4 * e + 3]), cs, -x0.w))));
         }
       }
       // publish the next tile's vectors.  Slot (n+1) % 3 was last read in tile n-2, which every warp has left:
@@ -557,10 +612,10 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const float4 x = ll[e];
-            const float p0 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 0]), c2, -x.x));
-            const float p1 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 1]), c2, -x.y));
-            const float p2 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 2]), c2, -x.z));
-            const float p3 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 3]), c2, -x.w));
+            const float p0 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 0]), cs, -x.x));
+            const float p1 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 1]), cs, -x.y));
+            const float p2 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 2]), cs, -x.z));
+            const float p3 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 3]), cs, -x.w));
             pk[2 * e] = pack_bf16x2(p0, p1);
             pk[2 * e + 1] = pack_bf16x2(p2, p3);
           }
@@ -576,6 +631,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         if (!ok) break;
         tc_fence_after();
         uint32_t w[16];
+        [[maybe_unused]] float ds[kBias ? 32 : 1];   // dS^T before its rounding
         {
           uint32_t dp[32];
           tmem_ld_x32(tmem_addr(tb, lane_base, Cfg::kColDP + qt * 32), dp);
@@ -587,8 +643,11 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             const uint32_t pa = pk[2 * e], pb = pk[2 * e + 1];
             const float p0 = __uint_as_float(pa << 16), p1 = __uint_as_float(pa & 0xffff0000u);
             const float p2 = __uint_as_float(pb << 16), p3 = __uint_as_float(pb & 0xffff0000u);
-            w[2 * e] = pack_bf16x2(p0 * (__uint_as_float(dp[4 * e + 0]) - x.x), p1 * (__uint_as_float(dp[4 * e + 1]) - x.y));
-            w[2 * e + 1] = pack_bf16x2(p2 * (__uint_as_float(dp[4 * e + 2]) - x.z), p3 * (__uint_as_float(dp[4 * e + 3]) - x.w));
+            const float d0 = p0 * (__uint_as_float(dp[4 * e + 0]) - x.x), d1 = p1 * (__uint_as_float(dp[4 * e + 1]) - x.y);
+            const float d2 = p2 * (__uint_as_float(dp[4 * e + 2]) - x.z), d3 = p3 * (__uint_as_float(dp[4 * e + 3]) - x.w);
+            w[2 * e] = pack_bf16x2(d0, d1);
+            w[2 * e + 1] = pack_bf16x2(d2, d3);
+            if constexpr (kBias) { ds[4 * e] = d0; ds[4 * e + 1] = d1; ds[4 * e + 2] = d2; ds[4 * e + 3] = d3; }
           }
         }
         // dS^T also goes to TMEM, over this thread's own (already consumed) dP^T columns: A operand of dK
@@ -609,7 +668,52 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&ds_full);
+        if constexpr (kBias) {   // (behind everything that others wait for)
+          const int d0 = bias_d0(i) + (int)lane_base - qt * 32;   // delta of this warp's 32 x 32 piece: d0 + lane - e
+          if (flat) {
+            const int bk = __ldg(p.rb.bucket + p.rb.half + d0);
+            if (bk != fbucket) { flush_flat(); fbucket = bk; }
+            float t0 = 0.f, t1 = 0.f;
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) { t0 += ds[e]; t1 += ds[e + 1]; }
+            fsum += t0 + t1;
+          } else {
+            // Sums of the piece's 63 diagonals: in step e lane l takes the value of lane (l + e) % 32, which lies on
+            // diagonal l, or, past the last lane, on diagonal l - 32.
+            float on = 0.f, below = 0.f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float t = __shfl_sync(0xffffffffu, ds[e], (lane + e) & 31);
+              if (lane + e < 32) on += t;
+              else below += t;
+            }
+            // ... and of the runs of diagonals that share a bucket (neighbours, since buckets are monotone along delta)
+#pragma unroll
+            for (int half_ = 0; half_ < 2; ++half_) {
+              float t = half_ ? below : on;
+              const int bk = __ldg(p.rb.bucket + p.rb.half + d0 + lane - (half_ ? 32 : 0));
+#pragma unroll
+              for (int m = 1; m < 32; m <<= 1) {
+                const float t2 = __shfl_down_sync(0xffffffffu, t, m);
+                const int bk2 = __shfl_down_sync(0xffffffffu, bk, m);
+                if (lane + m < 32 && bk2 == bk) t += t2;
+              }
+              const int before = __shfl_up_sync(0xffffffffu, bk, 1);
+              if (lane == 0 || before != bk) wsum[bk] += t;
+              __syncwarp();
+            }
+          }
+        }
         ++r;
+      }
+      if constexpr (kBias) {
+        if (last_of_head) {   // the head's sums of the table's gradient, from every warp (and zeros for the next head)
+          flush_flat();
+          fbucket = -1;
+          float* out = p.rb.part + ((((size_t)b * p.Hq + hkv * G + head(hq_n)) * p.Tk + j) * kBiasWarps + (warp - 4)) * p.rb.buckets;
+          for (int x = lane; x < p.rb.buckets; x += 32) { out[x] = wsum[x]; wsum[x] = 0.f; }
+          __syncwarp();
+        }
       }
       if (stat_thread && last_of_head) {   // last tile of this query head
         const size_t row = (size_t)(b * p.Hq + hkv * G + head(hq_n)) * p.Tk + j;
@@ -819,7 +923,7 @@ bwd_preprocess_kernel(const __nv_bfloat16* __restrict__ o, int64_t o_sb, int64_t
     if ((threadIdx.x & 15) == 0) {
       const int r = r0 + x * 16, row = p0 + r - qshift;
       const bool real = row >= 0 && row < N;
-      const float l2 = ls[x] * 1.4426950408889634f;
+      const float l2 = ls[x] == -INFINITY ? INFINITY : ls[x] * 1.4426950408889634f;   // (a row without a key: P = 0)
       const float L = causal ? (float)(row + 1 + (Nk - N)) : (float)Nk;   // visible keys
       lse2[w0 + r] = l2;
       bq[w0 + r] = real ? l2 + (log2_tau - log2f(L)) : INFINITY;
@@ -879,6 +983,7 @@ bwd_convert_dq_kernel(const float* __restrict__ acc, __nv_bfloat16* __restrict__
 }
 
 }  // namespace mala
+#ifndef MALA_KERNELS_ONLY   // (a translation unit with instantiations of its own needs the kernels' text alone)
 #include "mala_bwd_scout.cuh"
 namespace mala {
 
@@ -941,7 +1046,8 @@ inline int bwd_launch_scout(const CUtensorMap& tq, const CUtensorMap& tk, ScoutP
 inline int bwd_launch(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dout, const float* lse, mala_tout dq,
                       mala_tout dk, mala_tout dv, const mala_stats* st, int B, int Hq, int Hkv, int N, int Nk, int d,
                       int causal, float scale, float tau, void* ws, size_t ws_bytes, int* status, int sms, cudaStream_t stream,
-                      const int* cu = nullptr, int total = 0, const int* cu_k = nullptr, int total_k = 0) {
+                      const int* cu = nullptr, int total = 0, const int* cu_k = nullptr, int total_k = 0,
+                      const BwdBias* bias = nullptr) {
   // Packed sequences (cu): N = Nk = the longest sequence; the tensors are [1, total, H, d]; the per-query vectors and
   // the dQ accumulator are laid out per head over Np = total + 128 B rows (rounded up to a tile).
   const int D = padded_head_size(d);         // columns of the kernels and of the dQ accumulator
@@ -1005,11 +1111,18 @@ inline int bwd_launch(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin d
   // (whole backward, 1024 tokens, 2 heads of 64 columns: 27.7 us instead of 39.8, 29.9 instead of 42.2 with 128 columns and
   // nearly every tile skipped; 512 tokens, 32 / 8 heads: 61 instead of 87).
   const bool brief = (long long)Tk * Hkv * B <= sms && (Hq / Hkv) * T <= 16;
-  const bool two_pass = !dense && !brief && MALA_BWD_TWO_PASS && (Hq / Hkv) * wpad <= kBwdListWords && (Hq / Hkv) <= kBwdListHeads &&
+  const bool two_pass = !dense && !brief && !bias && MALA_BWD_TWO_PASS && (Hq / Hkv) * wpad <= kBwdListWords && (Hq / Hkv) <= kBwdListHeads &&
                         ws_bytes >= base_bytes + bwd_list_bytes(B, Hq, T, Tk);
   int rc;
   // (Where every key block has an SM: 1024 tokens, 2 heads of 64 columns, the whole backward 33 -> 28 us, 512 tokens 25 -> 19.)
-  if (!two_pass && !dense && (long long)Tk * Hkv * B <= sms) p.behind = kBehindPre;
+  if (!two_pass && !dense && !bias && (long long)Tk * Hkv * B <= sms) p.behind = kBehindPre;
+  if (bias) {
+    p.rb = bias->v;
+    // (blocks without a tile write no sums)
+    if (cudaMemsetAsync(p.rb.part, 0, (size_t)B * Hq * Tk * kBiasWarps * p.rb.buckets * sizeof(float), stream) != cudaSuccess)
+      return MALA_ERR_CUDA;
+    rc = bias_launch_bwd(D, dense, tq, tk, tv, tdo, tacc, p, stream);
+  } else
   if (two_pass) {
     uint8_t* lw = (uint8_t*)ws + base_bytes;
     ScoutParams sp;
@@ -1044,9 +1157,14 @@ inline int bwd_launch(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin d
     rc = dense ? bwd_launch_main<64, true>(tq, tk, tv, tdo, tacc, p, stream) : bwd_launch_main<64, false>(tq, tk, tv, tdo, tacc, p, stream);
   }
   if (rc != MALA_OK) return rc;
+  if (bias) {
+    rc = bias_launch_reduce(p.rb, B, Hq, Tk, bias->dtable, bias->sb, stream);
+    if (rc != MALA_OK) return rc;
+  }
   auto convert = D == 128 ? bwd_convert_dq_kernel<128> : bwd_convert_dq_kernel<64>;
   return launch_dependent(convert, dim3(T, Hq, B), dim3(256), stream, acc, (__nv_bfloat16*)dq.p, dq.sb, dq.sn, dq.sh, N, Np, scale, cu,
                           qshift, d, cu_k, causal) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
 }  // namespace mala
+#endif

@@ -222,7 +222,8 @@ struct DecPaging {
 inline int decode_launch_with_scratch(mala_tin q, mala_tin kc, mala_tin vc, mala_tout o, float* lse_opt,
                                       const mala_stats* st, int B, int Hq, int Hkv, int Nk, int d, float scale,
                                       float tau, int num_splits, float* o_part, float* lse_part, int* status,
-                                      cudaStream_t stream, const DecPaging* pg = nullptr, int Sq = 1) {
+                                      cudaStream_t stream, const DecPaging* pg = nullptr, int Sq = 1,
+                                      const RelBiasView* bias = nullptr) {
   if (!head_size_ok(d, 256)) return MALA_ERR_UNSUPPORTED;
   const int D = padded_head_size(d);
   const int G = Hq / Hkv;
@@ -277,6 +278,12 @@ inline int decode_launch_with_scratch(mala_tin q, mala_tin kc, mala_tin vc, mala
   const int grid = p.n_items < sms ? p.n_items : sms;   // persistent: one CTA per SM
   const bool sched = p.seqlens && decode_sched_fits(B, p.n_items, grid, 1, D == 256 ? DecCfgT<256>::kSchedItems : DecCfg::kSchedItems);
   const int R = G * Sq;   // rows of a work item
+  if (bias) {
+    p.rb = *bias;
+    const int rc = bias_launch_decode(D, tau == 0.f, sched, R, grid, tq, tk, tv, p, stream);
+    if (rc != MALA_OK) return rc;
+    return launch_decode_merge(D, B * Sq * Hq, o_part, lse_part, o, Sq > 1 ? o.sn : 0, lse_opt, Sq, Hq, num_splits, d, stream);
+  }
 #define MALA_DEC_LAUNCH3(DENSE, GP, MULTI, SCHED)                                                                           \
   {                                                                                                                  \
     if (D == 256) mala_decode_split_kernel<DENSE, GP, MULTI, 256, SCHED><<<grid, DecCfg::kThreads, DecCfgT<256>::kSmemBytes, stream>>>(tq, tk, tv, p); \
@@ -399,12 +406,12 @@ inline int decode_fp8_launch(mala_tin q, mala_tin kc, mala_tin vc, const float* 
 
 inline int decode_launch(mala_tin q, mala_tin kc, mala_tin vc, mala_tout o, float* lse_opt, const mala_stats* st, int B,
                          int Hq, int Hkv, int Nk, int d, float scale, float tau, int num_splits, void* ws, int* status,
-                         cudaStream_t stream, const DecPaging* pg = nullptr, int Sq = 1) {
+                         cudaStream_t stream, const DecPaging* pg = nullptr, int Sq = 1, const RelBiasView* bias = nullptr) {
   float* o_part = (float*)ws;
   float* lse_part =
       (float*)((uint8_t*)ws + decode_align256((size_t)B * Sq * Hq * num_splits * padded_head_size(d) * sizeof(float)));
   return decode_launch_with_scratch(q, kc, vc, o, lse_opt, st, B, Hq, Hkv, Nk, d, scale, tau, num_splits, o_part,
-                                    lse_part, status, stream, pg, Sq);
+                                    lse_part, status, stream, pg, Sq, bias);
 }
 
 }  // namespace mala

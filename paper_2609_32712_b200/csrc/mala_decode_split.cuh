@@ -28,6 +28,7 @@
 // the V tile's coordinates to the UMMA warp) and every sequence may have its own length (which then takes the
 // place of Nk in the item geometry, in L and in the mask of the newest tile).
 #pragma once
+#include "mala_bias.cuh"
 #include "mala_decode_sched.cuh"
 #include "sm100_ptx.cuh"
 
@@ -51,6 +52,7 @@ struct DecParams {
   int B, Hq, Hkv, Nk, tps, num_splits, words, n_items;   // Nk: longest cache the splits are laid out for
   FastDiv by_splits, by_hkv, by_tps;
   float scale_log2, log2_tau;
+  RelBiasView rb;                // relative position bias (kernels with kBias)
 };
 
 // D: columns of the kernel (64, 128 or 256).  With 256 a K / V tile is 64 KB (four panels), the rings hold two K
@@ -125,7 +127,9 @@ __device__ __forceinline__ void lds_row(const float* src, float (&dst)[N]) {
 // launch parameter: 19 sequences of 53645 keys (dense, 64 columns, 64 / 8 heads), which take the order of the numbers, 506 us
 // instead of 498; 4 of 16389 (four tokens, 32 / 8 heads) 84.5 instead of 80.1; 8 of up to 16000 in pages of 16 keys,
 // which take the list, 76.5 instead of 74.4.
-template <bool kDense, int GP, bool kMulti, int D, bool kSched>
+// kBias (with kMulti): the scores carry a relative position bias (mala_bias.cuh), read by distance; a tile whose keys all lie
+// beyond the last bucket's first distance takes one number per row.
+template <bool kDense, int GP, bool kMulti, int D, bool kSched, bool kBias = false>
 __global__ void __launch_bounds__(384, 1)
 mala_decode_split_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                          const __grid_constant__ CUtensorMap tmV, const DecParams p) {
@@ -163,6 +167,8 @@ mala_decode_split_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   const int G = p.Hq / p.Hkv;
   const int R = kMulti ? G * p.Sq : G;     // rows of a work item: row s * G + g = token s, head g of the group
   int* status = p.status;
+  static_assert(!kBias || kMulti, "");
+  if constexpr (kBias) wait_for_primary();
 
   // the Q tile of an item has R <= 16 rows; the other rows of the two stages are never written: clear them once
   for (int i = tid; i < 2 * DecCfg::kQBytes / 16; i += DecCfg::kThreads) reinterpret_cast<uint4*>(sQ)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -743,6 +749,17 @@ mala_decode_split_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         if (head && p.retained) p.retained[stat_row] = 0u;
         continue;
       }
+      // per row: the head's bias at the reach, and (row's position - reach): keys up to there share that number
+      [[maybe_unused]] const float* brow[kBias ? GH : 1];
+      [[maybe_unused]] float bfar[kBias ? GH : 1];
+      if constexpr (kBias) {
+#pragma unroll
+        for (int q = 0; q < GH; ++q) {
+          const int qa = min(rb + q, R - 1);
+          brow[q] = p.rb.b2 + (size_t)(hkv * G + qa % G) * (2 * p.rb.half + 1) + p.rb.half;
+          bfar[q] = __ldg(brow[q] - p.rb.reach);
+        }
+      }
       const int ip = ne & 1;
       const uint32_t colO = DecCfg::kColO + (uint32_t)ip * 16u;
       float m_ref[GH], l[GH], lgl[GH];
@@ -799,7 +816,15 @@ mala_decode_split_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         const int kpos = (j0 - t) * 128 + kt;   // only the newest tile of the sequence has keys that a row does not see
         float x[GH], mx[GH], tmax[GH];
 #pragma unroll
-        for (int q = 0; q < GH; ++q) { x[q] = (kpos < lim[q] && rb + q < R) ? __uint_as_float(sr[q]) * c2 : -INFINITY; mx[q] = x[q]; }
+        for (int q = 0; q < GH; ++q) {
+          float s_ = __uint_as_float(sr[q]) * c2;
+          if constexpr (kBias) {   // (the row's position is lim - 1; the oldest token's keys decide for all rows)
+            const bool far = (j0 - t) * 128 + 127 <= lim[0] - 1 - p.rb.reach;
+            s_ = fmaf(__uint_as_float(sr[q]), c2, far ? bfar[q] : __ldg(brow[q] + max(-p.rb.reach, min(0, kpos - (lim[q] - 1)))));
+          }
+          x[q] = (kpos < lim[q] && rb + q < R) ? s_ : -INFINITY;
+          mx[q] = x[q];
+        }
         RowReduce<GH, 16, true>::run(mx, lane);   // mx[0]: the warp's maximum of row pub_row
         ok = exchange(mx[0], tmax);
         if (!ok) break;

@@ -19,6 +19,7 @@
 //   warps 4-7    softmax group of block A, warps 8-11 of block B (one thread per query row)
 // All synchronisation is by mbarriers with bounded waits.
 #pragma once
+#include "mala_bias.cuh"
 #include "sm100_ptx.cuh"
 
 namespace mala {
@@ -64,7 +65,19 @@ struct FwdParams {
   float* lse_part;               // [B, Hq, num_splits, N] natural log
   float scale_log2;              // scale * log2(e)
   float log2_tau;                // log2(tau); unused by the dense kernel
+  RelBiasView rb;                // relative position bias (kernels with kBias)
 };
+
+// Rows first .. first + count - 1 of a packed sequence whose queries see no key: o = 0, lse = -inf (all threads of the block)
+__device__ __forceinline__ void empty_rows(const FwdParams& p, int b, int h, int row0, int Nq, int first, int count) {
+  const int per = p.d / 8;
+  for (int x = threadIdx.x; x < count * per; x += blockDim.x) {
+    const int row = first + x / per;
+    if (row >= Nq) break;
+    *reinterpret_cast<uint4*>(p.o + (int64_t)(row0 + row) * p.o_sn + (int64_t)h * p.o_sh + (x % per) * 8) = make_uint4(0u, 0u, 0u, 0u);
+    if (x % per == 0) p.lse[(size_t)h * p.total + row0 + row] = -INFINITY;
+  }
+}
 
 template <int D, bool kDense>
 struct FwdCfg {
@@ -80,8 +93,8 @@ struct FwdCfg {
 };
 
 // kSmall: the keys and values lie in pages smaller than a tile (a kernel of its own, so that the copy loop with its
-// table lookups costs the other layouts nothing).
-template <int D, bool kDense, bool kSmall = false>
+// table lookups costs the other layouts nothing).  kBias: the scores carry a relative position bias (mala_bias.cuh).
+template <int D, bool kDense, bool kSmall = false, bool kBias = false>
 __global__ void __launch_bounds__(384, 1)
 mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const FwdParams p) {
@@ -113,7 +126,11 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   // (paged: a length beyond what the block table's row can map is clamped, so no lookup ever leaves the row)
   const int Nkeys = p.block_table ? min(__ldg(p.seqlens_k + b), p.bt_stride * (p.ppt > 1 ? p.prows : p.tpp * 128))
                                   : (p.cu_k ? __ldg(p.cu_k + b + 1) - krow0 : (p.cu ? Nq : p.Nk));
-  if (own_keys && (Nkeys <= 0 || (p.causal && Nkeys < Nq))) return;   // (not defined: no keys, more queries than keys)
+  if constexpr (kBias) wait_for_primary();
+  if (own_keys && (Nkeys <= 0 || (p.causal && Nkeys < Nq))) {   // (not defined: no keys, more queries than keys)
+    if constexpr (kBias) empty_rows(p, b, h, row0, Nq, place.x * 256, 256);
+    return;
+  }
   const int koff = own_keys ? (p.causal ? (Nkeys - Nq) / 128 : 0) : p.koff;
   const int qshift = own_keys ? (p.causal ? (Nkeys - Nq) % 128 : 0) : p.qshift;
   // TMA coordinates (key row, outermost index) of key block jt
@@ -406,6 +423,9 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     const int first = (x == 0) ? firstA : 0;
     const int T = present_x ? (U - first) : 0;       // tiles of this block
     const bool mask_first = x ? (hB == dB) : (hA == dA);
+    // position of the block's first row among the keys, and the head's bias by distance
+    [[maybe_unused]] const int qpos0 = i * 128 + (p.causal ? koff * 128 : Nkeys - Nq);
+    [[maybe_unused]] const float* brow = kBias ? p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half : nullptr;
     // (l: sum of the keys 0-63 of the tiles, and of the keys 64-127 -- in this order, because mala_fwd_one_kernel has a thread for
     // either, and a row comes out the same bit for bit whichever kernel its call takes)
     float m_ref = -INFINITY, l0 = 0.f, l1 = 0.f, lg = -INFINITY;
@@ -435,6 +455,21 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       tmem_ld_x32(tmem_addr(tb, lane_base, colS + 64), s2);
       tmem_ld_x32(tmem_addr(tb, lane_base, colS + 96), s3);
       tmem_wait_ld();
+      float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
+      if constexpr (kBias) {
+        const int d0 = bias_within(p.rb, j * 128 - qpos0);
+        if (!bias_flat(p.rb, brow, d0, bs)) {
+          const float* bp = brow + d0 - rl;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            s0[e] = __float_as_uint(fmaf(__uint_as_float(s0[e]), c2, __ldg(bp + e)));
+            s1[e] = __float_as_uint(fmaf(__uint_as_float(s1[e]), c2, __ldg(bp + e + 32)));
+            s2[e] = __float_as_uint(fmaf(__uint_as_float(s2[e]), c2, __ldg(bp + e + 64)));
+            s3[e] = __float_as_uint(fmaf(__uint_as_float(s3[e]), c2, __ldg(bp + e + 96)));
+          }
+          cs = 1.f; bs = 0.f;
+        }
+      }
       if (t == 0 && mask_first) {
         // first visited tile, when it is the block's newest legal one: causal diagonal and / or the ragged end of
         // the keys
@@ -459,7 +494,8 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         mx[3] = max3(mx[3], __uint_as_float(s3[e]), __uint_as_float(s3[e + 1]));
       }
       // row maximum of the scaled scores, log2 domain
-      const float mt = fmaxf(max3(mx[0], mx[1], __uint_as_float(s0[31])), max3(mx[2], mx[3], fmaxf(fmaxf(__uint_as_float(s1[31]), __uint_as_float(s2[31])), __uint_as_float(s3[31])))) * c2;
+      float mt = fmaxf(max3(mx[0], mx[1], __uint_as_float(s0[31])), max3(mx[2], mx[3], fmaxf(fmaxf(__uint_as_float(s1[31]), __uint_as_float(s2[31])), __uint_as_float(s3[31])))) * cs;
+      if constexpr (kBias) mt = fmaxf(mt + bs, kBiasFloor);
       bool retain = true;
       if (!kDense) {
         // Eq. 3: skip iff rowmax - (m + log l) < log(tau / L) for every valid row
@@ -542,16 +578,16 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         if (!ok) break;
       }
       // P = exp2(s * c2 - m_ref), row sum in fp32 before the bf16 cast, P written over S
-      const float nm = -m_ref;
+      const float nm = kBias ? bs - m_ref : -m_ref;
       float sum0 = 0.f, sum1 = 0.f, sum2 = 0.f, sum3 = 0.f;
       uint32_t pk[16];
 #define MALA_P_CHUNK(SRC, COL)                                                         \
       {                                                                                \
         _Pragma("unroll") for (int e = 0; e < 8; ++e) {                                \
-          const float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), c2, nm));        \
-          const float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), c2, nm));    \
-          const float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), c2, nm));    \
-          const float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), c2, nm));    \
+          const float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), cs, nm));        \
+          const float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), cs, nm));    \
+          const float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), cs, nm));    \
+          const float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), cs, nm));    \
           sum0 += p0; sum1 += p1; sum2 += p2; sum3 += p3;                              \
           pk[2 * e] = pack_bf16x2(p0, p1);                                             \
           pk[2 * e + 1] = pack_bf16x2(p2, p3);                                         \
@@ -590,7 +626,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     if (ok && present_x && p.num_splits > 1) {
       // one range of the keys: normalised fp32 partial and the range's log-normalizer
       tc_fence_after();
-      const float inv = 1.f / l;
+      const float inv = (kBias && l == 0.f) ? 0.f : 1.f / l;   // (a row whose keys all carry -inf)
       const size_t prow = (((size_t)b * p.Hq + h) * p.num_splits + sp) * p.N + row;
 #pragma unroll
       for (int cc = 0; cc < D / 32; ++cc) {
@@ -617,7 +653,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       }
     } else if (ok && present_x) {
       tc_fence_after();
-      const float inv = 1.f / l;
+      const float inv = (kBias && l == 0.f) ? 0.f : 1.f / l;   // (a row whose keys all carry -inf)
       __nv_bfloat16* orow = p.o + (int64_t)bz * p.o_sb + (int64_t)(row0 + row) * p.o_sn + (int64_t)h * p.o_sh;
 #pragma unroll
       for (int cc = 0; cc < D / 32; ++cc) {

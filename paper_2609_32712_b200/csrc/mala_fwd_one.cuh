@@ -78,7 +78,7 @@ struct FwdOneCtl {
   int flag[4], v_tile[2], early_exit;
 };
 
-template <int D, bool kDense, bool kSmall = false>
+template <int D, bool kDense, bool kSmall = false, bool kBias = false>
 __global__ void __launch_bounds__(384, 1)
 mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const FwdParams p) {
@@ -111,7 +111,11 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   const int krow0 = p.cu_k ? __ldg(p.cu_k + b) : row0;
   const int Nkeys = p.block_table ? min(__ldg(p.seqlens_k + b), p.bt_stride * (p.ppt > 1 ? p.prows : p.tpp * 128))
                                   : (p.cu_k ? __ldg(p.cu_k + b + 1) - krow0 : (p.cu ? Nq : p.Nk));
-  if (own_keys && (Nkeys <= 0 || (p.causal && Nkeys < Nq))) return;
+  if constexpr (kBias) wait_for_primary();
+  if (own_keys && (Nkeys <= 0 || (p.causal && Nkeys < Nq))) {
+    if constexpr (kBias) empty_rows(p, b, h, row0, Nq, place.x * 128, 128);
+    return;
+  }
   const int koff = own_keys ? (p.causal ? (Nkeys - Nq) / 128 : 0) : p.koff;
   const int qshift = own_keys ? (p.causal ? (Nkeys - Nq) % 128 : 0) : p.qshift;
   const int Tr = p.cu ? (Nq + qshift + 127) / 128 : p.Tr;
@@ -334,6 +338,9 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const float Lq = p.causal ? (float)(prow_ + 1 + koff * 128) : (float)Nkeys;   // visible keys
     const float theta = kDense ? -INFINITY : (p.log2_tau - log2f(Lq));
     const bool mask_first = j0 == dI;
+    // position of the block's first row among the keys, and the head's bias by distance
+    [[maybe_unused]] const int qpos0 = i * 128 + (p.causal ? koff * 128 : Nkeys - Nq);
+    [[maybe_unused]] const float* brow = kBias ? p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half : nullptr;
     float m_ref = -INFINITY, l = 0.f;                 // l: this thread's keys only
     float lg = -INFINITY;                             // m_ref + log2(l of the row)
     int r = 0;
@@ -357,6 +364,19 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       tmem_ld_x32(tmem_addr(tb, lane_base, colS + 32), s1);
       const uint64_t before = *out_box;
       tmem_wait_ld();
+      float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
+      if constexpr (kBias) {
+        const int d0 = bias_within(p.rb, j * 128 - qpos0);
+        if (!bias_flat(p.rb, brow, d0, bs)) {
+          const float* bp = brow + d0 - rl + half * 64;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            s0[e] = __float_as_uint(fmaf(__uint_as_float(s0[e]), c2, __ldg(bp + e)));
+            s1[e] = __float_as_uint(fmaf(__uint_as_float(s1[e]), c2, __ldg(bp + e + 32)));
+          }
+          cs = 1.f; bs = 0.f;
+        }
+      }
       if (t == 0 && mask_first) {   // the newest legal tile: causal diagonal and / or the ragged end of the keys
         const int lim = (p.causal ? rl : (Nkeys - 1 - j * 128)) - half * 64;
         const uint32_t ninf = 0xff800000u;
@@ -380,7 +400,8 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           mx[c + 2] = max3(mx[c + 2], __uint_as_float(s1[e + c]), __uint_as_float(s1[e + c + 2]));
         }
       float mt = fmaxf(max3(mx[0], mx[1], fmaxf(__uint_as_float(s0[30]), __uint_as_float(s0[31]))),
-                       max3(mx[2], mx[3], fmaxf(__uint_as_float(s1[30]), __uint_as_float(s1[31])))) * c2;
+                       max3(mx[2], mx[3], fmaxf(__uint_as_float(s1[30]), __uint_as_float(s1[31])))) * cs;
+      if constexpr (kBias) mt = fmaxf(mt + bs, kBiasFloor);
       // the row's maximum, and its normalizer after the tile before, from both threads of the row: at once where the test
       // needs the new normalizer, else only if the tile is retained
       ok = letter_put(out_box, before, mt, l, status);
@@ -456,16 +477,16 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         }
       }
       // P = exp2(s * c2 - m_ref), row sum in fp32 before the bf16 cast, P over this thread's own scores
-      const float nm = -m_ref;
+      const float nm = kBias ? bs - m_ref : -m_ref;
       float sum0 = 0.f, sum1 = 0.f, sum2 = 0.f, sum3 = 0.f;
 #define MALA_P_PIECE(SRC, PIECE)                                                       \
       {                                                                                \
         uint32_t pk[16];                                                               \
         _Pragma("unroll") for (int e = 0; e < 8; ++e) {                                \
-          const float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), c2, nm));        \
-          const float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), c2, nm));    \
-          const float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), c2, nm));    \
-          const float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), c2, nm));    \
+          const float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), cs, nm));        \
+          const float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), cs, nm));    \
+          const float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), cs, nm));    \
+          const float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), cs, nm));    \
           sum0 += p0; sum1 += p1; sum2 += p2; sum3 += p3;                              \
           pk[2 * e] = pack_bf16x2(p0, p1);                                             \
           pk[2 * e + 1] = pack_bf16x2(p2, p3);                                         \
@@ -494,7 +515,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     if (ok) ok = mbar_wait_warp(&fin_bar, 0, status);
     if (ok) {
       tc_fence_after();
-      const float inv = 1.f / l;
+      const float inv = (kBias && l == 0.f) ? 0.f : 1.f / l;   // (a row whose keys all carry -inf)
       const bool parts = p.num_splits > 1;             // one range of the keys: normalised fp32 partial and its log-normalizer
       const size_t prow = (((size_t)b * p.Hq + h) * p.num_splits + sp) * p.N + row;
       __nv_bfloat16* orow = p.o + (int64_t)bz * p.o_sb + (int64_t)(row0 + row) * p.o_sn + (int64_t)h * p.o_sh;

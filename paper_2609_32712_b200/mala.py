@@ -38,6 +38,11 @@ class _Stats(ctypes.Structure):
                 ("totals", ctypes.c_void_p)]
 
 
+class _RelBias(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("sb", ctypes.c_int64), ("num_buckets", ctypes.c_int),
+                ("max_distance", ctypes.c_int), ("bidirectional", ctypes.c_int)]
+
+
 def lib():
     """Loads libmala.so (built in-tree by ``paper_2609_32712_b200.build``); fails loudly if absent."""
     global _lib
@@ -91,6 +96,20 @@ def lib():
         L.mala_decode_fp8_paged.restype = i
         L.mala_decode_static.argtypes = [_TIn, _TIn, _TIn, _TOut, vp, i, i, i, i, i, f, f, i, vp]
         L.mala_decode_static.restype = i
+        bp = ctypes.POINTER(_RelBias)
+        L.mala_fwd_bias.argtypes = [_TIn, _TIn, _TIn, bp, _TOut, vp, ctypes.POINTER(_Stats), i, i, i, i, i, i, i, f, f, vp, sz, vp]
+        L.mala_bwd_bias.argtypes = [_TIn, _TIn, _TIn, _TIn, _TIn, vp, bp, _TOut, _TOut, _TOut, vp, ctypes.c_int64,
+                                    ctypes.POINTER(_Stats), i, i, i, i, i, i, i, f, f, vp, sz, vp]
+        L.mala_fwd_varlen_bias.argtypes = [_TIn, _TIn, _TIn, vp, vp, bp, _TOut, vp, ctypes.POINTER(_Stats), i, i, i, i, i, i,
+                                           i, i, i, f, f, vp, sz, vp]
+        L.mala_bwd_varlen_bias.argtypes = [_TIn, _TIn, _TIn, _TIn, _TIn, vp, vp, vp, bp, _TOut, _TOut, _TOut, vp,
+                                           ctypes.c_int64, ctypes.POINTER(_Stats), i, i, i, i, i, i, i, i, i, f, f, vp, sz, vp]
+        L.mala_decode_paged_bias.argtypes = [_TIn, _TIn, _TIn, vp, vp, bp, _TOut, vp, ctypes.POINTER(_Stats), i, i, i, i, i, i,
+                                             i, i, f, f, i, vp, sz, vp]
+        L.mala_bias_workspace_bytes.argtypes = [i] * 11
+        L.mala_bias_workspace_bytes.restype = sz
+        for n in ("mala_fwd_bias", "mala_bwd_bias", "mala_fwd_varlen_bias", "mala_bwd_varlen_bias", "mala_decode_paged_bias"):
+            getattr(L, n).restype = i
         L.mala_test_expire_wait.argtypes = [ctypes.c_longlong, vp]
         L.mala_test_expire_wait.restype = i
         L.mala_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
@@ -547,3 +566,139 @@ def decode_static(q, kcache, vcache, scale: float, tau: float, num_splits: int, 
     if rc != 0:
         raise MalaError(rc, "mala_decode_static")
     return o, lse
+
+
+class RelativeBias:
+    """A learned relative position bias: ``table`` bf16 [num_buckets, Hq] (heads contiguous), the bias of a score being
+    ``table[bucket(key position - query position)][head]`` with the buckets of ``include/mala.h``."""
+
+    def __init__(self, table: torch.Tensor, max_distance: int = 128, bidirectional: bool = False):
+        assert table.dtype is _BF16 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1), \
+            "expects a bf16 table [num_buckets, Hq], heads contiguous"
+        self.table, self.max_distance, self.bidirectional = table, int(max_distance), bool(bidirectional)
+        self.num_buckets, self.heads = table.shape
+        self.c = _RelBias(table.data_ptr(), table.stride(0), self.num_buckets, self.max_distance, int(self.bidirectional))
+
+    def _for(self, q):
+        assert self.heads == q.shape[2] and self.table.device == q.device, "the table has a column per query head of q"
+        return ctypes.byref(self.c)
+
+
+def bias_workspace_bytes(op: int, B: int, Hq: int, Hkv: int, Nq: int, Nk: int, d: int, bias: RelativeBias, total_q: int = 0,
+                         num_splits: int = 0) -> int:
+    return int(lib().mala_bias_workspace_bytes(op, B, Hq, Hkv, Nq, Nk, total_q, d, num_splits, bias.num_buckets,
+                                               bias.max_distance))
+
+
+def fwd_bias(q, k, v, bias: RelativeBias, scale: float, tau: float, causal: bool = True, stats: bool = False, out=None,
+             lse=None, ws=None):
+    """mala_fwd_bias: fwd_chunk with a relative position bias.  q [B,Nq,Hq,d], k, v [B,Nk,Hkv,d]; the queries are the last Nq of
+    the Nk positions.  Returns (o [B,Nq,Hq,d] bf16, lse [B,Hq,Nq] fp32, Stats or None)."""
+    B, Nq, Hq, d = q.shape
+    Nk, Hkv = k.shape[1], k.shape[2]
+    o = torch.empty_like(q) if out is None else out
+    lse = q.new_empty((B, Hq, Nq), dtype=_F32) if lse is None else lse
+    Tq, Tk = -(-(Nq + ((Nk - Nq) % 128 if causal else 0)) // 128), -(-Nk // 128)
+    st = Stats((B, Hq, Tq), -(-Tk // 32), q.device) if stats else None
+    ws = _ws(bias_workspace_bytes(OP_FWD, B, Hq, Hkv, Nq, Nk, d, bias), q.device) if ws is None else ws
+    rc = lib().mala_fwd_bias(_view(q, _TIn), _view(k, _TIn), _view(v, _TIn), bias._for(q), _view(o, _TOut), lse.data_ptr(),
+                             ctypes.byref(st.c) if st else None, B, Hq, Hkv, Nq, Nk, d, int(causal), scale, tau,
+                             ws.data_ptr(), ws.numel(), _stream())
+    if rc != 0:
+        raise MalaError(rc, "mala_fwd_bias")
+    return o, lse, st
+
+
+def bwd_bias(q, k, v, o, do, lse, bias: RelativeBias, scale: float, tau: float, causal: bool = True, stats: bool = False,
+             ws=None, dq=None, dk=None, dv=None):
+    """mala_bwd_bias: returns (dq, dk, dv, dtable bf16 [num_buckets, Hq], Stats or None)."""
+    B, Nq, Hq, d = q.shape
+    Nk, Hkv = k.shape[1], k.shape[2]
+    dq = torch.empty_like(q) if dq is None else dq
+    dk = torch.empty_like(k) if dk is None else dk
+    dv = torch.empty_like(v) if dv is None else dv
+    dtable = q.new_empty((bias.num_buckets, Hq))
+    Tq, Tk = -(-(Nq + ((Nk - Nq) % 128 if causal and Nk >= Nq else 0)) // 128), -(-Nk // 128)
+    st = Stats((B, Hq, Tk), -(-Tq // 32), q.device) if stats else None
+    ws = _ws(bias_workspace_bytes(OP_BWD, B, Hq, Hkv, Nq, Nk, d, bias), q.device) if ws is None else ws
+    rc = lib().mala_bwd_bias(_view(q, _TIn), _view(k, _TIn), _view(v, _TIn), _view(o, _TIn), _view(do, _TIn), lse.data_ptr(),
+                             bias._for(q), _view(dq, _TOut), _view(dk, _TOut), _view(dv, _TOut), dtable.data_ptr(), Hq,
+                             ctypes.byref(st.c) if st else None, B, Hq, Hkv, Nq, Nk, d, int(causal), scale, tau,
+                             ws.data_ptr(), ws.numel(), _stream())
+    if rc != 0:
+        raise MalaError(rc, "mala_bwd_bias")
+    return dq, dk, dv, dtable, st
+
+
+def fwd_varlen_bias(q, k, v, cu_seqlens_q, cu_seqlens_k, max_seqlen_q: int, max_seqlen_k: int, bias: RelativeBias,
+                    scale: float, tau: float, causal: bool = True, stats: bool = False, ws=None):
+    """mala_fwd_varlen_bias: packed q [1,total_q,Hq,d] against packed k, v [1,total_k,Hkv,d] (offsets int32 [B+1] on the
+    device; the same tensor twice for self attention).  Returns (o, lse [Hq,total_q], Stats or None)."""
+    one, total_q, Hq, d = q.shape
+    total_k, Hkv = k.shape[1], k.shape[2]
+    for cu in (cu_seqlens_q, cu_seqlens_k):
+        assert one == 1 and cu.dtype == torch.int32 and cu.is_contiguous()
+    B = cu_seqlens_q.numel() - 1
+    assert cu_seqlens_k.numel() == B + 1
+    o = torch.empty_like(q)
+    lse = q.new_empty((Hq, total_q), dtype=_F32)
+    Tq, Tk = -(-(max_seqlen_q + 127) // 128), -(-max_seqlen_k // 128)
+    st = Stats((B, Hq, Tq), -(-Tk // 32), q.device) if stats else None
+    ws = _ws(bias_workspace_bytes(OP_FWD, B, Hq, Hkv, max_seqlen_q, max_seqlen_k, d, bias), q.device) if ws is None else ws
+    rc = lib().mala_fwd_varlen_bias(_view(q, _TIn), _view(k, _TIn), _view(v, _TIn), cu_seqlens_q.data_ptr(),
+                                    cu_seqlens_k.data_ptr(), bias._for(q), _view(o, _TOut), lse.data_ptr(),
+                                    ctypes.byref(st.c) if st else None, B, Hq, Hkv, total_q, total_k, max_seqlen_q,
+                                    max_seqlen_k, d, int(causal), scale, tau, ws.data_ptr(), ws.numel(), _stream())
+    if rc != 0:
+        raise MalaError(rc, "mala_fwd_varlen_bias")
+    return o, lse, st
+
+
+def bwd_varlen_bias(q, k, v, o, do, lse, cu_seqlens_q, cu_seqlens_k, max_seqlen_q: int, max_seqlen_k: int, bias: RelativeBias,
+                    scale: float, tau: float, causal: bool = True, stats: bool = False, ws=None):
+    """mala_bwd_varlen_bias: returns (dq [1,total_q,Hq,d], dk, dv [1,total_k,Hkv,d], dtable bf16 [num_buckets, Hq], Stats or
+    None)."""
+    one, total_q, Hq, d = q.shape
+    total_k, Hkv = k.shape[1], k.shape[2]
+    for cu in (cu_seqlens_q, cu_seqlens_k):
+        assert one == 1 and cu.dtype == torch.int32 and cu.is_contiguous()
+    B = cu_seqlens_q.numel() - 1
+    assert cu_seqlens_k.numel() == B + 1
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    dtable = q.new_empty((bias.num_buckets, Hq))
+    Tq, Tk = -(-(max_seqlen_q + 127) // 128), -(-max_seqlen_k // 128)
+    st = Stats((B, Hq, Tk), -(-Tq // 32), q.device) if stats else None
+    ws = _ws(bias_workspace_bytes(OP_BWD, B, Hq, Hkv, max_seqlen_q, max_seqlen_k, d, bias, total_q), q.device) if ws is None else ws
+    rc = lib().mala_bwd_varlen_bias(_view(q, _TIn), _view(k, _TIn), _view(v, _TIn), _view(o, _TIn), _view(do, _TIn),
+                                    lse.data_ptr(), cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(), bias._for(q),
+                                    _view(dq, _TOut), _view(dk, _TOut), _view(dv, _TOut), dtable.data_ptr(), Hq,
+                                    ctypes.byref(st.c) if st else None, B, Hq, Hkv, total_q, total_k, max_seqlen_q,
+                                    max_seqlen_k, d, int(causal), scale, tau, ws.data_ptr(), ws.numel(), _stream())
+    if rc != 0:
+        raise MalaError(rc, "mala_bwd_varlen_bias")
+    return dq, dk, dv, dtable, st
+
+
+def decode_paged_bias(q, kpages, vpages, block_table, seqlens, bias: RelativeBias, scale: float, tau: float, num_splits: int,
+                      stats: bool = False, ws=None, out=None, want_lse: bool = True):
+    """mala_decode_paged_bias: decode_paged with a relative position bias (a token's position is that of its own key)."""
+    B, Sq, Hq, d = q.shape
+    num_pages, page_size, Hkv = kpages.shape[0], kpages.shape[1], kpages.shape[2]
+    assert block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.shape[0] == B
+    assert seqlens is None or (seqlens.dtype == torch.int32 and seqlens.is_contiguous() and seqlens.shape == (B,))
+    max_pages = block_table.shape[1]
+    Nk = max_pages * page_size
+    o = torch.empty_like(q) if out is None else out
+    lse = q.new_empty((B, Hq) if Sq == 1 else (B, Sq, Hq), dtype=_F32) if want_lse else None
+    tps = -(-(-(-Nk // num_splits)) // 128)
+    st = Stats((B, Hkv, num_splits), -(-tps // 32), q.device) if stats else None
+    if ws is None:
+        ws = _ws(bias_workspace_bytes(OP_DECODE, B, Hq, Hkv, Sq, Nk, d, bias, num_splits=num_splits), q.device)
+    rc = lib().mala_decode_paged_bias(_view(q, _TIn), _view(kpages, _TIn), _view(vpages, _TIn), block_table.data_ptr(),
+                                      seqlens.data_ptr() if seqlens is not None else None, bias._for(q), _view(o, _TOut),
+                                      lse.data_ptr() if lse is not None else None, ctypes.byref(st.c) if st else None,
+                                      B, Hq, Hkv, num_pages, page_size, max_pages, Sq, d, scale, tau, num_splits,
+                                      ws.data_ptr(), ws.numel(), _stream())
+    if rc != 0:
+        raise MalaError(rc, "mala_decode_paged_bias")
+    return o, lse, st
