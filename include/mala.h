@@ -330,6 +330,53 @@ int mala_decode_paged_bias(mala_tin q, mala_tin kpages, mala_tin vpages, const i
 size_t mala_bias_workspace_bytes(int op, int B, int Hq, int Hkv, int Nq, int Nk, int total_q, int d, int num_splits,
                                  int num_buckets, int max_distance);
 
+/* ---- Filling a paged cache ----------------------------------------------------------------------------------------
+ * What the paged calls read, made on the GPU: a serving step of B requests releases the pages of finished requests, gives
+ * the others pages for their new tokens, and writes the tokens' keys and values into them.  All pointers are device
+ * pointers; nothing is read back to the host, so the calls can be captured in a CUDA graph.
+ *
+ * Pages are those of the paged calls (8, 16, 32, 64 or a multiple of 128 keys).  free_pages [num_pages] lists the free pages in its
+ * first free_count[0] entries; pages are taken off its end and given back behind it.  No output may be an input's buffer
+ * (block_table and free_pages apart): the next step reads what this one wrote.  B <= 16384.
+ *
+ * mala_page_tables: request b holds seqlens[b] tokens, whose pages stand in the first ceil(seqlens[b] / page_size) entries of its
+ * row of block_table [B, max_pages_per_seq], and gets new_tokens[b] more (below 0: none).
+ *   block_table     the new pages are entered behind the old ones; page number x that the step hands out, in the order of the
+ *                   requests, is free_pages[free_count[0] - 1 - x]
+ *   cu_seqlens      [B + 1] first row of each request among the step's new tokens (the sum of new_tokens below 2^31)
+ *   seqlens_out     [B] tokens that it holds afterwards
+ *   slots           int64 [rows] for each new token page * page_size + place in the page; -1 in rows behind the last request
+ *                   and for tokens without a place.  rows may be smaller or larger than the number of new tokens.
+ *   free_count_out  [1] free pages that are left
+ * A request that does not fit its row of the table, or that needs pages after the free ones have run out, gets none: its
+ * seqlens_out is its seqlens and its slots are -1 (requests that need no page are served all the same). */
+int mala_page_tables(const int32_t* seqlens, const int32_t* new_tokens, int32_t* block_table, const int32_t* free_pages,
+                     const int32_t* free_count, int32_t* cu_seqlens, int32_t* seqlens_out, int64_t* slots,
+                     int32_t* free_count_out, int B, int max_pages_per_seq, int page_size, int num_pages, int rows,
+                     void* cuda_stream);
+
+/* The pages of the requests with done[b] != 0 (bytes) go behind the free ones, request by request in the order of their
+ * tables; their seqlens_out is 0, the others' their seqlens.  block_table is left as it is. */
+int mala_release_pages(const uint8_t* done, const int32_t* seqlens, const int32_t* block_table, int32_t* free_pages,
+                       const int32_t* free_count, int32_t* seqlens_out, int32_t* free_count_out, int B, int max_pages_per_seq,
+                       int page_size, int num_pages, void* cuda_stream);
+
+/* k, v: bf16 [rows, Hkv, d] views (sn = row stride, sh = head stride, sb ignored); row t goes to slot slots[t] of kpages, vpages
+ * [num_pages, page_size, Hkv, d], rows whose slot is negative or beyond the pool nowhere.  d a multiple of 8 up to 256.
+ * Two rows with the same slot: either of them is written. */
+int mala_cache_write(mala_tin k, mala_tin v, const int64_t* slots, mala_tout kpages, mala_tout vpages, int rows, int Hkv,
+                     int num_pages, int page_size, int d, void* cuda_stream);
+
+/* The same into e4m3 pages with the scales of mala_decode_fp8_paged (kscale, vscale [num_pages, Hkv, max(1, page_size/128)]):
+ * d a multiple of 16 up to 128, page_size not 8.  The keys that share a scale are a unit (a tile of 128, or a smaller page).
+ * With m the largest magnitude among the unit's new rows of a head: a unit whose first key is among them gets the scale
+ * m / 448 (1 where m is 0); in another one, which holds keys already, the scale s becomes max(s, m / 448), and where that is
+ * larger the codes of the keys before the new ones are rounded again, e4m3(code * s_old / s_new).  New codes are
+ * e4m3(x / s), rounded to nearest even.  Values must be finite.  The rows of a unit must be neighbours with ascending
+ * slots, as mala_page_tables gives them, and no other call may write to these units at the same time. */
+int mala_cache_write_fp8(mala_tin k, mala_tin v, const int64_t* slots, mala_tout kpages8, mala_tout vpages8, float* kscale,
+                         float* vscale, int rows, int Hkv, int num_pages, int page_size, int d, void* cuda_stream);
+
 /* Decode for callers that cannot allocate device memory.  (The paper has no counterpart: this entry point
  * exists for integration reasons only and computes exactly what mala_decode computes.)
  *

@@ -10,6 +10,7 @@ namespace mala {
 int current_device_checked(int* dev_out);
 int device_setup(int dev, int** status_out);
 int sm_count(int dev);
+bool cache_set_attributes();   // (mala_cache.cu)
 
 // NVTX range and debug mode of one launching call (see the environment variables in include/mala.h)
 struct ApiScope {

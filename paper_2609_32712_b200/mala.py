@@ -110,6 +110,12 @@ def lib():
         L.mala_bias_workspace_bytes.restype = sz
         for n in ("mala_fwd_bias", "mala_bwd_bias", "mala_fwd_varlen_bias", "mala_bwd_varlen_bias", "mala_decode_paged_bias"):
             getattr(L, n).restype = i
+        L.mala_page_tables.argtypes = [vp] * 9 + [i] * 5 + [vp]
+        L.mala_release_pages.argtypes = [vp] * 7 + [i] * 4 + [vp]
+        L.mala_cache_write.argtypes = [_TIn, _TIn, vp, _TOut, _TOut, i, i, i, i, i, vp]
+        L.mala_cache_write_fp8.argtypes = [_TIn, _TIn, vp, _TOut, _TOut, vp, vp, i, i, i, i, i, vp]
+        for n in ("mala_page_tables", "mala_release_pages", "mala_cache_write", "mala_cache_write_fp8"):
+            getattr(L, n).restype = i
         L.mala_test_expire_wait.argtypes = [ctypes.c_longlong, vp]
         L.mala_test_expire_wait.restype = i
         L.mala_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
@@ -702,3 +708,77 @@ def decode_paged_bias(q, kpages, vpages, block_table, seqlens, bias: RelativeBia
     if rc != 0:
         raise MalaError(rc, "mala_decode_paged_bias")
     return o, lse, st
+
+
+def _ints(*ts):
+    for t in ts:
+        assert t.dtype is torch.int32 and t.is_contiguous(), "expects contiguous int32 tensors"
+
+
+def page_tables(seqlens, new_tokens, block_table, free_pages, free_count, page_size: int, rows: int):
+    """mala_page_tables: pages for the new tokens of a serving step.  seqlens, new_tokens int32 [B]; block_table int32
+    [B, max_pages_per_seq] (its new entries are written); free_pages int32 [num_pages], free_count int32 [1]; rows: how many
+    slots to write (at least the sum of new_tokens for all of them).  Returns (cu_seqlens int32 [B+1], seqlens int32 [B],
+    slots int64 [rows], free_count int32 [1])."""
+    _ints(seqlens, new_tokens, block_table, free_pages, free_count)
+    B, max_pages = block_table.shape
+    assert seqlens.shape == (B,) and new_tokens.shape == (B,)
+    cu, lens, left = seqlens.new_empty(B + 1), seqlens.new_empty(B), seqlens.new_empty(1)
+    slots = seqlens.new_empty(rows, dtype=torch.int64)
+    rc = lib().mala_page_tables(seqlens.data_ptr(), new_tokens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
+                                free_count.data_ptr(), cu.data_ptr(), lens.data_ptr(), slots.data_ptr(), left.data_ptr(), B,
+                                max_pages, page_size, free_pages.numel(), rows, _stream())
+    if rc != 0:
+        raise MalaError(rc, "mala_page_tables")
+    return cu, lens, slots, left
+
+
+def release_pages(done, seqlens, block_table, free_pages, free_count, page_size: int):
+    """mala_release_pages: the pages of the requests with done[b] (bool or uint8 [B]) go back to free_pages (written in
+    place).  Returns (seqlens int32 [B], free_count int32 [1])."""
+    _ints(seqlens, block_table, free_pages, free_count)
+    B, max_pages = block_table.shape
+    assert seqlens.shape == (B,) and done.shape == (B,) and done.element_size() == 1 and done.is_contiguous()
+    lens, left = seqlens.new_empty(B), seqlens.new_empty(1)
+    rc = lib().mala_release_pages(done.data_ptr(), seqlens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
+                                  free_count.data_ptr(), lens.data_ptr(), left.data_ptr(), B, max_pages, page_size,
+                                  free_pages.numel(), _stream())
+    if rc != 0:
+        raise MalaError(rc, "mala_release_pages")
+    return lens, left
+
+
+def _rows(t: torch.Tensor):
+    s = t.stride()
+    assert t.dtype is _BF16 and len(s) == 3 and s[2] == 1, "expects bf16 [rows,Hkv,d], last dim contiguous"
+    return _TIn(t.data_ptr(), 0, s[0], s[1])
+
+
+def cache_write(k, v, slots, kpages, vpages) -> None:
+    """mala_cache_write: rows of k, v [rows,Hkv,d] to their slots (int64 [rows], negative: nowhere) of the bf16 pages
+    [num_pages, page_size, Hkv, d]."""
+    rows, Hkv, d = k.shape
+    assert slots.dtype is torch.int64 and slots.is_contiguous() and slots.shape == (rows,) and v.shape == k.shape
+    num_pages, page_size = kpages.shape[0], kpages.shape[1]
+    assert kpages.shape == vpages.shape and kpages.shape[2:] == (Hkv, d)
+    rc = lib().mala_cache_write(_rows(k), _rows(v), slots.data_ptr(), _view(kpages, _TOut), _view(vpages, _TOut), rows, Hkv,
+                                num_pages, page_size, d, _stream())
+    if rc != 0:
+        raise MalaError(rc, "mala_cache_write")
+
+
+def cache_write_fp8(k, v, slots, kpages8, vpages8, kscale, vscale) -> None:
+    """mala_cache_write_fp8: the same into e4m3 pages (uint8 or float8_e4m3fn) with their scales, fp32
+    [num_pages, Hkv, max(1, page_size/128)]."""
+    rows, Hkv, d = k.shape
+    assert slots.dtype is torch.int64 and slots.is_contiguous() and slots.shape == (rows,) and v.shape == k.shape
+    num_pages, page_size = kpages8.shape[0], kpages8.shape[1]
+    assert kpages8.shape == vpages8.shape and kpages8.shape[2:] == (Hkv, d)
+    for t in (kscale, vscale):
+        assert t.dtype is _F32 and t.is_contiguous() and tuple(t.shape) == (num_pages, Hkv, max(1, page_size // 128))
+    kp, vp = _view8(kpages8), _view8(vpages8)
+    rc = lib().mala_cache_write_fp8(_rows(k), _rows(v), slots.data_ptr(), _TOut(kp.p, kp.sb, kp.sn, kp.sh),
+                                    _TOut(vp.p, vp.sb, vp.sn, vp.sh), kscale.data_ptr(), vscale.data_ptr(), rows, Hkv, num_pages,
+                                    page_size, d, _stream())
+    if rc != 0:
+        raise MalaError(rc, "mala_cache_write_fp8")
