@@ -264,9 +264,10 @@ def _own(s):
         splits = mala.decode_suggest_splits(c["B"], c["Hkv"], s["longest"])
         return mala.decode_paged_bias(s["q"], s["kpages"], s["vpages"], s["block_table"], s["seqlens"], bias, s["scale"], 0.0, splits)[:2]
     if kind == "tables":
-        held, count = mala.release_pages(s["done"], s["seqlens"], s["block_table"], s["free_pages"], s["free_count"], c["page"])
-        cu, lens, slots, left = mala.page_tables(held, s["new"], s["block_table"], s["free_pages"], count, c["page"], s["total"])
-        return s["block_table"], s["free_pages"], cu, lens, slots, left
+        table, free = s["block_table"].clone(), s["free_pages"].clone()    # (a step changes them: the next pass starts from these again)
+        held, count = mala.release_pages(s["done"], s["seqlens"], table, free, s["free_count"], c["page"])
+        cu, lens, slots, left = mala.page_tables(held, s["new"], table, free, count, c["page"], s["total"])
+        return table, free, cu, lens, slots, left
     if kind == "write":
         mala.cache_write(s["k"], s["v"], s["slots"], s["kpages"], s["vpages"])
         return s["kpages"], s["vpages"]
