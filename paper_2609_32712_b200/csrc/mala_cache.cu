@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "../../include/mala.h"
+#include "mala_decode_sched.cuh"
 #include "mala_internal.h"
 #include "sm100_ptx.cuh"
 
@@ -182,27 +183,43 @@ struct WriteParams {
   int64_t kp_sb, kp_sn, kp_sh, vp_sb, vp_sn, vp_sh;   // bytes
   const int64_t* slots;
   float* kscale; float* vscale;            // e4m3: [num_pages, Hkv, per_page]
-  int rows, Hkv, d, page_size, per_page;
+  int rows, Hkv, page_size, per_page;
+  int cols, per;                           // 16-byte pieces of a head's row of k or v, and of a whole row
+  int unit, chunk;                         // e4m3: keys that share a scale; rows among which a block looks for the first ones of units
   int64_t limit;                           // slots of the pool
+  FastDiv by_per, by_cols, by_page;
 };
 
-// One thread per 16 bytes of a row's K or V (blockIdx.y): a copy, bound by HBM.
+// A thread takes four 16-byte pieces of the call's rows, of K and of V: a copy with eight loads in flight, bound by HBM.
 __global__ void __launch_bounds__(256)
 cache_write_kernel(const WriteParams p) {
-  const int per = p.d / 8 * p.Hkv;
-  const bool is_v = blockIdx.y != 0;
-  const uint8_t* src = is_v ? p.v : p.k;
-  uint8_t* dst = is_v ? p.vp : p.kp;
-  const int64_t s_sn = is_v ? p.v_sn : p.k_sn, s_sh = is_v ? p.v_sh : p.k_sh;
-  const int64_t d_sb = is_v ? p.vp_sb : p.kp_sb, d_sn = is_v ? p.vp_sn : p.kp_sn, d_sh = is_v ? p.vp_sh : p.kp_sh;
-  const int64_t all = (int64_t)p.rows * per;
-  for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < all; x += (int64_t)gridDim.x * 256) {
-    const int row = (int)(x / per), c = (int)(x - (int64_t)row * per), h = c / (p.d / 8), col = c - h * (p.d / 8);
-    const int64_t slot = __ldg(p.slots + row);
-    if (slot < 0 || slot >= p.limit) continue;
-    const int64_t page = slot / p.page_size, at = slot - page * p.page_size;
-    *reinterpret_cast<uint4*>(dst + page * d_sb + at * d_sn + h * d_sh + col * 16) =
-        __ldg(reinterpret_cast<const uint4*>(src + row * s_sn + h * s_sh + col * 16));
+  const int64_t all = (int64_t)p.rows * p.per;
+  for (int64_t x0 = (int64_t)blockIdx.x * 1024 + threadIdx.x; x0 < all; x0 += (int64_t)gridDim.x * 1024) {
+    uint4 wk[4], wv[4];
+    int64_t to_k[4], to_v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t x = x0 + i * 256;
+      to_k[i] = to_v[i] = -1;
+      if (x < all) {
+        const int row = all <= 0xffffffffll ? (int)p.by_per.div((uint32_t)x) : (int)(x / p.per);
+        const int c = (int)(x - (int64_t)row * p.per), h = (int)p.by_cols.div((uint32_t)c), col = (c - h * p.cols) * 16;
+        const int64_t slot = __ldg(p.slots + row);
+        wk[i] = __ldg(reinterpret_cast<const uint4*>(p.k + row * p.k_sn + h * p.k_sh + col));
+        wv[i] = __ldg(reinterpret_cast<const uint4*>(p.v + row * p.v_sn + h * p.v_sh + col));
+        if (slot >= 0 && slot < p.limit) {
+          const int64_t page = p.limit <= 0xffffffffll ? (int64_t)p.by_page.div((uint32_t)slot) : slot / p.page_size, at = slot - page * p.page_size;
+          to_k[i] = page * p.kp_sb + at * p.kp_sn + h * p.kp_sh + col;
+          to_v[i] = page * p.vp_sb + at * p.vp_sn + h * p.vp_sh + col;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (to_k[i] >= 0) {
+        *reinterpret_cast<uint4*>(p.kp + to_k[i]) = wk[i];
+        *reinterpret_cast<uint4*>(p.vp + to_v[i]) = wv[i];
+      }
   }
 }
 
@@ -217,92 +234,143 @@ __device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
   return __half22float2(*reinterpret_cast<__half2*>(&h));
 }
 
-// e4m3 pages: keys in units of min(page_size, 128) that share a scale.  The rows of a unit are neighbours in the call; the
-// block that has the first of them takes the unit, for one KV head and K or V.  16 threads per row in 16-byte loads, 16 rows at a
-// time, held in registers between the two passes over them (largest magnitude, codes), so that they are read once.
-constexpr int kWrite8Rows = 16;    // rows among which a block looks for units that begin
-__global__ void __launch_bounds__(256)
-cache_write8_kernel(const WriteParams p) {
-  const bool is_v = blockIdx.z != 0;
-  const int h = blockIdx.y, t0 = blockIdx.x * kWrite8Rows;
-  const int unit = min(p.page_size, 128);
-  const uint8_t* src = (is_v ? p.v + h * p.v_sh : p.k + h * p.k_sh);
-  const int64_t s_sn = is_v ? p.v_sn : p.k_sn;
-  uint8_t* pages = is_v ? p.vp + h * p.vp_sh : p.kp + h * p.kp_sh;
-  const int64_t d_sb = is_v ? p.vp_sb : p.kp_sb, d_sn = is_v ? p.vp_sn : p.kp_sn;
-  float* scales = is_v ? p.vscale : p.kscale;
-  const int r0 = threadIdx.x >> 4, c = threadIdx.x & 15;
-  const bool mine = c * 8 < p.d;
-  __shared__ float red[8];
-  __shared__ int end_s;
-  for (int t = t0; t < min(p.rows, t0 + kWrite8Rows); ++t) {
-    const int64_t slot = p.slots[t];
-    if (slot < 0 || slot >= p.limit) continue;
-    if (t > 0 && slot % unit != 0 && p.slots[t - 1] + 1 == slot) continue;     // (not the first of its unit)
-    const int off = (int)(slot % unit);
-    // rows of the unit: neighbours whose slots follow one another
-    if (threadIdx.x == 0) end_s = unit - off;
-    __syncthreads();
-    for (int x = threadIdx.x; x < unit - off; x += 256)
-      if (t + x >= p.rows || p.slots[t + x] != slot + x) atomicMin(&end_s, x);
-    __syncthreads();
-    const int n = end_s;
-    const int64_t page = slot / p.page_size, at = slot - page * p.page_size;
-    uint8_t* dst = pages + page * d_sb + at * d_sn;
-    uint4 w[8];
-    float top = 0.f;
+// e4m3 pages: the keys of a unit (min(page_size, 128) of them) share a scale.  The rows of a unit are neighbours in the call, and
+// a block looks among p.chunk rows for those with which a unit begins, for one KV head and K or V.
+//
+// A team of kThreads threads writes one unit: 16 threads per row in 16-byte loads, eight loads in flight each, first the largest
+// magnitude, then the codes; what one round of loads covers (128 rows of a block, 16 of a warp) stays in registers between
+// the two and is read once.  Bound by HBM with many rows (3 bytes per element) and by the chain slots -> rows -> scale ->
+// codes with few.
+template <int kThreads>
+__device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int h, int t, int64_t slot, float* red) {
+  constexpr int kRows = kThreads / 16;
+  const int tid = threadIdx.x & (kThreads - 1), lane = threadIdx.x & 31, r0 = tid >> 4, c = tid & 15;
+  const int unit = p.unit;
+  const bool mine = c < p.cols;
+  const uint8_t* src = (is_v ? p.v + h * p.v_sh : p.k + h * p.k_sh) + c * 16;
+  const int64_t s_sn = is_v ? p.v_sn : p.k_sn, d_sn = is_v ? p.vp_sn : p.kp_sn;
+  const int64_t page = p.limit <= 0xffffffffll ? (int64_t)p.by_page.div((uint32_t)slot) : slot / p.page_size, at = slot - page * p.page_size;
+  const int off = (int)(at & (unit - 1));
+  uint8_t* dst = (is_v ? p.vp + h * p.vp_sh + page * p.vp_sb : p.kp + h * p.kp_sh + page * p.kp_sb) + at * d_sn + c * 8;
+  float* sp = (is_v ? p.vscale : p.kscale) + (page * p.Hkv + h) * p.per_page + at / 128;
+  const float old = *(volatile const float*)sp;   // (before the store below, which a cached load need not be)
+  // rows of the unit: as long as the slots follow one another (every warp finds out for itself)
+  int n = unit - off;
+  for (int x0 = 0; x0 < n; x0 += 32) {
+    const int x = x0 + lane;
+    const uint32_t out = __ballot_sync(0xffffffffu, x < n && (t + x >= p.rows || __ldg(p.slots + t + x) != slot + x));
+    if (out) n = x0 + __ffs(out) - 1;
+  }
+  uint4 w[8];
+  auto load = [&](int first) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+      const int r = first + r0 + i * kRows;
       w[i] = make_uint4(0u, 0u, 0u, 0u);
-      const int r = r0 + i * 16;
-      if (r < n && mine) w[i] = __ldg(reinterpret_cast<const uint4*>(src + (t + r) * s_sn + c * 16));
+      if (r < n && mine) w[i] = __ldg(reinterpret_cast<const uint4*>(src + (int64_t)(t + r) * s_sn));
     }
+  };
+  float top = 0.f;
+  for (int first = 0; first < n; first += 8 * kRows) {
+    load(first);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = max3(top, fabsf(__uint_as_float(u[e] << 16)), fabsf(__uint_as_float(u[e] & 0xffff0000u)));
     }
+  }
 #pragma unroll
-    for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = top;
-    __syncthreads();
-    top = red[0];
+  for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+  if constexpr (kThreads > 32) {
+    if (lane == 0) red[threadIdx.x >> 5] = top;
+    __syncthreads();                       // (and everyone has read the old scale)
 #pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, red[i]);
-    float* sp = scales + (page * p.Hkv + h) * p.per_page + at / 128;
-    const float want = __fdiv_rn(top, 448.f), old = *sp;
-    float s = off == 0 ? want : fmaxf(old, want);
-    if (!(s > 0.f)) s = 1.f;               // (nothing but zeros)
-    __syncthreads();                       // (everyone has read the old scale)
-    if (threadIdx.x == 0) *sp = s;
+    for (int i = 0; i < kThreads / 32; ++i) top = fmaxf(top, red[i]);
+  } else {
+    __syncwarp();
+  }
+  const float want = __fdiv_rn(top, 448.f);
+  float s = off == 0 ? want : fmaxf(old, want);
+  if (!(s > 0.f)) s = 1.f;                 // (nothing but zeros)
+  if (tid == 0) *sp = s;
+  // x / s, rounded as a division: with y = 1 / s correctly rounded, the quotient's first estimate x y is put right by its exact remainder
+  // (Markstein, Computation of elementary functions on the IBM RISC System/6000 processor, 1990).  Scales so small that y or the
+  // remainders leave the range are divided by.
+  const float y = __fdiv_rn(1.f, s);
+  const bool plain = s < 1e-30f || s > 1e30f;
+  auto over_s = [&](float x) -> float {
+    if (plain) return __fdiv_rn(x, s);
+    const float q = x * y;
+    return copysignf(fmaf(fmaf(-q, s, x), y, q), x);   // (a zero's sign would go in the remainder)
+  };
+  for (int first = 0; first < n; first += 8 * kRows) {
+    if (n > 8 * kRows) load(first);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int r = r0 + i * 16;
+      const int r = first + r0 + i * kRows;
       if (r < n && mine) {
         const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
         uint32_t q[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] = e4m3x2(__fdiv_rn(__uint_as_float(u[e] << 16), s), __fdiv_rn(__uint_as_float(u[e] & 0xffff0000u), s));
-        *reinterpret_cast<uint2*>(dst + r * d_sn + c * 8) = make_uint2(q[0] | (q[1] << 16), q[2] | (q[3] << 16));
+        for (int e = 0; e < 4; ++e) q[e] = e4m3x2(over_s(__uint_as_float(u[e] << 16)), over_s(__uint_as_float(u[e] & 0xffff0000u)));
+        *reinterpret_cast<uint2*>(dst + r * d_sn) = make_uint2(q[0] | (q[1] << 16), q[2] | (q[3] << 16));
       }
     }
-    if (off > 0 && s > old) {              // the keys that the unit held: on the new scale
-      for (int r = r0 - off; r < 0; r += 16) {
-        if (!mine) continue;
-        uint2* at8 = reinterpret_cast<uint2*>(dst + r * d_sn + c * 8);
-        const uint2 o = *at8;
-        const uint32_t u[2] = {o.x, o.y};
-        uint32_t q[2];
+  }
+  if (off > 0 && s > old) {                // the keys that the unit held: on the new scale
+    for (int first = -off; first < 0; first += 8 * kRows) {
+      uint2 o[8];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float2 a = from_e4m3x2((uint16_t)u[e]), b = from_e4m3x2((uint16_t)(u[e] >> 16));
-          q[e] = e4m3x2(__fdiv_rn(a.x * old, s), __fdiv_rn(a.y * old, s)) | (e4m3x2(__fdiv_rn(b.x * old, s), __fdiv_rn(b.y * old, s)) << 16);
+      for (int i = 0; i < 8; ++i) {
+        const int r = first + r0 + i * kRows;
+        if (r < 0 && mine) o[i] = *reinterpret_cast<const uint2*>(dst + r * d_sn);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = first + r0 + i * kRows;
+        if (r < 0 && mine) {
+          const uint32_t u[2] = {o[i].x, o[i].y};
+          uint32_t q[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float2 a = from_e4m3x2((uint16_t)u[e]), b = from_e4m3x2((uint16_t)(u[e] >> 16));
+            q[e] = e4m3x2(over_s(a.x * old), over_s(a.y * old)) | (e4m3x2(over_s(b.x * old), over_s(b.y * old)) << 16);
+          }
+          *reinterpret_cast<uint2*>(dst + r * d_sn) = make_uint2(q[0], q[1]);
         }
-        *at8 = make_uint2(q[0], q[1]);
       }
     }
-    __syncthreads();
+  }
+}
+
+__global__ void __launch_bounds__(256, 3)
+cache_write8_kernel(const WriteParams p) {
+  const bool is_v = blockIdx.z != 0;
+  const int h = blockIdx.y, t0 = blockIdx.x * p.chunk, lane = threadIdx.x & 31;
+  __shared__ float red[2][8];
+  // the rows of the chunk (at most 64) with which a unit begins
+  uint64_t begins = 0;
+  for (int x0 = 0; x0 < p.chunk; x0 += 32) {
+    const int t = t0 + x0 + lane;
+    bool first = false;
+    if (x0 + lane < p.chunk && t < p.rows) {
+      const int64_t slot = __ldg(p.slots + t), prev = t > 0 ? __ldg(p.slots + t - 1) : -2;
+      first = slot >= 0 && slot < p.limit && ((slot & (p.unit - 1)) == 0 || prev + 1 != slot);
+    }
+    begins |= (uint64_t)__ballot_sync(0xffffffffu, first) << x0;
+  }
+  // few of them: the whole block takes one after the other; many, which are short: a warp each
+  if (__popcll(begins) <= 2) {
+    for (int x = 0; begins; begins &= begins - 1, x ^= 1) {
+      const int t = t0 + __ffsll((long long)begins) - 1;
+      write8_unit<256>(p, is_v, h, t, __ldg(p.slots + t), red[x]);
+    }
+  } else {
+    for (int x = 0; begins; begins &= begins - 1, ++x) {
+      const int t = t0 + __ffsll((long long)begins) - 1;
+      if ((x & 7) == (int)(threadIdx.x >> 5)) write8_unit<32>(p, is_v, h, t, __ldg(p.slots + t), nullptr);
+    }
   }
 }
 
@@ -335,8 +403,12 @@ static int write_params(WriteParams* w, mala_tin k, mala_tin v, const int64_t* s
   w->kp_sb = kp.sb * item; w->kp_sn = kp.sn * item; w->kp_sh = kp.sh * item;
   w->vp_sb = vp.sb * item; w->vp_sn = vp.sn * item; w->vp_sh = vp.sh * item;
   w->slots = slots; w->kscale = w->vscale = nullptr;
-  w->rows = rows; w->Hkv = Hkv; w->d = d; w->page_size = page_size; w->per_page = page_size < 128 ? 1 : page_size / 128;
+  w->rows = rows; w->Hkv = Hkv; w->page_size = page_size; w->per_page = page_size < 128 ? 1 : page_size / 128;
   w->limit = (int64_t)num_pages * page_size;
+  w->cols = d / 8; w->per = d / 8 * Hkv;
+  w->unit = page_size < 128 ? page_size : 128;
+  w->chunk = 1;
+  w->by_per.set((uint32_t)(w->per > 0 ? w->per : 1)); w->by_cols.set((uint32_t)(w->cols > 0 ? w->cols : 1)); w->by_page.set((uint32_t)page_size);
   return MALA_OK;
 }
 
@@ -398,8 +470,8 @@ int mala_cache_write(mala_tin k, mala_tin v, const int64_t* slots, mala_tout kpa
   int dev = 0, *status = nullptr;
   MALA_TRY(current_device_checked(&dev));
   MALA_TRY(device_setup(dev, &status));
-  const long long blocks = ((long long)rows * Hkv * (d / 8) + 255) / 256, most = 8ll * sm_count(dev);
-  cache_write_kernel<<<dim3((unsigned)(blocks < most ? blocks : most), 2), 256, 0, (cudaStream_t)cuda_stream>>>(w);
+  const long long blocks = ((long long)rows * w.per + 1023) / 1024;
+  cache_write_kernel<<<dim3((unsigned)(blocks < 0x7fffffffll ? blocks : 0x7fffffffll)), 256, 0, (cudaStream_t)cuda_stream>>>(w);
   return scope.finish(cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA);
 }
 
@@ -416,7 +488,9 @@ int mala_cache_write_fp8(mala_tin k, mala_tin v, const int64_t* slots, mala_tout
   int dev = 0, *status = nullptr;
   MALA_TRY(current_device_checked(&dev));
   MALA_TRY(device_setup(dev, &status));
-  cache_write8_kernel<<<dim3((unsigned)((rows + kWrite8Rows - 1) / kWrite8Rows), Hkv, 2), 256, 0, (cudaStream_t)cuda_stream>>>(w);
+  // One row per block as long as all blocks run at once (three per SM); then more, so that few blocks find nothing to do, up to 64
+  while (w.chunk < 64 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 3ll * sm_count(dev)) w.chunk *= 2;
+  cache_write8_kernel<<<dim3((unsigned)((rows + w.chunk - 1) / w.chunk), Hkv, 2), 256, 0, (cudaStream_t)cuda_stream>>>(w);
   return scope.finish(cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA);
 }
 
