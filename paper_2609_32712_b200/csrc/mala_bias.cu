@@ -12,12 +12,31 @@
 namespace mala {
 
 // One thread per distance (blockIdx.x) and head (blockIdx.y): its bucket by counting the starts that it has passed, then one
-// table entry.
+// table entry.  Every block finds the range of its head's values for itself.
+__device__ __forceinline__ float bias_log2(const __nv_bfloat16* at) {
+  const float raw = __bfloat162float(*at), v = raw * 1.4426950408889634f;
+  return isinf(raw) || v != v ? v : fminf(fmaxf(v, -kBiasLimit), kBiasLimit);   // (infinite only where the table is)
+}
 __global__ void __launch_bounds__(256)
-bias_expand_kernel(const __nv_bfloat16* __restrict__ table, int64_t sb, const __grid_constant__ BiasStarts s, int half,
-                   float* __restrict__ b2, int* __restrict__ bucket) {
+bias_expand_kernel(const __nv_bfloat16* __restrict__ table, int64_t sb, const __grid_constant__ BiasStarts s, int buckets, int half,
+                   float* __restrict__ b2, float* __restrict__ vals, float* __restrict__ tops, int* __restrict__ bucket) {
   release_dependents();
-  const int x = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y;
+  const int x = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y, lane = threadIdx.x & 31;
+  float top = -INFINITY, low = INFINITY;
+  bool nan = false;
+  for (int b = lane; b < buckets; b += 32) {
+    const float v = bias_log2(table + (int64_t)b * sb + h);
+    nan = nan || v != v || v == INFINITY;
+    top = fmaxf(top, v);
+    if (v > -INFINITY) low = fminf(low, v);
+  }
+#pragma unroll
+  for (int m = 16; m > 0; m >>= 1) {
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+    low = fminf(low, __shfl_xor_sync(0xffffffffu, low, m));
+  }
+  if (__any_sync(0xffffffffu, nan) || !(top - low <= kBiasRange) || !(fabsf(top) < 1e9f)) top = NAN;
+  if (x == 0) tops[h] = top;
   if (x > 2 * half) return;
   const int delta = x - half;
   const int n = s.side ? abs(delta) : max(-delta, 0);
@@ -27,10 +46,9 @@ bias_expand_kernel(const __nv_bfloat16* __restrict__ table, int64_t sb, const __
     for (int j = 0; j < s.count; ++j) bk += n >= s.first[j];
   }
   if (s.side && delta > 0) bk += s.side;
-  const float v = __bfloat162float(table[(int64_t)bk * sb + h]) * 1.4426950408889634f;
-  // (infinite only where the table is)
-  const bool inf = isinf(__bfloat162float(table[(int64_t)bk * sb + h]));
-  b2[(size_t)h * (2 * half + 1) + x] = inf ? v : (v != v ? v : fminf(fmaxf(v, -kBiasLimit), kBiasLimit));
+  const float v = bias_log2(table + (int64_t)bk * sb + h);
+  b2[(size_t)h * (2 * half + 1) + x] = v;
+  vals[(size_t)h * (2 * half + 1) + x] = top == top ? exp2f(v - top) : v;
   if (h == 0) bucket[x] = bk;
 }
 
@@ -64,11 +82,16 @@ int bias_expand(const mala_rel_bias* bias, int Hq, void* ws, RelBiasView* view, 
   view->half = half;
   view->buckets = bias->num_buckets;
   view->part = nullptr;
+  const size_t per = bias_align256(n * Hq * sizeof(float));
   float* b2 = (float*)ws;
-  int* bucket = (int*)((uint8_t*)ws + bias_align256(n * Hq * sizeof(float)));
+  float* vals = (float*)((uint8_t*)ws + per);
+  int* bucket = (int*)((uint8_t*)ws + 2 * per);
+  float* tops = (float*)((uint8_t*)ws + 2 * per + bias_align256(n * sizeof(int)));
   view->b2 = b2;
+  view->vals = vals;
+  view->top = tops;
   view->bucket = bucket;
-  bias_expand_kernel<<<dim3((unsigned)((n + 255) / 256), Hq), 256, 0, stream>>>((const __nv_bfloat16*)bias->table, bias->sb, s, half, b2, bucket);
+  bias_expand_kernel<<<dim3((unsigned)((n + 255) / 256), Hq), 256, 0, stream>>>((const __nv_bfloat16*)bias->table, bias->sb, s, bias->num_buckets, half, b2, vals, tops, bucket);
   return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
@@ -77,8 +100,8 @@ static int launch_fwd_bias_as(bool one, const CUtensorMap& tq, const CUtensorMap
                               cudaStream_t stream) {
   dim3 grid(one ? p.Tr : (p.Tr + 1) / 2, p.Hq, p.B);
   const cudaError_t e =
-      one ? launch_dependent_smem(mala_fwd_one_kernel<D, kDense, false, true>, grid, dim3(FwdOneCfg<D>::kThreads), FwdOneCfg<D>::kSmemBytes, stream, tq, tk, tv, p)
-          : launch_dependent_smem(mala_fwd_kernel<D, kDense, false, true>, grid, dim3(FwdCfg<D, kDense>::kThreads), FwdCfg<D, kDense>::kSmemBytes, stream, tq, tk, tv, p);
+      one ? launch_dependent_smem(mala_fwd_one_kernel<D, kDense, false, true>, grid, dim3(FwdOneCfg<D, true>::kThreads), FwdOneCfg<D, true>::kSmemBytes, stream, tq, tk, tv, p)
+          : launch_dependent_smem(mala_fwd_kernel<D, kDense, false, true>, grid, dim3(FwdCfg<D, kDense, true>::kThreads), FwdCfg<D, kDense, true>::kSmemBytes, stream, tq, tk, tv, p);
   return e == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
@@ -143,8 +166,8 @@ static bool bias_smem_one(K kernel, int bytes) {
 
 template <int D, bool kDense>
 static bool bias_set_attributes_of() {
-  return bias_smem(mala_fwd_kernel<D, kDense, false, true>, FwdCfg<D, kDense>::kSmemBytes) &&
-         bias_smem_one(mala_fwd_one_kernel<D, kDense, false, true>, FwdOneCfg<D>::kSmemBytes) &&
+  return bias_smem(mala_fwd_kernel<D, kDense, false, true>, FwdCfg<D, kDense, true>::kSmemBytes) &&
+         bias_smem_one(mala_fwd_one_kernel<D, kDense, false, true>, FwdOneCfg<D, true>::kSmemBytes) &&
          bias_smem(mala_bwd_kernel<D, kDense, false, true>, BwdCfg<D>::kSmemBytes);
 }
 

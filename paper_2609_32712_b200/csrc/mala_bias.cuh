@@ -10,8 +10,8 @@
 //
 // Laid out by distance (bias_expand_kernel, once per call): b2[head][delta] = log2(e) * bias in fp32 and bucket[delta], for
 // |delta| <= reach + kBiasPad, where reach is the distance at which the last bucket begins.  A kernel's 128 x 128 tile spans
-// 255 values of delta.  Where they all lie in one bucket the tile's bias is one number, which goes into the exponential's
-// offset and costs nothing per score ("flat" tiles; all that lie beyond `reach`, and wide buckets' inside).
+// 255 values of delta.  Beyond `reach` they are one number, which goes into the exponential's offset and costs nothing per
+// score (a "far" tile); nearer, the 255 values of the tile are staged in shared memory.
 #pragma once
 #include <cuda_bf16.h>
 #include <math.h>
@@ -31,8 +31,18 @@ constexpr int kBiasPad = 256;
 // their exponentials are 0 and not NaN, and end as (0, -inf).
 constexpr float kBiasLimit = 2e38f, kBiasFloor = -3e38f;
 
+// The dense kernels take a tile that is not far by factors: exp2(s + b - m) = exp2(s + top - m) * exp2(b - top), with top the
+// head's largest bias.  m then only has to be no smaller than the scores are, so the row maximum needs no bias, and the factors
+// are read and multiplied beside the exponentials, which are bound by the exponential unit, not before them, where the
+// whole chain of the tile waits.  exp2(b - top) is as small as the head's values are apart: up to 2^-60 that costs no
+// precision (fp32 sums, bf16 P); heads with more, or with a NaN, have it added.  The kernels with the skip test add: Eq. 3
+// needs the rows' true maxima.
+constexpr float kBiasRange = 60.f;
+
 struct RelBiasView {
   const float* b2;        // [Hq][2 half + 1], delta at [half + delta]
+  const float* vals;      // what the dense kernels stage: exp2(b2 - top[head]), or b2 where top[head] is NaN
+  const float* top;       // [Hq] the head's largest b2; NaN where its values are too far apart for factors (see kBiasRange)
   const int* bucket;      // [2 half + 1]
   int reach, half;        // half = reach + kBiasPad
   float* part;            // backward: [B][Hq][Tk][kBiasWarps][buckets] partial sums of the table's gradient
@@ -40,18 +50,56 @@ struct RelBiasView {
 };
 constexpr int kBiasWarps = 16;   // warps of the backward's score group, each with sums of its own
 
-// The tile whose first key lies d0 after its first query (delta = d0 - 127 .. d0 + 127): whether its bias is one number, and
-// that number.  One that would swallow the scores it is added to is none (a row of lowest values then weighs its keys alike,
-// in this tile as in the others).
-__device__ __forceinline__ bool bias_flat(const RelBiasView& v, const float* row, int d0, float& value) {
-  if (d0 + 127 <= -v.reach) value = __ldg(row - v.reach);
-  else if (d0 - 127 >= v.reach) value = __ldg(row + v.reach);
-  else if (__ldg(v.bucket + v.half + d0 - 127) == __ldg(v.bucket + v.half + d0 + 127)) value = __ldg(row + d0);
-  else return false;
-  return fabsf(value) < 1e9f || value == -INFINITY;
-}
-// d0 moved to where the tile lies in the laid out part, with the same buckets
+template <bool V> struct BiasBool { static constexpr bool value = V; };
+
+// d0 of a tile (its first key lies d0 after its first query; delta = d0 - 127 .. d0 + 127), moved to where the tile lies in the
+// laid out part, with the same buckets
 __device__ __forceinline__ int bias_within(const RelBiasView& v, int d0) { return max(-v.reach - 128, min(v.reach + 128, d0)); }
+
+// A head's bias beyond the reach on either side.  A tile that lies there is far: its bias is that number -- unless it would
+// swallow the scores it is added to (a row of lowest values then weighs its keys alike, in this tile as in the nearer ones).
+struct BiasFar {
+  float before, after;
+  __device__ __forceinline__ void fetch(const RelBiasView& v, const float* row) {
+    before = __ldg(row - v.reach);
+    after = __ldg(row + v.reach);
+  }
+  static __device__ __forceinline__ bool small(float x) { return fabsf(x) < 1e9f || x == -INFINITY; }
+  __device__ __forceinline__ bool is(const RelBiasView& v, int d0) const {
+    return (d0 + 127 <= -v.reach && small(before)) || (d0 - 127 >= v.reach && small(after));
+  }
+  __device__ __forceinline__ float value(int d0) const { return d0 < 0 ? before : after; }
+};
+
+// The 255 values of a tile that is not far, in shared memory.  Value number y belongs to one diagonal, and a thread of row r needs
+// those from 127 - r on, one per column.  So that it can take them four at a time whatever r is, they lie there four times, copy c
+// moved by c places: a thread reads 16-byte pieces of copy (127 - r) % 4.  The copies' distance puts the eight lanes that are
+// served at once into different banks.
+constexpr int kBiasPitch = 264, kBiasSlotFloats = 4 * kBiasPitch;
+__device__ __forceinline__ void bias_put(float* slot, int y, float v) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    if (y >= c) slot[c * kBiasPitch + y - c] = v;
+}
+// where the thread whose first value is number y begins
+__device__ __forceinline__ const float4* bias_from(const float* slot, int y) {
+  return reinterpret_cast<const float4*>(slot + (y & 3) * kBiasPitch + (y & ~3));
+}
+// s = s * c + b for N scores
+template <int N>
+__device__ __forceinline__ void bias_add(uint32_t (&s)[N], float c, const float4* b) {
+  uint64_t cc;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(cc) : "f"(c));
+#pragma unroll
+  for (int e = 0; e < N / 4; ++e) {
+    const float4 v = b[e];
+    asm("{\n\t.reg .b64 x, y;\n\t"
+        "mov.b64 x, {%0, %1};\n\tmov.b64 y, {%5, %6};\n\tfma.rn.f32x2 x, x, %4, y;\n\tmov.b64 {%0, %1}, x;\n\t"
+        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%7, %8};\n\tfma.rn.f32x2 x, x, %4, y;\n\tmov.b64 {%2, %3}, x;\n\t}"
+        : "+r"(s[4 * e]), "+r"(s[4 * e + 1]), "+r"(s[4 * e + 2]), "+r"(s[4 * e + 3])
+        : "l"(cc), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w));
+  }
+}
 
 // The distances at which the buckets e + 1 .. h - 1 of a side begin.
 struct BiasStarts {
@@ -82,7 +130,7 @@ inline size_t bias_align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // Scratch of the expanded bias; `max_distance` bounds the reach.
 inline size_t bias_expand_bytes(int Hq, int max_distance) {
   const size_t n = 2 * ((size_t)max_distance + kBiasPad) + 1;
-  return bias_align256(n * Hq * sizeof(float)) + bias_align256(n * sizeof(int));
+  return 2 * bias_align256(n * Hq * sizeof(float)) + bias_align256(n * sizeof(int)) + bias_align256(Hq * sizeof(float));
 }
 inline size_t bias_part_bytes(long long B, int Hq, long long Tk, int num_buckets) {
   return bias_align256((size_t)B * Hq * Tk * kBiasWarps * num_buckets * sizeof(float));

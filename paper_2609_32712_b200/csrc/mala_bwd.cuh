@@ -95,7 +95,7 @@ struct BwdParams {
 };
 constexpr int kBehindPre = 1, kBehindList = 2;
 
-template <int D>
+template <int D, bool kBias = false>
 struct BwdCfg {
   static constexpr int kPanels = D / 64;
   static constexpr int kTileBytes = 128 * D * 2;
@@ -104,6 +104,12 @@ struct BwdCfg {
   // have consumed it (D = 128); for D = 64 a dO stage is too small, so two separate dS stages follow.
   static constexpr int kSmemBytes = 6 * kTileBytes + (D == 128 ? 0 : 2 * kDsBytes) + 1024;
   static constexpr int kThreads = 768;
+  // Registers of the issuing warpgroup, the score group's four and the dQ group: 768 x 80 in all.  With a bias the score group
+  // needs more than 72; with 64 columns the dQ group can give them.
+  static constexpr int kRegsIssue = kBias && D == 64 ? 32 : 40;
+  static constexpr int kRegsScore = kBias && D == 64 ? 88 : 72;
+  static constexpr int kRegsDq = kBias && D == 64 ? 96 : 152;
+  static_assert(kRegsIssue + 4 * kRegsScore + kRegsDq == 6 * 80, "");
   static constexpr uint32_t kColS = 0, kColDP = 128, kColDV = 256, kColDK = 384;
 };
 
@@ -141,7 +147,7 @@ __global__ void __launch_bounds__(768, 1)
 mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                 const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmDO,
                 const __grid_constant__ CUtensorMap tmAcc, const BwdParams p) {
-  using Cfg = BwdCfg<D>;
+  using Cfg = BwdCfg<D, kBias>;
   constexpr int PAN = Cfg::kPanels;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -194,6 +200,9 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   }
   static_assert(!kList || kDense, "the list mode runs the dense tile pipeline");
   static_assert(!kList || !kBias, "the first pass knows no bias");
+  // bias of tiles that are not far, and the buckets of its 255 distances: tile n's in slot n & 3
+  __shared__ __align__(16) float bias_s[kBias ? 4 : 1][kBias ? kBiasSlotFloats : 4];
+  __shared__ uint8_t bias_k[kBias ? 4 : 1][kBias ? 256 : 1];
   __shared__ float bsum[kBias ? kBiasWarps : 1][kBias ? kBiasMaxBuckets : 1];   // this head's sums of the table's gradient
   if constexpr (kBias)
     for (int x = threadIdx.x; x < kBiasWarps * kBiasMaxBuckets; x += blockDim.x) (&bsum[0][0])[x] = 0.f;
@@ -274,7 +283,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   const uint32_t tb = tmem_base_s;
 
   if (warp < 4) {
-  reg_dealloc<40>();
+  reg_dealloc<Cfg::kRegsIssue>();
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer
     if (lane == 0) {
@@ -444,7 +453,8 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     // columns 32..63, and so on (the four warps of a row reach the same TMEM lane quadrant).  A thread
     // reads its 32 score columns once; P^T (bf16, 16 packed columns) overwrites the first half of the
     // thread's own score columns, so no thread ever touches a column another thread still has to read.
-    reg_dealloc<72>();
+    if constexpr (Cfg::kRegsScore > 80) reg_alloc<Cfg::kRegsScore>();
+    else reg_dealloc<Cfg::kRegsScore>();
     const uint32_t lane_base = (uint32_t)(warp & 3) * 32u;
     const int rl = (int)lane_base + lane;
     const int qt = (warp - 4) >> 2;                 // column quarter
@@ -465,22 +475,47 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     int h_nx = 0, i_nx = i0;
     bool have_nx = true;
     if (kList) { it.init(lmask, p.wpad, G); have_nx = it.next(h_nx, i_nx); }
-    // Bias of tile i of query head hq_local: one number (true), which is folded into the tile's per-query vectors, or one per
-    // distance.  A tile's first key lies bias_d0(i) after its first query.
+    // Bias of tile i of a query head.  A far tile's number is folded into the tile's per-query vectors, which take in the head's
+    // largest value for a near one where that goes by factors (see kBiasRange).  A near tile's values are published two tiles
+    // ahead, behind all that others wait for in a tile.  (Slot n + 2 was last read in tile n - 2, which every warp has left
+    // when one is in tile n, and the readers see the values through the chain publisher's P^T of tile n + 1 -> UMMA warp ->
+    // scores of tile n + 2.)  The tile's first key lies bias_d0(i) after its first query, and value number y belongs to
+    // delta = bias_d0(i) + 127 - y.
     [[maybe_unused]] const int qoff = p.causal ? koff * 128 : Nkeys - Nq;
-    auto bias_row = [&](int hq_local) -> const float* {
-      return p.rb.b2 + (size_t)(hkv * G + hq_local) * (2 * p.rb.half + 1) + p.rb.half;
+    auto bias_d0 = [&](int i_) -> int { return j * 128 - i_ * 128 - qoff; };
+    auto bias_head = [&](int x) -> size_t { return (size_t)(hkv * G + head(x)) * (2 * p.rb.half + 1) + p.rb.half; };
+    [[maybe_unused]] BiasFar far_, far_next;
+    [[maybe_unused]] float btop = NAN, btop_next = NAN;
+    [[maybe_unused]] float bv0 = 0.f, bv1 = 0.f;
+    [[maybe_unused]] int bkt = 0;
+    auto bias_of_head = [&](int x, BiasFar& f, float& top_) {
+      f.fetch(p.rb, p.rb.b2 + bias_head(x));
+      if (kDense) top_ = __ldg(p.rb.top + hkv * G + head(x));
     };
-    auto bias_d0 = [&](int i_) -> int { return bias_within(p.rb, j * 128 - i_ * 128 - qoff); };
-    auto bias_of_tile = [&](int hq_local, int i_) -> float {
-      float b_ = 0.f;
-      return bias_flat(p.rb, bias_row(hq_local), bias_d0(i_), b_) ? b_ : 0.f;
+    auto bias_fold = [&](const BiasFar& f, float top_, int i_) -> float {
+      const int d0 = bias_d0(i_);
+      return f.is(p.rb, d0) ? f.value(d0) : (top_ == top_ ? top_ : 0.f);
     };
-    // the table's gradient: sum of the flat tiles since the bucket changed (per thread), and where the head's sums go
+    auto bias_fetch = [&](int x, int i_, const BiasFar& f) -> bool {   // (whether there is something to publish)
+      if (f.is(p.rb, bias_d0(i_))) return false;
+      const float* at = (kDense ? p.rb.vals : p.rb.b2) + bias_head(x);
+      const int d0 = bias_within(p.rb, bias_d0(i_));
+      bv0 = __ldg(at + d0 + 127 - (rl + qt));                // copy qt, places rl and rl + 128
+      bv1 = __ldg(at + d0 + 127 - min(rl + 128 + qt, 254));
+      if (qt < 2) bkt = __ldg(p.rb.bucket + p.rb.half + d0 + 127 - min(rl + qt * 128, 254));
+      return true;
+    };
+    auto bias_publish = [&](int n_) {
+      float* dst = bias_s[n_ & 3] + qt * kBiasPitch + rl;
+      dst[0] = bv0;
+      dst[128] = bv1;
+      if (qt < 2) bias_k[n_ & 3][rl + qt * 128] = (uint8_t)bkt;
+    };
+    // the table's gradient: sum of the far tiles since the side changed (per thread), and where the head's sums go
     [[maybe_unused]] float fsum = 0.f;
     [[maybe_unused]] int fbucket = -1;
     [[maybe_unused]] float* const wsum = bsum[kBias ? warp - 4 : 0];
-    auto flush_flat = [&]() {
+    auto flush_far = [&]() {
       if (fbucket >= 0) {
 #pragma unroll
         for (int m = 16; m > 0; m >>= 1) fsum += __shfl_xor_sync(0xffffffffu, fsum, m);
@@ -490,11 +525,20 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       fsum = 0.f;
     };
     // per-query vectors of tile 0 into slot 0 (published by the first column quarter), then a group sync
+    if constexpr (kBias) {
+      bias_of_head(0, far_, btop);
+      if (bias_fetch(0, i0, far_)) bias_publish(0);
+      if (n_tot > 1) {                 // tile 1: of this head, or the next one's first
+        if (ni > 1) far_next = far_;
+        else bias_of_head(1, far_next, btop_next);
+        if (bias_fetch(ni > 1 ? 0 : 1, ni > 1 ? i0 + 1 : i0, far_next)) bias_publish(1);
+      }
+    }
     if (qt == 0) {
       if (!kDense && p.behind == kBehindPre) wait_for_primary();
       const size_t x = vec_index(kList ? h_nx : head(0), kList ? i_nx : i0);
       float b0 = 0.f;
-      if constexpr (kBias) b0 = bias_of_tile(head(0), i0);
+      if constexpr (kBias) b0 = bias_fold(far_, btop, i0);
       vec[0][0][rl] = kBias ? p.lse2[x] - b0 : p.lse2[x];
       vec[0][1][rl] = kBias ? p.bq[x] - b0 : p.bq[x];
       vec[0][2][rl] = p.Dq[x];
@@ -514,10 +558,10 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       if (qt == 0 && n + 1 < n_tot) {
         const size_t x = kList ? vec_index(h_nx, i_nx) : (last_of_head ? vec_index(head(hq_n + 1), i0) : vec_index(head(hq_n), i + 1));
         nx0 = p.lse2[x]; nx1 = p.bq[x]; nx2 = p.Dq[x];
-        if constexpr (kBias) {
-          const float b1 = bias_of_tile(head(last_of_head ? hq_n + 1 : hq_n), last_of_head ? i0 : i + 1);
-          nx0 -= b1; nx1 -= b1;
-        }
+      }
+      if constexpr (kBias) {
+        if (first_of_head && n > 0) { far_ = far_next; btop = btop_next; }
+        if (last_of_head && n + 1 < n_tot) bias_of_head(hq_n + 1, far_next, btop_next);
       }
       ok = mbar_wait_warp(&s_full, n & 1, status);
       if (!ok) break;
@@ -526,17 +570,18 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       tmem_ld_x32(tmem_addr(tb, lane_base, Cfg::kColS + qt * 32), sc);
       tmem_wait_ld();
       float cs = c2;                  // the tile's scores in the log2 domain are sc * cs (+ the flat tile's bias, see above)
-      bool flat = true;
+      [[maybe_unused]] bool near = false, by_factors = false;
+      [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
-        float b_;
-        const float* brow = bias_row(head(hq_n));
-        const int d0 = bias_d0(i);
-        flat = bias_flat(p.rb, brow, d0, b_);
-        if (!flat) {
-          const float* bp = brow + d0 + rl - qt * 32;
-#pragma unroll
-          for (int e = 0; e < 32; ++e) sc[e] = __float_as_uint(fmaf(__uint_as_float(sc[e]), c2, __ldg(bp - e)));
-          cs = 1.f;
+        near = !far_.is(p.rb, bias_d0(i));
+        if (near) {
+          bp = bias_from(bias_s[n & 3], 127 - rl + qt * 32);
+          if (kDense && btop == btop) {
+            by_factors = true;
+          } else {
+            bias_add(sc, c2, bp);
+            cs = 1.f;
+          }
         }
       }
       // packed sequences: a row past this sequence's end holds the next one's key (and with a bias a row past the last key must
@@ -569,6 +614,10 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       // The readers in tile n+1 see the values through the chain arrive (P^T / vote) -> UMMA warp -> scores.
       if (qt == 0) {
         const int ns = (slot == 2 ? 0 : slot + 1);
+        if constexpr (kBias) {
+          const float b1 = last_of_head ? (n + 1 < n_tot ? bias_fold(far_next, btop_next, i0) : 0.f) : bias_fold(far_, btop, i + 1);
+          nx0 -= b1; nx1 -= b1;
+        }
         vec[ns][0][rl] = nx0; vec[ns][1][rl] = nx1; vec[ns][2][rl] = nx2;
       }
       bool retain = true;
@@ -591,6 +640,16 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
       }
       if (!kDense) retain = __all_sync(0xffffffffu, retain);   // same value in every lane: the branch below is uniform
+      [[maybe_unused]] bool publish = false;
+      if constexpr (kBias) {           // the values of tile n + 2
+        if (n + 2 < n_tot) {
+          int x = hq_n, i2 = i + 2;
+          while (i2 >= T) { i2 -= ni; ++x; }
+          BiasFar f = far_;
+          if (x != hq_n) f.fetch(p.rb, p.rb.b2 + bias_head(x));
+          publish = bias_fetch(x, i2, f);
+        }
+      }
       if (stat_thread && first_of_head) { r_head = 0; bm_bits = 0; bm_word = -1; }
       if (retain) {
         if (stat_thread) {
@@ -609,15 +668,31 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         uint32_t pk[16];
         {
           const float4* ll = reinterpret_cast<const float4*>(vec[slot][0]) + qt * 8;
+          auto exponentials = [&](auto with_factors) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float4 x = ll[e];
-            const float p0 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 0]), cs, -x.x));
-            const float p1 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 1]), cs, -x.y));
-            const float p2 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 2]), cs, -x.z));
-            const float p3 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 3]), cs, -x.w));
-            pk[2 * e] = pack_bf16x2(p0, p1);
-            pk[2 * e + 1] = pack_bf16x2(p2, p3);
+            for (int e = 0; e < 8; ++e) {
+              const float4 x = ll[e];
+              float p0 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 0]), cs, -x.x));
+              float p1 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 1]), cs, -x.y));
+              float p2 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 2]), cs, -x.z));
+              float p3 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 3]), cs, -x.w));
+              if (kBias && decltype(with_factors)::value) {
+                const float4 f = bp[e];
+                p0 *= f.x; p1 *= f.y; p2 *= f.z; p3 *= f.w;
+              }
+              pk[2 * e] = pack_bf16x2(p0, p1);
+              pk[2 * e + 1] = pack_bf16x2(p2, p3);
+              if constexpr (kBias) {   // (the sums along the diagonals cancel: dS from P before its rounding)
+                sc[4 * e] = __float_as_uint(p0); sc[4 * e + 1] = __float_as_uint(p1);
+                sc[4 * e + 2] = __float_as_uint(p2); sc[4 * e + 3] = __float_as_uint(p3);
+              }
+            }
+          };
+          if constexpr (kBias && kDense) {   // (warp-uniform)
+            if (by_factors) exponentials(BiasBool<true>{});
+            else exponentials(BiasBool<false>{});
+          } else {
+            exponentials(BiasBool<false>{});
           }
         }
         tmem_st_x16(tmem_addr(tb, lane_base, Cfg::kColS + qt * 32), pk);
@@ -631,8 +706,27 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         if (!ok) break;
         tc_fence_after();
         uint32_t w[16];
-        [[maybe_unused]] float ds[kBias ? 32 : 1];   // dS^T before its rounding
-        {
+        [[maybe_unused]] float t0 = 0.f, t1 = 0.f;    // sum of the tile's dS (far tiles)
+        if constexpr (kBias) {
+          // (from P before its rounding, since the sums of dS cancel; in halves, which need no more registers than packed P does)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t dp[16];
+            tmem_ld_x16(tmem_addr(tb, lane_base, Cfg::kColDP + qt * 32 + c * 16), dp);
+            tmem_wait_ld();
+            const float4* dd = reinterpret_cast<const float4*>(vec[slot][2]) + qt * 8 + c * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float4 x = dd[e];
+              const uint32_t* ps = sc + c * 16 + 4 * e;
+              const float d0 = __uint_as_float(ps[0]) * (__uint_as_float(dp[4 * e + 0]) - x.x), d1 = __uint_as_float(ps[1]) * (__uint_as_float(dp[4 * e + 1]) - x.y);
+              const float d2 = __uint_as_float(ps[2]) * (__uint_as_float(dp[4 * e + 2]) - x.z), d3 = __uint_as_float(ps[3]) * (__uint_as_float(dp[4 * e + 3]) - x.w);
+              w[c * 8 + 2 * e] = pack_bf16x2(d0, d1);
+              w[c * 8 + 2 * e + 1] = pack_bf16x2(d2, d3);
+              t0 += d0 + d2; t1 += d1 + d3;
+            }
+          }
+        } else {
           uint32_t dp[32];
           tmem_ld_x32(tmem_addr(tb, lane_base, Cfg::kColDP + qt * 32), dp);
           tmem_wait_ld();
@@ -643,11 +737,8 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             const uint32_t pa = pk[2 * e], pb = pk[2 * e + 1];
             const float p0 = __uint_as_float(pa << 16), p1 = __uint_as_float(pa & 0xffff0000u);
             const float p2 = __uint_as_float(pb << 16), p3 = __uint_as_float(pb & 0xffff0000u);
-            const float d0 = p0 * (__uint_as_float(dp[4 * e + 0]) - x.x), d1 = p1 * (__uint_as_float(dp[4 * e + 1]) - x.y);
-            const float d2 = p2 * (__uint_as_float(dp[4 * e + 2]) - x.z), d3 = p3 * (__uint_as_float(dp[4 * e + 3]) - x.w);
-            w[2 * e] = pack_bf16x2(d0, d1);
-            w[2 * e + 1] = pack_bf16x2(d2, d3);
-            if constexpr (kBias) { ds[4 * e] = d0; ds[4 * e + 1] = d1; ds[4 * e + 2] = d2; ds[4 * e + 3] = d3; }
+            w[2 * e] = pack_bf16x2(p0 * (__uint_as_float(dp[4 * e + 0]) - x.x), p1 * (__uint_as_float(dp[4 * e + 1]) - x.y));
+            w[2 * e + 1] = pack_bf16x2(p2 * (__uint_as_float(dp[4 * e + 2]) - x.z), p3 * (__uint_as_float(dp[4 * e + 3]) - x.w));
           }
         }
         // dS^T also goes to TMEM, over this thread's own (already consumed) dP^T columns: A operand of dK
@@ -669,29 +760,33 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         __syncwarp();
         if (lane == 0) mbar_arrive(&ds_full);
         if constexpr (kBias) {   // (behind everything that others wait for)
-          const int d0 = bias_d0(i) + (int)lane_base - qt * 32;   // delta of this warp's 32 x 32 piece: d0 + lane - e
-          if (flat) {
-            const int bk = __ldg(p.rb.bucket + p.rb.half + d0);
-            if (bk != fbucket) { flush_flat(); fbucket = bk; }
-            float t0 = 0.f, t1 = 0.f;
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) { t0 += ds[e]; t1 += ds[e + 1]; }
+          if (!near) {
+            const int bk = __ldg(p.rb.bucket + p.rb.half + (bias_d0(i) < 0 ? -p.rb.reach : p.rb.reach));
+            if (bk != fbucket) { flush_far(); fbucket = bk; }
             fsum += t0 + t1;
           } else {
-            // Sums of the piece's 63 diagonals: in step e lane l takes the value of lane (l + e) % 32, which lies on
-            // diagonal l, or, past the last lane, on diagonal l - 32.
-            float on = 0.f, below = 0.f;
+            // Sums of the 63 diagonals of this warp's 32 x 32 piece, from the rounded dS: for columns c and c + 1 lane l takes the pair
+            // of lane (l + c) % 32, whose first value lies on diagonal l, or, past the last lane, on diagonal l - 32, and
+            // whose second one on the diagonal before that.
+            float on0 = 0.f, on1 = 0.f, all0 = 0.f, all1 = 0.f;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float t = __shfl_sync(0xffffffffu, ds[e], (lane + e) & 31);
-              if (lane + e < 32) on += t;
-              else below += t;
+            for (int e = 0; e < 16; ++e) {
+              const uint32_t t = __shfl_sync(0xffffffffu, w[e], (lane + 2 * e) & 31);
+              const float a = __uint_as_float(t << 16), b_ = __uint_as_float(t & 0xffff0000u);
+              all0 += a; all1 += b_;
+              if (lane + 2 * e < 32) { on0 += a; on1 += b_; }
             }
+            float below0 = all0 - on0, below1 = all1 - on1;
+            const float first1 = __shfl_sync(0xffffffffu, on1, 0);
+            on1 = __shfl_down_sync(0xffffffffu, on1, 1);
+            below1 = __shfl_down_sync(0xffffffffu, below1, 1);
+            const float on = lane < 31 ? on0 + on1 : on0, below = below0 + (lane < 31 ? below1 : first1);
             // ... and of the runs of diagonals that share a bucket (neighbours, since buckets are monotone along delta)
+            const uint8_t* bk_at = bias_k[n & 3] + 127 - (int)lane_base + qt * 32 - lane;
 #pragma unroll
             for (int half_ = 0; half_ < 2; ++half_) {
               float t = half_ ? below : on;
-              const int bk = __ldg(p.rb.bucket + p.rb.half + d0 + lane - (half_ ? 32 : 0));
+              const int bk = bk_at[half_ * 32];
 #pragma unroll
               for (int m = 1; m < 32; m <<= 1) {
                 const float t2 = __shfl_down_sync(0xffffffffu, t, m);
@@ -707,8 +802,9 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         ++r;
       }
       if constexpr (kBias) {
+        if (publish) bias_publish(n + 2);
         if (last_of_head) {   // the head's sums of the table's gradient, from every warp (and zeros for the next head)
-          flush_flat();
+          flush_far();
           fbucket = -1;
           float* out = p.rb.part + ((((size_t)b * p.Hq + hkv * G + head(hq_n)) * p.Tk + j) * kBiasWarps + (warp - 4)) * p.rb.buckets;
           for (int x = lane; x < p.rb.buckets; x += 32) { out[x] = wsum[x]; wsum[x] = 0.f; }
@@ -782,7 +878,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     // registers; the others are staged as 32-column swizzled panels in the tile's dS^T stage -- free once
     // dQ has retired -- and added by TMA reduce-add; the stage goes back to the dO ring when the TMA has
     // read it.
-    reg_alloc<152>();
+    reg_alloc<Cfg::kRegsDq>();
     const uint32_t lane_base = (uint32_t)(warp & 3) * 32u;
     const int rl = (int)lane_base + lane;
     const bool elected = (warp == 20 && lane == 0);

@@ -79,15 +79,16 @@ __device__ __forceinline__ void empty_rows(const FwdParams& p, int b, int h, int
   }
 }
 
-template <int D, bool kDense>
+template <int D, bool kDense, bool kBias = false>
 struct FwdCfg {
   static constexpr int kPanels = D / 64;
   static constexpr int kTileBytes = 128 * D * 2;
   static_assert(D <= 128, "two blocks of up to 128 columns fill the tensor memory");
-  static constexpr int kKStages = 3;
+  static constexpr int kKStages = kBias && D == 128 ? 2 : 3;   // (a bias takes the third one's place)
   static constexpr int kBlocks = 2;                // Q tiles and V stages
+  static constexpr int kBiasAt = (kBlocks + kKStages + kBlocks) * kTileBytes;   // two slots of a tile's bias per block
   // Q_A, Q_B, K ring, V_A, V_B
-  static constexpr int kSmemBytes = (kBlocks + kKStages + kBlocks) * kTileBytes + 1024;
+  static constexpr int kSmemBytes = kBiasAt + (kBias ? 2 * kBlocks * kBiasSlotFloats * 4 : 0) + 1024;
   static constexpr int kThreads = 384;
   static constexpr uint32_t kTmemCols = 512;
 };
@@ -98,7 +99,7 @@ template <int D, bool kDense, bool kSmall = false, bool kBias = false>
 __global__ void __launch_bounds__(384, 1)
 mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const FwdParams p) {
-  using Cfg = FwdCfg<D, kDense>;
+  using Cfg = FwdCfg<D, kDense, kBias>;
   constexpr int KS = Cfg::kKStages, PAN = Cfg::kPanels, VS = Cfg::kBlocks;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -108,6 +109,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
 
   __shared__ uint64_t q_full, k_full[KS], k_empty[KS], v_full[2], v_empty[2], s_full[2], vote_bar[2], p_full[2][2],
       fin_bar, turn_bar[2];
+  __shared__ uint64_t bias_bar[kBias ? 2 : 1];
   __shared__ uint32_t tmem_base_s;
   __shared__ int flag[2][3];
   __shared__ int early_exit;
@@ -189,6 +191,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       mbar_init(&s_full[x], 1); mbar_init(&vote_bar[x], 4); mbar_init(&p_full[x][0], 4); mbar_init(&p_full[x][1], 4);
       flag[x][0] = flag[x][1] = flag[x][2] = 0;
     }
+    if constexpr (kBias) { mbar_init(&bias_bar[0], 4); mbar_init(&bias_bar[1], 4); }
     mbar_init(&fin_bar, 2);
     mbar_init(&turn_bar[0], 4); mbar_init(&turn_bar[1], 4);
     mbar_fence_init();
@@ -423,9 +426,33 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     const int first = (x == 0) ? firstA : 0;
     const int T = present_x ? (U - first) : 0;       // tiles of this block
     const bool mask_first = x ? (hB == dB) : (hA == dA);
-    // position of the block's first row among the keys, and the head's bias by distance
+    // The block's bias: the head's by distance, the position of its first row among the keys, and two slots for the values of
+    // tiles that are not far.  The group fetches those of the next tile as it begins a tile and stages them as it ends it.
+    // (Near tile m uses slot m & 1: a warp fills it behind its wait for the values of near tile m - 1, for which every warp
+    // arrived behind its use of near tile m - 2.)
     [[maybe_unused]] const int qpos0 = i * 128 + (p.causal ? koff * 128 : Nkeys - Nq);
-    [[maybe_unused]] const float* brow = kBias ? p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half : nullptr;
+    [[maybe_unused]] const float* brow = kBias ? (kDense ? p.rb.vals : p.rb.b2) + (size_t)h * (2 * p.rb.half + 1) + p.rb.half : nullptr;
+    [[maybe_unused]] const float btop = kBias && kDense ? __ldg(p.rb.top + h) : NAN;
+    [[maybe_unused]] const bool factors = btop == btop;
+    [[maybe_unused]] float* bslot = reinterpret_cast<float*>(smem + Cfg::kBiasAt) + x * 2 * kBiasSlotFloats;
+    [[maybe_unused]] BiasFar far_;
+    [[maybe_unused]] float bv0 = 0.f, bv1 = 0.f;
+    [[maybe_unused]] int nears = 0;                    // near tiles so far
+    [[maybe_unused]] bool near = false, near_next = false;
+    auto bias_fetch = [&](int jt) -> bool {            // (whether the tile is near)
+      if (far_.is(p.rb, jt * 128 - qpos0)) return false;
+      const int d0 = bias_within(p.rb, jt * 128 - qpos0);
+      bv0 = __ldg(brow + d0 - 127 + rl);
+      bv1 = __ldg(brow + d0 + 1 + min(rl, 126));
+      return true;
+    };
+    auto bias_stage = [&](int m) {
+      float* slot = bslot + (m & 1) * kBiasSlotFloats;
+      bias_put(slot, rl, bv0);
+      if (rl < 127) bias_put(slot, rl + 128, bv1);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bias_bar[x]);
+    };
     // (l: sum of the keys 0-63 of the tiles, and of the keys 64-127 -- in this order, because mala_fwd_one_kernel has a thread for
     // either, and a row comes out the same bit for bit whichever kernel its call takes)
     float m_ref = -INFINITY, l0 = 0.f, l1 = 0.f, lg = -INFINITY;
@@ -437,8 +464,17 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     const size_t stat_row = (size_t)(b * p.Hq + h) * p.Tr + i;
     uint32_t* bm_row = (p.bitmask && present_x) ? p.bitmask + stat_row * p.words : nullptr;
 
+    if constexpr (kBias) {
+      far_.fetch(p.rb, p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half);
+      if (T > 0) near_next = bias_fetch(j0 - first);
+      if (near_next) bias_stage(0);
+    }
     for (int t = 0; t < T; ++t) {
       const int j = j0 - first - t;
+      if constexpr (kBias) {
+        near = near_next;
+        near_next = t + 1 < T && bias_fetch(j - 1);
+      }
       // The row's normalizer so far, as the test needs it: here, beside the wait for the scores, with 64 columns, and behind the
       // sums below with 128 (1300 tokens, 32 heads of 64: 27.6 us, there 28.2; 2360 tokens, 16 heads of 128, every tile retained:
       // 49.2 us, here 50.6 -- but with nearly every tile skipped 34.1, here 32.5).
@@ -456,18 +492,23 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       tmem_ld_x32(tmem_addr(tb, lane_base, colS + 96), s3);
       tmem_wait_ld();
       float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
+      [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
-        const int d0 = bias_within(p.rb, j * 128 - qpos0);
-        if (!bias_flat(p.rb, brow, d0, bs)) {
-          const float* bp = brow + d0 - rl;
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            s0[e] = __float_as_uint(fmaf(__uint_as_float(s0[e]), c2, __ldg(bp + e)));
-            s1[e] = __float_as_uint(fmaf(__uint_as_float(s1[e]), c2, __ldg(bp + e + 32)));
-            s2[e] = __float_as_uint(fmaf(__uint_as_float(s2[e]), c2, __ldg(bp + e + 64)));
-            s3[e] = __float_as_uint(fmaf(__uint_as_float(s3[e]), c2, __ldg(bp + e + 96)));
+        if (!near) {
+          bs = far_.value(j * 128 - qpos0);
+        } else {
+          bp = bias_from(bslot + (nears & 1) * kBiasSlotFloats, 127 - rl);
+          if (kDense && factors) {       // (the factors are waited for where they are used)
+            bs = btop;
+          } else {
+            ok = mbar_wait_warp(&bias_bar[x], nears & 1, status);
+            if (!ok) break;
+            bias_add(s0, c2, bp);
+            bias_add(s1, c2, bp + 8);
+            bias_add(s2, c2, bp + 16);
+            bias_add(s3, c2, bp + 24);
+            cs = 1.f;
           }
-          cs = 1.f; bs = 0.f;
         }
       }
       if (t == 0 && mask_first) {
@@ -527,6 +568,10 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           __syncwarp();
           if (lane == 0 && (x == 0 || t >= firstA)) mbar_arrive(&turn_bar[1 - x]);
         }
+        if constexpr (kBias) {
+          if (near) ++nears;
+          if (near_next) bias_stage(nears);
+        }
         continue;
       }
       if (stat_thread && bm_row) {
@@ -584,30 +629,49 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
 #define MALA_P_CHUNK(SRC, COL)                                                         \
       {                                                                                \
         _Pragma("unroll") for (int e = 0; e < 8; ++e) {                                \
-          const float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), cs, nm));        \
-          const float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), cs, nm));    \
-          const float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), cs, nm));    \
-          const float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), cs, nm));    \
+          float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), cs, nm));              \
+          float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), cs, nm));          \
+          float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), cs, nm));          \
+          float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), cs, nm));          \
+          if (kBias && kDense && kFactors) {                                           \
+            const float4 f = bp[(COL) / 2 + e];                                        \
+            p0 *= f.x; p1 *= f.y; p2 *= f.z; p3 *= f.w;                                \
+          }                                                                            \
           sum0 += p0; sum1 += p1; sum2 += p2; sum3 += p3;                              \
           pk[2 * e] = pack_bf16x2(p0, p1);                                             \
           pk[2 * e + 1] = pack_bf16x2(p2, p3);                                         \
         }                                                                              \
         tmem_st_x16(tmem_addr(tb, lane_base, colS + (COL)), pk);                       \
       }
-      MALA_P_CHUNK(s0, 0)
-      MALA_P_CHUNK(s1, 16)
-      l0 += (sum0 + sum1) + (sum2 + sum3);
-      sum0 = sum1 = sum2 = sum3 = 0.f;
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&p_full[x][0]);   // keys 0..63 of P are in place
-      MALA_P_CHUNK(s2, 32)
-      // hand the exponential phase over a little before it ends: the other group needs a few hundred cycles
-      // to notice, and the MUFU would idle meanwhile
-      __syncwarp();
-      if (lane == 0 && hasB && (x == 0 || t >= firstA)) mbar_arrive(&turn_bar[1 - x]);
-      MALA_P_CHUNK(s3, 48)
+      // (the same phase with factors and without: warp-uniform)
+      auto exponentials = [&](auto with_factors) {
+        constexpr bool kFactors = decltype(with_factors)::value;
+        MALA_P_CHUNK(s0, 0)
+        MALA_P_CHUNK(s1, 16)
+        l0 += (sum0 + sum1) + (sum2 + sum3);
+        sum0 = sum1 = sum2 = sum3 = 0.f;
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[x][0]);   // keys 0..63 of P are in place
+        MALA_P_CHUNK(s2, 32)
+        // hand the exponential phase over a little before it ends: the other group needs a few hundred cycles
+        // to notice, and the MUFU would idle meanwhile
+        __syncwarp();
+        if (lane == 0 && hasB && (x == 0 || t >= firstA)) mbar_arrive(&turn_bar[1 - x]);
+        MALA_P_CHUNK(s3, 48)
+      };
+      if constexpr (kBias && kDense) {
+        if (near && factors) {
+          ok = mbar_wait_warp(&bias_bar[x], nears & 1, status);
+          if (!ok) break;
+          exponentials(BiasBool<true>{});
+        } else {
+          exponentials(BiasBool<false>{});
+        }
+      } else {
+        exponentials(BiasBool<false>{});
+      }
 #undef MALA_P_CHUNK
       l1 += (sum0 + sum1) + (sum2 + sum3);
       if constexpr (!kDense && D != 64) lg = m_ref + __log2f(l0 + l1);
@@ -615,6 +679,10 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&p_full[x][1]);
+      if constexpr (kBias) {
+        if (near) ++nears;
+        if (near_next) bias_stage(nears);
+      }
       ++r;
     }
 

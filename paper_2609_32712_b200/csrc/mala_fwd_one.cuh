@@ -23,15 +23,16 @@
 
 namespace mala {
 
-template <int D>
+template <int D, bool kBias = false>
 struct FwdOneCfg {
   static constexpr int kCols = D < 128 ? D : 128;         // columns of a slot
   static constexpr int kSub = D / kCols;                  // slots of a tile
   static constexpr int kPan = kCols / 64;                 // 64-column panels of a slot
   static constexpr int kSlotBytes = 128 * kCols * 2;
-  static constexpr int kKSlots = D > 128 ? 2 : 3, kVSlots = 3;
+  static constexpr int kKSlots = D > 128 || (kBias && D == 128) ? 2 : 3, kVSlots = 3;   // (a bias takes a slot's place)
   static constexpr int kTiles = (kSub + kKSlots + kVSlots) * kSlotBytes;
-  static constexpr int kSmemBytes = kTiles + 2560;        // + FwdOneCtl
+  static constexpr int kBiasAt = kTiles + 2560;           // two slots of a tile's bias, behind FwdOneCtl
+  static constexpr int kSmemBytes = kTiles + 2560 + (kBias ? 2 * kBiasSlotFloats * 4 : 0);
   static constexpr int kThreads = 384;
 };
 
@@ -72,7 +73,7 @@ __device__ __forceinline__ bool letter_get(volatile uint64_t* at, float& mx, flo
 
 // Barriers and letters, behind the tiles in the dynamic shared memory (with 256 columns the tiles leave 3 KB)
 struct FwdOneCtl {
-  uint64_t q_full, k_full[3], k_empty[3], v_full[3], v_empty[3], v_ask[2], s_full[2], vote_bar[2], p_full[2][2], pv_done, fin_bar;
+  uint64_t q_full, k_full[3], k_empty[3], v_full[3], v_empty[3], v_ask[2], s_full[2], vote_bar[2], p_full[2][2], pv_done, fin_bar, bias_bar;
   uint64_t letter[2][128];                       // [half that writes][row]: row maxima of a tile, sums of the retained tiles before it
   uint32_t tmem_base;
   int flag[4], v_tile[2], early_exit;
@@ -82,7 +83,7 @@ template <int D, bool kDense, bool kSmall = false, bool kBias = false>
 __global__ void __launch_bounds__(384, 1)
 mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const FwdParams p) {
-  using Cfg = FwdOneCfg<D>;
+  using Cfg = FwdOneCfg<D, kBias>;
   constexpr int KS = Cfg::kKSlots, VS = Cfg::kVSlots, SUB = Cfg::kSub, PAN = Cfg::kPan, SLOT = Cfg::kSlotBytes;
   constexpr uint32_t kColO = 256;
   static_assert(sizeof(FwdOneCtl) <= 2560 && KS <= 3 && VS <= 3, "");
@@ -167,6 +168,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       mbar_init(&v_ask[x], 1); mbar_init(&s_full[x], 1); mbar_init(&vote_bar[x], 8); mbar_init(&p_full[x][0], 8); mbar_init(&p_full[x][1], 8);
     }
     mbar_init(&pv_done, 1); mbar_init(&fin_bar, 1);
+    if constexpr (kBias) mbar_init(&ctl.bias_bar, 8);
     flag[0] = flag[1] = flag[2] = flag[3] = 0;
     mbar_fence_init();
   }
@@ -338,9 +340,26 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const float Lq = p.causal ? (float)(prow_ + 1 + koff * 128) : (float)Nkeys;   // visible keys
     const float theta = kDense ? -INFINITY : (p.log2_tau - log2f(Lq));
     const bool mask_first = j0 == dI;
-    // position of the block's first row among the keys, and the head's bias by distance
+    // the block's bias, as in mala_fwd_kernel (here by the threads of both halves, a value each)
     [[maybe_unused]] const int qpos0 = i * 128 + (p.causal ? koff * 128 : Nkeys - Nq);
-    [[maybe_unused]] const float* brow = kBias ? p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half : nullptr;
+    [[maybe_unused]] const float* brow = kBias ? (kDense ? p.rb.vals : p.rb.b2) + (size_t)h * (2 * p.rb.half + 1) + p.rb.half : nullptr;
+    [[maybe_unused]] const float btop = kBias && kDense ? __ldg(p.rb.top + h) : NAN;
+    [[maybe_unused]] const bool factors = btop == btop;
+    [[maybe_unused]] float* bslot = reinterpret_cast<float*>(smem + Cfg::kBiasAt);
+    [[maybe_unused]] BiasFar far_;
+    [[maybe_unused]] float bv = 0.f;
+    [[maybe_unused]] int nears = 0;                    // near tiles so far
+    [[maybe_unused]] bool near = false, near_next = false;
+    auto bias_fetch = [&](int jt) -> bool {            // (whether the tile is near)
+      if (far_.is(p.rb, jt * 128 - qpos0)) return false;
+      bv = __ldg(brow + bias_within(p.rb, jt * 128 - qpos0) - 127 + min(half * 128 + rl, 254));
+      return true;
+    };
+    auto bias_stage = [&](int m) {
+      if (half * 128 + rl < 255) bias_put(bslot + (m & 1) * kBiasSlotFloats, half * 128 + rl, bv);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.bias_bar);
+    };
     float m_ref = -INFINITY, l = 0.f;                 // l: this thread's keys only
     float lg = -INFINITY;                             // m_ref + log2(l of the row)
     int r = 0;
@@ -353,8 +372,17 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const size_t stat_row = (size_t)(b * p.Hq + h) * p.Tr + i;
     uint32_t* bm_row = p.bitmask ? p.bitmask + stat_row * p.words : nullptr;
 
+    if constexpr (kBias) {
+      far_.fetch(p.rb, p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half);
+      near_next = bias_fetch(j0);
+      if (near_next) bias_stage(0);
+    }
     for (int t = 0; t < U; ++t) {
       const int x = t & 1, j = j0 - t;
+      if constexpr (kBias) {
+        near = near_next;
+        near_next = t + 1 < U && bias_fetch(j - 1);
+      }
       ok = mbar_wait_warp(&s_full[x], (t >> 1) & 1, status);
       if (!ok) break;
       tc_fence_after();
@@ -365,16 +393,21 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       const uint64_t before = *out_box;
       tmem_wait_ld();
       float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
+      [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
-        const int d0 = bias_within(p.rb, j * 128 - qpos0);
-        if (!bias_flat(p.rb, brow, d0, bs)) {
-          const float* bp = brow + d0 - rl + half * 64;
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            s0[e] = __float_as_uint(fmaf(__uint_as_float(s0[e]), c2, __ldg(bp + e)));
-            s1[e] = __float_as_uint(fmaf(__uint_as_float(s1[e]), c2, __ldg(bp + e + 32)));
+        if (!near) {
+          bs = far_.value(j * 128 - qpos0);
+        } else {
+          bp = bias_from(bslot + (nears & 1) * kBiasSlotFloats, 127 - rl + half * 64);
+          if (kDense && factors) {       // (the factors are waited for where they are used)
+            bs = btop;
+          } else {
+            ok = mbar_wait_warp(&ctl.bias_bar, nears & 1, status);
+            if (!ok) break;
+            bias_add(s0, c2, bp);
+            bias_add(s1, c2, bp + 8);
+            cs = 1.f;
           }
-          cs = 1.f; bs = 0.f;
         }
       }
       if (t == 0 && mask_first) {   // the newest legal tile: causal diagonal and / or the ragged end of the keys
@@ -433,6 +466,10 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         if (!retain) {
           if (!fresh) *in_box = ~0ull;        // (both halves have voted behind their letters, so it is there)
           fresh = false;
+          if constexpr (kBias) {
+            if (near) ++nears;
+            if (near_next) bias_stage(nears);
+          }
           continue;
         }
         if (!fresh) {
@@ -483,10 +520,14 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       {                                                                                \
         uint32_t pk[16];                                                               \
         _Pragma("unroll") for (int e = 0; e < 8; ++e) {                                \
-          const float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), cs, nm));        \
-          const float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), cs, nm));    \
-          const float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), cs, nm));    \
-          const float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), cs, nm));    \
+          float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), cs, nm));              \
+          float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), cs, nm));    \
+          float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), cs, nm));    \
+          float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), cs, nm));    \
+          if (kBias && kDense && kFactors) {                                           \
+            const float4 f = bp[(PIECE) * 8 + e];                                      \
+            p0 *= f.x; p1 *= f.y; p2 *= f.z; p3 *= f.w;                                \
+          }                                                                            \
           sum0 += p0; sum1 += p1; sum2 += p2; sum3 += p3;                              \
           pk[2 * e] = pack_bf16x2(p0, p1);                                             \
           pk[2 * e + 1] = pack_bf16x2(p2, p3);                                         \
@@ -497,11 +538,29 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         __syncwarp();                                                                  \
         if (lane == 0) mbar_arrive(&p_full[x][PIECE]);                                 \
       }
-      MALA_P_PIECE(s0, 0)
-      MALA_P_PIECE(s1, 1)
+      auto exponentials = [&](auto with_factors) {   // (warp-uniform)
+        constexpr bool kFactors = decltype(with_factors)::value;
+        MALA_P_PIECE(s0, 0)
+        MALA_P_PIECE(s1, 1)
+      };
 #undef MALA_P_PIECE
+      if constexpr (kBias && kDense) {
+        if (near && factors) {
+          ok = mbar_wait_warp(&ctl.bias_bar, nears & 1, status);
+          if (!ok) break;
+          exponentials(BiasBool<true>{});
+        } else {
+          exponentials(BiasBool<false>{});
+        }
+      } else {
+        exponentials(BiasBool<false>{});
+      }
       l += (sum0 + sum1) + (sum2 + sum3);
       fresh = true;
+      if constexpr (kBias) {
+        if (near) ++nears;
+        if (near_next) bias_stage(nears);
+      }
       ++r;
     }
 
