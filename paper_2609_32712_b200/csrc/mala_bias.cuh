@@ -56,20 +56,21 @@ template <bool V> struct BiasBool { static constexpr bool value = V; };
 // laid out part, with the same buckets
 __device__ __forceinline__ int bias_within(const RelBiasView& v, int d0) { return max(-v.reach - 128, min(v.reach + 128, d0)); }
 
-// A head's bias beyond the reach on either side.  A tile that lies there is far: its bias is that number -- unless it would
-// swallow the scores it is added to (a row of lowest values then weighs its keys alike, in this tile as in the nearer ones).
-struct BiasFar {
-  float before, after;
-  __device__ __forceinline__ void fetch(const RelBiasView& v, const float* row) {
-    before = __ldg(row - v.reach);
-    after = __ldg(row + v.reach);
-  }
-  static __device__ __forceinline__ bool small(float x) { return fabsf(x) < 1e9f || x == -INFINITY; }
-  __device__ __forceinline__ bool is(const RelBiasView& v, int d0) const {
-    return (d0 + 127 <= -v.reach && small(before)) || (d0 - 127 >= v.reach && small(after));
-  }
-  __device__ __forceinline__ float value(int d0) const { return d0 < 0 ? before : after; }
-};
+// Tiles that are not far, in a row of tiles whose first key and first query move apart by 128 from one to the next: those
+// with |d0| < reach + 127, where d0 = at - 128 * x for tile x.  [lo, hi)
+__device__ __forceinline__ void bias_near_range(int reach, int at, int& lo, int& hi) {
+  hi = (at + reach + 126 + (1 << 30)) / 128 - (1 << 23) + 1;       // (sums that may be negative, rounded down)
+  lo = (at - reach - 127 + (1 << 30)) / 128 - (1 << 23) + 1;
+}
+// A far tile whose bias would swallow the scores it is added to: they count for nothing (a row of lowest values weighs its keys
+// alike, in this tile as in the nearer ones, where the sums round to the bias).
+__device__ __forceinline__ bool bias_swallows(float x) { return fabsf(x) >= 1e9f && x != -INFINITY; }
+template <int N>
+__device__ __forceinline__ void bias_flatten(uint32_t (&s)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (__uint_as_float(s[e]) != -INFINITY) s[e] = 0u;
+}
 
 // The 255 values of a tile that is not far, in shared memory.  Value number y belongs to one diagonal, and a thread of row r needs
 // those from 127 - r on, one per column.  So that it can take them four at a time whatever r is, they lie there four times, copy c
@@ -85,19 +86,46 @@ __device__ __forceinline__ void bias_put(float* slot, int y, float v) {
 __device__ __forceinline__ const float4* bias_from(const float* slot, int y) {
   return reinterpret_cast<const float4*>(slot + (y & 3) * kBiasPitch + (y & ~3));
 }
+// Two fp32 values side by side: one instruction for both (sm_100)
+__device__ __forceinline__ uint64_t f2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void f2_get(uint64_t x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// bf16 pair of two fp32 values
+__device__ __forceinline__ uint32_t f2_bf16(uint64_t x) {
+  float a, b;
+  f2_get(x, a, b);
+  return pack_bf16x2(a, b);
+}
 // s = s * c + b for N scores
 template <int N>
 __device__ __forceinline__ void bias_add(uint32_t (&s)[N], float c, const float4* b) {
-  uint64_t cc;
-  asm("mov.b64 %0, {%1, %1};" : "=l"(cc) : "f"(c));
+  const uint64_t cc = f2(c, c);
 #pragma unroll
   for (int e = 0; e < N / 4; ++e) {
-    const float4 v = b[e];
-    asm("{\n\t.reg .b64 x, y;\n\t"
-        "mov.b64 x, {%0, %1};\n\tmov.b64 y, {%5, %6};\n\tfma.rn.f32x2 x, x, %4, y;\n\tmov.b64 {%0, %1}, x;\n\t"
-        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%7, %8};\n\tfma.rn.f32x2 x, x, %4, y;\n\tmov.b64 {%2, %3}, x;\n\t}"
-        : "+r"(s[4 * e]), "+r"(s[4 * e + 1]), "+r"(s[4 * e + 2]), "+r"(s[4 * e + 3])
-        : "l"(cc), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w));
+    const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(b + e);
+    float x0, x1, x2, x3;
+    f2_get(f2_fma(f2(__uint_as_float(s[4 * e]), __uint_as_float(s[4 * e + 1])), cc, v.x), x0, x1);
+    f2_get(f2_fma(f2(__uint_as_float(s[4 * e + 2]), __uint_as_float(s[4 * e + 3])), cc, v.y), x2, x3);
+    s[4 * e] = __float_as_uint(x0); s[4 * e + 1] = __float_as_uint(x1);
+    s[4 * e + 2] = __float_as_uint(x2); s[4 * e + 3] = __float_as_uint(x3);
   }
 }
 

@@ -484,26 +484,31 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     [[maybe_unused]] const int qoff = p.causal ? koff * 128 : Nkeys - Nq;
     auto bias_d0 = [&](int i_) -> int { return j * 128 - i_ * 128 - qoff; };
     auto bias_head = [&](int x) -> size_t { return (size_t)(hkv * G + head(x)) * (2 * p.rb.half + 1) + p.rb.half; };
-    [[maybe_unused]] BiasFar far_, far_next;
-    [[maybe_unused]] float btop = NAN, btop_next = NAN;
+    [[maybe_unused]] int near_lo = 0, near_hi = 0;              // near query blocks
+    if constexpr (kBias) bias_near_range(p.rb.reach, j * 128 - qoff, near_lo, near_hi);
+    auto bias_near = [&](int i_) -> bool { return i_ >= near_lo && i_ < near_hi; };
+    [[maybe_unused]] float bbefore = 0.f, bafter = 0.f, btop = NAN;   // of this head, and of the next one
+    [[maybe_unused]] float bbefore_next = 0.f, bafter_next = 0.f, btop_next = NAN;
+    auto bias_of_head = [&](int x, float& before, float& after, float& top) {
+      const float* row = p.rb.b2 + bias_head(x);
+      before = __ldg(row - p.rb.reach);
+      after = __ldg(row + p.rb.reach);
+      if (kDense) top = __ldg(p.rb.top + hkv * G + head(x));
+    };
+    auto bias_far = [&](float before, float after, int i_) -> float { return i_ >= near_hi ? before : after; };
+    auto bias_fold = [&](float before, float after, float top, int i_) -> float {
+      return !bias_near(i_) ? bias_far(before, after, i_) : (top == top ? top : 0.f);
+    };
+    [[maybe_unused]] const int kbefore = kBias ? __ldg(p.rb.bucket + p.rb.half - p.rb.reach) : 0;
+    [[maybe_unused]] const int kafter = kBias ? __ldg(p.rb.bucket + p.rb.half + p.rb.reach) : 0;
     [[maybe_unused]] float bv0 = 0.f, bv1 = 0.f;
     [[maybe_unused]] int bkt = 0;
-    auto bias_of_head = [&](int x, BiasFar& f, float& top_) {
-      f.fetch(p.rb, p.rb.b2 + bias_head(x));
-      if (kDense) top_ = __ldg(p.rb.top + hkv * G + head(x));
-    };
-    auto bias_fold = [&](const BiasFar& f, float top_, int i_) -> float {
-      const int d0 = bias_d0(i_);
-      return f.is(p.rb, d0) ? f.value(d0) : (top_ == top_ ? top_ : 0.f);
-    };
-    auto bias_fetch = [&](int x, int i_, const BiasFar& f) -> bool {   // (whether there is something to publish)
-      if (f.is(p.rb, bias_d0(i_))) return false;
+    auto bias_fetch = [&](int x, int i_) {
       const float* at = (kDense ? p.rb.vals : p.rb.b2) + bias_head(x);
       const int d0 = bias_within(p.rb, bias_d0(i_));
       bv0 = __ldg(at + d0 + 127 - (rl + qt));                // copy qt, places rl and rl + 128
       bv1 = __ldg(at + d0 + 127 - min(rl + 128 + qt, 254));
       if (qt < 2) bkt = __ldg(p.rb.bucket + p.rb.half + d0 + 127 - min(rl + qt * 128, 254));
-      return true;
     };
     auto bias_publish = [&](int n_) {
       float* dst = bias_s[n_ & 3] + qt * kBiasPitch + rl;
@@ -526,22 +531,25 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     };
     // per-query vectors of tile 0 into slot 0 (published by the first column quarter), then a group sync
     if constexpr (kBias) {
-      bias_of_head(0, far_, btop);
-      if (bias_fetch(0, i0, far_)) bias_publish(0);
-      if (n_tot > 1) {                 // tile 1: of this head, or the next one's first
-        if (ni > 1) far_next = far_;
-        else bias_of_head(1, far_next, btop_next);
-        if (bias_fetch(ni > 1 ? 0 : 1, ni > 1 ? i0 + 1 : i0, far_next)) bias_publish(1);
+      bias_of_head(0, bbefore, bafter, btop);
+      if (__any_sync(0xffffffffu, bias_near(i0))) {
+        bias_fetch(0, i0);
+        bias_publish(0);
+      }
+      const int i1 = ni > 1 ? i0 + 1 : i0;         // tile 1: of this head, or the next one's first
+      if (__any_sync(0xffffffffu, n_tot > 1 && bias_near(i1))) {
+        bias_fetch(ni > 1 ? 0 : 1, i1);
+        bias_publish(1);
       }
     }
     if (qt == 0) {
       if (!kDense && p.behind == kBehindPre) wait_for_primary();
       const size_t x = vec_index(kList ? h_nx : head(0), kList ? i_nx : i0);
       float b0 = 0.f;
-      if constexpr (kBias) b0 = bias_fold(far_, btop, i0);
-      vec[0][0][rl] = kBias ? p.lse2[x] - b0 : p.lse2[x];
+      if constexpr (kBias) b0 = bias_fold(bbefore, bafter, btop, i0);
+      vec[0][0][rl] = kBias ? b0 - p.lse2[x] : p.lse2[x];   // (with a bias the vectors' negatives, which are what is added)
       vec[0][1][rl] = kBias ? p.bq[x] - b0 : p.bq[x];
-      vec[0][2][rl] = p.Dq[x];
+      vec[0][2][rl] = kBias ? -p.Dq[x] : p.Dq[x];
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&grp_bar);
@@ -560,8 +568,8 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         nx0 = p.lse2[x]; nx1 = p.bq[x]; nx2 = p.Dq[x];
       }
       if constexpr (kBias) {
-        if (first_of_head && n > 0) { far_ = far_next; btop = btop_next; }
-        if (last_of_head && n + 1 < n_tot) bias_of_head(hq_n + 1, far_next, btop_next);
+        if (first_of_head && n > 0) { bbefore = bbefore_next; bafter = bafter_next; btop = btop_next; }
+        if (last_of_head && n + 1 < n_tot) bias_of_head(hq_n + 1, bbefore_next, bafter_next, btop_next);
       }
       ok = mbar_wait_warp(&s_full, n & 1, status);
       if (!ok) break;
@@ -573,10 +581,12 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       [[maybe_unused]] bool near = false, by_factors = false;
       [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
-        near = !far_.is(p.rb, bias_d0(i));
-        if (near) {
+        near = __any_sync(0xffffffffu, bias_near(i));   // (votes: to the compiler no other value is the same in all lanes)
+        if (!near) {
+          if (__any_sync(0xffffffffu, bias_swallows(bias_far(bbefore, bafter, i)))) bias_flatten(sc);
+        } else {
           bp = bias_from(bias_s[n & 3], 127 - rl + qt * 32);
-          if (kDense && btop == btop) {
+          if (kDense && __any_sync(0xffffffffu, btop == btop)) {
             by_factors = true;
           } else {
             bias_add(sc, c2, bp);
@@ -586,7 +596,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       }
       // packed sequences: a row past this sequence's end holds the next one's key (and with a bias a row past the last key must
       // not reach the sums along the diagonals)
-      if ((kBias || p.cu) && !valid_key) {
+      if ((p.cu || (kBias && (j + 1) * 128 > Nkeys)) && !valid_key) {
         const uint32_t ninf = 0xff800000u;
 #pragma unroll
         for (int e = 0; e < 32; ++e) sc[e] = ninf;
@@ -615,8 +625,8 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       if (qt == 0) {
         const int ns = (slot == 2 ? 0 : slot + 1);
         if constexpr (kBias) {
-          const float b1 = last_of_head ? (n + 1 < n_tot ? bias_fold(far_next, btop_next, i0) : 0.f) : bias_fold(far_, btop, i + 1);
-          nx0 -= b1; nx1 -= b1;
+          const float b1 = last_of_head ? bias_fold(bbefore_next, bafter_next, btop_next, i0) : bias_fold(bbefore, bafter, btop, i + 1);
+          nx0 = b1 - nx0; nx1 -= b1; nx2 = -nx2;
         }
         vec[ns][0][rl] = nx0; vec[ns][1][rl] = nx1; vec[ns][2][rl] = nx2;
       }
@@ -640,15 +650,13 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
       }
       if (!kDense) retain = __all_sync(0xffffffffu, retain);   // same value in every lane: the branch below is uniform
+      // the values of tile n + 2: whether there are any, and whose they are
       [[maybe_unused]] bool publish = false;
-      if constexpr (kBias) {           // the values of tile n + 2
-        if (n + 2 < n_tot) {
-          int x = hq_n, i2 = i + 2;
-          while (i2 >= T) { i2 -= ni; ++x; }
-          BiasFar f = far_;
-          if (x != hq_n) f.fetch(p.rb, p.rb.b2 + bias_head(x));
-          publish = bias_fetch(x, i2, f);
-        }
+      [[maybe_unused]] int x2 = hq_n, i2 = i + 2;
+      if constexpr (kBias) {
+        while (i2 >= T) { i2 -= ni; ++x2; }
+        publish = __any_sync(0xffffffffu, n + 2 < n_tot && bias_near(i2));
+        if (!kDense && publish) bias_fetch(x2, i2);
       }
       if (stat_thread && first_of_head) { r_head = 0; bm_bits = 0; bm_word = -1; }
       if (retain) {
@@ -666,33 +674,41 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
         // P^T = exp2(s * c2 - lse2_q) (bf16), written over S^T in TMEM as the A operand of dV
         uint32_t pk[16];
-        {
-          const float4* ll = reinterpret_cast<const float4*>(vec[slot][0]) + qt * 8;
+        [[maybe_unused]] uint64_t p2[kBias ? 16 : 1];   // P^T before its rounding (with a bias: the sums of dS cancel)
+        if constexpr (kBias) {
+          const ulonglong2* ll = reinterpret_cast<const ulonglong2*>(vec[slot][0]) + qt * 8;
+          const uint64_t cc = f2(cs, cs);
           auto exponentials = [&](auto with_factors) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float4 x = ll[e];
-              float p0 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 0]), cs, -x.x));
-              float p1 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 1]), cs, -x.y));
-              float p2 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 2]), cs, -x.z));
-              float p3 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 3]), cs, -x.w));
-              if (kBias && decltype(with_factors)::value) {
-                const float4 f = bp[e];
-                p0 *= f.x; p1 *= f.y; p2 *= f.z; p3 *= f.w;
+              const ulonglong2 x = ll[e];
+              float a0, a1, a2, a3;
+              f2_get(f2_fma(f2(__uint_as_float(sc[4 * e]), __uint_as_float(sc[4 * e + 1])), cc, x.x), a0, a1);
+              f2_get(f2_fma(f2(__uint_as_float(sc[4 * e + 2]), __uint_as_float(sc[4 * e + 3])), cc, x.y), a2, a3);
+              p2[2 * e] = f2(fast_exp2(a0), fast_exp2(a1));
+              p2[2 * e + 1] = f2(fast_exp2(a2), fast_exp2(a3));
+              if (decltype(with_factors)::value) {
+                const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(bp + e);
+                p2[2 * e] = f2_mul(p2[2 * e], f.x);
+                p2[2 * e + 1] = f2_mul(p2[2 * e + 1], f.y);
               }
-              pk[2 * e] = pack_bf16x2(p0, p1);
-              pk[2 * e + 1] = pack_bf16x2(p2, p3);
-              if constexpr (kBias) {   // (the sums along the diagonals cancel: dS from P before its rounding)
-                sc[4 * e] = __float_as_uint(p0); sc[4 * e + 1] = __float_as_uint(p1);
-                sc[4 * e + 2] = __float_as_uint(p2); sc[4 * e + 3] = __float_as_uint(p3);
-              }
+              pk[2 * e] = f2_bf16(p2[2 * e]);
+              pk[2 * e + 1] = f2_bf16(p2[2 * e + 1]);
             }
           };
-          if constexpr (kBias && kDense) {   // (warp-uniform)
-            if (by_factors) exponentials(BiasBool<true>{});
-            else exponentials(BiasBool<false>{});
-          } else {
-            exponentials(BiasBool<false>{});
+          if (kDense && __any_sync(0xffffffffu, by_factors)) exponentials(BiasBool<true>{});
+          else exponentials(BiasBool<false>{});
+        } else {
+          const float4* ll = reinterpret_cast<const float4*>(vec[slot][0]) + qt * 8;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float4 x = ll[e];
+            const float p0 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 0]), c2, -x.x));
+            const float p1 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 1]), c2, -x.y));
+            const float p2_ = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 2]), c2, -x.z));
+            const float p3 = fast_exp2(fmaf(__uint_as_float(sc[4 * e + 3]), c2, -x.w));
+            pk[2 * e] = pack_bf16x2(p0, p1);
+            pk[2 * e + 1] = pack_bf16x2(p2_, p3);
           }
         }
         tmem_st_x16(tmem_addr(tb, lane_base, Cfg::kColS + qt * 32), pk);
@@ -700,30 +716,32 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_full);
+        if constexpr (kBias && kDense) {
+          if (publish) bias_fetch(x2, i2);
+        }
         // dS^T = P^T o (dP^T - D_q): values first, then, once dV has also finished reading the dO stage that
         // dS^T overwrites (D = 128), into shared memory for the dQ and dK MMAs
         ok = mbar_wait_warp(&dp_full, r & 1, status);
         if (!ok) break;
         tc_fence_after();
         uint32_t w[16];
-        [[maybe_unused]] float t0 = 0.f, t1 = 0.f;    // sum of the tile's dS (far tiles)
+        [[maybe_unused]] uint64_t tsum = 0;           // sum of the tile's dS (far tiles), in two halves
         if constexpr (kBias) {
-          // (from P before its rounding, since the sums of dS cancel; in halves, which need no more registers than packed P does)
+          // (in halves, which need no more registers than packed P does)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             uint32_t dp[16];
             tmem_ld_x16(tmem_addr(tb, lane_base, Cfg::kColDP + qt * 32 + c * 16), dp);
             tmem_wait_ld();
-            const float4* dd = reinterpret_cast<const float4*>(vec[slot][2]) + qt * 8 + c * 4;
+            const ulonglong2* dd = reinterpret_cast<const ulonglong2*>(vec[slot][2]) + qt * 8 + c * 4;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float4 x = dd[e];
-              const uint32_t* ps = sc + c * 16 + 4 * e;
-              const float d0 = __uint_as_float(ps[0]) * (__uint_as_float(dp[4 * e + 0]) - x.x), d1 = __uint_as_float(ps[1]) * (__uint_as_float(dp[4 * e + 1]) - x.y);
-              const float d2 = __uint_as_float(ps[2]) * (__uint_as_float(dp[4 * e + 2]) - x.z), d3 = __uint_as_float(ps[3]) * (__uint_as_float(dp[4 * e + 3]) - x.w);
-              w[c * 8 + 2 * e] = pack_bf16x2(d0, d1);
-              w[c * 8 + 2 * e + 1] = pack_bf16x2(d2, d3);
-              t0 += d0 + d2; t1 += d1 + d3;
+              const ulonglong2 x = dd[e];
+              const uint64_t d0 = f2_mul(p2[c * 8 + 2 * e], f2_add(f2(__uint_as_float(dp[4 * e]), __uint_as_float(dp[4 * e + 1])), x.x));
+              const uint64_t d1 = f2_mul(p2[c * 8 + 2 * e + 1], f2_add(f2(__uint_as_float(dp[4 * e + 2]), __uint_as_float(dp[4 * e + 3])), x.y));
+              w[c * 8 + 2 * e] = f2_bf16(d0);
+              w[c * 8 + 2 * e + 1] = f2_bf16(d1);
+              tsum = f2_add(tsum, f2_add(d0, d1));
             }
           }
         } else {
@@ -760,9 +778,11 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         __syncwarp();
         if (lane == 0) mbar_arrive(&ds_full);
         if constexpr (kBias) {   // (behind everything that others wait for)
-          if (!near) {
-            const int bk = __ldg(p.rb.bucket + p.rb.half + (bias_d0(i) < 0 ? -p.rb.reach : p.rb.reach));
+          if (!__any_sync(0xffffffffu, near)) {
+            const int bk = i >= near_hi ? kbefore : kafter;
             if (bk != fbucket) { flush_far(); fbucket = bk; }
+            float t0, t1;
+            f2_get(tsum, t0, t1);
             fsum += t0 + t1;
           } else {
             // Sums of the 63 diagonals of this warp's 32 x 32 piece, from the rounded dS: for columns c and c + 1 lane l takes the pair
@@ -802,7 +822,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         ++r;
       }
       if constexpr (kBias) {
-        if (publish) bias_publish(n + 2);
+        if (__any_sync(0xffffffffu, publish)) bias_publish(n + 2);
         if (last_of_head) {   // the head's sums of the table's gradient, from every warp (and zeros for the next head)
           flush_far();
           fbucket = -1;

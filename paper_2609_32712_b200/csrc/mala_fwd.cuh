@@ -435,16 +435,23 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     [[maybe_unused]] const float btop = kBias && kDense ? __ldg(p.rb.top + h) : NAN;
     [[maybe_unused]] const bool factors = btop == btop;
     [[maybe_unused]] float* bslot = reinterpret_cast<float*>(smem + Cfg::kBiasAt) + x * 2 * kBiasSlotFloats;
-    [[maybe_unused]] BiasFar far_;
+    [[maybe_unused]] const float bbefore = kBias ? __ldg(p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half - p.rb.reach) : 0.f;
+    [[maybe_unused]] const float bafter = kBias ? __ldg(p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half + p.rb.reach) : 0.f;
+    [[maybe_unused]] int near_lo = 0, near_hi = 0;     // near key blocks
+    if constexpr (kBias) {                             // (d0 = 128 * block - qpos0: the range of -block)
+      int lo, hi;
+      bias_near_range(p.rb.reach, -qpos0, lo, hi);
+      near_lo = 1 - hi;
+      near_hi = 1 - lo;
+    }
     [[maybe_unused]] float bv0 = 0.f, bv1 = 0.f;
     [[maybe_unused]] int nears = 0;                    // near tiles so far
     [[maybe_unused]] bool near = false, near_next = false;
-    auto bias_fetch = [&](int jt) -> bool {            // (whether the tile is near)
-      if (far_.is(p.rb, jt * 128 - qpos0)) return false;
+    auto bias_near = [&](int jt) -> bool { return jt >= near_lo && jt < near_hi; };
+    auto bias_fetch = [&](int jt) {
       const int d0 = bias_within(p.rb, jt * 128 - qpos0);
       bv0 = __ldg(brow + d0 - 127 + rl);
       bv1 = __ldg(brow + d0 + 1 + min(rl, 126));
-      return true;
     };
     auto bias_stage = [&](int m) {
       float* slot = bslot + (m & 1) * kBiasSlotFloats;
@@ -465,15 +472,18 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     uint32_t* bm_row = (p.bitmask && present_x) ? p.bitmask + stat_row * p.words : nullptr;
 
     if constexpr (kBias) {
-      far_.fetch(p.rb, p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half);
-      if (T > 0) near_next = bias_fetch(j0 - first);
-      if (near_next) bias_stage(0);
+      near_next = __any_sync(0xffffffffu, T > 0 && bias_near(j0 - first));
+      if (near_next) {
+        bias_fetch(j0 - first);
+        bias_stage(0);
+      }
     }
     for (int t = 0; t < T; ++t) {
       const int j = j0 - first - t;
       if constexpr (kBias) {
         near = near_next;
-        near_next = t + 1 < T && bias_fetch(j - 1);
+        near_next = __any_sync(0xffffffffu, t + 1 < T && bias_near(j - 1));
+        if (near_next) bias_fetch(j - 1);
       }
       // The row's normalizer so far, as the test needs it: here, beside the wait for the scores, with 64 columns, and behind the
       // sums below with 128 (1300 tokens, 32 heads of 64: 27.6 us, there 28.2; 2360 tokens, 16 heads of 128, every tile retained:
@@ -494,11 +504,14 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
       [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
-        if (!near) {
-          bs = far_.value(j * 128 - qpos0);
+        if (!__any_sync(0xffffffffu, near)) {
+          bs = j * 128 < qpos0 ? bbefore : bafter;
+          if (__any_sync(0xffffffffu, bias_swallows(bs))) {
+            bias_flatten(s0); bias_flatten(s1); bias_flatten(s2); bias_flatten(s3);
+          }
         } else {
           bp = bias_from(bslot + (nears & 1) * kBiasSlotFloats, 127 - rl);
-          if (kDense && factors) {       // (the factors are waited for where they are used)
+          if (kDense && __any_sync(0xffffffffu, factors)) {   // (the factors are waited for where they are used)
             bs = btop;
           } else {
             ok = mbar_wait_warp(&bias_bar[x], nears & 1, status);
@@ -570,7 +583,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
         if constexpr (kBias) {
           if (near) ++nears;
-          if (near_next) bias_stage(nears);
+          if (__any_sync(0xffffffffu, near_next)) bias_stage(nears);
         }
         continue;
       }
@@ -624,19 +637,36 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       }
       // P = exp2(s * c2 - m_ref), row sum in fp32 before the bf16 cast, P written over S
       const float nm = kBias ? bs - m_ref : -m_ref;
+      [[maybe_unused]] const uint64_t cs2 = f2(cs, cs), nm2 = f2(nm, nm);   // (two scores at a time with a bias)
+      [[maybe_unused]] uint64_t sums0 = 0, sums1 = 0;
+      [[maybe_unused]] auto take_sums = [&](float& a, float& b, float& c, float& d) {
+        f2_get(sums0, a, b);
+        f2_get(sums1, c, d);
+        sums0 = sums1 = 0;
+      };
       float sum0 = 0.f, sum1 = 0.f, sum2 = 0.f, sum3 = 0.f;
       uint32_t pk[16];
 #define MALA_P_CHUNK(SRC, COL)                                                         \
       {                                                                                \
         _Pragma("unroll") for (int e = 0; e < 8; ++e) {                                \
-          float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), cs, nm));              \
-          float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), cs, nm));          \
-          float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), cs, nm));          \
-          float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), cs, nm));          \
-          if (kBias && kDense && kFactors) {                                           \
-            const float4 f = bp[(COL) / 2 + e];                                        \
-            p0 *= f.x; p1 *= f.y; p2 *= f.z; p3 *= f.w;                                \
+          if constexpr (kBias) {                                                       \
+            float a0, a1, a2, a3;                                                      \
+            f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e]), __uint_as_float(SRC[4 * e + 1])), cs2, nm2), a0, a1);     \
+            f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e + 2]), __uint_as_float(SRC[4 * e + 3])), cs2, nm2), a2, a3); \
+            uint64_t x0 = f2(fast_exp2(a0), fast_exp2(a1)), x1 = f2(fast_exp2(a2), fast_exp2(a3));                  \
+            if (kFactors) {                                                            \
+              const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(bp + (COL) / 2 + e); \
+              x0 = f2_mul(x0, f.x); x1 = f2_mul(x1, f.y);                              \
+            }                                                                          \
+            sums0 = f2_add(sums0, x0); sums1 = f2_add(sums1, x1);                      \
+            pk[2 * e] = f2_bf16(x0);                                                   \
+            pk[2 * e + 1] = f2_bf16(x1);                                               \
+            continue;                                                                  \
           }                                                                            \
+          const float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), c2, nm));        \
+          const float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), c2, nm));    \
+          const float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), c2, nm));    \
+          const float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), c2, nm));    \
           sum0 += p0; sum1 += p1; sum2 += p2; sum3 += p3;                              \
           pk[2 * e] = pack_bf16x2(p0, p1);                                             \
           pk[2 * e + 1] = pack_bf16x2(p2, p3);                                         \
@@ -648,6 +678,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         constexpr bool kFactors = decltype(with_factors)::value;
         MALA_P_CHUNK(s0, 0)
         MALA_P_CHUNK(s1, 16)
+        if constexpr (kBias) take_sums(sum0, sum1, sum2, sum3);
         l0 += (sum0 + sum1) + (sum2 + sum3);
         sum0 = sum1 = sum2 = sum3 = 0.f;
         tmem_wait_st();
@@ -662,7 +693,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         MALA_P_CHUNK(s3, 48)
       };
       if constexpr (kBias && kDense) {
-        if (near && factors) {
+        if (__any_sync(0xffffffffu, near && factors)) {   // (a vote: to the compiler no other value is the same in all lanes)
           ok = mbar_wait_warp(&bias_bar[x], nears & 1, status);
           if (!ok) break;
           exponentials(BiasBool<true>{});
@@ -673,6 +704,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         exponentials(BiasBool<false>{});
       }
 #undef MALA_P_CHUNK
+      if constexpr (kBias) take_sums(sum0, sum1, sum2, sum3);
       l1 += (sum0 + sum1) + (sum2 + sum3);
       if constexpr (!kDense && D != 64) lg = m_ref + __log2f(l0 + l1);
       tmem_wait_st();
@@ -681,7 +713,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       if (lane == 0) mbar_arrive(&p_full[x][1]);
       if constexpr (kBias) {
         if (near) ++nears;
-        if (near_next) bias_stage(nears);
+        if (__any_sync(0xffffffffu, near_next)) bias_stage(nears);
       }
       ++r;
     }

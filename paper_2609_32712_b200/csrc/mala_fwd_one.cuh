@@ -346,14 +346,21 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     [[maybe_unused]] const float btop = kBias && kDense ? __ldg(p.rb.top + h) : NAN;
     [[maybe_unused]] const bool factors = btop == btop;
     [[maybe_unused]] float* bslot = reinterpret_cast<float*>(smem + Cfg::kBiasAt);
-    [[maybe_unused]] BiasFar far_;
+    [[maybe_unused]] const float bbefore = kBias ? __ldg(p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half - p.rb.reach) : 0.f;
+    [[maybe_unused]] const float bafter = kBias ? __ldg(p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half + p.rb.reach) : 0.f;
+    [[maybe_unused]] int near_lo = 0, near_hi = 0;     // near key blocks
+    if constexpr (kBias) {                             // (d0 = 128 * block - qpos0: the range of -block)
+      int lo, hi;
+      bias_near_range(p.rb.reach, -qpos0, lo, hi);
+      near_lo = 1 - hi;
+      near_hi = 1 - lo;
+    }
     [[maybe_unused]] float bv = 0.f;
     [[maybe_unused]] int nears = 0;                    // near tiles so far
     [[maybe_unused]] bool near = false, near_next = false;
-    auto bias_fetch = [&](int jt) -> bool {            // (whether the tile is near)
-      if (far_.is(p.rb, jt * 128 - qpos0)) return false;
+    auto bias_near = [&](int jt) -> bool { return jt >= near_lo && jt < near_hi; };
+    auto bias_fetch = [&](int jt) {
       bv = __ldg(brow + bias_within(p.rb, jt * 128 - qpos0) - 127 + min(half * 128 + rl, 254));
-      return true;
     };
     auto bias_stage = [&](int m) {
       if (half * 128 + rl < 255) bias_put(bslot + (m & 1) * kBiasSlotFloats, half * 128 + rl, bv);
@@ -373,15 +380,18 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     uint32_t* bm_row = p.bitmask ? p.bitmask + stat_row * p.words : nullptr;
 
     if constexpr (kBias) {
-      far_.fetch(p.rb, p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half);
-      near_next = bias_fetch(j0);
-      if (near_next) bias_stage(0);
+      near_next = __any_sync(0xffffffffu, bias_near(j0));
+      if (near_next) {
+        bias_fetch(j0);
+        bias_stage(0);
+      }
     }
     for (int t = 0; t < U; ++t) {
       const int x = t & 1, j = j0 - t;
       if constexpr (kBias) {
         near = near_next;
-        near_next = t + 1 < U && bias_fetch(j - 1);
+        near_next = __any_sync(0xffffffffu, t + 1 < U && bias_near(j - 1));
+        if (near_next) bias_fetch(j - 1);
       }
       ok = mbar_wait_warp(&s_full[x], (t >> 1) & 1, status);
       if (!ok) break;
@@ -395,11 +405,14 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
       [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
-        if (!near) {
-          bs = far_.value(j * 128 - qpos0);
+        if (!__any_sync(0xffffffffu, near)) {
+          bs = j * 128 < qpos0 ? bbefore : bafter;
+          if (__any_sync(0xffffffffu, bias_swallows(bs))) {
+            bias_flatten(s0); bias_flatten(s1);
+          }
         } else {
           bp = bias_from(bslot + (nears & 1) * kBiasSlotFloats, 127 - rl + half * 64);
-          if (kDense && factors) {       // (the factors are waited for where they are used)
+          if (kDense && __any_sync(0xffffffffu, factors)) {   // (the factors are waited for where they are used)
             bs = btop;
           } else {
             ok = mbar_wait_warp(&ctl.bias_bar, nears & 1, status);
@@ -468,7 +481,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           fresh = false;
           if constexpr (kBias) {
             if (near) ++nears;
-            if (near_next) bias_stage(nears);
+            if (__any_sync(0xffffffffu, near_next)) bias_stage(nears);
           }
           continue;
         }
@@ -515,19 +528,36 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       }
       // P = exp2(s * c2 - m_ref), row sum in fp32 before the bf16 cast, P over this thread's own scores
       const float nm = kBias ? bs - m_ref : -m_ref;
+      [[maybe_unused]] const uint64_t cs2 = f2(cs, cs), nm2 = f2(nm, nm);   // (two scores at a time with a bias)
+      [[maybe_unused]] uint64_t sums0 = 0, sums1 = 0;
+      [[maybe_unused]] auto take_sums = [&](float& a, float& b, float& c, float& d) {
+        f2_get(sums0, a, b);
+        f2_get(sums1, c, d);
+        sums0 = sums1 = 0;
+      };
       float sum0 = 0.f, sum1 = 0.f, sum2 = 0.f, sum3 = 0.f;
 #define MALA_P_PIECE(SRC, PIECE)                                                       \
       {                                                                                \
         uint32_t pk[16];                                                               \
         _Pragma("unroll") for (int e = 0; e < 8; ++e) {                                \
-          float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), cs, nm));              \
-          float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), cs, nm));    \
-          float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), cs, nm));    \
-          float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), cs, nm));    \
-          if (kBias && kDense && kFactors) {                                           \
-            const float4 f = bp[(PIECE) * 8 + e];                                      \
-            p0 *= f.x; p1 *= f.y; p2 *= f.z; p3 *= f.w;                                \
+          if constexpr (kBias) {                                                       \
+            float a0, a1, a2, a3;                                                      \
+            f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e]), __uint_as_float(SRC[4 * e + 1])), cs2, nm2), a0, a1);     \
+            f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e + 2]), __uint_as_float(SRC[4 * e + 3])), cs2, nm2), a2, a3); \
+            uint64_t x0 = f2(fast_exp2(a0), fast_exp2(a1)), x1 = f2(fast_exp2(a2), fast_exp2(a3));                  \
+            if (kFactors) {                                                            \
+              const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(bp + (PIECE) * 8 + e); \
+              x0 = f2_mul(x0, f.x); x1 = f2_mul(x1, f.y);                              \
+            }                                                                          \
+            sums0 = f2_add(sums0, x0); sums1 = f2_add(sums1, x1);                      \
+            pk[2 * e] = f2_bf16(x0);                                                   \
+            pk[2 * e + 1] = f2_bf16(x1);                                               \
+            continue;                                                                  \
           }                                                                            \
+          const float p0 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e]), c2, nm));        \
+          const float p1 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 1]), c2, nm));    \
+          const float p2 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 2]), c2, nm));    \
+          const float p3 = fast_exp2(fmaf(__uint_as_float(SRC[4 * e + 3]), c2, nm));    \
           sum0 += p0; sum1 += p1; sum2 += p2; sum3 += p3;                              \
           pk[2 * e] = pack_bf16x2(p0, p1);                                             \
           pk[2 * e + 1] = pack_bf16x2(p2, p3);                                         \
@@ -545,7 +575,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       };
 #undef MALA_P_PIECE
       if constexpr (kBias && kDense) {
-        if (near && factors) {
+        if (__any_sync(0xffffffffu, near && factors)) {   // (a vote: to the compiler no other value is the same in all lanes)
           ok = mbar_wait_warp(&ctl.bias_bar, nears & 1, status);
           if (!ok) break;
           exponentials(BiasBool<true>{});
@@ -555,11 +585,12 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       } else {
         exponentials(BiasBool<false>{});
       }
+      if constexpr (kBias) take_sums(sum0, sum1, sum2, sum3);
       l += (sum0 + sum1) + (sum2 + sum3);
       fresh = true;
       if constexpr (kBias) {
         if (near) ++nears;
-        if (near_next) bias_stage(nears);
+        if (__any_sync(0xffffffffu, near_next)) bias_stage(nears);
       }
       ++r;
     }
