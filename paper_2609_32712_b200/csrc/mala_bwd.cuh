@@ -567,9 +567,18 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         const size_t x = kList ? vec_index(h_nx, i_nx) : (last_of_head ? vec_index(head(hq_n + 1), i0) : vec_index(head(hq_n), i + 1));
         nx0 = p.lse2[x]; nx1 = p.bq[x]; nx2 = p.Dq[x];
       }
+      [[maybe_unused]] bool near = false, by_factors = false, swallows = false, publish = false;
+      [[maybe_unused]] int x2 = hq_n, i2 = i + 2;     // tile n + 2
       if constexpr (kBias) {
         if (first_of_head && n > 0) { bbefore = bbefore_next; bafter = bafter_next; btop = btop_next; }
         if (last_of_head && n + 1 < n_tot) bias_of_head(hq_n + 1, bbefore_next, bafter_next, btop_next);
+        // what kind of tile this one is and whether tile n + 2 has values: beside the wait for the scores, and by votes, because to
+        // the compiler no other value is the same in all lanes
+        near = __any_sync(0xffffffffu, bias_near(i));
+        by_factors = kDense && __any_sync(0xffffffffu, near && btop == btop);
+        swallows = __any_sync(0xffffffffu, !near && bias_swallows(bias_far(bbefore, bafter, i)));
+        while (i2 >= T) { i2 -= ni; ++x2; }
+        publish = __any_sync(0xffffffffu, n + 2 < n_tot && bias_near(i2));
       }
       ok = mbar_wait_warp(&s_full, n & 1, status);
       if (!ok) break;
@@ -578,20 +587,16 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       tmem_ld_x32(tmem_addr(tb, lane_base, Cfg::kColS + qt * 32), sc);
       tmem_wait_ld();
       float cs = c2;                  // the tile's scores in the log2 domain are sc * cs (+ the flat tile's bias, see above)
-      [[maybe_unused]] bool near = false, by_factors = false;
       [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
-        near = __any_sync(0xffffffffu, bias_near(i));   // (votes: to the compiler no other value is the same in all lanes)
-        if (!near) {
-          if (__any_sync(0xffffffffu, bias_swallows(bias_far(bbefore, bafter, i)))) bias_flatten(sc);
-        } else {
+        if (near) {
           bp = bias_from(bias_s[n & 3], 127 - rl + qt * 32);
-          if (kDense && __any_sync(0xffffffffu, btop == btop)) {
-            by_factors = true;
-          } else {
+          if (!by_factors) {
             bias_add(sc, c2, bp);
             cs = 1.f;
           }
+        } else if (swallows) {
+          bias_flatten(sc);
         }
       }
       // packed sequences: a row past this sequence's end holds the next one's key (and with a bias a row past the last key must
@@ -650,13 +655,8 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
       }
       if (!kDense) retain = __all_sync(0xffffffffu, retain);   // same value in every lane: the branch below is uniform
-      // the values of tile n + 2: whether there are any, and whose they are
-      [[maybe_unused]] bool publish = false;
-      [[maybe_unused]] int x2 = hq_n, i2 = i + 2;
-      if constexpr (kBias) {
-        while (i2 >= T) { i2 -= ni; ++x2; }
-        publish = __any_sync(0xffffffffu, n + 2 < n_tot && bias_near(i2));
-        if (!kDense && publish) bias_fetch(x2, i2);
+      if constexpr (kBias && !kDense) {
+        if (publish) bias_fetch(x2, i2);
       }
       if (stat_thread && first_of_head) { r_head = 0; bm_bits = 0; bm_word = -1; }
       if (retain) {
@@ -696,7 +696,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
               pk[2 * e + 1] = f2_bf16(p2[2 * e + 1]);
             }
           };
-          if (kDense && __any_sync(0xffffffffu, by_factors)) exponentials(BiasBool<true>{});
+          if (by_factors) exponentials(BiasBool<true>{});
           else exponentials(BiasBool<false>{});
         } else {
           const float4* ll = reinterpret_cast<const float4*>(vec[slot][0]) + qt * 8;
@@ -778,7 +778,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         __syncwarp();
         if (lane == 0) mbar_arrive(&ds_full);
         if constexpr (kBias) {   // (behind everything that others wait for)
-          if (!__any_sync(0xffffffffu, near)) {
+          if (!near) {
             const int bk = i >= near_hi ? kbefore : kafter;
             if (bk != fbucket) { flush_far(); fbucket = bk; }
             float t0, t1;
@@ -822,7 +822,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         ++r;
       }
       if constexpr (kBias) {
-        if (__any_sync(0xffffffffu, publish)) bias_publish(n + 2);
+        if (publish) bias_publish(n + 2);
         if (last_of_head) {   // the head's sums of the table's gradient, from every warp (and zeros for the next head)
           flush_far();
           fbucket = -1;

@@ -446,7 +446,6 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     }
     [[maybe_unused]] float bv0 = 0.f, bv1 = 0.f;
     [[maybe_unused]] int nears = 0;                    // near tiles so far
-    [[maybe_unused]] bool near = false, near_next = false;
     auto bias_near = [&](int jt) -> bool { return jt >= near_lo && jt < near_hi; };
     auto bias_fetch = [&](int jt) {
       const int d0 = bias_within(p.rb, jt * 128 - qpos0);
@@ -472,16 +471,22 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     uint32_t* bm_row = (p.bitmask && present_x) ? p.bitmask + stat_row * p.words : nullptr;
 
     if constexpr (kBias) {
-      near_next = __any_sync(0xffffffffu, T > 0 && bias_near(j0 - first));
-      if (near_next) {
+      if (__any_sync(0xffffffffu, T > 0 && bias_near(j0 - first))) {
         bias_fetch(j0 - first);
         bias_stage(0);
       }
     }
     for (int t = 0; t < T; ++t) {
       const int j = j0 - first - t;
+      float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
+      // what kind of tile this and the next one are: beside the wait for the scores, and by votes, because to the compiler no other
+      // value is the same in all lanes (a vote where the branch stands is on the chain of the tile)
+      [[maybe_unused]] bool near = false, by_factors = false, swallows = false, near_next = false;
       if constexpr (kBias) {
-        near = near_next;
+        near = __any_sync(0xffffffffu, bias_near(j));
+        by_factors = kDense && __any_sync(0xffffffffu, near && factors);
+        bs = j * 128 < qpos0 ? bbefore : bafter;
+        swallows = __any_sync(0xffffffffu, !near && bias_swallows(bs));
         near_next = __any_sync(0xffffffffu, t + 1 < T && bias_near(j - 1));
         if (near_next) bias_fetch(j - 1);
       }
@@ -501,17 +506,15 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       tmem_ld_x32(tmem_addr(tb, lane_base, colS + 64), s2);
       tmem_ld_x32(tmem_addr(tb, lane_base, colS + 96), s3);
       tmem_wait_ld();
-      float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
       [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
-        if (!__any_sync(0xffffffffu, near)) {
-          bs = j * 128 < qpos0 ? bbefore : bafter;
-          if (__any_sync(0xffffffffu, bias_swallows(bs))) {
+        if (!near) {
+          if (swallows) {
             bias_flatten(s0); bias_flatten(s1); bias_flatten(s2); bias_flatten(s3);
           }
         } else {
           bp = bias_from(bslot + (nears & 1) * kBiasSlotFloats, 127 - rl);
-          if (kDense && __any_sync(0xffffffffu, factors)) {   // (the factors are waited for where they are used)
+          if (by_factors) {              // (the factors are waited for where they are used)
             bs = btop;
           } else {
             ok = mbar_wait_warp(&bias_bar[x], nears & 1, status);
@@ -520,7 +523,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             bias_add(s1, c2, bp + 8);
             bias_add(s2, c2, bp + 16);
             bias_add(s3, c2, bp + 24);
-            cs = 1.f;
+            cs = 1.f; bs = 0.f;
           }
         }
       }
@@ -583,7 +586,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
         if constexpr (kBias) {
           if (near) ++nears;
-          if (__any_sync(0xffffffffu, near_next)) bias_stage(nears);
+          if (near_next) bias_stage(nears);
         }
         continue;
       }
@@ -693,7 +696,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         MALA_P_CHUNK(s3, 48)
       };
       if constexpr (kBias && kDense) {
-        if (__any_sync(0xffffffffu, near && factors)) {   // (a vote: to the compiler no other value is the same in all lanes)
+        if (by_factors) {
           ok = mbar_wait_warp(&bias_bar[x], nears & 1, status);
           if (!ok) break;
           exponentials(BiasBool<true>{});
@@ -713,7 +716,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       if (lane == 0) mbar_arrive(&p_full[x][1]);
       if constexpr (kBias) {
         if (near) ++nears;
-        if (__any_sync(0xffffffffu, near_next)) bias_stage(nears);
+        if (near_next) bias_stage(nears);
       }
       ++r;
     }

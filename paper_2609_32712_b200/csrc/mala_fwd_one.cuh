@@ -357,7 +357,6 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     }
     [[maybe_unused]] float bv = 0.f;
     [[maybe_unused]] int nears = 0;                    // near tiles so far
-    [[maybe_unused]] bool near = false, near_next = false;
     auto bias_near = [&](int jt) -> bool { return jt >= near_lo && jt < near_hi; };
     auto bias_fetch = [&](int jt) {
       bv = __ldg(brow + bias_within(p.rb, jt * 128 - qpos0) - 127 + min(half * 128 + rl, 254));
@@ -380,16 +379,22 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     uint32_t* bm_row = p.bitmask ? p.bitmask + stat_row * p.words : nullptr;
 
     if constexpr (kBias) {
-      near_next = __any_sync(0xffffffffu, bias_near(j0));
-      if (near_next) {
+      if (__any_sync(0xffffffffu, bias_near(j0))) {
         bias_fetch(j0);
         bias_stage(0);
       }
     }
     for (int t = 0; t < U; ++t) {
       const int x = t & 1, j = j0 - t;
+      float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
+      // what kind of tile this and the next one are: beside the wait for the scores, and by votes, because to the compiler no other
+      // value is the same in all lanes (a vote where the branch stands is on the chain of the tile)
+      [[maybe_unused]] bool near = false, by_factors = false, swallows = false, near_next = false;
       if constexpr (kBias) {
-        near = near_next;
+        near = __any_sync(0xffffffffu, bias_near(j));
+        by_factors = kDense && __any_sync(0xffffffffu, near && factors);
+        bs = j * 128 < qpos0 ? bbefore : bafter;
+        swallows = __any_sync(0xffffffffu, !near && bias_swallows(bs));
         near_next = __any_sync(0xffffffffu, t + 1 < U && bias_near(j - 1));
         if (near_next) bias_fetch(j - 1);
       }
@@ -402,24 +407,22 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       tmem_ld_x32(tmem_addr(tb, lane_base, colS + 32), s1);
       const uint64_t before = *out_box;
       tmem_wait_ld();
-      float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
       [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
-        if (!__any_sync(0xffffffffu, near)) {
-          bs = j * 128 < qpos0 ? bbefore : bafter;
-          if (__any_sync(0xffffffffu, bias_swallows(bs))) {
+        if (!near) {
+          if (swallows) {
             bias_flatten(s0); bias_flatten(s1);
           }
         } else {
           bp = bias_from(bslot + (nears & 1) * kBiasSlotFloats, 127 - rl + half * 64);
-          if (kDense && __any_sync(0xffffffffu, factors)) {   // (the factors are waited for where they are used)
+          if (by_factors) {              // (the factors are waited for where they are used)
             bs = btop;
           } else {
             ok = mbar_wait_warp(&ctl.bias_bar, nears & 1, status);
             if (!ok) break;
             bias_add(s0, c2, bp);
             bias_add(s1, c2, bp + 8);
-            cs = 1.f;
+            cs = 1.f; bs = 0.f;
           }
         }
       }
@@ -481,7 +484,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           fresh = false;
           if constexpr (kBias) {
             if (near) ++nears;
-            if (__any_sync(0xffffffffu, near_next)) bias_stage(nears);
+            if (near_next) bias_stage(nears);
           }
           continue;
         }
@@ -575,7 +578,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       };
 #undef MALA_P_PIECE
       if constexpr (kBias && kDense) {
-        if (__any_sync(0xffffffffu, near && factors)) {   // (a vote: to the compiler no other value is the same in all lanes)
+        if (by_factors) {
           ok = mbar_wait_warp(&ctl.bias_bar, nears & 1, status);
           if (!ok) break;
           exponentials(BiasBool<true>{});
@@ -590,7 +593,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       fresh = true;
       if constexpr (kBias) {
         if (near) ++nears;
-        if (__any_sync(0xffffffffu, near_next)) bias_stage(nears);
+        if (near_next) bias_stage(nears);
       }
       ++r;
     }
