@@ -486,6 +486,7 @@ static int bwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dou
     bb.v.part = (float*)((uint8_t*)ws + base + bias_expand_bytes(Hq, bias->max_distance));
     bb.dtable = dtable;
     bb.sb = dtable_sb;
+    bb.group = Hq / Hkv;
   }
   return bwd_launch(q, k, v, o, dout, lse, dq, dk, dv, st, B0, Hq, Hkv, N0, Nk0, d, causal ? 1 : 0, scale, tau, ws,
                     ws_bytes, status, sm_count(dev), (cudaStream_t)cuda_stream, cu, total, cu_k, total_k, bias ? &bb : nullptr);

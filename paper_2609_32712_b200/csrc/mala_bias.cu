@@ -1,5 +1,5 @@
-// The attention kernels' variants with a learned relative position bias, and the two kernels of their own that these calls
-// have: the layout of the bias by distance in front, and the sum of its gradient behind the backward.
+// The attention kernels' variants with a learned relative position bias, and the kernel of their own that these calls have,
+// the layout of the bias by distance in front.
 #include <cuda_runtime.h>
 
 #define MALA_KERNELS_ONLY
@@ -52,27 +52,6 @@ bias_expand_kernel(const __nv_bfloat16* __restrict__ table, int64_t sb, const __
   if (h == 0) bucket[x] = bk;
 }
 
-// dtable[bucket][head] = sum over batch entries, key blocks and warps of the partial sums, in a fixed order: one block per
-// (head, bucket).
-__global__ void __launch_bounds__(128)
-bias_reduce_kernel(const float* __restrict__ part, int B, int Hq, long long per_head, int buckets, __nv_bfloat16* __restrict__ out,
-                   int64_t sb) {
-  const int bk = blockIdx.x, h = blockIdx.y;
-  double t = 0.0;
-  for (int b = 0; b < B; ++b) {
-    const float* src = part + ((size_t)b * Hq + h) * per_head * buckets + bk;
-    for (long long x = threadIdx.x; x < per_head; x += 128) t += (double)src[x * buckets];
-  }
-  __shared__ double red[128];
-  red[threadIdx.x] = t;
-  __syncthreads();
-  for (int m = 64; m > 0; m >>= 1) {
-    if (threadIdx.x < m) red[threadIdx.x] += red[threadIdx.x + m];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) out[(int64_t)bk * sb + h] = __float2bfloat16((float)red[0]);
-}
-
 int bias_expand(const mala_rel_bias* bias, int Hq, void* ws, RelBiasView* view, cudaStream_t stream) {
   BiasStarts s;
   if (!bias_starts(bias->num_buckets, bias->max_distance, bias->bidirectional, &s)) return MALA_ERR_UNSUPPORTED;
@@ -114,6 +93,9 @@ int bias_launch_fwd(int D, bool dense, bool one, const CUtensorMap& tq, const CU
 template <int D, bool kDense>
 static int launch_bwd_bias_as(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tdo,
                               const CUtensorMap& tacc, const BwdParams& p, cudaStream_t stream) {
+  if (p.behind)
+    return launch_dependent_smem(mala_bwd_kernel<D, kDense, false, true>, dim3(p.Tk, p.Hkv, p.B), dim3(BwdCfg<D>::kThreads), BwdCfg<D>::kSmemBytes,
+                                 stream, tq, tk, tv, tdo, tacc, p) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
   mala_bwd_kernel<D, kDense, false, true><<<dim3(p.Tk, p.Hkv, p.B), BwdCfg<D>::kThreads, BwdCfg<D>::kSmemBytes, stream>>>(tq, tk, tv, tdo, tacc, p);
   return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
@@ -122,11 +104,6 @@ int bias_launch_bwd(int D, bool dense, const CUtensorMap& tq, const CUtensorMap&
                     const CUtensorMap& tacc, const BwdParams& p, cudaStream_t stream) {
   if (D == 128) return dense ? launch_bwd_bias_as<128, true>(tq, tk, tv, tdo, tacc, p, stream) : launch_bwd_bias_as<128, false>(tq, tk, tv, tdo, tacc, p, stream);
   return dense ? launch_bwd_bias_as<64, true>(tq, tk, tv, tdo, tacc, p, stream) : launch_bwd_bias_as<64, false>(tq, tk, tv, tdo, tacc, p, stream);
-}
-
-int bias_launch_reduce(const RelBiasView& v, int B, int Hq, int Tk, void* dtable, int64_t sb, cudaStream_t stream) {
-  bias_reduce_kernel<<<dim3(v.buckets, Hq), 128, 0, stream>>>(v.part, B, Hq, (long long)Tk * kBiasWarps, v.buckets, (__nv_bfloat16*)dtable, sb);
-  return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
 // The decode kernels with a bias handle one token as several (kMulti).

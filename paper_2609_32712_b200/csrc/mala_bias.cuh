@@ -45,10 +45,12 @@ struct RelBiasView {
   const float* top;       // [Hq] the head's largest b2; NaN where its values are too far apart for factors (see kBiasRange)
   const int* bucket;      // [2 half + 1]
   int reach, half;        // half = reach + kBiasPad
-  float* part;            // backward: [B][Hq][Tk][kBiasWarps][buckets] partial sums of the table's gradient
+  float* part;            // backward: [B][Hq][Tk][bias_parts][buckets] partial sums of the table's gradient
   int buckets;
 };
 constexpr int kBiasWarps = 16;   // warps of the backward's score group, each with sums of its own
+// partial sums of a key block and query head: every warp's where the block goes on with the group's next head, else their sum
+__host__ __device__ constexpr int bias_parts(int group) { return group > 1 ? kBiasWarps : 1; }
 
 template <bool V> struct BiasBool { static constexpr bool value = V; };
 
@@ -169,6 +171,7 @@ struct BwdBias {
   RelBiasView v;
   void* dtable;       // bf16 [buckets, Hq], rows sb apart
   int64_t sb;
+  int group;          // query heads per KV head
 };
 
 // Host side (mala_bias.cu)
@@ -181,7 +184,6 @@ int bias_launch_fwd(int D, bool dense, bool one, const CUtensorMap& tq, const CU
                     const FwdParams& p, cudaStream_t stream);
 int bias_launch_bwd(int D, bool dense, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tdo,
                     const CUtensorMap& tacc, const BwdParams& p, cudaStream_t stream);
-int bias_launch_reduce(const RelBiasView& v, int B, int Hq, int Tk, void* dtable, int64_t sb, cudaStream_t stream);
 int bias_launch_decode(int D, bool dense, bool sched, int rows, int grid, const CUtensorMap& tq, const CUtensorMap& tk,
                        const CUtensorMap& tv, const DecParams& p, cudaStream_t stream);
 

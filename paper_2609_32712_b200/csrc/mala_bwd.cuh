@@ -141,7 +141,7 @@ constexpr int kBwdListHeads = 16;     // query heads of a group in the two-pass 
 // the dense tile pipeline on a sparse tile sequence.
 // kBias: the scores carry a relative position bias (mala_bias.cuh), whose gradient, the sums of dS over the tiles' diagonals,
 // the score group takes beside dS^T: a flat tile's sum goes to one bucket, another tile's diagonals to theirs, and every warp
-// keeps its own sums, per query head, which bias_reduce_kernel adds up in a fixed order.
+// keeps its own sums, per query head, which bwd_convert_dq_kernel adds up in a fixed order.
 template <int D, bool kDense, bool kList = false, bool kBias = false>
 __global__ void __launch_bounds__(768, 1)
 mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -183,12 +183,19 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   // The kernel behind this one may start where blocks of this one no longer fill the SMs, and this one starts like that behind the
   // kernel before it (p.behind): it waits where it needs that one's results, and is never over before that one is.
   // (Not the dense kernel: 2 % slower with the checks, 24.3 against 23.8 ms at 32K and 32 / 8 heads.)
-  auto settle = [&]() { if (!kDense && p.behind) wait_for_primary(); };
+  auto settle = [&]() { if ((!kDense || kBias) && p.behind) wait_for_primary(); };
   if (kList || (!kDense && p.behind == kBehindPre)) release_dependents();
-  if (p.cu && j >= (Nkeys + 127) / 128) { settle(); return; }        // (a sequence shorter than the longest one)
+  // (a block without tiles has no part in the table's gradient)
+  auto no_sums = [&]() {
+    if constexpr (kBias)
+      for (int x = threadIdx.x, per = bias_parts(G) * p.rb.buckets; x < G * per; x += blockDim.x)
+        p.rb.part[(((size_t)b * p.Hq + hkv * G + x / per) * p.Tk + j) * per + x % per] = 0.f;
+  };
+  if (p.cu && j >= (Nkeys + 127) / 128) { settle(); no_sums(); return; }        // (a sequence shorter than the longest one)
   if (p.cu_k && (Nq <= 0 || (p.causal && Nkeys < Nq))) {
     // keys without queries (or lengths the call does not allow): their gradients are zero
     settle();
+    no_sums();
     for (int x = threadIdx.x; x < 128 * (p.d / 8); x += blockDim.x) {
       const int key = j * 128 + x / (p.d / 8), c = (x % (p.d / 8)) * 8;
       if (key < Nkeys) {
@@ -455,6 +462,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     // thread's own score columns, so no thread ever touches a column another thread still has to read.
     if constexpr (Cfg::kRegsScore > 80) reg_alloc<Cfg::kRegsScore>();
     else reg_dealloc<Cfg::kRegsScore>();
+    if constexpr (kBias) settle();
     const uint32_t lane_base = (uint32_t)(warp & 3) * 32u;
     const int rl = (int)lane_base + lane;
     const int qt = (warp - 4) >> 2;                 // column quarter
@@ -530,27 +538,28 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       fsum = 0.f;
     };
     // per-query vectors of tile 0 into slot 0 (published by the first column quarter), then a group sync
-    if constexpr (kBias) {
+    float v0 = 0.f, v1 = 0.f, v2 = 0.f;
+    if (qt == 0) {
+      if (!kDense && !kBias && p.behind == kBehindPre) wait_for_primary();
+      const size_t x = vec_index(kList ? h_nx : head(0), kList ? i_nx : i0);
+      v0 = p.lse2[x]; v1 = p.bq[x]; v2 = p.Dq[x];
+    }
+    if constexpr (kBias) {             // (all of a block's first loads together)
       bias_of_head(0, bbefore, bafter, btop);
+      bias_fetch(0, i0);
+      const float a0 = bv0, a1 = bv1;
+      const int k0 = bkt, i1 = ni > 1 ? i0 + 1 : i0;         // tile 1: of this head, or the next one's first
+      const bool two = __any_sync(0xffffffffu, n_tot > 1 && bias_near(i1));
+      if (two) bias_fetch(ni > 1 ? 0 : 1, i1);
+      if (two) bias_publish(1);
       if (__any_sync(0xffffffffu, bias_near(i0))) {
-        bias_fetch(0, i0);
+        bv0 = a0; bv1 = a1; bkt = k0;
         bias_publish(0);
       }
-      const int i1 = ni > 1 ? i0 + 1 : i0;         // tile 1: of this head, or the next one's first
-      if (__any_sync(0xffffffffu, n_tot > 1 && bias_near(i1))) {
-        bias_fetch(ni > 1 ? 0 : 1, i1);
-        bias_publish(1);
-      }
+      const float b0 = bias_fold(bbefore, bafter, btop, i0);   // (with a bias the vectors' negatives, which are what is added)
+      v0 = b0 - v0; v1 -= b0; v2 = -v2;
     }
-    if (qt == 0) {
-      if (!kDense && p.behind == kBehindPre) wait_for_primary();
-      const size_t x = vec_index(kList ? h_nx : head(0), kList ? i_nx : i0);
-      float b0 = 0.f;
-      if constexpr (kBias) b0 = bias_fold(bbefore, bafter, btop, i0);
-      vec[0][0][rl] = kBias ? b0 - p.lse2[x] : p.lse2[x];   // (with a bias the vectors' negatives, which are what is added)
-      vec[0][1][rl] = kBias ? p.bq[x] - b0 : p.bq[x];
-      vec[0][2][rl] = kBias ? -p.Dq[x] : p.Dq[x];
-    }
+    if (qt == 0) { vec[0][0][rl] = v0; vec[0][1][rl] = v1; vec[0][2][rl] = v2; }
     __syncwarp();
     if (lane == 0) mbar_arrive(&grp_bar);
     ok = mbar_wait_warp(&grp_bar, 0, status);
@@ -570,7 +579,9 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       [[maybe_unused]] bool near = false, by_factors = false, swallows = false, publish = false;
       [[maybe_unused]] int x2 = hq_n, i2 = i + 2;     // tile n + 2
       if constexpr (kBias) {
-        if (first_of_head && n > 0) { bbefore = bbefore_next; bafter = bafter_next; btop = btop_next; }
+        if (first_of_head && n > 0) {
+          bbefore = bbefore_next; bafter = bafter_next; btop = btop_next;
+        }
         if (last_of_head && n + 1 < n_tot) bias_of_head(hq_n + 1, bbefore_next, bafter_next, btop_next);
         // what kind of tile this one is and whether tile n + 2 has values: beside the wait for the scores, and by votes, because to
         // the compiler no other value is the same in all lanes
@@ -823,9 +834,10 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       }
       if constexpr (kBias) {
         if (publish) bias_publish(n + 2);
-        if (last_of_head) {   // the head's sums of the table's gradient, from every warp (and zeros for the next head)
+        if (last_of_head && G > 1) {   // the head's sums of the table's gradient, from every warp (and zeros for the next head)
           flush_far();
           fbucket = -1;
+          __syncwarp();
           float* out = p.rb.part + ((((size_t)b * p.Hq + hkv * G + head(hq_n)) * p.Tk + j) * kBiasWarps + (warp - 4)) * p.rb.buckets;
           for (int x = lane; x < p.rb.buckets; x += 32) { out[x] = wsum[x]; wsum[x] = 0.f; }
           __syncwarp();
@@ -842,6 +854,22 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       }
     }
 
+    if constexpr (kBias) {
+      if (ok && G == 1) {   // one query head: the sums of all warps, added up by the first four, a bucket per thread
+        flush_far();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&grp_bar);
+        if (qt == 0) {
+          ok = mbar_wait_warp(&grp_bar, 1, status);
+          if (ok && rl < p.rb.buckets) {
+            float t = 0.f;
+#pragma unroll
+            for (int x = 0; x < kBiasWarps; ++x) t += bsum[x][rl];
+            p.rb.part[(((size_t)b * p.Hq + hkv) * p.Tk + j) * p.rb.buckets + rl] = t;
+          }
+        }
+      }
+    }
     // epilogue: dK_j (x scale), dV_j -> global; the four threads of a row store a quarter of its columns each
     settle();
     if (ok) {
@@ -999,7 +1027,7 @@ bwd_preprocess_kernel(const __nv_bfloat16* __restrict__ o, int64_t o_sb, int64_t
     N = __ldg(cu + b + 1) - row0;
     Nk = cu_k ? __ldg(cu_k + b + 1) - __ldg(cu_k + b) : N;
     if (cu_k) qshift = (causal && Nk >= N) ? (Nk - N) % 128 : 0;   // (per sequence)
-    if (p0 / 128 * 128 >= N + qshift) return;                      // beyond this sequence's padded rows
+    if (p0 / 128 * 128 >= N + qshift) { wait_for_primary(); return; }   // beyond this sequence's padded rows
     prow0 = ((row0 + (cu_k ? 384 : 128) * b) / 128) * 128;
     b = 0;
   }
@@ -1046,6 +1074,46 @@ bwd_preprocess_kernel(const __nv_bfloat16* __restrict__ o, int64_t o_sb, int64_t
       Dq[w0 + r] = sum;
     }
   }
+  wait_for_primary();   // (launched behind the bias's layout: not over before that is)
+}
+
+// dtable[.][h] from the partial sums of all batch entries, key blocks and warps: 32 buckets at a time by a block of the first batch
+// entry, a lane per bucket, eight warps on every eighth sum, sixteen of them in flight each.  Hidden behind the conversion
+// (32 x 512 tokens, 16 heads: 2048 sums per bucket and head; with a warp per bucket, which reads a sector for every sum, the
+// kernel took 69 us instead of 15).
+__device__ __forceinline__ void bias_reduce(const BwdBias& bias, int h, int Hq, int B, int Tk, float* red) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, nb = bias.v.buckets, rows = Tk * bias_parts(bias.group);
+  for (int b0 = blockIdx.x * 32; b0 < nb; b0 += gridDim.x * 32) {
+    const int bk = b0 + lane;
+    float t = 0.f;
+    if (bk < nb) {
+      const float* src = bias.v.part + ((size_t)h * rows + w) * nb + bk;
+      const size_t next = (size_t)(Hq - 1) * rows * nb;   // from the end of a batch entry's sums to the next one's
+      int r = w;
+      while (r >= rows) { r -= rows; src += next; }       // (fewer than eight sums per batch entry)
+      float s4[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int left = (int)(((long long)rows * B - w + 7) / 8); left > 0; left -= 16) {
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          v[e] = e < left ? __ldcg(src) : 0.f;
+          src += (size_t)8 * nb;
+          r += 8;
+          while (r >= rows) { r -= rows; src += next; }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s4[e & 3] += v[e];
+      }
+      t = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+    }
+    red[w * 32 + lane] = t;
+    __syncthreads();
+    if (w == 0 && bk < nb) {
+      for (int x = 1; x < 8; ++x) t += red[x * 32 + lane];
+      reinterpret_cast<__nv_bfloat16*>(bias.dtable)[(int64_t)bk * bias.sb + h] = __float2bfloat16(t);
+    }
+    __syncthreads();
+  }
 }
 
 // dq = bf16(scale * acc), one block per 128 x D tile of the accumulator (blockIdx as above).  The accumulator is tiled
@@ -1056,12 +1124,13 @@ template <int D>
 __global__ void __launch_bounds__(256)
 bwd_convert_dq_kernel(const float* __restrict__ acc, __nv_bfloat16* __restrict__ dq, int64_t sb, int64_t sn, int64_t sh,
                       int N, int Np, float scale, const int* __restrict__ cu, int qshift, int d,
-                      const int* __restrict__ cu_k, int causal) {
+                      const int* __restrict__ cu_k, int causal, const __grid_constant__ BwdBias bias, int B, int Tk) {
   constexpr int kHalf = D / 2, kRow = D * 2 + 16;   // bytes of a staged row (padded: its 16-byte stores spread over the banks)
   __shared__ __align__(16) uint8_t stage[128 * kRow];
   wait_for_primary();
   const int i = blockIdx.x, h = blockIdx.y, Hq = gridDim.y;
   int b = blockIdx.z, row0 = 0, prow0 = 0;
+  if (bias.dtable && b == 0) bias_reduce(bias, h, Hq, B, Tk, reinterpret_cast<float*>(stage));
   if (cu) {
     row0 = __ldg(cu + b);
     N = __ldg(cu + b + 1) - row0;
@@ -1211,10 +1280,17 @@ inline int bwd_launch(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin d
 
   {
     auto pre = D == 128 ? bwd_preprocess_kernel<128> : bwd_preprocess_kernel<64>;
-    pre<<<dim3(4 * T, Hq, B), 256, 0, stream>>>((const __nv_bfloat16*)o.p, o.sb, o.sn, o.sh, (const __nv_bfloat16*)dout.p, dout.sb,
-                                    dout.sn, dout.sh, lse, lse2, bq, Dq, acc, N, Np, Nk, d, causal,
-                                    tau > 0.f ? log2f(tau) : -INFINITY, cu, total, qshift, cu_k);
-    if (cudaGetLastError() != cudaSuccess) return MALA_ERR_CUDA;
+    if (bias) {   // (behind the kernel that lays the bias out, of which it needs nothing: the two run side by side)
+      if (launch_dependent(pre, dim3(4 * T, Hq, B), dim3(256), stream, (const __nv_bfloat16*)o.p, o.sb, o.sn, o.sh,
+                           (const __nv_bfloat16*)dout.p, dout.sb, dout.sn, dout.sh, lse, lse2, bq, Dq, acc, N, Np, Nk, d, causal,
+                           tau > 0.f ? log2f(tau) : -INFINITY, cu, total, qshift, cu_k) != cudaSuccess)
+        return MALA_ERR_CUDA;
+    } else {
+      pre<<<dim3(4 * T, Hq, B), 256, 0, stream>>>((const __nv_bfloat16*)o.p, o.sb, o.sn, o.sh, (const __nv_bfloat16*)dout.p, dout.sb,
+                                      dout.sn, dout.sh, lse, lse2, bq, Dq, acc, N, Np, Nk, d, causal,
+                                      tau > 0.f ? log2f(tau) : -INFINITY, cu, total, qshift, cu_k);
+      if (cudaGetLastError() != cudaSuccess) return MALA_ERR_CUDA;
+    }
   }
   const bool dense = (tau == 0.f);
   // tau > 0: two passes where their limits hold and the workspace has room for the masks -- the test of every legal
@@ -1234,9 +1310,8 @@ inline int bwd_launch(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin d
   if (!two_pass && !dense && !bias && (long long)Tk * Hkv * B <= sms) p.behind = kBehindPre;
   if (bias) {
     p.rb = bias->v;
-    // (blocks without a tile write no sums)
-    if (cudaMemsetAsync(p.rb.part, 0, (size_t)B * Hq * Tk * kBiasWarps * p.rb.buckets * sizeof(float), stream) != cudaSuccess)
-      return MALA_ERR_CUDA;
+    // (as above: a small call's launches wait for one another on the device)
+    if ((long long)Tk * Hkv * B <= sms) p.behind = kBehindPre;
     rc = bias_launch_bwd(D, dense, tq, tk, tv, tdo, tacc, p, stream);
   } else
   if (two_pass) {
@@ -1273,13 +1348,9 @@ inline int bwd_launch(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin d
     rc = dense ? bwd_launch_main<64, true>(tq, tk, tv, tdo, tacc, p, stream) : bwd_launch_main<64, false>(tq, tk, tv, tdo, tacc, p, stream);
   }
   if (rc != MALA_OK) return rc;
-  if (bias) {
-    rc = bias_launch_reduce(p.rb, B, Hq, Tk, bias->dtable, bias->sb, stream);
-    if (rc != MALA_OK) return rc;
-  }
   auto convert = D == 128 ? bwd_convert_dq_kernel<128> : bwd_convert_dq_kernel<64>;
   return launch_dependent(convert, dim3(T, Hq, B), dim3(256), stream, acc, (__nv_bfloat16*)dq.p, dq.sb, dq.sn, dq.sh, N, Np, scale, cu,
-                          qshift, d, cu_k, causal) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+                          qshift, d, cu_k, causal, bias ? *bias : BwdBias{}, B, Tk) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
 }  // namespace mala

@@ -168,7 +168,6 @@ mala_decode_split_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   const int R = kMulti ? G * p.Sq : G;     // rows of a work item: row s * G + g = token s, head g of the group
   int* status = p.status;
   static_assert(!kBias || kMulti, "");
-  if constexpr (kBias) wait_for_primary();
 
   // the Q tile of an item has R <= 16 rows; the other rows of the two stages are never written: clear them once
   for (int i = tid; i < 2 * DecCfg::kQBytes / 16; i += DecCfg::kThreads) reinterpret_cast<uint4*>(sQ)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -195,7 +194,10 @@ mala_decode_split_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     mbar_fence_init();
   }
   __syncthreads();
-  if (early_exit) return;
+  if (early_exit) {
+    if constexpr (kBias) wait_for_primary();   // (as the softmax groups do: no block ends before the kernel that lays the bias out)
+    return;
+  }
   if (warp == 0) { tmem_alloc(&tmem_base_s, DecCfg::kTmemCols); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
@@ -665,6 +667,7 @@ mala_decode_split_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     // warps of a group: every warp publishes the per-row maxima of its 32 keys of this tile together with its
     // per-row sums of P of the previous retained tile; after one group barrier every thread holds the tile's row
     // maxima and the up-to-date normalizers and evaluates Eq. 3 for the group's rows itself.
+    if constexpr (kBias) wait_for_primary();
     const int w = warp & 3;
     const int grp = (warp - 4) >> 2;               // softmax group
     const int rb = grp * GH;                       // its first row

@@ -128,8 +128,10 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   // (paged: a length beyond what the block table's row can map is clamped, so no lookup ever leaves the row)
   const int Nkeys = p.block_table ? min(__ldg(p.seqlens_k + b), p.bt_stride * (p.ppt > 1 ? p.prows : p.tpp * 128))
                                   : (p.cu_k ? __ldg(p.cu_k + b + 1) - krow0 : (p.cu ? Nq : p.Nk));
-  if constexpr (kBias) wait_for_primary();
+  // (with a bias the kernel is a dependent of the one that lays it out: the softmax warps wait for that, and blocks without work)
+  auto settle = [&]() { if constexpr (kBias) wait_for_primary(); };
   if (own_keys && (Nkeys <= 0 || (p.causal && Nkeys < Nq))) {   // (not defined: no keys, more queries than keys)
+    settle();
     if constexpr (kBias) empty_rows(p, b, h, row0, Nq, place.x * 256, 256);
     return;
   }
@@ -161,7 +163,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   const int npairs = (Tr + 1) / 2;
   // longest pairs first: of this head and sequence, or (by_size) of all of them, the longest sequence's last pair in front
   const int c = (p.by_size ? (int)gridDim.x : npairs) - 1 - place.x;
-  if (c < 0 || c >= npairs) return;                  // (a sequence shorter than the longest one)
+  if (c < 0 || c >= npairs) { settle(); return; }    // (a sequence shorter than the longest one)
   int iA = 2 * c, iB = 2 * c + 1;
   bool hasB = iB < Tr;
   int dA = p.causal ? iA + koff : Tk - 1;            // newest key block with a legal key, per block
@@ -197,7 +199,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     mbar_fence_init();
   }
   __syncthreads();
-  if (early_exit) return;
+  if (early_exit) { settle(); return; }
   if (warp == 0) { tmem_alloc(&tmem_base_s, Cfg::kTmemCols); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
@@ -431,6 +433,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     // (Near tile m uses slot m & 1: a warp fills it behind its wait for the values of near tile m - 1, for which every warp
     // arrived behind its use of near tile m - 2.)
     [[maybe_unused]] const int qpos0 = i * 128 + (p.causal ? koff * 128 : Nkeys - Nq);
+    settle();
     [[maybe_unused]] const float* brow = kBias ? (kDense ? p.rb.vals : p.rb.b2) + (size_t)h * (2 * p.rb.half + 1) + p.rb.half : nullptr;
     [[maybe_unused]] const float btop = kBias && kDense ? __ldg(p.rb.top + h) : NAN;
     [[maybe_unused]] const bool factors = btop == btop;

@@ -112,8 +112,10 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   const int krow0 = p.cu_k ? __ldg(p.cu_k + b) : row0;
   const int Nkeys = p.block_table ? min(__ldg(p.seqlens_k + b), p.bt_stride * (p.ppt > 1 ? p.prows : p.tpp * 128))
                                   : (p.cu_k ? __ldg(p.cu_k + b + 1) - krow0 : (p.cu ? Nq : p.Nk));
-  if constexpr (kBias) wait_for_primary();
+  // (with a bias the kernel is a dependent of the one that lays it out: the softmax warps wait for that, and blocks without work)
+  auto settle = [&]() { if constexpr (kBias) wait_for_primary(); };
   if (own_keys && (Nkeys <= 0 || (p.causal && Nkeys < Nq))) {
+    settle();
     if constexpr (kBias) empty_rows(p, b, h, row0, Nq, place.x * 128, 128);
     return;
   }
@@ -124,7 +126,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   const int bz = p.cu ? 0 : b;
   // longest blocks first: of this head and sequence, or (by_size) of all of them
   const int i = (p.by_size ? (int)gridDim.x : Tr) - 1 - place.x;
-  if (i < 0 || i >= Tr) return;
+  if (i < 0 || i >= Tr) { settle(); return; }
   const int dI = p.causal ? i + koff : Tk - 1;       // newest key block with a legal key
   int jlo = 0, jhi = Tk - 1;                         // key blocks of this CTA
   if (p.num_splits > 1) {
@@ -174,7 +176,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   }
   if (tid < 256) ctl.letter[tid >> 7][tid & 127] = ~0ull;
   __syncthreads();
-  if (ctl.early_exit) return;
+  if (ctl.early_exit) { settle(); return; }
   if (warp == 0) { tmem_alloc(&ctl.tmem_base, 512); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
@@ -342,6 +344,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const bool mask_first = j0 == dI;
     // the block's bias, as in mala_fwd_kernel (here by the threads of both halves, a value each)
     [[maybe_unused]] const int qpos0 = i * 128 + (p.causal ? koff * 128 : Nkeys - Nq);
+    settle();
     [[maybe_unused]] const float* brow = kBias ? (kDense ? p.rb.vals : p.rb.b2) + (size_t)h * (2 * p.rb.half + 1) + p.rb.half : nullptr;
     [[maybe_unused]] const float btop = kBias && kDense ? __ldg(p.rb.top + h) : NAN;
     [[maybe_unused]] const bool factors = btop == btop;
