@@ -88,34 +88,6 @@ __device__ __forceinline__ void bias_put(float* slot, int y, float v) {
 __device__ __forceinline__ const float4* bias_from(const float* slot, int y) {
   return reinterpret_cast<const float4*>(slot + (y & 3) * kBiasPitch + (y & ~3));
 }
-// Two fp32 values side by side: one instruction for both (sm_100)
-__device__ __forceinline__ uint64_t f2(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void f2_get(uint64_t x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
-__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-// bf16 pair of two fp32 values
-__device__ __forceinline__ uint32_t f2_bf16(uint64_t x) {
-  float a, b;
-  f2_get(x, a, b);
-  return pack_bf16x2(a, b);
-}
 // s = s * c + b for N scores
 template <int N>
 __device__ __forceinline__ void bias_add(uint32_t (&s)[N], float c, const float4* b) {

@@ -165,12 +165,6 @@ static int launch_tables(const TableParams& p, cudaStream_t stream) {
   return launch_dependent_smem(page_tables_kernel<kRelease>, dim3(grid), dim3(kTableThreads), smem, stream, p) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
-bool cache_set_attributes() {
-  const int most = 2 * (kTableMaxB + 1) * (int)sizeof(int);
-  return cudaFuncSetAttribute(page_tables_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess &&
-         cudaFuncSetAttribute(page_tables_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
-}
-
 static bool page_size_ok(int ps) { return ps >= 8 && (ps % 128 == 0 || 128 % ps == 0); }
 
 // ------------------------------------------------------------------------------------------------
@@ -228,6 +222,11 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 __device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
   uint32_t h;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(c));
@@ -237,54 +236,54 @@ __device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
 // e4m3 pages: the keys of a unit (min(page_size, 128) of them) share a scale.  The rows of a unit are neighbours in the call, and
 // a block looks among p.chunk rows for those with which a unit begins, for one KV head and K or V.
 //
-// A team of kThreads threads writes one unit: 16 threads per row in 16-byte loads, eight loads in flight each, first the largest
-// magnitude, then the codes; what one round of loads covers (128 rows of a block, 16 of a warp) stays in registers between
-// the two and is read once.  Bound by HBM with many rows (3 bytes per element) and by the chain slots -> rows -> scale ->
-// codes with few.
-template <int kThreads>
-__device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int h, int t, int64_t slot, float* red) {
+// A team of kThreads threads writes one unit: 16 threads per row in 16-byte copies, first the largest magnitude, then the codes.
+// The rows wait in shared memory between the two (a block's team: all of a unit; a warp's: a share of that at a time), each
+// thread's in places of its own, so that they are read once.  With many rows (28000 of 8 x 128: 3 bytes per element are 33 us at
+// the copy rate) blocks of two warps: what a warp does once per unit -- where it lies, its maximum, its scale -- weighs as much
+// as 1000 of its elements (eight warps: 67 us; with the rows in registers, three blocks per SM: 129).  Few rows are bound
+// by the chain slots -> rows -> scale -> codes, and get blocks of eight warps.
+__device__ __forceinline__ void copy16_async(uint4* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+template <int kThreads, int kBuffer>
+__device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int h, int t, int n, int64_t slot, uint4* buf, float* red) {
   constexpr int kRows = kThreads / 16;
   const int tid = threadIdx.x & (kThreads - 1), lane = threadIdx.x & 31, r0 = tid >> 4, c = tid & 15;
-  const int unit = p.unit;
+  const int batch = kBuffer == kThreads ? p.unit : p.unit * kThreads / kBuffer;   // rows that its part of the buffer holds
   const bool mine = c < p.cols;
-  const uint8_t* src = (is_v ? p.v + h * p.v_sh : p.k + h * p.k_sh) + c * 16;
-  const int64_t s_sn = is_v ? p.v_sn : p.k_sn, d_sn = is_v ? p.vp_sn : p.kp_sn;
+  const int64_t s_sn = is_v ? p.v_sn : p.k_sn, s_sh = is_v ? p.v_sh : p.k_sh, d_sn = is_v ? p.vp_sn : p.kp_sn, d_sh = is_v ? p.vp_sh : p.kp_sh;
   const int64_t page = p.limit <= 0xffffffffll ? (int64_t)p.by_page.div((uint32_t)slot) : slot / p.page_size, at = slot - page * p.page_size;
-  const int off = (int)(at & (unit - 1));
-  uint8_t* dst = (is_v ? p.vp + h * p.vp_sh + page * p.vp_sb : p.kp + h * p.kp_sh + page * p.kp_sb) + at * d_sn + c * 8;
+  const int off = (int)(at & (p.unit - 1));
+  const uint8_t* src = (is_v ? p.v : p.k) + h * s_sh + (int64_t)(t + r0) * s_sn + c * 16;
+  uint8_t* dst = (is_v ? p.vp + page * p.vp_sb : p.kp + page * p.kp_sb) + h * d_sh + (at + r0) * d_sn + c * 8;
   float* sp = (is_v ? p.vscale : p.kscale) + (page * p.Hkv + h) * p.per_page + at / 128;
-  const float old = *(volatile const float*)sp;   // (before the store below, which a cached load need not be)
-  // rows of the unit: as long as the slots follow one another (every warp finds out for itself)
-  int n = unit - off;
-  for (int x0 = 0; x0 < n; x0 += 32) {
-    const int x = x0 + lane;
-    const uint32_t out = __ballot_sync(0xffffffffu, x < n && (t + x >= p.rows || __ldg(p.slots + t + x) != slot + x));
-    if (out) n = x0 + __ffs(out) - 1;
-  }
-  uint4 w[8];
-  auto load = [&](int first) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = first + r0 + i * kRows;
-      w[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (r < n && mine) w[i] = __ldg(reinterpret_cast<const uint4*>(src + (int64_t)(t + r) * s_sn));
-    }
+  buf += tid;
+  auto load = [&](const uint8_t* from, uint4* to, int first) {
+    if (mine)
+      for (int r = first + r0, end = min(first + batch, n); r < end; r += kRows, to += kThreads, from += kRows * s_sn) copy16_async(to, from);
   };
-  float top = 0.f;
-  for (int first = 0; first < n; first += 8 * kRows) {
-    load(first);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) top = max3(top, fabsf(__uint_as_float(u[e] << 16)), fabsf(__uint_as_float(u[e] & 0xffff0000u)));
-    }
+  load(src, buf, 0);
+  const float old = *(volatile const float*)sp;   // (before the store below, which a cached load need not be)
+  uint32_t top2 = 0;                     // largest magnitudes of the even and the odd columns (bf16 magnitudes are ordered like their bits)
+  for (int first = 0; first < n; first += batch) {
+    if (first > 0) load(src + (int64_t)first * s_sn, buf, first);
+    copies_wait();
+    const uint4* from = buf;
+    if (mine)
+      for (int r = first + r0, end = min(first + batch, n); r < end; r += kRows, from += kThreads) {
+        const uint4 w = *from;
+        top2 = max_u16x2(max_u16x2(top2, w.x & 0x7fff7fffu), w.y & 0x7fff7fffu);
+        top2 = max_u16x2(max_u16x2(top2, w.z & 0x7fff7fffu), w.w & 0x7fff7fffu);
+      }
   }
+  float top = fmaxf(__uint_as_float(top2 << 16), __uint_as_float(top2 & 0xffff0000u));
 #pragma unroll
   for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
   if constexpr (kThreads > 32) {
     if (lane == 0) red[threadIdx.x >> 5] = top;
-    __syncthreads();                       // (and everyone has read the old scale)
+    __syncthreads();                     // (and everyone has read the old scale)
 #pragma unroll
     for (int i = 0; i < kThreads / 32; ++i) top = fmaxf(top, red[i]);
   } else {
@@ -292,86 +291,110 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int
   }
   const float want = __fdiv_rn(top, 448.f);
   float s = off == 0 ? want : fmaxf(old, want);
-  if (!(s > 0.f)) s = 1.f;                 // (nothing but zeros)
+  if (!(s > 0.f)) s = 1.f;               // (nothing but zeros)
   if (tid == 0) *sp = s;
-  // x / s, rounded as a division: with y = 1 / s correctly rounded, the quotient's first estimate x y is put right by its exact remainder
-  // (Markstein, Computation of elementary functions on the IBM RISC System/6000 processor, 1990).  Scales so small that y or the
-  // remainders leave the range are divided by.
-  const float y = __fdiv_rn(1.f, s);
-  const bool plain = s < 1e-30f || s > 1e30f;
-  auto over_s = [&](float x) -> float {
-    if (plain) return __fdiv_rn(x, s);
-    const float q = x * y;
-    return copysignf(fmaf(fmaf(-q, s, x), y, q), x);   // (a zero's sign would go in the remainder)
+  // x / s, rounded as a division: with y = 1 / s correctly rounded, the quotient's first estimate x y is put right by its exact
+  // remainder (Markstein, Computation of elementary functions on the IBM RISC System/6000 processor, 1990), two at a time; the codes
+  // take the sign of x, which a zero loses on the way.  Both are first moved by a power of two where y or the remainders would
+  // leave the range (what then becomes too small to be exact has a quotient far below the smallest code).
+  const float move = s < 1e-20f ? 0x1p64f : s > 1e20f ? 0x1p-64f : 1.f, s_ = s * move, y = __fdiv_rn(1.f, s_);
+  const uint64_t move2 = f2(move, move), y2 = f2(y, y), minus_s2 = f2(-s_, -s_);
+  auto codes2 = [&](float a, float b) -> uint32_t {
+    const uint64_t x = f2_mul(f2(a, b), move2), q = f2_mul(x, y2);
+    float qa, qb;
+    f2_get(f2_fma(f2_fma(q, minus_s2, x), y2, q), qa, qb);
+    return e4m3x2(qa, qb);
   };
-  for (int first = 0; first < n; first += 8 * kRows) {
-    if (n > 8 * kRows) load(first);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = first + r0 + i * kRows;
-      if (r < n && mine) {
-        const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-        uint32_t q[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] = e4m3x2(over_s(__uint_as_float(u[e] << 16)), over_s(__uint_as_float(u[e] & 0xffff0000u)));
-        *reinterpret_cast<uint2*>(dst + r * d_sn) = make_uint2(q[0] | (q[1] << 16), q[2] | (q[3] << 16));
-      }
+  auto signs = [&](uint32_t codes, uint32_t high) -> uint32_t { return (codes & 0x7f7f7f7fu) | (high & 0x80808080u); };
+  for (int first = 0; first < n; first += batch) {
+    if (n > batch) {
+      load(src + (int64_t)first * s_sn, buf, first);
+      copies_wait();
     }
+    const uint4* from = buf;
+    uint8_t* to = dst + first * d_sn;
+    if (mine)
+      for (int r = first + r0, end = min(first + batch, n); r < end; r += kRows, from += kThreads, to += kRows * d_sn) {
+        const uint4 w = *from;
+        auto four = [&](uint32_t u, uint32_t v) -> uint32_t {
+          const uint32_t q = codes2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)) |
+                             (codes2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)) << 16);
+          return signs(q, __byte_perm(u, v, 0x7531));
+        };
+        *reinterpret_cast<uint2*>(to) = make_uint2(four(w.x, w.y), four(w.z, w.w));
+      }
   }
-  if (off > 0 && s > old) {                // the keys that the unit held: on the new scale
-    for (int first = -off; first < 0; first += 8 * kRows) {
+  if (off > 0 && s > old && mine) {      // the keys that the unit held: on the new scale
+    for (int first = r0 - off; first < 0; first += 8 * kRows) {
+      uint8_t* const to = dst + (first - r0) * d_sn;
       uint2 o[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = first + r0 + i * kRows;
-        if (r < 0 && mine) o[i] = *reinterpret_cast<const uint2*>(dst + r * d_sn);
-      }
+      for (int i = 0; i < 8; ++i)
+        if (first + i * kRows < 0) o[i] = *reinterpret_cast<const uint2*>(to + i * kRows * d_sn);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int r = first + r0 + i * kRows;
-        if (r < 0 && mine) {
-          const uint32_t u[2] = {o[i].x, o[i].y};
-          uint32_t q[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float2 a = from_e4m3x2((uint16_t)u[e]), b = from_e4m3x2((uint16_t)(u[e] >> 16));
-            q[e] = e4m3x2(over_s(a.x * old), over_s(a.y * old)) | (e4m3x2(over_s(b.x * old), over_s(b.y * old)) << 16);
-          }
-          *reinterpret_cast<uint2*>(dst + r * d_sn) = make_uint2(q[0], q[1]);
+        if (first + i * kRows < 0) {
+          auto four = [&](uint32_t u) -> uint32_t {
+            const float2 a = from_e4m3x2((uint16_t)u), b = from_e4m3x2((uint16_t)(u >> 16));
+            return signs(codes2(a.x * old, a.y * old) | (codes2(b.x * old, b.y * old) << 16), u);
+          };
+          *reinterpret_cast<uint2*>(to + i * kRows * d_sn) = make_uint2(four(o[i].x), four(o[i].y));
         }
       }
     }
   }
 }
 
-__global__ void __launch_bounds__(256, 3)
+template <int kBlock>
+__global__ void __launch_bounds__(kBlock, kBlock == 64 ? 14 : 4)
 cache_write8_kernel(const WriteParams p) {
+  extern __shared__ __align__(16) uint4 rows_s[];       // 256 bytes per key of a unit
+  constexpr int kWarps = kBlock / 32;
   const bool is_v = blockIdx.z != 0;
-  const int h = blockIdx.y, t0 = blockIdx.x * p.chunk, lane = threadIdx.x & 31;
-  __shared__ float red[2][8];
-  // the rows of the chunk (at most 64) with which a unit begins
-  uint64_t begins = 0;
-  for (int x0 = 0; x0 < p.chunk; x0 += 32) {
-    const int t = t0 + x0 + lane;
-    bool first = false;
-    if (x0 + lane < p.chunk && t < p.rows) {
-      const int64_t slot = __ldg(p.slots + t), prev = t > 0 ? __ldg(p.slots + t - 1) : -2;
-      first = slot >= 0 && slot < p.limit && ((slot & (p.unit - 1)) == 0 || prev + 1 != slot);
+  const int h = blockIdx.y, t0 = blockIdx.x * p.chunk, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ float red[2][kWarps];
+  __shared__ uint32_t ends_s[8], valid_s[8];
+  // Rows at which something begins or has no place, among the chunk's (at most 64) and as many behind them as a unit has: a bit each,
+  // and a bit for those with a place; a unit begins at a row with both and reaches up to the next one with the first.
+  for (int w = warp; w < (p.chunk + p.unit + 31) / 32; w += kWarps) {   // (at most six words)
+    const int t = t0 + w * 32 + lane;
+    int64_t slot = -1, prev = -2;
+    if (t < p.rows) {
+      slot = __ldg(p.slots + t);
+      if (t > 0) prev = __ldg(p.slots + t - 1);
     }
-    begins |= (uint64_t)__ballot_sync(0xffffffffu, first) << x0;
+    const bool valid = slot >= 0 && slot < p.limit;
+    const uint32_t ends = __ballot_sync(0xffffffffu, !valid || (slot & (p.unit - 1)) == 0 || prev + 1 != slot);
+    const uint32_t places = __ballot_sync(0xffffffffu, valid);
+    if (lane == 0) { ends_s[w] = ends; valid_s[w] = places; }
   }
-  // few of them: the whole block takes one after the other; many, which are short: a warp each
-  if (__popcll(begins) <= 2) {
-    for (int x = 0; begins; begins &= begins - 1, x ^= 1) {
-      const int t = t0 + __ffsll((long long)begins) - 1;
-      write8_unit<256>(p, is_v, h, t, __ldg(p.slots + t), red[x]);
+  __syncthreads();
+  uint64_t begins = ends_s[0] & valid_s[0];
+  if (p.chunk > 32) begins |= (uint64_t)(ends_s[1] & valid_s[1]) << 32;
+  else if (p.chunk < 32) begins &= (1u << p.chunk) - 1u;
+  // few units: the whole block takes one after the other; many, which are short: a warp each
+  const bool few = __popcll(begins) <= (kBlock == 64 ? 2 : 1);
+  for (int i = 0; begins; begins &= begins - 1, ++i) {
+    const int x = __ffsll((long long)begins) - 1;
+    if (!few && i % kWarps != warp) continue;
+    const int64_t at = __ldg(p.slots + t0 + x);
+    const int last = x + p.unit - (int)(at & (p.unit - 1));
+    int end = x + 1;                                      // the next row with a bit, within the unit
+    while (end < last) {
+      const uint32_t rest = ends_s[end >> 5] >> (end & 31);
+      if (rest) { end += __ffs(rest) - 1; break; }
+      end = (end | 31) + 1;
     }
-  } else {
-    for (int x = 0; begins; begins &= begins - 1, ++x) {
-      const int t = t0 + __ffsll((long long)begins) - 1;
-      if ((x & 7) == (int)(threadIdx.x >> 5)) write8_unit<32>(p, is_v, h, t, __ldg(p.slots + t), nullptr);
-    }
+    end = min(end, last);
+    if (few) write8_unit<kBlock, kBlock>(p, is_v, h, t0 + x, end - x, at, rows_s, red[i & 1]);
+    else write8_unit<32, kBlock>(p, is_v, h, t0 + x, end - x, at, rows_s + warp * (p.unit * 16 / kWarps), nullptr);
   }
+}
+
+bool cache_set_attributes() {
+  const int most = 2 * (kTableMaxB + 1) * (int)sizeof(int);
+  return cudaFuncSetAttribute(page_tables_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess &&
+         cudaFuncSetAttribute(page_tables_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
 }
 
 static bool aligned16(const void* p) { return (((uintptr_t)p) & 15) == 0; }
@@ -488,9 +511,15 @@ int mala_cache_write_fp8(mala_tin k, mala_tin v, const int64_t* slots, mala_tout
   int dev = 0, *status = nullptr;
   MALA_TRY(current_device_checked(&dev));
   MALA_TRY(device_setup(dev, &status));
-  // One row per block as long as all blocks run at once (three per SM); then more, so that few blocks find nothing to do, up to 64
-  while (w.chunk < 64 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 3ll * sm_count(dev)) w.chunk *= 2;
-  cache_write8_kernel<<<dim3((unsigned)((rows + w.chunk - 1) / w.chunk), Hkv, 2), 256, 0, (cudaStream_t)cuda_stream>>>(w);
+  // Blocks of eight warps and of so few rows that all blocks run at once (four per SM); where that would take more than eight rows
+  // each, 64 rows per block of two warps (so that few blocks find nothing to do)
+  while (w.chunk < 16 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 4ll * sm_count(dev)) w.chunk *= 2;
+  const bool many = w.chunk == 16;
+  if (many) w.chunk = 64;
+  const dim3 grid((unsigned)((rows + w.chunk - 1) / w.chunk), Hkv, 2);
+  const size_t smem = (size_t)w.unit * 256;
+  if (many) cache_write8_kernel<64><<<grid, 64, smem, (cudaStream_t)cuda_stream>>>(w);
+  else cache_write8_kernel<256><<<grid, 256, smem, (cudaStream_t)cuda_stream>>>(w);
   return scope.finish(cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA);
 }
 
