@@ -45,9 +45,8 @@ __device__ __forceinline__ uint64_t scan_block(uint64_t x, uint64_t* warp_sums) 
   return x + (w ? warp_sums[w - 1] : 0);
 }
 
-// Largest index b in [0, n) with at[b] <= x (at[0] = 0, non-decreasing)
-__device__ __forceinline__ int find_last(const int* at, int n, int x) {
-  int lo = 0, hi = n;
+// Largest index b in [lo, hi) with at[b] <= x (at[lo] <= x, non-decreasing)
+__device__ __forceinline__ int find_last(const int* at, int lo, int hi, int x) {
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (at[mid] <= x) lo = mid;
@@ -62,6 +61,7 @@ struct TableParams {
   int* free_pages; const int* free_count;
   int* cu; int* seqlens_out; int64_t* slots; int* free_out;
   int B, max_pages, page_size, num_pages, rows;
+  FastDiv by_page;
 };
 
 // kRelease: the pages of finished requests go behind the free ones, in their order.
@@ -71,6 +71,7 @@ page_tables_kernel(const TableParams p) {
   extern __shared__ int table_smem[];
   int* rows_at = table_smem;              // [B + 1] first row of a request
   int* pages_at = table_smem + p.B + 1;   // [B + 1] its first page among the step's
+  int* lens = pages_at + p.B + 1;         // [B] tokens that it holds
   __shared__ uint64_t warp_sums[32];
   __shared__ uint32_t refused[kTableMaxB / 32];
   wait_for_primary();
@@ -101,6 +102,7 @@ page_tables_kernel(const TableParams p) {
     if (b < p.B) {
       rows_at[b] = rows - n;
       pages_at[b] = pages - need;
+      lens[b] = len;
       if (b == p.B - 1) { rows_at[p.B] = rows; pages_at[p.B] = pages; }
     }
     const uint32_t no = __ballot_sync(0xffffffffu, b < p.B && !ok);
@@ -124,45 +126,61 @@ page_tables_kernel(const TableParams p) {
   __syncthreads();
   taken = taken_s;
   if (blockIdx.x == 0 && tid == 0) *p.free_out = kRelease ? min(p.num_pages, count + taken) : count - taken;
-  const int at = blockIdx.x * kTableThreads + tid, step = gridDim.x * kTableThreads;
-  // pages: number x of the step belongs to the request whose pages begin at or before x
-  for (int x = at; x < taken; x += step) {
-    const int b = find_last(pages_at, p.B, x);
-    const int len = (int)max(0ll, min(room, (long long)p.seqlens[b]));
+  const int step = gridDim.x * kTableThreads, at = blockIdx.x * kTableThreads + tid;
+  // pages: number x of the step belongs to the request whose pages begin at or before x (from the last threads on: in a small step
+  // the first ones have rows)
+  for (int x = step - 1 - at; x < taken; x += step) {
+    const int b = find_last(pages_at, 0, p.B, x);
     const int64_t row = (int64_t)b * p.max_pages;
     if (kRelease) {
       if (count + x < p.num_pages) p.free_pages[count + x] = p.block_table[row + (x - pages_at[b])];
     } else {
-      p.block_table[row + (len + ps - 1) / ps + (x - pages_at[b])] = p.free_pages[count - 1 - x];
+      p.block_table[row + (int)p.by_page.div((uint32_t)lens[b] + ps - 1) + (x - pages_at[b])] = p.free_pages[count - 1 - x];
     }
   }
   if (kRelease) return;
   const int total = rows_at[p.B];
-  for (int t = at; t < p.rows; t += step) {
-    int64_t slot = -1;
-    if (t < total) {
-      const int b = find_last(rows_at, p.B, t);
-      if (!((refused[b >> 5] >> (b & 31)) & 1u)) {
-        const int len = (int)max(0ll, min(room, (long long)p.seqlens[b]));
-        const int pos = len + (t - rows_at[b]), have = (len + ps - 1) / ps, x = pos / ps;
-        const int page = x < have ? p.block_table[(int64_t)b * p.max_pages + x] : p.free_pages[count - 1 - (pages_at[b] + x - have)];
-        slot = page >= 0 ? (int64_t)page * ps + (pos - x * ps) : -1;
-      }
+  auto slot_of = [&](int t, int lo, int hi) -> int64_t {   // row t, whose request is one of lo .. hi - 1
+    const int b = find_last(rows_at, lo, hi, t);
+    if ((refused[b >> 5] >> (b & 31)) & 1u) return -1;
+    const int len = lens[b], pos = len + (t - rows_at[b]), have = (int)p.by_page.div((uint32_t)len + ps - 1), x = (int)p.by_page.div((uint32_t)pos);
+    const int page = x < have ? p.block_table[(int64_t)b * p.max_pages + x] : p.free_pages[count - 1 - (pages_at[b] + x - have)];
+    return page >= 0 ? (int64_t)page * ps + (pos - x * ps) : -1;
+  };
+  if (p.rows <= step) {
+    if (at < p.rows) p.slots[at] = at < total ? slot_of(at, 0, p.B) : -1;
+    return;
+  }
+  // many rows, 128 at a time by a warp: where the first and the last of them belong is searched once, and between the two is seldom much
+  for (int t0 = at / 32 * 128; t0 < p.rows; t0 += step * 4) {
+    const int lo = t0 < total ? find_last(rows_at, 0, p.B, t0) : 0;
+    const int hi = t0 < total ? find_last(rows_at, lo, p.B, min(t0 + 127, total - 1)) + 1 : 0;
+    int64_t slot[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + i * 32 + (tid & 31);
+      slot[i] = t < total && t < p.rows ? slot_of(t, lo, hi) : -1;
     }
-    p.slots[t] = slot;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + i * 32 + (tid & 31);
+      if (t < p.rows) p.slots[t] = slot[i];
+    }
   }
 }
 
 template <bool kRelease>
 static int launch_tables(const TableParams& p, cudaStream_t stream) {
-  const size_t smem = 2 * ((size_t)p.B + 1) * sizeof(int);
+  const size_t smem = (3 * (size_t)p.B + 2) * sizeof(int);
+  TableParams q = p;
+  q.by_page.set((uint32_t)p.page_size);
   int dev = 0, *status = nullptr;
   MALA_TRY(current_device_checked(&dev));
   MALA_TRY(device_setup(dev, &status));
   // (four rows a thread before there is another block)
   const long long want = ((long long)(kRelease ? p.B : p.rows) + 4 * kTableThreads - 1) / (4 * kTableThreads);
   const int grid = (int)(want < 1 ? 1 : want > sm_count(dev) ? sm_count(dev) : want);
-  return launch_dependent_smem(page_tables_kernel<kRelease>, dim3(grid), dim3(kTableThreads), smem, stream, p) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+  return launch_dependent_smem(page_tables_kernel<kRelease>, dim3(grid), dim3(kTableThreads), smem, stream, q) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
 static bool page_size_ok(int ps) { return ps >= 8 && (ps % 128 == 0 || 128 % ps == 0); }
@@ -392,7 +410,7 @@ cache_write8_kernel(const WriteParams p) {
 }
 
 bool cache_set_attributes() {
-  const int most = 2 * (kTableMaxB + 1) * (int)sizeof(int);
+  const int most = (3 * kTableMaxB + 2) * (int)sizeof(int);
   return cudaFuncSetAttribute(page_tables_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess &&
          cudaFuncSetAttribute(page_tables_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
 }
