@@ -64,14 +64,23 @@ __device__ __forceinline__ void bias_near_range(int reach, int at, int& lo, int&
   hi = (at + reach + 126 + (1 << 30)) / 128 - (1 << 23) + 1;       // (sums that may be negative, rounded down)
   lo = (at - reach - 127 + (1 << 30)) / 128 - (1 << 23) + 1;
 }
-// A far tile whose bias would swallow the scores it is added to: they count for nothing (a row of lowest values weighs its keys
-// alike, in this tile as in the nearer ones, where the sums round to the bias).
+// A far tile whose bias would swallow the scores it is added to cannot be an offset: a row of lowest values weighs its keys alike, in
+// this tile as in the nearer ones, where the sums round to the bias.
 __device__ __forceinline__ bool bias_swallows(float x) { return fabsf(x) >= 1e9f && x != -INFINITY; }
-template <int N>
-__device__ __forceinline__ void bias_flatten(uint32_t (&s)[N]) {
-#pragma unroll
-  for (int e = 0; e < N; ++e)
-    if (__uint_as_float(s[e]) != -INFINITY) s[e] = 0u;
+// Such a tile, and in a dense kernel a near one without factors, are rare: the bias is added in tensor memory, where the scores are
+// read behind this as always, column by column in a loop of a few instructions (unrolled over registers the two cost the
+// backward 3-5 % in every tile, by what they displace from the instruction cache).  x = s * c + bias for the thread's own
+// row, n columns from `col` on; `at`: a value per column, or null for `far` in all of them.
+__device__ __forceinline__ void bias_add_in_place(uint32_t col, int n, float c, const float* at, float far) {
+#pragma unroll 1
+  for (int e = 0; e < n; ++e) {
+    uint32_t v;
+    tmem_ld_x1(col + (uint32_t)e, v);
+    tmem_wait_ld();
+    v = __float_as_uint(fmaf(__uint_as_float(v), c, at ? at[e] : far));
+    tmem_st_x1(col + (uint32_t)e, v);
+  }
+  tmem_wait_st();
 }
 
 // The 255 values of a tile that is not far, in shared memory.  Value number y belongs to one diagonal, and a thread of row r needs

@@ -505,7 +505,8 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     };
     auto bias_far = [&](float before, float after, int i_) -> float { return i_ >= near_hi ? before : after; };
     auto bias_fold = [&](float before, float after, float top, int i_) -> float {
-      return !bias_near(i_) ? bias_far(before, after, i_) : (top == top ? top : 0.f);
+      const float far = bias_far(before, after, i_);
+      return bias_near(i_) ? (top == top ? top : 0.f) : (bias_swallows(far) ? 0.f : far);
     };
     [[maybe_unused]] const int kbefore = kBias ? __ldg(p.rb.bucket + p.rb.half - p.rb.reach) : 0;
     [[maybe_unused]] const int kafter = kBias ? __ldg(p.rb.bucket + p.rb.half + p.rb.reach) : 0;
@@ -576,7 +577,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         const size_t x = kList ? vec_index(h_nx, i_nx) : (last_of_head ? vec_index(head(hq_n + 1), i0) : vec_index(head(hq_n), i + 1));
         nx0 = p.lse2[x]; nx1 = p.bq[x]; nx2 = p.Dq[x];
       }
-      [[maybe_unused]] bool near = false, by_factors = false, swallows = false, publish = false;
+      [[maybe_unused]] bool near = false, by_factors = false, rare = false, publish = false;
       [[maybe_unused]] int x2 = hq_n, i2 = i + 2;     // tile n + 2
       if constexpr (kBias) {
         if (first_of_head && n > 0) {
@@ -587,27 +588,30 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         // the compiler no other value is the same in all lanes
         near = __any_sync(0xffffffffu, bias_near(i));
         by_factors = kDense && __any_sync(0xffffffffu, near && btop == btop);
-        swallows = __any_sync(0xffffffffu, !near && bias_swallows(bias_far(bbefore, bafter, i)));
+        rare = __any_sync(0xffffffffu, near ? kDense && !(btop == btop) : bias_swallows(bias_far(bbefore, bafter, i)));
         while (i2 >= T) { i2 -= ni; ++x2; }
         publish = __any_sync(0xffffffffu, n + 2 < n_tot && bias_near(i2));
       }
       ok = mbar_wait_warp(&s_full, n & 1, status);
       if (!ok) break;
       tc_fence_after();
+      float cs = c2;                  // the tile's scores in the log2 domain are sc * cs (+ what the vectors have taken in, see above)
+      [[maybe_unused]] const float4* bp = nullptr;
+      if constexpr (kBias) {
+        if (near) bp = bias_from(bias_s[n & 3], 127 - rl + qt * 32);
+        if (rare) {
+          bias_add_in_place(tmem_addr(tb, lane_base, Cfg::kColS + qt * 32), 32, c2, near ? reinterpret_cast<const float*>(bp) : nullptr,
+                            bias_far(bbefore, bafter, i));
+          cs = 1.f;
+        }
+      }
       uint32_t sc[32];
       tmem_ld_x32(tmem_addr(tb, lane_base, Cfg::kColS + qt * 32), sc);
       tmem_wait_ld();
-      float cs = c2;                  // the tile's scores in the log2 domain are sc * cs (+ the flat tile's bias, see above)
-      [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
-        if (near) {
-          bp = bias_from(bias_s[n & 3], 127 - rl + qt * 32);
-          if (!by_factors) {
-            bias_add(sc, c2, bp);
-            cs = 1.f;
-          }
-        } else if (swallows) {
-          bias_flatten(sc);
+        if (!kDense && near) {
+          bias_add(sc, c2, bp);
+          cs = 1.f;
         }
       }
       // packed sequences: a row past this sequence's end holds the next one's key (and with a bias a row past the last key must

@@ -484,12 +484,12 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
       // what kind of tile this and the next one are: beside the wait for the scores, and by votes, because to the compiler no other
       // value is the same in all lanes (a vote where the branch stands is on the chain of the tile)
-      [[maybe_unused]] bool near = false, by_factors = false, swallows = false, near_next = false;
+      [[maybe_unused]] bool near = false, by_factors = false, rare = false, near_next = false;
       if constexpr (kBias) {
         near = __any_sync(0xffffffffu, bias_near(j));
         by_factors = kDense && __any_sync(0xffffffffu, near && factors);
         bs = j * 128 < qpos0 ? bbefore : bafter;
-        swallows = __any_sync(0xffffffffu, !near && bias_swallows(bs));
+        rare = __any_sync(0xffffffffu, near ? kDense && !factors : bias_swallows(bs));
         near_next = __any_sync(0xffffffffu, t + 1 < T && bias_near(j - 1));
         if (near_next) bias_fetch(j - 1);
       }
@@ -503,31 +503,32 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       ok = mbar_wait_warp(&s_full[x], t & 1, status);
       if (!ok) break;
       tc_fence_after();
+      [[maybe_unused]] const float4* bp = nullptr;
+      if constexpr (kBias) {
+        if (near) {
+          bp = bias_from(bslot + (nears & 1) * kBiasSlotFloats, 127 - rl);
+          if (by_factors) bs = btop;     // (the factors are waited for where they are used)
+          else ok = mbar_wait_warp(&bias_bar[x], nears & 1, status);
+          if (!ok) break;
+        }
+        if (rare) {
+          bias_add_in_place(tmem_addr(tb, lane_base, colS), 128, c2, near ? reinterpret_cast<const float*>(bp) : nullptr, bs);
+          cs = 1.f; bs = 0.f;
+        }
+      }
       uint32_t s0[32], s1[32], s2[32], s3[32];
       tmem_ld_x32(tmem_addr(tb, lane_base, colS + 0), s0);
       tmem_ld_x32(tmem_addr(tb, lane_base, colS + 32), s1);
       tmem_ld_x32(tmem_addr(tb, lane_base, colS + 64), s2);
       tmem_ld_x32(tmem_addr(tb, lane_base, colS + 96), s3);
       tmem_wait_ld();
-      [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
-        if (!near) {
-          if (swallows) {
-            bias_flatten(s0); bias_flatten(s1); bias_flatten(s2); bias_flatten(s3);
-          }
-        } else {
-          bp = bias_from(bslot + (nears & 1) * kBiasSlotFloats, 127 - rl);
-          if (by_factors) {              // (the factors are waited for where they are used)
-            bs = btop;
-          } else {
-            ok = mbar_wait_warp(&bias_bar[x], nears & 1, status);
-            if (!ok) break;
-            bias_add(s0, c2, bp);
-            bias_add(s1, c2, bp + 8);
-            bias_add(s2, c2, bp + 16);
-            bias_add(s3, c2, bp + 24);
-            cs = 1.f; bs = 0.f;
-          }
+        if (!kDense && near) {
+          bias_add(s0, c2, bp);
+          bias_add(s1, c2, bp + 8);
+          bias_add(s2, c2, bp + 16);
+          bias_add(s3, c2, bp + 24);
+          cs = 1.f; bs = 0.f;
         }
       }
       if (t == 0 && mask_first) {
