@@ -49,6 +49,47 @@ class _MalaAttentionPacked(torch.autograd.Function):
         return dq, dk, dv, None, None, None, None, None, None, None
 
 
+class _MalaAttentionBias(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, table, max_distance: int, bidirectional: bool, tau: float, scale: float, causal: bool):
+        bias = mala.RelativeBias(table, max_distance, bidirectional)
+        o, lse, _ = mala.fwd_bias(q, k, v, bias, scale, tau, causal=causal)
+        ctx.save_for_backward(q, k, v, table, o, lse)
+        ctx.args = (max_distance, bidirectional, tau, scale, causal)
+        return o
+
+    @staticmethod
+    def backward(ctx, do):
+        q, k, v, table, o, lse = ctx.saved_tensors
+        max_distance, bidirectional, tau, scale, causal = ctx.args
+        if do.stride(-1) != 1:
+            do = do.contiguous()
+        dq, dk, dv, dtable, _ = mala.bwd_bias(q, k, v, o, do, lse, mala.RelativeBias(table, max_distance, bidirectional), scale,
+                                              tau, causal=causal)
+        return dq, dk, dv, dtable, None, None, None, None, None
+
+
+class _MalaAttentionBiasPacked(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, table, cu_q, cu_k, max_q: int, max_k: int, max_distance: int, bidirectional: bool, tau: float,
+                scale: float, causal: bool):
+        bias = mala.RelativeBias(table, max_distance, bidirectional)
+        o, lse, _ = mala.fwd_varlen_bias(q, k, v, cu_q, cu_k, max_q, max_k, bias, scale, tau, causal=causal)
+        ctx.save_for_backward(q, k, v, table, o, lse, cu_q, cu_k)
+        ctx.args = (max_q, max_k, max_distance, bidirectional, tau, scale, causal)
+        return o
+
+    @staticmethod
+    def backward(ctx, do):
+        q, k, v, table, o, lse, cu_q, cu_k = ctx.saved_tensors
+        max_q, max_k, max_distance, bidirectional, tau, scale, causal = ctx.args
+        if do.stride(-1) != 1:
+            do = do.contiguous()
+        dq, dk, dv, dtable, _ = mala.bwd_varlen_bias(q, k, v, o, do, lse, cu_q, cu_k, max_q, max_k,
+                                                     mala.RelativeBias(table, max_distance, bidirectional), scale, tau, causal=causal)
+        return dq, dk, dv, dtable, None, None, None, None, None, None, None, None, None
+
+
 def mala_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tau: float, scale: Optional[float] = None,
                    causal: bool = True) -> torch.Tensor:
     """MALA attention of bf16 q [B,Nq,Hq,d] against k, v [B,Nk,Hkv,d] on a B200 (tau = 0: FullAttn), differentiable
@@ -69,3 +110,25 @@ def mala_attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_
         scale = 1.0 / math.sqrt(q.shape[-1])
     return _MalaAttentionPacked.apply(q, k, v, cu_seqlens_q, cu_seqlens_k, int(max_seqlen_q), int(max_seqlen_k),
                                       float(tau), float(scale), bool(causal))
+
+
+def mala_attention_bias(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, tau: float,
+                        max_distance: int = 128, bidirectional: bool = False, scale: Optional[float] = None,
+                        causal: bool = True) -> torch.Tensor:
+    """``mala_attention`` with a learned relative position bias: ``table`` bf16 [num_buckets, Hq], added to the scaled scores by
+    the bucket of key position - query position (see ``mala_rel_bias`` in ``include/mala.h``; the queries are the last Nq of
+    the Nk positions).  Differentiable with respect to q, k, v and the table."""
+    if scale is None:
+        scale = 1.0 / math.sqrt(q.shape[-1])
+    return _MalaAttentionBias.apply(q, k, v, table, int(max_distance), bool(bidirectional), float(tau), float(scale), bool(causal))
+
+
+def mala_attention_bias_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, cu_seqlens_q: torch.Tensor,
+                               cu_seqlens_k: torch.Tensor, max_seqlen_q: int, max_seqlen_k: int, tau: float,
+                               max_distance: int = 128, bidirectional: bool = False, scale: Optional[float] = None,
+                               causal: bool = True) -> torch.Tensor:
+    """``mala_attention_packed`` with a learned relative position bias (``mala_attention_bias``): one table for all sequences."""
+    if scale is None:
+        scale = 1.0 / math.sqrt(q.shape[-1])
+    return _MalaAttentionBiasPacked.apply(q, k, v, table, cu_seqlens_q, cu_seqlens_k, int(max_seqlen_q), int(max_seqlen_k),
+                                          int(max_distance), bool(bidirectional), float(tau), float(scale), bool(causal))

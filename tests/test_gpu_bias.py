@@ -399,3 +399,90 @@ def test_decode_paged(mala, lens, Hq, Hkv, d, page, Sq, bidir, nb, md, splits, t
                 extra = 0.0 if tau == 0 else tau * 2
                 _check(o[b, s, h], r["o"][0], (U + extra) * (r["o"][0].abs() + r["a"][0]) * 1.02 + 1e-5 + extra * float(v.abs().max()), f"o {b} {s} {h}")
                 assert abs(float(lse[b, s, h]) - float(r["lse"][0])) <= LSE_ABS + 2 * tau
+
+
+def test_autograd_functions(mala):
+    """The differentiable calls give the kernels' gradients to q, k, v and the table, dense and packed."""
+    from paper_2609_32712_b200.autograd import mala_attention_bias, mala_attention_bias_packed
+    q, k, v, do, table = _inputs(91, 2, 4, 2, 300, 300, 64, 32)
+    leaves = [t.requires_grad_(True) for t in (q, k, v, table)]
+    o = mala_attention_bias(q, k, v, table, 0.0, max_distance=100, bidirectional=True, causal=False)
+    o.backward(do)
+    bias = mala.RelativeBias(table.detach(), 100, True)
+    o2, lse, _ = mala.fwd_bias(q.detach(), k.detach(), v.detach(), bias, 0.125, 0.0, causal=False)
+    want = mala.bwd_bias(q.detach(), k.detach(), v.detach(), o2, do, lse, bias, 0.125, 0.0, causal=False)
+    assert torch.equal(o.detach(), o2)
+    for t, w in zip(leaves[1:], want[1:4]):
+        assert torch.equal(t.grad, w)
+    assert (q.grad.float() - want[0].float()).abs().max() <= 2 * U * want[0].float().abs().max()
+    cu = torch.tensor([0, 100, 300], dtype=torch.int32, device="cuda")
+    x = [t.detach()[:1].clone().requires_grad_(True) for t in (q, k, v)] + [table.detach().clone().requires_grad_(True)]
+    o = mala_attention_bias_packed(*x, cu, cu, 200, 200, 0.0, max_distance=100)
+    # (a gradient whose last dimension is not contiguous)
+    o.backward(do[:1].transpose(2, 3).contiguous().transpose(2, 3))
+    bias = mala.RelativeBias(x[3].detach(), 100)
+    y = [t.detach() for t in x[:3]]
+    o2, lse, _ = mala.fwd_varlen_bias(*y, cu, cu, 200, 200, bias, 0.125, 0.0)
+    want = mala.bwd_varlen_bias(*y, o2, do[:1].contiguous(), lse, cu, cu, 200, 200, bias, 0.125, 0.0)
+    assert torch.equal(o.detach(), o2)
+    for t, w in zip(x[1:], want[1:4]):
+        assert torch.equal(t.grad, w)
+
+
+def test_table_gradient_by_differences(mala):
+    """The gradient of sum(o * do) with respect to a bucket's entry against the difference of two forwards, whose outputs carry
+    half a step of bf16 each: sum |do| u (|o| + a) of both over twice the step, plus the table's own rounding."""
+    B, H, N, d, nb, md = 1, 2, 500, 64, 16, 60
+    q, k, v, do, table = _inputs(95, B, H, H, N, N, d, nb)
+    table = torch.round(table.float() * 4).div(4).to(torch.bfloat16)       # (so that the steps are exact)
+    bias = mala.RelativeBias(table, md)
+    o, lse, _ = mala.fwd_bias(q, k, v, bias, 0.125, 0.0)
+    dtable = mala.bwd_bias(q, k, v, o, do, lse, bias, 0.125, 0.0)[3].double()
+    step = 0.25
+    for b in (0, 3, 8, nb - 1):
+        two = []
+        for sgn in (1, -1):
+            t = table.clone()
+            t[b] += sgn * step
+            x = mala.fwd_bias(q, k, v, mala.RelativeBias(t, md), 0.125, 0.0)[0].double()
+            two.append((x * do.double()).sum((0, 1, 3)))
+        for h in range(H):
+            # the same difference in 64 bits: how far a step of that size is from the derivative, and the outputs' error bound
+            err, exact = 0.0, []
+            for sgn in (1, -1):
+                t = table[:, h].double().clone()
+                t[b] += sgn * step
+                r = R.head(q[0, :, h].double(), k[0, :, h].double(), v[0, :, h].double(), t, None, 0.125, nb, md, False, True)
+                exact.append((r["o"] * do[0, :, h].double()).sum())
+                # (independent roundings: the root of the sum of squares, six times)
+                err += 6 * float(((U * (r["o"].abs() + r["a"]) * do[0, :, h].double().abs()) ** 2).sum().sqrt())
+            got, want = (two[0][h] - two[1][h]) / (2 * step), (exact[0] - exact[1]) / (2 * step)
+            assert abs(float(got - want)) <= err / (2 * step)
+            r = R.head(q[0, :, h].double(), k[0, :, h].double(), v[0, :, h].double(), table[:, h].double(), do[0, :, h].double(), 0.125, nb, md, False, True)
+            curvature = abs(float(want - r["dtable"][b]))
+            assert abs(float(got - dtable[b, h])) <= err / (2 * step) + curvature + float(r["dtable_err"][b]) * 1.05 + U * abs(float(dtable[b, h])) + 1e-4
+
+
+@pytest.mark.parametrize("top", [3.0, 40.0, 90.0, 3e4, 1e10])
+def test_values_far_apart(mala, top):
+    """Heads whose values are so far apart that they go by sums, beside heads that go by factors."""
+    B, H, N, d, nb, md = 1, 4, 600, 64, 32, 128
+    q, k, v, do, table = _inputs(101, B, H, H, N, N, d, nb)
+    table[5:9, 0] -= top
+    table[nb - 1, 1] += top
+    table[2, 2] = -top
+    for causal, bidir in ((True, False), (False, True)):
+        bias = mala.RelativeBias(table, md, bidir)
+        o, lse, _ = mala.fwd_bias(q, k, v, bias, 0.125, 0.0, causal=causal)
+        dq, dk, dv, dtable, _ = mala.bwd_bias(q, k, v, o, do, lse, bias, 0.125, 0.0, causal=causal)
+        for t in (o, dq, dk, dv, dtable):
+            assert torch.isfinite(t.float()).all()
+        for h in range(H):
+            if top > 1e3 and h == 1:
+                continue        # (x = s + top in fp32 keeps no digits of s: compared below 2^10 alone)
+            r = R.head(q[0, :, h].double(), k[0, :, h].double(), v[0, :, h].double(), table[:, h].double(), do[0, :, h].double(), 0.125, nb, md, bidir, causal)
+            _check(o[0, :, h], r["o"], U * (r["o"].abs() + r["a"]) * 1.02 + 1e-5, f"o head {h}")
+            assert (lse[0, h].double() - r["lse"]).abs().max() <= LSE_ABS
+            _check_table(dtable[:, h], r["dtable"], r["dtable_err"])
+            for got, want in ((dq, r["dq"]), (dk, r["dk"]), (dv, r["dv"])):
+                parity.check_grad(got[0, :, h].double().cpu().numpy(), want.cpu().numpy(), f"head {h}")
