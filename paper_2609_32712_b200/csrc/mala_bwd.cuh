@@ -752,8 +752,9 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const ulonglong2 x = dd[e];
-              const uint64_t d0 = f2_mul(p2[c * 8 + 2 * e], f2_add(f2(__uint_as_float(dp[4 * e]), __uint_as_float(dp[4 * e + 1])), x.x));
-              const uint64_t d1 = f2_mul(p2[c * 8 + 2 * e + 1], f2_add(f2(__uint_as_float(dp[4 * e + 2]), __uint_as_float(dp[4 * e + 3])), x.y));
+              uint64_t &d0 = p2[c * 8 + 2 * e], &d1 = p2[c * 8 + 2 * e + 1];   // (dS^T in the place of P^T)
+              d0 = f2_mul(d0, f2_add(f2(__uint_as_float(dp[4 * e]), __uint_as_float(dp[4 * e + 1])), x.x));
+              d1 = f2_mul(d1, f2_add(f2(__uint_as_float(dp[4 * e + 2]), __uint_as_float(dp[4 * e + 3])), x.y));
               w[c * 8 + 2 * e] = f2_bf16(d0);
               w[c * 8 + 2 * e + 1] = f2_bf16(d1);
               tsum = f2_add(tsum, f2_add(d0, d1));
@@ -800,22 +801,21 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             f2_get(tsum, t0, t1);
             fsum += t0 + t1;
           } else {
-            // Sums of the 63 diagonals of this warp's 32 x 32 piece, from the rounded dS: for columns c and c + 1 lane l takes the pair
-            // of lane (l + c) % 32, whose first value lies on diagonal l, or, past the last lane, on diagonal l - 32, and
-            // whose second one on the diagonal before that.
-            float on0 = 0.f, on1 = 0.f, all0 = 0.f, all1 = 0.f;
+            // Sums of the 63 diagonals of this warp's 32 x 32 piece: in step e lane l takes the value of lane (l + e) % 32, which lies
+            // on diagonal l, or, past the last lane, on diagonal l - 32.  (Not from the rounded dS: where one bucket has most of a
+            // row's mass its sum is what is left of far larger ones, and a rounding of 2^-9 in each then shows as 2^-8 in it.)
+            float on = 0.f, all = 0.f;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const uint32_t t = __shfl_sync(0xffffffffu, w[e], (lane + 2 * e) & 31);
-              const float a = __uint_as_float(t << 16), b_ = __uint_as_float(t & 0xffff0000u);
-              all0 += a; all1 += b_;
-              if (lane + 2 * e < 32) { on0 += a; on1 += b_; }
+              float a, b_;
+              f2_get(p2[e], a, b_);
+              a = __shfl_sync(0xffffffffu, a, (lane + 2 * e) & 31);
+              b_ = __shfl_sync(0xffffffffu, b_, (lane + 2 * e + 1) & 31);
+              all += a; all += b_;
+              if (lane + 2 * e < 32) on += a;
+              if (lane + 2 * e + 1 < 32) on += b_;
             }
-            float below0 = all0 - on0, below1 = all1 - on1;
-            const float first1 = __shfl_sync(0xffffffffu, on1, 0);
-            on1 = __shfl_down_sync(0xffffffffu, on1, 1);
-            below1 = __shfl_down_sync(0xffffffffu, below1, 1);
-            const float on = lane < 31 ? on0 + on1 : on0, below = below0 + (lane < 31 ? below1 : first1);
+            const float below = all - on;
             // ... and of the runs of diagonals that share a bucket (neighbours, since buckets are monotone along delta)
             const uint8_t* bk_at = bias_k[n & 3] + 127 - (int)lane_base + qt * 32 - lane;
 #pragma unroll
