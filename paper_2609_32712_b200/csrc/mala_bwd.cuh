@@ -503,6 +503,10 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       after = __ldg(row + p.rb.reach);
       if (kDense) top = __ldg(p.rb.top + hkv * G + head(x));
     };
+    [[maybe_unused]] bool odd = false;      // the head may have tiles to which the bias is added in place
+    auto odd_head = [&]() -> bool {
+      return __any_sync(0xffffffffu, (kDense && !(btop == btop)) || bias_swallows(bbefore) || bias_swallows(bafter));
+    };
     auto bias_far = [&](float before, float after, int i_) -> float { return i_ >= near_hi ? before : after; };
     auto bias_fold = [&](float before, float after, float top, int i_) -> float {
       const float far = bias_far(before, after, i_);
@@ -557,6 +561,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         bv0 = a0; bv1 = a1; bkt = k0;
         bias_publish(0);
       }
+      odd = odd_head();
       const float b0 = bias_fold(bbefore, bafter, btop, i0);   // (with a bias the vectors' negatives, which are what is added)
       v0 = b0 - v0; v1 -= b0; v2 = -v2;
     }
@@ -577,20 +582,15 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         const size_t x = kList ? vec_index(h_nx, i_nx) : (last_of_head ? vec_index(head(hq_n + 1), i0) : vec_index(head(hq_n), i + 1));
         nx0 = p.lse2[x]; nx1 = p.bq[x]; nx2 = p.Dq[x];
       }
-      [[maybe_unused]] bool near = false, by_factors = false, rare = false, publish = false;
-      [[maybe_unused]] int x2 = hq_n, i2 = i + 2;     // tile n + 2
+      [[maybe_unused]] bool near = false, by_factors = false, publish = false;
       if constexpr (kBias) {
         if (first_of_head && n > 0) {
           bbefore = bbefore_next; bafter = bafter_next; btop = btop_next;
+          odd = odd_head();
         }
         if (last_of_head && n + 1 < n_tot) bias_of_head(hq_n + 1, bbefore_next, bafter_next, btop_next);
-        // what kind of tile this one is and whether tile n + 2 has values: beside the wait for the scores, and by votes, because to
-        // the compiler no other value is the same in all lanes
-        near = __any_sync(0xffffffffu, bias_near(i));
-        by_factors = kDense && __any_sync(0xffffffffu, near && btop == btop);
-        rare = __any_sync(0xffffffffu, near ? kDense && !(btop == btop) : bias_swallows(bias_far(bbefore, bafter, i)));
-        while (i2 >= T) { i2 -= ni; ++x2; }
-        publish = __any_sync(0xffffffffu, n + 2 < n_tot && bias_near(i2));
+        near = bias_near(i);             // (no vote: the same in all lanes, and what hangs on it needs none until the sums)
+        by_factors = kDense && near && btop == btop;
       }
       ok = mbar_wait_warp(&s_full, n & 1, status);
       if (!ok) break;
@@ -599,7 +599,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       [[maybe_unused]] const float4* bp = nullptr;
       if constexpr (kBias) {
         if (near) bp = bias_from(bias_s[n & 3], 127 - rl + qt * 32);
-        if (rare) {
+        if (odd && __any_sync(0xffffffffu, near ? kDense && !(btop == btop) : bias_swallows(bias_far(bbefore, bafter, i)))) {
           bias_add_in_place(tmem_addr(tb, lane_base, Cfg::kColS + qt * 32), 32, c2, near ? reinterpret_cast<const float*>(bp) : nullptr,
                             bias_far(bbefore, bafter, i));
           cs = 1.f;
@@ -670,9 +670,14 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
       }
       if (!kDense) retain = __all_sync(0xffffffffu, retain);   // same value in every lane: the branch below is uniform
-      if constexpr (kBias && !kDense) {
+      // the values of tile n + 2, where it has any (dense: fetched behind P^T)
+      auto fetch_ahead = [&]() {
+        int x2 = hq_n, i2 = i + 2;
+        while (i2 >= T) { i2 -= ni; ++x2; }
+        publish = n + 2 < n_tot && bias_near(i2);
         if (publish) bias_fetch(x2, i2);
-      }
+      };
+      if constexpr (kBias && !kDense) fetch_ahead();
       if (stat_thread && first_of_head) { r_head = 0; bm_bits = 0; bm_word = -1; }
       if (retain) {
         if (stat_thread) {
@@ -731,9 +736,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_full);
-        if constexpr (kBias && kDense) {
-          if (publish) bias_fetch(x2, i2);
-        }
+        if constexpr (kBias && kDense) fetch_ahead();
         // dS^T = P^T o (dP^T - D_q): values first, then, once dV has also finished reading the dO stage that
         // dS^T overwrites (D = 128), into shared memory for the dQ and dK MMAs
         ok = mbar_wait_warp(&dp_full, r & 1, status);
@@ -794,7 +797,7 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         __syncwarp();
         if (lane == 0) mbar_arrive(&ds_full);
         if constexpr (kBias) {   // (behind everything that others wait for)
-          if (!near) {
+          if (!__any_sync(0xffffffffu, near)) {
             const int bk = i >= near_hi ? kbefore : kafter;
             if (bk != fbucket) { flush_far(); fbucket = bk; }
             float t0, t1;
