@@ -555,8 +555,8 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         mx[3] = max3(mx[3], __uint_as_float(s3[e]), __uint_as_float(s3[e + 1]));
       }
       // row maximum of the scaled scores, log2 domain
-      float mt = fmaxf(max3(mx[0], mx[1], __uint_as_float(s0[31])), max3(mx[2], mx[3], fmaxf(fmaxf(__uint_as_float(s1[31]), __uint_as_float(s2[31])), __uint_as_float(s3[31])))) * cs;
-      if constexpr (kBias) mt = fmaxf(mt + bs, kBiasFloor);
+      const float top_ = fmaxf(max3(mx[0], mx[1], __uint_as_float(s0[31])), max3(mx[2], mx[3], fmaxf(fmaxf(__uint_as_float(s1[31]), __uint_as_float(s2[31])), __uint_as_float(s3[31]))));
+      const float mt = kBias ? fmaxf(top_ * cs + bs, kBiasFloor) : top_ * c2;
       bool retain = true;
       if (!kDense) {
         // Eq. 3: skip iff rowmax - (m + log l) < log(tau / L) for every valid row
@@ -681,35 +681,37 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         tmem_st_x16(tmem_addr(tb, lane_base, colS + (COL)), pk);                       \
       }
       // (the same phase with factors and without: warp-uniform)
-      auto exponentials = [&](auto with_factors) {
-        constexpr bool kFactors = decltype(with_factors)::value;
-        MALA_P_CHUNK(s0, 0)
-        MALA_P_CHUNK(s1, 16)
-        if constexpr (kBias) take_sums(sum0, sum1, sum2, sum3);
-        l0 += (sum0 + sum1) + (sum2 + sum3);
-        sum0 = sum1 = sum2 = sum3 = 0.f;
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full[x][0]);   // keys 0..63 of P are in place
-        MALA_P_CHUNK(s2, 32)
-        // hand the exponential phase over a little before it ends: the other group needs a few hundred cycles
-        // to notice, and the MUFU would idle meanwhile
-        __syncwarp();
-        if (lane == 0 && hasB && (x == 0 || t >= firstA)) mbar_arrive(&turn_bar[1 - x]);
-        MALA_P_CHUNK(s3, 48)
-      };
+#define MALA_P_PHASE(FACTORS)                                                          \
+      {                                                                                \
+        constexpr bool kFactors = FACTORS;                                             \
+        MALA_P_CHUNK(s0, 0)                                                            \
+        MALA_P_CHUNK(s1, 16)                                                           \
+        if constexpr (kBias) take_sums(sum0, sum1, sum2, sum3);                        \
+        l0 += (sum0 + sum1) + (sum2 + sum3);                                           \
+        sum0 = sum1 = sum2 = sum3 = 0.f;                                               \
+        tmem_wait_st();                                                                \
+        tc_fence_before();                                                             \
+        __syncwarp();                                                                  \
+        if (lane == 0) mbar_arrive(&p_full[x][0]);   /* keys 0..63 of P are in place */ \
+        MALA_P_CHUNK(s2, 32)                                                           \
+        /* hand the exponential phase over a little before it ends: the other group needs a few hundred cycles */ \
+        /* to notice, and the MUFU would idle meanwhile */                             \
+        __syncwarp();                                                                  \
+        if (lane == 0 && hasB && (x == 0 || t >= firstA)) mbar_arrive(&turn_bar[1 - x]); \
+        MALA_P_CHUNK(s3, 48)                                                           \
+      }
       if constexpr (kBias && kDense) {
         if (by_factors) {
           ok = mbar_wait_warp(&bias_bar[x], nears & 1, status);
           if (!ok) break;
-          exponentials(BiasBool<true>{});
+          MALA_P_PHASE(true)
         } else {
-          exponentials(BiasBool<false>{});
+          MALA_P_PHASE(false)
         }
       } else {
-        exponentials(BiasBool<false>{});
+        MALA_P_PHASE(false)
       }
+#undef MALA_P_PHASE
 #undef MALA_P_CHUNK
       if constexpr (kBias) take_sums(sum0, sum1, sum2, sum3);
       l1 += (sum0 + sum1) + (sum2 + sum3);
