@@ -436,7 +436,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     settle();
     [[maybe_unused]] const float* brow = kBias ? (kDense ? p.rb.vals : p.rb.b2) + (size_t)h * (2 * p.rb.half + 1) + p.rb.half : nullptr;
     [[maybe_unused]] const float btop = kBias && kDense ? __ldg(p.rb.top + h) : NAN;
-    [[maybe_unused]] const bool factors = btop == btop;
+    [[maybe_unused]] const bool factors = __any_sync(0xffffffffu, btop == btop);
     [[maybe_unused]] float* bslot = reinterpret_cast<float*>(smem + Cfg::kBiasAt) + x * 2 * kBiasSlotFloats;
     [[maybe_unused]] const float bbefore = kBias ? __ldg(p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half - p.rb.reach) : 0.f;
     [[maybe_unused]] const float bafter = kBias ? __ldg(p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half + p.rb.reach) : 0.f;
@@ -449,6 +449,9 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     }
     [[maybe_unused]] float bv0 = 0.f, bv1 = 0.f;
     [[maybe_unused]] int nears = 0;                    // near tiles so far
+    [[maybe_unused]] bool near_next = false;
+    // whether the head may have tiles to which the bias is added in place
+    [[maybe_unused]] const bool odd = kBias && __any_sync(0xffffffffu, (kDense && !factors) || bias_swallows(bbefore) || bias_swallows(bafter));
     auto bias_near = [&](int jt) -> bool { return jt >= near_lo && jt < near_hi; };
     auto bias_fetch = [&](int jt) {
       const int d0 = bias_within(p.rb, jt * 128 - qpos0);
@@ -474,7 +477,8 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     uint32_t* bm_row = (p.bitmask && present_x) ? p.bitmask + stat_row * p.words : nullptr;
 
     if constexpr (kBias) {
-      if (__any_sync(0xffffffffu, T > 0 && bias_near(j0 - first))) {
+      near_next = __any_sync(0xffffffffu, T > 0 && bias_near(j0 - first));
+      if (near_next) {
         bias_fetch(j0 - first);
         bias_stage(0);
       }
@@ -482,14 +486,14 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     for (int t = 0; t < T; ++t) {
       const int j = j0 - first - t;
       float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
-      // what kind of tile this and the next one are: beside the wait for the scores, and by votes, because to the compiler no other
+      // what kind of tile this is, and the next one: beside the wait for the scores, and from votes, because to the compiler no other
       // value is the same in all lanes (a vote where the branch stands is on the chain of the tile)
-      [[maybe_unused]] bool near = false, by_factors = false, rare = false, near_next = false;
+      [[maybe_unused]] bool near = false, by_factors = false, rare = false;
       if constexpr (kBias) {
-        near = __any_sync(0xffffffffu, bias_near(j));
-        by_factors = kDense && __any_sync(0xffffffffu, near && factors);
+        near = near_next;
+        by_factors = kDense && near && factors;
         bs = j * 128 < qpos0 ? bbefore : bafter;
-        rare = __any_sync(0xffffffffu, near ? kDense && !factors : bias_swallows(bs));
+        rare = odd && __any_sync(0xffffffffu, near ? kDense && !factors : bias_swallows(bs));
         near_next = __any_sync(0xffffffffu, t + 1 < T && bias_near(j - 1));
         if (near_next) bias_fetch(j - 1);
       }

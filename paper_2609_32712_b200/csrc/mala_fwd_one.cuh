@@ -347,7 +347,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     settle();
     [[maybe_unused]] const float* brow = kBias ? (kDense ? p.rb.vals : p.rb.b2) + (size_t)h * (2 * p.rb.half + 1) + p.rb.half : nullptr;
     [[maybe_unused]] const float btop = kBias && kDense ? __ldg(p.rb.top + h) : NAN;
-    [[maybe_unused]] const bool factors = btop == btop;
+    [[maybe_unused]] const bool factors = __any_sync(0xffffffffu, btop == btop);
     [[maybe_unused]] float* bslot = reinterpret_cast<float*>(smem + Cfg::kBiasAt);
     [[maybe_unused]] const float bbefore = kBias ? __ldg(p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half - p.rb.reach) : 0.f;
     [[maybe_unused]] const float bafter = kBias ? __ldg(p.rb.b2 + (size_t)h * (2 * p.rb.half + 1) + p.rb.half + p.rb.reach) : 0.f;
@@ -360,6 +360,9 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     }
     [[maybe_unused]] float bv = 0.f;
     [[maybe_unused]] int nears = 0;                    // near tiles so far
+    [[maybe_unused]] bool near_next = false;
+    // whether the head may have tiles to which the bias is added in place
+    [[maybe_unused]] const bool odd = kBias && __any_sync(0xffffffffu, (kDense && !factors) || bias_swallows(bbefore) || bias_swallows(bafter));
     auto bias_near = [&](int jt) -> bool { return jt >= near_lo && jt < near_hi; };
     auto bias_fetch = [&](int jt) {
       bv = __ldg(brow + bias_within(p.rb, jt * 128 - qpos0) - 127 + min(half * 128 + rl, 254));
@@ -382,7 +385,8 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     uint32_t* bm_row = p.bitmask ? p.bitmask + stat_row * p.words : nullptr;
 
     if constexpr (kBias) {
-      if (__any_sync(0xffffffffu, bias_near(j0))) {
+      near_next = __any_sync(0xffffffffu, bias_near(j0));
+      if (near_next) {
         bias_fetch(j0);
         bias_stage(0);
       }
@@ -390,14 +394,14 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     for (int t = 0; t < U; ++t) {
       const int x = t & 1, j = j0 - t;
       float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
-      // what kind of tile this and the next one are: beside the wait for the scores, and by votes, because to the compiler no other
+      // what kind of tile this is, and the next one: beside the wait for the scores, and from votes, because to the compiler no other
       // value is the same in all lanes (a vote where the branch stands is on the chain of the tile)
-      [[maybe_unused]] bool near = false, by_factors = false, rare = false, near_next = false;
+      [[maybe_unused]] bool near = false, by_factors = false, rare = false;
       if constexpr (kBias) {
-        near = __any_sync(0xffffffffu, bias_near(j));
-        by_factors = kDense && __any_sync(0xffffffffu, near && factors);
+        near = near_next;
+        by_factors = kDense && near && factors;
         bs = j * 128 < qpos0 ? bbefore : bafter;
-        rare = __any_sync(0xffffffffu, near ? kDense && !factors : bias_swallows(bs));
+        rare = odd && __any_sync(0xffffffffu, near ? kDense && !factors : bias_swallows(bs));
         near_next = __any_sync(0xffffffffu, t + 1 < U && bias_near(j - 1));
         if (near_next) bias_fetch(j - 1);
       }
