@@ -337,7 +337,8 @@ size_t mala_bias_workspace_bytes(int op, int B, int Hq, int Hkv, int Nq, int Nk,
  *
  * Pages are those of the paged calls (8, 16, 32, 64 or a multiple of 128 keys).  free_pages [num_pages] lists the free pages in its
  * first free_count[0] entries; pages are taken off its end and given back behind it.  No output may be an input's buffer
- * (block_table and free_pages apart): the next step reads what this one wrote.  B <= 16384.
+ * (block_table and free_pages apart): the next step reads what this one wrote.  B <= 16384, B * max_pages_per_seq
+ * below 2^31, at most 2^30 rows in a call.
  *
  * mala_page_tables: request b holds seqlens[b] tokens, whose pages stand in the first ceil(seqlens[b] / page_size) entries of its
  * row of block_table [B, max_pages_per_seq], and gets new_tokens[b] more (below 0: none).
@@ -363,7 +364,7 @@ int mala_release_pages(const uint8_t* done, const int32_t* seqlens, const int32_
 
 /* k, v: bf16 [rows, Hkv, d] views (sn = row stride, sh = head stride, sb ignored); row t goes to slot slots[t] of kpages, vpages
  * [num_pages, page_size, Hkv, d], rows whose slot is negative or beyond the pool nowhere.  d a multiple of 8 up to 256.
- * Two rows with the same slot: either of them is written. */
+ * A slot stands for one row at most: one that is given twice holds, 8 columns by 8 columns, either row's. */
 int mala_cache_write(mala_tin k, mala_tin v, const int64_t* slots, mala_tout kpages, mala_tout vpages, int rows, int Hkv,
                      int num_pages, int page_size, int d, void* cuda_stream);
 

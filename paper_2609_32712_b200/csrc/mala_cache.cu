@@ -21,6 +21,7 @@ namespace mala {
 // a few hundred bytes; 1000 requests of 2000 rows: 8 MB of slots), so each is one launch without any exchange between
 // blocks: every block works out the prefix sums for itself, in its shared memory.
 constexpr int kTableThreads = 1024, kTableMaxB = 16384;
+constexpr int kMaxRows = 1 << 30;         // (rows of a call: places up to a grid's step behind them are counted in 32 bits)
 
 // Inclusive prefix sum over the block of two 32-bit counts side by side (their totals stay below 2^31)
 __device__ __forceinline__ uint64_t scan_block(uint64_t x, uint64_t* warp_sums) {
@@ -429,7 +430,7 @@ static int check_cache_view(const void* p, int64_t sb, int64_t sn, int64_t sh, i
 static int write_params(WriteParams* w, mala_tin k, mala_tin v, const int64_t* slots, mala_tout kp, mala_tout vp, int rows, int Hkv,
                         int num_pages, int page_size, int d, int item) {
   if (rows < 0 || Hkv <= 0 || num_pages <= 0 || page_size <= 0 || d <= 0) return MALA_ERR_INVALID_ARG;
-  if (!page_size_ok(page_size) || Hkv > 65535) return MALA_ERR_UNSUPPORTED;
+  if (!page_size_ok(page_size) || Hkv > 65535 || rows > kMaxRows) return MALA_ERR_UNSUPPORTED;
   if (rows > 0 && !slots) return MALA_ERR_INVALID_ARG;
   if ((((uintptr_t)slots) & 7) != 0) return MALA_ERR_MISALIGNED;
   if (rows > 0) {
@@ -462,7 +463,8 @@ static int check_tables(const int32_t* seqlens, const int32_t* block_table, cons
   if (all & 3) return MALA_ERR_MISALIGNED;
   // (every block reads the inputs for itself, so nothing that one of them writes may be among them)
   if (seqlens_out == seqlens || free_count_out == free_count) return MALA_ERR_INVALID_ARG;
-  if (B > kTableMaxB || !page_size_ok(page_size) || (long long)max_pages * page_size > 0x7fffffffLL) return MALA_ERR_UNSUPPORTED;
+  if (B > kTableMaxB || !page_size_ok(page_size) || (long long)max_pages * page_size > 0x7fffffffLL || (long long)B * max_pages > 0x7fffffffLL)
+    return MALA_ERR_UNSUPPORTED;                        // (the last one: all pages of all requests are counted in 32 bits)
   return MALA_OK;
 }
 
@@ -480,6 +482,7 @@ int mala_page_tables(const int32_t* seqlens, const int32_t* new_tokens, int32_t*
   MALA_TRY(check_tables(seqlens, block_table, free_pages, free_count, seqlens_out, free_count_out, B, max_pages_per_seq, page_size, num_pages));
   if (!new_tokens || !cu_seqlens || rows < 0 || (rows > 0 && !slots)) return MALA_ERR_INVALID_ARG;
   if ((((uintptr_t)new_tokens) & 3) != 0 || (((uintptr_t)cu_seqlens) & 3) != 0 || (((uintptr_t)slots) & 7) != 0) return MALA_ERR_MISALIGNED;
+  if (rows > kMaxRows) return MALA_ERR_UNSUPPORTED;
   if (cu_seqlens == seqlens || cu_seqlens == new_tokens || seqlens_out == new_tokens) return MALA_ERR_INVALID_ARG;
   TableParams p = {};
   p.seqlens = seqlens; p.new_tokens = new_tokens; p.block_table = block_table; p.free_pages = (int*)free_pages; p.free_count = free_count;

@@ -587,7 +587,7 @@ class RelativeBias:
 
     def _for(self, q):
         assert self.heads == q.shape[2] and self.table.device == q.device, "the table has a column per query head of q"
-        self.c.table = self.table.data_ptr()     # (a parameter's storage may have been replaced)
+        self.c.table, self.c.sb = self.table.data_ptr(), self.table.stride(0)   # (a parameter's storage may have been replaced)
         return ctypes.byref(self.c)
 
 

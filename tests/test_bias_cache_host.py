@@ -159,6 +159,7 @@ def test_table_calls_refuse(mala, args):
     assert tables(lens=at(0)) == -1 and tables(left=at(4)) == -1 and tables(cu=at(0)) == -1 and tables(cu=at(1)) == -1 and tables(lens=at(1)) == -1
     assert tables(B=0) == -1 and tables(mp=0) == -1 and tables(ps=0) == -1 and tables(np_=0) == -1 and tables(rows=-1) == -1
     assert tables(B=16385) == -2 and tables(ps=24) == -2 and tables(ps=4) == -2 and tables(ps=130) == -2 and tables(mp=1 << 28) == -2
+    assert tables(rows=(1 << 30) + 1) == -2 and tables(B=16384, mp=1 << 17, ps=8) == -2
 
     def release(B=2, mp=4, ps=16, np_=8, **kw):
         a = [kw.get(n, at(x)) for x, n in enumerate(("done", "seqlens", "table", "free", "count", "lens", "left"))]
@@ -175,12 +176,12 @@ def test_cache_writes_refuse(mala, args):
                                         kw.get("np", 4), kw.get("ps", 16), kw.get("d", 128), None)
     assert w(s=None) == -1 and w(rows=-1) == -1 and w(np=0) == -1 and w(ps=0) == -1 and w(d=0) == -1 and w(k=mala._TIn(None, 0, 256, 128)) == -1
     assert w(kp=mala._TOut(base, 0, 256, 128)) == -1
-    assert w(ps=24) == -2 and w(d=12) == -2 and w(d=264) == -2
+    assert w(ps=24) == -2 and w(d=12) == -2 and w(d=264) == -2 and w(rows=(1 << 30) + 1) == -2
     assert w(s=base + 4) == -3 and w(k=tin(off=8)) == -3 and w(k=tin(sn=130)) == -3 and w(kp=tout(off=8)) == -3
     assert w(rows=0) == 0 and w(rows=0, s=None) == 0           # (nothing to do, also without a GPU)
     z = lambda **kw: L.mala_cache_write_fp8(tin(), tin(), base, kw.get("kp", tout()), tout(), kw.get("ks", base), kw.get("vs", base), kw.get("rows", 4),   # noqa: E731
                                             2, 4, kw.get("ps", 16), kw.get("d", 128), None)
-    assert z(ks=None) == -1 and z(vs=None) == -1 and z(ps=8) == -2 and z(d=24) == -2 and z(d=144) == -2
+    assert z(ks=None) == -1 and z(vs=None) == -1 and z(ps=8) == -2 and z(d=24) == -2 and z(d=144) == -2 and z(rows=(1 << 30) + 1) == -2
     assert z(ks=base + 2) == -3 and z(kp=mala._TOut(base, 1024, 264, 128)) == -3
     assert z(rows=0) == 0
 
