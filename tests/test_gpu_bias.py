@@ -352,6 +352,31 @@ def test_captured_on_a_side_stream(mala):
         assert (out[2].float() - want[2].float()).abs().max() <= 2 * U * want[2].float().abs().max()   # (dQ: reductions in any order)
 
 
+def test_two_streams_at_once(mala):
+    """The same calls with different tables and inputs on two streams, many in flight on each: what each returns alone."""
+    sets = [_inputs(81, 1, 4, 2, 700, 700, 64, 32), _inputs(91, 2, 4, 4, 260, 900, 128, 16)]
+    args = [(0.125, 0.0), (0.09, 1e-4)]
+
+    def run(i):
+        q, k, v, do, table = sets[i]
+        bias = mala.RelativeBias(table, bidirectional=bool(i))
+        o, lse, _ = mala.fwd_bias(q, k, v, bias, *args[i])
+        return (o, lse) + mala.bwd_bias(q, k, v, o, do, lse, bias, *args[i])[1:4]
+    want = [run(0), run(1)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(10):
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(run(i))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for one in got[i]:
+            assert all(torch.equal(x, y) for x, y in zip(one, want[i]))
+
+
 def _paged(seed, lens, page, Hkv, d):
     per = [-(-n // page) for n in lens]
     pool = sum(per) + 3

@@ -117,6 +117,30 @@ def test_slots_beyond_32_bits(mala):
     assert slots.tolist() == want and lens.item() == 2500 and left.item() == 2
 
 
+def test_pages_beyond_32_bits(mala):
+    """Pages of which the last ones begin behind 2^32 bytes, in a call that writes the first and the last one, bf16 and e4m3."""
+    for item, ps, Hkv, d in ((2, 128, 8, 128), (1, 128, 8, 128)):
+        num = (1 << 32) // (ps * Hkv * d * item) + 3
+        pages = [torch.empty((num, ps, Hkv, d), dtype=torch.bfloat16 if item == 2 else torch.float8_e4m3fn, device="cuda") for _ in range(2)]
+        slots = torch.cat([torch.arange(ps), torch.arange(ps) + (num - 1) * ps]).cuda()
+        g = torch.Generator(device="cuda").manual_seed(7)
+        k, v = (torch.randn((2 * ps, Hkv, d), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+        if item == 2:
+            mala.cache_write(k, v, slots, *pages)
+            for x, p in zip((k, v), pages):
+                assert torch.equal(p[0], x[:ps]) and torch.equal(p[-1], x[ps:])
+        else:
+            scales = [torch.zeros((num, Hkv, 1), device="cuda") for _ in range(2)]
+            mala.cache_write_fp8(k, v, slots, *pages, *scales)
+            for x, p, s in zip((k, v), pages, scales):
+                for at, rows in ((0, x[:ps]), (num - 1, x[ps:])):
+                    want = rows.abs().amax((0, 2)).float() / torch.full((Hkv,), 448., device="cuda")
+                    assert torch.equal(s[at, :, 0], want)
+                    err = (p[at].float() * want[:, None] - rows.float()).abs()
+                    assert (err <= 2.0 ** -4 * rows.float().abs() + 2.0 ** -10 * want[:, None] * 1.01).all()
+        del pages
+
+
 def _slots(B, longest, most, ps, seed, num_extra=3):
     r = random.Random(seed)
     lens = [r.randint(0, longest) for _ in range(B)]
