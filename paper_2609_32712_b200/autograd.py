@@ -10,6 +10,7 @@ import math
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import mala
 
@@ -59,6 +60,7 @@ class _MalaAttentionBias(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do):
         q, k, v, table, o, lse = ctx.saved_tensors
         max_distance, bidirectional, tau, scale, causal = ctx.args
@@ -80,6 +82,7 @@ class _MalaAttentionBiasPacked(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do):
         q, k, v, table, o, lse, cu_q, cu_k = ctx.saved_tensors
         max_q, max_k, max_distance, bidirectional, tau, scale, causal = ctx.args
@@ -117,7 +120,9 @@ def mala_attention_bias(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table
                         causal: bool = True) -> torch.Tensor:
     """``mala_attention`` with a learned relative position bias: ``table`` bf16 [num_buckets, Hq], added to the scaled scores by
     the bucket of key position - query position (see ``mala_rel_bias`` in ``include/mala.h``; the queries are the last Nq of
-    the Nk positions).  Differentiable with respect to q, k, v and the table."""
+    the Nk positions).  Differentiable with respect to q, k, v and the table (once).  To
+    capture the backward pass in a CUDA graph, let no other autograd graph of the same leaves be alive: torch adds up their
+    gradients on the stream on which that one was built, outside the capture."""
     if scale is None:
         scale = 1.0 / math.sqrt(q.shape[-1])
     return _MalaAttentionBias.apply(q, k, v, table, int(max_distance), bool(bidirectional), float(tau), float(scale), bool(causal))

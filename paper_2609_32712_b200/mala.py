@@ -591,6 +591,14 @@ class RelativeBias:
         return ctypes.byref(self.c)
 
 
+def _here(*ts) -> int:
+    """The current stream of the current device, on which all of ts have to lie (a kernel given another one's memory faults)."""
+    dev = torch.cuda.current_device()
+    for t in ts:
+        assert t is None or t.get_device() == dev, "expects tensors on the current device"
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(dev)
+
+
 def bias_workspace_bytes(op: int, B: int, Hq: int, Hkv: int, Nq: int, Nk: int, d: int, bias: RelativeBias, total_q: int = 0,
                          num_splits: int = 0) -> int:
     return int(lib().mala_bias_workspace_bytes(op, B, Hq, Hkv, Nq, Nk, total_q, d, num_splits, bias.num_buckets,
@@ -603,14 +611,16 @@ def fwd_bias(q, k, v, bias: RelativeBias, scale: float, tau: float, causal: bool
     the Nk positions.  Returns (o [B,Nq,Hq,d] bf16, lse [B,Hq,Nq] fp32, Stats or None)."""
     B, Nq, Hq, d = q.shape
     Nk, Hkv = k.shape[1], k.shape[2]
+    assert k.shape == v.shape == (B, Nk, Hkv, d)
     o = torch.empty_like(q) if out is None else out
     lse = q.new_empty((B, Hq, Nq), dtype=_F32) if lse is None else lse
     Tq, Tk = -(-(Nq + ((Nk - Nq) % 128 if causal else 0)) // 128), -(-Nk // 128)
+    assert o.shape == q.shape and lse.dtype is _F32 and lse.shape == (B, Hq, Nq) and lse.is_contiguous()
     st = Stats((B, Hq, Tq), -(-Tk // 32), q.device) if stats else None
     ws = _ws(bias_workspace_bytes(OP_FWD, B, Hq, Hkv, Nq, Nk, d, bias), q.device) if ws is None else ws
     rc = lib().mala_fwd_bias(_view(q, _TIn), _view(k, _TIn), _view(v, _TIn), bias._for(q), _view(o, _TOut), lse.data_ptr(),
                              ctypes.byref(st.c) if st else None, B, Hq, Hkv, Nq, Nk, d, int(causal), scale, tau,
-                             ws.data_ptr(), ws.numel(), _stream())
+                             ws.data_ptr(), ws.numel(), _here(q, k, v, o, lse, ws))
     if rc != 0:
         raise MalaError(rc, "mala_fwd_bias")
     return o, lse, st
@@ -621,17 +631,20 @@ def bwd_bias(q, k, v, o, do, lse, bias: RelativeBias, scale: float, tau: float, 
     """mala_bwd_bias: returns (dq, dk, dv, dtable bf16 [num_buckets, Hq], Stats or None)."""
     B, Nq, Hq, d = q.shape
     Nk, Hkv = k.shape[1], k.shape[2]
+    assert k.shape == v.shape == (B, Nk, Hkv, d) and q.shape == o.shape == do.shape
+    assert lse.dtype is _F32 and lse.shape == (B, Hq, Nq) and lse.is_contiguous()
     dq = torch.empty_like(q) if dq is None else dq
     dk = torch.empty_like(k) if dk is None else dk
     dv = torch.empty_like(v) if dv is None else dv
     dtable = q.new_empty((bias.num_buckets, Hq))
+    assert dq.shape == q.shape and dk.shape == dv.shape == k.shape
     Tq, Tk = -(-(Nq + ((Nk - Nq) % 128 if causal and Nk >= Nq else 0)) // 128), -(-Nk // 128)
     st = Stats((B, Hq, Tk), -(-Tq // 32), q.device) if stats else None
     ws = _ws(bias_workspace_bytes(OP_BWD, B, Hq, Hkv, Nq, Nk, d, bias), q.device) if ws is None else ws
     rc = lib().mala_bwd_bias(_view(q, _TIn), _view(k, _TIn), _view(v, _TIn), _view(o, _TIn), _view(do, _TIn), lse.data_ptr(),
                              bias._for(q), _view(dq, _TOut), _view(dk, _TOut), _view(dv, _TOut), dtable.data_ptr(), Hq,
                              ctypes.byref(st.c) if st else None, B, Hq, Hkv, Nq, Nk, d, int(causal), scale, tau,
-                             ws.data_ptr(), ws.numel(), _stream())
+                             ws.data_ptr(), ws.numel(), _here(q, k, v, o, do, lse, dq, dk, dv, ws))
     if rc != 0:
         raise MalaError(rc, "mala_bwd_bias")
     return dq, dk, dv, dtable, st
@@ -643,6 +656,7 @@ def fwd_varlen_bias(q, k, v, cu_seqlens_q, cu_seqlens_k, max_seqlen_q: int, max_
     device; the same tensor twice for self attention).  Returns (o, lse [Hq,total_q], Stats or None)."""
     one, total_q, Hq, d = q.shape
     total_k, Hkv = k.shape[1], k.shape[2]
+    assert k.shape == v.shape == (1, total_k, Hkv, d)
     for cu in (cu_seqlens_q, cu_seqlens_k):
         assert one == 1 and cu.dtype == torch.int32 and cu.is_contiguous()
     B = cu_seqlens_q.numel() - 1
@@ -655,7 +669,8 @@ def fwd_varlen_bias(q, k, v, cu_seqlens_q, cu_seqlens_k, max_seqlen_q: int, max_
     rc = lib().mala_fwd_varlen_bias(_view(q, _TIn), _view(k, _TIn), _view(v, _TIn), cu_seqlens_q.data_ptr(),
                                     cu_seqlens_k.data_ptr(), bias._for(q), _view(o, _TOut), lse.data_ptr(),
                                     ctypes.byref(st.c) if st else None, B, Hq, Hkv, total_q, total_k, max_seqlen_q,
-                                    max_seqlen_k, d, int(causal), scale, tau, ws.data_ptr(), ws.numel(), _stream())
+                                    max_seqlen_k, d, int(causal), scale, tau, ws.data_ptr(), ws.numel(),
+                                    _here(q, k, v, cu_seqlens_q, cu_seqlens_k, ws))
     if rc != 0:
         raise MalaError(rc, "mala_fwd_varlen_bias")
     return o, lse, st
@@ -667,6 +682,8 @@ def bwd_varlen_bias(q, k, v, o, do, lse, cu_seqlens_q, cu_seqlens_k, max_seqlen_
     None)."""
     one, total_q, Hq, d = q.shape
     total_k, Hkv = k.shape[1], k.shape[2]
+    assert k.shape == v.shape == (1, total_k, Hkv, d) and q.shape == o.shape == do.shape
+    assert lse.dtype is _F32 and lse.shape == (Hq, total_q) and lse.is_contiguous()
     for cu in (cu_seqlens_q, cu_seqlens_k):
         assert one == 1 and cu.dtype == torch.int32 and cu.is_contiguous()
     B = cu_seqlens_q.numel() - 1
@@ -680,7 +697,8 @@ def bwd_varlen_bias(q, k, v, o, do, lse, cu_seqlens_q, cu_seqlens_k, max_seqlen_
                                     lse.data_ptr(), cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(), bias._for(q),
                                     _view(dq, _TOut), _view(dk, _TOut), _view(dv, _TOut), dtable.data_ptr(), Hq,
                                     ctypes.byref(st.c) if st else None, B, Hq, Hkv, total_q, total_k, max_seqlen_q,
-                                    max_seqlen_k, d, int(causal), scale, tau, ws.data_ptr(), ws.numel(), _stream())
+                                    max_seqlen_k, d, int(causal), scale, tau, ws.data_ptr(), ws.numel(),
+                                    _here(q, k, v, o, do, lse, cu_seqlens_q, cu_seqlens_k, ws))
     if rc != 0:
         raise MalaError(rc, "mala_bwd_varlen_bias")
     return dq, dk, dv, dtable, st
@@ -693,9 +711,11 @@ def decode_paged_bias(q, kpages, vpages, block_table, seqlens, bias: RelativeBia
     num_pages, page_size, Hkv = kpages.shape[0], kpages.shape[1], kpages.shape[2]
     assert block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.shape[0] == B
     assert seqlens is None or (seqlens.dtype == torch.int32 and seqlens.is_contiguous() and seqlens.shape == (B,))
+    assert kpages.shape == vpages.shape and kpages.shape[3] == d
     max_pages = block_table.shape[1]
     Nk = max_pages * page_size
     o = torch.empty_like(q) if out is None else out
+    assert o.shape == q.shape
     lse = q.new_empty((B, Hq) if Sq == 1 else (B, Sq, Hq), dtype=_F32) if want_lse else None
     tps = -(-(-(-Nk // num_splits)) // 128)
     st = Stats((B, Hkv, num_splits), -(-tps // 32), q.device) if stats else None
@@ -705,7 +725,7 @@ def decode_paged_bias(q, kpages, vpages, block_table, seqlens, bias: RelativeBia
                                       seqlens.data_ptr() if seqlens is not None else None, bias._for(q), _view(o, _TOut),
                                       lse.data_ptr() if lse is not None else None, ctypes.byref(st.c) if st else None,
                                       B, Hq, Hkv, num_pages, page_size, max_pages, Sq, d, scale, tau, num_splits,
-                                      ws.data_ptr(), ws.numel(), _stream())
+                                      ws.data_ptr(), ws.numel(), _here(q, kpages, vpages, block_table, seqlens, o, ws))
     if rc != 0:
         raise MalaError(rc, "mala_decode_paged_bias")
     return o, lse, st
@@ -723,12 +743,13 @@ def page_tables(seqlens, new_tokens, block_table, free_pages, free_count, page_s
     slots int64 [rows], free_count int32 [1])."""
     _ints(seqlens, new_tokens, block_table, free_pages, free_count)
     B, max_pages = block_table.shape
-    assert seqlens.shape == (B,) and new_tokens.shape == (B,)
+    assert seqlens.shape == (B,) and new_tokens.shape == (B,) and free_count.shape == (1,)
     cu, lens, left = seqlens.new_empty(B + 1), seqlens.new_empty(B), seqlens.new_empty(1)
     slots = seqlens.new_empty(rows, dtype=torch.int64)
     rc = lib().mala_page_tables(seqlens.data_ptr(), new_tokens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
                                 free_count.data_ptr(), cu.data_ptr(), lens.data_ptr(), slots.data_ptr(), left.data_ptr(), B,
-                                max_pages, page_size, free_pages.numel(), rows, _stream())
+                                max_pages, page_size, free_pages.numel(), rows,
+                                _here(seqlens, new_tokens, block_table, free_pages, free_count))
     if rc != 0:
         raise MalaError(rc, "mala_page_tables")
     return cu, lens, slots, left
@@ -739,11 +760,12 @@ def release_pages(done, seqlens, block_table, free_pages, free_count, page_size:
     place).  Returns (seqlens int32 [B], free_count int32 [1])."""
     _ints(seqlens, block_table, free_pages, free_count)
     B, max_pages = block_table.shape
-    assert seqlens.shape == (B,) and done.shape == (B,) and done.element_size() == 1 and done.is_contiguous()
+    assert seqlens.shape == (B,) and free_count.shape == (1,) and done.shape == (B,)
+    assert done.element_size() == 1 and done.is_contiguous()
     lens, left = seqlens.new_empty(B), seqlens.new_empty(1)
     rc = lib().mala_release_pages(done.data_ptr(), seqlens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
                                   free_count.data_ptr(), lens.data_ptr(), left.data_ptr(), B, max_pages, page_size,
-                                  free_pages.numel(), _stream())
+                                  free_pages.numel(), _here(done, seqlens, block_table, free_pages, free_count))
     if rc != 0:
         raise MalaError(rc, "mala_release_pages")
     return lens, left
@@ -763,7 +785,7 @@ def cache_write(k, v, slots, kpages, vpages) -> None:
     num_pages, page_size = kpages.shape[0], kpages.shape[1]
     assert kpages.shape == vpages.shape and kpages.shape[2:] == (Hkv, d)
     rc = lib().mala_cache_write(_rows(k), _rows(v), slots.data_ptr(), _view(kpages, _TOut), _view(vpages, _TOut), rows, Hkv,
-                                num_pages, page_size, d, _stream())
+                                num_pages, page_size, d, _here(k, v, slots, kpages, vpages))
     if rc != 0:
         raise MalaError(rc, "mala_cache_write")
 
@@ -780,6 +802,6 @@ def cache_write_fp8(k, v, slots, kpages8, vpages8, kscale, vscale) -> None:
     kp, vp = _view8(kpages8), _view8(vpages8)
     rc = lib().mala_cache_write_fp8(_rows(k), _rows(v), slots.data_ptr(), _TOut(kp.p, kp.sb, kp.sn, kp.sh),
                                     _TOut(vp.p, vp.sb, vp.sn, vp.sh), kscale.data_ptr(), vscale.data_ptr(), rows, Hkv, num_pages,
-                                    page_size, d, _stream())
+                                    page_size, d, _here(k, v, slots, kpages8, vpages8, kscale, vscale))
     if rc != 0:
         raise MalaError(rc, "mala_cache_write_fp8")

@@ -196,3 +196,16 @@ def test_python_checks(mala):
         mala.page_tables(i.long(), i, torch.zeros(4, 2, dtype=torch.int32), i, i[:1], 16, 4)
     with pytest.raises(AssertionError):
         mala.cache_write(torch.zeros(4, 2, 64, dtype=torch.bfloat16), torch.zeros(4, 2, 64, dtype=torch.bfloat16), i, None, None)
+    b16 = lambda *n: torch.zeros(n, dtype=torch.bfloat16)   # noqa: E731
+    q, k, bias = b16(1, 4, 2, 64), b16(1, 6, 2, 64), mala.RelativeBias(b16(32, 2))
+    lse = torch.zeros(1, 2, 4)
+    for bad in (lambda: mala.fwd_bias(q, k, k[:, :5], bias, 0.1, 0.0), lambda: mala.fwd_bias(q, k, k, bias, 0.1, 0.0, lse=lse[:, :, :3]),
+                lambda: mala.fwd_bias(q, k, k, bias, 0.1, 0.0, out=q[:, :3]), lambda: mala.bwd_bias(q, k, k, q, q[:, :3], lse, bias, 0.1, 0.0),
+                lambda: mala.bwd_bias(q, k, k, q, q, lse.double(), bias, 0.1, 0.0), lambda: mala.bwd_bias(q, k, k, q, q, lse, bias, 0.1, 0.0, dk=q),
+                lambda: mala.fwd_varlen_bias(q, k, k[:, :3], i[:2], i[:2], 4, 6, bias, 0.1, 0.0),
+                lambda: mala.bwd_varlen_bias(q, k, k, q, q, lse, i[:2], i[:2], 4, 6, bias, 0.1, 0.0),
+                lambda: mala.decode_paged_bias(q, b16(3, 16, 2, 64), b16(2, 16, 2, 64), i[:2].view(1, 2), i[:1], bias, 0.1, 0.0, 2),
+                lambda: mala.page_tables(i, i, torch.zeros(4, 2, dtype=torch.int32), i, i[:0], 16, 4),
+                lambda: mala.release_pages(i > 0, i, torch.zeros(4, 2, dtype=torch.int32), i, i[:2], 16)):
+        with pytest.raises(AssertionError):
+            bad()

@@ -377,6 +377,25 @@ def test_two_streams_at_once(mala):
             assert all(torch.equal(x, y) for x, y in zip(one, want[i]))
 
 
+def test_a_second_derivative_is_refused(mala):
+    from paper_2609_32712_b200.autograd import mala_attention_bias
+    q, k, v, _, table = (t.requires_grad_() for t in _inputs(97, 1, 2, 2, 20, 20, 64, 32))
+    (dq,) = torch.autograd.grad(mala_attention_bias(q, k, v, table, 0.0).float().square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError):
+        dq.float().sum().backward()
+
+
+def test_tensors_elsewhere_are_refused(mala):
+    q, k, v, do, table = _inputs(95, 1, 2, 2, 20, 20, 64, 32)
+    for x, y in ((q, k.cpu()), (q.cpu(), k)):
+        with pytest.raises(AssertionError):
+            mala.fwd_bias(x, y, v, mala.RelativeBias(table), 0.125, 0.0)
+    with pytest.raises(AssertionError):
+        mala.fwd_bias(q, k, v, mala.RelativeBias(table.cpu()), 0.125, 0.0)
+    with pytest.raises(AssertionError):
+        mala.cache_write(k[0], v[0], torch.arange(20), k.view(1, 20, 2, 64)[:, :16], v[:, :16])
+
+
 def _paged(seed, lens, page, Hkv, d):
     per = [-(-n // page) for n in lens]
     pool = sum(per) + 3
