@@ -260,8 +260,8 @@ __device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
 // A team of kThreads threads writes one unit: 16 threads per row in 16-byte copies, first the largest magnitude, then the codes.
 // The rows wait in shared memory between the two (a block's team: all of a unit; a warp's: a share of that at a time), each
 // thread's in places of its own, so that they are read once.  With many rows (35000 of 8 x 128: 3 bytes per element are 33 us at
-// the copy rate, this kernel takes 47) blocks of two warps: what a warp does once per unit -- where it lies, its maximum, its scale -- weighs as much
-// as 1000 of its elements (eight warps: 67 us; with the rows in registers, three blocks per SM: 129).  Few rows are bound
+// the copy rate, this kernel takes 45) blocks of two warps: what a warp does once per unit -- where it lies, its maximum, its scale --
+// weighs as much as 1000 of its elements (eight warps: 67 us; with the rows in registers, three blocks per SM: 129).  Few rows are bound
 // by the chain slots -> rows -> scale -> codes, and get blocks of eight warps.
 __device__ __forceinline__ void copy16_async(uint4* to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
@@ -375,6 +375,11 @@ cache_write8_kernel(const WriteParams p) {
   const int h = blockIdx.y, t0 = blockIdx.x * p.chunk, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __shared__ float red[2][kWarps];
   __shared__ uint32_t ends_s[8], valid_s[8];
+  // The chunk's rows set out for L2 while their slots are looked at (between them the blocks fetch every row once; 35000 rows 45 us,
+  // without it 47).
+  for (int x = threadIdx.x; x < 2 * p.chunk; x += kBlock)
+    if (t0 + x / 2 < p.rows && x % 2 * 8 < p.cols)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"((is_v ? p.v : p.k) + (int64_t)(t0 + x / 2) * (is_v ? p.v_sn : p.k_sn) + h * (is_v ? p.v_sh : p.k_sh) + x % 2 * 128));
   // Rows at which something begins or has no place, among the chunk's (at most 64) and as many behind them as a unit has: a bit each,
   // and a bit for those with a place; a unit begins at a row with both and reaches up to the next one with the first.
   for (int w = warp; w < (p.chunk + p.unit + 31) / 32; w += kWarps) {   // (at most six words)
