@@ -260,7 +260,7 @@ __device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
 // A team of kThreads threads writes one unit: 16 threads per row in 16-byte copies, first the largest magnitude, then the codes.
 // The rows wait in shared memory between the two (a block's team: all of a unit; a warp's: a share of that at a time), each
 // thread's in places of its own, so that they are read once.  With many rows (35000 of 8 x 128: 3 bytes per element are 33 us at
-// the copy rate, this kernel takes 45) blocks of two warps: what a warp does once per unit -- where it lies, its maximum, its scale --
+// the copy rate, this kernel takes 39-43 at pages of 128 to 16 keys) blocks of two warps: what a warp does once per unit -- where it lies, its maximum, its scale --
 // weighs as much as 1000 of its elements (eight warps: 67 us; with the rows in registers, three blocks per SM: 129).  Few rows are bound
 // by the chain slots -> rows -> scale -> codes, and get blocks of eight warps.
 __device__ __forceinline__ void copy16_async(uint4* to, const void* from) {
@@ -268,11 +268,12 @@ __device__ __forceinline__ void copy16_async(uint4* to, const void* from) {
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-template <int kThreads, int kBuffer>
+// kRow threads per row (8 where a row has at most as many 16-byte pieces, else 16); kBatch rows fit the team's part of the buffer
+template <int kThreads, int kRow, int kBatch>
 __device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int h, int t, int n, int64_t slot, uint4* buf, float* red) {
-  constexpr int kRows = kThreads / 16;
-  const int tid = threadIdx.x & (kThreads - 1), lane = threadIdx.x & 31, r0 = tid >> 4, c = tid & 15;
-  const int batch = kBuffer == kThreads ? p.unit : p.unit * kThreads / kBuffer;   // rows that its part of the buffer holds
+  constexpr int kRows = kThreads / kRow;
+  static_assert(kBatch % kRows == 0, "a thread's places are its own");
+  const int tid = threadIdx.x & (kThreads - 1), lane = threadIdx.x & 31, r0 = tid / kRow, c = tid % kRow;
   const bool mine = c < p.cols;
   const int64_t s_sn = is_v ? p.v_sn : p.k_sn, s_sh = is_v ? p.v_sh : p.k_sh, d_sn = is_v ? p.vp_sn : p.kp_sn, d_sh = is_v ? p.vp_sh : p.kp_sh;
   const int64_t page = p.limit <= 0xffffffffll ? (int64_t)p.by_page.div((uint32_t)slot) : slot / p.page_size, at = slot - page * p.page_size;
@@ -283,17 +284,17 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int
   buf += tid;
   auto load = [&](const uint8_t* from, uint4* to, int first) {
     if (mine)
-      for (int r = first + r0, end = min(first + batch, n); r < end; r += kRows, to += kThreads, from += kRows * s_sn) copy16_async(to, from);
+      for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, to += kThreads, from += kRows * s_sn) copy16_async(to, from);
   };
   load(src, buf, 0);
   const float old = *(volatile const float*)sp;   // (before the store below, which a cached load need not be)
   uint32_t top2 = 0;                     // largest magnitudes of the even and the odd columns (bf16 magnitudes are ordered like their bits)
-  for (int first = 0; first < n; first += batch) {
+  for (int first = 0; first < n; first += kBatch) {
     if (first > 0) load(src + (int64_t)first * s_sn, buf, first);
     copies_wait();
     const uint4* from = buf;
     if (mine)
-      for (int r = first + r0, end = min(first + batch, n); r < end; r += kRows, from += kThreads) {
+      for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, from += kThreads) {
         const uint4 w = *from;
         top2 = max_u16x2(max_u16x2(top2, w.x & 0x7fff7fffu), w.y & 0x7fff7fffu);
         top2 = max_u16x2(max_u16x2(top2, w.z & 0x7fff7fffu), w.w & 0x7fff7fffu);
@@ -327,15 +328,15 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int
     return e4m3x2(qa, qb);
   };
   auto signs = [&](uint32_t codes, uint32_t high) -> uint32_t { return (codes & 0x7f7f7f7fu) | (high & 0x80808080u); };
-  for (int first = 0; first < n; first += batch) {
-    if (n > batch) {
+  for (int first = 0; first < n; first += kBatch) {
+    if (n > kBatch) {
       load(src + (int64_t)first * s_sn, buf, first);
       copies_wait();
     }
     const uint4* from = buf;
     uint8_t* to = dst + first * d_sn;
     if (mine)
-      for (int r = first + r0, end = min(first + batch, n); r < end; r += kRows, from += kThreads, to += kRows * d_sn) {
+      for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, from += kThreads, to += kRows * d_sn) {
         const uint4 w = *from;
         auto four = [&](uint32_t u, uint32_t v) -> uint32_t {
           const uint32_t q = codes2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)) |
@@ -366,17 +367,17 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int
   }
 }
 
-template <int kBlock>
-__global__ void __launch_bounds__(kBlock, kBlock == 64 ? 14 : 4)
+template <int kBlock, int kRow>
+__global__ void __launch_bounds__(kBlock, kBlock == 64 ? 13 : kBlock == 128 ? 6 : 4)
 cache_write8_kernel(const WriteParams p) {
-  extern __shared__ __align__(16) uint4 rows_s[];       // 256 bytes per key of a unit
-  constexpr int kWarps = kBlock / 32;
+  constexpr int kWarps = kBlock / 32, kAll = (kBlock == 64 ? 1024 : 2048) / kRow, kShare = kAll / kWarps;   // rows (all of a unit), a warp's
+  __shared__ __align__(16) uint4 rows_s[kAll * kRow];
   const bool is_v = blockIdx.z != 0;
   const int h = blockIdx.y, t0 = blockIdx.x * p.chunk, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __shared__ float red[2][kWarps];
   __shared__ uint32_t ends_s[8], valid_s[8];
-  // The chunk's rows set out for L2 while their slots are looked at (between them the blocks fetch every row once; 35000 rows 45 us,
-  // without it 47).
+  // The chunk's rows set out for L2 while their slots are looked at (between them the blocks fetch every row once; 35000 rows 45 us instead
+  // of 47 in an earlier form).
   for (int x = threadIdx.x; x < 2 * p.chunk; x += kBlock)
     if (t0 + x / 2 < p.rows && x % 2 * 8 < p.cols)
       asm volatile("prefetch.global.L2 [%0];" ::"l"((is_v ? p.v : p.k) + (int64_t)(t0 + x / 2) * (is_v ? p.v_sn : p.k_sn) + h * (is_v ? p.v_sh : p.k_sh) + x % 2 * 128));
@@ -399,7 +400,7 @@ cache_write8_kernel(const WriteParams p) {
   if (p.chunk > 32) begins |= (uint64_t)(ends_s[1] & valid_s[1]) << 32;
   else if (p.chunk < 32) begins &= (1u << p.chunk) - 1u;
   // few units: the whole block takes one after the other; many, which are short: a warp each
-  const bool few = __popcll(begins) <= (kBlock == 64 ? 2 : 1);
+  const bool few = __popcll(begins) <= (kBlock == 256 ? 1 : 2);
   for (int i = 0; begins; begins &= begins - 1, ++i) {
     const int x = __ffsll((long long)begins) - 1;
     if (!few && i % kWarps != warp) continue;
@@ -412,8 +413,8 @@ cache_write8_kernel(const WriteParams p) {
       end = (end | 31) + 1;
     }
     end = min(end, last);
-    if (few) write8_unit<kBlock, kBlock>(p, is_v, h, t0 + x, end - x, at, rows_s, red[i & 1]);
-    else write8_unit<32, kBlock>(p, is_v, h, t0 + x, end - x, at, rows_s + warp * (p.unit * 16 / kWarps), nullptr);
+    if (few) write8_unit<kBlock, kRow, kAll>(p, is_v, h, t0 + x, end - x, at, rows_s, red[i & 1]);
+    else write8_unit<32, kRow, kShare>(p, is_v, h, t0 + x, end - x, at, rows_s + warp * (kShare * kRow), nullptr);
   }
 }
 
@@ -540,14 +541,17 @@ int mala_cache_write_fp8(mala_tin k, mala_tin v, const int64_t* slots, mala_tout
   MALA_TRY(current_device_checked(&dev));
   MALA_TRY(device_setup(dev, &status));
   // Blocks of eight warps and of so few rows that all blocks run at once (four per SM); where that would take more than eight rows
-  // each, 64 rows per block of two warps (so that few blocks find nothing to do)
+  // each, 64 rows per block of two warps (so that few blocks find nothing to do), or of four where a unit takes 32 KB
   while (w.chunk < 16 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 4ll * sm_count(dev)) w.chunk *= 2;
-  const bool many = w.chunk == 16;
+  const bool many = w.chunk == 16, narrow = w.cols <= 8;
   if (many) w.chunk = 64;
   const dim3 grid((unsigned)((rows + w.chunk - 1) / w.chunk), Hkv, 2);
-  const size_t smem = (size_t)w.unit * 256;
-  if (many) cache_write8_kernel<64><<<grid, 64, smem, (cudaStream_t)cuda_stream>>>(w);
-  else cache_write8_kernel<256><<<grid, 256, smem, (cudaStream_t)cuda_stream>>>(w);
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  if (!many && narrow) cache_write8_kernel<256, 8><<<grid, 256, 0, stream>>>(w);
+  else if (!many) cache_write8_kernel<256, 16><<<grid, 256, 0, stream>>>(w);
+  else if (narrow) cache_write8_kernel<64, 8><<<grid, 64, 0, stream>>>(w);
+  else if (w.unit < 128) cache_write8_kernel<64, 16><<<grid, 64, 0, stream>>>(w);
+  else cache_write8_kernel<128, 16><<<grid, 128, 0, stream>>>(w);
   return scope.finish(cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA);
 }
 
