@@ -260,8 +260,8 @@ __device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
 // A team of kThreads threads writes one unit: 16 threads per row in 16-byte copies, first the largest magnitude, then the codes.
 // The rows wait in shared memory between the two (a block's team: all of a unit; a warp's: a share of that at a time), each
 // thread's in places of its own, so that they are read once.  With many rows (35000 of 8 x 128: 3 bytes per element are 33 us at
-// the copy rate, this kernel takes 39-43 at pages of 128 to 16 keys) blocks of two warps: what a warp does once per unit -- where it lies, its maximum, its scale --
-// weighs as much as 1000 of its elements (eight warps: 67 us; with the rows in registers, three blocks per SM: 129).  Few rows are bound
+// the copy rate, this kernel takes 39-43 at pages of 128 to 16 keys) blocks of two warps: what a warp does once per unit -- where it
+// lies, its maximum, its scale -- weighs as much as 1000 of its elements (eight warps: 67 us; with the rows in registers, three blocks per SM: 129).  Few rows are bound
 // by the chain slots -> rows -> scale -> codes, and get blocks of eight warps.
 __device__ __forceinline__ void copy16_async(uint4* to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
@@ -541,10 +541,12 @@ int mala_cache_write_fp8(mala_tin k, mala_tin v, const int64_t* slots, mala_tout
   MALA_TRY(current_device_checked(&dev));
   MALA_TRY(device_setup(dev, &status));
   // Blocks of eight warps and of so few rows that all blocks run at once (four per SM); where that would take more than eight rows
-  // each, 64 rows per block of two warps (so that few blocks find nothing to do), or of four where a unit takes 32 KB
+  // each, blocks of two warps, or of four where a unit takes 32 KB, and of 64 rows (so that few blocks find nothing to do) or fewer while
+  // they run at once (16 requests of up to 40 rows, pages of 16 keys: 5.8 us, with 64 rows per block 11.0)
   while (w.chunk < 16 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 4ll * sm_count(dev)) w.chunk *= 2;
   const bool many = w.chunk == 16, narrow = w.cols <= 8;
-  if (many) w.chunk = 64;
+  if (many)
+    while (w.chunk < 64 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 8ll * sm_count(dev)) w.chunk *= 2;
   const dim3 grid((unsigned)((rows + w.chunk - 1) / w.chunk), Hkv, 2);
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   if (!many && narrow) cache_write8_kernel<256, 8><<<grid, 256, 0, stream>>>(w);
