@@ -29,7 +29,7 @@ bias_expand_kernel(const __nv_bfloat16* __restrict__ table, int64_t sb, const __
     const float v = bias_log2(table + (int64_t)b * sb + h);
     nan = nan || v != v || v == INFINITY;
     top = fmaxf(top, v);
-    if (v > -INFINITY) low = fminf(low, v);
+    low = fminf(low, v);               // (-inf too: how far a masked key's score lies above the others has no bound)
   }
 #pragma unroll
   for (int m = 16; m > 0; m >>= 1) {

@@ -43,9 +43,10 @@ constexpr float kBiasLimit = 2e38f, kBiasFloor = -3e38f;
 // The dense kernels take a tile that is not far by factors: exp2(s + b - m) = exp2(s + top - m) * exp2(b - top), with top the
 // head's largest bias.  m then only has to be no smaller than the scores are, so the row maximum needs no bias, and the factors
 // are read and multiplied beside the exponentials, which are bound by the exponential unit, not before them, where the
-// whole chain of the tile waits.  exp2(b - top) is as small as the head's values are apart: up to 2^-60 that costs no
-// precision (fp32 sums, bf16 P); heads with more, or with a NaN, have it added.  The kernels with the skip test add: Eq. 3
-// needs the rows' true maxima.
+// whole chain of the tile waits.  exp2(b - top) is as small as the head's values are apart, and m lies above the row's true
+// maximum by no more than that: up to 2^-60 it costs no precision (fp32 sums, bf16 P).  Heads with more have it added, and heads
+// with a NaN or a -inf: a masked key's score would count in m, as far above the visible ones as it may be.  The kernels with the
+// skip test add: Eq. 3 needs the rows' true maxima.
 constexpr float kBiasRange = 60.f;
 
 struct RelBiasView {

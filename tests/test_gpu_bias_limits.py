@@ -1,0 +1,80 @@
+"""GPU parity of the calls with a relative position bias at the borders of what they allow: masked keys whose scores lie far above the
+visible ones, values that swallow the scores, buckets that begin just above a whole number, gradients far below their neighbours'."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import bias_reference as R
+from tests import parity
+from tests.test_gpu_bias import U, _check, _inputs, _paged, _randn
+
+pytestmark = pytest.mark.gpu
+S_ABS = parity.LSE_ABS   # scores in fp32 and their log-sum-exp: the limit of the other calls' tests, for each of the two
+
+
+@pytest.fixture(scope="module")
+def mala():
+    from paper_2609_32712_b200 import mala as m
+    m.lib()
+    return m
+
+
+def _reference(q, k, v, do, table, scale, nb, md, bidir, causal):
+    """One head in 64 bits with the error bounds of its results.  P carries the scores' and the normalizer's error (2 S_ABS, relative)
+    and, as an operand, a rounding to bf16; D comes from the bf16 output; every result is rounded once."""
+    r = R.head(*(t.double() for t in (q, k, v, table, do)), scale, nb, md, bidir, causal)
+    p, _ = R.softmax_rows(r["x"])
+    do, k, q, v = (t.double() for t in (do, k, q, v))
+    e_o = (U * (r["o"].abs() + r["a"]) * 1.02 + 2 * S_ABS * r["a"]) + 1e-5
+    dp = do @ v.T
+    off = (dp - (r["o"] * do).sum(-1, keepdim=True)).abs()
+    e_ds = p * off * (U + 4 * S_ABS) + p * (e_o * do.abs()).sum(-1, keepdim=True) * 1.02
+    sums = lambda t: torch.stack([(t * (r["bk"] == b)).sum() for b in range(nb)])  # noqa: E731
+    err = dict(o=e_o, dq=e_ds @ k.abs() * scale, dk=e_ds.T @ q.abs() * scale, dv=(p * (U + 4 * S_ABS)).T @ do.abs(), dtable=sums(e_ds))
+    for n in ("dq", "dk", "dv", "dtable"):
+        err[n] = err[n] * 1.02 + U * r[n].abs() + 1e-5
+    return r, err
+
+
+@pytest.mark.parametrize("causal,bidir", [(True, False), (False, True)])
+@pytest.mark.parametrize("B,H,N,packed", [(1, 2, 300, False), (2, 16, 1300, False), (1, 2, 900, True), (1, 32, 2000, True)])
+def test_a_masked_key_far_above_the_others(mala, B, H, N, packed, causal, bidir):
+    """Bucket 0 is masked and q = k without a scale: a query's own key, which it does not see, scores about 128 nats, the others 11 or
+    so.  One query block per CTA and two, dense and packed."""
+    d, nb, md, scale = 128, 32, 128, 1.0
+    q, _, v, do, table = _inputs(3 + N + causal, B, H, H, N, N, d, nb)
+    k = q.clone()
+    table = (table.float() * 0.5).to(torch.bfloat16)
+    table[0] = -math.inf
+    bias = mala.RelativeBias(table, md, bidir)
+    if packed:
+        ends = [0, N // 3, N // 3 + 1, N]
+        cu = torch.tensor(ends, dtype=torch.int32, device="cuda")
+        args = (cu, cu, N - N // 3 - 1, N - N // 3 - 1, bias, scale, 0.0)
+        o, lse, _ = mala.fwd_varlen_bias(q, k, v, *args, causal=causal)
+        dq, dk, dv, dtable, _ = mala.bwd_varlen_bias(q, k, v, o, do, lse, *args, causal=causal)
+        lse = lse[None]
+        parts = [(0, slice(a, b)) for a, b in zip(ends, ends[1:])]
+    else:
+        o, lse, _ = mala.fwd_bias(q, k, v, bias, scale, 0.0, causal=causal)
+        dq, dk, dv, dtable, _ = mala.bwd_bias(q, k, v, o, do, lse, bias, scale, 0.0, causal=causal)
+        parts = [(b, slice(0, N)) for b in range(B)]
+    torch.cuda.synchronize()
+    assert mala.device_status() == 0
+    for h in sorted({0, H // 2, H - 1}):
+        dt = de = 0
+        above = 0
+        for b, s in parts:
+            r, err = _reference(q[b, s, h], k[b, s, h], v[b, s, h], do[b, s, h], table[:, h], scale, nb, md, bidir, causal)
+            above += int((q[b, s, h].double().square().sum(-1) - r["x"].max(-1).values > 90).sum())
+            _check(o[b, s, h], r["o"], err["o"], f"o {b} {h}")
+            empty = torch.isinf(r["lse"])
+            assert torch.equal(torch.isinf(lse[b, h, s]), empty)
+            assert (lse[b, h, s].double() - r["lse"])[~empty].abs().amax().nan_to_num(0.0).item() <= S_ABS if (~empty).any() else True
+            for got, n in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
+                _check(got[b, s, h], r[n], err[n], f"{n} {b} {h}")
+            dt, de = dt + r["dtable"], de + err["dtable"]
+        assert above > 0                                   # (the input is what it is meant to be)
+        _check(dtable[:, h], dt, de, f"dtable {h}")
