@@ -751,8 +751,9 @@ static int decode_paged_impl(const ApiScope& scope, const mala_rel_bias* bias, m
   MALA_TRY(check_view(o.p, o.sb, Sq > 1 ? o.sn : 8, o.sh, B, Sq, Hq));
   if ((((uintptr_t)ws) & 255) != 0) return MALA_ERR_MISALIGNED;
   if (ws_bytes < decode_workspace_bytes(B * Sq, Hq, padded_head_size(d), num_splits)) return MALA_ERR_WORKSPACE_TOO_SMALL;
-  const size_t base = decode_workspace_bytes(B * Sq, Hq, padded_head_size(d), num_splits);   // (the bias by distance lies behind it)
-  if (bias) MALA_TRY(check_bias(bias, Hq, ws, ws_bytes - base));
+  // (behind it the partials' sums, and the bias by distance)
+  const size_t base = decode_workspace_bytes(B * Sq, Hq, padded_head_size(d), num_splits) + decode_sums_bytes(B * Sq, Hq, num_splits);
+  if (bias) MALA_TRY(check_bias(bias, Hq, ws, ws_bytes > base ? ws_bytes - base : 0));
   int dev = 0;
   MALA_TRY(current_device_checked(&dev));
   int* status = nullptr;
@@ -800,7 +801,8 @@ size_t mala_bias_workspace_bytes(int op, int B, int Hq, int Hkv, int Nq, int Nk,
   if (op == MALA_OP_BWD)
     return (total_q ? bwd_base_workspace_bytes(1, Hq, total_q + 384 * B, D) : bwd_base_workspace_bytes(B, Hq, Nq + 127, D)) + table +
            bias_part_bytes(B, Hq, (Nk + 127) / 128, num_buckets);
-  if (op == MALA_OP_DECODE) return num_splits > 0 ? decode_workspace_bytes(B * Nq, Hq, D, num_splits) + table : 0;
+  if (op == MALA_OP_DECODE)
+    return num_splits > 0 ? decode_workspace_bytes(B * Nq, Hq, D, num_splits) + decode_sums_bytes(B * Nq, Hq, num_splits) + table : 0;
   return 0;
 }
 

@@ -18,9 +18,12 @@ namespace mala {
 // 512 x 28) a step took 629 and 93.4 us (8 x 131072 keys; four tokens over 4 x 16389 keys), now 624 and 87.8.
 // Launched as a dependent of the split kernel: it may be resident before that kernel has finished and waits here (and reads
 // past the L1, which may hold lines from before).
-template <int D>
+// kSums (calls with a bias): lse_part holds the partials' references in the log2 domain and l_part their sums, lse_s =
+// (lse_part + log2 l_part) ln 2.  With values of a type's lowest among the biases a reference may be as low as -2e38, where adding
+// the logarithm would change nothing and all splits would weigh alike, however many keys they hold.
+template <int D, bool kSums = false>
 __global__ void __launch_bounds__(128)
-decode_merge_kernel(const float* __restrict__ o_part, const float* __restrict__ lse_part, __nv_bfloat16* __restrict__ o,
+decode_merge_kernel(const float* __restrict__ o_part, const float* __restrict__ lse_part, const float* __restrict__ l_part, __nv_bfloat16* __restrict__ o,
                     int64_t o_sb, int64_t o_sn, int64_t o_sh, float* __restrict__ lse_out, int Sq, int Hq,
                     int num_splits, int d) {   // d <= D: columns of o
   constexpr int L4 = D / 4;                      // float4 per partial: one or two per lane, or half a warp per partial
@@ -60,7 +63,9 @@ decode_merge_kernel(const float* __restrict__ o_part, const float* __restrict__ 
       }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const float f = ls[u] != -INFINITY ? exp2f((ls[u] - mx) * 1.4426950408889634f) : 0.f;
+      float f = 0.f;
+      if (ls[u] != -INFINITY)
+        f = kSums ? exp2f(ls[u] - mx) * __ldcg(l_part + (size_t)bh * num_splits + s0 + u * 4 * PER) : exp2f((ls[u] - mx) * 1.4426950408889634f);
       Z += f;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
@@ -86,7 +91,7 @@ decode_merge_kernel(const float* __restrict__ o_part, const float* __restrict__ 
     for (int x = 0; x < 4 * PER; ++x) t += sum[x][c];
     o[b * o_sb + tok * o_sn + h * o_sh + c] = __float2bfloat16(any ? t * inv : 0.f);
   }
-  if (lse_out && threadIdx.x == 0) lse_out[bh] = any ? mx + logf(Z) : -INFINITY;
+  if (lse_out && threadIdx.x == 0) lse_out[bh] = any ? (kSums ? mx * 0.6931471805599453f : mx) + logf(Z) : -INFINITY;
 }
 
 // The same for up to 32 splits, one warp per (b, token, query head) and eight of them per block.  With few splits the
@@ -94,9 +99,9 @@ decode_merge_kernel(const float* __restrict__ o_part, const float* __restrict__ 
 // and thousands of rows take many rounds of such blocks.  Here nothing crosses between warps, the log-normalizers are read
 // once (lane s: split s) and the first partials are requested along with them.  16416 rows of one split, 128 columns: 7.5 us
 // (12.6 MB of partials and outputs), 23 with the block above, 18 with a thread per column.
-template <int D>
+template <int D, bool kSums = false>
 __global__ void __launch_bounds__(256)
-decode_merge_few_kernel(const float* __restrict__ o_part, const float* __restrict__ lse_part, __nv_bfloat16* __restrict__ o,
+decode_merge_few_kernel(const float* __restrict__ o_part, const float* __restrict__ lse_part, const float* __restrict__ l_part, __nv_bfloat16* __restrict__ o,
                         int64_t o_sb, int64_t o_sn, int64_t o_sh, float* __restrict__ lse_out, int rows, int Sq, int Hq,
                         int num_splits, int d) {
   constexpr uint32_t kAll = 0xffffffffu;
@@ -107,6 +112,7 @@ decode_merge_few_kernel(const float* __restrict__ o_part, const float* __restric
   const float4* op = reinterpret_cast<const float4*>(o_part + (size_t)bh * num_splits * D) + col;
   wait_for_primary();
   const float ls = lane < num_splits ? __ldcg(lse_part + (size_t)bh * num_splits + lane) : -INFINITY;
+  const float sum = kSums && lane < num_splits ? __ldcg(l_part + (size_t)bh * num_splits + lane) : 0.f;
   float mx = 0.f, wt = 0.f, Z = 0.f;
   float4 acc[V];
 #pragma unroll
@@ -125,7 +131,7 @@ decode_merge_few_kernel(const float* __restrict__ o_part, const float* __restric
       mx = ls;
 #pragma unroll
       for (int m = 16; m > 0; m >>= 1) mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, m));
-      wt = ls != -INFINITY ? exp2f((ls - mx) * 1.4426950408889634f) : 0.f;
+      wt = ls == -INFINITY ? 0.f : kSums ? exp2f(ls - mx) * sum : exp2f((ls - mx) * 1.4426950408889634f);
       Z = wt;
 #pragma unroll
       for (int m = 16; m > 0; m >>= 1) Z += __shfl_xor_sync(kAll, Z, m);
@@ -154,23 +160,25 @@ decode_merge_few_kernel(const float* __restrict__ o_part, const float* __restric
       *reinterpret_cast<uint2*>(o + b * o_sb + tok * o_sn + h * o_sh + (v * 32 + col) * 4) =
           make_uint2(pack_bf16x2(acc[v].x * inv, acc[v].y * inv), pack_bf16x2(acc[v].z * inv, acc[v].w * inv));
   }
-  if (lse_out && lane == 0) lse_out[bh] = any ? mx + logf(Z) : -INFINITY;
+  if (lse_out && lane == 0) lse_out[bh] = any ? (kSums ? mx * 0.6931471805599453f : mx) + logf(Z) : -INFINITY;
 }
 
 // The merge as a programmatic dependent of the split kernel before it on the stream (which has let it go ahead): its
 // launch latency passes while the split kernel still runs.
 inline int launch_decode_merge(int D, int rows, const float* o_part, const float* lse_part, mala_tout o, int64_t o_sn,
-                               float* lse_opt, int Sq, int Hq, int num_splits, int d, cudaStream_t stream) {
+                               float* lse_opt, int Sq, int Hq, int num_splits, int d, cudaStream_t stream, const float* l_part = nullptr) {
   // Up to twelve splits (three rounds of four loads) a warp per row is the faster form at every number of rows; a step of
   // 128 / 4096 rows with one tile per split takes 7.9 / 16.3 us instead of 8.6 / 20.1 (one split), 12.2 / 101.9 instead
   // of 12.4 / 106.1 (twelve), 12.4 / 133.5 instead of 12.4 / 136.8 (sixteen) and 17.9 instead of 17.2 (32 splits, 128 rows).
   if (num_splits <= 12) {
     auto few = D == 256 ? decode_merge_few_kernel<256> : D == 128 ? decode_merge_few_kernel<128> : decode_merge_few_kernel<64>;
-    return launch_dependent(few, dim3((unsigned)((rows + 7) / 8)), dim3(256), stream, o_part, lse_part, (__nv_bfloat16*)o.p,
+    if (l_part) few = D == 128 ? decode_merge_few_kernel<128, true> : decode_merge_few_kernel<64, true>;
+    return launch_dependent(few, dim3((unsigned)((rows + 7) / 8)), dim3(256), stream, o_part, lse_part, l_part, (__nv_bfloat16*)o.p,
                             o.sb, o_sn, o.sh, lse_opt, rows, Sq, Hq, num_splits, d) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
   }
   auto kernel = D == 256 ? decode_merge_kernel<256> : D == 128 ? decode_merge_kernel<128> : decode_merge_kernel<64>;
-  return launch_dependent(kernel, dim3((unsigned)rows), dim3(128), stream, o_part, lse_part, (__nv_bfloat16*)o.p, o.sb, o_sn,
+  if (l_part) kernel = D == 128 ? decode_merge_kernel<128, true> : decode_merge_kernel<64, true>;
+  return launch_dependent(kernel, dim3((unsigned)rows), dim3(128), stream, o_part, lse_part, l_part, (__nv_bfloat16*)o.p, o.sb, o_sn,
                           o.sh, lse_opt, Sq, Hq, num_splits, d) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
@@ -180,6 +188,8 @@ inline size_t decode_align256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline size_t decode_workspace_bytes(int B, int Hq, int d, int S) {   // d: the padded head size
   return decode_align256((size_t)B * Hq * S * d * sizeof(float)) + decode_align256((size_t)B * Hq * S * sizeof(float));
 }
+// the partials' sums behind it (calls with a bias)
+inline size_t decode_sums_bytes(int B, int Hq, int S) { return decode_align256((size_t)B * Hq * S * sizeof(float)); }
 
 inline bool decode_set_attributes() {
   bool ok = true;
@@ -280,9 +290,10 @@ inline int decode_launch_with_scratch(mala_tin q, mala_tin kc, mala_tin vc, mala
   const int R = G * Sq;   // rows of a work item
   if (bias) {
     p.rb = *bias;
+    p.l_part = (float*)((uint8_t*)lse_part + decode_sums_bytes(B * Sq, Hq, num_splits));
     const int rc = bias_launch_decode(D, tau == 0.f, sched, R, grid, tq, tk, tv, p, stream);
     if (rc != MALA_OK) return rc;
-    return launch_decode_merge(D, B * Sq * Hq, o_part, lse_part, o, Sq > 1 ? o.sn : 0, lse_opt, Sq, Hq, num_splits, d, stream);
+    return launch_decode_merge(D, B * Sq * Hq, o_part, lse_part, o, Sq > 1 ? o.sn : 0, lse_opt, Sq, Hq, num_splits, d, stream, p.l_part);
   }
 #define MALA_DEC_LAUNCH3(DENSE, GP, MULTI, SCHED)                                                                           \
   {                                                                                                                  \

@@ -53,6 +53,7 @@ struct DecParams {
   FastDiv by_splits, by_hkv, by_tps;
   float scale_log2, log2_tau;
   RelBiasView rb;                // relative position bias (kernels with kBias)
+  float* l_part;                 // kBias: the partials' sums, beside their references in lse_part (see decode_merge_kernel)
 };
 
 // D: columns of the kernel (64, 128 or 256).  With 256 a K / V tile is 64 KB (four panels), the rings hold two K
@@ -863,7 +864,8 @@ mala_decode_split_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         }
         if (r == 0) {
 #pragma unroll
-          for (int q = 0; q < GH; ++q) m_ref[q] = kMulti ? fmaxf(tmax[q], -1e30f) : tmax[q];   // (finite also for a row that sees no key yet)
+          for (int q = 0; q < GH; ++q)   // (finite also for a row that sees no key yet, and below all that a bias can make of a score)
+            m_ref[q] = kMulti ? fmaxf(tmax[q], kBias ? kBiasFloor : -1e30f) : tmax[q];
         } else {
           float alpha[GH];
           bool resc = false;
@@ -961,8 +963,14 @@ mala_decode_split_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
       for (int q = 0; q < GH; ++q) pend_l[q] = l[q];
 #pragma unroll
       for (int q = 0; q < GH; ++q)
-        if (rb + q < R && kt == q)
-          p.lse_part[prow0 + rowoff[q]] = (!kMulti || l[q] > 0.f) ? (m_ref[q] + lgl[q]) * 0.6931471805599453f : -INFINITY;
+        if (rb + q < R && kt == q) {
+          if constexpr (kBias) {   // (reference and sum apart: beside a type's lowest value the sum's logarithm would vanish)
+            p.lse_part[prow0 + rowoff[q]] = l[q] > 0.f ? m_ref[q] : -INFINITY;
+            p.l_part[prow0 + rowoff[q]] = l[q];
+          } else {
+            p.lse_part[prow0 + rowoff[q]] = (!kMulti || l[q] > 0.f) ? (m_ref[q] + lgl[q]) * 0.6931471805599453f : -INFINITY;
+          }
+        }
       if (head) {
         if (bm_row && bm_word >= 0) bm_row[bm_word] = bm_bits;
         if (p.retained) p.retained[stat_row] = (uint32_t)r;

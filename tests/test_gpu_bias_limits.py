@@ -78,3 +78,54 @@ def test_a_masked_key_far_above_the_others(mala, B, H, N, packed, causal, bidir)
             dt, de = dt + r["dtable"], de + err["dtable"]
         assert above > 0                                   # (the input is what it is meant to be)
         _check(dtable[:, h], dt, de, f"dtable {h}")
+
+
+@pytest.mark.parametrize("tau", [0.0, 1e-4])
+@pytest.mark.parametrize("Sq,Hq,Hkv,d,page", [(1, 2, 1, 64, 16), (3, 8, 2, 128, 128), (1, 8, 8, 96, 64), (2, 16, 2, 128, 32)])
+@pytest.mark.parametrize("case", ["masked near", "masked far", "only far", "lowest near", "lowest far", "lowest everywhere"])
+@pytest.mark.parametrize("splits", [1, 3, 14])
+def test_decode_with_masked_buckets(mala, case, splits, Sq, Hq, Hkv, d, page, tau):
+    """As in a prompt: -inf masks a bucket's keys, also all of a split or of a row; a type's lowest value does too, but a row of nothing
+    else weighs its keys alike, however they are divided among the splits."""
+    lens, nb, md = [1, 5, 150, 700, 1999], 16, 200
+    kp, vp, bt, sl = _paged(7, lens, page, Hkv, d)
+    q, table = _randn(8, len(lens), Sq, Hq, d), _randn(9, nb, Hq)
+    low = torch.finfo(torch.bfloat16).min
+    if case == "masked near":
+        table[:5] = -math.inf            # (the first two requests see nothing)
+    elif case == "masked far":
+        table[nb - 1] = -math.inf        # (the last request's older splits see nothing)
+    elif case == "only far":
+        table[:nb - 1] = -math.inf
+    elif case == "lowest near":
+        table[:nb - 1] = low             # (the shortest requests have no other)
+    elif case == "lowest far":
+        table[nb - 2:] = low
+    else:
+        table[:] = low
+    scale = 1 / math.sqrt(d)
+    o, lse, _ = mala.decode_paged_bias(q, kp, vp, bt, sl, mala.RelativeBias(table, md), scale, tau, splits)
+    torch.cuda.synchronize()
+    assert mala.device_status() == 0
+    lse = lse.view(len(lens), Sq, Hq)
+    for b, n in enumerate(lens):
+        idx = bt[b, :-(-n // page)].long()
+        k, v = (t[idx].reshape(-1, Hkv, d)[:n].double() for t in (kp, vp))
+        for s in range(Sq):
+            seen = n - Sq + s + 1
+            for h in range(0, Hq, max(1, Hq // 4)):
+                if seen <= 0:
+                    assert (o[b, s, h] == 0).all() and lse[b, s, h] == -math.inf
+                    continue
+                g = h // (Hq // Hkv)
+                r = R.head(q[b, s, h:h + 1].double(), k[:seen, g], v[:seen, g], table[:, h].double(), None, scale, nb, md, False, True)
+                want = float(r["lse"][0])
+                if 1e6 < -want < math.inf:       # (the normalizer's logarithm is below 2^-53 of such a bias: the weights without it)
+                    w = torch.softmax(r["x"], -1)
+                    r.update(o=w @ v[:seen, g], a=w @ v[:seen, g].abs())
+                # (tau: a skipped tile's mass is at most tau of the row's, Proposition 1; a row of lowest values has no tile below another)
+                _check(o[b, s, h], r["o"][0], (U + 2 * tau) * (r["o"][0].abs() + r["a"][0]) * 1.02 + 1e-5 + 2 * tau * float(v.abs().max()), f"o {b} {s} {h}")
+                if abs(want) < 1e6:
+                    assert abs(float(lse[b, s, h]) - want) <= S_ABS + 2 * tau
+                else:
+                    assert float(lse[b, s, h]) == want if math.isinf(want) else -math.inf < float(lse[b, s, h]) < -1e38
