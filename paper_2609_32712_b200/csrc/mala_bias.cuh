@@ -23,15 +23,14 @@
 // the first line's pair.
 #pragma once
 #include <cuda_bf16.h>
-#include <math.h>
 #include <stdint.h>
 
 #include "../../include/mala.h"
+#include "mala_bias_starts.h"
 #include "sm100_ptx.cuh"
 
 namespace mala {
 
-constexpr int kBiasMaxBuckets = 128, kBiasMaxDistance = 1 << 16;
 // Entries beyond `reach` on either side, so that a tile that is not flat needs no clamping: it has a delta in
 // (-reach, reach) and spans 254 more.
 constexpr int kBiasPad = 256;
@@ -122,31 +121,6 @@ __device__ __forceinline__ void bias_add(uint32_t (&s)[N], float c, const float4
     s[4 * e] = __float_as_uint(x0); s[4 * e + 1] = __float_as_uint(x1);
     s[4 * e + 2] = __float_as_uint(x2); s[4 * e + 3] = __float_as_uint(x3);
   }
-}
-
-// The distances at which the buckets e + 1 .. h - 1 of a side begin.
-struct BiasStarts {
-  int first[kBiasMaxBuckets];
-  int count, exact, side;    // `side`: h where the keys after the query have buckets of their own, else 0
-  int reach;
-};
-
-// (On the host.)  A start that is a whole number is one exactly: the double result is within 1e-11 of it.
-inline bool bias_starts(int num_buckets, int max_distance, int bidirectional, BiasStarts* s) {
-  const int h = bidirectional ? num_buckets / 2 : num_buckets;
-  if (num_buckets < 2 || num_buckets > kBiasMaxBuckets || (bidirectional && num_buckets % 2) || h < 2) return false;
-  const int e = h / 2;
-  if (max_distance <= e || max_distance > kBiasMaxDistance) return false;
-  s->exact = e;
-  s->side = bidirectional ? h : 0;
-  s->count = h - e - 1;
-  const double step = log((double)max_distance / e) / (h - e);
-  for (int j = 1; j < h - e; ++j) {
-    const double x = e * exp(j * step), r = nearbyint(x);
-    s->first[j - 1] = (int)(fabs(x - r) < 1e-9 * x ? r : ceil(x));
-  }
-  s->reach = s->count > 0 ? s->first[s->count - 1] : e;
-  return true;
 }
 
 inline size_t bias_align256(size_t x) { return (x + 255) & ~(size_t)255; }

@@ -3,6 +3,7 @@ GPU tests compare with is pinned (buckets, softmax, gradients by differences), a
 import ctypes
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -209,3 +210,46 @@ def test_python_checks(mala):
                 lambda: mala.release_pages(i > 0, i, torch.zeros(4, 2, dtype=torch.int32), i, i[:2], 16)):
         with pytest.raises(AssertionError):
             bad()
+
+
+# ---- where the buckets begin, as the kernels have it
+
+def test_starts_of_the_buckets(tmp_path):
+    """The library's own function against whole-number powers: every number of buckets with the distances up to 1500 and a spread of larger
+    ones, and pairs where a bucket begins less than 1e-9 above a whole number."""
+    import os
+    import subprocess
+    here = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_32712_b200", "csrc")
+    src = tmp_path / "starts.cpp"
+    src.write_text('#include "mala_bias_starts.h"\nextern "C" int starts(int nb, int md, int bidir, int* out) { mala::BiasStarts s; if '
+                   '(!mala::bias_starts(nb, md, bidir, &s)) return -1; for (int i = 0; i < s.count; ++i) out[i] = s.first[i]; out[s.count] = s.reach; '
+                   'return s.count; }\n')
+    so = tmp_path / "starts.so"
+    subprocess.check_call(["g++", "-O2", "-shared", "-fPIC", f"-I{here}", str(src), "-o", str(so)])
+    f = ctypes.CDLL(str(so)).starts
+    out = (ctypes.c_int * 129)()
+
+    def check(nb, md, bidir):
+        e, h, want = R.bucket_starts(nb, md, bidir)
+        assert f(nb, md, int(bidir), out) == len(want)
+        assert list(out[:len(want)]) == want, (nb, md, bidir)
+        assert out[len(want)] == (want[-1] if want else e)
+    named = [(73, 905), (64, 21228), (32, 43921)]
+    for nb, md in named:
+        check(nb, md, False)
+    for nb in range(2, 129):
+        e = nb // 2
+        dists = np.concatenate([np.arange(e + 1, 1501), np.unique(np.geomspace(1501, 65536, 60).astype(int)), [2 ** x for x in range(11, 17)]])
+        w = nb - e
+        x = e * np.exp(np.arange(1, w)[:, None] * np.log(dists / e) / w)
+        near = (np.abs(x - np.rint(x)) < 1e-8 * x).any(0)      # (elsewhere the ceiling is beyond doubt)
+        assert f(nb, 65536, 0, out) == w - 1
+        for md, c, is_near in zip(dists.tolist(), np.ceil(x).T.astype(int).tolist(), near.tolist()):
+            if is_near:
+                check(nb, md, False)
+            else:
+                assert f(nb, md, 0, out) == w - 1 and list(out[:w - 1]) == c, (nb, md)
+    for nb, md in ((4, 2), (32, 128), (24, 768), (128, 65536), (128, 40)):
+        check(nb, md, True)
+    for bad in ((1, 128, 0), (129, 128, 0), (33, 128, 1), (2, 128, 1), (32, 16, 0), (32, 65537, 0), (32, 0, 0)):
+        assert f(*bad, out) == -1

@@ -129,3 +129,22 @@ def test_decode_with_masked_buckets(mala, case, splits, Sq, Hq, Hkv, d, page, ta
                     assert abs(float(lse[b, s, h]) - want) <= S_ABS + 2 * tau
                 else:
                     assert float(lse[b, s, h]) == want if math.isinf(want) else -math.inf < float(lse[b, s, h]) < -1e38
+
+
+@pytest.mark.parametrize("nb,md,n", [(73, 905, 347), (64, 21228, 9423), (32, 43921, 16325)])
+def test_buckets_that_begin_just_above_a_whole_number(mala, nb, md, n):
+    """Distance n lies below the start of a bucket by less than 1e-9 of itself.  q = 0 and neighbouring values 8 apart: the output is the
+    weight of that one key, which the wrong bucket changes by e^8."""
+    starts = R.bucket_starts(nb, md, False)[2]
+    assert n + 1 in starts and n not in starts
+    table = (torch.arange(nb, device="cuda") % 2 * 8 - 4).to(torch.bfloat16)[:, None].contiguous()
+    table[0] = -4
+    for at in (n - 1, n, n + 1):
+        k = _randn(1, 1, at + 1, 1, 64)
+        x, bk = R.scores(torch.zeros((1, 64), dtype=torch.float64, device="cuda"), k[0, :, 0].double(), table[:, 0].double(), 1.0, nb, md, False, True)
+        v = torch.zeros_like(k)
+        v[0, 0] = 1.0                      # (the key at distance `at`)
+        o, _, _ = mala.fwd_bias(torch.zeros_like(k[:, :1]), k, v, mala.RelativeBias(table, md), 1.0, 0.0)
+        p, _ = R.softmax_rows(x)
+        want = float(p[0, 0])
+        assert abs(float(o[0, 0, 0, 0]) / want - 1) <= 3 * U, at     # (two roundings to bf16; the wrong bucket: e^8)
