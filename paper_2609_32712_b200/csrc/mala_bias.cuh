@@ -38,6 +38,10 @@ constexpr int kBiasPad = 256;
 // a row of nothing but lowest values would be empty).  Rows whose keys all carry -inf start from kBiasFloor, so that
 // their exponentials are 0 and not NaN, and end as (0, -inf).
 constexpr float kBiasLimit = 2e38f, kBiasFloor = -3e38f;
+// The backward has P from lse, whose half step in fp32 is an error of |lse| 2^-24 in nats (and as much again in the log2 domain): 2^-3
+// at this limit.  Beyond it lie rows that see nothing but keys biased as far as that, up to values beside which lse says nothing of their number
+// (a row of lowest values has P = 1 for each of its keys from it); they get no gradient.
+constexpr float kBiasMaxLse = 1048576.f;
 
 // The dense kernels take a tile that is not far by factors: exp2(s + b - m) = exp2(s + top - m) * exp2(b - top), with top the
 // head's largest bias.  m then only has to be no smaller than the scores are, so the row maximum needs no bias, and the factors

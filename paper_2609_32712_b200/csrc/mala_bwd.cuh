@@ -1028,7 +1028,7 @@ bwd_preprocess_kernel(const __nv_bfloat16* __restrict__ o, int64_t o_sb, int64_t
                       const float* __restrict__ lse, float* __restrict__ lse2, float* __restrict__ bq,
                       float* __restrict__ Dq, float* __restrict__ acc, int N, int Np, int Nk, int d, int causal,
                       float log2_tau, const int* __restrict__ cu, int total_rows, int qshift,
-                      const int* __restrict__ cu_k) {
+                      const int* __restrict__ cu_k, float lse_limit) {
   release_dependents();
   const int h = blockIdx.y, Hq = gridDim.y, p0 = blockIdx.x * 32;   // p0: first entry of the head's (sequence's) padded rows
   int b = blockIdx.z, row0 = 0, prow0 = 0;
@@ -1077,7 +1077,7 @@ bwd_preprocess_kernel(const __nv_bfloat16* __restrict__ o, int64_t o_sb, int64_t
     if ((threadIdx.x & 15) == 0) {
       const int r = r0 + x * 16, row = p0 + r - qshift;
       const bool real = row >= 0 && row < N;
-      const float l2 = ls[x] == -INFINITY ? INFINITY : ls[x] * 1.4426950408889634f;   // (a row without a key: P = 0)
+      const float l2 = fabsf(ls[x]) >= lse_limit ? INFINITY : ls[x] * 1.4426950408889634f;   // (a row without a key, see kBiasMaxLse: P = 0)
       const float L = causal ? (float)(row + 1 + (Nk - N)) : (float)Nk;   // visible keys
       lse2[w0 + r] = l2;
       bq[w0 + r] = real ? l2 + (log2_tau - log2f(L)) : INFINITY;
@@ -1293,12 +1293,12 @@ inline int bwd_launch(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin d
     if (bias) {   // (behind the kernel that lays the bias out, of which it needs nothing: the two run side by side)
       if (launch_dependent(pre, dim3(4 * T, Hq, B), dim3(256), stream, (const __nv_bfloat16*)o.p, o.sb, o.sn, o.sh,
                            (const __nv_bfloat16*)dout.p, dout.sb, dout.sn, dout.sh, lse, lse2, bq, Dq, acc, N, Np, Nk, d, causal,
-                           tau > 0.f ? log2f(tau) : -INFINITY, cu, total, qshift, cu_k) != cudaSuccess)
+                           tau > 0.f ? log2f(tau) : -INFINITY, cu, total, qshift, cu_k, kBiasMaxLse) != cudaSuccess)
         return MALA_ERR_CUDA;
     } else {
       pre<<<dim3(4 * T, Hq, B), 256, 0, stream>>>((const __nv_bfloat16*)o.p, o.sb, o.sn, o.sh, (const __nv_bfloat16*)dout.p, dout.sb,
                                       dout.sn, dout.sh, lse, lse2, bq, Dq, acc, N, Np, Nk, d, causal,
-                                      tau > 0.f ? log2f(tau) : -INFINITY, cu, total, qshift, cu_k);
+                                      tau > 0.f ? log2f(tau) : -INFINITY, cu, total, qshift, cu_k, INFINITY);
       if (cudaGetLastError() != cudaSuccess) return MALA_ERR_CUDA;
     }
   }

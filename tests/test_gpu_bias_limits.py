@@ -148,3 +148,45 @@ def test_buckets_that_begin_just_above_a_whole_number(mala, nb, md, n):
         p, _ = R.softmax_rows(x)
         want = float(p[0, 0])
         assert abs(float(o[0, 0, 0, 0]) / want - 1) <= 3 * U, at     # (two roundings to bf16; the wrong bucket: e^8)
+
+
+@pytest.mark.parametrize("low", [-1e7, -1e9, -1.7e10, -1e20, -2e38, float(torch.finfo(torch.bfloat16).min)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_rows_whose_normalizer_has_swallowed_the_scores_get_no_gradient(mala, low, packed):
+    """The first rows see nothing but keys whose bias is so low that their lse in fp32 says nothing of the scores any more: no gradient,
+    and every other row's as if these were not there."""
+    N, d, nb, md, H = 700, 64, 16, 200, 2
+    q, k, v, do, table = _inputs(17, 1, H, H, N, N, d, nb)
+    table[0:3] = low
+    bias = mala.RelativeBias(table, md)
+    scale = 1 / math.sqrt(d)
+    if packed:
+        cu = torch.tensor([0, N], dtype=torch.int32, device="cuda")
+        o, lse, _ = mala.fwd_varlen_bias(q, k, v, cu, cu, N, N, bias, scale, 0.0)
+        dq, dk, dv, dtable, _ = mala.bwd_varlen_bias(q, k, v, o, do, lse, cu, cu, N, N, bias, scale, 0.0)
+    else:
+        o, lse, _ = mala.fwd_bias(q, k, v, bias, scale, 0.0)
+        dq, dk, dv, dtable, _ = mala.bwd_bias(q, k, v, o, do, lse, bias, scale, 0.0)
+    torch.cuda.synchronize()
+    assert mala.device_status() == 0
+    assert (dq[0, :3] == 0).all()
+    rest = do.clone()
+    rest[:, :3] = 0
+    for h in range(H):
+        r, err = _reference(q[0, :, h], k[0, :, h], v[0, :, h], rest[0, :, h], table[:, h], scale, nb, md, False, True)
+        for got, n in ((dq[0, :, h], "dq"), (dk[0, :, h], "dk"), (dv[0, :, h], "dv"), (dtable[:, h], "dtable")):
+            _check(got, r[n], err[n], f"{n} {h}")
+
+
+def test_rows_below_that_limit_keep_their_gradient(mala):
+    """A bias of -1e4 under all keys of the first rows: lse carries it with half a step of 2^-11, so P does to 2^-10."""
+    N, d, nb, md, H = 300, 64, 16, 200, 2
+    q, k, v, do, table = _inputs(18, 1, H, H, N, N, d, nb)
+    table[:] = -1e4
+    bias = mala.RelativeBias(table, md)
+    o, lse, _ = mala.fwd_bias(q, k, v, bias, 0.125, 0.0)
+    grads = mala.bwd_bias(q, k, v, o, do, lse, bias, 0.125, 0.0)
+    for h in range(H):
+        r, err = _reference(q[0, :, h], k[0, :, h], v[0, :, h], do[0, :, h], table[:, h], 0.125, nb, md, False, True)
+        for got, n in ((grads[0][0, :, h], "dq"), (grads[1][0, :, h], "dk"), (grads[2][0, :, h], "dv"), (grads[3][:, h], "dtable")):
+            _check(got, r[n], err[n], f"{n} {h}")
