@@ -809,19 +809,19 @@ mala_bwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           } else {
             // Sums of the 63 diagonals of this warp's 32 x 32 piece: in step e lane l takes the value of lane (l + e) % 32, which lies
             // on diagonal l, or, past the last lane, on diagonal l - 32.  (Not from the rounded dS: where one bucket has most of a
-            // row's mass its sum is what is left of far larger ones, and a rounding of 2^-9 in each then shows as 2^-8 in it.)
-            float on = 0.f, all = 0.f;
+            // row's mass its sum is what is left of far larger ones, and a rounding of 2^-9 in each then shows as 2^-8 in it.)  Each sum of its
+            // own terms alone: as the sum of both less the other one, a bucket whose keys weigh next to nothing kept the rounding of its
+            // neighbours' (a gradient of 1.6e-11 came out as 2.5e-12).
+            float on = 0.f, below = 0.f;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               float a, b_;
               f2_get(p2[e], a, b_);
               a = __shfl_sync(0xffffffffu, a, (lane + 2 * e) & 31);
               b_ = __shfl_sync(0xffffffffu, b_, (lane + 2 * e + 1) & 31);
-              all += a; all += b_;
-              if (lane + 2 * e < 32) on += a;
-              if (lane + 2 * e + 1 < 32) on += b_;
+              add_either(lane, 32 - 2 * e, on, below, a);
+              add_either(lane, 31 - 2 * e, on, below, b_);
             }
-            const float below = all - on;
             // ... and of the runs of diagonals that share a bucket (neighbours, since buckets are monotone along delta)
             const uint8_t* bk_at = bias_k[n & 3] + 127 - (int)lane_base + qt * 32 - lane;
 #pragma unroll

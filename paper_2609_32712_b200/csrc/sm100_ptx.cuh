@@ -382,6 +382,11 @@ __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+// x added to the first sum where i < n and to the second one elsewhere: one instruction under a predicate for each, no selections
+__device__ __forceinline__ void add_either(int i, int n, float& a, float& b, float x) {
+  asm("{\n\t.reg .pred p;\n\tsetp.lt.s32 p, %3, %4;\n\t@p add.rn.f32 %0, %0, %2;\n\t@!p add.rn.f32 %1, %1, %2;\n\t}"
+      : "+f"(a), "+f"(b) : "f"(x), "r"(i), "r"(n));
+}
 // bf16 pair of two fp32 values
 __device__ __forceinline__ uint32_t f2_bf16(uint64_t x) {
   float a, b;

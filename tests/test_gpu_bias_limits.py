@@ -190,3 +190,24 @@ def test_rows_below_that_limit_keep_their_gradient(mala):
         r, err = _reference(q[0, :, h], k[0, :, h], v[0, :, h], do[0, :, h], table[:, h], 0.125, nb, md, False, True)
         for got, n in ((grads[0][0, :, h], "dq"), (grads[1][0, :, h], "dk"), (grads[2][0, :, h], "dv"), (grads[3][:, h], "dtable")):
             _check(got, r[n], err[n], f"{n} {h}")
+
+
+@pytest.mark.parametrize("causal,bidir", [(True, False), (False, True)])
+def test_gradient_of_a_bucket_far_below_its_neighbours(mala, causal, bidir):
+    """Buckets whose keys weigh 2^-43 of the others': their gradient is a sum of their own terms alone, without what the neighbouring
+    diagonals' rounding leaves (2^-24 of far larger sums).  A row's incoming gradient is the value three keys before it, so that all
+    terms of bucket 3 have the same sign."""
+    N, d, nb, md, H = 600, 64, 32, 128, 2
+    q, k, v, do, table = _inputs(61, 1, H, H, N, N, d, nb)
+    low = 3
+    table[low] -= 30.0
+    do = v.roll(low, 1)
+    bias = mala.RelativeBias(table, md, bidir)
+    o, lse, _ = mala.fwd_bias(q, k, v, bias, 0.125, 0.0, causal=causal)
+    dtable = mala.bwd_bias(q, k, v, o, do, lse, bias, 0.125, 0.0, causal=causal)[3]
+    for h in range(H):
+        r, err = _reference(q[0, :, h], k[0, :, h], v[0, :, h], do[0, :, h], table[:, h], 0.125, nb, md, bidir, causal)
+        bound = err["dtable"] - 1e-5               # (nothing absolute: what is left is relative to the bucket's own terms)
+        want = float(r["dtable"][low])
+        assert 0 < want < 1e-8 and float(bound[low]) < 0.1 * want
+        assert abs(float(dtable[low, h]) - want) <= float(bound[low])
