@@ -15,6 +15,15 @@ from torch.autograd.function import once_differentiable
 from . import mala
 
 
+def _incoming(do: torch.Tensor) -> torch.Tensor:
+    """An incoming gradient as the kernels read it: autograd also hands over one row for all rows (a stride of 0, from a sum or a mean)
+    and slices of wider tensors, which are copied where a row does not begin on 16 bytes."""
+    s = do.stride()
+    if s[3] == 1 and do.data_ptr() % 16 == 0 and all(n == 1 or (x > 0 and x % 8 == 0) for n, x in zip(do.shape[:3], s)):
+        return do
+    return do.clone(memory_format=torch.contiguous_format)
+
+
 class _MalaAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, tau: float, scale: float, causal: bool):
@@ -26,8 +35,7 @@ class _MalaAttention(torch.autograd.Function):
     @staticmethod
     def backward(ctx, do):
         q, k, v, o, lse = ctx.saved_tensors
-        if do.stride(-1) != 1:
-            do = do.contiguous()
+        do = _incoming(do)
         dq, dk, dv, _ = mala.bwd_chunk(q, k, v, o, do, lse, ctx.scale, ctx.tau, causal=ctx.causal)
         return dq, dk, dv, None, None, None
 
@@ -44,8 +52,7 @@ class _MalaAttentionPacked(torch.autograd.Function):
     def backward(ctx, do):
         q, k, v, o, lse, cu_q, cu_k = ctx.saved_tensors
         max_q, max_k, scale, tau, causal = ctx.args
-        if do.stride(-1) != 1:
-            do = do.contiguous()
+        do = _incoming(do)
         dq, dk, dv, _ = mala.bwd_varlen_prefix(q, k, v, o, do, lse, cu_q, cu_k, max_q, max_k, scale, tau, causal=causal)
         return dq, dk, dv, None, None, None, None, None, None, None
 
@@ -64,8 +71,7 @@ class _MalaAttentionBias(torch.autograd.Function):
     def backward(ctx, do):
         q, k, v, table, o, lse = ctx.saved_tensors
         max_distance, bidirectional, tau, scale, causal = ctx.args
-        if do.stride(-1) != 1:
-            do = do.contiguous()
+        do = _incoming(do)
         dq, dk, dv, dtable, _ = mala.bwd_bias(q, k, v, o, do, lse, mala.RelativeBias(table, max_distance, bidirectional), scale,
                                               tau, causal=causal)
         return dq, dk, dv, dtable, None, None, None, None, None
@@ -86,8 +92,7 @@ class _MalaAttentionBiasPacked(torch.autograd.Function):
     def backward(ctx, do):
         q, k, v, table, o, lse, cu_q, cu_k = ctx.saved_tensors
         max_q, max_k, max_distance, bidirectional, tau, scale, causal = ctx.args
-        if do.stride(-1) != 1:
-            do = do.contiguous()
+        do = _incoming(do)
         dq, dk, dv, dtable, _ = mala.bwd_varlen_bias(q, k, v, o, do, lse, cu_q, cu_k, max_q, max_k,
                                                      mala.RelativeBias(table, max_distance, bidirectional), scale, tau, causal=causal)
         return dq, dk, dv, dtable, None, None, None, None, None, None, None, None, None

@@ -211,3 +211,26 @@ def test_gradient_of_a_bucket_far_below_its_neighbours(mala, causal, bidir):
         want = float(r["dtable"][low])
         assert 0 < want < 1e-8 and float(bound[low]) < 0.1 * want
         assert abs(float(dtable[low, h]) - want) <= float(bound[low])
+
+
+def test_gradients_of_a_mean_over_the_rows(mala):
+    """The incoming gradient of a pooled output is one row for all of them (a stride of 0), and one that starts off 16 bytes is a slice
+    of a wider one: the calls take both, with a bias and without."""
+    from paper_2609_32712_b200 import autograd as A
+    q, k, v, _, table = _inputs(81, 2, 4, 2, 200, 200, 64, 32)
+    w = _randn(82, 2, 4, 64)
+    wide = _randn(83, 2, 200, 4, 72)
+    cu = torch.tensor([0, 60, 200], dtype=torch.int32, device="cuda")
+    calls = [(lambda q, k, v, t: A.mala_attention_bias(q, k, v, t, 0.0), 2), (lambda q, k, v, t: A.mala_attention(q, k, v, 0.0), 2),
+             (lambda q, k, v, t: A.mala_attention_bias_packed(q, k, v, t, cu, cu, 140, 140, 0.0), 1),
+             (lambda q, k, v, t: A.mala_attention_packed(q, k, v, cu, cu, 140, 140, 0.0), 1)]
+    for f, B in calls:
+        for do in (w[:B, None].expand(B, 200, 4, 64), wide[:B, ..., 1:65]):
+            grads = []
+            for g in (do, do.contiguous()):
+                leaves = [t[:B].clone().requires_grad_(True) for t in (q, k, v)] + [table.clone().requires_grad_(True)]
+                f(*leaves).backward(g)
+                grads.append([t.grad for t in leaves])
+            for x, y in zip(grads[0][1:], grads[1][1:]):
+                assert (x is None and y is None) or torch.equal(x, y)
+            assert (grads[0][0].float() - grads[1][0].float()).abs().max() <= 2 * U * grads[1][0].float().abs().max()
