@@ -213,6 +213,52 @@ def test_gradient_of_a_bucket_far_below_its_neighbours(mala, causal, bidir):
         assert abs(float(dtable[low, h]) - want) <= float(bound[low])
 
 
+@pytest.mark.parametrize("tau", [1e-3, 0.3])
+@pytest.mark.parametrize("lq,lk,Hq,Hkv,d,causal", [([333, 0, 1, 517, 900], None, 4, 2, 64, True), ([200, 640, 7], [900, 700, 500], 2, 2, 128, True),
+                                                   ([130, 256, 400], [500, 130, 700], 2, 1, 64, False)])
+def test_packed_sequences_skip_tiles_like_single_ones(mala, lq, lk, Hq, Hkv, d, causal, tau):
+    """Packed, tau > 0: every sequence's masks, output and gradients are those of the call with that sequence alone (whose masks and
+    results are compared with the plain implementation elsewhere)."""
+    nb, md = 32, 600
+    lk = lq if lk is None else lk
+    q, k, v, do, table = _inputs(71, 1, Hq, Hkv, sum(lq), sum(lk), d, nb)
+    table = (table.float() - torch.arange(nb, device="cuda")[:, None] * 0.5).to(torch.bfloat16)
+    cu, ck = (torch.tensor([0] + list(np.cumsum(x)), dtype=torch.int32, device="cuda") for x in (lq, lk))
+    scale = 1 / math.sqrt(d)
+    bias = mala.RelativeBias(table, md)
+    mq, mk = max(lq), max(lk)
+    o, lse, fst = mala.fwd_varlen_bias(q, k, v, cu, ck, mq, mk, bias, scale, tau, causal=causal, stats=True)
+    dq, dk, dv, dtable, bst = mala.bwd_varlen_bias(q, k, v, o, do, lse, cu, ck, mq, mk, bias, scale, tau, causal=causal, stats=True)
+    torch.cuda.synchronize()
+    assert mala.device_status() == 0
+    Tk = -(-mk // 128)
+    fm, bm = fst.mask(Tk).cpu(), bst.mask(-(-(mq + 127) // 128)).cpu()
+    sums = torch.zeros((nb, Hq), dtype=torch.float64, device="cuda")
+    skipped = 0
+    for x, (n, m) in enumerate(zip(lq, lk)):
+        if n == 0:
+            continue
+        a, b = int(cu[x]), int(ck[x])
+        qs, ks, vs, ds = q[:, a:a + n], k[:, b:b + m], v[:, b:b + m], do[:, a:a + n]
+        o1, lse1, f1 = mala.fwd_bias(qs, ks, vs, bias, scale, tau, causal=causal, stats=True)
+        g1 = mala.bwd_bias(qs, ks, vs, o1, ds, lse1, bias, scale, tau, causal=causal, stats=True)
+        tq, tk = -(-(n + ((m - n) % 128 if causal else 0)) // 128), -(-m // 128)
+        one, back = f1.mask(tk).cpu(), g1[4].mask(tq).cpu()
+        assert torch.equal(fm[x, :, :tq, :tk], one[0]) and torch.equal(bm[x, :, :tk, :tq], back[0])
+        legal = sum(min(tk, i + 1 + (m - n) // 128) if causal else tk for i in range(tq)) * Hq
+        skipped += legal - int(one.sum())
+        assert torch.equal(o[:, a:a + n], o1) and torch.equal(lse[:, a:a + n], lse1[0])
+        assert torch.equal(dk[:, b:b + m], g1[1]) and torch.equal(dv[:, b:b + m], g1[2])
+        # (dQ: fp32 sums in any order, then one rounding, which may go either way)
+        assert (dq[:, a:a + n].float() - g1[0].float()).abs().max() <= 2 * U * g1[0].float().abs().max()
+        sums += g1[3].double()
+    # (the single calls' tables are rounded to bf16 one by one)
+    assert ((dtable.double() - sums).abs() <= 2 * U * len(lq) * sums.abs().max()).all()
+    # (the bias falls by 15.5 at most, and the largest of a tile's 16384 scores lies about 4 above the others: enough for
+    # ln(0.3 / L) = -8, not for ln(1e-3 / L) = -13.7 in sequences that end at 900 keys)
+    assert skipped > 0 or tau < 0.1
+
+
 def test_gradients_of_a_mean_over_the_rows(mala):
     """The incoming gradient of a pooled output is one row for all of them (a stride of 0), and one that starts off 16 bytes is a slice
     of a wider one: the calls take both, with a bias and without."""
