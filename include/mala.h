@@ -347,7 +347,8 @@ size_t mala_bias_workspace_bytes(int op, int B, int Hq, int Hkv, int Nq, int Nk,
  * row of block_table [B, max_pages_per_seq], and gets new_tokens[b] more (below 0: none).
  *   block_table     the new pages are entered behind the old ones; page number x that the step hands out, in the order of the
  *                   requests, is free_pages[free_count[0] - 1 - x]
- *   cu_seqlens      [B + 1] first row of each request among the step's new tokens (the sum of new_tokens below 2^31)
+ *   cu_seqlens      [B + 1] first row of each request among the step's new tokens (the sum of new_tokens below 2^31: with more,
+ *                   what the call gives has no meaning, but stays within its buffers)
  *   seqlens_out     [B] tokens that it holds afterwards
  *   slots           int64 [rows] for each new token page * page_size + place in the page; -1 in rows behind the last request
  *                   and for tokens without a place.  rows may be smaller or larger than the number of new tokens.

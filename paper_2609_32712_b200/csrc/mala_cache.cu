@@ -67,6 +67,8 @@ struct TableParams {
 };
 
 // kRelease: the pages of finished requests go behind the free ones, in their order.
+// The checks of table entries and pages in the loops below hold by themselves while the sums stay below 2^31; more rows than that, which
+// the host cannot see, leave slots and pages without meaning, but nothing outside the buffers is read or written.
 template <bool kRelease>
 __global__ void __launch_bounds__(kTableThreads)
 page_tables_kernel(const TableParams p) {
@@ -89,12 +91,13 @@ page_tables_kernel(const TableParams p) {
     bool fits = true;
     if (b < p.B) {
       len = (int)max(0ll, min(room, (long long)p.seqlens[b]));
+      const int held = (int)(((uint32_t)len + ps - 1) / ps);
       if (kRelease) {
-        need = p.done[b] ? (len + ps - 1) / ps : 0;
+        need = p.done[b] ? held : 0;
       } else {
         n = max(0, p.new_tokens[b]);
         fits = len + (long long)n <= room;
-        need = fits ? (int)(((long long)len + n + ps - 1) / ps) - (len + ps - 1) / ps : 0;
+        need = fits ? (int)(((long long)len + n + ps - 1) / ps) - held : 0;
       }
     }
     const uint64_t mine = ((uint64_t)need << 32) | (uint32_t)n;
@@ -137,7 +140,8 @@ page_tables_kernel(const TableParams p) {
     if (kRelease) {
       if (count + x < p.num_pages) p.free_pages[count + x] = p.block_table[row + (x - pages_at[b])];
     } else {
-      p.block_table[row + (int)p.by_page.div((uint32_t)lens[b] + ps - 1) + (x - pages_at[b])] = p.free_pages[count - 1 - x];
+      const int entry = (int)p.by_page.div((uint32_t)lens[b] + ps - 1) + (x - pages_at[b]);
+      if (entry < p.max_pages) p.block_table[row + entry] = p.free_pages[count - 1 - x];
     }
   }
   if (kRelease) return;
@@ -145,9 +149,11 @@ page_tables_kernel(const TableParams p) {
   auto slot_of = [&](int t, int lo, int hi) -> int64_t {   // row t, whose request is one of lo .. hi - 1
     const int b = find_last(rows_at, lo, hi, t);
     if ((refused[b >> 5] >> (b & 31)) & 1u) return -1;
-    const int len = lens[b], pos = len + (t - rows_at[b]), have = (int)p.by_page.div((uint32_t)len + ps - 1), x = (int)p.by_page.div((uint32_t)pos);
-    const int page = x < have ? p.block_table[(int64_t)b * p.max_pages + x] : p.free_pages[count - 1 - (pages_at[b] + x - have)];
-    return page >= 0 ? (int64_t)page * ps + (pos - x * ps) : -1;
+    const uint32_t len = (uint32_t)lens[b], pos = len + ((uint32_t)t - (uint32_t)rows_at[b]);
+    const uint32_t have = p.by_page.div(len + ps - 1), x = p.by_page.div(pos), given = (uint32_t)pages_at[b] + x - have;
+    if (x >= (uint32_t)p.max_pages || (x >= have && given >= (uint32_t)count)) return -1;
+    const int page = x < have ? p.block_table[(int64_t)b * p.max_pages + x] : p.free_pages[count - 1 - (int)given];
+    return page >= 0 ? (int64_t)page * ps + (pos - x * (uint32_t)ps) : -1;
   };
   if (p.rows <= step) {
     if (at < p.rows) p.slots[at] = at < total ? slot_of(at, 0, p.B) : -1;

@@ -345,3 +345,21 @@ def test_captured_step(mala):
         _, want = pool.add([1] * B)
         assert slots.tolist() == want and lens.tolist() == pool.lens and left.item() == len(pool.free)
         assert torch.equal(kp.view(-1, Hkv, d)[slots], k) and torch.equal(vp.view(-1, Hkv, d)[slots], v)
+
+
+@pytest.mark.parametrize("new", [[2 ** 31 - 1, 5, 2 ** 31 - 1, 9, 1], [2 ** 31 - 1] * 5, [2 ** 30 + 7] * 4 + [3], [3, 2 ** 31 - 2, 2 ** 31 - 1, 3, 3]])
+@pytest.mark.parametrize("rows", [40, 5000])
+def test_more_rows_than_32_bits_count_stay_within_the_buffers(mala, new, rows):
+    """The sum of new_tokens has to stay below 2^31.  Where it does not, table, list and slots are written nowhere else."""
+    ps, width, B, pages = 16, 2 ** 31 // 16 // 2 ** 20 * 2 ** 10, 5, 64      # (a table of rows of 131072 entries)
+    big = torch.full((B + 2, width), -3, dtype=torch.int32, device="cuda")
+    table = big[1:-1]
+    table[:, :3] = torch.arange(15, device="cuda", dtype=torch.int32).view(5, 3)
+    free = torch.arange(20, 20 + pages, dtype=torch.int32, device="cuda")
+    list_ = free.clone()
+    cu, lens, slots, left = mala.page_tables(_i32([40, 33, 48, 1, 20]), _i32(new), table, list_, _i32([30]), ps, rows)
+    torch.cuda.synchronize()
+    assert (big[0] == -3).all() and (big[-1] == -3).all() and torch.equal(free, list_)
+    given = table[:, 3:]
+    assert ((given == -3) | ((given >= 20) & (given < 50))).all()
+    assert (slots >= -1).all() and (slots < 50 * ps).all() and 0 <= left.item() <= 30
