@@ -377,7 +377,7 @@ int mala_cache_write(mala_tin k, mala_tin v, const int64_t* slots, mala_tout kpa
  * With m the largest magnitude among the unit's new rows of a head: a unit whose first key is among them gets the scale
  * m / 448 (1 where m is 0); in another one, which holds keys already, the scale s becomes max(s, m / 448), and where that is
  * larger the codes of the keys before the new ones are rounded again, e4m3(code * s_old / s_new).  New codes are
- * e4m3(x / s), rounded to nearest even.  Values must be finite.  The rows of a unit must be neighbours with ascending
+ * e4m3(x / s), rounded to nearest even.  Values must be finite.  The rows of a unit must be neighbours with consecutive
  * slots, as mala_page_tables gives them, and no other call may write to these units at the same time. */
 int mala_cache_write_fp8(mala_tin k, mala_tin v, const int64_t* slots, mala_tout kpages8, mala_tout vpages8, float* kscale,
                          float* vscale, int rows, int Hkv, int num_pages, int page_size, int d, void* cuda_stream);

@@ -794,13 +794,16 @@ size_t mala_bias_workspace_bytes(int op, int B, int Hq, int Hkv, int Nq, int Nk,
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Nq <= 0 || Nk <= 0 || total_q < 0 || !head_size_ok(d, 128) || num_buckets < 2 ||
       num_buckets > kBiasMaxBuckets || max_distance < 1 || max_distance > kBiasMaxDistance)
     return 0;
+  // (padded rows, and rows of a decode step, are counted in 32 bits)
+  const long long padded = op == MALA_OP_BWD ? (total_q ? total_q + 384LL * B : Nq + 254LL) : op == MALA_OP_DECODE ? (long long)B * Nq : 0;
+  if (padded + 127 > 0x7fffffffLL) return 0;
   const size_t table = bias_expand_bytes(Hq, max_distance);
   const int D = padded_head_size(d);
   if (op == MALA_OP_FWD) return table;
   // (a causal chunk that starts inside a tile has up to 127 more padded rows)
   if (op == MALA_OP_BWD)
     return (total_q ? bwd_base_workspace_bytes(1, Hq, total_q + 384 * B, D) : bwd_base_workspace_bytes(B, Hq, Nq + 127, D)) + table +
-           bias_part_bytes(B, Hq, (Nk + 127) / 128, num_buckets);
+           bias_part_bytes(B, Hq, (Nk + 127LL) / 128, num_buckets);
   if (op == MALA_OP_DECODE)
     return num_splits > 0 ? decode_workspace_bytes(B * Nq, Hq, D, num_splits) + decode_sums_bytes(B * Nq, Hq, num_splits) + table : 0;
   return 0;

@@ -253,3 +253,17 @@ def test_starts_of_the_buckets(tmp_path):
         check(nb, md, True)
     for bad in ((1, 128, 0), (129, 128, 0), (33, 128, 1), (2, 128, 1), (32, 16, 0), (32, 65537, 0), (32, 0, 0)):
         assert f(*bad, out) == -1
+
+
+def test_workspace_sizes_beyond_32_bits(mala):
+    """Rows that do not count in 32 bits have no workspace; the largest ones that do have one that grows as it should."""
+    f = mala.lib().mala_bias_workspace_bytes
+    f_ = lambda op, B, Nq, Nk, tq, S=0: int(f(op, B, 1, 1, Nq, Nk, tq, 64, S, 32, 128))   # noqa: E731
+    big = 2 ** 31 - 1
+    assert f_(mala.OP_BWD, 1, 128, 128, big) == 0 and f_(mala.OP_BWD, 65535, 128, 128, big - 384 * 65535 + 1) == 0
+    assert f_(mala.OP_BWD, 1, big, 128, 0) == 0 and f_(mala.OP_DECODE, 65535, 65535, 128, 0, 1) == 0
+    for tq in (2 ** 30, big - 511):
+        rows = -(-(tq + 384) // 128) * 128
+        assert rows * 64 * 4 <= f_(mala.OP_BWD, 1, 128, 128, tq) <= rows * (64 + 3) * 4 + 10 ** 6
+    a, b = f_(mala.OP_BWD, 1, 128, big, 0), f_(mala.OP_BWD, 1, 128, 2 ** 30, 0)
+    assert a - b == (2 ** 24 - 2 ** 23) * 16 * 32 * 4
