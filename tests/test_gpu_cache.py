@@ -363,3 +363,48 @@ def test_more_rows_than_32_bits_count_stay_within_the_buffers(mala, new, rows):
     given = table[:, 3:]
     assert ((given == -3) | ((given >= 20) & (given < 50))).all()
     assert (slots >= -1).all() and (slots < 50 * ps).all() and 0 <= left.item() <= 30
+
+
+@pytest.mark.parametrize("ps,Hkv,d", [(128, 2, 128), (16, 4, 64), (256, 1, 48)])
+def test_write_fp8_head_major_pages(mala, ps, Hkv, d):
+    """Pages whose heads lie apart (a unit's rows of one head side by side), some rows to units that hold keys."""
+    slots, pages, _, _ = _slots(5, 300, 200, ps, 77)
+    rows = slots.numel()
+    k, v = _randn(4, rows, Hkv, d) * 3, _randn(5, rows, Hkv, d)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    kp, vp = ((torch.randn((pages, Hkv, ps, d), generator=g, device="cuda") * 100).clamp(-448, 448).to(torch.float8_e4m3fn).transpose(1, 2) for _ in range(2))
+    ks, vs = (torch.rand((pages, Hkv, max(1, ps // 128)), generator=g, device="cuda") * 0.01 + 0.004 for _ in range(2))
+    want = [_plain_write8(a, b.contiguous(), c, slots) for a, b, c in ((k, kp, ks), (v, vp, vs))]
+    mala.cache_write_fp8(k, v, slots, kp, vp, ks, vs)
+    for (codes, scale), p, s in zip(want, (kp, vp), (ks, vs)):
+        assert torch.equal(s, scale)
+        assert torch.equal(p.contiguous().view(torch.uint8), codes.view(torch.uint8))
+
+
+@pytest.mark.parametrize("ps", [16, 128])
+@pytest.mark.parametrize("grow", [False, True])
+def test_a_unit_filled_token_by_token(mala, ps, grow):
+    """What decode steps do: a unit's keys one call after the other.  Its scale ends as that of one call, and with n roundings after a key's own
+    (one for each time the scale has grown since) the key is off by at most ((1 + 2^-4)^(n + 1) - 1) |x| + (n + 1) (1 + 2^-4)^n 2^-10 s: half
+    a step of 2^-4 of the value or of 2^-10 of the scale each."""
+    Hkv, d = 2, 64
+    k, v = _randn(8, ps, Hkv, d), _randn(9, ps, Hkv, d)
+    if grow:                                    # (a scale that grows with every key)
+        k = (k.float() * 1.1 ** torch.arange(ps, device="cuda")[:, None, None]).to(torch.bfloat16)
+    kp, vp = (torch.zeros((2, ps, Hkv, d), device="cuda").to(torch.float8_e4m3fn) for _ in range(2))
+    ks, vs = (torch.full((2, Hkv, 1), 7.0, device="cuda") for _ in range(2))
+    history = []
+    for t in range(ps):
+        mala.cache_write_fp8(k[t:t + 1], v[t:t + 1], torch.tensor([ps + t], device="cuda"), kp, vp, ks, vs)
+        history.append((ks[1, :, 0].clone(), vs[1, :, 0].clone()))
+    for x, p, s, i in ((k, kp, ks, 0), (v, vp, vs, 1)):
+        scales = torch.stack([h[i] for h in history])                       # [ps, Hkv]
+        top = x.float().abs().amax((0, 2))
+        assert torch.equal(s[1, :, 0], top / torch.full_like(top, 448.0)) and (s[0] == 7).all()
+        grown = (scales[1:] > scales[:-1]).double()
+        n = torch.cat([grown.flip(0).cumsum(0).flip(0), torch.zeros_like(grown[:1])])[..., None]
+        assert not grow or i or n.max() > ps // 3
+        xd, f = x.double(), (1 + 2.0 ** -4) ** n
+        bound = (f * (1 + 2.0 ** -4) - 1) * xd.abs() + (n + 1) * f * 2.0 ** -10 * s[1, :, 0].double()[None, :, None]
+        err = (p[1].double() * s[1, :, 0].double()[None, :, None] - xd).abs()
+        assert (err <= bound * (1 + 1e-5)).all()
