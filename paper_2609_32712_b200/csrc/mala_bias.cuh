@@ -18,7 +18,7 @@
 //     the same, 32 buckets up to 128                                           239 -> 268       741 -> 799
 //     8192 tokens, causal, 16 heads on 4 x 64, 32 buckets up to 128            211 -> 227       502 -> 631
 //     32 x 512 tokens, not causal, 16 heads x 64, 32 buckets up to 128          98 -> 112       254 -> 301
-// A launch of 4 us (the layout) is in each; the rest is issue slots of the softmax and score warps, which both kernels are
+// A launch of 4 us (the layout, for distances up to a few thousand; 35-65 us up to 65536) is in each; the rest is issue slots of the softmax and score warps, which both kernels are
 // short of beside the exponentials.  Values read from global memory by every thread for itself, the first form: 1386 us for
 // the first line's pair.
 #pragma once
