@@ -285,7 +285,8 @@ int mala_decode_paged(mala_tin q, mala_tin kpages, mala_tin vpages, const int32_
  *   belongs to the bucket that begins there.  2 <= num_buckets <= 128 (4 <= when bidirectional), e < max_distance <= 65536.
  *   table: bf16, entry of bucket b and query head h at [b * sb + h].  Finite values, or -inf: keys of such a bucket are
  *   masked, and a row that sees no other key gets o = 0, lse = -inf and no gradient.
- *   A row of nothing but a type's lowest values weighs its keys alike (its lse is about -1.4e38).
+ *   Scores are in fp32: a row whose keys all have biases of magnitude M has scores to M 2^-24, and one of nothing
+ *   but a type's lowest values weighs its keys alike (its lse is about -1.4e38).
  *   The backward calls have P from lse: to |lse| 2^-23 of it, and rows with |lse| >= 2^20, where every visible key or the heaviest
  *   ones have a bias as large as that, get no gradient.
  * Head sizes: multiples of 8 up to 128 in all of these calls.  Not causal: any Nq and Nk.

@@ -280,3 +280,61 @@ def test_gradients_of_a_mean_over_the_rows(mala):
             for x, y in zip(grads[0][1:], grads[1][1:]):
                 assert (x is None and y is None) or torch.equal(x, y)
             assert (grads[0][0].float() - grads[1][0].float()).abs().max() <= 2 * U * grads[1][0].float().abs().max()
+
+
+@pytest.mark.parametrize("case", ["masked near", "masked far", "only far", "lowest near", "lowest far", "lowest everywhere"])
+@pytest.mark.parametrize("tau", [1e-3, 0.3])
+@pytest.mark.parametrize("N,H,causal", [(700, 2, True), (1500, 30, True), (700, 2, False)])
+def test_masked_buckets_with_skipped_tiles(mala, N, H, causal, tau, case):
+    """tau > 0: masked and lowest buckets on the tiles that the call says it has retained, one query block per CTA and two."""
+    d, nb, md = 64, 16, 200
+    q, k, v, do, table = _inputs(19 + N, 1, H, H, N, N, d, nb)
+    low = torch.finfo(torch.bfloat16).min
+    if case == "masked near":
+        table[0:3] = -math.inf
+    elif case == "masked far":
+        table[nb - 1] = -math.inf
+    elif case == "only far":
+        table[:nb - 1] = -math.inf
+    elif case == "lowest near":
+        table[:3] = low
+    elif case == "lowest far":
+        table[nb - 4:] = low
+    else:
+        table[:] = low
+    bias, scale = mala.RelativeBias(table, md), 1 / math.sqrt(d)
+    o, lse, fst = mala.fwd_bias(q, k, v, bias, scale, tau, causal=causal, stats=True)
+    dq, dk, dv, dtable, bst = mala.bwd_bias(q, k, v, o, do, lse, bias, scale, tau, causal=causal, stats=True)
+    torch.cuda.synchronize()
+    assert mala.device_status() == 0
+    T = -(-N // 128)
+    fm, bm = fst.mask(T).cpu(), bst.mask(T).cpu()
+    for h in sorted({0, H - 1}):
+        keep = R.expand(torch.where(fm[0, h], 2, 0), N, N).cuda()
+        qd, kd, vd, dd, td = (t.double() for t in (q[0, :, h], k[0, :, h], v[0, :, h], do[0, :, h], table[:, h]))
+        r = R.head(qd, kd, vd, td, None, scale, nb, md, False, causal, keep)
+        x = r["x"]
+        # (a row's weights by softmax: beside a lowest value the normalizer's logarithm vanishes in 64 bits too)
+        p = torch.where((x == -math.inf).all(1, keepdim=True), torch.zeros_like(x), torch.softmax(x, 1).nan_to_num(0.0))
+        ro, ra = p @ vd, p @ vd.abs()
+        _check(o[0, :, h], ro, U * (ro.abs() + ra) * 1.02 + 2 * S_ABS * ra + 1e-5, f"o {h}")
+        gone = (r["lse"].abs() >= 2.0 ** 20)                 # (nothing visible, or nothing but lowest values: no gradient)
+        assert torch.equal(torch.isinf(lse[0, h]), (x == -math.inf).all(1))
+        assert (lse[0, h].double() - r["lse"])[~gone].abs().max().item() <= S_ABS if (~gone).any() else True
+        # what is skipped weighs no more than Eq. 3 says: a tile's key below tau / L of the normalizer (with the scores' error)
+        full, _ = R.scores(qd, kd, td, scale, nb, md, False, causal)
+        L = torch.arange(1, N + 1, device="cuda").double() if causal else torch.full((N,), float(N), device="cuda", dtype=torch.float64)
+        lost = (~keep) & (full > -math.inf)
+        assert ((full - r["lse"][:, None])[lost] <= (torch.log(tau / L)[:, None].expand_as(full))[lost] + 4 * S_ABS).all()
+        backkeep = R.expand(torch.where(bm[0, h].T, 2, 0), N, N).cuda()
+        xb = torch.where(backkeep, full, torch.full_like(full, -math.inf))
+        pb = torch.where(gone[:, None], torch.zeros_like(xb), torch.exp(xb - torch.where(gone, torch.zeros_like(r["lse"]), lse[0, h].double())[:, None]))
+        dp = dd @ vd.T
+        D = (o[0, :, h].double() * dd).sum(1, keepdim=True)
+        ds = pb * (dp - D)
+        e_ds = pb * (dp - D).abs() * (U + 4 * S_ABS)
+        one = lambda t: torch.stack([(t * (r["bk"] == b)).sum() for b in range(nb)])  # noqa: E731
+        for got, want, err, n in ((dq, ds @ kd * scale, e_ds @ kd.abs() * scale, "dq"), (dk, ds.T @ qd * scale, e_ds.T @ qd.abs() * scale, "dk"),
+                                  (dv, pb.T @ dd, (pb * (U + 4 * S_ABS)).T @ dd.abs(), "dv")):
+            _check(got[0, :, h], want, err * 1.02 + U * want.abs() + 1e-5, f"{n} {h}")
+        _check(dtable[:, h], one(ds), one(e_ds) * 1.02 + U * one(ds).abs() + 1e-4, f"dtable {h}")
