@@ -383,6 +383,95 @@ int mala_cache_write(mala_tin k, mala_tin v, const int64_t* slots, mala_tout kpa
 int mala_cache_write_fp8(mala_tin k, mala_tin v, const int64_t* slots, mala_tout kpages8, mala_tout vpages8, float* kscale,
                          float* vscale, int rows, int Hkv, int num_pages, int page_size, int d, void* cuda_stream);
 
+/* mala_page_tables that also gives the positions of the new tokens in their sequences: int32 [rows], 0 in rows without a slot. */
+int mala_page_tables_positions(const int32_t* seqlens, const int32_t* new_tokens, int32_t* block_table, const int32_t* free_pages,
+                               const int32_t* free_count, int32_t* cu_seqlens, int32_t* seqlens_out, int64_t* slots,
+                               int32_t* positions, int32_t* free_count_out, int B, int max_pages_per_seq, int page_size,
+                               int num_pages, int rows, void* cuda_stream);
+
+/* ---- Reading a paged cache back -----------------------------------------------------------------------------------
+ * Keys and values of B sequences out of their pages, packed one sequence behind the other: k_out, v_out bf16
+ * [rows, Hkv, d] views (sn = row stride, sh = head stride, sb ignored), cu_seqlens [B + 1] (written) the first row of each.
+ * kpages, vpages, block_table [B, max_pages_per_seq] and seqlens [B] as for mala_decode_paged / mala_fwd_paged; a length counts as
+ * what its row of the table can map.  rows: room in the outputs, at least the sum of the lengths; of a sequence that reaches
+ * beyond it only what fits is there, in cu_seqlens too.  A key whose page is not one of the pool's is 0.  The first 128 rows behind the last
+ * sequence (as far as there are) are set to 0, so that the tiles of the packed calls may cover them; the others stay as they were.
+ * d a multiple of 8 up to 256. */
+int mala_cache_read(mala_tin kpages, mala_tin vpages, const int32_t* block_table, const int32_t* seqlens, mala_tout k_out,
+                    mala_tout v_out, int32_t* cu_seqlens, int B, int Hkv, int num_pages, int page_size,
+                    int max_pages_per_seq, int rows, int d, void* cuda_stream);
+
+/* The same out of e4m3 pages with the scales of mala_decode_fp8_paged: bf16(scale * code), rounded once.  d a multiple of 16 up to 128,
+ * page_size not 8. */
+int mala_cache_read_fp8(mala_tin kpages8, mala_tin vpages8, const float* kscale, const float* vscale,
+                        const int32_t* block_table, const int32_t* seqlens, mala_tout k_out, mala_tout v_out,
+                        int32_t* cu_seqlens, int B, int Hkv, int num_pages, int page_size, int max_pages_per_seq, int rows,
+                        int d, void* cuda_stream);
+
+/* mala_fwd_paged over an e4m3 cache: keys and values are bf16(scale * code).  total_k: room for keys in the workspace, at least the sum of
+ * seqlens_k (see mala_cache_read_fp8 for what lies beyond it: the sequences that reach beyond have no meaningful result).
+ * Workspace: mala_paged_fp8_workspace_bytes.  d a multiple of 16 up to 128, page_size not 8; everything else as
+ * mala_fwd_paged; telemetry laid out for max_seqlen_k = min(max_pages_per_seq * page_size, total_k). */
+int mala_fwd_paged_fp8(mala_tin q, mala_tin kpages8, mala_tin vpages8, const float* kscale, const float* vscale,
+                       const int32_t* cu_seqlens_q, const int32_t* block_table, const int32_t* seqlens_k, mala_tout o,
+                       float* lse, const mala_stats* st, int B, int Hq, int Hkv, int total_q, int max_seqlen_q, int total_k,
+                       int num_pages, int page_size, int max_pages_per_seq, int d, int causal, float scale, float tau,
+                       void* ws, size_t ws_bytes, void* cuda_stream);
+/* 0 for unsupported arguments */
+size_t mala_paged_fp8_workspace_bytes(int B, int Hkv, int total_k, int d);
+
+/* ---- Rotary positions ---------------------------------------------------------------------------------------------
+ * The first `rotary` columns of a head's row (even, 2 .. d) are rotated in pairs by the angle position * inv_freq[i]: pair i is
+ * the columns i and i + rotary / 2, or, interleaved != 0, 2 i and 2 i + 1:
+ *     (y1, y2) -> magnitude * (y1 cos - y2 sin, y2 cos + y1 sin);   columns from rotary on stay as they are.
+ * inv_freq: DEVICE pointer, doubles [rotary / 2], radians per position (scaled for long contexts or not); the struct itself is read during the
+ * call.  Angles are exact to about 2^-31 of a turn wherever the position lies.
+ * norm (may be NULL): before its rotation each head's row is normed, y = x / sqrt(mean(x^2) + eps) * weight, over all d columns;
+ * weights [d] on the device, bf16 or (weights_fp32 != 0) fp32, NULL: 1.  All arithmetic is fp32, rounded once to bf16.
+ * d a multiple of 8 up to 256; at most 2^30 rows per tensor. */
+typedef struct { const double* inv_freq; int rotary; int interleaved; float magnitude; } mala_rotary;
+typedef struct { const void* q_weight; const void* k_weight; int weights_fp32; float eps; } mala_head_norm;
+
+/* q, q_out [B,Nq,Hq,d]; k, k_out [B,Nk,Hkv,d] (k.p and k_out.p NULL: no keys).  The queries are the last Nq of the Nk positions, as in
+ * mala_fwd_chunk.  positions: int32 [B,Nk], or NULL for 0 .. Nk - 1 (query row n of entry b has positions[b][n + Nk - Nq]); any
+ * int32 value.  An output may be its own input (same view); otherwise they must not overlap. */
+int mala_rotary_fwd(mala_tin q, mala_tin k, const int32_t* positions, const mala_rotary* rotary, const mala_head_norm* norm,
+                    mala_tout q_out, mala_tout k_out, int B, int Nq, int Nk, int Hq, int Hkv, int d, void* cuda_stream);
+
+/* Its gradients: dq, dk those of the outputs, dq_out, dk_out those of q and k (an output may be its own incoming gradient, not q or k).
+ * With a norm: q, k as they went into mala_rotary_fwd, and dq_weight, dk_weight fp32 [d] (either may be NULL), overwritten with the weights'
+ * gradients, summed over rows and heads in fp32 in a fixed order; ws of mala_rotary_workspace_bytes(d), 256-byte aligned (not needed where both
+ * are NULL).  Without one q, k and ws are ignored and dq_weight, dk_weight must be NULL. */
+int mala_rotary_bwd(mala_tin dq, mala_tin dk, mala_tin q, mala_tin k, const int32_t* positions, const mala_rotary* rotary,
+                    const mala_head_norm* norm, mala_tout dq_out, mala_tout dk_out, float* dq_weight, float* dk_weight, int B,
+                    int Nq, int Nk, int Hq, int Hkv, int d, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* Packed sequences: q [1,total_q,Hq,d], k [1,total_k,Hkv,d], offsets as in mala_fwd_varlen_prefix (pass the same twice for self attention):
+ * the key in row t of sequence b has position t - cu_seqlens_k[b], and its queries are the last positions.  Rows that no sequence has are copied
+ * as they are (their gradients too) and have no part in the weights' gradients. */
+int mala_rotary_fwd_varlen(mala_tin q, mala_tin k, const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k,
+                           const mala_rotary* rotary, const mala_head_norm* norm, mala_tout q_out, mala_tout k_out, int B,
+                           int Hq, int Hkv, int total_q, int total_k, int d, void* cuda_stream);
+int mala_rotary_bwd_varlen(mala_tin dq, mala_tin dk, mala_tin q, mala_tin k, const int32_t* cu_seqlens_q,
+                           const int32_t* cu_seqlens_k, const mala_rotary* rotary, const mala_head_norm* norm,
+                           mala_tout dq_out, mala_tout dk_out, float* dq_weight, float* dk_weight, int B, int Hq, int Hkv,
+                           int total_q, int total_k, int d, void* ws, size_t ws_bytes, void* cuda_stream);
+size_t mala_rotary_workspace_bytes(int d);
+
+/* A serving step in one call: q [rows,Hq,d] is rotated into q_out (which may be q itself), k [rows,Hkv,d] into its slots of kpages, v goes to its
+ * slots of vpages (views, slots and pages as for mala_cache_write; rows without a slot: q_out only).  positions int32 [rows], as
+ * mala_page_tables_positions gives them. */
+int mala_rotary_write(mala_tin q, mala_tin k, mala_tin v, const int32_t* positions, const int64_t* slots,
+                      const mala_rotary* rotary, const mala_head_norm* norm, mala_tout q_out, mala_tout kpages,
+                      mala_tout vpages, int rows, int Hq, int Hkv, int num_pages, int page_size, int d, void* cuda_stream);
+
+/* The same into e4m3 pages, by the rules of mala_cache_write_fp8 (on the rotated keys in fp32: codes and scales are rounded once, not
+ * behind a rounding to bf16). */
+int mala_rotary_write_fp8(mala_tin q, mala_tin k, mala_tin v, const int32_t* positions, const int64_t* slots,
+                          const mala_rotary* rotary, const mala_head_norm* norm, mala_tout q_out, mala_tout kpages8,
+                          mala_tout vpages8, float* kscale, float* vscale, int rows, int Hq, int Hkv, int num_pages,
+                          int page_size, int d, void* cuda_stream);
+
 /* Decode for callers that cannot allocate device memory.  (The paper has no counterpart: this entry point
  * exists for integration reasons only and computes exactly what mala_decode computes.)
  *

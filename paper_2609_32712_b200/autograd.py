@@ -98,6 +98,71 @@ class _MalaAttentionBiasPacked(torch.autograd.Function):
         return dq, dk, dv, dtable, None, None, None, None, None, None, None, None, None
 
 
+def _head_norm(eps: Optional[float], q_weight, k_weight):
+    return None if eps is None else mala.HeadNorm(q_weight, k_weight, eps)
+
+
+def _weight_grads(dwq, dwk, q_weight, k_weight):
+    return (None if dwq is None else dwq.to(q_weight.dtype)), (None if dwk is None else dwk.to(k_weight.dtype))
+
+
+class _RotaryPositions(torch.autograd.Function):
+    """q and k rotated; packed: (cu_q, cu_k), else positions or None."""
+
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, rot, positions, packed, eps):
+        norm = _head_norm(eps, q_weight, k_weight)
+        qo, ko = mala.rotary_varlen(q, k, *packed, rot, norm) if packed else mala.rotary(q, k, rot, positions, norm)
+        ctx.save_for_backward(*((q, k) if norm else (None, None)), q_weight, k_weight)
+        ctx.args = (rot, positions, packed, eps)
+        return qo, ko
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq, dk):
+        q, k, q_weight, k_weight = ctx.saved_tensors
+        rot, positions, packed, eps = ctx.args
+        norm, weights = _head_norm(eps, q_weight, k_weight), any(ctx.needs_input_grad[2:4])
+        dq, dk = _incoming(dq), _incoming(dk)
+        if packed:
+            dq, dk, dwq, dwk = mala.rotary_varlen_bwd(dq, dk, *packed, rot, norm, q, k, weights=weights)
+        else:
+            dq, dk, dwq, dwk = mala.rotary_bwd(dq, dk, rot, positions, norm, q, k, weights=weights)
+        return (dq, dk, *_weight_grads(dwq, dwk, q_weight, k_weight), None, None, None, None)
+
+
+class _MalaAttentionRotary(torch.autograd.Function):
+    """Rotary positions and attention; packed: (cu_q, cu_k, max_q, max_k).  The gradients of the rotated q and k are rotated back in place."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, q_weight, k_weight, rot, positions, packed, eps, tau: float, scale: float, causal: bool):
+        norm = _head_norm(eps, q_weight, k_weight)
+        if packed:
+            qr, kr = mala.rotary_varlen(q, k, *packed[:2], rot, norm)
+            o, lse, _ = mala.fwd_varlen_prefix(qr, kr, v, *packed, scale, tau, causal=causal)
+        else:
+            qr, kr = mala.rotary(q, k, rot, positions, norm)
+            o, lse, _ = mala.fwd_chunk(qr, kr, v, scale, tau, causal=causal)
+        ctx.save_for_backward(qr, kr, v, o, lse, *((q, k) if norm else (None, None)), q_weight, k_weight)
+        ctx.args = (rot, positions, packed, eps, tau, scale, causal)
+        return o
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, do):
+        qr, kr, v, o, lse, q, k, q_weight, k_weight = ctx.saved_tensors
+        rot, positions, packed, eps, tau, scale, causal = ctx.args
+        norm, weights = _head_norm(eps, q_weight, k_weight), any(ctx.needs_input_grad[3:5])
+        do = _incoming(do)
+        if packed:
+            dq, dk, dv, _ = mala.bwd_varlen_prefix(qr, kr, v, o, do, lse, *packed, scale, tau, causal=causal)
+            dq, dk, dwq, dwk = mala.rotary_varlen_bwd(dq, dk, *packed[:2], rot, norm, q, k, dq_out=dq, dk_out=dk, weights=weights)
+        else:
+            dq, dk, dv, _ = mala.bwd_chunk(qr, kr, v, o, do, lse, scale, tau, causal=causal)
+            dq, dk, dwq, dwk = mala.rotary_bwd(dq, dk, rot, positions, norm, q, k, dq_out=dq, dk_out=dk, weights=weights)
+        return (dq, dk, dv, *_weight_grads(dwq, dwk, q_weight, k_weight), *[None] * 7)
+
+
 def mala_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, tau: float, scale: Optional[float] = None,
                    causal: bool = True) -> torch.Tensor:
     """MALA attention of bf16 q [B,Nq,Hq,d] against k, v [B,Nk,Hkv,d] on a B200 (tau = 0: FullAttn), differentiable
@@ -142,3 +207,43 @@ def mala_attention_bias_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor
         scale = 1.0 / math.sqrt(q.shape[-1])
     return _MalaAttentionBiasPacked.apply(q, k, v, table, cu_seqlens_q, cu_seqlens_k, int(max_seqlen_q), int(max_seqlen_k),
                                           int(max_distance), bool(bidirectional), float(tau), float(scale), bool(causal))
+
+
+def rotary(q: torch.Tensor, k: torch.Tensor, rot: mala.Rotary, positions: Optional[torch.Tensor] = None,
+           q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: Optional[float] = None):
+    """Rotary positions of bf16 q [B,Nq,Hq,d] and k [B,Nk,Hkv,d] (``mala.rotary``), differentiable once with respect to q and k; with
+    eps each head's row goes through a root-mean-square norm first, differentiable in its weights [d] too (None: 1).  Returns (q', k')."""
+    assert eps is not None or (q_weight is None and k_weight is None), "weights belong to a norm: give its eps"
+    return _RotaryPositions.apply(q, k, q_weight, k_weight, rot, positions, None, eps)
+
+
+def rotary_packed(q: torch.Tensor, k: torch.Tensor, cu_seqlens_q: torch.Tensor, cu_seqlens_k: torch.Tensor, rot: mala.Rotary,
+                  q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: Optional[float] = None):
+    """``rotary`` on packed sequences (``mala.rotary_varlen``)."""
+    assert eps is not None or (q_weight is None and k_weight is None), "weights belong to a norm: give its eps"
+    return _RotaryPositions.apply(q, k, q_weight, k_weight, rot, None, (cu_seqlens_q, cu_seqlens_k), eps)
+
+
+def mala_attention_rotary(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rot: mala.Rotary, tau: float,
+                          positions: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                          k_weight: Optional[torch.Tensor] = None, eps: Optional[float] = None, scale: Optional[float] = None,
+                          causal: bool = True) -> torch.Tensor:
+    """``mala_attention`` of q and k at rotary positions (``rotary``: norm of each head with eps, positions int32 [B,Nk] or 0 .. Nk - 1).
+    Differentiable once with respect to q, k, v and the weights.  To capture the backward pass in a CUDA graph, let no other autograd
+    graph of the same leaves be alive: torch adds up their gradients on the stream on which that one was built, outside the capture."""
+    assert eps is not None or (q_weight is None and k_weight is None), "weights belong to a norm: give its eps"
+    if scale is None:
+        scale = 1.0 / math.sqrt(q.shape[-1])
+    return _MalaAttentionRotary.apply(q, k, v, q_weight, k_weight, rot, positions, None, eps, float(tau), float(scale), bool(causal))
+
+
+def mala_attention_rotary_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens_q: torch.Tensor, cu_seqlens_k: torch.Tensor,
+                                 max_seqlen_q: int, max_seqlen_k: int, rot: mala.Rotary, tau: float,
+                                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                                 eps: Optional[float] = None, scale: Optional[float] = None, causal: bool = True) -> torch.Tensor:
+    """``mala_attention_packed`` of q and k at rotary positions, which count within a sequence's keys (``mala_attention_rotary``)."""
+    assert eps is not None or (q_weight is None and k_weight is None), "weights belong to a norm: give its eps"
+    if scale is None:
+        scale = 1.0 / math.sqrt(q.shape[-1])
+    return _MalaAttentionRotary.apply(q, k, v, q_weight, k_weight, rot, None, (cu_seqlens_q, cu_seqlens_k, int(max_seqlen_q), int(max_seqlen_k)),
+                                      eps, float(tau), float(scale), bool(causal))

@@ -568,6 +568,46 @@ int mala_fwd_paged(mala_tin q, mala_tin kpages, mala_tin vpages, const int32_t* 
                   cu_seqlens_q, total_q, 1, nullptr, 0, nullptr, 0, &pg));
 }
 
+// Workspace of mala_fwd_paged_fp8: keys, values and offsets
+static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+size_t mala_paged_fp8_workspace_bytes(int B, int Hkv, int total_k, int d) {
+  if (B <= 0 || Hkv <= 0 || total_k <= 0 || d <= 0 || d % 16 != 0 || d > 128) return 0;
+  return 2 * up256((size_t)total_k * Hkv * d * 2) + up256(((size_t)B + 1) * sizeof(int));
+}
+
+int mala_fwd_paged_fp8(mala_tin q, mala_tin kpages8, mala_tin vpages8, const float* kscale, const float* vscale, const int32_t* cu_seqlens_q,
+                       const int32_t* block_table, const int32_t* seqlens_k, mala_tout o, float* lse, const mala_stats* st, int B, int Hq, int Hkv,
+                       int total_q, int max_seqlen_q, int total_k, int num_pages, int page_size, int max_pages_per_seq, int d, int causal,
+                       float scale, float tau, void* ws, size_t ws_bytes, void* cuda_stream) {
+  ApiScope scope("mala_fwd_paged_fp8", cuda_stream);
+  MALA_TRY(check_packed(cu_seqlens_q, B, total_q, max_seqlen_q));
+  if (!block_table || !seqlens_k || num_pages <= 0 || page_size <= 0 || max_pages_per_seq <= 0 || total_k <= 0) return MALA_ERR_INVALID_ARG;
+  if ((long long)max_pages_per_seq * page_size > 0x7fffffffLL) return MALA_ERR_UNSUPPORTED;
+  const int row = max_pages_per_seq * page_size, max_k = row < total_k ? row : total_k;
+  MALA_TRY(check_packed(cu_seqlens_q, B, total_k, max_k));
+  if (causal && max_k < max_seqlen_q) return MALA_ERR_UNSUPPORTED;
+  // (everything that the attention's launch checks is checked before the cache is read: nothing is launched on error)
+  MALA_TRY(check_common(B, Hq, Hkv, max_seqlen_q, d, scale, tau, 128));
+  if (!lse || !ws) return MALA_ERR_INVALID_ARG;
+  MALA_TRY(check_view(q.p, q.sb, q.sn, q.sh, 1, total_q, Hq));
+  MALA_TRY(check_view(o.p, o.sb, o.sn, o.sh, 1, total_q, Hq));
+  const size_t bytes = mala_paged_fp8_workspace_bytes(B, Hkv, total_k, d);
+  if (bytes == 0) return MALA_ERR_UNSUPPORTED;
+  if ((((uintptr_t)ws) & 255) != 0) return MALA_ERR_MISALIGNED;
+  if (ws_bytes < bytes) return MALA_ERR_WORKSPACE_TOO_SMALL;
+  const size_t part = up256((size_t)total_k * Hkv * d * 2);
+  mala_tout k, v;
+  k.p = ws; v.p = (uint8_t*)ws + part;
+  k.sb = v.sb = 0; k.sn = v.sn = (int64_t)Hkv * d; k.sh = v.sh = d;
+  int32_t* const cu_k = (int32_t*)((uint8_t*)ws + 2 * part);
+  MALA_TRY(mala_cache_read_fp8(kpages8, vpages8, kscale, vscale, block_table, seqlens_k, k, v, cu_k, B, Hkv, num_pages, page_size, max_pages_per_seq,
+                               total_k, d, cuda_stream));
+  const mala_tin ki = {k.p, 0, k.sn, k.sh}, vi = {v.p, 0, v.sn, v.sh};
+  return scope.finish(fwd_impl(q, ki, vi, o, lse, st, B, Hq, Hkv, max_seqlen_q, max_k, d, causal, scale, tau, cuda_stream, cu_seqlens_q, total_q, 1, nullptr,
+                               0, cu_k, total_k));
+}
+
 int mala_bwd_varlen(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dout, const float* lse,
                     const int32_t* cu_seqlens, mala_tout dq, mala_tout dk, mala_tout dv, const mala_stats* st, int B,
                     int Hq, int Hkv, int total, int max_seqlen, int d, int causal, float scale, float tau, void* ws,

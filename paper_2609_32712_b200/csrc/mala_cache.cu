@@ -3,10 +3,12 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "../../include/mala.h"
 #include "mala_decode_sched.cuh"
 #include "mala_internal.h"
+#include "mala_rotary.cuh"
 #include "sm100_ptx.cuh"
 
 namespace mala {
@@ -62,6 +64,7 @@ struct TableParams {
   int* block_table;
   int* free_pages; const int* free_count;
   int* cu; int* seqlens_out; int64_t* slots; int* free_out;
+  int* positions;                         // of the new tokens, or null
   int B, max_pages, page_size, num_pages, rows;
   FastDiv by_page;
 };
@@ -146,17 +149,22 @@ page_tables_kernel(const TableParams p) {
   }
   if (kRelease) return;
   const int total = rows_at[p.B];
-  auto slot_of = [&](int t, int lo, int hi) -> int64_t {   // row t, whose request is one of lo .. hi - 1
+  auto slot_of = [&](int t, int lo, int hi, int& at_pos) -> int64_t {   // row t, whose request is one of lo .. hi - 1
+    at_pos = 0;
     const int b = find_last(rows_at, lo, hi, t);
     if ((refused[b >> 5] >> (b & 31)) & 1u) return -1;
     const uint32_t len = (uint32_t)lens[b], pos = len + ((uint32_t)t - (uint32_t)rows_at[b]);
     const uint32_t have = p.by_page.div(len + ps - 1), x = p.by_page.div(pos), given = (uint32_t)pages_at[b] + x - have;
     if (x >= (uint32_t)p.max_pages || (x >= have && given >= (uint32_t)count)) return -1;
     const int page = x < have ? p.block_table[(int64_t)b * p.max_pages + x] : p.free_pages[count - 1 - (int)given];
-    return page >= 0 ? (int64_t)page * ps + (pos - x * (uint32_t)ps) : -1;
+    if (page < 0) return -1;
+    at_pos = (int)pos;
+    return (int64_t)page * ps + (pos - x * (uint32_t)ps);
   };
   if (p.rows <= step) {
-    if (at < p.rows) p.slots[at] = at < total ? slot_of(at, 0, p.B) : -1;
+    int pos = 0;
+    if (at < p.rows) p.slots[at] = at < total ? slot_of(at, 0, p.B, pos) : -1;
+    if (at < p.rows && p.positions) p.positions[at] = pos;
     return;
   }
   // many rows, 128 at a time by a warp: where the first and the last of them belong is searched once, and between the two is seldom much
@@ -164,15 +172,18 @@ page_tables_kernel(const TableParams p) {
     const int lo = t0 < total ? find_last(rows_at, 0, p.B, t0) : 0;
     const int hi = t0 < total ? find_last(rows_at, lo, p.B, min(t0 + 127, total - 1)) + 1 : 0;
     int64_t slot[4];
+    int pos[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int t = t0 + i * 32 + (tid & 31);
-      slot[i] = t < total && t < p.rows ? slot_of(t, lo, hi) : -1;
+      pos[i] = 0;
+      slot[i] = t < total && t < p.rows ? slot_of(t, lo, hi, pos[i]) : -1;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int t = t0 + i * 32 + (tid & 31);
       if (t < p.rows) p.slots[t] = slot[i];
+      if (t < p.rows && p.positions) p.positions[t] = pos[i];
     }
   }
 }
@@ -208,6 +219,10 @@ struct WriteParams {
   int unit, chunk;                         // e4m3: keys that share a scale; rows among which a block looks for the first ones of units
   int64_t limit;                           // slots of the pool
   FastDiv by_per, by_cols, by_page;
+  RotaryRule rule;                         // e4m3, keys that are rotated on their way: rule, positions [rows], norm
+  const int* positions;
+  const void* weight; int weights_fp32, normed;
+  float eps, inv_d;
 };
 
 // A thread takes four 16-byte pieces of the call's rows, of K and of V: a copy with eight loads in flight, bound by HBM:
@@ -275,9 +290,45 @@ __device__ __forceinline__ void copy16_async(uint4* to, const void* from) {
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
+constexpr int kNoTurn = -1;
+
+// A row of keys that are rotated on their way, as a thread of its kRow has it in fp32: its eight columns from w, a place in shared
+// memory whose neighbours hold the rest of the row.
+template <int kRow, int kTurn>
+__device__ __forceinline__ void rotated8(const WriteParams& p, const LaneTurns<kTurn>& turns, const uint4* from, int c, int pos, float (&x)[8]) {
+  const int at = c < p.cols ? c : 0;     // (threads beyond the row's columns: any of it)
+  const uint4 w = *from;
+  float y[8], C[8], S[8];
+  unpack8(c < p.cols ? w : make_uint4(0u, 0u, 0u, 0u), x);
+  if constexpr (kTurn == kHalves) unpack8(from[partner_of<kHalves>(8 * at, p.rule.rotary) / 8 - c], y);
+  else partners<kTurn>(w, x, 0, reinterpret_cast<const __nv_bfloat16*>(from - c), at, p.rule.rotary, 0u, y);
+  turns.at(p.rule, c, pos, C, S);
+  float r = 1.f;
+  if (p.normed) {
+    const uint32_t group = (kRow == 8 ? 0xffu : 0xffffu) << ((threadIdx.x & 31) / kRow * kRow);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+#pragma unroll
+    for (int m = kRow / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(group, sum, m);
+    r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      C[e] *= weight_at(p.weight, p.weights_fp32, 8 * at + e);
+      S[e] *= weight_at(p.weight, p.weights_fp32, partner_of<kTurn>(8 * at + e, p.rule.rotary));
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    x[e] *= C[e];
+    if (turns.on(e)) x[e] = fmaf(y[e], S[e], x[e]);
+    x[e] *= r;
+  }
+}
+
 // kRow threads per row (8 where a row has at most as many 16-byte pieces, else 16); kBatch rows fit the team's part of the buffer
-template <int kThreads, int kRow, int kBatch>
-__device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int h, int t, int n, int64_t slot, uint4* buf, float* red) {
+template <int kThreads, int kRow, int kBatch, int kTurn, class Turns>
+__device__ __forceinline__ void write8_unit(const WriteParams& p, const Turns& turns, bool is_v, int h, int t, int n, int64_t slot, uint4* buf, float* red) {
   constexpr int kRows = kThreads / kRow;
   static_assert(kBatch % kRows == 0, "a thread's places are its own");
   const int tid = threadIdx.x & (kThreads - 1), lane = threadIdx.x & 31, r0 = tid / kRow, c = tid % kRow;
@@ -290,16 +341,34 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int
   float* sp = (is_v ? p.vscale : p.kscale) + (page * p.Hkv + h) * p.per_page + at / 128;
   buf += tid;
   auto load = [&](const uint8_t* from, uint4* to, int first) {
+    if (kTurn != kNoTurn) __syncwarp();  // (a row's other threads have read what lay there)
     if (mine)
       for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, to += kThreads, from += kRows * s_sn) copy16_async(to, from);
+  };
+  auto arrived = [&]() {
+    copies_wait();
+    if (kTurn != kNoTurn) __syncwarp();
   };
   load(src, buf, 0);
   const float old = *(volatile const float*)sp;   // (before the store below, which a cached load need not be)
   uint32_t top2 = 0;                     // largest magnitudes of the even and the odd columns (bf16 magnitudes are ordered like their bits)
+  float top_turned = 0.f;
   for (int first = 0; first < n; first += kBatch) {
     if (first > 0) load(src + (int64_t)first * s_sn, buf, first);
-    copies_wait();
+    arrived();
     const uint4* from = buf;
+    if constexpr (kTurn != kNoTurn) {
+      if (!is_v) {
+        for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, from += kThreads) {
+          float x[8];
+          rotated8<kRow, kTurn>(p, turns, from, c, __ldg(p.positions + t + r), x);
+          if (mine)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top_turned = fmaxf(top_turned, fabsf(x[e]));
+        }
+        continue;
+      }
+    }
     if (mine)
       for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, from += kThreads) {
         const uint4 w = *from;
@@ -308,6 +377,7 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int
       }
   }
   float top = fmaxf(__uint_as_float(top2 << 16), __uint_as_float(top2 & 0xffff0000u));
+  if (kTurn != kNoTurn) top = fmaxf(top, top_turned);
 #pragma unroll
   for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
   if constexpr (kThreads > 32) {
@@ -338,10 +408,25 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int
   for (int first = 0; first < n; first += kBatch) {
     if (n > kBatch) {
       load(src + (int64_t)first * s_sn, buf, first);
-      copies_wait();
+      arrived();
     }
     const uint4* from = buf;
     uint8_t* to = dst + first * d_sn;
+    if constexpr (kTurn != kNoTurn) {
+      if (!is_v) {
+        for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, from += kThreads, to += kRows * d_sn) {
+          float x[8];
+          rotated8<kRow, kTurn>(p, turns, from, c, __ldg(p.positions + t + r), x);
+          auto four = [&](float x0, float x1, float x2, float x3) -> uint32_t {
+            const uint32_t high = __byte_perm(__byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x0073),
+                                              __byte_perm(__float_as_uint(x2), __float_as_uint(x3), 0x0073), 0x5410);
+            return signs(codes2(x0, x1) | (codes2(x2, x3) << 16), high);
+          };
+          if (mine) *reinterpret_cast<uint2*>(to) = make_uint2(four(x[0], x[1], x[2], x[3]), four(x[4], x[5], x[6], x[7]));
+        }
+        continue;
+      }
+    }
     if (mine)
       for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, from += kThreads, to += kRows * d_sn) {
         const uint4 w = *from;
@@ -374,8 +459,11 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int
   }
 }
 
-template <int kBlock, int kRow>
-__global__ void __launch_bounds__(kBlock, kBlock == 64 ? 13 : kBlock == 128 ? 6 : 4)
+struct NoTurns {};
+
+// kTurn: keys are rotated on their way (how their columns are paired), or kNoTurn
+template <int kBlock, int kRow, int kTurn>
+__global__ void __launch_bounds__(kBlock, kTurn != kNoTurn ? 512 / kBlock : kBlock == 64 ? 13 : kBlock == 128 ? 6 : 4)
 cache_write8_kernel(const WriteParams p) {
   constexpr int kWarps = kBlock / 32, kAll = (kBlock == 64 ? 1024 : 2048) / kRow, kShare = kAll / kWarps;   // rows (all of a unit), a warp's
   __shared__ __align__(16) uint4 rows_s[kAll * kRow];
@@ -408,6 +496,9 @@ cache_write8_kernel(const WriteParams p) {
   else if (p.chunk < 32) begins &= (1u << p.chunk) - 1u;
   // few units: the whole block takes one after the other; many, which are short: a warp each
   const bool few = __popcll(begins) <= (kBlock == 256 ? 1 : 2);
+  std::conditional_t<kTurn == kNoTurn, NoTurns, LaneTurns<kTurn>> turns;
+  if constexpr (kTurn != kNoTurn)
+    if (!is_v && begins) turns.load(p.rule, threadIdx.x % kRow);
   for (int i = 0; begins; begins &= begins - 1, ++i) {
     const int x = __ffsll((long long)begins) - 1;
     if (!few && i % kWarps != warp) continue;
@@ -420,15 +511,151 @@ cache_write8_kernel(const WriteParams p) {
       end = (end | 31) + 1;
     }
     end = min(end, last);
-    if (few) write8_unit<kBlock, kRow, kAll>(p, is_v, h, t0 + x, end - x, at, rows_s, red[i & 1]);
-    else write8_unit<32, kRow, kShare>(p, is_v, h, t0 + x, end - x, at, rows_s + warp * (kShare * kRow), nullptr);
+    if (few) write8_unit<kBlock, kRow, kAll, kTurn>(p, turns, is_v, h, t0 + x, end - x, at, rows_s, red[i & 1]);
+    else write8_unit<32, kRow, kShare, kTurn>(p, turns, is_v, h, t0 + x, end - x, at, rows_s + warp * (kShare * kRow), nullptr);
   }
 }
 
+// ------------------------------------------------------------------------------------------------
+// Reads out of the pages
+// ------------------------------------------------------------------------------------------------
+struct ReadParams {
+  const uint8_t* kp; const uint8_t* vp;    // [num_pages, page_size, Hkv, d]
+  int64_t kp_sb, kp_sn, kp_sh, vp_sb, vp_sn, vp_sh;   // bytes
+  const float* kscale; const float* vscale;           // e4m3: [num_pages, Hkv, per_page]
+  uint8_t* k; uint8_t* v;                  // [rows, Hkv, d] bf16
+  int64_t k_sn, k_sh, v_sn, v_sh;          // bytes
+  const int* block_table; const int* seqlens; int* cu;
+  int B, max_pages, page_size, num_pages, per_page, rows, Hkv;
+  int cols, per;                           // 16-byte pieces of a head's row in the pages, and of a whole row
+  FastDiv by_per, by_cols, by_page;
+};
+
+// A block adds up the lengths for itself (as the tables do) and takes a thousand pieces of the packed rows at a time: which
+// sequence the first and the last of them belong to is searched once.  A thread has four 16-byte pieces of K and of V in flight.
+template <bool kFp8>
+__global__ void __launch_bounds__(256)
+cache_read_kernel(const ReadParams p) {
+  extern __shared__ int cu_s[];            // [B + 1]
+  __shared__ uint64_t warp_sums[32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long room = (long long)p.max_pages * p.page_size;
+  long long before = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 256) {
+    const int b = b0 + tid;
+    long long x = b < p.B ? max(0ll, min(room, (long long)__ldg(p.seqlens + b))) : 0;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, x, m);
+      if (lane >= m) x += y;
+    }
+    if (lane == 31) warp_sums[warp] = (uint64_t)x;
+    __syncthreads();
+    long long sum = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      if (w == warp) x += before + sum;
+      sum += (long long)warp_sums[w];
+    }
+    before += sum;
+    if (b < p.B) cu_s[b + 1] = (int)min((long long)p.rows, x);
+    __syncthreads();
+  }
+  if (tid == 0) cu_s[0] = 0;
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int b = tid; b <= p.B; b += 256) p.cu[b] = cu_s[b];
+  const int have = cu_s[p.B], reach = min(p.rows, have + 128);
+  const int64_t all = (int64_t)reach * p.per;
+  for (int64_t base = (int64_t)blockIdx.x * 1024; base < all; base += (int64_t)gridDim.x * 1024) {
+    auto row_of = [&](int64_t x) { return all <= 0xffffffffll ? (int)p.by_per.div((uint32_t)x) : (int)(x / p.per); };
+    const int first = min(row_of(base), max(have - 1, 0)), last = min(row_of(min(base + 1023, all - 1)), max(have - 1, 0));
+    const int lo = find_last(cu_s, 0, p.B, first), hi = find_last(cu_s, lo, p.B, last) + 1;
+    uint4 wk[4], wv[4];
+    float sk[4], sv[4];
+    int64_t to_k[4], to_v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t x = base + i * 256 + tid;
+      to_k[i] = -1;
+      wk[i] = wv[i] = make_uint4(0u, 0u, 0u, 0u);
+      sk[i] = sv[i] = 0.f;
+      if (x < all) {
+        const int row = row_of(x), c = (int)(x - (int64_t)row * p.per), h = (int)p.by_cols.div((uint32_t)c), col = (c - h * p.cols) * 16;
+        to_k[i] = row * p.k_sn + h * p.k_sh + col * (kFp8 ? 2 : 1);
+        to_v[i] = row * p.v_sn + h * p.v_sh + col * (kFp8 ? 2 : 1);
+        if (row < have) {
+          const int b = find_last(cu_s, lo, hi, row), pos = row - cu_s[b], entry = (int)p.by_page.div((uint32_t)pos);
+          const int page = __ldg(p.block_table + (int64_t)b * p.max_pages + entry), at = pos - entry * p.page_size;
+          if (page >= 0 && page < p.num_pages) {
+            wk[i] = __ldg(reinterpret_cast<const uint4*>(p.kp + page * p.kp_sb + at * p.kp_sn + h * p.kp_sh + col));
+            wv[i] = __ldg(reinterpret_cast<const uint4*>(p.vp + page * p.vp_sb + at * p.vp_sn + h * p.vp_sh + col));
+            if (kFp8) {
+              const int64_t unit = ((int64_t)page * p.Hkv + h) * p.per_page + at / 128;
+              sk[i] = __ldg(p.kscale + unit);
+              sv[i] = __ldg(p.vscale + unit);
+            }
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (to_k[i] < 0) continue;
+      if constexpr (kFp8) {
+        auto pair = [](uint32_t codes, float s) -> uint32_t {
+          const float2 a = from_e4m3x2((uint16_t)codes);
+          return pack_bf16x2(a.x * s, a.y * s);
+        };
+        auto eight = [&](uint32_t a, uint32_t b, float s) { return make_uint4(pair(a, s), pair(a >> 16, s), pair(b, s), pair(b >> 16, s)); };
+        uint4* const to = reinterpret_cast<uint4*>(p.k + to_k[i]);
+        uint4* const to2 = reinterpret_cast<uint4*>(p.v + to_v[i]);
+        to[0] = eight(wk[i].x, wk[i].y, sk[i]);
+        to[1] = eight(wk[i].z, wk[i].w, sk[i]);
+        to2[0] = eight(wv[i].x, wv[i].y, sv[i]);
+        to2[1] = eight(wv[i].z, wv[i].w, sv[i]);
+      } else {
+        *reinterpret_cast<uint4*>(p.k + to_k[i]) = wk[i];
+        *reinterpret_cast<uint4*>(p.v + to_v[i]) = wv[i];
+      }
+    }
+  }
+}
+
+constexpr int kReadMaxB = 16384;
+
+int cache_read(mala_tin kp, mala_tin vp, const float* kscale, const float* vscale, const int32_t* block_table, const int32_t* seqlens, mala_tout k,
+               mala_tout v, int32_t* cu, int B, int Hkv, int num_pages, int page_size, int max_pages, int rows, int d, bool fp8, cudaStream_t stream) {
+  ReadParams p = {};
+  const int item = fp8 ? 1 : 2;
+  p.kp = (const uint8_t*)kp.p; p.vp = (const uint8_t*)vp.p;
+  p.kp_sb = kp.sb * item; p.kp_sn = kp.sn * item; p.kp_sh = kp.sh * item;
+  p.vp_sb = vp.sb * item; p.vp_sn = vp.sn * item; p.vp_sh = vp.sh * item;
+  p.kscale = kscale; p.vscale = vscale;
+  p.k = (uint8_t*)k.p; p.v = (uint8_t*)v.p;
+  p.k_sn = k.sn * 2; p.k_sh = k.sh * 2; p.v_sn = v.sn * 2; p.v_sh = v.sh * 2;
+  p.block_table = block_table; p.seqlens = seqlens; p.cu = cu;
+  p.B = B; p.max_pages = max_pages; p.page_size = page_size; p.num_pages = num_pages; p.per_page = page_size < 128 ? 1 : page_size / 128;
+  p.rows = rows; p.Hkv = Hkv;
+  p.cols = d * item / 16; p.per = p.cols * Hkv;
+  p.by_per.set((uint32_t)p.per); p.by_cols.set((uint32_t)p.cols); p.by_page.set((uint32_t)page_size);
+  int dev = 0, *status = nullptr;
+  MALA_TRY(current_device_checked(&dev));
+  MALA_TRY(device_setup(dev, &status));
+  const long long want = ((long long)rows * p.per + 1023) / 1024, most = 8ll * sm_count(dev);
+  const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
+  const size_t smem = ((size_t)B + 1) * sizeof(int);
+  if (fp8) cache_read_kernel<true><<<grid, 256, smem, stream>>>(p);
+  else cache_read_kernel<false><<<grid, 256, smem, stream>>>(p);
+  return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+}
+
 bool cache_set_attributes() {
-  const int most = (3 * kTableMaxB + 2) * (int)sizeof(int);
+  const int most = (3 * kTableMaxB + 2) * (int)sizeof(int), most_read = (kReadMaxB + 1) * (int)sizeof(int);
   return cudaFuncSetAttribute(page_tables_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess &&
-         cudaFuncSetAttribute(page_tables_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
+         cudaFuncSetAttribute(page_tables_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess &&
+         cudaFuncSetAttribute(cache_read_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_read) == cudaSuccess &&
+         cudaFuncSetAttribute(cache_read_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_read) == cudaSuccess;
 }
 
 static bool aligned16(const void* p) { return (((uintptr_t)p) & 15) == 0; }
@@ -469,6 +696,28 @@ static int write_params(WriteParams* w, mala_tin k, mala_tin v, const int64_t* s
   return MALA_OK;
 }
 
+template <int kTurn>
+static int launch_write8(WriteParams& w, cudaStream_t stream) {
+  const int rows = w.rows, Hkv = w.Hkv;
+  int dev = 0, *status = nullptr;
+  MALA_TRY(current_device_checked(&dev));
+  MALA_TRY(device_setup(dev, &status));
+  // Blocks of eight warps and of so few rows that all blocks run at once (four per SM); where that would take more than eight rows
+  // each, blocks of two warps, or of four where a unit takes 32 KB, and of 64 rows (so that few blocks find nothing to do) or fewer while
+  // they run at once (16 requests of up to 40 rows, pages of 16 keys: 5.8 us, with 64 rows per block 11.0)
+  while (w.chunk < 16 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 4ll * sm_count(dev)) w.chunk *= 2;
+  const bool many = w.chunk == 16, narrow = w.cols <= 8;
+  if (many)
+    while (w.chunk < 64 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 8ll * sm_count(dev)) w.chunk *= 2;
+  const dim3 grid((unsigned)((rows + w.chunk - 1) / w.chunk), Hkv, 2);
+  if (!many && narrow) cache_write8_kernel<256, 8, kTurn><<<grid, 256, 0, stream>>>(w);
+  else if (!many) cache_write8_kernel<256, 16, kTurn><<<grid, 256, 0, stream>>>(w);
+  else if (narrow) cache_write8_kernel<64, 8, kTurn><<<grid, 64, 0, stream>>>(w);
+  else if (w.unit < 128) cache_write8_kernel<64, 16, kTurn><<<grid, 64, 0, stream>>>(w);
+  else cache_write8_kernel<128, 16, kTurn><<<grid, 128, 0, stream>>>(w);
+  return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+}
+
 static int check_tables(const int32_t* seqlens, const int32_t* block_table, const int32_t* free_pages, const int32_t* free_count,
                         const int32_t* seqlens_out, const int32_t* free_count_out, int B, int max_pages, int page_size, int num_pages) {
   if (!seqlens || !block_table || !free_pages || !free_count || !seqlens_out || !free_count_out) return MALA_ERR_INVALID_ARG;
@@ -489,21 +738,39 @@ using namespace mala;
 
 extern "C" {
 
-int mala_page_tables(const int32_t* seqlens, const int32_t* new_tokens, int32_t* block_table, const int32_t* free_pages,
-                     const int32_t* free_count, int32_t* cu_seqlens, int32_t* seqlens_out, int64_t* slots,
-                     int32_t* free_count_out, int B, int max_pages_per_seq, int page_size, int num_pages, int rows,
-                     void* cuda_stream) {
-  ApiScope scope("mala_page_tables", cuda_stream);
+static int page_tables(const char* name, const int32_t* seqlens, const int32_t* new_tokens, int32_t* block_table, const int32_t* free_pages,
+                       const int32_t* free_count, int32_t* cu_seqlens, int32_t* seqlens_out, int64_t* slots, int32_t* positions,
+                       int32_t* free_count_out, int B, int max_pages_per_seq, int page_size, int num_pages, int rows, void* cuda_stream) {
+  ApiScope scope(name, cuda_stream);
   MALA_TRY(check_tables(seqlens, block_table, free_pages, free_count, seqlens_out, free_count_out, B, max_pages_per_seq, page_size, num_pages));
   if (!new_tokens || !cu_seqlens || rows < 0 || (rows > 0 && !slots)) return MALA_ERR_INVALID_ARG;
   if ((((uintptr_t)new_tokens) & 3) != 0 || (((uintptr_t)cu_seqlens) & 3) != 0 || (((uintptr_t)slots) & 7) != 0) return MALA_ERR_MISALIGNED;
   if (rows > kMaxRows) return MALA_ERR_UNSUPPORTED;
   if (cu_seqlens == seqlens || cu_seqlens == new_tokens || seqlens_out == new_tokens) return MALA_ERR_INVALID_ARG;
+  if ((((uintptr_t)positions) & 3) != 0) return MALA_ERR_MISALIGNED;
+  if (positions && (positions == seqlens || positions == new_tokens)) return MALA_ERR_INVALID_ARG;
   TableParams p = {};
   p.seqlens = seqlens; p.new_tokens = new_tokens; p.block_table = block_table; p.free_pages = (int*)free_pages; p.free_count = free_count;
-  p.cu = cu_seqlens; p.seqlens_out = seqlens_out; p.slots = slots; p.free_out = free_count_out;
+  p.cu = cu_seqlens; p.seqlens_out = seqlens_out; p.slots = slots; p.free_out = free_count_out; p.positions = positions;
   p.B = B; p.max_pages = max_pages_per_seq; p.page_size = page_size; p.num_pages = num_pages; p.rows = rows;
   return scope.finish(launch_tables<false>(p, (cudaStream_t)cuda_stream));
+}
+
+int mala_page_tables(const int32_t* seqlens, const int32_t* new_tokens, int32_t* block_table, const int32_t* free_pages,
+                     const int32_t* free_count, int32_t* cu_seqlens, int32_t* seqlens_out, int64_t* slots,
+                     int32_t* free_count_out, int B, int max_pages_per_seq, int page_size, int num_pages, int rows,
+                     void* cuda_stream) {
+  return page_tables("mala_page_tables", seqlens, new_tokens, block_table, free_pages, free_count, cu_seqlens, seqlens_out, slots, nullptr, free_count_out,
+                     B, max_pages_per_seq, page_size, num_pages, rows, cuda_stream);
+}
+
+int mala_page_tables_positions(const int32_t* seqlens, const int32_t* new_tokens, int32_t* block_table, const int32_t* free_pages,
+                               const int32_t* free_count, int32_t* cu_seqlens, int32_t* seqlens_out, int64_t* slots,
+                               int32_t* positions, int32_t* free_count_out, int B, int max_pages_per_seq, int page_size,
+                               int num_pages, int rows, void* cuda_stream) {
+  if (rows > 0 && !positions) return MALA_ERR_INVALID_ARG;
+  return page_tables("mala_page_tables_positions", seqlens, new_tokens, block_table, free_pages, free_count, cu_seqlens, seqlens_out, slots, positions,
+                     free_count_out, B, max_pages_per_seq, page_size, num_pages, rows, cuda_stream);
 }
 
 int mala_release_pages(const uint8_t* done, const int32_t* seqlens, const int32_t* block_table, int32_t* free_pages,
@@ -544,24 +811,78 @@ int mala_cache_write_fp8(mala_tin k, mala_tin v, const int64_t* slots, mala_tout
   if (d % 16 != 0 || d > 128 || page_size == 8) return MALA_ERR_UNSUPPORTED;
   if (rows == 0) return MALA_OK;
   w.kscale = kscale; w.vscale = vscale;
-  int dev = 0, *status = nullptr;
-  MALA_TRY(current_device_checked(&dev));
-  MALA_TRY(device_setup(dev, &status));
-  // Blocks of eight warps and of so few rows that all blocks run at once (four per SM); where that would take more than eight rows
-  // each, blocks of two warps, or of four where a unit takes 32 KB, and of 64 rows (so that few blocks find nothing to do) or fewer while
-  // they run at once (16 requests of up to 40 rows, pages of 16 keys: 5.8 us, with 64 rows per block 11.0)
-  while (w.chunk < 16 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 4ll * sm_count(dev)) w.chunk *= 2;
-  const bool many = w.chunk == 16, narrow = w.cols <= 8;
-  if (many)
-    while (w.chunk < 64 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 8ll * sm_count(dev)) w.chunk *= 2;
-  const dim3 grid((unsigned)((rows + w.chunk - 1) / w.chunk), Hkv, 2);
+  return scope.finish(launch_write8<kNoTurn>(w, (cudaStream_t)cuda_stream));
+}
+
+static int check_read(mala_tin kp, mala_tin vp, const int32_t* block_table, const int32_t* seqlens, mala_tout k, mala_tout v, const int32_t* cu, int B, int Hkv,
+                      int num_pages, int page_size, int max_pages, int rows, int d, int item) {
+  if (B <= 0 || Hkv <= 0 || num_pages <= 0 || page_size <= 0 || max_pages <= 0 || rows < 0 || d <= 0) return MALA_ERR_INVALID_ARG;
+  if (!block_table || !seqlens || !cu || cu == seqlens) return MALA_ERR_INVALID_ARG;
+  if ((((uintptr_t)block_table | (uintptr_t)seqlens | (uintptr_t)cu) & 3) != 0) return MALA_ERR_MISALIGNED;
+  if (!page_size_ok(page_size) || B > kReadMaxB || Hkv > 65535 || rows > kMaxRows || (long long)max_pages * page_size > 0x7fffffffLL) return MALA_ERR_UNSUPPORTED;
+  MALA_TRY(check_cache_view(kp.p, kp.sb, kp.sn, kp.sh, num_pages, page_size, Hkv, item));
+  MALA_TRY(check_cache_view(vp.p, vp.sb, vp.sn, vp.sh, num_pages, page_size, Hkv, item));
+  if (rows == 0) return MALA_OK;
+  MALA_TRY(check_cache_view(k.p, 0, k.sn, k.sh, 1, rows, Hkv, 2));
+  return check_cache_view(v.p, 0, v.sn, v.sh, 1, rows, Hkv, 2);
+}
+
+int mala_cache_read(mala_tin kpages, mala_tin vpages, const int32_t* block_table, const int32_t* seqlens, mala_tout k_out, mala_tout v_out,
+                    int32_t* cu_seqlens, int B, int Hkv, int num_pages, int page_size, int max_pages_per_seq, int rows, int d, void* cuda_stream) {
+  ApiScope scope("mala_cache_read", cuda_stream);
+  MALA_TRY(check_read(kpages, vpages, block_table, seqlens, k_out, v_out, cu_seqlens, B, Hkv, num_pages, page_size, max_pages_per_seq, rows, d, 2));
+  if (d % 8 != 0 || d > 256) return MALA_ERR_UNSUPPORTED;
+  return scope.finish(cache_read(kpages, vpages, nullptr, nullptr, block_table, seqlens, k_out, v_out, cu_seqlens, B, Hkv, num_pages, page_size,
+                                 max_pages_per_seq, rows, d, false, (cudaStream_t)cuda_stream));
+}
+
+int mala_cache_read_fp8(mala_tin kpages8, mala_tin vpages8, const float* kscale, const float* vscale, const int32_t* block_table, const int32_t* seqlens,
+                        mala_tout k_out, mala_tout v_out, int32_t* cu_seqlens, int B, int Hkv, int num_pages, int page_size, int max_pages_per_seq,
+                        int rows, int d, void* cuda_stream) {
+  ApiScope scope("mala_cache_read_fp8", cuda_stream);
+  MALA_TRY(check_read(kpages8, vpages8, block_table, seqlens, k_out, v_out, cu_seqlens, B, Hkv, num_pages, page_size, max_pages_per_seq, rows, d, 1));
+  if (!kscale || !vscale) return MALA_ERR_INVALID_ARG;
+  if ((((uintptr_t)kscale | (uintptr_t)vscale) & 3) != 0) return MALA_ERR_MISALIGNED;
+  if (d % 16 != 0 || d > 128 || page_size == 8) return MALA_ERR_UNSUPPORTED;
+  return scope.finish(cache_read(kpages8, vpages8, kscale, vscale, block_table, seqlens, k_out, v_out, cu_seqlens, B, Hkv, num_pages, page_size,
+                                 max_pages_per_seq, rows, d, true, (cudaStream_t)cuda_stream));
+}
+
+int mala_rotary_write(mala_tin q, mala_tin k, mala_tin v, const int32_t* positions, const int64_t* slots, const mala_rotary* rotary,
+                      const mala_head_norm* norm, mala_tout q_out, mala_tout kpages, mala_tout vpages, int rows, int Hq, int Hkv, int num_pages,
+                      int page_size, int d, void* cuda_stream) {
+  ApiScope scope("mala_rotary_write", cuda_stream);
+  WriteParams w;
+  MALA_TRY(write_params(&w, k, v, slots, kpages, vpages, rows, Hkv, num_pages, page_size, d, 2));
+  MALA_TRY(check_rotary_step(q, positions, q_out, rotary, norm, rows, Hq, d));
+  if (rows == 0) return MALA_OK;
+  return scope.finish(rotary_step(q, k, v, positions, slots, q_out, kpages, vpages, rotary, norm, rows, Hq, Hkv, w.limit, page_size, d,
+                                  (cudaStream_t)cuda_stream));
+}
+
+int mala_rotary_write_fp8(mala_tin q, mala_tin k, mala_tin v, const int32_t* positions, const int64_t* slots, const mala_rotary* rotary,
+                          const mala_head_norm* norm, mala_tout q_out, mala_tout kpages8, mala_tout vpages8, float* kscale, float* vscale, int rows,
+                          int Hq, int Hkv, int num_pages, int page_size, int d, void* cuda_stream) {
+  ApiScope scope("mala_rotary_write_fp8", cuda_stream);
+  WriteParams w;
+  MALA_TRY(write_params(&w, k, v, slots, kpages8, vpages8, rows, Hkv, num_pages, page_size, d, 1));
+  if (!kscale || !vscale) return MALA_ERR_INVALID_ARG;
+  if ((((uintptr_t)kscale) & 3) != 0 || (((uintptr_t)vscale) & 3) != 0) return MALA_ERR_MISALIGNED;
+  if (d % 16 != 0 || d > 128 || page_size == 8) return MALA_ERR_UNSUPPORTED;
+  MALA_TRY(check_rotary_step(q, positions, q_out, rotary, norm, rows, Hq, d));
+  if (rows == 0) return MALA_OK;
+  w.kscale = kscale; w.vscale = vscale;
+  w.rule.inv_freq = rotary->inv_freq; w.rule.rotary = rotary->rotary; w.rule.d = d;
+  w.rule.magnitude = w.rule.turned = rotary->magnitude;
+  w.positions = positions;
+  w.normed = norm != nullptr; w.weight = norm ? norm->k_weight : nullptr; w.weights_fp32 = norm ? norm->weights_fp32 : 0;
+  w.eps = norm ? norm->eps : 0.f; w.inv_d = 1.f / (float)d;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
-  if (!many && narrow) cache_write8_kernel<256, 8><<<grid, 256, 0, stream>>>(w);
-  else if (!many) cache_write8_kernel<256, 16><<<grid, 256, 0, stream>>>(w);
-  else if (narrow) cache_write8_kernel<64, 8><<<grid, 64, 0, stream>>>(w);
-  else if (w.unit < 128) cache_write8_kernel<64, 16><<<grid, 64, 0, stream>>>(w);
-  else cache_write8_kernel<128, 16><<<grid, 128, 0, stream>>>(w);
-  return scope.finish(cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA);
+  MALA_TRY(rotary_step(q, mala_tin{nullptr, 0, 0, 0}, mala_tin{nullptr, 0, 0, 0}, positions, nullptr, q_out, mala_tout{nullptr, 0, 0, 0},
+                       mala_tout{nullptr, 0, 0, 0}, rotary, norm, rows, Hq, 0, 0, 1, d, stream));
+  const int pairs = pairs_kind(rotary->rotary, rotary->interleaved);
+  return scope.finish(pairs == kHalves ? launch_write8<kHalves>(w, stream)
+                                       : pairs == kHalvesOdd ? launch_write8<kHalvesOdd>(w, stream) : launch_write8<kNeighbours>(w, stream));
 }
 
 }  // extern "C"

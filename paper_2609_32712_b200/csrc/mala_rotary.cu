@@ -1,0 +1,551 @@
+// Rotary positions of queries and keys, with a root-mean-square norm of each head in front or without: forward, backward, and the
+// form of a serving step, whose keys and values go into the pages of a cache.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/mala.h"
+#include "mala_internal.h"
+#include "mala_rotary.cuh"
+
+namespace mala {
+
+constexpr int kMaxRows = 1 << 30;
+constexpr int kRotaryThreads = 256, kRotaryWarps = kRotaryThreads / 32;
+constexpr int kNormBlocks = 1024;          // most blocks of the norm's backward (each leaves a sum per column)
+
+// One of a call's tensors: x is read and y written, rows x heads of d columns; strides in bytes
+struct RotaryTensor {
+  const uint8_t* x; const uint8_t* g; uint8_t* y;          // (g: the incoming gradient in the norm's backward)
+  int64_t x_sb, x_sn, x_sh, g_sb, g_sn, g_sh, y_sb, y_sn, y_sh;
+  const void* weight;
+  float* dw;
+  int rows, N, H, first;                   // rows of the tensor (B * N), its heads, position index of a batch entry's first row
+  int items, span;                         // a warp's items: a row and `span` of its heads
+  FastDiv by_n, by_spans;
+};
+struct RotaryParams {
+  RotaryTensor t[3];                       // q, k, and (into pages) v
+  RotaryRule rule;
+  const int* positions; int pos_n;         // [B, pos_n], or null: a row's own index
+  const int* cu_q; const int* cu_k; int B; // packed sequences
+  const int64_t* slots; int64_t limit; int page_size; FastDiv by_page;   // into pages
+  int weights_fp32; float eps, inv_d;
+  float* partial;                          // the norm's backward: [blocks, d] sums
+  int q_blocks;
+};
+
+// Position of row t of tensor `which`; false: no sequence has it
+__device__ __forceinline__ bool position_of(const RotaryParams& p, const RotaryTensor& a, int which, int t, int b, int n, int& pos) {
+  if (p.cu_q) {
+    const int* own = which == 0 ? p.cu_q : p.cu_k;
+    int lo = 0, hi = p.B;
+    if (t < __ldg(own) || t >= __ldg(own + p.B)) return false;
+    while (hi - lo > 1) {                  // the last sequence that begins at or before t
+      const int mid = (lo + hi) >> 1;
+      if (__ldg(own + mid) <= t) lo = mid;
+      else hi = mid;
+    }
+    pos = t - __ldg(own + lo);
+    if (which == 0) pos += (__ldg(p.cu_k + lo + 1) - __ldg(p.cu_k + lo)) - (__ldg(p.cu_q + lo + 1) - __ldg(p.cu_q + lo));
+    return true;
+  }
+  pos = n + a.first;
+  if (p.positions) pos = __ldg(p.positions + (int64_t)b * p.pos_n + pos);
+  return true;
+}
+
+// Rotations.  A row of d columns lies in the registers of L lanes, eight columns each, and a warp works on 32 / L heads of a token
+// at a time, four such loads in flight: the angles of a token are worked out once for all heads that a warp takes.
+template <int L, int kPairs, bool kNorm, bool kPages>
+__global__ void __launch_bounds__(kRotaryThreads)
+rotary_kernel(const RotaryParams p) {
+  constexpr int P = 32 / L, U = 4;
+  __shared__ uint4 rows_s[kPairs == kHalvesOdd ? kRotaryWarps * 32 : 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, i = lane % L;
+  const bool mine = 8 * i < p.rule.d;
+  const int from = g * L + (mine ? partner_of<kHalves>(8 * i, p.rule.rotary) / 8 : i);
+  uint4* const buf = rows_s + (kPairs == kHalvesOdd ? warp * 32 : 0);
+  LaneTurns<kPairs> turns;
+  turns.load(p.rule, i);
+  const uint32_t nq = p.t[0].items, nk = p.t[1].items, all = nq + nk + (kPages ? p.t[2].items : 0);   // (at most 3 * 2^30)
+  for (uint32_t item = blockIdx.x * kRotaryWarps + warp; item < all; item += gridDim.x * kRotaryWarps) {
+    const int which = item < nq ? 0 : item < nq + nk ? 1 : 2, x0 = (int)(item - (which == 0 ? 0 : which == 1 ? nq : nq + nk));
+    const RotaryTensor& a = p.t[which];
+    const int t = (int)a.by_spans.div((uint32_t)x0), h0 = (x0 - t * (int)a.by_spans.d) * a.span, h1 = min(h0 + a.span, a.H);
+    const int b = (int)a.by_n.div((uint32_t)t), n = t - b * a.N;
+    int pos = 0;
+    const bool turn = which < 2 && position_of(p, a, which, t, b, n, pos);
+    const uint8_t* src = a.x + b * a.x_sb + n * a.x_sn + i * 16;
+    uint8_t* dst = a.y + i * 16;
+    if (kPages && which > 0) {
+      const int64_t slot = __ldg(p.slots + t);
+      if (slot < 0 || slot >= p.limit) continue;
+      const int64_t page = p.limit <= 0xffffffffll ? (int64_t)p.by_page.div((uint32_t)slot) : slot / p.page_size;
+      dst += page * a.y_sb + (slot - page * p.page_size) * a.y_sn;
+    } else {
+      dst += b * a.y_sb + n * a.y_sn;
+    }
+    uint4 w[U];
+    auto load = [&](int hb) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = hb + u * P + g;
+        w[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (mine && h < h1) w[u] = *reinterpret_cast<const uint4*>(src + h * a.x_sh);
+      }
+    };
+    auto store = [&](int hb) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = hb + u * P + g;
+        if (mine && h < h1) *reinterpret_cast<uint4*>(dst + h * a.y_sh) = w[u];
+      }
+    };
+    load(h0);
+    if (!turn) {                           // values, and rows that no sequence has
+      for (int hb = h0;;) {
+        store(hb);
+        if ((hb += P * U) >= h1) break;
+        load(hb);
+      }
+      continue;
+    }
+    float C[8], S[8];
+    turns.at(p.rule, i, pos, C, S);
+    if constexpr (kNorm) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = min(8 * i + e, p.rule.d - 1);
+        C[e] *= weight_at(a.weight, p.weights_fp32, c);
+        S[e] *= weight_at(a.weight, p.weights_fp32, partner_of<kPairs>(c, p.rule.rotary));
+      }
+    }
+    for (int hb = h0;;) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float x[8], y[8];
+        unpack8(w[u], x);
+        if constexpr (kPairs == kHalvesOdd) {
+          __syncwarp();
+          buf[lane] = w[u];
+          __syncwarp();
+        }
+        partners<kPairs>(w[u], x, from, reinterpret_cast<const __nv_bfloat16*>(buf + g * L), mine ? i : 0, p.rule.rotary, 0xffffffffu, y);
+        float r = 1.f;
+        if constexpr (kNorm) {
+          float sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+#pragma unroll
+          for (int m = L / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+          r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[e] *= C[e];
+          if (turns.on(e)) x[e] = fmaf(y[e], S[e], x[e]);
+          if constexpr (kNorm) x[e] *= r;
+        }
+        w[u] = pack8(x);
+      }
+      store(hb);
+      if ((hb += P * U) >= h1) break;
+      load(hb);
+    }
+  }
+}
+
+// The norm's backward, n = x r, r = (mean(x^2) + eps)^(-1/2):  with g the gradient behind the norm and its weight, rotated back,
+//   dx = r (g w - n mean(g w n)),   dw = sum over rows and heads of g n.
+// A block works on q or on k alone, keeps its sums per column in registers and leaves them in the workspace.
+template <int L, int kPairs>
+__global__ void __launch_bounds__(kRotaryThreads)
+rotary_norm_bwd_kernel(const RotaryParams p) {
+  constexpr int P = 32 / L, U = 2;
+  __shared__ uint4 rows_s[kPairs == kHalvesOdd ? kRotaryWarps * 32 : 1];
+  __shared__ float sums_s[kRotaryWarps][256];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, i = lane % L;
+  const bool mine = 8 * i < p.rule.d;
+  const int from = g * L + (mine ? partner_of<kHalves>(8 * i, p.rule.rotary) / 8 : i);
+  uint4* const buf = rows_s + (kPairs == kHalvesOdd ? warp * 32 : 0);
+  const int which = (int)blockIdx.x < p.q_blocks ? 0 : 1, block = blockIdx.x - (which ? p.q_blocks : 0);
+  const int blocks = which ? gridDim.x - p.q_blocks : p.q_blocks;
+  const RotaryTensor& a = p.t[which];
+  LaneTurns<kPairs> turns;
+  turns.load(p.rule, i);
+  float W[8], dw[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    W[e] = weight_at(a.weight, p.weights_fp32, min(8 * i + e, p.rule.d - 1));
+    dw[e] = 0.f;
+  }
+  for (int item = block * kRotaryWarps + warp; item < a.items; item += blocks * kRotaryWarps) {
+    const int t = (int)a.by_spans.div((uint32_t)item), h0 = (item - t * (int)a.by_spans.d) * a.span, h1 = min(h0 + a.span, a.H);
+    const int b = (int)a.by_n.div((uint32_t)t), n = t - b * a.N;
+    int pos = 0;
+    const bool turn = position_of(p, a, which, t, b, n, pos);
+    const uint8_t* gp = a.g + b * a.g_sb + n * a.g_sn + i * 16;
+    const uint8_t* xp = a.x + b * a.x_sb + n * a.x_sn + i * 16;
+    uint8_t* dst = a.y + b * a.y_sb + n * a.y_sn + i * 16;
+    float C[8], S[8];
+    if (turn) turns.at(p.rule, i, pos, C, S);
+    for (int hb = h0; hb < h1; hb += P * U) {
+      uint4 wg[U], wx[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = hb + u * P + g;
+        wg[u] = wx[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (mine && h < h1) {
+          wg[u] = *reinterpret_cast<const uint4*>(gp + h * a.g_sh);
+          wx[u] = *reinterpret_cast<const uint4*>(xp + h * a.x_sh);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = hb + u * P + g;
+        if (turn) {
+          float x[8], y[8], z[8];
+          unpack8(wg[u], x);
+          if constexpr (kPairs == kHalvesOdd) {
+            __syncwarp();
+            buf[lane] = wg[u];
+            __syncwarp();
+          }
+          partners<kPairs>(wg[u], x, from, reinterpret_cast<const __nv_bfloat16*>(buf + g * L), mine ? i : 0, p.rule.rotary, 0xffffffffu, y);
+          unpack8(wx[u], z);
+          float sum = 0.f, dot = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[e] *= C[e];
+            if (turns.on(e)) x[e] = fmaf(y[e], S[e], x[e]);
+            sum = fmaf(z[e], z[e], sum);
+            dot = fmaf(x[e] * W[e], z[e], dot);
+          }
+#pragma unroll
+          for (int m = L / 2; m > 0; m >>= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, m);
+            dot += __shfl_xor_sync(0xffffffffu, dot, m);
+          }
+          const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps)), back = r * r * dot * p.inv_d;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            dw[e] = fmaf(x[e], z[e] * r, dw[e]);
+            x[e] = r * fmaf(-z[e], back, x[e] * W[e]);
+          }
+          wg[u] = pack8(x);
+        }
+        if (mine && h < h1) *reinterpret_cast<uint4*>(dst + h * a.y_sh) = wg[u];
+      }
+    }
+  }
+  if (!a.dw) return;                       // (the same for all of a block)
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+#pragma unroll
+    for (int m = L; m < 32; m <<= 1) dw[e] += __shfl_xor_sync(0xffffffffu, dw[e], m);
+    if (g == 0 && mine) sums_s[warp][8 * i + e] = dw[e];
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < p.rule.d) {
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kRotaryWarps; ++w) sum += sums_s[w][threadIdx.x];
+    p.partial[(size_t)blockIdx.x * p.rule.d + threadIdx.x] = sum;
+  }
+}
+
+// dw from the blocks' sums, 32 columns by a block, in a fixed order
+__global__ void __launch_bounds__(1024)
+rotary_norm_sum_kernel(const float* partial, float* dwq, float* dwk, int d, int q_blocks, int blocks) {
+  __shared__ float sums_s[32][33];
+  wait_for_primary();
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+  float* const out = blockIdx.y ? dwk : dwq;
+  float sum = 0.f;
+  if (out && c < d)
+    for (int x = (blockIdx.y ? q_blocks : 0) + w; x < (blockIdx.y ? blocks : q_blocks); x += 32) sum += partial[(size_t)x * d + c];
+  sums_s[w][threadIdx.x & 31] = sum;
+  __syncthreads();
+  sum = sums_s[threadIdx.x & 31][w];       // (warp w: column w, a lane per share)
+#pragma unroll
+  for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+  const int mine = blockIdx.x * 32 + w;
+  if ((threadIdx.x & 31) == 0 && out && mine < d) out[mine] = sum;
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+static bool aligned16(const void* p) { return (((uintptr_t)p) & 15) == 0; }
+
+static int check_rule(const mala_rotary* r, const mala_head_norm* norm, int d) {
+  if (!r || !r->inv_freq) return MALA_ERR_INVALID_ARG;
+  if (!(r->magnitude > 0.f) || !isfinite(r->magnitude)) return MALA_ERR_INVALID_ARG;
+  if (d <= 0) return MALA_ERR_INVALID_ARG;
+  if (d % 8 != 0 || d > 256 || r->rotary < 2 || r->rotary % 2 != 0 || r->rotary > d) return MALA_ERR_UNSUPPORTED;
+  if ((((uintptr_t)r->inv_freq) & 7) != 0) return MALA_ERR_MISALIGNED;
+  if (norm) {
+    if (!(norm->eps >= 0.f) || !isfinite(norm->eps)) return MALA_ERR_INVALID_ARG;
+    const uintptr_t odd = norm->weights_fp32 ? 3 : 1;
+    if ((((uintptr_t)norm->q_weight) & odd) != 0 || (((uintptr_t)norm->k_weight) & odd) != 0) return MALA_ERR_MISALIGNED;
+  }
+  return MALA_OK;
+}
+
+static int check_heads_view(const void* p, int64_t sb, int64_t sn, int64_t sh, int B, int N, int H) {
+  if (!p) return MALA_ERR_INVALID_ARG;
+  if (!aligned16(p)) return MALA_ERR_MISALIGNED;
+  if ((B > 1 && sb <= 0) || (N > 1 && sn <= 0) || (H > 1 && sh <= 0)) return MALA_ERR_INVALID_ARG;
+  if ((B > 1 && sb % 8) || (N > 1 && sn % 8) || (H > 1 && sh % 8)) return MALA_ERR_MISALIGNED;
+  return MALA_OK;
+}
+
+static void set_rule(RotaryParams* p, const mala_rotary* r, const mala_head_norm* norm, int d, bool back) {
+  p->rule.inv_freq = r->inv_freq; p->rule.rotary = r->rotary; p->rule.d = d;
+  p->rule.magnitude = r->magnitude; p->rule.turned = back ? -r->magnitude : r->magnitude;
+  p->weights_fp32 = norm ? norm->weights_fp32 : 0; p->eps = norm ? norm->eps : 0.f; p->inv_d = 1.f / (float)d;
+  p->t[0].weight = norm ? norm->q_weight : nullptr;
+  p->t[1].weight = norm ? norm->k_weight : nullptr;
+}
+
+static void set_tensor(RotaryTensor* t, mala_tin x, mala_tout y, int B, int N, int H, int first) {
+  t->x = (const uint8_t*)x.p; t->x_sb = x.sb * 2; t->x_sn = x.sn * 2; t->x_sh = x.sh * 2;
+  t->y = (uint8_t*)y.p; t->y_sb = y.sb * 2; t->y_sn = y.sn * 2; t->y_sh = y.sh * 2;
+  t->rows = B * N; t->N = N; t->H = H; t->first = first;
+  t->by_n.set((uint32_t)N);
+}
+
+static int lanes_of(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
+
+// Heads per item: all of a row's while that leaves every SM 32 warps, fewer where there are few rows (one load of a warp at least)
+static void set_items(RotaryParams* p, int tensors, int sms) {
+  const int per = 32 / lanes_of(p->rule.d);
+  long long loads = 0;
+  for (int x = 0; x < tensors; ++x) loads += (long long)p->t[x].rows * ((p->t[x].H + per - 1) / per);
+  const long long want = loads / (32ll * sms);
+  for (int x = 0; x < tensors; ++x) {
+    RotaryTensor& t = p->t[x];
+    const int most = (t.H + per - 1) / per, take = (int)(want < 1 ? 1 : want > most ? most : want);
+    t.span = take * per;
+    const int spans = t.H > 0 ? (t.H + t.span - 1) / t.span : 1;
+    t.by_spans.set((uint32_t)spans);
+    t.items = t.rows * spans;
+  }
+}
+
+template <int L, int kPairs, bool kNorm, bool kPages>
+static int launch_rotary_as(const RotaryParams& p, int sms, cudaStream_t stream) {
+  const long long items = (long long)p.t[0].items + p.t[1].items + (kPages ? p.t[2].items : 0);
+  const long long blocks = (items + kRotaryWarps - 1) / kRotaryWarps, most = 4ll * sms;
+  if (blocks == 0) return MALA_OK;
+  rotary_kernel<L, kPairs, kNorm, kPages><<<(unsigned)(blocks < most ? blocks : most), kRotaryThreads, 0, stream>>>(p);
+  return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+}
+template <int L, bool kNorm, bool kPages>
+static int launch_rotary_by(const RotaryParams& p, int interleaved, int sms, cudaStream_t stream) {
+  switch (pairs_kind(p.rule.rotary, interleaved)) {
+    case kHalves: return launch_rotary_as<L, kHalves, kNorm, kPages>(p, sms, stream);
+    case kHalvesOdd: return launch_rotary_as<L, kHalvesOdd, kNorm, kPages>(p, sms, stream);
+    default: return launch_rotary_as<L, kNeighbours, kNorm, kPages>(p, sms, stream);
+  }
+}
+template <bool kNorm, bool kPages>
+static int launch_rotary(const RotaryParams& p, int interleaved, int sms, cudaStream_t stream) {
+  const int L = lanes_of(p.rule.d);
+  return L == 8 ? launch_rotary_by<8, kNorm, kPages>(p, interleaved, sms, stream)
+                : L == 16 ? launch_rotary_by<16, kNorm, kPages>(p, interleaved, sms, stream) : launch_rotary_by<32, kNorm, kPages>(p, interleaved, sms, stream);
+}
+
+template <int L>
+static int launch_norm_bwd_by(const RotaryParams& p, int interleaved, int blocks, cudaStream_t stream) {
+  switch (pairs_kind(p.rule.rotary, interleaved)) {
+    case kHalves: rotary_norm_bwd_kernel<L, kHalves><<<blocks, kRotaryThreads, 0, stream>>>(p); break;
+    case kHalvesOdd: rotary_norm_bwd_kernel<L, kHalvesOdd><<<blocks, kRotaryThreads, 0, stream>>>(p); break;
+    default: rotary_norm_bwd_kernel<L, kNeighbours><<<blocks, kRotaryThreads, 0, stream>>>(p);
+  }
+  return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+}
+
+static int launch_norm_bwd(RotaryParams& p, int interleaved, float* dwq, float* dwk, int sms, cudaStream_t stream) {
+  const long long nq = (p.t[0].items + kRotaryWarps - 1) / kRotaryWarps, nk = (p.t[1].items + kRotaryWarps - 1) / kRotaryWarps;
+  const long long most = 4ll * sms < kNormBlocks ? 4ll * sms : kNormBlocks;
+  // the blocks in the share of the tensors' rows and heads
+  const double loads_q = (double)p.t[0].rows * p.t[0].H, loads_k = (double)p.t[1].rows * p.t[1].H;
+  long long gq = nq, gk = nk;
+  if (gq + gk > most) {
+    gq = (long long)(most * (loads_q / (loads_q + loads_k)) + 0.5);
+    gq = gq < 1 ? 1 : gq > most - (nk > 0) ? most - (nk > 0) : gq;
+    gk = nk > 0 ? most - gq : 0;
+    gq = gq > nq ? nq : gq;
+    gk = gk > nk ? nk : gk;
+  }
+  p.q_blocks = (int)gq;
+  const int blocks = (int)(gq + gk), L = lanes_of(p.rule.d);
+  MALA_TRY(L == 8 ? launch_norm_bwd_by<8>(p, interleaved, blocks, stream)
+                  : L == 16 ? launch_norm_bwd_by<16>(p, interleaved, blocks, stream) : launch_norm_bwd_by<32>(p, interleaved, blocks, stream));
+  if (!dwq && !dwk) return MALA_OK;
+  return launch_dependent(rotary_norm_sum_kernel, dim3((p.rule.d + 31) / 32, 2), dim3(1024), stream, (const float*)p.partial, dwq, dwk, p.rule.d,
+                          p.q_blocks, blocks) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+}
+
+// What the calls have in common: q [B,Nq,Hq,d], k [B,Nk,Hkv,d] (or none), the queries being the last Nq of Nk positions; cu: packed
+struct RotaryCall {
+  int B, Nq, Nk, Hq, Hkv, d;
+  const int32_t* positions; const int32_t* cu_q; const int32_t* cu_k; int sequences;
+};
+
+static int check_call(const RotaryCall& c, bool with_k) {
+  if (c.B <= 0 || c.Nq <= 0 || c.Hq <= 0 || (with_k && c.Hkv <= 0) || c.Nk <= 0) return MALA_ERR_INVALID_ARG;
+  if ((!c.cu_q && c.Nk < c.Nq) || c.Hq > 65535 || (with_k && c.Hkv > 65535)) return MALA_ERR_UNSUPPORTED;
+  if ((long long)c.B * c.Nq > kMaxRows || (long long)c.B * c.Nk > kMaxRows) return MALA_ERR_UNSUPPORTED;
+  if ((((uintptr_t)c.positions | (uintptr_t)c.cu_q | (uintptr_t)c.cu_k) & 3) != 0) return MALA_ERR_MISALIGNED;
+  return MALA_OK;
+}
+
+// Forward; or, back: the same rotation in the other sense, from gradients to gradients (no norm)
+static int rotate(const RotaryCall& c, mala_tin q, mala_tin k, mala_tout qo, mala_tout ko, const mala_rotary* r, const mala_head_norm* norm, bool back,
+                  cudaStream_t stream) {
+  const bool with_k = k.p != nullptr || ko.p != nullptr;
+  MALA_TRY(check_call(c, with_k));
+  MALA_TRY(check_rule(r, norm, c.d));
+  MALA_TRY(check_heads_view(q.p, q.sb, q.sn, q.sh, c.B, c.Nq, c.Hq));
+  MALA_TRY(check_heads_view(qo.p, qo.sb, qo.sn, qo.sh, c.B, c.Nq, c.Hq));
+  if (with_k) {
+    MALA_TRY(check_heads_view(k.p, k.sb, k.sn, k.sh, c.B, c.Nk, c.Hkv));
+    MALA_TRY(check_heads_view(ko.p, ko.sb, ko.sn, ko.sh, c.B, c.Nk, c.Hkv));
+  }
+  int dev = 0, *status = nullptr;
+  MALA_TRY(current_device_checked(&dev));
+  MALA_TRY(device_setup(dev, &status));
+  RotaryParams p = {};
+  set_rule(&p, r, norm, c.d, back);
+  set_tensor(&p.t[0], q, qo, c.B, c.Nq, c.Hq, c.Nk - c.Nq);
+  if (with_k) set_tensor(&p.t[1], k, ko, c.B, c.Nk, c.Hkv, 0);
+  p.positions = c.positions; p.pos_n = c.Nk;
+  p.cu_q = c.cu_q; p.cu_k = c.cu_k; p.B = c.sequences;
+  set_items(&p, with_k ? 2 : 1, sm_count(dev));
+  return norm ? launch_rotary<true, false>(p, r->interleaved, sm_count(dev), stream) : launch_rotary<false, false>(p, r->interleaved, sm_count(dev), stream);
+}
+
+static int rotate_back(const RotaryCall& c, mala_tin dq, mala_tin dk, mala_tin q, mala_tin k, mala_tout dqo, mala_tout dko, const mala_rotary* r,
+                       const mala_head_norm* norm, float* dwq, float* dwk, void* ws, size_t ws_bytes, cudaStream_t stream) {
+  const bool with_k = dk.p != nullptr || dko.p != nullptr;
+  if (!norm) {
+    if (dwq || dwk) return MALA_ERR_INVALID_ARG;
+    return rotate(c, dq, dk, dqo, dko, r, nullptr, true, stream);
+  }
+  MALA_TRY(check_call(c, with_k));
+  MALA_TRY(check_rule(r, norm, c.d));
+  MALA_TRY(check_heads_view(dq.p, dq.sb, dq.sn, dq.sh, c.B, c.Nq, c.Hq));
+  MALA_TRY(check_heads_view(q.p, q.sb, q.sn, q.sh, c.B, c.Nq, c.Hq));
+  MALA_TRY(check_heads_view(dqo.p, dqo.sb, dqo.sn, dqo.sh, c.B, c.Nq, c.Hq));
+  if (with_k) {
+    MALA_TRY(check_heads_view(dk.p, dk.sb, dk.sn, dk.sh, c.B, c.Nk, c.Hkv));
+    MALA_TRY(check_heads_view(k.p, k.sb, k.sn, k.sh, c.B, c.Nk, c.Hkv));
+    MALA_TRY(check_heads_view(dko.p, dko.sb, dko.sn, dko.sh, c.B, c.Nk, c.Hkv));
+  }
+  if ((dwq && !norm->q_weight) || (dwk && (!norm->k_weight || !with_k))) return MALA_ERR_INVALID_ARG;
+  if ((((uintptr_t)dwq | (uintptr_t)dwk) & 3) != 0) return MALA_ERR_MISALIGNED;
+  if (dwq || dwk) {
+    if (!ws) return MALA_ERR_INVALID_ARG;
+    if ((((uintptr_t)ws) & 255) != 0) return MALA_ERR_MISALIGNED;
+    if (ws_bytes < mala_rotary_workspace_bytes(c.d)) return MALA_ERR_WORKSPACE_TOO_SMALL;
+  }
+  int dev = 0, *status = nullptr;
+  MALA_TRY(current_device_checked(&dev));
+  MALA_TRY(device_setup(dev, &status));
+  RotaryParams p = {};
+  set_rule(&p, r, norm, c.d, true);
+  set_tensor(&p.t[0], q, dqo, c.B, c.Nq, c.Hq, c.Nk - c.Nq);
+  p.t[0].g = (const uint8_t*)dq.p; p.t[0].g_sb = dq.sb * 2; p.t[0].g_sn = dq.sn * 2; p.t[0].g_sh = dq.sh * 2;
+  p.t[0].dw = dwq;
+  if (with_k) {
+    set_tensor(&p.t[1], k, dko, c.B, c.Nk, c.Hkv, 0);
+    p.t[1].g = (const uint8_t*)dk.p; p.t[1].g_sb = dk.sb * 2; p.t[1].g_sn = dk.sn * 2; p.t[1].g_sh = dk.sh * 2;
+    p.t[1].dw = dwk;
+  }
+  p.positions = c.positions; p.pos_n = c.Nk;
+  p.cu_q = c.cu_q; p.cu_k = c.cu_k; p.B = c.sequences;
+  p.partial = (float*)ws;
+  set_items(&p, with_k ? 2 : 1, sm_count(dev));
+  return launch_norm_bwd(p, r->interleaved, dwq, dwk, sm_count(dev), stream);
+}
+
+static int packed_call(RotaryCall* c, const int32_t* cu_q, const int32_t* cu_k, int B, int total_q, int total_k, int Hq, int Hkv, int d) {
+  if (!cu_q || !cu_k || B <= 0) return MALA_ERR_INVALID_ARG;
+  *c = RotaryCall{1, total_q, total_k, Hq, Hkv, d, nullptr, cu_q, cu_k, B};
+  return MALA_OK;
+}
+
+// A serving step, bf16 pages: q to q_out, k and v into their slots.  (Also q alone, in front of the e4m3 write.)
+int rotary_step(mala_tin q, mala_tin k, mala_tin v, const int32_t* positions, const int64_t* slots, mala_tout qo, mala_tout kp, mala_tout vp,
+                const mala_rotary* r, const mala_head_norm* norm, int rows, int Hq, int Hkv, int64_t limit, int page_size, int d, cudaStream_t stream) {
+  int dev = 0, *status = nullptr;
+  MALA_TRY(current_device_checked(&dev));
+  MALA_TRY(device_setup(dev, &status));
+  RotaryParams p = {};
+  set_rule(&p, r, norm, d, false);
+  set_tensor(&p.t[0], q, qo, 1, rows, Hq, 0);
+  if (k.p) {
+    set_tensor(&p.t[1], k, kp, 1, rows, Hkv, 0);
+    set_tensor(&p.t[2], v, vp, 1, rows, Hkv, 0);
+    p.slots = slots; p.limit = limit; p.page_size = page_size; p.by_page.set((uint32_t)page_size);
+  }
+  p.positions = positions; p.pos_n = rows;
+  set_items(&p, k.p ? 3 : 1, sm_count(dev));
+  return norm ? launch_rotary<true, true>(p, r->interleaved, sm_count(dev), stream) : launch_rotary<false, true>(p, r->interleaved, sm_count(dev), stream);
+}
+
+int check_rotary_step(mala_tin q, const int32_t* positions, mala_tout qo, const mala_rotary* r, const mala_head_norm* norm, int rows, int Hq, int d) {
+  if (rows < 0 || Hq <= 0) return MALA_ERR_INVALID_ARG;
+  if (rows > kMaxRows || Hq > 65535) return MALA_ERR_UNSUPPORTED;
+  MALA_TRY(check_rule(r, norm, d));
+  if (rows == 0) return MALA_OK;
+  if (!positions) return MALA_ERR_INVALID_ARG;
+  if ((((uintptr_t)positions) & 3) != 0) return MALA_ERR_MISALIGNED;
+  MALA_TRY(check_heads_view(q.p, 0, q.sn, q.sh, 1, rows, Hq));
+  return check_heads_view(qo.p, 0, qo.sn, qo.sh, 1, rows, Hq);
+}
+
+}  // namespace mala
+
+using namespace mala;
+
+extern "C" {
+
+size_t mala_rotary_workspace_bytes(int d) { return d > 0 && d <= 256 && d % 8 == 0 ? (size_t)kNormBlocks * d * sizeof(float) : 0; }
+
+int mala_rotary_fwd(mala_tin q, mala_tin k, const int32_t* positions, const mala_rotary* rotary, const mala_head_norm* norm, mala_tout q_out,
+                    mala_tout k_out, int B, int Nq, int Nk, int Hq, int Hkv, int d, void* cuda_stream) {
+  ApiScope scope("mala_rotary_fwd", cuda_stream);
+  return scope.finish(rotate(RotaryCall{B, Nq, Nk, Hq, Hkv, d, positions, nullptr, nullptr, 0}, q, k, q_out, k_out, rotary, norm, false, (cudaStream_t)cuda_stream));
+}
+
+int mala_rotary_bwd(mala_tin dq, mala_tin dk, mala_tin q, mala_tin k, const int32_t* positions, const mala_rotary* rotary, const mala_head_norm* norm,
+                    mala_tout dq_out, mala_tout dk_out, float* dq_weight, float* dk_weight, int B, int Nq, int Nk, int Hq, int Hkv, int d, void* ws,
+                    size_t ws_bytes, void* cuda_stream) {
+  ApiScope scope("mala_rotary_bwd", cuda_stream);
+  return scope.finish(rotate_back(RotaryCall{B, Nq, Nk, Hq, Hkv, d, positions, nullptr, nullptr, 0}, dq, dk, q, k, dq_out, dk_out, rotary, norm, dq_weight,
+                                  dk_weight, ws, ws_bytes, (cudaStream_t)cuda_stream));
+}
+
+int mala_rotary_fwd_varlen(mala_tin q, mala_tin k, const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, const mala_rotary* rotary,
+                           const mala_head_norm* norm, mala_tout q_out, mala_tout k_out, int B, int Hq, int Hkv, int total_q, int total_k, int d,
+                           void* cuda_stream) {
+  ApiScope scope("mala_rotary_fwd_varlen", cuda_stream);
+  RotaryCall c;
+  MALA_TRY(packed_call(&c, cu_seqlens_q, cu_seqlens_k, B, total_q, total_k, Hq, Hkv, d));
+  return scope.finish(rotate(c, q, k, q_out, k_out, rotary, norm, false, (cudaStream_t)cuda_stream));
+}
+
+int mala_rotary_bwd_varlen(mala_tin dq, mala_tin dk, mala_tin q, mala_tin k, const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k,
+                           const mala_rotary* rotary, const mala_head_norm* norm, mala_tout dq_out, mala_tout dk_out, float* dq_weight, float* dk_weight,
+                           int B, int Hq, int Hkv, int total_q, int total_k, int d, void* ws, size_t ws_bytes, void* cuda_stream) {
+  ApiScope scope("mala_rotary_bwd_varlen", cuda_stream);
+  RotaryCall c;
+  MALA_TRY(packed_call(&c, cu_seqlens_q, cu_seqlens_k, B, total_q, total_k, Hq, Hkv, d));
+  return scope.finish(rotate_back(c, dq, dk, q, k, dq_out, dk_out, rotary, norm, dq_weight, dk_weight, ws, ws_bytes, (cudaStream_t)cuda_stream));
+}
+
+}  // extern "C"

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 from typing import Optional
 
@@ -42,6 +43,16 @@ class _Stats(ctypes.Structure):
 class _RelBias(ctypes.Structure):
     _fields_ = [("table", ctypes.c_void_p), ("sb", ctypes.c_int64), ("num_buckets", ctypes.c_int),
                 ("max_distance", ctypes.c_int), ("bidirectional", ctypes.c_int)]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rotary", ctypes.c_int), ("interleaved", ctypes.c_int),
+                ("magnitude", ctypes.c_float)]
+
+
+class _HeadNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("weights_fp32", ctypes.c_int),
+                ("eps", ctypes.c_float)]
 
 
 def lib():
@@ -116,6 +127,25 @@ def lib():
         L.mala_cache_write.argtypes = [_TIn, _TIn, vp, _TOut, _TOut, i, i, i, i, i, vp]
         L.mala_cache_write_fp8.argtypes = [_TIn, _TIn, vp, _TOut, _TOut, vp, vp, i, i, i, i, i, vp]
         for n in ("mala_page_tables", "mala_release_pages", "mala_cache_write", "mala_cache_write_fp8"):
+            getattr(L, n).restype = i
+        L.mala_page_tables_positions.argtypes = [vp] * 10 + [i] * 5 + [vp]
+        L.mala_cache_read.argtypes = [_TIn, _TIn, vp, vp, _TOut, _TOut, vp] + [i] * 7 + [vp]
+        L.mala_cache_read_fp8.argtypes = [_TIn, _TIn, vp, vp, vp, vp, _TOut, _TOut, vp] + [i] * 7 + [vp]
+        L.mala_fwd_paged_fp8.argtypes = [_TIn, _TIn, _TIn, vp, vp, vp, vp, vp, _TOut, vp, ctypes.POINTER(_Stats)] + [i] * 11 + \
+            [f, f, vp, sz, vp]
+        L.mala_paged_fp8_workspace_bytes.argtypes = [i] * 4
+        rp, np_ = ctypes.POINTER(_Rotary), ctypes.POINTER(_HeadNorm)
+        L.mala_rotary_fwd.argtypes = [_TIn, _TIn, vp, rp, np_, _TOut, _TOut] + [i] * 6 + [vp]
+        L.mala_rotary_bwd.argtypes = [_TIn, _TIn, _TIn, _TIn, vp, rp, np_, _TOut, _TOut, vp, vp] + [i] * 6 + [vp, sz, vp]
+        L.mala_rotary_fwd_varlen.argtypes = [_TIn, _TIn, vp, vp, rp, np_, _TOut, _TOut] + [i] * 6 + [vp]
+        L.mala_rotary_bwd_varlen.argtypes = [_TIn, _TIn, _TIn, _TIn, vp, vp, rp, np_, _TOut, _TOut, vp, vp] + [i] * 6 + [vp, sz, vp]
+        L.mala_rotary_write.argtypes = [_TIn, _TIn, _TIn, vp, vp, rp, np_, _TOut, _TOut, _TOut] + [i] * 6 + [vp]
+        L.mala_rotary_write_fp8.argtypes = [_TIn, _TIn, _TIn, vp, vp, rp, np_, _TOut, _TOut, _TOut, vp, vp] + [i] * 6 + [vp]
+        L.mala_rotary_workspace_bytes.argtypes = [i]
+        for n in ("mala_paged_fp8_workspace_bytes", "mala_rotary_workspace_bytes"):
+            getattr(L, n).restype = sz
+        for n in ("mala_page_tables_positions", "mala_cache_read", "mala_cache_read_fp8", "mala_fwd_paged_fp8", "mala_rotary_fwd",
+                  "mala_rotary_bwd", "mala_rotary_fwd_varlen", "mala_rotary_bwd_varlen", "mala_rotary_write", "mala_rotary_write_fp8"):
             getattr(L, n).restype = i
         L.mala_test_expire_wait.argtypes = [ctypes.c_longlong, vp]
         L.mala_test_expire_wait.restype = i
@@ -741,16 +771,25 @@ def _ints(*ts):
         assert t.dtype is torch.int32 and t.is_contiguous(), "expects contiguous int32 tensors"
 
 
-def page_tables(seqlens, new_tokens, block_table, free_pages, free_count, page_size: int, rows: int):
+def page_tables(seqlens, new_tokens, block_table, free_pages, free_count, page_size: int, rows: int, positions: bool = False):
     """mala_page_tables: pages for the new tokens of a serving step.  seqlens, new_tokens int32 [B]; block_table int32
     [B, max_pages_per_seq] (its new entries are written); free_pages int32 [num_pages], free_count int32 [1]; rows: how many
     slots to write (at least the sum of new_tokens for all of them).  Returns (cu_seqlens int32 [B+1], seqlens int32 [B],
-    slots int64 [rows], free_count int32 [1])."""
+    slots int64 [rows], free_count int32 [1]), and with positions the new tokens' positions int32 [rows] behind them."""
     _ints(seqlens, new_tokens, block_table, free_pages, free_count)
     B, max_pages = block_table.shape
     assert seqlens.shape == (B,) and new_tokens.shape == (B,) and free_count.shape == (1,)
     cu, lens, left = seqlens.new_empty(B + 1), seqlens.new_empty(B), seqlens.new_empty(1)
     slots = seqlens.new_empty(rows, dtype=torch.int64)
+    if positions:
+        pos = seqlens.new_empty(rows)
+        rc = lib().mala_page_tables_positions(seqlens.data_ptr(), new_tokens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
+                                              free_count.data_ptr(), cu.data_ptr(), lens.data_ptr(), slots.data_ptr(),
+                                              pos.data_ptr(), left.data_ptr(), B, max_pages, page_size, free_pages.numel(), rows,
+                                              _here(seqlens, new_tokens, block_table, free_pages, free_count))
+        if rc != 0:
+            raise MalaError(rc, "mala_page_tables_positions")
+        return cu, lens, slots, left, pos
     rc = lib().mala_page_tables(seqlens.data_ptr(), new_tokens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
                                 free_count.data_ptr(), cu.data_ptr(), lens.data_ptr(), slots.data_ptr(), left.data_ptr(), B,
                                 max_pages, page_size, free_pages.numel(), rows,
@@ -810,3 +849,303 @@ def cache_write_fp8(k, v, slots, kpages8, vpages8, kscale, vscale) -> None:
                                     page_size, d, _here(k, v, slots, kpages8, vpages8, kscale, vscale))
     if rc != 0:
         raise MalaError(rc, "mala_cache_write_fp8")
+
+
+def _scales(kscale, vscale, num_pages: int, Hkv: int, page_size: int):
+    for t in (kscale, vscale):
+        assert t.dtype is _F32 and t.is_contiguous() and tuple(t.shape) == (num_pages, Hkv, max(1, page_size // 128))
+
+
+def cache_read(kpages, vpages, block_table, seqlens, rows: int):
+    """mala_cache_read: keys and values of the requests of block_table int32 [B, max_pages_per_seq] with seqlens int32 [B] tokens
+    out of bf16 pages [num_pages, page_size, Hkv, d], packed.  rows: how many rows to make room for (at least the sum of the lengths for all
+    of them).  Returns (k, v [1,rows,Hkv,d] bf16, cu_seqlens int32 [B+1]), as ``fwd_varlen_prefix`` takes them."""
+    return _cache_read(kpages, vpages, None, None, block_table, seqlens, rows)
+
+
+def cache_read_fp8(kpages8, vpages8, kscale, vscale, block_table, seqlens, rows: int):
+    """mala_cache_read_fp8: the same out of e4m3 pages (uint8 or float8_e4m3fn) with their scales fp32
+    [num_pages, Hkv, max(1, page_size/128)]."""
+    return _cache_read(kpages8, vpages8, kscale, vscale, block_table, seqlens, rows)
+
+
+def _cache_read(kp, vp, ks, vs, block_table, seqlens, rows):
+    _ints(block_table, seqlens)
+    num_pages, page_size, Hkv, d = kp.shape
+    B, max_pages = block_table.shape
+    assert seqlens.shape == (B,) and kp.shape == vp.shape
+    if ks is not None:
+        _scales(ks, vs, num_pages, Hkv, page_size)
+    k, v = (kp.new_empty((1, rows, Hkv, d), dtype=_BF16) for _ in range(2))
+    cu = seqlens.new_empty(B + 1)
+    stream = _here(kp, vp, ks, vs, block_table, seqlens)
+    tail = (block_table.data_ptr(), seqlens.data_ptr(), _view(k, _TOut), _view(v, _TOut), cu.data_ptr(), B, Hkv, num_pages, page_size,
+            max_pages, rows, d, stream)
+    if ks is None:
+        rc, name = lib().mala_cache_read(_view(kp, _TIn), _view(vp, _TIn), *tail), "mala_cache_read"
+    else:
+        rc, name = lib().mala_cache_read_fp8(_view8(kp), _view8(vp), ks.data_ptr(), vs.data_ptr(), *tail), "mala_cache_read_fp8"
+    if rc != 0:
+        raise MalaError(rc, name)
+    return k, v, cu
+
+
+def fwd_paged_fp8(q, kpages8, vpages8, kscale, vscale, cu_seqlens_q, block_table, seqlens_k, max_seqlen_q: int, total_k: int,
+                  scale: float, tau: float, causal: bool = True, stats: bool = False, ws=None):
+    """mala_fwd_paged_fp8: ``fwd_paged`` over e4m3 pages with their scales; total_k: at least the sum of seqlens_k (room in the
+    workspace).  Returns (o, lse [Hq,total_q], Stats or None)."""
+    one, total_q, Hq, d = q.shape
+    num_pages, page_size, Hkv = kpages8.shape[0], kpages8.shape[1], kpages8.shape[2]
+    B, max_pages = block_table.shape
+    _ints(cu_seqlens_q, block_table, seqlens_k)
+    assert one == 1 and cu_seqlens_q.shape == (B + 1,) and seqlens_k.shape == (B,)
+    assert kpages8.shape == vpages8.shape and kpages8.shape[3] == d
+    _scales(kscale, vscale, num_pages, Hkv, page_size)
+    o = torch.empty_like(q)
+    lse = q.new_empty((Hq, total_q), dtype=_F32)
+    Tq, Tk = -(-(max_seqlen_q + 127) // 128), -(-min(max_pages * page_size, total_k) // 128)
+    st = Stats((B, Hq, Tq), -(-Tk // 32), q.device) if stats else None
+    ws = _ws(int(lib().mala_paged_fp8_workspace_bytes(B, Hkv, total_k, d)), q.device) if ws is None else ws
+    rc = lib().mala_fwd_paged_fp8(_view(q, _TIn), _view8(kpages8), _view8(vpages8), kscale.data_ptr(), vscale.data_ptr(),
+                                  cu_seqlens_q.data_ptr(), block_table.data_ptr(), seqlens_k.data_ptr(), _view(o, _TOut),
+                                  lse.data_ptr(), ctypes.byref(st.c) if st else None, B, Hq, Hkv, total_q, max_seqlen_q, total_k,
+                                  num_pages, page_size, max_pages, d, int(causal), scale, tau, ws.data_ptr(), ws.numel(),
+                                  _here(q, kpages8, vpages8, kscale, vscale, cu_seqlens_q, block_table, seqlens_k, ws))
+    if rc != 0:
+        raise MalaError(rc, "mala_fwd_paged_fp8")
+    return o, lse, st
+
+
+def rotary_frequencies(rotary: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0, original: int = 8192,
+                       fast: float = 32.0, slow: float = 1.0, low: float = 1.0, high: float = 4.0):
+    """(radians per position of the ``rotary // 2`` pairs, float64 on the host; the magnitude) for ``Rotary``: base ** (-2 i / rotary),
+    for contexts of ``factor`` times the ``original`` length
+
+    - ``"linear"``: divided by factor;
+    - ``"ntk"``: with the base raised to base * factor ** (rotary / (rotary - 2)), which divides the last pair's by factor;
+    - ``"yarn"`` (Peng et al., 2023): pairs that make ``fast`` turns and more within the original length as they are, those below
+      ``slow`` divided by factor, a ramp over the pairs between; magnitude 0.1 ln(factor) + 1;
+    - ``"bands"``: by wavelength, those up to original / high as they are, beyond original / low divided by factor, blended between.
+    """
+    assert rotary >= 2 and rotary % 2 == 0 and base > 0 and factor > 0 and original > 0
+    i = torch.arange(rotary // 2, dtype=torch.float64)
+    f = base ** (-2 * i / rotary)
+    if scaling is None:
+        return f, 1.0
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling == "ntk":
+        return (f if rotary == 2 else (base * factor ** (rotary / (rotary - 2))) ** (-2 * i / rotary)), 1.0
+    if scaling == "yarn":
+        at = [rotary * math.log(original / (turns * 2 * math.pi)) / (2 * math.log(base)) for turns in (fast, slow)]
+        lo, hi = max(math.floor(at[0]), 0), min(math.ceil(at[1]), rotary - 1)
+        ramp = ((i - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
+        return f / factor * ramp + f * (1 - ramp), (0.1 * math.log(factor) + 1 if factor > 1 else 1.0)
+    if scaling == "bands":
+        keep = ((original * f / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
+        return f / factor * (1 - keep) + f * keep, 1.0
+    raise ValueError(f"unknown scaling {scaling!r}")
+
+
+class Rotary:
+    """Rotary positions: ``inv_freq`` (radians per position, one per pair of columns; kept as float64 on the device) for the first
+    2 * len(inv_freq) columns of a head, paired as halves or, interleaved, as neighbours; ``magnitude`` scales the rotated columns."""
+
+    def __init__(self, inv_freq: torch.Tensor, interleaved: bool = False, magnitude: float = 1.0, device=None):
+        assert inv_freq.dim() == 1 and inv_freq.numel() >= 1 and inv_freq.is_floating_point(), "expects a frequency per pair of columns"
+        if device is None and not inv_freq.is_cuda:
+            device = "cuda"
+        self.inv_freq = inv_freq.detach().to(device=device, dtype=torch.float64).contiguous()
+        self.rotary, self.interleaved, self.magnitude = 2 * inv_freq.numel(), bool(interleaved), float(magnitude)
+        self.c = _Rotary(self.inv_freq.data_ptr(), self.rotary, int(self.interleaved), self.magnitude)
+
+
+class HeadNorm:
+    """A root-mean-square norm of each head's row in front of its rotation: x / sqrt(mean(x^2) + eps) * weight, with weights [d] for
+    queries and keys (bf16 or fp32, the same for both; None: 1)."""
+
+    def __init__(self, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor], eps: float = 1e-6):
+        both = [w for w in (q_weight, k_weight) if w is not None]
+        for w in both:
+            assert w.dim() == 1 and w.is_contiguous() and w.dtype in (_BF16, _F32) and w.dtype == both[0].dtype and w.shape == both[0].shape, \
+                "expects contiguous weights [d] of one type, bf16 or fp32"
+        self.q_weight, self.k_weight, self.eps = q_weight, k_weight, float(eps)
+        self.fp32 = int(bool(both) and both[0].dtype is _F32)
+
+    def _for(self, d: int):
+        for w in (self.q_weight, self.k_weight):
+            assert w is None or w.shape == (d,), "a weight per column of a head"
+        q, k = (None if w is None else w.data_ptr() for w in (self.q_weight, self.k_weight))
+        self.c = _HeadNorm(q, k, self.fp32, self.eps)
+        return ctypes.byref(self.c)
+
+
+def _norm_of(norm: Optional[HeadNorm], d: int):
+    return (None, None, None) if norm is None else (norm._for(d), norm.q_weight, norm.k_weight)
+
+
+_NO_IN, _NO_OUT = _TIn(None, 0, 0, 0), _TOut(None, 0, 0, 0)
+
+
+def _like(x, out):
+    """A new tensor for rotated rows (contiguous, whatever wider tensor x is a part of), or the given one."""
+    if out is None:
+        return x.new_empty(x.shape)
+    assert out.shape == x.shape
+    return out
+
+
+def _positions(positions, B: int, Nq: int, Nk: int):
+    if positions is None:
+        return None
+    _ints(positions)
+    assert positions.shape == (B, Nk) and Nk >= Nq, "expects a position per row of k (or of q, without keys)"
+    return positions.data_ptr()
+
+
+def rotary(q, k, rot: Rotary, positions=None, norm: Optional[HeadNorm] = None, q_out=None, k_out=None):
+    """mala_rotary_fwd: rotary positions of q [B,Nq,Hq,d] and k [B,Nk,Hkv,d] (or None), bf16.  The queries are the last Nq of the Nk
+    positions; positions int32 [B,Nk] (default 0 .. Nk - 1).  q_out, k_out may be q and k themselves.  Returns (q', k')."""
+    B, Nq, Hq, d = q.shape
+    Nk, Hkv = (Nq, 0) if k is None else k.shape[1:3]
+    assert k is None or (k.shape[0] == B and k.shape[3] == d)
+    qo, ko = _like(q, q_out), None if k is None else _like(k, k_out)
+    n, wq, wk = _norm_of(norm, d)
+    rc = lib().mala_rotary_fwd(_view(q, _TIn), _NO_IN if k is None else _view(k, _TIn), _positions(positions, B, Nq, Nk),
+                               ctypes.byref(rot.c), n, _view(qo, _TOut), _NO_OUT if k is None else _view(ko, _TOut), B, Nq, Nk, Hq,
+                               Hkv, d, _here(q, k, positions, rot.inv_freq, qo, ko, wq, wk))
+    if rc != 0:
+        raise MalaError(rc, "mala_rotary_fwd")
+    return qo, ko
+
+
+def _rotary_grads(norm, d: int, with_k: bool, weights: bool, q):
+    """(dq_weight, dk_weight, ws) of a backward call: where there is a weight."""
+    if norm is None or not weights:
+        return None, None, None
+    dwq = q.new_empty(d, dtype=_F32) if norm.q_weight is not None else None
+    dwk = q.new_empty(d, dtype=_F32) if norm.k_weight is not None and with_k else None
+    ws = _ws(int(lib().mala_rotary_workspace_bytes(d)), q.device) if dwq is not None or dwk is not None else None
+    return dwq, dwk, ws
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def rotary_bwd(dq, dk, rot: Rotary, positions=None, norm: Optional[HeadNorm] = None, q=None, k=None, dq_out=None, dk_out=None,
+               weights: bool = True):
+    """mala_rotary_bwd: the gradients of q and k from those of rotary's outputs, dq and dk (or None); with a norm q and k as they went into it.
+    dq_out, dk_out may be dq and dk themselves.  Returns (dq, dk, dq_weight, dk_weight), the weights' fp32 [d], None where there is
+    none (or with weights false)."""
+    B, Nq, Hq, d = dq.shape
+    Nk, Hkv = (Nq, 0) if dk is None else dk.shape[1:3]
+    assert dk is None or (dk.shape[0] == B and dk.shape[3] == d)
+    if norm is not None:
+        assert q is not None and q.shape == dq.shape and (dk is None or (k is not None and k.shape == dk.shape)), "with a norm: q and k"
+    else:
+        q = k = None
+    if dk is None:
+        k = None
+    qo, ko = _like(dq, dq_out), None if dk is None else _like(dk, dk_out)
+    n, wq, wk = _norm_of(norm, d)
+    dwq, dwk, ws = _rotary_grads(norm, d, dk is not None, weights, dq)
+    rc = lib().mala_rotary_bwd(_view(dq, _TIn), _NO_IN if dk is None else _view(dk, _TIn), _NO_IN if q is None else _view(q, _TIn),
+                               _NO_IN if k is None else _view(k, _TIn), _positions(positions, B, Nq, Nk), ctypes.byref(rot.c), n,
+                               _view(qo, _TOut), _NO_OUT if dk is None else _view(ko, _TOut), _ptr(dwq), _ptr(dwk), B, Nq, Nk, Hq, Hkv,
+                               d, _ptr(ws), 0 if ws is None else ws.numel(), _here(dq, dk, q, k, positions, rot.inv_freq, qo, ko, wq, wk))
+    if rc != 0:
+        raise MalaError(rc, "mala_rotary_bwd")
+    return qo, ko, dwq, dwk
+
+
+def _packed(cu_q, cu_k, q, k):
+    _ints(cu_q, cu_k)
+    assert cu_q.shape == cu_k.shape and cu_q.dim() == 1 and q.shape[0] == 1
+    assert k is None or (k.shape[0] == 1 and k.shape[3] == q.shape[3])
+    return cu_q.numel() - 1
+
+
+def rotary_varlen(q, k, cu_seqlens_q, cu_seqlens_k, rot: Rotary, norm: Optional[HeadNorm] = None, q_out=None, k_out=None):
+    """mala_rotary_fwd_varlen: rotary on packed sequences, q [1,total_q,Hq,d], k [1,total_k,Hkv,d] (or None) with offsets int32 [B+1] on
+    the device (the same tensor twice for self attention); positions count within a sequence's keys.  Returns (q', k')."""
+    one, total_q, Hq, d = q.shape
+    B = _packed(cu_seqlens_q, cu_seqlens_k, q, k)
+    total_k, Hkv = (total_q, 0) if k is None else k.shape[1:3]
+    qo, ko = _like(q, q_out), None if k is None else _like(k, k_out)
+    n, wq, wk = _norm_of(norm, d)
+    rc = lib().mala_rotary_fwd_varlen(_view(q, _TIn), _NO_IN if k is None else _view(k, _TIn), cu_seqlens_q.data_ptr(),
+                                      cu_seqlens_k.data_ptr(), ctypes.byref(rot.c), n, _view(qo, _TOut),
+                                      _NO_OUT if k is None else _view(ko, _TOut), B, Hq, Hkv, total_q, total_k, d,
+                                      _here(q, k, cu_seqlens_q, cu_seqlens_k, rot.inv_freq, qo, ko, wq, wk))
+    if rc != 0:
+        raise MalaError(rc, "mala_rotary_fwd_varlen")
+    return qo, ko
+
+
+def rotary_varlen_bwd(dq, dk, cu_seqlens_q, cu_seqlens_k, rot: Rotary, norm: Optional[HeadNorm] = None, q=None, k=None, dq_out=None,
+                      dk_out=None, weights: bool = True):
+    """mala_rotary_bwd_varlen: as rotary_bwd, on packed sequences."""
+    one, total_q, Hq, d = dq.shape
+    B = _packed(cu_seqlens_q, cu_seqlens_k, dq, dk)
+    total_k, Hkv = (total_q, 0) if dk is None else dk.shape[1:3]
+    if norm is not None:
+        assert q is not None and q.shape == dq.shape and (dk is None or (k is not None and k.shape == dk.shape)), "with a norm: q and k"
+    else:
+        q = k = None
+    if dk is None:
+        k = None
+    qo, ko = _like(dq, dq_out), None if dk is None else _like(dk, dk_out)
+    n, wq, wk = _norm_of(norm, d)
+    dwq, dwk, ws = _rotary_grads(norm, d, dk is not None, weights, dq)
+    rc = lib().mala_rotary_bwd_varlen(_view(dq, _TIn), _NO_IN if dk is None else _view(dk, _TIn), _NO_IN if q is None else _view(q, _TIn),
+                                      _NO_IN if k is None else _view(k, _TIn), cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(),
+                                      ctypes.byref(rot.c), n, _view(qo, _TOut), _NO_OUT if dk is None else _view(ko, _TOut), _ptr(dwq),
+                                      _ptr(dwk), B, Hq, Hkv, total_q, total_k, d, _ptr(ws), 0 if ws is None else ws.numel(),
+                                      _here(dq, dk, q, k, cu_seqlens_q, cu_seqlens_k, rot.inv_freq, qo, ko, wq, wk))
+    if rc != 0:
+        raise MalaError(rc, "mala_rotary_bwd_varlen")
+    return qo, ko, dwq, dwk
+
+
+def _step(q, k, v, positions, slots, kpages, vpages, out, rot, norm):
+    """What the calls of a serving step check alike; (q_out, rows, Hq, Hkv, num_pages, page_size, d, norm, stream)."""
+    rows, Hq, d = q.shape
+    Hkv = k.shape[1]
+    assert k.shape == v.shape == (rows, Hkv, d) and slots.dtype is torch.int64 and slots.is_contiguous() and slots.shape == (rows,)
+    _ints(positions)
+    assert positions.shape == (rows,) and kpages.shape == vpages.shape and kpages.shape[2:] == (Hkv, d)
+    qo = _like(q, out)
+    n, wq, wk = _norm_of(norm, d)
+    return qo, rows, Hq, Hkv, kpages.shape[0], kpages.shape[1], d, n, _here(q, k, v, positions, slots, kpages, vpages, qo, rot.inv_freq, wq, wk)
+
+
+def _rows_out(t: torch.Tensor):
+    x = _rows(t)
+    return _TOut(x.p, 0, x.sn, x.sh)
+
+
+def rotary_write(q, k, v, positions, slots, kpages, vpages, rot: Rotary, norm: Optional[HeadNorm] = None, q_out=None):
+    """mala_rotary_write: a serving step's rows q [rows,Hq,d], k, v [rows,Hkv,d] at positions int32 [rows]: k rotated into its slots
+    (int64 [rows], negative: nowhere) of the bf16 pages [num_pages, page_size, Hkv, d], v into its own.  Returns q' (q_out may be q)."""
+    qo, rows, Hq, Hkv, num_pages, page_size, d, n, stream = _step(q, k, v, positions, slots, kpages, vpages, q_out, rot, norm)
+    rc = lib().mala_rotary_write(_rows(q), _rows(k), _rows(v), positions.data_ptr(), slots.data_ptr(), ctypes.byref(rot.c), n,
+                                 _rows_out(qo), _view(kpages, _TOut), _view(vpages, _TOut), rows, Hq, Hkv, num_pages, page_size, d, stream)
+    if rc != 0:
+        raise MalaError(rc, "mala_rotary_write")
+    return qo
+
+
+def rotary_write_fp8(q, k, v, positions, slots, kpages8, vpages8, kscale, vscale, rot: Rotary, norm: Optional[HeadNorm] = None,
+                     q_out=None):
+    """mala_rotary_write_fp8: the same into e4m3 pages (uint8 or float8_e4m3fn) with their scales (see ``cache_write_fp8``)."""
+    qo, rows, Hq, Hkv, num_pages, page_size, d, n, _ = _step(q, k, v, positions, slots, kpages8, vpages8, q_out, rot, norm)
+    _scales(kscale, vscale, num_pages, Hkv, page_size)
+    kp, vp = _view8(kpages8), _view8(vpages8)
+    rc = lib().mala_rotary_write_fp8(_rows(q), _rows(k), _rows(v), positions.data_ptr(), slots.data_ptr(), ctypes.byref(rot.c), n,
+                                     _rows_out(qo), _TOut(kp.p, kp.sb, kp.sn, kp.sh), _TOut(vp.p, vp.sb, vp.sn, vp.sh),
+                                     kscale.data_ptr(), vscale.data_ptr(), rows, Hq, Hkv, num_pages, page_size, d,
+                                     _here(kscale, vscale))
+    if rc != 0:
+        raise MalaError(rc, "mala_rotary_write_fp8")
+    return qo
