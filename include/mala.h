@@ -408,7 +408,8 @@ int mala_cache_read_fp8(mala_tin kpages8, mala_tin vpages8, const float* kscale,
                         int32_t* cu_seqlens, int B, int Hkv, int num_pages, int page_size, int max_pages_per_seq, int rows,
                         int d, void* cuda_stream);
 
-/* mala_fwd_paged over an e4m3 cache: keys and values are bf16(scale * code).  total_k: room for keys in the workspace, at least the sum of
+/* mala_fwd_paged over an e4m3 cache: keys and values are scale * code, not rounded on their way (the codes are multiplied, the scales come in
+ * at the softmax; beyond 2^-60 .. 2^60, or not positive, bf16(scale * code)).  total_k: room for keys in the workspace, at least the sum of
  * seqlens_k (see mala_cache_read_fp8 for what lies beyond it: the sequences that reach beyond have no meaningful result).
  * Workspace: mala_paged_fp8_workspace_bytes.  d a multiple of 16 up to 128, page_size not 8; everything else as
  * mala_fwd_paged; telemetry laid out for max_seqlen_k = min(max_pages_per_seq * page_size, total_k). */

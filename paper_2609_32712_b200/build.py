@@ -6,7 +6,8 @@ import subprocess
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRCS = [os.path.join(HERE, "csrc", n) for n in ("mala_api.cu", "mala_bias.cu", "mala_cache.cu", "mala_rotary.cu")]
+SRCS = [os.path.join(HERE, "csrc", n) for n in ("mala_api.cu", "mala_bias.cu", "mala_cache.cu", "mala_rotary.cu", "mala_rotary_write8.cu",
+                                                "mala_scaled.cu")]
 LIB = os.path.join(HERE, "libmala.so")
 
 

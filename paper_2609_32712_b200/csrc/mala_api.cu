@@ -15,6 +15,7 @@
 #include "mala_fwd.cuh"
 #include "mala_fwd_one.cuh"
 #include "mala_internal.h"
+#include "mala_scaled.h"
 #include "tensor_map.h"
 
 namespace mala {
@@ -118,6 +119,7 @@ int device_setup(int dev, int** status_out) {
     ok = ok && bwd_set_attributes();
     ok = ok && decode_set_attributes();
     ok = ok && bias_set_attributes();
+    ok = ok && scaled_set_attributes();
     ok = ok && cache_set_attributes();
     if (!ok) return MALA_ERR_CUDA;
     g_attr_done[dev] = true;
@@ -325,7 +327,8 @@ static int fwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse,
                     int Hkv, int N, int Nk, int d, int causal, float scale, float tau, void* cuda_stream,
                     const int32_t* cu = nullptr, int total = 0, int num_splits = 1, void* ws = nullptr,
                     size_t ws_bytes = 0, const int32_t* cu_k = nullptr, int total_k = 0,
-                    const FwdPaging* pg = nullptr, const mala_rel_bias* bias = nullptr) {
+                    const FwdPaging* pg = nullptr, const mala_rel_bias* bias = nullptr, const float* kv_scales = nullptr,
+                    int scale_tiles = 0) {
   if (num_splits < 1) return MALA_ERR_INVALID_ARG;
   if (num_splits > 1) {
     if (cu || num_splits > 65535 || (long long)B * num_splits > 65535) return MALA_ERR_UNSUPPORTED;
@@ -415,6 +418,10 @@ static int fwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse,
   if (bias) {
     MALA_TRY(bias_expand(bias, Hq, ws, &p.rb, stream));
     return bias_launch_fwd(D, dense, one, tq, tk, tv, p, stream);
+  }
+  if (kv_scales) {
+    p.kv_scales = kv_scales; p.scale_tiles = scale_tiles;
+    return scaled_launch_fwd(D, dense, one, tq, tk, tv, p, stream);
   }
   if (D == 256) rc = launch_fwd<256>(dense, one, tq, tk, tv, p, stream);
   else if (D == 128) rc = launch_fwd<128>(dense, one, tq, tk, tv, p, stream);
@@ -568,12 +575,13 @@ int mala_fwd_paged(mala_tin q, mala_tin kpages, mala_tin vpages, const int32_t* 
                   cu_seqlens_q, total_q, 1, nullptr, 0, nullptr, 0, &pg));
 }
 
-// Workspace of mala_fwd_paged_fp8: keys, values and offsets
+// Workspace of mala_fwd_paged_fp8: the keys' codes, the values', their scales, offsets
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+static long long scale_tiles_of(int B, int total_k) { return (long long)total_k / 128 + B + 1; }
 
 size_t mala_paged_fp8_workspace_bytes(int B, int Hkv, int total_k, int d) {
   if (B <= 0 || Hkv <= 0 || total_k <= 0 || d <= 0 || d % 16 != 0 || d > 128) return 0;
-  return 2 * up256((size_t)total_k * Hkv * d * 2) + up256(((size_t)B + 1) * sizeof(int));
+  return 2 * up256((size_t)total_k * Hkv * d * 2) + up256((size_t)scale_tiles_of(B, total_k) * Hkv * 24 * sizeof(float)) + up256(((size_t)B + 1) * sizeof(int));
 }
 
 int mala_fwd_paged_fp8(mala_tin q, mala_tin kpages8, mala_tin vpages8, const float* kscale, const float* vscale, const int32_t* cu_seqlens_q,
@@ -600,12 +608,15 @@ int mala_fwd_paged_fp8(mala_tin q, mala_tin kpages8, mala_tin vpages8, const flo
   mala_tout k, v;
   k.p = ws; v.p = (uint8_t*)ws + part;
   k.sb = v.sb = 0; k.sn = v.sn = (int64_t)Hkv * d; k.sh = v.sh = d;
-  int32_t* const cu_k = (int32_t*)((uint8_t*)ws + 2 * part);
-  MALA_TRY(mala_cache_read_fp8(kpages8, vpages8, kscale, vscale, block_table, seqlens_k, k, v, cu_k, B, Hkv, num_pages, page_size, max_pages_per_seq,
-                               total_k, d, cuda_stream));
+  CacheScales cs;
+  cs.tiles = (int)scale_tiles_of(B, total_k);
+  cs.out = (float*)((uint8_t*)ws + 2 * part);
+  int32_t* const cu_k = (int32_t*)((uint8_t*)cs.out + up256((size_t)cs.tiles * Hkv * 24 * sizeof(float)));
+  MALA_TRY(cache_read_checked(kpages8, vpages8, kscale, vscale, block_table, seqlens_k, k, v, cu_k, B, Hkv, num_pages, page_size, max_pages_per_seq,
+                              total_k, d, true, &cs, (cudaStream_t)cuda_stream));
   const mala_tin ki = {k.p, 0, k.sn, k.sh}, vi = {v.p, 0, v.sn, v.sh};
   return scope.finish(fwd_impl(q, ki, vi, o, lse, st, B, Hq, Hkv, max_seqlen_q, max_k, d, causal, scale, tau, cuda_stream, cu_seqlens_q, total_q, 1, nullptr,
-                               0, cu_k, total_k));
+                               0, cu_k, total_k, nullptr, nullptr, cs.out, cs.tiles));
 }
 
 int mala_bwd_varlen(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dout, const float* lse,

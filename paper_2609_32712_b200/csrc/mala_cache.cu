@@ -3,12 +3,11 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
-#include <type_traits>
 
 #include "../../include/mala.h"
 #include "mala_decode_sched.cuh"
+#include "mala_e4m3.cuh"
 #include "mala_internal.h"
-#include "mala_rotary.cuh"
 #include "sm100_ptx.cuh"
 
 namespace mala {
@@ -219,10 +218,6 @@ struct WriteParams {
   int unit, chunk;                         // e4m3: keys that share a scale; rows among which a block looks for the first ones of units
   int64_t limit;                           // slots of the pool
   FastDiv by_per, by_cols, by_page;
-  RotaryRule rule;                         // e4m3, keys that are rotated on their way: rule, positions [rows], norm
-  const int* positions;
-  const void* weight; int weights_fp32, normed;
-  float eps, inv_d;
 };
 
 // A thread takes four 16-byte pieces of the call's rows, of K and of V: a copy with eight loads in flight, bound by HBM:
@@ -259,22 +254,6 @@ cache_write_kernel(const WriteParams p) {
   }
 }
 
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-__device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(c));
-  return __half22float2(*reinterpret_cast<__half2*>(&h));
-}
-
 // e4m3 pages: the keys of a unit (min(page_size, 128) of them) share a scale.  The rows of a unit are neighbours in the call, and
 // a block looks among p.chunk rows for those with which a unit begins, for one KV head and K or V.
 //
@@ -290,45 +269,9 @@ __device__ __forceinline__ void copy16_async(uint4* to, const void* from) {
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-constexpr int kNoTurn = -1;
-
-// A row of keys that are rotated on their way, as a thread of its kRow has it in fp32: its eight columns from w, a place in shared
-// memory whose neighbours hold the rest of the row.
-template <int kRow, int kTurn>
-__device__ __forceinline__ void rotated8(const WriteParams& p, const LaneTurns<kTurn>& turns, const uint4* from, int c, int pos, float (&x)[8]) {
-  const int at = c < p.cols ? c : 0;     // (threads beyond the row's columns: any of it)
-  const uint4 w = *from;
-  float y[8], C[8], S[8];
-  unpack8(c < p.cols ? w : make_uint4(0u, 0u, 0u, 0u), x);
-  if constexpr (kTurn == kHalves) unpack8(from[partner_of<kHalves>(8 * at, p.rule.rotary) / 8 - c], y);
-  else partners<kTurn>(w, x, 0, reinterpret_cast<const __nv_bfloat16*>(from - c), at, p.rule.rotary, 0u, y);
-  turns.at(p.rule, c, pos, C, S);
-  float r = 1.f;
-  if (p.normed) {
-    const uint32_t group = (kRow == 8 ? 0xffu : 0xffffu) << ((threadIdx.x & 31) / kRow * kRow);
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
-#pragma unroll
-    for (int m = kRow / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(group, sum, m);
-    r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      C[e] *= weight_at(p.weight, p.weights_fp32, 8 * at + e);
-      S[e] *= weight_at(p.weight, p.weights_fp32, partner_of<kTurn>(8 * at + e, p.rule.rotary));
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    x[e] *= C[e];
-    if (turns.on(e)) x[e] = fmaf(y[e], S[e], x[e]);
-    x[e] *= r;
-  }
-}
-
 // kRow threads per row (8 where a row has at most as many 16-byte pieces, else 16); kBatch rows fit the team's part of the buffer
-template <int kThreads, int kRow, int kBatch, int kTurn, class Turns>
-__device__ __forceinline__ void write8_unit(const WriteParams& p, const Turns& turns, bool is_v, int h, int t, int n, int64_t slot, uint4* buf, float* red) {
+template <int kThreads, int kRow, int kBatch>
+__device__ __forceinline__ void write8_unit(const WriteParams& p, bool is_v, int h, int t, int n, int64_t slot, uint4* buf, float* red) {
   constexpr int kRows = kThreads / kRow;
   static_assert(kBatch % kRows == 0, "a thread's places are its own");
   const int tid = threadIdx.x & (kThreads - 1), lane = threadIdx.x & 31, r0 = tid / kRow, c = tid % kRow;
@@ -341,34 +284,16 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, const Turns& t
   float* sp = (is_v ? p.vscale : p.kscale) + (page * p.Hkv + h) * p.per_page + at / 128;
   buf += tid;
   auto load = [&](const uint8_t* from, uint4* to, int first) {
-    if (kTurn != kNoTurn) __syncwarp();  // (a row's other threads have read what lay there)
     if (mine)
       for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, to += kThreads, from += kRows * s_sn) copy16_async(to, from);
-  };
-  auto arrived = [&]() {
-    copies_wait();
-    if (kTurn != kNoTurn) __syncwarp();
   };
   load(src, buf, 0);
   const float old = *(volatile const float*)sp;   // (before the store below, which a cached load need not be)
   uint32_t top2 = 0;                     // largest magnitudes of the even and the odd columns (bf16 magnitudes are ordered like their bits)
-  float top_turned = 0.f;
   for (int first = 0; first < n; first += kBatch) {
     if (first > 0) load(src + (int64_t)first * s_sn, buf, first);
-    arrived();
+    copies_wait();
     const uint4* from = buf;
-    if constexpr (kTurn != kNoTurn) {
-      if (!is_v) {
-        for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, from += kThreads) {
-          float x[8];
-          rotated8<kRow, kTurn>(p, turns, from, c, __ldg(p.positions + t + r), x);
-          if (mine)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top_turned = fmaxf(top_turned, fabsf(x[e]));
-        }
-        continue;
-      }
-    }
     if (mine)
       for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, from += kThreads) {
         const uint4 w = *from;
@@ -377,7 +302,6 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, const Turns& t
       }
   }
   float top = fmaxf(__uint_as_float(top2 << 16), __uint_as_float(top2 & 0xffff0000u));
-  if (kTurn != kNoTurn) top = fmaxf(top, top_turned);
 #pragma unroll
   for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
   if constexpr (kThreads > 32) {
@@ -408,25 +332,10 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, const Turns& t
   for (int first = 0; first < n; first += kBatch) {
     if (n > kBatch) {
       load(src + (int64_t)first * s_sn, buf, first);
-      arrived();
+      copies_wait();
     }
     const uint4* from = buf;
     uint8_t* to = dst + first * d_sn;
-    if constexpr (kTurn != kNoTurn) {
-      if (!is_v) {
-        for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, from += kThreads, to += kRows * d_sn) {
-          float x[8];
-          rotated8<kRow, kTurn>(p, turns, from, c, __ldg(p.positions + t + r), x);
-          auto four = [&](float x0, float x1, float x2, float x3) -> uint32_t {
-            const uint32_t high = __byte_perm(__byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x0073),
-                                              __byte_perm(__float_as_uint(x2), __float_as_uint(x3), 0x0073), 0x5410);
-            return signs(codes2(x0, x1) | (codes2(x2, x3) << 16), high);
-          };
-          if (mine) *reinterpret_cast<uint2*>(to) = make_uint2(four(x[0], x[1], x[2], x[3]), four(x[4], x[5], x[6], x[7]));
-        }
-        continue;
-      }
-    }
     if (mine)
       for (int r = first + r0, end = min(first + kBatch, n); r < end; r += kRows, from += kThreads, to += kRows * d_sn) {
         const uint4 w = *from;
@@ -459,11 +368,8 @@ __device__ __forceinline__ void write8_unit(const WriteParams& p, const Turns& t
   }
 }
 
-struct NoTurns {};
-
-// kTurn: keys are rotated on their way (how their columns are paired), or kNoTurn
-template <int kBlock, int kRow, int kTurn>
-__global__ void __launch_bounds__(kBlock, kTurn != kNoTurn ? 512 / kBlock : kBlock == 64 ? 13 : kBlock == 128 ? 6 : 4)
+template <int kBlock, int kRow>
+__global__ void __launch_bounds__(kBlock, kBlock == 64 ? 13 : kBlock == 128 ? 6 : 4)
 cache_write8_kernel(const WriteParams p) {
   constexpr int kWarps = kBlock / 32, kAll = (kBlock == 64 ? 1024 : 2048) / kRow, kShare = kAll / kWarps;   // rows (all of a unit), a warp's
   __shared__ __align__(16) uint4 rows_s[kAll * kRow];
@@ -496,9 +402,6 @@ cache_write8_kernel(const WriteParams p) {
   else if (p.chunk < 32) begins &= (1u << p.chunk) - 1u;
   // few units: the whole block takes one after the other; many, which are short: a warp each
   const bool few = __popcll(begins) <= (kBlock == 256 ? 1 : 2);
-  std::conditional_t<kTurn == kNoTurn, NoTurns, LaneTurns<kTurn>> turns;
-  if constexpr (kTurn != kNoTurn)
-    if (!is_v && begins) turns.load(p.rule, threadIdx.x % kRow);
   for (int i = 0; begins; begins &= begins - 1, ++i) {
     const int x = __ffsll((long long)begins) - 1;
     if (!few && i % kWarps != warp) continue;
@@ -511,8 +414,8 @@ cache_write8_kernel(const WriteParams p) {
       end = (end | 31) + 1;
     }
     end = min(end, last);
-    if (few) write8_unit<kBlock, kRow, kAll, kTurn>(p, turns, is_v, h, t0 + x, end - x, at, rows_s, red[i & 1]);
-    else write8_unit<32, kRow, kShare, kTurn>(p, turns, is_v, h, t0 + x, end - x, at, rows_s + warp * (kShare * kRow), nullptr);
+    if (few) write8_unit<kBlock, kRow, kAll>(p, is_v, h, t0 + x, end - x, at, rows_s, red[i & 1]);
+    else write8_unit<32, kRow, kShare>(p, is_v, h, t0 + x, end - x, at, rows_s + warp * (kShare * kRow), nullptr);
   }
 }
 
@@ -526,16 +429,24 @@ struct ReadParams {
   uint8_t* k; uint8_t* v;                  // [rows, Hkv, d] bf16
   int64_t k_sn, k_sh, v_sn, v_sh;          // bytes
   const int* block_table; const int* seqlens; int* cu;
+  float* scales; int tiles;                // codes and scales apart (see CacheScales)
   int B, max_pages, page_size, num_pages, per_page, rows, Hkv;
   int cols, per;                           // 16-byte pieces of a head's row in the pages, and of a whole row
   FastDiv by_per, by_cols, by_page;
 };
 
+enum { kReadRows = 0, kReadFp8 = 1, kReadCodes = 2 };
+
+// Scales that the forward takes apart from their codes: far enough from the ends of fp32 for its factors and logarithms.  (With another one the
+// codes are read as values.)
+__device__ __forceinline__ bool scale_apart(float s) { return s >= 0x1p-60f && s <= 0x1p60f; }
+
 // A block adds up the lengths for itself (as the tables do) and takes a thousand pieces of the packed rows at a time: which
 // sequence the first and the last of them belong to is searched once.  A thread has four 16-byte pieces of K and of V in flight.
-template <bool kFp8>
+template <int kKind>
 __global__ void __launch_bounds__(256)
 cache_read_kernel(const ReadParams p) {
+  constexpr bool kFp8 = kKind != kReadRows;
   extern __shared__ int cu_s[];            // [B + 1]
   __shared__ uint64_t warp_sums[32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -594,6 +505,10 @@ cache_read_kernel(const ReadParams p) {
               const int64_t unit = ((int64_t)page * p.Hkv + h) * p.per_page + at / 128;
               sk[i] = __ldg(p.kscale + unit);
               sv[i] = __ldg(p.vscale + unit);
+              if (kKind == kReadCodes) {
+                if (scale_apart(sk[i])) sk[i] = 1.f;
+                if (scale_apart(sv[i])) sv[i] = 1.f;
+              }
             }
           }
         }
@@ -620,42 +535,34 @@ cache_read_kernel(const ReadParams p) {
       }
     }
   }
-}
-
-constexpr int kReadMaxB = 16384;
-
-int cache_read(mala_tin kp, mala_tin vp, const float* kscale, const float* vscale, const int32_t* block_table, const int32_t* seqlens, mala_tout k,
-               mala_tout v, int32_t* cu, int B, int Hkv, int num_pages, int page_size, int max_pages, int rows, int d, bool fp8, cudaStream_t stream) {
-  ReadParams p = {};
-  const int item = fp8 ? 1 : 2;
-  p.kp = (const uint8_t*)kp.p; p.vp = (const uint8_t*)vp.p;
-  p.kp_sb = kp.sb * item; p.kp_sn = kp.sn * item; p.kp_sh = kp.sh * item;
-  p.vp_sb = vp.sb * item; p.vp_sn = vp.sn * item; p.vp_sh = vp.sh * item;
-  p.kscale = kscale; p.vscale = vscale;
-  p.k = (uint8_t*)k.p; p.v = (uint8_t*)v.p;
-  p.k_sn = k.sn * 2; p.k_sh = k.sh * 2; p.v_sn = v.sn * 2; p.v_sh = v.sh * 2;
-  p.block_table = block_table; p.seqlens = seqlens; p.cu = cu;
-  p.B = B; p.max_pages = max_pages; p.page_size = page_size; p.num_pages = num_pages; p.per_page = page_size < 128 ? 1 : page_size / 128;
-  p.rows = rows; p.Hkv = Hkv;
-  p.cols = d * item / 16; p.per = p.cols * Hkv;
-  p.by_per.set((uint32_t)p.per); p.by_cols.set((uint32_t)p.cols); p.by_page.set((uint32_t)page_size);
-  int dev = 0, *status = nullptr;
-  MALA_TRY(current_device_checked(&dev));
-  MALA_TRY(device_setup(dev, &status));
-  const long long want = ((long long)rows * p.per + 1023) / 1024, most = 8ll * sm_count(dev);
-  const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
-  const size_t smem = ((size_t)B + 1) * sizeof(int);
-  if (fp8) cache_read_kernel<true><<<grid, 256, smem, stream>>>(p);
-  else cache_read_kernel<false><<<grid, 256, smem, stream>>>(p);
-  return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
-}
-
-bool cache_set_attributes() {
-  const int most = (3 * kTableMaxB + 2) * (int)sizeof(int), most_read = (kReadMaxB + 1) * (int)sizeof(int);
-  return cudaFuncSetAttribute(page_tables_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess &&
-         cudaFuncSetAttribute(page_tables_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess &&
-         cudaFuncSetAttribute(cache_read_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_read) == cudaSuccess &&
-         cudaFuncSetAttribute(cache_read_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_read) == cudaSuccess;
+  if constexpr (kKind == kReadCodes) {     // the scales: a thread per KV head, key block and group of 16 keys
+    const int64_t groups = (int64_t)p.tiles * 8, n = groups * p.Hkv;
+    for (int64_t x = (int64_t)blockIdx.x * 256 + tid; x < n; x += (int64_t)gridDim.x * 256) {
+      const int h = (int)(x / groups), g = (int)(x - h * groups), tile = g / 8;
+      int lo = 0, hi = p.B;                // the last sequence whose first block is at or before this one
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (cu_s[mid] / 128 + mid <= tile) lo = mid;
+        else hi = mid;
+      }
+      const int pos = (tile - cu_s[lo] / 128 - lo) * 128 + g % 8 * 16;
+      float k = 1.f, v = 1.f;
+      if (pos < cu_s[lo + 1] - cu_s[lo]) {
+        const int entry = (int)p.by_page.div((uint32_t)pos), page = __ldg(p.block_table + (int64_t)lo * p.max_pages + entry);
+        if (page >= 0 && page < p.num_pages) {
+          const int64_t unit = ((int64_t)page * p.Hkv + h) * p.per_page + (pos - entry * p.page_size) / 128;
+          k = __ldg(p.kscale + unit);
+          v = __ldg(p.vscale + unit);
+          if (!scale_apart(k)) k = 1.f;
+          if (!scale_apart(v)) v = 1.f;
+        }
+      }
+      float* const to = p.scales + ((int64_t)h * p.tiles + tile) * 24 + g % 8;
+      to[0] = k;
+      to[8] = log2f(v);
+      to[16] = 1.f / v;
+    }
+  }
 }
 
 static bool aligned16(const void* p) { return (((uintptr_t)p) & 15) == 0; }
@@ -667,6 +574,71 @@ static int check_cache_view(const void* p, int64_t sb, int64_t sn, int64_t sh, i
   if ((pages > 1 && sb <= 0) || (n > 1 && sn <= 0) || (H > 1 && sh <= 0)) return MALA_ERR_INVALID_ARG;
   if ((pages > 1 && sb * item % 16) || (n > 1 && sn * item % 16) || (H > 1 && sh * item % 16)) return MALA_ERR_MISALIGNED;
   return MALA_OK;
+}
+
+constexpr int kReadMaxB = 16384;
+
+static int check_read(mala_tin kp, mala_tin vp, const int32_t* block_table, const int32_t* seqlens, mala_tout k, mala_tout v, const int32_t* cu, int B, int Hkv,
+                      int num_pages, int page_size, int max_pages, int rows, int d, int item) {
+  if (B <= 0 || Hkv <= 0 || num_pages <= 0 || page_size <= 0 || max_pages <= 0 || rows < 0 || d <= 0) return MALA_ERR_INVALID_ARG;
+  if (!block_table || !seqlens || !cu || cu == seqlens) return MALA_ERR_INVALID_ARG;
+  if ((((uintptr_t)block_table | (uintptr_t)seqlens | (uintptr_t)cu) & 3) != 0) return MALA_ERR_MISALIGNED;
+  if (!page_size_ok(page_size) || B > kReadMaxB || Hkv > 65535 || rows > kMaxRows || (long long)max_pages * page_size > 0x7fffffffLL) return MALA_ERR_UNSUPPORTED;
+  MALA_TRY(check_cache_view(kp.p, kp.sb, kp.sn, kp.sh, num_pages, page_size, Hkv, item));
+  MALA_TRY(check_cache_view(vp.p, vp.sb, vp.sn, vp.sh, num_pages, page_size, Hkv, item));
+  if (rows == 0) return MALA_OK;
+  MALA_TRY(check_cache_view(k.p, 0, k.sn, k.sh, 1, rows, Hkv, 2));
+  return check_cache_view(v.p, 0, v.sn, v.sh, 1, rows, Hkv, 2);
+}
+
+static int cache_read(mala_tin kp, mala_tin vp, const float* kscale, const float* vscale, const int32_t* block_table, const int32_t* seqlens, mala_tout k,
+               mala_tout v, int32_t* cu, int B, int Hkv, int num_pages, int page_size, int max_pages, int rows, int d, bool fp8,
+                      const CacheScales* scales, cudaStream_t stream) {
+  ReadParams p = {};
+  const int item = fp8 ? 1 : 2;
+  p.kp = (const uint8_t*)kp.p; p.vp = (const uint8_t*)vp.p;
+  p.kp_sb = kp.sb * item; p.kp_sn = kp.sn * item; p.kp_sh = kp.sh * item;
+  p.vp_sb = vp.sb * item; p.vp_sn = vp.sn * item; p.vp_sh = vp.sh * item;
+  p.kscale = kscale; p.vscale = vscale;
+  p.k = (uint8_t*)k.p; p.v = (uint8_t*)v.p;
+  p.k_sn = k.sn * 2; p.k_sh = k.sh * 2; p.v_sn = v.sn * 2; p.v_sh = v.sh * 2;
+  p.block_table = block_table; p.seqlens = seqlens; p.cu = cu;
+  p.scales = scales ? scales->out : nullptr; p.tiles = scales ? scales->tiles : 0;
+  p.B = B; p.max_pages = max_pages; p.page_size = page_size; p.num_pages = num_pages; p.per_page = page_size < 128 ? 1 : page_size / 128;
+  p.rows = rows; p.Hkv = Hkv;
+  p.cols = d * item / 16; p.per = p.cols * Hkv;
+  p.by_per.set((uint32_t)p.per); p.by_cols.set((uint32_t)p.cols); p.by_page.set((uint32_t)page_size);
+  int dev = 0, *status = nullptr;
+  MALA_TRY(current_device_checked(&dev));
+  MALA_TRY(device_setup(dev, &status));
+  const long long want = ((long long)rows * p.per + 1023) / 1024, most = 8ll * sm_count(dev);
+  const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
+  const size_t smem = ((size_t)B + 1) * sizeof(int);
+  if (scales) cache_read_kernel<kReadCodes><<<grid, 256, smem, stream>>>(p);
+  else if (fp8) cache_read_kernel<kReadFp8><<<grid, 256, smem, stream>>>(p);
+  else cache_read_kernel<kReadRows><<<grid, 256, smem, stream>>>(p);
+  return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+}
+
+int cache_read_checked(mala_tin kp, mala_tin vp, const float* kscale, const float* vscale, const int32_t* block_table, const int32_t* seqlens, mala_tout k,
+                       mala_tout v, int32_t* cu, int B, int Hkv, int num_pages, int page_size, int max_pages, int rows, int d, bool fp8,
+                       const CacheScales* scales, cudaStream_t stream) {
+  MALA_TRY(check_read(kp, vp, block_table, seqlens, k, v, cu, B, Hkv, num_pages, page_size, max_pages, rows, d, fp8 ? 1 : 2));
+  if (fp8) {
+    if (!kscale || !vscale) return MALA_ERR_INVALID_ARG;
+    if ((((uintptr_t)kscale | (uintptr_t)vscale) & 3) != 0) return MALA_ERR_MISALIGNED;
+  }
+  if (d % (fp8 ? 16 : 8) != 0 || d > (fp8 ? 128 : 256) || (fp8 && page_size == 8)) return MALA_ERR_UNSUPPORTED;
+  return cache_read(kp, vp, kscale, vscale, block_table, seqlens, k, v, cu, B, Hkv, num_pages, page_size, max_pages, rows, d, fp8, scales, stream);
+}
+
+bool cache_set_attributes() {
+  const int most = (3 * kTableMaxB + 2) * (int)sizeof(int), most_read = (kReadMaxB + 1) * (int)sizeof(int);
+  return cudaFuncSetAttribute(page_tables_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess &&
+         cudaFuncSetAttribute(page_tables_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess &&
+         cudaFuncSetAttribute(cache_read_kernel<kReadRows>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_read) == cudaSuccess &&
+         cudaFuncSetAttribute(cache_read_kernel<kReadFp8>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_read) == cudaSuccess &&
+         cudaFuncSetAttribute(cache_read_kernel<kReadCodes>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_read) == cudaSuccess;
 }
 
 static int write_params(WriteParams* w, mala_tin k, mala_tin v, const int64_t* slots, mala_tout kp, mala_tout vp, int rows, int Hkv,
@@ -696,26 +668,16 @@ static int write_params(WriteParams* w, mala_tin k, mala_tin v, const int64_t* s
   return MALA_OK;
 }
 
-template <int kTurn>
-static int launch_write8(WriteParams& w, cudaStream_t stream) {
-  const int rows = w.rows, Hkv = w.Hkv;
-  int dev = 0, *status = nullptr;
-  MALA_TRY(current_device_checked(&dev));
-  MALA_TRY(device_setup(dev, &status));
-  // Blocks of eight warps and of so few rows that all blocks run at once (four per SM); where that would take more than eight rows
-  // each, blocks of two warps, or of four where a unit takes 32 KB, and of 64 rows (so that few blocks find nothing to do) or fewer while
-  // they run at once (16 requests of up to 40 rows, pages of 16 keys: 5.8 us, with 64 rows per block 11.0)
-  while (w.chunk < 16 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 4ll * sm_count(dev)) w.chunk *= 2;
-  const bool many = w.chunk == 16, narrow = w.cols <= 8;
-  if (many)
-    while (w.chunk < 64 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 8ll * sm_count(dev)) w.chunk *= 2;
-  const dim3 grid((unsigned)((rows + w.chunk - 1) / w.chunk), Hkv, 2);
-  if (!many && narrow) cache_write8_kernel<256, 8, kTurn><<<grid, 256, 0, stream>>>(w);
-  else if (!many) cache_write8_kernel<256, 16, kTurn><<<grid, 256, 0, stream>>>(w);
-  else if (narrow) cache_write8_kernel<64, 8, kTurn><<<grid, 64, 0, stream>>>(w);
-  else if (w.unit < 128) cache_write8_kernel<64, 16, kTurn><<<grid, 64, 0, stream>>>(w);
-  else cache_write8_kernel<128, 16, kTurn><<<grid, 128, 0, stream>>>(w);
-  return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+// (for the calls that rotate on the way)
+int check_cache_write(mala_tin k, mala_tin v, const int64_t* slots, mala_tout kp, mala_tout vp, const float* kscale, const float* vscale, int rows, int Hkv,
+                      int num_pages, int page_size, int d, bool fp8) {
+  WriteParams w;
+  MALA_TRY(write_params(&w, k, v, slots, kp, vp, rows, Hkv, num_pages, page_size, d, fp8 ? 1 : 2));
+  if (fp8) {
+    if (!kscale || !vscale) return MALA_ERR_INVALID_ARG;
+    if ((((uintptr_t)kscale | (uintptr_t)vscale) & 3) != 0) return MALA_ERR_MISALIGNED;
+  }
+  return d % (fp8 ? 16 : 8) != 0 || d > (fp8 ? 128 : 256) || (fp8 && page_size == 8) ? MALA_ERR_UNSUPPORTED : MALA_OK;
 }
 
 static int check_tables(const int32_t* seqlens, const int32_t* block_table, const int32_t* free_pages, const int32_t* free_count,
@@ -811,78 +773,39 @@ int mala_cache_write_fp8(mala_tin k, mala_tin v, const int64_t* slots, mala_tout
   if (d % 16 != 0 || d > 128 || page_size == 8) return MALA_ERR_UNSUPPORTED;
   if (rows == 0) return MALA_OK;
   w.kscale = kscale; w.vscale = vscale;
-  return scope.finish(launch_write8<kNoTurn>(w, (cudaStream_t)cuda_stream));
-}
-
-static int check_read(mala_tin kp, mala_tin vp, const int32_t* block_table, const int32_t* seqlens, mala_tout k, mala_tout v, const int32_t* cu, int B, int Hkv,
-                      int num_pages, int page_size, int max_pages, int rows, int d, int item) {
-  if (B <= 0 || Hkv <= 0 || num_pages <= 0 || page_size <= 0 || max_pages <= 0 || rows < 0 || d <= 0) return MALA_ERR_INVALID_ARG;
-  if (!block_table || !seqlens || !cu || cu == seqlens) return MALA_ERR_INVALID_ARG;
-  if ((((uintptr_t)block_table | (uintptr_t)seqlens | (uintptr_t)cu) & 3) != 0) return MALA_ERR_MISALIGNED;
-  if (!page_size_ok(page_size) || B > kReadMaxB || Hkv > 65535 || rows > kMaxRows || (long long)max_pages * page_size > 0x7fffffffLL) return MALA_ERR_UNSUPPORTED;
-  MALA_TRY(check_cache_view(kp.p, kp.sb, kp.sn, kp.sh, num_pages, page_size, Hkv, item));
-  MALA_TRY(check_cache_view(vp.p, vp.sb, vp.sn, vp.sh, num_pages, page_size, Hkv, item));
-  if (rows == 0) return MALA_OK;
-  MALA_TRY(check_cache_view(k.p, 0, k.sn, k.sh, 1, rows, Hkv, 2));
-  return check_cache_view(v.p, 0, v.sn, v.sh, 1, rows, Hkv, 2);
+  int dev = 0, *status = nullptr;
+  MALA_TRY(current_device_checked(&dev));
+  MALA_TRY(device_setup(dev, &status));
+  // Blocks of eight warps and of so few rows that all blocks run at once (four per SM); where that would take more than eight rows
+  // each, blocks of two warps, or of four where a unit takes 32 KB, and of 64 rows (so that few blocks find nothing to do) or fewer while
+  // they run at once (16 requests of up to 40 rows, pages of 16 keys: 5.8 us, with 64 rows per block 11.0)
+  while (w.chunk < 16 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 4ll * sm_count(dev)) w.chunk *= 2;
+  const bool many = w.chunk == 16, narrow = w.cols <= 8;
+  if (many)
+    while (w.chunk < 64 && ((long long)rows + w.chunk - 1) / w.chunk * Hkv * 2 > 8ll * sm_count(dev)) w.chunk *= 2;
+  const dim3 grid((unsigned)((rows + w.chunk - 1) / w.chunk), Hkv, 2);
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  if (!many && narrow) cache_write8_kernel<256, 8><<<grid, 256, 0, stream>>>(w);
+  else if (!many) cache_write8_kernel<256, 16><<<grid, 256, 0, stream>>>(w);
+  else if (narrow) cache_write8_kernel<64, 8><<<grid, 64, 0, stream>>>(w);
+  else if (w.unit < 128) cache_write8_kernel<64, 16><<<grid, 64, 0, stream>>>(w);
+  else cache_write8_kernel<128, 16><<<grid, 128, 0, stream>>>(w);
+  return scope.finish(cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA);
 }
 
 int mala_cache_read(mala_tin kpages, mala_tin vpages, const int32_t* block_table, const int32_t* seqlens, mala_tout k_out, mala_tout v_out,
                     int32_t* cu_seqlens, int B, int Hkv, int num_pages, int page_size, int max_pages_per_seq, int rows, int d, void* cuda_stream) {
   ApiScope scope("mala_cache_read", cuda_stream);
-  MALA_TRY(check_read(kpages, vpages, block_table, seqlens, k_out, v_out, cu_seqlens, B, Hkv, num_pages, page_size, max_pages_per_seq, rows, d, 2));
-  if (d % 8 != 0 || d > 256) return MALA_ERR_UNSUPPORTED;
-  return scope.finish(cache_read(kpages, vpages, nullptr, nullptr, block_table, seqlens, k_out, v_out, cu_seqlens, B, Hkv, num_pages, page_size,
-                                 max_pages_per_seq, rows, d, false, (cudaStream_t)cuda_stream));
+  return scope.finish(cache_read_checked(kpages, vpages, nullptr, nullptr, block_table, seqlens, k_out, v_out, cu_seqlens, B, Hkv, num_pages, page_size,
+                                         max_pages_per_seq, rows, d, false, nullptr, (cudaStream_t)cuda_stream));
 }
 
 int mala_cache_read_fp8(mala_tin kpages8, mala_tin vpages8, const float* kscale, const float* vscale, const int32_t* block_table, const int32_t* seqlens,
                         mala_tout k_out, mala_tout v_out, int32_t* cu_seqlens, int B, int Hkv, int num_pages, int page_size, int max_pages_per_seq,
                         int rows, int d, void* cuda_stream) {
   ApiScope scope("mala_cache_read_fp8", cuda_stream);
-  MALA_TRY(check_read(kpages8, vpages8, block_table, seqlens, k_out, v_out, cu_seqlens, B, Hkv, num_pages, page_size, max_pages_per_seq, rows, d, 1));
-  if (!kscale || !vscale) return MALA_ERR_INVALID_ARG;
-  if ((((uintptr_t)kscale | (uintptr_t)vscale) & 3) != 0) return MALA_ERR_MISALIGNED;
-  if (d % 16 != 0 || d > 128 || page_size == 8) return MALA_ERR_UNSUPPORTED;
-  return scope.finish(cache_read(kpages8, vpages8, kscale, vscale, block_table, seqlens, k_out, v_out, cu_seqlens, B, Hkv, num_pages, page_size,
-                                 max_pages_per_seq, rows, d, true, (cudaStream_t)cuda_stream));
-}
-
-int mala_rotary_write(mala_tin q, mala_tin k, mala_tin v, const int32_t* positions, const int64_t* slots, const mala_rotary* rotary,
-                      const mala_head_norm* norm, mala_tout q_out, mala_tout kpages, mala_tout vpages, int rows, int Hq, int Hkv, int num_pages,
-                      int page_size, int d, void* cuda_stream) {
-  ApiScope scope("mala_rotary_write", cuda_stream);
-  WriteParams w;
-  MALA_TRY(write_params(&w, k, v, slots, kpages, vpages, rows, Hkv, num_pages, page_size, d, 2));
-  MALA_TRY(check_rotary_step(q, positions, q_out, rotary, norm, rows, Hq, d));
-  if (rows == 0) return MALA_OK;
-  return scope.finish(rotary_step(q, k, v, positions, slots, q_out, kpages, vpages, rotary, norm, rows, Hq, Hkv, w.limit, page_size, d,
-                                  (cudaStream_t)cuda_stream));
-}
-
-int mala_rotary_write_fp8(mala_tin q, mala_tin k, mala_tin v, const int32_t* positions, const int64_t* slots, const mala_rotary* rotary,
-                          const mala_head_norm* norm, mala_tout q_out, mala_tout kpages8, mala_tout vpages8, float* kscale, float* vscale, int rows,
-                          int Hq, int Hkv, int num_pages, int page_size, int d, void* cuda_stream) {
-  ApiScope scope("mala_rotary_write_fp8", cuda_stream);
-  WriteParams w;
-  MALA_TRY(write_params(&w, k, v, slots, kpages8, vpages8, rows, Hkv, num_pages, page_size, d, 1));
-  if (!kscale || !vscale) return MALA_ERR_INVALID_ARG;
-  if ((((uintptr_t)kscale) & 3) != 0 || (((uintptr_t)vscale) & 3) != 0) return MALA_ERR_MISALIGNED;
-  if (d % 16 != 0 || d > 128 || page_size == 8) return MALA_ERR_UNSUPPORTED;
-  MALA_TRY(check_rotary_step(q, positions, q_out, rotary, norm, rows, Hq, d));
-  if (rows == 0) return MALA_OK;
-  w.kscale = kscale; w.vscale = vscale;
-  w.rule.inv_freq = rotary->inv_freq; w.rule.rotary = rotary->rotary; w.rule.d = d;
-  w.rule.magnitude = w.rule.turned = rotary->magnitude;
-  w.positions = positions;
-  w.normed = norm != nullptr; w.weight = norm ? norm->k_weight : nullptr; w.weights_fp32 = norm ? norm->weights_fp32 : 0;
-  w.eps = norm ? norm->eps : 0.f; w.inv_d = 1.f / (float)d;
-  cudaStream_t stream = (cudaStream_t)cuda_stream;
-  MALA_TRY(rotary_step(q, mala_tin{nullptr, 0, 0, 0}, mala_tin{nullptr, 0, 0, 0}, positions, nullptr, q_out, mala_tout{nullptr, 0, 0, 0},
-                       mala_tout{nullptr, 0, 0, 0}, rotary, norm, rows, Hq, 0, 0, 1, d, stream));
-  const int pairs = pairs_kind(rotary->rotary, rotary->interleaved);
-  return scope.finish(pairs == kHalves ? launch_write8<kHalves>(w, stream)
-                                       : pairs == kHalvesOdd ? launch_write8<kHalvesOdd>(w, stream) : launch_write8<kNeighbours>(w, stream));
+  return scope.finish(cache_read_checked(kpages8, vpages8, kscale, vscale, block_table, seqlens, k_out, v_out, cu_seqlens, B, Hkv, num_pages, page_size,
+                                         max_pages_per_seq, rows, d, true, nullptr, (cudaStream_t)cuda_stream));
 }
 
 }  // extern "C"

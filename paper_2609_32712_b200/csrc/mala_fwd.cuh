@@ -66,7 +66,28 @@ struct FwdParams {
   float scale_log2;              // scale * log2(e)
   float log2_tau;                // log2(tau); unused by the dense kernel
   RelBiasView rb;                // relative position bias (kernels with kBias)
+  const float* kv_scales;        // scales of 16 keys each (kernels with kScaled, packed sequences with cu_k): for KV head h and key block j of
+  int scale_tiles;               // sequence b 24 floats at 24 * (h * scale_tiles + cu_k[b] / 128 + b + j), see kv_scales_of
 };
+
+// The scales of a key block, a lane's share of them: keys' (times c2) in lanes 0-7, log2 of the values' in 8-15 and their inverses in 16-23
+__device__ __forceinline__ float kv_scales_of(const FwdParams& p, int hkv, int b, int krow0, int j, int lane, float c2) {
+  if (lane >= 24) return 0.f;
+  const float s = __ldg(p.kv_scales + ((size_t)hkv * p.scale_tiles + krow0 / 128 + b + j) * 24 + lane);
+  return lane < 8 ? s * c2 : s;
+}
+// Largest of 32 scores, two groups of 16 with scales of their own (lanes g and g + 1 of sc)
+__device__ __forceinline__ float scaled_max(const uint32_t (&s)[32], float sc, int g) {
+  float m[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    m[x] = __uint_as_float(s[16 * x]);
+#pragma unroll
+    for (int e = 1; e < 15; e += 2) m[x] = max3(m[x], __uint_as_float(s[16 * x + e]), __uint_as_float(s[16 * x + e + 1]));
+    m[x] = fmaxf(m[x], __uint_as_float(s[16 * x + 15])) * __shfl_sync(0xffffffffu, sc, g + x);
+  }
+  return fmaxf(m[0], m[1]);
+}
 
 // Rows first .. first + count - 1 of a packed sequence whose queries see no key: o = 0, lse = -inf (all threads of the block)
 __device__ __forceinline__ void empty_rows(const FwdParams& p, int b, int h, int row0, int Nq, int first, int count) {
@@ -97,7 +118,11 @@ struct FwdCfg {
 // table lookups costs the other layouts nothing).  kBias: the scores carry a relative position bias (mala_bias.cuh): 282 us for 8192
 // tokens, causal, 16 heads on 4 KV heads of 128 columns, 64 buckets up to 2048 (275 GFLOP at 976 TFLOP/s; 238 without a bias), bound by
 // the softmax warps' chain per tile, in which the exponentials are the longest part.
-template <int D, bool kDense, bool kSmall = false, bool kBias = false>
+//
+// kScaled: keys and values are codes of a cache, whole numbers of their scales, and the scales (one per 16 keys) come in here: a key's is the
+// factor of its score in the maximum and in the exponential's argument; a value's is a summand there, P then carries it, and
+// the row's sum takes it out again.  So nothing is rounded that a cache of wider values would not round.
+template <int D, bool kDense, bool kSmall = false, bool kBias = false, bool kScaled = false>
 __global__ void __launch_bounds__(384, 1)
 mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const FwdParams p) {
@@ -450,6 +475,9 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       near_hi = 1 - lo;
     }
     [[maybe_unused]] float bv0 = 0.f, bv1 = 0.f;
+    [[maybe_unused]] float sc = 0.f, sc_next = 0.f;    // this tile's scales and the next one's
+    if constexpr (kScaled)
+      if (T > 0) sc_next = kv_scales_of(p, hkv, b, krow0, j0 - first, lane, c2);
     [[maybe_unused]] int nears = 0;                    // near tiles so far
     [[maybe_unused]] bool near_next = false;
     // whether the head may have tiles to which the bias is added in place
@@ -488,6 +516,10 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     for (int t = 0; t < T; ++t) {
       const int j = j0 - first - t;
       float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
+      if constexpr (kScaled) {
+        sc = sc_next;
+        if (t + 1 < T) sc_next = kv_scales_of(p, hkv, b, krow0, j - 1, lane, c2);
+      }
       // what kind of tile this is, and the next one: beside the wait for the scores, and from votes, because to the compiler no other
       // value is the same in all lanes (a vote where the branch stands is on the chain of the tile)
       [[maybe_unused]] bool near = false, by_factors = false, rare = false;
@@ -551,6 +583,10 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
       }
       // row maximum of the 128 scores: four chains of three-input maxima (half the instructions of pairwise maxima)
+      float mt;
+      if constexpr (kScaled) {
+        mt = fmaxf(fmaxf(scaled_max(s0, sc, 0), scaled_max(s1, sc, 2)), fmaxf(scaled_max(s2, sc, 4), scaled_max(s3, sc, 6)));
+      } else {
       float mx[4];
       mx[0] = __uint_as_float(s0[0]); mx[1] = __uint_as_float(s1[0]); mx[2] = __uint_as_float(s2[0]); mx[3] = __uint_as_float(s3[0]);
 #pragma unroll
@@ -562,7 +598,8 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       }
       // row maximum of the scaled scores, log2 domain
       const float top_ = fmaxf(max3(mx[0], mx[1], __uint_as_float(s0[31])), max3(mx[2], mx[3], fmaxf(fmaxf(__uint_as_float(s1[31]), __uint_as_float(s2[31])), __uint_as_float(s3[31]))));
-      const float mt = kBias ? fmaxf(top_ * cs + bs, kBiasFloor) : top_ * c2;
+      mt = kBias ? fmaxf(top_ * cs + bs, kBiasFloor) : top_ * c2;
+      }
       bool retain = true;
       if (!kDense) {
         // Eq. 3: skip iff rowmax - (m + log l) < log(tau / L) for every valid row
@@ -658,10 +695,34 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         sums0 = sums1 = 0;
       };
       float sum0 = 0.f, sum1 = 0.f, sum2 = 0.f, sum3 = 0.f;
+      [[maybe_unused]] uint64_t gk2 = 0, gn2 = 0;      // a group's factor and summand
       uint32_t pk[16];
+      [[maybe_unused]] auto scaled_group = [&](int g) {
+        const float k_ = __shfl_sync(0xffffffffu, sc, g), n_ = __shfl_sync(0xffffffffu, sc, 8 + g) - m_ref;
+        gk2 = f2(k_, k_);
+        gn2 = f2(n_, n_);
+      };
+      [[maybe_unused]] auto scaled_sum = [&](int g) {  // (into sum0: the group's sum without the values' scale)
+        float a, b_, c_, d_;
+        take_sums(a, b_, c_, d_);
+        sum0 = fmaf((a + b_) + (c_ + d_), __shfl_sync(0xffffffffu, sc, 16 + g), sum0);
+      };
 #define MALA_P_CHUNK(SRC, COL)                                                         \
       {                                                                                \
         _Pragma("unroll") for (int e = 0; e < 8; ++e) {                                \
+          if constexpr (kScaled) {                                                     \
+            const int g = (COL) / 8 + e / 4;                                           \
+            if (e % 4 == 0) scaled_group(g);                                           \
+            float a0, a1, a2, a3;                                                      \
+            f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e]), __uint_as_float(SRC[4 * e + 1])), gk2, gn2), a0, a1);     \
+            f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e + 2]), __uint_as_float(SRC[4 * e + 3])), gk2, gn2), a2, a3); \
+            const uint64_t x0 = f2(fast_exp2(a0), fast_exp2(a1)), x1 = f2(fast_exp2(a2), fast_exp2(a3));            \
+            sums0 = f2_add(sums0, x0); sums1 = f2_add(sums1, x1);                      \
+            pk[2 * e] = f2_bf16(x0);                                                   \
+            pk[2 * e + 1] = f2_bf16(x1);                                               \
+            if (e % 4 == 3) scaled_sum(g);                                             \
+            continue;                                                                  \
+          }                                                                            \
           if constexpr (kBias) {                                                       \
             float a0, a1, a2, a3;                                                      \
             f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e]), __uint_as_float(SRC[4 * e + 1])), cs2, nm2), a0, a1);     \

@@ -79,7 +79,7 @@ struct FwdOneCtl {
   int flag[4], v_tile[2], early_exit;
 };
 
-template <int D, bool kDense, bool kSmall = false, bool kBias = false>
+template <int D, bool kDense, bool kSmall = false, bool kBias = false, bool kScaled = false>
 __global__ void __launch_bounds__(384, 1)
 mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const FwdParams p) {
@@ -359,6 +359,8 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       near_hi = 1 - lo;
     }
     [[maybe_unused]] float bv = 0.f;
+    [[maybe_unused]] float sc = 0.f, sc_next = 0.f;    // this tile's scales and the next one's
+    if constexpr (kScaled) sc_next = kv_scales_of(p, hkv, b, krow0, j0, lane, c2);
     [[maybe_unused]] int nears = 0;                    // near tiles so far
     [[maybe_unused]] bool near_next = false;
     // whether the head may have tiles to which the bias is added in place
@@ -394,6 +396,10 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     for (int t = 0; t < U; ++t) {
       const int x = t & 1, j = j0 - t;
       float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
+      if constexpr (kScaled) {
+        sc = sc_next;
+        if (t + 1 < U) sc_next = kv_scales_of(p, hkv, b, krow0, j - 1, lane, c2);
+      }
       // what kind of tile this is, and the next one: beside the wait for the scores, and from votes, because to the compiler no other
       // value is the same in all lanes (a vote where the branch stands is on the chain of the tile)
       [[maybe_unused]] bool near = false, by_factors = false, rare = false;
@@ -443,6 +449,10 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           if (e + 32 > lim) s1[e] = ninf;
         }
       }
+      float mt;
+      if constexpr (kScaled) {
+        mt = fmaxf(scaled_max(s0, sc, half * 4), scaled_max(s1, sc, half * 4 + 2));
+      } else {
       float mx[4];
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -456,8 +466,9 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           mx[c] = max3(mx[c], __uint_as_float(s0[e + c]), __uint_as_float(s0[e + c + 2]));
           mx[c + 2] = max3(mx[c + 2], __uint_as_float(s1[e + c]), __uint_as_float(s1[e + c + 2]));
         }
-      float mt = fmaxf(max3(mx[0], mx[1], fmaxf(__uint_as_float(s0[30]), __uint_as_float(s0[31]))),
+      mt = fmaxf(max3(mx[0], mx[1], fmaxf(__uint_as_float(s0[30]), __uint_as_float(s0[31]))),
                        max3(mx[2], mx[3], fmaxf(__uint_as_float(s1[30]), __uint_as_float(s1[31])))) * cs;
+      }
       if constexpr (kBias) mt = fmaxf(mt + bs, kBiasFloor);
       // the row's maximum, and its normalizer after the tile before, from both threads of the row: at once where the test
       // needs the new normalizer, else only if the tile is retained
@@ -547,10 +558,34 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         sums0 = sums1 = 0;
       };
       float sum0 = 0.f, sum1 = 0.f, sum2 = 0.f, sum3 = 0.f;
+      [[maybe_unused]] uint64_t gk2 = 0, gn2 = 0;      // a group's factor and summand
+      [[maybe_unused]] auto scaled_group = [&](int g) {
+        const float k_ = __shfl_sync(0xffffffffu, sc, g), n_ = __shfl_sync(0xffffffffu, sc, 8 + g) - m_ref;
+        gk2 = f2(k_, k_);
+        gn2 = f2(n_, n_);
+      };
+      [[maybe_unused]] auto scaled_sum = [&](int g) {  // (into sum0: the group's sum without the values' scale)
+        float a, b_, c_, d_;
+        take_sums(a, b_, c_, d_);
+        sum0 = fmaf((a + b_) + (c_ + d_), __shfl_sync(0xffffffffu, sc, 16 + g), sum0);
+      };
 #define MALA_P_PIECE(SRC, PIECE)                                                       \
       {                                                                                \
         uint32_t pk[16];                                                               \
         _Pragma("unroll") for (int e = 0; e < 8; ++e) {                                \
+          if constexpr (kScaled) {                                                     \
+            const int g = half * 4 + (PIECE) * 2 + e / 4;                              \
+            if (e % 4 == 0) scaled_group(g);                                           \
+            float a0, a1, a2, a3;                                                      \
+            f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e]), __uint_as_float(SRC[4 * e + 1])), gk2, gn2), a0, a1);     \
+            f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e + 2]), __uint_as_float(SRC[4 * e + 3])), gk2, gn2), a2, a3); \
+            const uint64_t x0 = f2(fast_exp2(a0), fast_exp2(a1)), x1 = f2(fast_exp2(a2), fast_exp2(a3));            \
+            sums0 = f2_add(sums0, x0); sums1 = f2_add(sums1, x1);                      \
+            pk[2 * e] = f2_bf16(x0);                                                   \
+            pk[2 * e + 1] = f2_bf16(x1);                                               \
+            if (e % 4 == 3) scaled_sum(g);                                             \
+            continue;                                                                  \
+          }                                                                            \
           if constexpr (kBias) {                                                       \
             float a0, a1, a2, a3;                                                      \
             f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e]), __uint_as_float(SRC[4 * e + 1])), cs2, nm2), a0, a1);     \

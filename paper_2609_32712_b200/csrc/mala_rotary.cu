@@ -57,27 +57,42 @@ __device__ __forceinline__ bool position_of(const RotaryParams& p, const RotaryT
 }
 
 // Rotations.  A row of d columns lies in the registers of L lanes, eight columns each, and a warp works on 32 / L heads of a token
-// at a time, four such loads in flight: the angles of a token are worked out once for all heads that a warp takes.
+// at a time, four such loads in flight behind the four that it works on: the angles of a token are worked out once for all heads
+// that a warp takes.
 template <int L, int kPairs, bool kNorm, bool kPages>
-__global__ void __launch_bounds__(kRotaryThreads)
+__global__ void __launch_bounds__(kRotaryThreads, 2)
 rotary_kernel(const RotaryParams p) {
   constexpr int P = 32 / L, U = 4;
+  constexpr uint32_t kAll = 0xffffffffu;
+  __shared__ uint64_t turns_s[kMaxPairs];
   __shared__ uint4 rows_s[kPairs == kHalvesOdd ? kRotaryWarps * 32 : 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, i = lane % L;
   const bool mine = 8 * i < p.rule.d;
-  const int from = g * L + (mine ? partner_of<kHalves>(8 * i, p.rule.rotary) / 8 : i);
   uint4* const buf = rows_s + (kPairs == kHalvesOdd ? warp * 32 : 0);
   LaneTurns<kPairs> turns;
-  turns.load(p.rule, i);
+  turns.set(p.rule, i, g * L);
+  load_turns(p.rule, turns_s);
+  __syncthreads();
   const uint32_t nq = p.t[0].items, nk = p.t[1].items, all = nq + nk + (kPages ? p.t[2].items : 0);   // (at most 3 * 2^30)
   for (uint32_t item = blockIdx.x * kRotaryWarps + warp; item < all; item += gridDim.x * kRotaryWarps) {
     const int which = item < nq ? 0 : item < nq + nk ? 1 : 2, x0 = (int)(item - (which == 0 ? 0 : which == 1 ? nq : nq + nk));
     const RotaryTensor& a = p.t[which];
     const int t = (int)a.by_spans.div((uint32_t)x0), h0 = (x0 - t * (int)a.by_spans.d) * a.span, h1 = min(h0 + a.span, a.H);
     const int b = (int)a.by_n.div((uint32_t)t), n = t - b * a.N;
+    const uint8_t* src = a.x + b * a.x_sb + n * a.x_sn + i * 16;
+    const int64_t x_sh = a.x_sh, y_sh = a.y_sh;
+    uint4 w[U];
+    auto load = [&](int hb, uint4 (&to)[U]) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = hb + u * P + g;
+        to[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (mine && h < h1) to[u] = *reinterpret_cast<const uint4*>(src + h * x_sh);
+      }
+    };
+    load(h0, w);
     int pos = 0;
     const bool turn = which < 2 && position_of(p, a, which, t, b, n, pos);
-    const uint8_t* src = a.x + b * a.x_sb + n * a.x_sn + i * 16;
     uint8_t* dst = a.y + i * 16;
     if (kPages && which > 0) {
       const int64_t slot = __ldg(p.slots + t);
@@ -87,72 +102,54 @@ rotary_kernel(const RotaryParams p) {
     } else {
       dst += b * a.y_sb + n * a.y_sn;
     }
-    uint4 w[U];
-    auto load = [&](int hb) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = hb + u * P + g;
-        w[u] = make_uint4(0u, 0u, 0u, 0u);
-        if (mine && h < h1) w[u] = *reinterpret_cast<const uint4*>(src + h * a.x_sh);
-      }
-    };
-    auto store = [&](int hb) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = hb + u * P + g;
-        if (mine && h < h1) *reinterpret_cast<uint4*>(dst + h * a.y_sh) = w[u];
-      }
-    };
-    load(h0);
-    if (!turn) {                           // values, and rows that no sequence has
-      for (int hb = h0;;) {
-        store(hb);
-        if ((hb += P * U) >= h1) break;
-        load(hb);
-      }
-      continue;
-    }
-    float C[8], S[8];
-    turns.at(p.rule, i, pos, C, S);
-    if constexpr (kNorm) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = min(8 * i + e, p.rule.d - 1);
-        C[e] *= weight_at(a.weight, p.weights_fp32, c);
-        S[e] *= weight_at(a.weight, p.weights_fp32, partner_of<kPairs>(c, p.rule.rotary));
-      }
-    }
-    for (int hb = h0;;) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float x[8], y[8];
-        unpack8(w[u], x);
-        if constexpr (kPairs == kHalvesOdd) {
-          __syncwarp();
-          buf[lane] = w[u];
-          __syncwarp();
-        }
-        partners<kPairs>(w[u], x, from, reinterpret_cast<const __nv_bfloat16*>(buf + g * L), mine ? i : 0, p.rule.rotary, 0xffffffffu, y);
-        float r = 1.f;
-        if constexpr (kNorm) {
-          float sum = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
-#pragma unroll
-          for (int m = L / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-          r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
-        }
+    uint64_t C2[4], S2[4];
+    if (turn) {
+      float C[8], S[8];
+      turns.at(p.rule, turns_s, pos, kAll, C, S);
+      if constexpr (kNorm) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          x[e] *= C[e];
-          if (turns.on(e)) x[e] = fmaf(y[e], S[e], x[e]);
-          if constexpr (kNorm) x[e] *= r;
+          const int c = 8 * turns.i + e;
+          C[e] *= weight_at(a.weight, p.weights_fp32, c);
+          S[e] *= weight_at(a.weight, p.weights_fp32, partner_of<kPairs>(c, p.rule.rotary));
         }
-        w[u] = pack8(x);
       }
-      store(hb);
-      if ((hb += P * U) >= h1) break;
-      load(hb);
+      pack_turns(C, S, C2, S2);
+    }
+    for (int hb = h0; hb < h1; hb += P * U) {
+      uint4 next[U];
+      if (hb + P * U < h1) load(hb + P * U, next);
+      if (turn) {                          // (not: values, and rows that no sequence has)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          uint64_t x[4], y[4];
+          if constexpr (kPairs == kHalvesOdd) {
+            __syncwarp();
+            buf[lane] = w[u];
+            __syncwarp();
+          }
+          pairs_of(w[u], x);
+          turns.partners(w[u], reinterpret_cast<const __nv_bfloat16*>(buf + g * L), p.rule.rotary, kAll, y);
+          if constexpr (kNorm) {
+            float sum = f2_sum(f2_fma(x[0], x[0], f2_fma(x[1], x[1], f2_fma(x[2], x[2], f2_mul(x[3], x[3])))));
+#pragma unroll
+            for (int m = L / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(kAll, sum, m);
+            const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
+            turn_pairs(x, y, C2, S2);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = f2_mul(x[j], f2(r, r));
+          } else {
+            turn_pairs(x, y, C2, S2);
+          }
+          w[u] = rows_of(x);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = hb + u * P + g;
+        if (mine && h < h1) *reinterpret_cast<uint4*>(dst + h * y_sh) = w[u];
+        w[u] = next[u];
+      }
     }
   }
 }
@@ -161,91 +158,115 @@ rotary_kernel(const RotaryParams p) {
 //   dx = r (g w - n mean(g w n)),   dw = sum over rows and heads of g n.
 // A block works on q or on k alone, keeps its sums per column in registers and leaves them in the workspace.
 template <int L, int kPairs>
-__global__ void __launch_bounds__(kRotaryThreads)
+__global__ void __launch_bounds__(kRotaryThreads, 2)
 rotary_norm_bwd_kernel(const RotaryParams p) {
   constexpr int P = 32 / L, U = 2;
+  constexpr uint32_t kAll = 0xffffffffu;
+  __shared__ uint64_t turns_s[kMaxPairs];
   __shared__ uint4 rows_s[kPairs == kHalvesOdd ? kRotaryWarps * 32 : 1];
   __shared__ float sums_s[kRotaryWarps][256];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, i = lane % L;
   const bool mine = 8 * i < p.rule.d;
-  const int from = g * L + (mine ? partner_of<kHalves>(8 * i, p.rule.rotary) / 8 : i);
   uint4* const buf = rows_s + (kPairs == kHalvesOdd ? warp * 32 : 0);
   const int which = (int)blockIdx.x < p.q_blocks ? 0 : 1, block = blockIdx.x - (which ? p.q_blocks : 0);
   const int blocks = which ? gridDim.x - p.q_blocks : p.q_blocks;
   const RotaryTensor& a = p.t[which];
   LaneTurns<kPairs> turns;
-  turns.load(p.rule, i);
-  float W[8], dw[8];
+  turns.set(p.rule, i, g * L);
+  load_turns(p.rule, turns_s);
+  __syncthreads();
+  uint64_t W[4], dw[4];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    W[e] = weight_at(a.weight, p.weights_fp32, min(8 * i + e, p.rule.d - 1));
-    dw[e] = 0.f;
+  for (int j = 0; j < 4; ++j) {
+    W[j] = f2(weight_at(a.weight, p.weights_fp32, 8 * turns.i + 2 * j), weight_at(a.weight, p.weights_fp32, 8 * turns.i + 2 * j + 1));
+    dw[j] = 0;
   }
   for (int item = block * kRotaryWarps + warp; item < a.items; item += blocks * kRotaryWarps) {
     const int t = (int)a.by_spans.div((uint32_t)item), h0 = (item - t * (int)a.by_spans.d) * a.span, h1 = min(h0 + a.span, a.H);
     const int b = (int)a.by_n.div((uint32_t)t), n = t - b * a.N;
-    int pos = 0;
-    const bool turn = position_of(p, a, which, t, b, n, pos);
     const uint8_t* gp = a.g + b * a.g_sb + n * a.g_sn + i * 16;
     const uint8_t* xp = a.x + b * a.x_sb + n * a.x_sn + i * 16;
     uint8_t* dst = a.y + b * a.y_sb + n * a.y_sn + i * 16;
-    float C[8], S[8];
-    if (turn) turns.at(p.rule, i, pos, C, S);
-    for (int hb = h0; hb < h1; hb += P * U) {
-      uint4 wg[U], wx[U];
+    uint4 wg[U], wx[U];
+    auto load = [&](int hb, uint4 (&tg)[U], uint4 (&tx)[U]) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int h = hb + u * P + g;
-        wg[u] = wx[u] = make_uint4(0u, 0u, 0u, 0u);
+        tg[u] = tx[u] = make_uint4(0u, 0u, 0u, 0u);
         if (mine && h < h1) {
-          wg[u] = *reinterpret_cast<const uint4*>(gp + h * a.g_sh);
-          wx[u] = *reinterpret_cast<const uint4*>(xp + h * a.x_sh);
+          tg[u] = *reinterpret_cast<const uint4*>(gp + h * a.g_sh);
+          tx[u] = *reinterpret_cast<const uint4*>(xp + h * a.x_sh);
         }
       }
+    };
+    load(h0, wg, wx);
+    int pos = 0;
+    const bool turn = position_of(p, a, which, t, b, n, pos);
+    uint64_t C2[4], S2[4];
+    if (turn) {
+      float C[8], S[8];
+      turns.at(p.rule, turns_s, pos, kAll, C, S);
+      pack_turns(C, S, C2, S2);
+    }
+    for (int hb = h0; hb < h1; hb += P * U) {
+      uint4 ng[U], nx[U];
+      if (hb + P * U < h1) load(hb + P * U, ng, nx);
+      if (turn) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = hb + u * P + g;
-        if (turn) {
-          float x[8], y[8], z[8];
-          unpack8(wg[u], x);
+        for (int u = 0; u < U; ++u) {
+          uint64_t x[4], y[4], z[4];
           if constexpr (kPairs == kHalvesOdd) {
             __syncwarp();
             buf[lane] = wg[u];
             __syncwarp();
           }
-          partners<kPairs>(wg[u], x, from, reinterpret_cast<const __nv_bfloat16*>(buf + g * L), mine ? i : 0, p.rule.rotary, 0xffffffffu, y);
-          unpack8(wx[u], z);
-          float sum = 0.f, dot = 0.f;
+          pairs_of(wg[u], x);
+          turns.partners(wg[u], reinterpret_cast<const __nv_bfloat16*>(buf + g * L), p.rule.rotary, kAll, y);
+          turn_pairs(x, y, C2, S2);
+          pairs_of(wx[u], z);
+          uint64_t gw[4], s2 = 0, d2 = 0;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x[e] *= C[e];
-            if (turns.on(e)) x[e] = fmaf(y[e], S[e], x[e]);
-            sum = fmaf(z[e], z[e], sum);
-            dot = fmaf(x[e] * W[e], z[e], dot);
+          for (int j = 0; j < 4; ++j) {
+            gw[j] = f2_mul(x[j], W[j]);
+            s2 = f2_fma(z[j], z[j], s2);
+            d2 = f2_fma(gw[j], z[j], d2);
           }
+          float sum = f2_sum(s2), dot = f2_sum(d2);
 #pragma unroll
           for (int m = L / 2; m > 0; m >>= 1) {
-            sum += __shfl_xor_sync(0xffffffffu, sum, m);
-            dot += __shfl_xor_sync(0xffffffffu, dot, m);
+            sum += __shfl_xor_sync(kAll, sum, m);
+            dot += __shfl_xor_sync(kAll, dot, m);
           }
-          const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps)), back = r * r * dot * p.inv_d;
+          const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps)), back = -(r * r * dot * p.inv_d);
+          const uint64_t r2 = f2(r, r), back2 = f2(back, back);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            dw[e] = fmaf(x[e], z[e] * r, dw[e]);
-            x[e] = r * fmaf(-z[e], back, x[e] * W[e]);
+          for (int j = 0; j < 4; ++j) {
+            dw[j] = f2_fma(x[j], f2_mul(z[j], r2), dw[j]);
+            x[j] = f2_mul(r2, f2_fma(z[j], back2, gw[j]));
           }
-          wg[u] = pack8(x);
+          wg[u] = rows_of(x);
         }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = hb + u * P + g;
         if (mine && h < h1) *reinterpret_cast<uint4*>(dst + h * a.y_sh) = wg[u];
+        wg[u] = ng[u];
+        wx[u] = nx[u];
       }
     }
   }
   if (!a.dw) return;                       // (the same for all of a block)
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int j = 0; j < 4; ++j) {
+    float s[2];
+    f2_get(dw[j], s[0], s[1]);
 #pragma unroll
-    for (int m = L; m < 32; m <<= 1) dw[e] += __shfl_xor_sync(0xffffffffu, dw[e], m);
-    if (g == 0 && mine) sums_s[warp][8 * i + e] = dw[e];
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int m = L; m < 32; m <<= 1) s[e] += __shfl_xor_sync(kAll, s[e], m);
+      if (g == 0 && mine) sums_s[warp][8 * i + 2 * j + e] = s[e];
+    }
   }
   __syncthreads();
   if ((int)threadIdx.x < p.rule.d) {
@@ -478,23 +499,11 @@ static int packed_call(RotaryCall* c, const int32_t* cu_q, const int32_t* cu_k, 
   return MALA_OK;
 }
 
-// A serving step, bf16 pages: q to q_out, k and v into their slots.  (Also q alone, in front of the e4m3 write.)
-int rotary_step(mala_tin q, mala_tin k, mala_tin v, const int32_t* positions, const int64_t* slots, mala_tout qo, mala_tout kp, mala_tout vp,
-                const mala_rotary* r, const mala_head_norm* norm, int rows, int Hq, int Hkv, int64_t limit, int page_size, int d, cudaStream_t stream) {
-  int dev = 0, *status = nullptr;
-  MALA_TRY(current_device_checked(&dev));
-  MALA_TRY(device_setup(dev, &status));
-  RotaryParams p = {};
-  set_rule(&p, r, norm, d, false);
-  set_tensor(&p.t[0], q, qo, 1, rows, Hq, 0);
-  if (k.p) {
-    set_tensor(&p.t[1], k, kp, 1, rows, Hkv, 0);
-    set_tensor(&p.t[2], v, vp, 1, rows, Hkv, 0);
-    p.slots = slots; p.limit = limit; p.page_size = page_size; p.by_page.set((uint32_t)page_size);
-  }
-  p.positions = positions; p.pos_n = rows;
-  set_items(&p, k.p ? 3 : 1, sm_count(dev));
-  return norm ? launch_rotary<true, true>(p, r->interleaved, sm_count(dev), stream) : launch_rotary<false, true>(p, r->interleaved, sm_count(dev), stream);
+// Rows of q alone at their positions (in front of the e4m3 write)
+int rotate_queries(mala_tin q, const int32_t* positions, mala_tout qo, const mala_rotary* r, const mala_head_norm* norm, int rows, int Hq, int d,
+                   cudaStream_t stream) {
+  return rotate(RotaryCall{1, rows, rows, Hq, 0, d, positions, nullptr, nullptr, 0}, q, mala_tin{nullptr, 0, 0, 0}, qo, mala_tout{nullptr, 0, 0, 0}, r, norm, false,
+                stream);
 }
 
 int check_rotary_step(mala_tin q, const int32_t* positions, mala_tout qo, const mala_rotary* r, const mala_head_norm* norm, int rows, int Hq, int d) {
@@ -546,6 +555,30 @@ int mala_rotary_bwd_varlen(mala_tin dq, mala_tin dk, mala_tin q, mala_tin k, con
   RotaryCall c;
   MALA_TRY(packed_call(&c, cu_seqlens_q, cu_seqlens_k, B, total_q, total_k, Hq, Hkv, d));
   return scope.finish(rotate_back(c, dq, dk, q, k, dq_out, dk_out, rotary, norm, dq_weight, dk_weight, ws, ws_bytes, (cudaStream_t)cuda_stream));
+}
+
+// k and v into bf16 pages: q's rows, k's and v's in one launch
+int mala_rotary_write(mala_tin q, mala_tin k, mala_tin v, const int32_t* positions, const int64_t* slots, const mala_rotary* rotary,
+                      const mala_head_norm* norm, mala_tout q_out, mala_tout kpages, mala_tout vpages, int rows, int Hq, int Hkv, int num_pages,
+                      int page_size, int d, void* cuda_stream) {
+  ApiScope scope("mala_rotary_write", cuda_stream);
+  MALA_TRY(check_cache_write(k, v, slots, kpages, vpages, nullptr, nullptr, rows, Hkv, num_pages, page_size, d, false));
+  MALA_TRY(check_rotary_step(q, positions, q_out, rotary, norm, rows, Hq, d));
+  if (rows == 0) return MALA_OK;
+  int dev = 0, *status = nullptr;
+  MALA_TRY(current_device_checked(&dev));
+  MALA_TRY(device_setup(dev, &status));
+  RotaryParams p = {};
+  set_rule(&p, rotary, norm, d, false);
+  set_tensor(&p.t[0], q, q_out, 1, rows, Hq, 0);
+  set_tensor(&p.t[1], k, kpages, 1, rows, Hkv, 0);
+  set_tensor(&p.t[2], v, vpages, 1, rows, Hkv, 0);
+  p.slots = slots; p.limit = (int64_t)num_pages * page_size; p.page_size = page_size; p.by_page.set((uint32_t)page_size);
+  p.positions = positions; p.pos_n = rows;
+  set_items(&p, 3, sm_count(dev));
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  return scope.finish(norm ? launch_rotary<true, true>(p, rotary->interleaved, sm_count(dev), stream)
+                           : launch_rotary<false, true>(p, rotary->interleaved, sm_count(dev), stream));
 }
 
 }  // extern "C"

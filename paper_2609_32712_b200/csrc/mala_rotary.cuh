@@ -39,46 +39,12 @@ __device__ __forceinline__ void cos_sin(uint64_t f, int pos, float& c, float& s)
   s = __uint_as_float(__float_as_uint(b) ^ ((quarter & 2) << 30));
 }
 
-// What a lane that holds the columns 8 i .. 8 i + 7 of a row needs for its rotations: out = C x + S x', x' the column's partner.
-template <int kPairs>
-struct LaneTurns {
-  static constexpr int kAngles = kPairs == kNeighbours ? 4 : 8;
-  uint64_t f[kAngles];
-  uint32_t rotated;         // bit e: column 8 i + e is one of the rotated ones
-  __device__ __forceinline__ void load(const RotaryRule& r, int i) {
-    rotated = 0;
-#pragma unroll
-    for (int j = 0; j < kAngles; ++j) {
-      const int c = kPairs == kNeighbours ? 8 * i + 2 * j : 8 * i + j, half = r.rotary / 2;
-      const int pair = kPairs == kNeighbours ? c / 2 : c < half ? c : c - half;
-      f[j] = 0;
-      if (c < r.rotary) {
-        f[j] = turns_of(__ldg(r.inv_freq + pair));
-        rotated |= (kPairs == kNeighbours ? 3u << (2 * j) : 1u << j);
-      }
-    }
-  }
-  // C and S of the lane's columns at a position (columns that are not rotated: 1 and nothing)
-  __device__ __forceinline__ void at(const RotaryRule& r, int i, int pos, float (&C)[8], float (&S)[8]) const {
-#pragma unroll
-    for (int j = 0; j < kAngles; ++j) {
-      float c, s;
-      cos_sin(f[j], pos, c, s);
-      c *= r.magnitude;
-      s *= r.turned;
-      if constexpr (kPairs == kNeighbours) {
-        const bool on = (rotated >> (2 * j)) & 1;
-        C[2 * j] = C[2 * j + 1] = on ? c : 1.f;
-        S[2 * j] = -s;
-        S[2 * j + 1] = s;
-      } else {
-        C[j] = (rotated >> j) & 1 ? c : 1.f;
-        S[j] = 8 * i + j < r.rotary / 2 ? -s : s;
-      }
-    }
-  }
-  __device__ __forceinline__ bool on(int e) const { return (rotated >> e) & 1; }
-};
+constexpr int kMaxPairs = 128;    // of 256 columns
+
+// The frequencies of a block's rotations, in its shared memory (the caller synchronises the block)
+__device__ __forceinline__ void load_turns(const RotaryRule& r, uint64_t* turns) {
+  for (int x = threadIdx.x; x < r.rotary / 2; x += blockDim.x) turns[x] = turns_of(__ldg(r.inv_freq + x));
+}
 
 // Column that c is paired with (itself where it is not rotated)
 template <int kPairs>
@@ -88,28 +54,108 @@ __device__ __forceinline__ int partner_of(int c, int rotary) {
   return c < rotary / 2 ? c + rotary / 2 : c - rotary / 2;
 }
 
-__device__ __forceinline__ void unpack8(const uint4& w, float (&x)[8]) {
-  x[0] = __uint_as_float(w.x << 16); x[1] = __uint_as_float(w.x & 0xffff0000u);
-  x[2] = __uint_as_float(w.y << 16); x[3] = __uint_as_float(w.y & 0xffff0000u);
-  x[4] = __uint_as_float(w.z << 16); x[5] = __uint_as_float(w.z & 0xffff0000u);
-  x[6] = __uint_as_float(w.w << 16); x[7] = __uint_as_float(w.w & 0xffff0000u);
-}
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-  return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+// bf16 pairs as fp32 side by side, and back
+__device__ __forceinline__ uint64_t pair_of(uint32_t w) { return f2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ uint64_t crossed_pair_of(uint32_t w) { return f2(__uint_as_float(w & 0xffff0000u), __uint_as_float(w << 16)); }
+__device__ __forceinline__ void pairs_of(const uint4& w, uint64_t (&x)[4]) { x[0] = pair_of(w.x); x[1] = pair_of(w.y); x[2] = pair_of(w.z); x[3] = pair_of(w.w); }
+__device__ __forceinline__ uint4 rows_of(const uint64_t (&x)[4]) { return make_uint4(f2_bf16(x[0]), f2_bf16(x[1]), f2_bf16(x[2]), f2_bf16(x[3])); }
+__device__ __forceinline__ float f2_sum(uint64_t x) {
+  float a, b;
+  f2_get(x, a, b);
+  return a + b;
 }
 
-// The partners of a lane's columns: the row lies in the registers of the lanes of a group, its columns 8 i .. in lane i (kHalves: i is
-// `from`, a lane of the warp), or in shared memory at `row` (kHalvesOdd; written by the group before).
+// What a lane needs to rotate its columns 8 i .. 8 i + 7:  out = C x + S x',  x' the column's partner, two columns at a time.  Where a column is
+// not rotated C = 1, S = -0 and x' is read as 0, so that it stays whatever it is.
 template <int kPairs>
-__device__ __forceinline__ void partners(const uint4& w, const float (&x)[8], int from, const __nv_bfloat16* row, int i, int rotary, uint32_t group, float (&y)[8]) {
-  if constexpr (kPairs == kHalves) {
-    unpack8(make_uint4(__shfl_sync(group, w.x, from), __shfl_sync(group, w.y, from), __shfl_sync(group, w.z, from), __shfl_sync(group, w.w, from)), y);
-  } else if constexpr (kPairs == kNeighbours) {
+struct LaneTurns {
+  int i, from;              // (kHalves: the lane of the warp that holds the partners)
+  uint32_t rotated;         // bit e: column 8 i + e is one of the rotated ones
+  // lane_of_row: of the lanes that hold a row, the first one of which is lane `base` of the warp
+  __device__ __forceinline__ void set(const RotaryRule& r, int lane_of_row, int base) {
+    const bool mine = 8 * lane_of_row < r.d;
+    i = mine ? lane_of_row : 0;                          // (lanes behind the row: any of it)
+    from = base + (mine ? partner_of<kHalves>(8 * i, r.rotary) / 8 : lane_of_row);
+    rotated = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = x[e ^ 1];
-  } else {
+    for (int e = 0; e < 8; ++e) rotated |= (8 * i + e < r.rotary ? 1u : 0u) << e;
+  }
+  // a mask of a register with the columns 8 i + 2 j and 8 i + 2 j + 1: those that are rotated
+  __device__ __forceinline__ uint32_t mask(int j) const {
+    if (kPairs == kHalves) return rotated ? 0xffffffffu : 0u;
+    return ((rotated >> (2 * j)) & 1 ? 0xffffu : 0u) | ((rotated >> (2 * j + 1)) & 1 ? 0xffff0000u : 0u);
+  }
+  // C and S at a position; `group`: the lanes that make this call together (their rows in full)
+  __device__ __forceinline__ void at(const RotaryRule& r, const uint64_t* turns, int pos, uint32_t group, float (&C)[8], float (&S)[8]) const {
+    const int half = r.rotary / 2;
+    if constexpr (kPairs == kHalves) {
+      // the two lanes of a pair need the same eight angles: four each, and the others' by shuffles
+      const bool first = 8 * i < half;
+      const uint64_t* f = turns + (rotated ? first ? 8 * i : 8 * i - half + 4 : 0);
+      float c[4], s[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = __bfloat162float(row[partner_of<kPairs>(8 * i + e, rotary)]);
+      for (int j = 0; j < 4; ++j) {
+        cos_sin(f[j], pos, c[j], s[j]);
+        c[j] *= r.magnitude;
+        s[j] *= r.turned;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float c2 = __shfl_sync(group, c[j], from), s2 = __shfl_sync(group, s[j], from);
+        C[j] = rotated ? first ? c[j] : c2 : 1.f;
+        C[j + 4] = rotated ? first ? c2 : c[j] : 1.f;
+        S[j] = rotated ? first ? -s[j] : s2 : -0.f;
+        S[j + 4] = rotated ? first ? -s2 : s[j] : -0.f;
+      }
+    } else {
+      constexpr int kAngles = kPairs == kNeighbours ? 4 : 8;
+#pragma unroll
+      for (int j = 0; j < kAngles; ++j) {
+        const int col = kPairs == kNeighbours ? 8 * i + 2 * j : 8 * i + j;
+        const bool turn = col < r.rotary;
+        float c, s;
+        cos_sin(turns[!turn ? 0 : kPairs == kNeighbours ? col / 2 : col < half ? col : col - half], pos, c, s);
+        c = turn ? c * r.magnitude : 1.f;
+        s = turn ? s * r.turned : -0.f;
+        if constexpr (kPairs == kNeighbours) {
+          C[2 * j] = C[2 * j + 1] = c;
+          S[2 * j] = turn ? -s : s;
+          S[2 * j + 1] = s;
+        } else {
+          C[j] = c;
+          S[j] = turn && col < half ? -s : s;
+        }
+      }
+    }
+  }
+  // x' of the lane's columns: the row lies in the registers of the lanes of `group`, or (kHalvesOdd) in shared memory at `row`, written before
+  __device__ __forceinline__ void partners(const uint4& w, const __nv_bfloat16* row, int rotary, uint32_t group, uint64_t (&y)[4]) const {
+    const uint32_t own[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (kPairs == kHalves) {
+        y[j] = pair_of(__shfl_sync(group, own[j], from) & mask(j));
+      } else if constexpr (kPairs == kNeighbours) {
+        y[j] = crossed_pair_of(own[j] & mask(j));
+      } else {
+        const float a = __bfloat162float(row[partner_of<kPairs>(8 * i + 2 * j, rotary)]);
+        const float b = __bfloat162float(row[partner_of<kPairs>(8 * i + 2 * j + 1, rotary)]);
+        y[j] = f2((rotated >> (2 * j)) & 1 ? a : 0.f, (rotated >> (2 * j + 1)) & 1 ? b : 0.f);
+      }
+    }
+  }
+};
+
+// x <- C x + S x'
+__device__ __forceinline__ void turn_pairs(uint64_t (&x)[4], const uint64_t (&y)[4], const uint64_t (&C)[4], const uint64_t (&S)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = f2_fma(y[j], S[j], f2_mul(x[j], C[j]));
+}
+__device__ __forceinline__ void pack_turns(const float (&C)[8], const float (&S)[8], uint64_t (&C2)[4], uint64_t (&S2)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    C2[j] = f2(C[2 * j], C[2 * j + 1]);
+    S2[j] = f2(S[2 * j], S[2 * j + 1]);
   }
 }
 

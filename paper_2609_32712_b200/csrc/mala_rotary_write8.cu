@@ -1,0 +1,394 @@
+// A serving step's keys and values into e4m3 pages, the keys rotated (and normed) on their way.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/mala.h"
+#include "mala_decode_sched.cuh"
+#include "mala_e4m3.cuh"
+#include "mala_internal.h"
+#include "mala_rotary.cuh"
+
+namespace mala {
+
+constexpr int kWriteThreads = 512, kWriteRows = 128;   // threads of a block; most rows that it has at once (a unit's)
+
+struct RotaryWriteParams {
+  const uint8_t* k; const uint8_t* v;      // [rows, Hkv, d] bf16
+  int64_t k_sn, k_sh, v_sn, v_sh;          // bytes
+  uint8_t* kp; uint8_t* vp;                // [num_pages, page_size, Hkv, d] codes
+  int64_t kp_sb, kp_sn, kp_sh, vp_sb, vp_sn, vp_sh;
+  float* kscale; float* vscale;            // [num_pages, Hkv, per_page]
+  const int64_t* slots; const int* positions;
+  int rows, Hkv, d, page_size, per_page, unit, chunk, heads, lanes;   // rows and heads of a block; lanes of a row
+  int64_t limit;
+  FastDiv by_page;
+  RotaryRule rule;
+  const void* weight; int weights_fp32, weighted, normed;   // (weighted 0: weight is not read, but a pointer all the same)
+  float eps, inv_d;
+};
+
+// A unit's scale follows from all of its rows, behind their rotation, so a block holds a unit's rows in registers, in fp32, between its
+// maximum and its codes: they are read once and rotated once.  The block takes the units that begin among `chunk` rows of the call, up to
+// kWriteRows rows of them at a time, and `heads` heads one after the other: a row's angles are worked out once for all of
+// them, and the next head's rows are on their way meanwhile.  A row's lanes have two pieces of eight columns each: columns and their
+// partners (halves), or neighbouring pieces.  Between maxima and codes of a head the block meets once; the units' maxima
+// change places among three buffers, so that one is emptied while two are in use.
+template <int kPairs, int kPer>            // kPer: rows of a thread
+__global__ void __launch_bounds__(kWriteThreads, 1)
+rotary_write8_kernel(const RotaryWriteParams p) {
+  constexpr uint32_t kAll = 0xffffffffu;
+  __shared__ uint64_t turns_s[kMaxPairs];
+  __shared__ int64_t slot_s[kWriteRows];
+  __shared__ uint32_t ends_s[kWriteRows / 32], valid_s[kWriteRows / 32];
+  __shared__ float max_s[3][kWriteRows], old_s[2][kWriteRows], weight_s[128];
+  __shared__ uint4 odd_s[kPairs == kHalvesOdd ? kWriteThreads * 2 : 1];
+  const bool is_v = blockIdx.z != 0;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int lanes = p.lanes, c = tid & (lanes - 1), r0 = tid / lanes, step = kWriteThreads / lanes, window = min(kWriteRows, kPer * step);
+  const int t0 = blockIdx.x * p.chunk, t1 = min(t0 + p.chunk, p.rows), h0 = blockIdx.y * p.heads, h1 = min(h0 + p.heads, p.Hkv);
+  // this thread's pieces: columns 8 pa .. and 8 pb ..
+  const int pieces = p.d / 8, turned = p.rule.rotary / 16;          // (halves: lanes whose pieces are partners)
+  const bool pair = kPairs == kHalves && c < turned;
+  const int pa = pair ? c : 2 * c, pb = pair ? c + turned : 2 * c + 1;
+  const bool mine = 2 * c < pieces;
+  const uint8_t* const src = (is_v ? p.v : p.k);
+  const int64_t s_sn = is_v ? p.v_sn : p.k_sn, s_sh = is_v ? p.v_sh : p.k_sh;
+  uint8_t* const pages = is_v ? p.vp : p.kp;
+  const int64_t d_sb = is_v ? p.vp_sb : p.kp_sb, d_sn = is_v ? p.vp_sn : p.kp_sn, d_sh = is_v ? p.vp_sh : p.kp_sh;
+  float* const scales = is_v ? p.vscale : p.kscale;
+  if (!is_v) {
+    load_turns(p.rule, turns_s);
+    for (int x = tid; x < p.d; x += kWriteThreads) weight_s[x] = p.weighted ? weight_at(p.weight, p.weights_fp32, x) : 1.f;
+  }
+  auto page_of = [&](int64_t slot, int64_t& at) -> int64_t {
+    const int64_t page = p.limit <= 0xffffffffll ? (int64_t)p.by_page.div((uint32_t)slot) : slot / p.page_size;
+    at = slot - page * p.page_size;
+    return page;
+  };
+
+  for (int s = t0; s < t1;) {              // rounds: rows s .. s + window - 1
+    __syncthreads();                       // (the round before is over)
+    if (tid < window) {
+      const int t = s + tid;
+      int64_t slot = -1, prev = -2;
+      if (t < p.rows) {
+        slot = __ldg(p.slots + t);
+        if (t > 0) prev = __ldg(p.slots + t - 1);
+      }
+      const bool valid = slot >= 0 && slot < p.limit;
+      slot_s[tid] = slot;
+      const uint32_t ends = __ballot_sync(kAll, !valid || (slot & (p.unit - 1)) == 0 || prev + 1 != slot), places = __ballot_sync(kAll, valid);
+      if (lane == 0) { ends_s[warp] = ends; valid_s[warp] = places; }
+      max_s[0][tid] = max_s[1][tid] = max_s[2][tid] = 0.f;
+    }
+    __syncthreads();
+    const int words = window / 32;
+    // first row at or behind j with a bit (window: none)
+    auto next_end = [&](int j) -> int {
+      for (int w = j >> 5; w < words; ++w) {
+        const uint32_t bits = w == j >> 5 ? ends_s[w] >> (j & 31) << (j & 31) : ends_s[w];
+        if (bits) return w * 32 + __ffs(bits) - 1;
+      }
+      return window;
+    };
+    // a unit that begins at row j of the window belongs to this round: to this block, and all of it is in the window
+    auto taken = [&](int j) -> bool {
+      if (!((valid_s[j >> 5] & ends_s[j >> 5]) >> (j & 31) & 1u) || s + j >= t1) return false;
+      return min(next_end(j + 1), j + p.unit - (int)(slot_s[j] & (p.unit - 1))) < window || j + p.unit - (int)(slot_s[j] & (p.unit - 1)) <= window;
+    };
+    // a round begins with a unit of this block
+    int begin = next_end(0);
+    while (begin < window && !((valid_s[begin >> 5] >> (begin & 31)) & 1u)) begin = next_end(begin + 1);
+    if (begin >= window || s + begin >= t1) {
+      if (begin < window || s + window >= t1) break;
+      s += window;                         // (nothing but rows without a place, or another block's)
+      continue;
+    }
+    if (begin > 0) {
+      s += begin;
+      continue;
+    }
+    // this thread's rows: the row their unit begins at (-1: none), and where they go
+    int unit_at[kPer];
+    int64_t to[kPer];
+    uint32_t pos[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int j = r0 + i * step;
+      unit_at[i] = -1;
+      to[i] = 0;
+      pos[i] = 0;
+      if (j < window && ((valid_s[j >> 5] >> (j & 31)) & 1u)) {
+        int b = j;                         // the last row at or before j with a bit
+        for (int w = j >> 5; w >= 0; --w) {
+          const uint32_t bits = w == j >> 5 ? ends_s[w] << (31 - (j & 31)) >> (31 - (j & 31)) : ends_s[w];
+          if (bits) { b = w * 32 + 31 - __clz((int)bits); break; }
+          b = -1;
+        }
+        // (a unit cut off at the window's front begins in another block, or was this one's before)
+        if (b >= 0 && taken(b)) {
+          int64_t at;
+          const int64_t page = page_of(slot_s[j], at);
+          unit_at[i] = b;
+          to[i] = page * d_sb + at * d_sn;
+          if (!is_v) pos[i] = (uint32_t)__ldg(p.positions + s + j);
+        }
+      }
+    }
+    // where the next round begins: the first unit of this block that is not taken
+    int next = t1;
+    for (int j = next_end(0); j < window && s + j < t1; j = next_end(j + 1))
+      if (((valid_s[j >> 5] >> (j & 31)) & 1u) && !taken(j)) { next = s + j; break; }
+    // this thread's unit, if it keeps one: row tid begins it
+    const bool keeper = tid < window && taken(tid);
+    float* scale = scales;
+    if (keeper) {
+      int64_t at;
+      const int64_t page = page_of(slot_s[tid], at);
+      scale += page * p.Hkv * p.per_page + at / 128;
+    }
+    float C[kPer][8], S[kPer][8];
+    if (!is_v && kPairs != kHalvesOdd) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int x = 8 * c + e;
+          const bool on = x < p.rule.rotary / 2;
+          cos_sin(turns_s[on ? x : 0], (int)pos[i], C[i][e], S[i][e]);
+          C[i][e] = on ? C[i][e] * p.rule.magnitude : 1.f;
+          S[i][e] = on ? S[i][e] * p.rule.turned : 0.f;
+        }
+    }
+    // whether all of the warp's rows have one unit (then the warp adds to its maximum once)
+    int one = unit_at[0];
+#pragma unroll
+    for (int i = 1; i < kPer; ++i) one = unit_at[i] == one ? one : -1;
+    one = __all_sync(kAll, one == __shfl_sync(kAll, one, 0)) ? one : -1;
+
+    uint4 ra[kPer], rb[kPer];
+    float old_next = 0.f;
+    auto load = [&](int h) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        ra[i] = rb[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (mine && unit_at[i] >= 0) {
+          const uint8_t* from = src + (int64_t)(s + r0 + i * step) * s_sn + h * s_sh;
+          ra[i] = *reinterpret_cast<const uint4*>(from + pa * 16);
+          rb[i] = *reinterpret_cast<const uint4*>(from + pb * 16);
+        }
+      }
+      if (keeper) old_next = *(volatile const float*)(scale + (int64_t)h * p.per_page);
+    };
+    load(h0);
+    int buf = 0;
+    for (int h = h0; h < h1; ++h, buf = buf == 2 ? 0 : buf + 1) {
+      uint64_t a[kPer][4], b[kPer][4];     // the rows in fp32
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        pairs_of(ra[i], a[i]);
+        pairs_of(rb[i], b[i]);
+      }
+      if (kPairs == kHalvesOdd && !is_v) { // (rare: partners out of shared memory, angles column by column, one row of the thread after the other)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          __syncwarp();
+          odd_s[2 * tid] = ra[i];
+          odd_s[2 * tid + 1] = rb[i];
+          __syncwarp();
+          const __nv_bfloat16* row = reinterpret_cast<const __nv_bfloat16*>(odd_s + 2 * (tid - c));
+          float sum = f2_sum(f2_fma(a[i][0], a[i][0], f2_fma(a[i][1], a[i][1], f2_fma(a[i][2], a[i][2], f2_mul(a[i][3], a[i][3]))))) +
+                      f2_sum(f2_fma(b[i][0], b[i][0], f2_fma(b[i][1], b[i][1], f2_fma(b[i][2], b[i][2], f2_mul(b[i][3], b[i][3])))));
+          for (int m = lanes / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(kAll, sum, m);
+          const float r = p.normed ? rsqrtf(fmaf(sum, p.inv_d, p.eps)) : 1.f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int col = mine ? 16 * c + e : 0, half = p.rule.rotary / 2;
+            float x = __bfloat162float(row[col]) * r * weight_s[col];
+            if (col < p.rule.rotary) {
+              const int other = partner_of<kHalvesOdd>(col, p.rule.rotary);
+              float cs, sn;
+              cos_sin(turns_s[col < half ? col : col - half], (int)pos[i], cs, sn);
+              const float y = __bfloat162float(row[other]) * r * weight_s[other];
+              x = fmaf(y, (col < half ? -sn : sn) * p.rule.turned, x * (cs * p.rule.magnitude));
+            }
+            x = mine ? x : 0.f;
+            uint64_t& to2 = e < 8 ? a[i][e / 2] : b[i][(e - 8) / 2];
+            float lo, hi;
+            f2_get(to2, lo, hi);
+            to2 = e % 2 ? f2(lo, x) : f2(x, hi);
+          }
+        }
+      }
+      const float was_mine = old_next;
+      if (h + 1 < h1) load(h + 1);
+      float top[kPer];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (!is_v && kPairs != kHalvesOdd) {
+          if (p.normed) {
+            float sum = f2_sum(f2_fma(a[i][0], a[i][0], f2_fma(a[i][1], a[i][1], f2_fma(a[i][2], a[i][2], f2_mul(a[i][3], a[i][3]))))) +
+                        f2_sum(f2_fma(b[i][0], b[i][0], f2_fma(b[i][1], b[i][1], f2_fma(b[i][2], b[i][2], f2_mul(b[i][3], b[i][3])))));
+            for (int m = lanes / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(kAll, sum, m);
+            const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
+            const float* wa = weight_s + (mine ? 8 * pa : 0);
+            const float* wb = weight_s + (mine ? 8 * pb : 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              a[i][j] = f2_mul(f2_mul(a[i][j], f2(r, r)), f2(wa[2 * j], wa[2 * j + 1]));
+              b[i][j] = f2_mul(f2_mul(b[i][j], f2(r, r)), f2(wb[2 * j], wb[2 * j + 1]));
+            }
+          }
+          if constexpr (kPairs == kHalves) {
+            if (pair) {                    // (a, b) -> (a cos - b sin, b cos + a sin)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint64_t cs = f2(C[i][2 * j], C[i][2 * j + 1]), sn = f2(S[i][2 * j], S[i][2 * j + 1]), minus = f2(-S[i][2 * j], -S[i][2 * j + 1]);
+                const uint64_t x = a[i][j];
+                a[i][j] = f2_fma(b[i][j], minus, f2_mul(x, cs));
+                b[i][j] = f2_fma(x, sn, f2_mul(b[i][j], cs));
+              }
+            }
+          } else {                         // pairs 8 c .. 8 c + 3 in a, the next four in b
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              uint64_t& x = e < 4 ? a[i][e] : b[i][e - 4];
+              float lo, hi;
+              f2_get(x, lo, hi);
+              x = f2_fma(f2(hi, lo), f2(-S[i][e], S[i][e]), f2_mul(x, f2(C[i][e], C[i][e])));
+            }
+          }
+        }
+        top[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float x, y;
+          f2_get(a[i][j], x, y);
+          top[i] = max3(top[i], fabsf(x), fabsf(y));
+          f2_get(b[i][j], x, y);
+          top[i] = max3(top[i], fabsf(x), fabsf(y));
+        }
+      }
+      // the units' maxima (not negative: ordered like their bits)
+      if (one >= 0) {
+        float most = top[0];
+#pragma unroll
+        for (int i = 1; i < kPer; ++i) most = fmaxf(most, top[i]);
+#pragma unroll
+        for (int m = 16; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor_sync(kAll, most, m));
+        if (lane == 0) atomicMax(reinterpret_cast<int*>(&max_s[buf][one]), __float_as_int(most));
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          for (int m = lanes / 2; m > 0; m >>= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(kAll, top[i], m));
+          if (c == 0 && unit_at[i] >= 0) atomicMax(reinterpret_cast<int*>(&max_s[buf][unit_at[i]]), __float_as_int(top[i]));
+        }
+      }
+      const int par = (h - h0) & 1;
+      if (keeper) old_s[par][tid] = was_mine;
+      __syncthreads();
+      auto scale_of = [&](int u) -> float {
+        const float want = __fdiv_rn(max_s[buf][u], 448.f);
+        const float x = (slot_s[u] & (p.unit - 1)) == 0 ? want : fmaxf(old_s[par][u], want);
+        return x > 0.f ? x : 1.f;          // (nothing but zeros)
+      };
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (unit_at[i] < 0) continue;
+        const Quotients by(scale_of(unit_at[i]));
+        if (mine) {
+          uint8_t* at = pages + to[i] + h * d_sh;
+          *reinterpret_cast<uint2*>(at + 8 * pa) = make_uint2(by.four(a[i][0], a[i][1]), by.four(a[i][2], a[i][3]));
+          *reinterpret_cast<uint2*>(at + 8 * pb) = make_uint2(by.four(b[i][0], b[i][1]), by.four(b[i][2], b[i][3]));
+        }
+      }
+      if (keeper) scale[(int64_t)h * p.per_page] = scale_of(tid);
+      // units that hold keys already, and whose scale grows: these keys' codes on the new scale, by the whole block
+      for (int j = next_end(0); j < window; j = next_end(j + 1)) {
+        const int off = (int)(slot_s[j] & (p.unit - 1));
+        if (off == 0 || !taken(j)) continue;
+        const float was = old_s[par][j], now = scale_of(j);
+        if (!(now > was)) continue;
+        const Quotients by(now);
+        int64_t at;
+        const int64_t page = page_of(slot_s[j], at);
+        uint8_t* first = pages + page * d_sb + (at - off) * d_sn + h * d_sh + 16 * c;
+        if (mine)
+          for (int r = r0; r < off; r += step) {
+            uint4 o = *reinterpret_cast<const uint4*>(first + r * d_sn);
+            auto four = [&](uint32_t u) -> uint32_t {
+              const float2 x = from_e4m3x2((uint16_t)u), y = from_e4m3x2((uint16_t)(u >> 16));
+              return ((by.two(f2(x.x * was, x.y * was)) | (by.two(f2(y.x * was, y.y * was)) << 16)) & 0x7f7f7f7fu) | (u & 0x80808080u);
+            };
+            *reinterpret_cast<uint4*>(first + r * d_sn) = make_uint4(four(o.x), four(o.y), four(o.z), four(o.w));
+          }
+      }
+      // the buffer of the head behind the next one (last read before this head's meeting)
+      if (tid < window) max_s[buf == 0 ? 2 : buf - 1][tid] = 0.f;
+    }
+    s = next;
+  }
+}
+
+template <int kPairs>
+static int launch_write8(const RotaryWriteParams& p, bool two, dim3 grid, cudaStream_t stream) {
+  if (two) rotary_write8_kernel<kPairs, 2><<<grid, kWriteThreads, 0, stream>>>(p);
+  else rotary_write8_kernel<kPairs, 1><<<grid, kWriteThreads, 0, stream>>>(p);
+  return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+}
+
+}  // namespace mala
+
+using namespace mala;
+
+extern "C" int mala_rotary_write_fp8(mala_tin q, mala_tin k, mala_tin v, const int32_t* positions, const int64_t* slots, const mala_rotary* rotary,
+                                     const mala_head_norm* norm, mala_tout q_out, mala_tout kpages8, mala_tout vpages8, float* kscale, float* vscale,
+                                     int rows, int Hq, int Hkv, int num_pages, int page_size, int d, void* cuda_stream) {
+  ApiScope scope("mala_rotary_write_fp8", cuda_stream);
+  MALA_TRY(check_cache_write(k, v, slots, kpages8, vpages8, kscale, vscale, rows, Hkv, num_pages, page_size, d, true));
+  MALA_TRY(check_rotary_step(q, positions, q_out, rotary, norm, rows, Hq, d));
+  if (rows == 0) return MALA_OK;
+  int dev = 0, *status = nullptr;
+  MALA_TRY(current_device_checked(&dev));
+  MALA_TRY(device_setup(dev, &status));
+  cudaStream_t stream = (cudaStream_t)cuda_stream;
+  MALA_TRY(rotate_queries(q, positions, q_out, rotary, norm, rows, Hq, d, stream));
+  RotaryWriteParams p = {};
+  p.k = (const uint8_t*)k.p; p.v = (const uint8_t*)v.p;
+  p.k_sn = k.sn * 2; p.k_sh = k.sh * 2; p.v_sn = v.sn * 2; p.v_sh = v.sh * 2;
+  p.kp = (uint8_t*)kpages8.p; p.vp = (uint8_t*)vpages8.p;
+  p.kp_sb = kpages8.sb; p.kp_sn = kpages8.sn; p.kp_sh = kpages8.sh; p.vp_sb = vpages8.sb; p.vp_sn = vpages8.sn; p.vp_sh = vpages8.sh;
+  p.kscale = kscale; p.vscale = vscale; p.slots = slots; p.positions = positions;
+  p.rows = rows; p.Hkv = Hkv; p.d = d; p.page_size = page_size; p.per_page = page_size < 128 ? 1 : page_size / 128;
+  p.unit = page_size < 128 ? page_size : 128;
+  p.limit = (int64_t)num_pages * page_size;
+  p.by_page.set((uint32_t)page_size);
+  p.rule.inv_freq = rotary->inv_freq; p.rule.rotary = rotary->rotary; p.rule.d = d;
+  p.rule.magnitude = p.rule.turned = rotary->magnitude;
+  p.normed = norm ? 1 : 0;
+  p.weighted = norm && norm->k_weight ? 1 : 0;
+  p.weight = p.weighted ? norm->k_weight : (const void*)rotary->inv_freq;
+  p.weights_fp32 = norm ? norm->weights_fp32 : 0;
+  p.eps = norm ? norm->eps : 0.f; p.inv_d = 1.f / (float)d;
+  p.lanes = 1;
+  while (16 * p.lanes < d) p.lanes *= 2;
+  // A thread has two rows where a unit's rows need that; else one, and more registers for rows on their way
+  const int step = kWriteThreads / p.lanes;
+  const bool two = p.unit > step;
+  const int window = two ? kWriteRows : step < kWriteRows ? step : kWriteRows;
+  // Rows of a block: as few as leave every SM a block (a decode step: each unit's latency counts), at most the window; then heads of a block:
+  // as many as leave every SM four blocks
+  const long long sms = sm_count(dev);
+  p.chunk = 1; p.heads = 1;
+  auto blocks = [&]() { return ((long long)rows + p.chunk - 1) / p.chunk * ((Hkv + p.heads - 1) / p.heads) * 2; };
+  while (p.chunk < window && blocks() > sms) p.chunk *= 2;
+  while (p.heads < Hkv && blocks() > 8 * sms) p.heads *= 2;
+  const dim3 grid((unsigned)((rows + p.chunk - 1) / p.chunk), (unsigned)((Hkv + p.heads - 1) / p.heads), 2);
+  switch (pairs_kind(rotary->rotary, rotary->interleaved)) {
+    case kHalves: return scope.finish(launch_write8<kHalves>(p, two, grid, stream));
+    case kHalvesOdd: return scope.finish(launch_write8<kHalvesOdd>(p, two, grid, stream));
+    default: return scope.finish(launch_write8<kNeighbours>(p, two, grid, stream));
+  }
+}

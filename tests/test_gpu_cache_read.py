@@ -169,30 +169,114 @@ def test_reads_of_many_sequences(mala):
 
 # ---- prompts over an e4m3 cache
 
-@pytest.mark.parametrize("lens,new", [([200, 40, 129], [70, 40, 1]), ([3000], [200]), ([128], [128]), ([50, 0, 300, 10], [0, 0, 300, 10]), ([1], [1])])
-@pytest.mark.parametrize("ps,Hq,Hkv,d", [(64, 4, 2, 64), (128, 8, 2, 128), (16, 2, 2, 96), (256, 6, 1, 128)])
-@pytest.mark.parametrize("tau", [0.0, 0.05])
-def test_prompts(mala, lens, new, ps, Hq, Hkv, d, tau):
-    """Bit for bit the packed forward on the cache's values; dense, against attention in 64 bits within the kernels' roundings."""
+PROMPTS = [([200, 40, 129], [70, 40, 1]), ([3000], [200]), ([128], [128]), ([50, 0, 300, 10], [0, 0, 300, 10]), ([1], [1]), ([900] * 40, [260] * 40)]
+
+
+def _keys(kp, vp, ks, vs, table, lens, ps):
+    """Keys and values of each request in 64 bits."""
+    out = []
+    for b, n in enumerate(lens):
+        x = torch.arange(n, device="cuda")
+        page, at = table[b][x // ps].long(), x % ps
+        out.append([t.view(torch.uint8)[page, at].view(torch.float8_e4m3fn).double() * s[page, :, at // 128].double()[..., None] for t, s in ((kp, ks), (vp, vs))])
+    return out
+
+
+@pytest.mark.parametrize("lens,new", PROMPTS)
+@pytest.mark.parametrize("ps,Hq,Hkv,d", [(64, 4, 2, 64), (128, 8, 2, 128), (16, 2, 2, 96), (256, 6, 1, 128), (32, 4, 4, 16)])
+def test_prompts(mala, lens, new, ps, Hq, Hkv, d):
+    """Attention over scale * code in 64 bits: o within the kernels' roundings of P and o to bf16, lse within those of fp32 -- keys and values are not
+    rounded on their way."""
     (kp, vp), (ks, vs), table = _cache(11, True, lens, ps, Hkv, d)
     cu = [sum(new[:b]) for b in range(len(new) + 1)]
     q = _randn(4, 1, cu[-1], Hq, d)
     scale, total = 1 / math.sqrt(d), sum(lens)
-    o, lse, st = mala.fwd_paged_fp8(q, kp, vp, ks, vs, _i32(cu), table, _i32(lens), max(new), total + 9, scale, tau, stats=True)
-    k, v, cu_k = mala.cache_read_fp8(kp, vp, ks, vs, table, _i32(lens), total + 200)
-    o2, lse2, st2 = mala.fwd_varlen_prefix(q, k, v, _i32(cu), cu_k, max(new), min(table.shape[1] * ps, total + 9), scale, tau, stats=True)
-    assert torch.equal(o, o2) and torch.equal(lse, lse2) and torch.equal(st.totals, st2.totals) and torch.equal(st.bitmask, st2.bitmask)
-    assert mala.device_status() == 0
-    if tau:
-        return
-    kf, vf = k[0].double(), v[0].double()
-    at = 0
-    for b, (n, m) in enumerate(zip(lens, new)):
-        for h in range(Hq if m else 0):
-            w, z, a = R.attention(q[0, cu[b]:cu[b + 1], h].double(), kf[at:at + n, h // (Hq // Hkv)], vf[at:at + n, h // (Hq // Hkv)], scale)
+    o, lse, st = mala.fwd_paged_fp8(q, kp, vp, ks, vs, _i32(cu), table, _i32(lens), max(new), total + 9, scale, 0.0, stats=True)
+    assert mala.device_status() == 0 and int(st.totals[0]) == int(st.totals[1])
+    for b, (k, v) in enumerate(_keys(kp, vp, ks, vs, table, lens, ps)[:6]):
+        for h in range(Hq if new[b] else 0):
+            qd = q[0, cu[b]:cu[b + 1], h].double()
+            w, z, a = R.attention(qd, k[:, h // (Hq // Hkv)], v[:, h // (Hq // Hkv)], scale)
             parity.check_output(o[0, cu[b]:cu[b + 1], h].double().cpu().numpy(), w.cpu().numpy(), a_ref=a.cpu().numpy())
-            assert (lse[h, cu[b]:cu[b + 1]].double() - z).abs().max() <= parity.LSE_ABS
-        at += n
+            # scores: fp32 sums of d products, off by at most (d + 4) 2^-24 of the sum of their magnitudes; exp2 and the sums by a few 2^-23 more
+            most = (qd.abs() @ k[:, h // (Hq // Hkv)].abs().T).amax(1) * scale
+            err = (lse[h, cu[b]:cu[b + 1]].double() - z).abs()
+            assert (err <= (d + 4) * 2.0 ** -24 * most + 2.0 ** -20 * (1 + z.abs())).all(), err.max().item()
+
+
+def _dequantised(kp, vp, ks, vs, pow2):
+    """bf16 pages with the same values (exact where the scales are powers of two)."""
+    assert pow2
+    out = []
+    for t, s in ((kp, ks), (vp, vs)):
+        P, ps, Hkv, d = t.shape
+        x = t.float().view(P, s.shape[2], -1, Hkv, d) * s.permute(0, 2, 1)[:, :, None, :, None]
+        out.append(x.view(P, ps, Hkv, d).to(torch.bfloat16))
+    return out
+
+
+@pytest.mark.parametrize("lens,new", PROMPTS)
+@pytest.mark.parametrize("ps,Hq,Hkv,d", [(64, 4, 2, 64), (128, 8, 2, 128), (16, 2, 2, 96)])
+@pytest.mark.parametrize("tau", [0.0, 1e-3, 0.05])
+def test_prompts_against_bf16_pages(mala, lens, new, ps, Hq, Hkv, d, tau):
+    """Scales that are powers of two: the same values lie in bf16 pages, and mala_fwd_paged decides alike, tile by tile."""
+    (kp, vp), (ks, vs), table = _cache(11, True, lens, ps, Hkv, d)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    ks, vs = (2.0 ** -torch.randint(5, 10, t.shape, generator=g, device="cuda").float() for t in (ks, vs))
+    cu = [sum(new[:b]) for b in range(len(new) + 1)]
+    q = _randn(4, 1, cu[-1], Hq, d) * 2
+    most = max(new)
+    o, lse, st = mala.fwd_paged_fp8(q, kp, vp, ks, vs, _i32(cu), table, _i32(lens), most, sum(lens), 0.1, tau, stats=True)
+    k16, v16 = _dequantised(kp, vp, ks, vs, True)
+    o2, lse2, st2 = mala.fwd_paged(q, k16, v16, _i32(cu), table, _i32(lens), most, 0.1, tau, stats=True)
+    T = min(st.bitmask.shape[-1], st2.bitmask.shape[-1])
+    assert torch.equal(st.bitmask[..., :T], st2.bitmask[..., :T]) and torch.equal(st.totals, st2.totals)
+    rows = torch.cat([torch.arange(cu[b], cu[b + 1]) for b in range(len(new))]).cuda()
+    a, b, c, e = o[0, rows].double(), o2[0, rows].double(), lse[:, rows], lse2[:, rows]
+    assert ((a - b).norm() <= 2.0 ** -8 * 2 * b.norm()) and ((c - e).abs() <= 2.0 ** -20 * (1 + e.abs())).all()
+
+
+@pytest.mark.parametrize("ps,Hq,Hkv,d,new", [(64, 4, 2, 64, 300), (128, 8, 2, 128, 1500), (16, 2, 2, 96, 40)])
+def test_prompts_that_skip(mala, ps, Hq, Hkv, d, new):
+    """Queries that look for their own key: tiles are skipped, the same ones as over bf16 pages of the same values."""
+    lens, scale, tau = [2500], 1.0, 1e-3
+    (kp, vp), (ks, vs), table = _cache(17, True, lens, ps, Hkv, d)
+    ks, vs = torch.full_like(ks, 2.0 ** -7), torch.full_like(vs, 2.0 ** -8)
+    k, _, _ = mala.cache_read_fp8(kp, vp, ks, vs, table, _i32(lens), 2500)
+    q = k[:, 2500 - new:].repeat_interleave(Hq // Hkv, 2).contiguous()
+    args = (_i32([0, new]), table, _i32(lens), new)
+    o, lse, st = mala.fwd_paged_fp8(q, kp, vp, ks, vs, *args, 2500, scale, tau, stats=True)
+    o2, lse2, st2 = mala.fwd_paged(q, *_dequantised(kp, vp, ks, vs, True), *args, scale, tau, stats=True)
+    T = min(st.bitmask.shape[-1], st2.bitmask.shape[-1])
+    assert torch.equal(st.bitmask[..., :T], st2.bitmask[..., :T]) and torch.equal(st.totals, st2.totals)
+    assert int(st.totals[0]) < int(st.totals[1])      # (tiles are skipped: what the comparison is about)
+    assert ((o.double() - o2.double()).norm() <= 2.0 ** -8 * 2 * o2.double().norm()) and ((lse - lse2).abs() <= 2.0 ** -20 * (1 + lse2.abs())).all()
+
+
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("value", [0.0, -0.01, 1e-30, 1e25, 2.0 ** -61, 2.0 ** -60])
+def test_prompts_with_far_scales(mala, which, value):
+    """Scales that no cache write gives (0, below 0, near the ends of fp32) in some units: bf16(scale * code) there."""
+    lens, new, ps, Hq, Hkv, d = [700], [130], 64, 4, 2, 64
+    (kp, vp), (ks, vs), table = _cache(13, True, lens, ps, Hkv, d)
+    used = table[0, [2, 5]].long()
+    (ks if which == "k" else vs)[used, 1] = value
+    if which == "k" and value > 1:
+        for x in used.tolist():            # (finite scores: one key of small codes)
+            kp[x] = torch.full_like(kp[x].float(), 2.0 ** -9).to(torch.float8_e4m3fn)
+    q = _randn(4, 1, 130, Hq, d)
+    o, lse, _ = mala.fwd_paged_fp8(q, kp, vp, ks, vs, _i32([0, 130]), table, _i32(lens), 130, 700, 1 / 8, 0.0)
+    k, v, cu = mala.cache_read_fp8(kp, vp, ks, vs, table, _i32(lens), 900)
+    o2, lse2, _ = mala.fwd_varlen_prefix(q, k, v, _i32([0, 130]), cu, 130, 700, 1 / 8, 0.0)
+    # as finite as the forward over these values.  (Scores of 1e23 are beyond its exponent: fma(s, c, -m) with m = fl(s c) leaves up to |m| 2^-24 = 6e15 instead of
+    # 0 for the row's largest score, whatever the cache's type; every other case here is finite in both.)
+    assert torch.isfinite(o[torch.isfinite(o2)]).all()
+    if value <= 1 or which == "v":
+        assert torch.isfinite(o2).all()
+    # against keys rounded to bf16 (2^-8 of a key): scores of up to a few units times 2^-8
+    if value <= 1 or which == "v":
+        assert (lse - lse2).abs().max() <= 0.05 and ((o.double() - o2.double()).norm() <= 0.05 * o2.double().norm())
+    assert mala.device_status() == 0
 
 
 def test_prompts_with_a_workspace_and_refusals(mala):
