@@ -3,6 +3,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "../../include/mala.h"
 #include "mala_decode_sched.cuh"
@@ -431,8 +432,9 @@ struct ReadParams {
   const int* block_table; const int* seqlens; int* cu;
   float* scales; int tiles;                // codes and scales apart (see CacheScales)
   int B, max_pages, page_size, num_pages, per_page, rows, Hkv;
-  int cols, per;                           // 16-byte pieces of a head's row in the pages, and of a whole row
-  FastDiv by_per, by_cols, by_page;
+  int cols, per;                           // pieces of eight columns of a head's row, and of a whole row
+  int at_once, chunks;                     // rows that a block has beside one another; parts of 256 pieces of a row (of more)
+  FastDiv by_cols, by_page;
 };
 
 enum { kReadRows = 0, kReadFp8 = 1, kReadCodes = 2 };
@@ -441,12 +443,15 @@ enum { kReadRows = 0, kReadFp8 = 1, kReadCodes = 2 };
 // codes are read as values.)
 __device__ __forceinline__ bool scale_apart(float s) { return s >= 0x1p-60f && s <= 0x1p60f; }
 
-// A block adds up the lengths for itself (as the tables do) and takes a thousand pieces of the packed rows at a time: which
-// sequence the first and the last of them belong to is searched once.  A thread has four 16-byte pieces of K and of V in flight.
+// A block adds up the lengths for itself (as the tables do) and takes a few rows at a time: which sequence the first and the last of them
+// belong to is searched once.  A thread has eight columns of a head, of K and of V, in four rows (e4m3: eight) in flight, and the same
+// columns throughout; what it reads (16 bytes, e4m3 8) and writes (16) lies beside its neighbours'.
 template <int kKind>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 3)
 cache_read_kernel(const ReadParams p) {
   constexpr bool kFp8 = kKind != kReadRows;
+  constexpr int U = kFp8 ? 8 : 4;
+  using Piece = std::conditional_t<kFp8, uint2, uint4>;
   extern __shared__ int cu_s[];            // [B + 1]
   __shared__ uint64_t warp_sums[32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -476,62 +481,58 @@ cache_read_kernel(const ReadParams p) {
   __syncthreads();
   if (blockIdx.x == 0)
     for (int b = tid; b <= p.B; b += 256) p.cu[b] = cu_s[b];
-  const int have = cu_s[p.B], reach = min(p.rows, have + 128);
-  const int64_t all = (int64_t)reach * p.per;
-  for (int64_t base = (int64_t)blockIdx.x * 1024; base < all; base += (int64_t)gridDim.x * 1024) {
-    auto row_of = [&](int64_t x) { return all <= 0xffffffffll ? (int)p.by_per.div((uint32_t)x) : (int)(x / p.per); };
-    const int first = min(row_of(base), max(have - 1, 0)), last = min(row_of(min(base + 1023, all - 1)), max(have - 1, 0));
-    const int lo = find_last(cu_s, 0, p.B, first), hi = find_last(cu_s, lo, p.B, last) + 1;
-    uint4 wk[4], wv[4];
-    float sk[4], sv[4];
-    int64_t to_k[4], to_v[4];
+  const int have = cu_s[p.B], reach = min(p.rows, have + 128), rows_of_block = p.at_once * U;
+  const int ahead = p.per <= 256 ? tid / p.per : 0, c0 = tid - ahead * p.per;
+  const int64_t all = (int64_t)((reach + rows_of_block - 1) / rows_of_block) * p.chunks;
+  for (int64_t w = blockIdx.x; w < all; w += gridDim.x) {
+    const int64_t group = p.chunks == 1 ? w : w / p.chunks;
+    const int first = (int)(group * rows_of_block), c = c0 + (int)(w - group * p.chunks) * 256;
+    if (ahead >= p.at_once || c >= p.per) continue;
+    const int most = max(have - 1, 0), lo = find_last(cu_s, 0, p.B, min(first, most)), hi = find_last(cu_s, lo, p.B, min(first + rows_of_block - 1, most)) + 1;
+    const int h = (int)p.by_cols.div((uint32_t)c), col = (c - h * p.cols) * 8;
+    const uint8_t* const kp = p.kp + h * p.kp_sh + col * (kFp8 ? 1 : 2);
+    const uint8_t* const vp = p.vp + h * p.vp_sh + col * (kFp8 ? 1 : 2);
+    Piece wk[U], wv[U];
+    float sk[U], sv[U];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t x = base + i * 256 + tid;
-      to_k[i] = -1;
-      wk[i] = wv[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < U; ++i) {
+      const int row = first + i * p.at_once + ahead;
+      wk[i] = wv[i] = Piece{};
       sk[i] = sv[i] = 0.f;
-      if (x < all) {
-        const int row = row_of(x), c = (int)(x - (int64_t)row * p.per), h = (int)p.by_cols.div((uint32_t)c), col = (c - h * p.cols) * 16;
-        to_k[i] = row * p.k_sn + h * p.k_sh + col * (kFp8 ? 2 : 1);
-        to_v[i] = row * p.v_sn + h * p.v_sh + col * (kFp8 ? 2 : 1);
-        if (row < have) {
-          const int b = find_last(cu_s, lo, hi, row), pos = row - cu_s[b], entry = (int)p.by_page.div((uint32_t)pos);
-          const int page = __ldg(p.block_table + (int64_t)b * p.max_pages + entry), at = pos - entry * p.page_size;
-          if (page >= 0 && page < p.num_pages) {
-            wk[i] = __ldg(reinterpret_cast<const uint4*>(p.kp + page * p.kp_sb + at * p.kp_sn + h * p.kp_sh + col));
-            wv[i] = __ldg(reinterpret_cast<const uint4*>(p.vp + page * p.vp_sb + at * p.vp_sn + h * p.vp_sh + col));
-            if (kFp8) {
-              const int64_t unit = ((int64_t)page * p.Hkv + h) * p.per_page + at / 128;
-              sk[i] = __ldg(p.kscale + unit);
-              sv[i] = __ldg(p.vscale + unit);
-              if (kKind == kReadCodes) {
-                if (scale_apart(sk[i])) sk[i] = 1.f;
-                if (scale_apart(sv[i])) sv[i] = 1.f;
-              }
+      if (row < have) {
+        const int b = find_last(cu_s, lo, hi, row), pos = row - cu_s[b], entry = (int)p.by_page.div((uint32_t)pos);
+        const int page = __ldg(p.block_table + (int64_t)b * p.max_pages + entry), at = pos - entry * p.page_size;
+        if (page >= 0 && page < p.num_pages) {
+          wk[i] = __ldg(reinterpret_cast<const Piece*>(kp + page * p.kp_sb + at * p.kp_sn));
+          wv[i] = __ldg(reinterpret_cast<const Piece*>(vp + page * p.vp_sb + at * p.vp_sn));
+          if constexpr (kFp8) {
+            const int64_t unit = ((int64_t)page * p.Hkv + h) * p.per_page + at / 128;
+            sk[i] = __ldg(p.kscale + unit);
+            sv[i] = __ldg(p.vscale + unit);
+            if (kKind == kReadCodes) {
+              if (scale_apart(sk[i])) sk[i] = 1.f;
+              if (scale_apart(sv[i])) sv[i] = 1.f;
             }
           }
         }
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (to_k[i] < 0) continue;
+    for (int i = 0; i < U; ++i) {
+      const int row = first + i * p.at_once + ahead;
+      if (row >= reach) continue;
+      uint4* const to_k = reinterpret_cast<uint4*>(p.k + row * p.k_sn + h * p.k_sh + col * 2);
+      uint4* const to_v = reinterpret_cast<uint4*>(p.v + row * p.v_sn + h * p.v_sh + col * 2);
       if constexpr (kFp8) {
         auto pair = [](uint32_t codes, float s) -> uint32_t {
           const float2 a = from_e4m3x2((uint16_t)codes);
-          return pack_bf16x2(a.x * s, a.y * s);
+          return f2_bf16(f2_mul(f2(a.x, a.y), f2(s, s)));
         };
-        auto eight = [&](uint32_t a, uint32_t b, float s) { return make_uint4(pair(a, s), pair(a >> 16, s), pair(b, s), pair(b >> 16, s)); };
-        uint4* const to = reinterpret_cast<uint4*>(p.k + to_k[i]);
-        uint4* const to2 = reinterpret_cast<uint4*>(p.v + to_v[i]);
-        to[0] = eight(wk[i].x, wk[i].y, sk[i]);
-        to[1] = eight(wk[i].z, wk[i].w, sk[i]);
-        to2[0] = eight(wv[i].x, wv[i].y, sv[i]);
-        to2[1] = eight(wv[i].z, wv[i].w, sv[i]);
+        *to_k = make_uint4(pair(wk[i].x, sk[i]), pair(wk[i].x >> 16, sk[i]), pair(wk[i].y, sk[i]), pair(wk[i].y >> 16, sk[i]));
+        *to_v = make_uint4(pair(wv[i].x, sv[i]), pair(wv[i].x >> 16, sv[i]), pair(wv[i].y, sv[i]), pair(wv[i].y >> 16, sv[i]));
       } else {
-        *reinterpret_cast<uint4*>(p.k + to_k[i]) = wk[i];
-        *reinterpret_cast<uint4*>(p.v + to_v[i]) = wv[i];
+        *to_k = wk[i];
+        *to_v = wv[i];
       }
     }
   }
@@ -606,12 +607,14 @@ static int cache_read(mala_tin kp, mala_tin vp, const float* kscale, const float
   p.scales = scales ? scales->out : nullptr; p.tiles = scales ? scales->tiles : 0;
   p.B = B; p.max_pages = max_pages; p.page_size = page_size; p.num_pages = num_pages; p.per_page = page_size < 128 ? 1 : page_size / 128;
   p.rows = rows; p.Hkv = Hkv;
-  p.cols = d * item / 16; p.per = p.cols * Hkv;
-  p.by_per.set((uint32_t)p.per); p.by_cols.set((uint32_t)p.cols); p.by_page.set((uint32_t)page_size);
+  p.cols = d / 8; p.per = p.cols * Hkv;
+  p.at_once = p.per <= 256 ? 256 / p.per : 1; p.chunks = (p.per + 255) / 256;
+  p.by_cols.set((uint32_t)p.cols); p.by_page.set((uint32_t)page_size);
   int dev = 0, *status = nullptr;
   MALA_TRY(current_device_checked(&dev));
   MALA_TRY(device_setup(dev, &status));
-  const long long want = ((long long)rows * p.per + 1023) / 1024, most = 8ll * sm_count(dev);
+  const int rows_of_block = p.at_once * (fp8 ? 8 : 4);
+  const long long want = ((long long)rows + rows_of_block - 1) / rows_of_block * p.chunks, most = 6ll * sm_count(dev);
   const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
   const size_t smem = ((size_t)B + 1) * sizeof(int);
   if (scales) cache_read_kernel<kReadCodes><<<grid, 256, smem, stream>>>(p);

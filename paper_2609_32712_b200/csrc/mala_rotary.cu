@@ -36,64 +36,73 @@ struct RotaryParams {
   int q_blocks;
 };
 
-// Position of row t of tensor `which`; false: no sequence has it
-__device__ __forceinline__ bool position_of(const RotaryParams& p, const RotaryTensor& a, int which, int t, int b, int n, int& pos) {
-  if (p.cu_q) {
-    const int* own = which == 0 ? p.cu_q : p.cu_k;
-    int lo = 0, hi = p.B;
-    if (t < __ldg(own) || t >= __ldg(own + p.B)) return false;
-    while (hi - lo > 1) {                  // the last sequence that begins at or before t
-      const int mid = (lo + hi) >> 1;
-      if (__ldg(own + mid) <= t) lo = mid;
-      else hi = mid;
+// Positions of the rows of one tensor after another
+struct Positions {
+  int which = -1, from = 0, to = 0, shift = 0;   // packed: the rows of the sequence found last, and what a row's position has more than its number
+  // position of row t (n of batch entry b) of tensor w; false: no sequence has it
+  __device__ __forceinline__ bool of(const RotaryParams& p, const RotaryTensor& a, int w, int t, int b, int n, int& pos) {
+    if (p.cu_q) {
+      if (w != which || t < from || t >= to) {
+        const int* own = w == 0 ? p.cu_q : p.cu_k;
+        if (t < __ldg(own) || t >= __ldg(own + p.B)) return false;
+        int lo = 0, hi = p.B;
+        while (hi - lo > 1) {              // the last sequence that begins at or before t
+          const int mid = (lo + hi) >> 1;
+          if (__ldg(own + mid) <= t) lo = mid;
+          else hi = mid;
+        }
+        which = w;
+        from = __ldg(own + lo);
+        to = __ldg(own + lo + 1);
+        shift = -from;
+        if (w == 0) shift += (__ldg(p.cu_k + lo + 1) - __ldg(p.cu_k + lo)) - (to - from);
+      }
+      pos = t + shift;
+      return true;
     }
-    pos = t - __ldg(own + lo);
-    if (which == 0) pos += (__ldg(p.cu_k + lo + 1) - __ldg(p.cu_k + lo)) - (__ldg(p.cu_q + lo + 1) - __ldg(p.cu_q + lo));
+    pos = n + a.first;
+    if (p.positions) pos = __ldg(p.positions + (int64_t)b * p.pos_n + pos);
     return true;
   }
-  pos = n + a.first;
-  if (p.positions) pos = __ldg(p.positions + (int64_t)b * p.pos_n + pos);
-  return true;
+};
+
+__device__ __forceinline__ uint4 piece_at(const uint8_t* row, int piece, bool has) {
+  return has ? *reinterpret_cast<const uint4*>(row + piece * 16) : make_uint4(0u, 0u, 0u, 0u);
+}
+// What the rows of a warp leave in shared memory, columns in order, for partners that begin inside a piece
+__device__ __forceinline__ void stage_row(uint4* buf, int lane, const uint4& a, const uint4& b) {
+  __syncwarp();
+  buf[2 * lane] = a;
+  buf[2 * lane + 1] = b;
+  __syncwarp();
 }
 
-// Rotations.  A row of d columns lies in the registers of L lanes, eight columns each, and a warp works on 32 / L heads of a token
-// at a time, four such loads in flight behind the four that it works on: the angles of a token are worked out once for all heads
-// that a warp takes.
+// Rotations.  A row lies in the registers of L lanes, and a warp works on 32 / L heads of a token at a time, two such loads in flight behind
+// the two that it works on: the angles of a token are worked out once for all heads that a warp takes, and a warp's tokens are
+// neighbours.
 template <int L, int kPairs, bool kNorm, bool kPages>
 __global__ void __launch_bounds__(kRotaryThreads, 2)
 rotary_kernel(const RotaryParams p) {
-  constexpr int P = 32 / L, U = 4;
-  constexpr uint32_t kAll = 0xffffffffu;
+  constexpr int P = 32 / L, U = 2;
   __shared__ uint64_t turns_s[kMaxPairs];
-  __shared__ uint4 rows_s[kPairs == kHalvesOdd ? kRotaryWarps * 32 : 1];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, i = lane % L;
-  const bool mine = 8 * i < p.rule.d;
-  uint4* const buf = rows_s + (kPairs == kHalvesOdd ? warp * 32 : 0);
-  LaneTurns<kPairs> turns;
-  turns.set(p.rule, i, g * L);
+  __shared__ uint4 rows_s[kPairs == kHalvesOdd ? kRotaryWarps * 64 : 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, c = lane % L;
+  uint4* const buf = rows_s + (kPairs == kHalvesOdd ? warp * 64 : 0);
+  LanePieces<kPairs> l;
+  l.set(p.rule, c);
   load_turns(p.rule, turns_s);
   __syncthreads();
   const uint32_t nq = p.t[0].items, nk = p.t[1].items, all = nq + nk + (kPages ? p.t[2].items : 0);   // (at most 3 * 2^30)
-  for (uint32_t item = blockIdx.x * kRotaryWarps + warp; item < all; item += gridDim.x * kRotaryWarps) {
+  const uint32_t share = (all + gridDim.x * kRotaryWarps - 1) / (gridDim.x * kRotaryWarps);
+  const uint64_t first = (uint64_t)(blockIdx.x * kRotaryWarps + warp) * share;
+  Positions positions;
+  for (uint64_t x = first; x < first + share && x < all; ++x) {
+    const uint32_t item = (uint32_t)x;
     const int which = item < nq ? 0 : item < nq + nk ? 1 : 2, x0 = (int)(item - (which == 0 ? 0 : which == 1 ? nq : nq + nk));
     const RotaryTensor& a = p.t[which];
     const int t = (int)a.by_spans.div((uint32_t)x0), h0 = (x0 - t * (int)a.by_spans.d) * a.span, h1 = min(h0 + a.span, a.H);
     const int b = (int)a.by_n.div((uint32_t)t), n = t - b * a.N;
-    const uint8_t* src = a.x + b * a.x_sb + n * a.x_sn + i * 16;
-    const int64_t x_sh = a.x_sh, y_sh = a.y_sh;
-    uint4 w[U];
-    auto load = [&](int hb, uint4 (&to)[U]) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = hb + u * P + g;
-        to[u] = make_uint4(0u, 0u, 0u, 0u);
-        if (mine && h < h1) to[u] = *reinterpret_cast<const uint4*>(src + h * x_sh);
-      }
-    };
-    load(h0, w);
-    int pos = 0;
-    const bool turn = which < 2 && position_of(p, a, which, t, b, n, pos);
-    uint8_t* dst = a.y + i * 16;
+    uint8_t* dst = a.y;
     if (kPages && which > 0) {
       const int64_t slot = __ldg(p.slots + t);
       if (slot < 0 || slot >= p.limit) continue;
@@ -102,53 +111,63 @@ rotary_kernel(const RotaryParams p) {
     } else {
       dst += b * a.y_sb + n * a.y_sn;
     }
-    uint64_t C2[4], S2[4];
-    if (turn) {
-      float C[8], S[8];
-      turns.at(p.rule, turns_s, pos, kAll, C, S);
-      if constexpr (kNorm) {
+    const uint8_t* src = a.x + b * a.x_sb + n * a.x_sn;
+    const int64_t x_sh = a.x_sh, y_sh = a.y_sh;
+    uint4 wa[U], wb[U];
+    auto load = [&](int hb, uint4 (&to_a)[U], uint4 (&to_b)[U]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int c = 8 * turns.i + e;
-          C[e] *= weight_at(a.weight, p.weights_fp32, c);
-          S[e] *= weight_at(a.weight, p.weights_fp32, partner_of<kPairs>(c, p.rule.rotary));
-        }
+      for (int u = 0; u < U; ++u) {
+        const int h = hb + u * P + g;
+        to_a[u] = piece_at(src + h * x_sh, l.pa, l.has_a && h < h1);
+        to_b[u] = piece_at(src + h * x_sh, l.pb, l.has_b && h < h1);
       }
-      pack_turns(C, S, C2, S2);
+    };
+    load(h0, wa, wb);
+    int pos = 0;
+    const bool turn = which < 2 && positions.of(p, a, which, t, b, n, pos);
+    LaneFactors<kPairs> f;
+    if (turn) {
+      float C[kAngles<kPairs>], S[kAngles<kPairs>];
+      angles_at<L, kPairs>(p.rule, turns_s, c, g, pos, C, S);
+      f.template set<kNorm>(p.rule, c, l, C, S, a.weight, p.weights_fp32);
     }
     for (int hb = h0; hb < h1; hb += P * U) {
-      uint4 next[U];
-      if (hb + P * U < h1) load(hb + P * U, next);
+      uint4 na[U], nb[U];
+      if (hb + P * U < h1) load(hb + P * U, na, nb);
       if (turn) {                          // (not: values, and rows that no sequence has)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          uint64_t x[4], y[4];
-          if constexpr (kPairs == kHalvesOdd) {
-            __syncwarp();
-            buf[lane] = w[u];
-            __syncwarp();
-          }
-          pairs_of(w[u], x);
-          turns.partners(w[u], reinterpret_cast<const __nv_bfloat16*>(buf + g * L), p.rule.rotary, kAll, y);
+          uint64_t xa[4], xb[4];
+          if constexpr (kPairs == kHalvesOdd) stage_row(buf, lane, wa[u], wb[u]);
+          pairs_of(wa[u], xa);
+          pairs_of(wb[u], xb);
+          float sum = 0.f;
           if constexpr (kNorm) {
-            float sum = f2_sum(f2_fma(x[0], x[0], f2_fma(x[1], x[1], f2_fma(x[2], x[2], f2_mul(x[3], x[3])))));
+            sum = squares(xa, xb);
 #pragma unroll
-            for (int m = L / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(kAll, sum, m);
-            const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
-            turn_pairs(x, y, C2, S2);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = f2_mul(x[j], f2(r, r));
-          } else {
-            turn_pairs(x, y, C2, S2);
+            for (int m = L / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
           }
-          w[u] = rows_of(x);
+          rotate_pieces<kPairs, kNorm>(p.rule, c, l, f, reinterpret_cast<const __nv_bfloat16*>(buf + 2 * g * L), xa, xb);
+          if constexpr (kNorm) {
+            const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              xa[j] = f2_mul(xa[j], f2(r, r));
+              xb[j] = f2_mul(xb[j], f2(r, r));
+            }
+          }
+          wa[u] = rows_of(xa);
+          wb[u] = rows_of(xb);
         }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int h = hb + u * P + g;
-        if (mine && h < h1) *reinterpret_cast<uint4*>(dst + h * y_sh) = w[u];
-        w[u] = next[u];
+        uint8_t* const to = dst + h * y_sh;
+        if (l.has_a && h < h1) *reinterpret_cast<uint4*>(to + l.pa * 16) = wa[u];
+        if (l.has_b && h < h1) *reinterpret_cast<uint4*>(to + l.pb * 16) = wb[u];
+        wa[u] = na[u];
+        wb[u] = nb[u];
       }
     }
   }
@@ -160,112 +179,114 @@ rotary_kernel(const RotaryParams p) {
 template <int L, int kPairs>
 __global__ void __launch_bounds__(kRotaryThreads, 2)
 rotary_norm_bwd_kernel(const RotaryParams p) {
-  constexpr int P = 32 / L, U = 2;
+  constexpr int P = 32 / L;
   constexpr uint32_t kAll = 0xffffffffu;
   __shared__ uint64_t turns_s[kMaxPairs];
-  __shared__ uint4 rows_s[kPairs == kHalvesOdd ? kRotaryWarps * 32 : 1];
+  __shared__ uint4 rows_s[kPairs == kHalvesOdd ? kRotaryWarps * 64 : 1];
   __shared__ float sums_s[kRotaryWarps][256];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, i = lane % L;
-  const bool mine = 8 * i < p.rule.d;
-  uint4* const buf = rows_s + (kPairs == kHalvesOdd ? warp * 32 : 0);
+  __shared__ __align__(16) float weight_s[256];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, c = lane % L;
+  uint4* const buf = rows_s + (kPairs == kHalvesOdd ? warp * 64 : 0);
   const int which = (int)blockIdx.x < p.q_blocks ? 0 : 1, block = blockIdx.x - (which ? p.q_blocks : 0);
   const int blocks = which ? gridDim.x - p.q_blocks : p.q_blocks;
   const RotaryTensor& a = p.t[which];
-  LaneTurns<kPairs> turns;
-  turns.set(p.rule, i, g * L);
+  LanePieces<kPairs> l;
+  l.set(p.rule, c);
   load_turns(p.rule, turns_s);
+  for (int x = threadIdx.x; x < p.rule.d; x += kRotaryThreads) weight_s[x] = weight_at(a.weight, p.weights_fp32, x);
   __syncthreads();
-  uint64_t W[4], dw[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    W[j] = f2(weight_at(a.weight, p.weights_fp32, 8 * turns.i + 2 * j), weight_at(a.weight, p.weights_fp32, 8 * turns.i + 2 * j + 1));
-    dw[j] = 0;
-  }
-  for (int item = block * kRotaryWarps + warp; item < a.items; item += blocks * kRotaryWarps) {
+  uint64_t dw[8] = {0, 0, 0, 0, 0, 0, 0, 0};   // of the columns of a, and of b
+  const float4* const weights_a = reinterpret_cast<const float4*>(weight_s) + (l.has_a ? 2 * l.pa : 0);
+  const float4* const weights_b = reinterpret_cast<const float4*>(weight_s) + (l.has_b ? 2 * l.pb : 0);
+  const int share = (a.items + blocks * kRotaryWarps - 1) / (blocks * kRotaryWarps);
+  const int64_t first = (int64_t)(block * kRotaryWarps + warp) * share;
+  Positions positions;
+  for (int64_t x = first; x < first + share && x < a.items; ++x) {
+    const int item = (int)x;
     const int t = (int)a.by_spans.div((uint32_t)item), h0 = (item - t * (int)a.by_spans.d) * a.span, h1 = min(h0 + a.span, a.H);
     const int b = (int)a.by_n.div((uint32_t)t), n = t - b * a.N;
-    const uint8_t* gp = a.g + b * a.g_sb + n * a.g_sn + i * 16;
-    const uint8_t* xp = a.x + b * a.x_sb + n * a.x_sn + i * 16;
-    uint8_t* dst = a.y + b * a.y_sb + n * a.y_sn + i * 16;
-    uint4 wg[U], wx[U];
-    auto load = [&](int hb, uint4 (&tg)[U], uint4 (&tx)[U]) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = hb + u * P + g;
-        tg[u] = tx[u] = make_uint4(0u, 0u, 0u, 0u);
-        if (mine && h < h1) {
-          tg[u] = *reinterpret_cast<const uint4*>(gp + h * a.g_sh);
-          tx[u] = *reinterpret_cast<const uint4*>(xp + h * a.x_sh);
-        }
-      }
+    const uint8_t* gp = a.g + b * a.g_sb + n * a.g_sn;
+    const uint8_t* xp = a.x + b * a.x_sb + n * a.x_sn;
+    uint8_t* dst = a.y + b * a.y_sb + n * a.y_sn;
+    const int64_t g_sh = a.g_sh, x_sh = a.x_sh, y_sh = a.y_sh;
+    uint4 ga, gb, za, zb;
+    auto load = [&](int hb, uint4& to_ga, uint4& to_gb, uint4& to_za, uint4& to_zb) {
+      const int h = hb + g;
+      to_ga = piece_at(gp + h * g_sh, l.pa, l.has_a && h < h1);
+      to_gb = piece_at(gp + h * g_sh, l.pb, l.has_b && h < h1);
+      to_za = piece_at(xp + h * x_sh, l.pa, l.has_a && h < h1);
+      to_zb = piece_at(xp + h * x_sh, l.pb, l.has_b && h < h1);
     };
-    load(h0, wg, wx);
+    load(h0, ga, gb, za, zb);
     int pos = 0;
-    const bool turn = position_of(p, a, which, t, b, n, pos);
-    uint64_t C2[4], S2[4];
+    const bool turn = positions.of(p, a, which, t, b, n, pos);
+    LaneFactors<kPairs> f;
     if (turn) {
-      float C[8], S[8];
-      turns.at(p.rule, turns_s, pos, kAll, C, S);
-      pack_turns(C, S, C2, S2);
+      float C[kAngles<kPairs>], S[kAngles<kPairs>];
+      angles_at<L, kPairs>(p.rule, turns_s, c, g, pos, C, S);
+      f.template set<false>(p.rule, c, l, C, S, nullptr, 0);
     }
-    for (int hb = h0; hb < h1; hb += P * U) {
-      uint4 ng[U], nx[U];
-      if (hb + P * U < h1) load(hb + P * U, ng, nx);
+    for (int hb = h0; hb < h1; hb += P) {
+      uint4 nga, ngb, nza, nzb;
+      if (hb + P < h1) load(hb + P, nga, ngb, nza, nzb);
       if (turn) {
+        uint64_t xa[4], xb[4], ya[4], yb[4];
+        if constexpr (kPairs == kHalvesOdd) stage_row(buf, lane, ga, gb);
+        pairs_of(ga, xa);
+        pairs_of(gb, xb);
+        rotate_pieces<kPairs, false>(p.rule, c, l, f, reinterpret_cast<const __nv_bfloat16*>(buf + 2 * g * L), xa, xb);
+        pairs_of(za, ya);
+        pairs_of(zb, yb);
+        float sum = squares(ya, yb);
+        uint64_t wga[4], wgb[4], da = 0, db = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          uint64_t x[4], y[4], z[4];
-          if constexpr (kPairs == kHalvesOdd) {
-            __syncwarp();
-            buf[lane] = wg[u];
-            __syncwarp();
-          }
-          pairs_of(wg[u], x);
-          turns.partners(wg[u], reinterpret_cast<const __nv_bfloat16*>(buf + g * L), p.rule.rotary, kAll, y);
-          turn_pairs(x, y, C2, S2);
-          pairs_of(wx[u], z);
-          uint64_t gw[4], s2 = 0, d2 = 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            gw[j] = f2_mul(x[j], W[j]);
-            s2 = f2_fma(z[j], z[j], s2);
-            d2 = f2_fma(gw[j], z[j], d2);
-          }
-          float sum = f2_sum(s2), dot = f2_sum(d2);
-#pragma unroll
-          for (int m = L / 2; m > 0; m >>= 1) {
-            sum += __shfl_xor_sync(kAll, sum, m);
-            dot += __shfl_xor_sync(kAll, dot, m);
-          }
-          const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps)), back = -(r * r * dot * p.inv_d);
-          const uint64_t r2 = f2(r, r), back2 = f2(back, back);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            dw[j] = f2_fma(x[j], f2_mul(z[j], r2), dw[j]);
-            x[j] = f2_mul(r2, f2_fma(z[j], back2, gw[j]));
-          }
-          wg[u] = rows_of(x);
+        for (int j = 0; j < 4; j += 2) {
+          const float4 va = weights_a[j / 2], vb = weights_b[j / 2];
+          wga[j] = f2_mul(xa[j], f2(va.x, va.y));
+          wga[j + 1] = f2_mul(xa[j + 1], f2(va.z, va.w));
+          wgb[j] = f2_mul(xb[j], f2(vb.x, vb.y));
+          wgb[j + 1] = f2_mul(xb[j + 1], f2(vb.z, vb.w));
         }
-      }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = hb + u * P + g;
-        if (mine && h < h1) *reinterpret_cast<uint4*>(dst + h * a.y_sh) = wg[u];
-        wg[u] = ng[u];
-        wx[u] = nx[u];
+        for (int j = 0; j < 4; ++j) {
+          da = f2_fma(wga[j], ya[j], da);
+          db = f2_fma(wgb[j], yb[j], db);
+        }
+        float dot = f2_sum(da) + f2_sum(db);
+#pragma unroll
+        for (int m = L / 2; m > 0; m >>= 1) {
+          sum += __shfl_xor_sync(kAll, sum, m);
+          dot += __shfl_xor_sync(kAll, dot, m);
+        }
+        const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps)), back = -(r * r * dot * p.inv_d);
+        const uint64_t r2 = f2(r, r), back2 = f2(back, back);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          dw[j] = f2_fma(xa[j], f2_mul(ya[j], r2), dw[j]);
+          dw[4 + j] = f2_fma(xb[j], f2_mul(yb[j], r2), dw[4 + j]);
+          xa[j] = f2_mul(r2, f2_fma(ya[j], back2, wga[j]));
+          xb[j] = f2_mul(r2, f2_fma(yb[j], back2, wgb[j]));
+        }
+        ga = rows_of(xa);
+        gb = rows_of(xb);
       }
+      const int h = hb + g;
+      uint8_t* const to = dst + h * y_sh;
+      if (l.has_a && h < h1) *reinterpret_cast<uint4*>(to + l.pa * 16) = ga;
+      if (l.has_b && h < h1) *reinterpret_cast<uint4*>(to + l.pb * 16) = gb;
+      ga = nga; gb = ngb; za = nza; zb = nzb;
     }
   }
   if (!a.dw) return;                       // (the same for all of a block)
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < 8; ++j) {
     float s[2];
     f2_get(dw[j], s[0], s[1]);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
 #pragma unroll
       for (int m = L; m < 32; m <<= 1) s[e] += __shfl_xor_sync(kAll, s[e], m);
-      if (g == 0 && mine) sums_s[warp][8 * i + 2 * j + e] = s[e];
+      if (g == 0 && (j < 4 ? l.has_a : l.has_b)) sums_s[warp][8 * (j < 4 ? l.pa : l.pb) + j % 4 * 2 + e] = s[e];
     }
   }
   __syncthreads();
@@ -337,7 +358,7 @@ static void set_tensor(RotaryTensor* t, mala_tin x, mala_tout y, int B, int N, i
   t->by_n.set((uint32_t)N);
 }
 
-static int lanes_of(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
+static int lanes_of(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
 
 // Heads per item: all of a row's while that leaves every SM 32 warps, fewer where there are few rows (one load of a warp at least)
 static void set_items(RotaryParams* p, int tensors, int sms) {
@@ -374,8 +395,8 @@ static int launch_rotary_by(const RotaryParams& p, int interleaved, int sms, cud
 template <bool kNorm, bool kPages>
 static int launch_rotary(const RotaryParams& p, int interleaved, int sms, cudaStream_t stream) {
   const int L = lanes_of(p.rule.d);
-  return L == 8 ? launch_rotary_by<8, kNorm, kPages>(p, interleaved, sms, stream)
-                : L == 16 ? launch_rotary_by<16, kNorm, kPages>(p, interleaved, sms, stream) : launch_rotary_by<32, kNorm, kPages>(p, interleaved, sms, stream);
+  return L == 4 ? launch_rotary_by<4, kNorm, kPages>(p, interleaved, sms, stream)
+                : L == 8 ? launch_rotary_by<8, kNorm, kPages>(p, interleaved, sms, stream) : launch_rotary_by<16, kNorm, kPages>(p, interleaved, sms, stream);
 }
 
 template <int L>
@@ -403,8 +424,8 @@ static int launch_norm_bwd(RotaryParams& p, int interleaved, float* dwq, float* 
   }
   p.q_blocks = (int)gq;
   const int blocks = (int)(gq + gk), L = lanes_of(p.rule.d);
-  MALA_TRY(L == 8 ? launch_norm_bwd_by<8>(p, interleaved, blocks, stream)
-                  : L == 16 ? launch_norm_bwd_by<16>(p, interleaved, blocks, stream) : launch_norm_bwd_by<32>(p, interleaved, blocks, stream));
+  MALA_TRY(L == 4 ? launch_norm_bwd_by<4>(p, interleaved, blocks, stream)
+                  : L == 8 ? launch_norm_bwd_by<8>(p, interleaved, blocks, stream) : launch_norm_bwd_by<16>(p, interleaved, blocks, stream));
   if (!dwq && !dwk) return MALA_OK;
   return launch_dependent(rotary_norm_sum_kernel, dim3((p.rule.d + 31) / 32, 2), dim3(1024), stream, (const float*)p.partial, dwq, dwk, p.rule.d,
                           p.q_blocks, blocks) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;

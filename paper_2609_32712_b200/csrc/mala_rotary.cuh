@@ -65,104 +65,168 @@ __device__ __forceinline__ float f2_sum(uint64_t x) {
   return a + b;
 }
 
-// What a lane needs to rotate its columns 8 i .. 8 i + 7:  out = C x + S x',  x' the column's partner, two columns at a time.  Where a column is
-// not rotated C = 1, S = -0 and x' is read as 0, so that it stays whatever it is.
+// A weight of a norm (bf16 or fp32; 1 without)
+__device__ __forceinline__ float weight_at(const void* w, int fp32, int c) {
+  if (!w) return 1.f;
+  return fp32 ? __ldg((const float*)w + c) : __bfloat162float(__ldg((const __nv_bfloat16*)w + c));
+}
+
+// A row of d columns in L lanes, two pieces of eight columns each: pieces whose columns are paired (halves), so that a pair lies in one lane, or
+// neighbouring pieces.
 template <int kPairs>
-struct LaneTurns {
-  int i, from;              // (kHalves: the lane of the warp that holds the partners)
-  uint32_t rotated;         // bit e: column 8 i + e is one of the rotated ones
-  // lane_of_row: of the lanes that hold a row, the first one of which is lane `base` of the warp
-  __device__ __forceinline__ void set(const RotaryRule& r, int lane_of_row, int base) {
-    const bool mine = 8 * lane_of_row < r.d;
-    i = mine ? lane_of_row : 0;                          // (lanes behind the row: any of it)
-    from = base + (mine ? partner_of<kHalves>(8 * i, r.rotary) / 8 : lane_of_row);
-    rotated = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) rotated |= (8 * i + e < r.rotary ? 1u : 0u) << e;
+struct LanePieces {
+  int pa, pb;               // the pieces
+  bool has_a, has_b, pair;  // whether the row has them; whether a's columns are paired with b's (halves)
+  int turns;                // neighbours: whether all eight pairs of columns are rotated (2), some (1) or none (0)
+  __device__ __forceinline__ void set(const RotaryRule& r, int c) {
+    const int turned = r.rotary / 16;
+    pair = kPairs == kHalves && c < turned;
+    pa = pair ? c : 2 * c;
+    pb = pair ? c + turned : 2 * c + 1;
+    has_a = 8 * pa < r.d;
+    has_b = 8 * pb < r.d;
+    turns = 16 * c + 16 <= r.rotary ? 2 : 16 * c < r.rotary ? 1 : 0;
   }
-  // a mask of a register with the columns 8 i + 2 j and 8 i + 2 j + 1: those that are rotated
-  __device__ __forceinline__ uint32_t mask(int j) const {
-    if (kPairs == kHalves) return rotated ? 0xffffffffu : 0u;
-    return ((rotated >> (2 * j)) & 1 ? 0xffffu : 0u) | ((rotated >> (2 * j + 1)) & 1 ? 0xffff0000u : 0u);
+};
+
+// cos and sin (with magnitude and sense) of the angles of lane c of a row at one position: kAngles of them, of the pairs 8 c + e, or (kHalvesOdd) of the
+// columns 16 c + e; where nothing is rotated 1 and 0.  All 32 / L rows of the warp are at this position, so each lane works out its share of the angles and gets
+// the others by shuffles.
+template <int kPairs>
+constexpr int kAngles = kPairs == kHalvesOdd ? 16 : 8;
+template <int L, int kPairs>
+__device__ __forceinline__ void angles_at(const RotaryRule& r, const uint64_t* turns, int c, int g, int pos, float (&C)[kAngles<kPairs>], float (&S)[kAngles<kPairs>]) {
+  constexpr int kShare = kAngles<kPairs> * L / 32;
+  static_assert(kShare >= 1, "a lane has an angle at least");
+  const int half = r.rotary / 2;
+  float cs[kShare], sn[kShare];
+#pragma unroll
+  for (int j = 0; j < kShare; ++j) {
+    const int x = kAngles<kPairs> * c + g * kShare + j;
+    const bool on = x < (kPairs == kHalvesOdd ? r.rotary : half);
+    cos_sin(turns[!on ? 0 : kPairs == kHalvesOdd && x >= half ? x - half : x], pos, cs[j], sn[j]);
+    cs[j] = on ? cs[j] * r.magnitude : 1.f;
+    sn[j] = on ? sn[j] * (kPairs == kHalvesOdd && x < half ? -r.turned : r.turned) : 0.f;
   }
-  // C and S at a position; `group`: the lanes that make this call together (their rows in full)
-  __device__ __forceinline__ void at(const RotaryRule& r, const uint64_t* turns, int pos, uint32_t group, float (&C)[8], float (&S)[8]) const {
-    const int half = r.rotary / 2;
-    if constexpr (kPairs == kHalves) {
-      // the two lanes of a pair need the same eight angles: four each, and the others' by shuffles
-      const bool first = 8 * i < half;
-      const uint64_t* f = turns + (rotated ? first ? 8 * i : 8 * i - half + 4 : 0);
-      float c[4], s[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        cos_sin(f[j], pos, c[j], s[j]);
-        c[j] *= r.magnitude;
-        s[j] *= r.turned;
-      }
+  for (int e = 0; e < kAngles<kPairs>; ++e) {
+    const int from = e / kShare * L + c;
+    C[e] = __shfl_sync(0xffffffffu, cs[e % kShare], from);
+    S[e] = __shfl_sync(0xffffffffu, sn[e % kShare], from);
+  }
+}
+
+// What a lane multiplies with, two columns at a time: halves  a <- a C - b S', b <- b C' + a S  (C, C' and S, S' differ by a norm's weights only); neighbours
+// pair by pair  x <- x C - y S', y <- y C' + x S;  kHalvesOdd: column by column  x <- x C + partner S.
+template <int kPairs>
+struct LaneFactors {
+  uint64_t ca[4], cb[4], sa[4], sb[4];     // C, C', S, -S'  (kHalvesOdd: C of a and b, S of a and b)
+  template <bool kNorm>
+  __device__ __forceinline__ void set(const RotaryRule& r, int c, const LanePieces<kPairs>& l, const float (&C)[kAngles<kPairs>], const float (&S)[kAngles<kPairs>],
+                                      const void* weight, int fp32) {
+    float w[16], v[16];                    // weights of the lane's columns and (kHalvesOdd) of their partners
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float c2 = __shfl_sync(group, c[j], from), s2 = __shfl_sync(group, s[j], from);
-        C[j] = rotated ? first ? c[j] : c2 : 1.f;
-        C[j + 4] = rotated ? first ? c2 : c[j] : 1.f;
-        S[j] = rotated ? first ? -s[j] : s2 : -0.f;
-        S[j + 4] = rotated ? first ? -s2 : s[j] : -0.f;
-      }
-    } else {
-      constexpr int kAngles = kPairs == kNeighbours ? 4 : 8;
-#pragma unroll
-      for (int j = 0; j < kAngles; ++j) {
-        const int col = kPairs == kNeighbours ? 8 * i + 2 * j : 8 * i + j;
-        const bool turn = col < r.rotary;
-        float c, s;
-        cos_sin(turns[!turn ? 0 : kPairs == kNeighbours ? col / 2 : col < half ? col : col - half], pos, c, s);
-        c = turn ? c * r.magnitude : 1.f;
-        s = turn ? s * r.turned : -0.f;
-        if constexpr (kPairs == kNeighbours) {
-          C[2 * j] = C[2 * j + 1] = c;
-          S[2 * j] = turn ? -s : s;
-          S[2 * j + 1] = s;
-        } else {
-          C[j] = c;
-          S[j] = turn && col < half ? -s : s;
-        }
-      }
+    for (int e = 0; e < 16; ++e) {
+      const int col = kNorm ? min(8 * (e < 8 ? l.pa : l.pb) + e % 8, r.d - 1) : 0;
+      w[e] = kNorm ? weight_at(weight, fp32, col) : 1.f;
+      v[e] = kNorm && kPairs == kHalvesOdd ? weight_at(weight, fp32, partner_of<kPairs>(col, r.rotary)) : 1.f;
     }
-  }
-  // x' of the lane's columns: the row lies in the registers of the lanes of `group`, or (kHalvesOdd) in shared memory at `row`, written before
-  __device__ __forceinline__ void partners(const uint4& w, const __nv_bfloat16* row, int rotary, uint32_t group, uint64_t (&y)[4]) const {
-    const uint32_t own[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if constexpr (kPairs == kHalves) {
-        y[j] = pair_of(__shfl_sync(group, own[j], from) & mask(j));
+        ca[j] = f2(w[2 * j] * C[2 * j], w[2 * j + 1] * C[2 * j + 1]);
+        cb[j] = f2(w[8 + 2 * j] * C[2 * j], w[9 + 2 * j] * C[2 * j + 1]);
+        sa[j] = f2(w[2 * j] * S[2 * j], w[2 * j + 1] * S[2 * j + 1]);
+        sb[j] = f2(-w[8 + 2 * j] * S[2 * j], -w[9 + 2 * j] * S[2 * j + 1]);
       } else if constexpr (kPairs == kNeighbours) {
-        y[j] = crossed_pair_of(own[j] & mask(j));
+        // pair j of a, and of b:  (x, y) times (C, C') and (y, x) times (-S', S)
+        ca[j] = f2(w[2 * j] * C[j], w[2 * j + 1] * C[j]);
+        cb[j] = f2(w[8 + 2 * j] * C[4 + j], w[9 + 2 * j] * C[4 + j]);
+        sa[j] = f2(-w[2 * j + 1] * S[j], w[2 * j] * S[j]);
+        sb[j] = f2(-w[9 + 2 * j] * S[4 + j], w[8 + 2 * j] * S[4 + j]);
       } else {
-        const float a = __bfloat162float(row[partner_of<kPairs>(8 * i + 2 * j, rotary)]);
-        const float b = __bfloat162float(row[partner_of<kPairs>(8 * i + 2 * j + 1, rotary)]);
-        y[j] = f2((rotated >> (2 * j)) & 1 ? a : 0.f, (rotated >> (2 * j + 1)) & 1 ? b : 0.f);
+        ca[j] = f2(w[2 * j] * C[2 * j], w[2 * j + 1] * C[2 * j + 1]);
+        cb[j] = f2(w[8 + 2 * j] * C[8 + 2 * j], w[9 + 2 * j] * C[9 + 2 * j]);
+        sa[j] = f2(v[2 * j] * S[2 * j], v[2 * j + 1] * S[2 * j + 1]);
+        sb[j] = f2(v[8 + 2 * j] * S[8 + 2 * j], v[9 + 2 * j] * S[9 + 2 * j]);
       }
     }
   }
 };
 
-// x <- C x + S x'
-__device__ __forceinline__ void turn_pairs(uint64_t (&x)[4], const uint64_t (&y)[4], const uint64_t (&C)[4], const uint64_t (&S)[4]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = f2_fma(y[j], S[j], f2_mul(x[j], C[j]));
+__device__ __forceinline__ uint64_t crossed(uint64_t x) {
+  float a, b;
+  f2_get(x, a, b);
+  return f2(b, a);
 }
-__device__ __forceinline__ void pack_turns(const float (&C)[8], const float (&S)[8], uint64_t (&C2)[4], uint64_t (&S2)[4]) {
+
+// A lane's two pieces rotated (and multiplied by the norm's weights).  kHalvesOdd: the row lies in shared memory at `row`, its columns in order.  What is not rotated is
+// multiplied by its weight alone, whatever stands beside it.
+template <int kPairs, bool kNorm>
+__device__ __forceinline__ void rotate_pieces(const RotaryRule& r, int c, const LanePieces<kPairs>& l, const LaneFactors<kPairs>& f, const __nv_bfloat16* row, uint64_t (&a)[4],
+                                              uint64_t (&b)[4]) {
+  if constexpr (kPairs == kHalves) {
+    if (l.pair) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    C2[j] = f2(C[2 * j], C[2 * j + 1]);
-    S2[j] = f2(S[2 * j], S[2 * j + 1]);
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t x = a[j];
+        a[j] = f2_fma(b[j], f.sb[j], f2_mul(x, f.ca[j]));
+        b[j] = f2_fma(x, f.sa[j], f2_mul(b[j], f.cb[j]));
+      }
+      return;
+    }
+  } else if constexpr (kPairs == kNeighbours) {
+    if (l.turns == 2) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        a[j] = f2_fma(crossed(a[j]), f.sa[j], f2_mul(a[j], f.ca[j]));
+        b[j] = f2_fma(crossed(b[j]), f.sb[j], f2_mul(b[j], f.cb[j]));
+      }
+      return;
+    }
+    if (l.turns == 1) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t x = f2_mul(a[j], f.ca[j]), y = f2_mul(b[j], f.cb[j]);
+        a[j] = 16 * c + 2 * j < r.rotary ? f2_fma(crossed(a[j]), f.sa[j], x) : x;
+        b[j] = 16 * c + 8 + 2 * j < r.rotary ? f2_fma(crossed(b[j]), f.sb[j], y) : y;
+      }
+      return;
+    }
+  } else {
+    if (l.turns > 0) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int col = 16 * c + e;
+        uint64_t& x2 = e < 8 ? a[e / 2] : b[e / 2 - 4];
+        float x[2], k[2], s[2];
+        f2_get(x2, x[0], x[1]);
+        f2_get(e < 8 ? f.ca[e / 2] : f.cb[e / 2 - 4], k[0], k[1]);
+        f2_get(e < 8 ? f.sa[e / 2] : f.sb[e / 2 - 4], s[0], s[1]);
+        x[e % 2] *= k[e % 2];
+        if (col < r.rotary) x[e % 2] = fmaf(__bfloat162float(row[partner_of<kPairs>(col, r.rotary)]), s[e % 2], x[e % 2]);
+        x2 = f2(x[0], x[1]);
+      }
+      return;
+    }
+  }
+  if constexpr (kNorm) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      a[j] = f2_mul(a[j], f.ca[j]);
+      b[j] = f2_mul(b[j], f.cb[j]);
+    }
   }
 }
 
-// A weight of a norm (bf16 or fp32; 1 without)
-__device__ __forceinline__ float weight_at(const void* w, int fp32, int c) {
-  if (!w) return 1.f;
-  return fp32 ? __ldg((const float*)w + c) : __bfloat162float(__ldg((const __nv_bfloat16*)w + c));
+__device__ __forceinline__ float squares(const uint64_t (&a)[4], const uint64_t (&b)[4]) {
+  uint64_t s = f2_mul(a[0], a[0]), t = f2_mul(b[0], b[0]);
+#pragma unroll
+  for (int j = 1; j < 4; ++j) {
+    s = f2_fma(a[j], a[j], s);
+    t = f2_fma(b[j], b[j], t);
+  }
+  return f2_sum(s) + f2_sum(t);
 }
 
 inline int pairs_kind(int rotary, int interleaved) { return interleaved ? kNeighbours : rotary % 16 == 0 ? kHalves : kHalvesOdd; }

@@ -139,8 +139,12 @@ rotary_write8_kernel(const RotaryWriteParams p) {
     }
     // where the next round begins: the first unit of this block that is not taken
     int next = t1;
-    for (int j = next_end(0); j < window && s + j < t1; j = next_end(j + 1))
-      if (((valid_s[j >> 5] >> (j & 31)) & 1u) && !taken(j)) { next = s + j; break; }
+    bool held = false;                     // whether a unit of the round holds keys already
+    for (int j = 0; j < window && s + j < t1; j = next_end(j + 1)) {
+      if (!((valid_s[j >> 5] >> (j & 31)) & 1u)) continue;
+      if (!taken(j)) { next = s + j; break; }
+      held = held || (slot_s[j] & (p.unit - 1)) != 0;
+    }
     // this thread's unit, if it keeps one: row tid begins it
     const bool keeper = tid < window && taken(tid);
     float* scale = scales;
@@ -306,7 +310,7 @@ rotary_write8_kernel(const RotaryWriteParams p) {
       }
       if (keeper) scale[(int64_t)h * p.per_page] = scale_of(tid);
       // units that hold keys already, and whose scale grows: these keys' codes on the new scale, by the whole block
-      for (int j = next_end(0); j < window; j = next_end(j + 1)) {
+      for (int j = 0; held && j < window && s + j < t1; j = next_end(j + 1)) {
         const int off = (int)(slot_s[j] & (p.unit - 1));
         if (off == 0 || !taken(j)) continue;
         const float was = old_s[par][j], now = scale_of(j);
