@@ -121,6 +121,7 @@ int device_setup(int dev, int** status_out) {
     ok = ok && bias_set_attributes();
     ok = ok && scaled_set_attributes();
     ok = ok && cache_set_attributes();
+    ok = ok && rotary_set_attributes();
     if (!ok) return MALA_ERR_CUDA;
     g_attr_done[dev] = true;
   }

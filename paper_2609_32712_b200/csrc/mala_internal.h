@@ -11,6 +11,7 @@ int current_device_checked(int* dev_out);
 int device_setup(int dev, int** status_out);
 int sm_count(int dev);
 bool cache_set_attributes();   // (mala_cache.cu)
+bool rotary_set_attributes();  // (mala_rotary.cu)
 
 // mala_cache.cu: reads of a paged cache; fp8 with `scales`: bf16(code), the scales in a table of 24 floats per KV head and key block of 128 keys
 // of a sequence (the keys' scales of its eight groups of 16, log2 of the values' and their inverses), key block j of sequence b at

@@ -66,108 +66,176 @@ struct Positions {
   }
 };
 
-__device__ __forceinline__ uint4 piece_at(const uint8_t* row, int piece, bool has) {
-  return has ? *reinterpret_cast<const uint4*>(row + piece * 16) : make_uint4(0u, 0u, 0u, 0u);
-}
-// What the rows of a warp leave in shared memory, columns in order, for partners that begin inside a piece
-__device__ __forceinline__ void stage_row(uint4* buf, int lane, const uint4& a, const uint4& b) {
-  __syncwarp();
-  buf[2 * lane] = a;
-  buf[2 * lane + 1] = b;
-  __syncwarp();
-}
+// A row's address, heads and place among a tensor's, item by item: a row and `span` of its heads
+struct Item {
+  int which, t, b, n, h0, h1;
+  __device__ __forceinline__ void at(const RotaryParams& p, uint32_t nq, uint32_t nk, uint32_t item) {
+    which = item < nq ? 0 : item < nq + nk ? 1 : 2;
+    const int x0 = (int)(item - (which == 0 ? 0 : which == 1 ? nq : nq + nk));
+    const RotaryTensor& a = p.t[which];
+    t = (int)a.by_spans.div((uint32_t)x0);
+    h0 = (x0 - t * (int)a.by_spans.d) * a.span;
+    h1 = min(h0 + a.span, a.H);
+    b = (int)a.by_n.div((uint32_t)t);
+    n = t - b * a.N;
+  }
+};
 
-// Rotations.  A row lies in the registers of L lanes, and a warp works on 32 / L heads of a token at a time, two such loads in flight behind
-// the two that it works on: the angles of a token are worked out once for all heads that a warp takes, and a warp's tokens are
-// neighbours.
+// Rows on their way: a warp's rows come into a ring of kDepth places in shared memory, up to kDepth - 1 batches (a head each for the 32 / L groups of the warp) ahead
+// and across its items, each lane's pieces into places of the lane: the first ones of all lanes, then the second ones, so that neighbours in memory are neighbours
+// here (with a lane's two side by side every 32-byte sector was fetched twice).  In registers the same depth would leave half the warps.
+__device__ __forceinline__ void piece_async(uint4* to, const uint8_t* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void batch_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kAhead>
+__device__ __forceinline__ void batch_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory"); }
+
+// kBoth: the incoming gradient and x, else x alone.  (Places of pieces that a row does not have are 0 throughout.)
+template <int L, int kPairs, bool kBoth>
+struct Rows {
+  static constexpr int P = 32 / L, kDepth = kBoth ? 4 : 8, kPlace = kBoth ? 128 : 64;   // places of a batch (16 bytes)
+  uint4 *ring, *put;        // this lane's places of the first batch, and of the next one to be asked for
+  const uint4* got;         // ... of the next one to be taken
+  uint64_t next;            // items: this one, and every `stride`th behind it
+  uint32_t end, stride, nq, nk;
+  int batches, left;        // of the item whose rows are asked for: batches, and heads from this group's on
+  const uint8_t *x, *g;     // this lane's first piece of the next batch
+  int64_t x_step, g_step;
+  int to_b;                 // from a lane's first piece to its second one
+  __device__ __forceinline__ void item(const RotaryParams& p, const LanePieces<L, kPairs>& l, int group) {
+    batches = 0;
+    left = 0;
+    if (next >= end) return;
+    Item it;
+    it.at(p, nq, nk, (uint32_t)next);
+    next += stride;
+    const RotaryTensor& a = p.t[it.which];
+    x = a.x + it.b * a.x_sb + it.n * a.x_sn + (it.h0 + group) * a.x_sh + l.pa * 16;
+    x_step = P * a.x_sh;
+    if (kBoth) {
+      g = a.g + it.b * a.g_sb + it.n * a.g_sn + (it.h0 + group) * a.g_sh + l.pa * 16;
+      g_step = P * a.g_sh;
+    }
+    batches = (it.h1 - it.h0 + P - 1) / P;
+    left = it.h1 - it.h0 - group;
+  }
+  __device__ __forceinline__ void ask(const RotaryParams& p, const LanePieces<L, kPairs>& l, int group) {
+    if (kPairs == kHalvesOdd) __syncwarp();              // (partners have been read)
+    if (left > 0) {
+      if (l.has_a) piece_async(put, x);
+      if (l.has_b) piece_async(put + 32, x + to_b);
+      if (kBoth) {
+        if (l.has_a) piece_async(put + 64, g);
+        if (l.has_b) piece_async(put + 96, g + to_b);
+      }
+    }
+    batch_done();
+    put = put == ring + (kDepth - 1) * kPlace ? ring : put + kPlace;
+    x += x_step;
+    if (kBoth) g += g_step;
+    left -= P;
+    if (--batches == 0) item(p, l, group);
+  }
+  __device__ __forceinline__ void begin(const RotaryParams& p, const LanePieces<L, kPairs>& l, int group, uint4* ring_, uint32_t first, uint32_t end_, uint32_t stride_,
+                                        uint32_t nq_, uint32_t nk_) {
+    ring = put = ring_;
+    got = ring_;
+    next = first; end = end_; stride = stride_; nq = nq_; nk = nk_;
+    x = g = nullptr; x_step = g_step = 0;
+    to_b = (l.pb - l.pa) * 16;
+#pragma unroll
+    for (int i = 0; i < kDepth; ++i) {
+      if (!l.has_a) ring[i * kPlace] = make_uint4(0u, 0u, 0u, 0u);
+      if (!l.has_b) ring[i * kPlace + 32] = make_uint4(0u, 0u, 0u, 0u);
+      if (kBoth && !l.has_a) ring[i * kPlace + 64] = make_uint4(0u, 0u, 0u, 0u);
+      if (kBoth && !l.has_b) ring[i * kPlace + 96] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    item(p, l, group);
+    for (int i = 0; i < kDepth - 1; ++i) ask(p, l, group);
+  }
+  // this lane's places of the next batch, which has arrived (one more is asked for)
+  __device__ __forceinline__ const uint4* take(const RotaryParams& p, const LanePieces<L, kPairs>& l, int group) {
+    ask(p, l, group);
+    batch_wait<kDepth - 1>();
+    if (kPairs == kHalvesOdd) __syncwarp();
+    const uint4* const at = got;
+    got = got == ring + (kDepth - 1) * kPlace ? ring : got + kPlace;
+    return at;
+  }
+};
+constexpr int kRingBytes = kRotaryWarps * 8192;
+
+// Rotations.  A row lies in the registers of L lanes, and a warp works on 32 / L heads of a token at a time: the angles of a token are worked out once for
+// all heads that a warp takes, and a warp's tokens are neighbours.
 template <int L, int kPairs, bool kNorm, bool kPages>
-__global__ void __launch_bounds__(kRotaryThreads, 2)
+__global__ void __launch_bounds__(kRotaryThreads, kNorm || kPairs == kHalvesOdd ? 2 : 3)
 rotary_kernel(const RotaryParams p) {
-  constexpr int P = 32 / L, U = 2;
+  constexpr int P = 32 / L;
+  extern __shared__ uint4 ring_s[];
   __shared__ uint64_t turns_s[kMaxPairs];
-  __shared__ uint4 rows_s[kPairs == kHalvesOdd ? kRotaryWarps * 64 : 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, c = lane % L;
-  uint4* const buf = rows_s + (kPairs == kHalvesOdd ? warp * 64 : 0);
-  LanePieces<kPairs> l;
+  LanePieces<L, kPairs> l;
   l.set(p.rule, c);
+  const uint32_t nq = p.t[0].items, nk = p.t[1].items, all = nq + nk + (kPages ? p.t[2].items : 0);   // (at most 3 * 2^30)
+  const uint32_t stride = gridDim.x * kRotaryWarps, first = blockIdx.x * kRotaryWarps + warp;
+  Rows<L, kPairs, false> rows;
+  rows.begin(p, l, g, ring_s + warp * 512 + lane, first, all, stride, nq, nk);
   load_turns(p.rule, turns_s);
   __syncthreads();
-  const uint32_t nq = p.t[0].items, nk = p.t[1].items, all = nq + nk + (kPages ? p.t[2].items : 0);   // (at most 3 * 2^30)
-  const uint32_t share = (all + gridDim.x * kRotaryWarps - 1) / (gridDim.x * kRotaryWarps);
-  const uint64_t first = (uint64_t)(blockIdx.x * kRotaryWarps + warp) * share;
   Positions positions;
-  for (uint64_t x = first; x < first + share && x < all; ++x) {
-    const uint32_t item = (uint32_t)x;
-    const int which = item < nq ? 0 : item < nq + nk ? 1 : 2, x0 = (int)(item - (which == 0 ? 0 : which == 1 ? nq : nq + nk));
-    const RotaryTensor& a = p.t[which];
-    const int t = (int)a.by_spans.div((uint32_t)x0), h0 = (x0 - t * (int)a.by_spans.d) * a.span, h1 = min(h0 + a.span, a.H);
-    const int b = (int)a.by_n.div((uint32_t)t), n = t - b * a.N;
+  for (uint64_t x = first; x < all; x += stride) {
+    Item it;
+    it.at(p, nq, nk, (uint32_t)x);
+    const RotaryTensor& a = p.t[it.which];
     uint8_t* dst = a.y;
-    if (kPages && which > 0) {
-      const int64_t slot = __ldg(p.slots + t);
-      if (slot < 0 || slot >= p.limit) continue;
+    bool place = true;
+    if (kPages && it.which > 0) {
+      const int64_t slot = __ldg(p.slots + it.t);
+      place = slot >= 0 && slot < p.limit;
       const int64_t page = p.limit <= 0xffffffffll ? (int64_t)p.by_page.div((uint32_t)slot) : slot / p.page_size;
       dst += page * a.y_sb + (slot - page * p.page_size) * a.y_sn;
     } else {
-      dst += b * a.y_sb + n * a.y_sn;
+      dst += it.b * a.y_sb + it.n * a.y_sn;
     }
-    const uint8_t* src = a.x + b * a.x_sb + n * a.x_sn;
-    const int64_t x_sh = a.x_sh, y_sh = a.y_sh;
-    uint4 wa[U], wb[U];
-    auto load = [&](int hb, uint4 (&to_a)[U], uint4 (&to_b)[U]) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = hb + u * P + g;
-        to_a[u] = piece_at(src + h * x_sh, l.pa, l.has_a && h < h1);
-        to_b[u] = piece_at(src + h * x_sh, l.pb, l.has_b && h < h1);
-      }
-    };
-    load(h0, wa, wb);
     int pos = 0;
-    const bool turn = which < 2 && positions.of(p, a, which, t, b, n, pos);
-    LaneFactors<kPairs> f;
+    const bool turn = it.which < 2 && positions.of(p, a, it.which, it.t, it.b, it.n, pos);
+    LaneFactors<L, kPairs> f;
     if (turn) {
       float C[kAngles<kPairs>], S[kAngles<kPairs>];
-      angles_at<L, kPairs>(p.rule, turns_s, c, g, pos, C, S);
-      f.template set<kNorm>(p.rule, c, l, C, S, a.weight, p.weights_fp32);
+      angles_at<L, kPairs>(p.rule, turns_s, l, c, g, pos, C, S);
+      f.template set<kNorm>(p.rule, l, C, S, a.weight, p.weights_fp32);
     }
-    for (int hb = h0; hb < h1; hb += P * U) {
-      uint4 na[U], nb[U];
-      if (hb + P * U < h1) load(hb + P * U, na, nb);
+    uint8_t* to = dst + (it.h0 + g) * a.y_sh + l.pa * 16;
+    const int64_t y_step = P * a.y_sh;
+    for (int h = it.h0 + g, hb = it.h0; hb < it.h1; hb += P, h += P, to += y_step) {
+      const uint4* const at = rows.take(p, l, g);
+      uint4 wa = at[0], wb = at[32];
       if (turn) {                          // (not: values, and rows that no sequence has)
+        uint64_t xa[4], xb[4];
+        pairs_of(wa, xa);
+        pairs_of(wb, xb);
+        float sum = 0.f;
+        if constexpr (kNorm) {
+          sum = squares(xa, xb);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          uint64_t xa[4], xb[4];
-          if constexpr (kPairs == kHalvesOdd) stage_row(buf, lane, wa[u], wb[u]);
-          pairs_of(wa[u], xa);
-          pairs_of(wb[u], xb);
-          float sum = 0.f;
-          if constexpr (kNorm) {
-            sum = squares(xa, xb);
-#pragma unroll
-            for (int m = L / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-          }
-          rotate_pieces<kPairs, kNorm>(p.rule, c, l, f, reinterpret_cast<const __nv_bfloat16*>(buf + 2 * g * L), xa, xb);
-          if constexpr (kNorm) {
-            const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              xa[j] = f2_mul(xa[j], f2(r, r));
-              xb[j] = f2_mul(xb[j], f2(r, r));
-            }
-          }
-          wa[u] = rows_of(xa);
-          wb[u] = rows_of(xb);
+          for (int m = L / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
         }
-      }
+        rotate_pieces<L, kPairs, kNorm>(p.rule, l, f, reinterpret_cast<const __nv_bfloat16*>(at - c), xa, xb);
+        if constexpr (kNorm) {
+          const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = hb + u * P + g;
-        uint8_t* const to = dst + h * y_sh;
-        if (l.has_a && h < h1) *reinterpret_cast<uint4*>(to + l.pa * 16) = wa[u];
-        if (l.has_b && h < h1) *reinterpret_cast<uint4*>(to + l.pb * 16) = wb[u];
-        wa[u] = na[u];
-        wb[u] = nb[u];
+          for (int j = 0; j < 4; ++j) {
+            xa[j] = f2_mul(xa[j], f2(r, r));
+            xb[j] = f2_mul(xb[j], f2(r, r));
+          }
+        }
+        wa = rows_of(xa);
+        wb = rows_of(xb);
+      }
+      if (h < it.h1 && place) {
+        if (l.has_a) *reinterpret_cast<uint4*>(to) = wa;
+        if (l.has_b) *reinterpret_cast<uint4*>(to + rows.to_b) = wb;
       }
     }
   }
@@ -181,62 +249,50 @@ __global__ void __launch_bounds__(kRotaryThreads, 2)
 rotary_norm_bwd_kernel(const RotaryParams p) {
   constexpr int P = 32 / L;
   constexpr uint32_t kAll = 0xffffffffu;
+  extern __shared__ uint4 ring_s[];
   __shared__ uint64_t turns_s[kMaxPairs];
-  __shared__ uint4 rows_s[kPairs == kHalvesOdd ? kRotaryWarps * 64 : 1];
-  __shared__ float sums_s[kRotaryWarps][256];
   __shared__ __align__(16) float weight_s[256];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, c = lane % L;
-  uint4* const buf = rows_s + (kPairs == kHalvesOdd ? warp * 64 : 0);
   const int which = (int)blockIdx.x < p.q_blocks ? 0 : 1, block = blockIdx.x - (which ? p.q_blocks : 0);
   const int blocks = which ? gridDim.x - p.q_blocks : p.q_blocks;
   const RotaryTensor& a = p.t[which];
-  LanePieces<kPairs> l;
+  LanePieces<L, kPairs> l;
   l.set(p.rule, c);
+  const uint32_t nq = p.t[0].items, before = which ? nq : 0, stride = blocks * kRotaryWarps, first = before + block * kRotaryWarps + warp, end = before + a.items;
+  Rows<L, kPairs, true> rows;
+  rows.begin(p, l, g, ring_s + warp * 512 + lane, first, end, stride, nq, p.t[1].items);
   load_turns(p.rule, turns_s);
   for (int x = threadIdx.x; x < p.rule.d; x += kRotaryThreads) weight_s[x] = weight_at(a.weight, p.weights_fp32, x);
   __syncthreads();
   uint64_t dw[8] = {0, 0, 0, 0, 0, 0, 0, 0};   // of the columns of a, and of b
   const float4* const weights_a = reinterpret_cast<const float4*>(weight_s) + (l.has_a ? 2 * l.pa : 0);
   const float4* const weights_b = reinterpret_cast<const float4*>(weight_s) + (l.has_b ? 2 * l.pb : 0);
-  const int share = (a.items + blocks * kRotaryWarps - 1) / (blocks * kRotaryWarps);
-  const int64_t first = (int64_t)(block * kRotaryWarps + warp) * share;
   Positions positions;
-  for (int64_t x = first; x < first + share && x < a.items; ++x) {
-    const int item = (int)x;
-    const int t = (int)a.by_spans.div((uint32_t)item), h0 = (item - t * (int)a.by_spans.d) * a.span, h1 = min(h0 + a.span, a.H);
-    const int b = (int)a.by_n.div((uint32_t)t), n = t - b * a.N;
-    const uint8_t* gp = a.g + b * a.g_sb + n * a.g_sn;
-    const uint8_t* xp = a.x + b * a.x_sb + n * a.x_sn;
-    uint8_t* dst = a.y + b * a.y_sb + n * a.y_sn;
-    const int64_t g_sh = a.g_sh, x_sh = a.x_sh, y_sh = a.y_sh;
-    uint4 ga, gb, za, zb;
-    auto load = [&](int hb, uint4& to_ga, uint4& to_gb, uint4& to_za, uint4& to_zb) {
-      const int h = hb + g;
-      to_ga = piece_at(gp + h * g_sh, l.pa, l.has_a && h < h1);
-      to_gb = piece_at(gp + h * g_sh, l.pb, l.has_b && h < h1);
-      to_za = piece_at(xp + h * x_sh, l.pa, l.has_a && h < h1);
-      to_zb = piece_at(xp + h * x_sh, l.pb, l.has_b && h < h1);
-    };
-    load(h0, ga, gb, za, zb);
+  for (uint64_t x = first; x < end; x += stride) {
+    Item it;
+    it.at(p, nq, p.t[1].items, (uint32_t)x);
+    uint8_t* const dst = a.y + it.b * a.y_sb + it.n * a.y_sn;
     int pos = 0;
-    const bool turn = positions.of(p, a, which, t, b, n, pos);
-    LaneFactors<kPairs> f;
+    const bool turn = positions.of(p, a, which, it.t, it.b, it.n, pos);
+    LaneFactors<L, kPairs> f;
     if (turn) {
       float C[kAngles<kPairs>], S[kAngles<kPairs>];
-      angles_at<L, kPairs>(p.rule, turns_s, c, g, pos, C, S);
-      f.template set<false>(p.rule, c, l, C, S, nullptr, 0);
+      angles_at<L, kPairs>(p.rule, turns_s, l, c, g, pos, C, S);
+      f.template set<false>(p.rule, l, C, S, nullptr, 0);
     }
-    for (int hb = h0; hb < h1; hb += P) {
-      uint4 nga, ngb, nza, nzb;
-      if (hb + P < h1) load(hb + P, nga, ngb, nza, nzb);
+    uint8_t* to = dst + (it.h0 + g) * a.y_sh + l.pa * 16;
+    const int64_t y_step = P * a.y_sh;
+    for (int h = it.h0 + g, hb = it.h0; hb < it.h1; hb += P, h += P, to += y_step) {
+      const uint4* const at = rows.take(p, l, g);
+      const bool mine = h < it.h1;
+      uint4 ga = at[64], gb = at[96];
       if (turn) {
         uint64_t xa[4], xb[4], ya[4], yb[4];
-        if constexpr (kPairs == kHalvesOdd) stage_row(buf, lane, ga, gb);
         pairs_of(ga, xa);
         pairs_of(gb, xb);
-        rotate_pieces<kPairs, false>(p.rule, c, l, f, reinterpret_cast<const __nv_bfloat16*>(buf + 2 * g * L), xa, xb);
-        pairs_of(za, ya);
-        pairs_of(zb, yb);
+        rotate_pieces<L, kPairs, false>(p.rule, l, f, reinterpret_cast<const __nv_bfloat16*>(at + 64 - c), xa, xb);
+        pairs_of(at[0], ya);
+        pairs_of(at[32], yb);
         float sum = squares(ya, yb);
         uint64_t wga[4], wgb[4], da = 0, db = 0;
 #pragma unroll
@@ -262,22 +318,26 @@ rotary_norm_bwd_kernel(const RotaryParams p) {
         const uint64_t r2 = f2(r, r), back2 = f2(back, back);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          dw[j] = f2_fma(xa[j], f2_mul(ya[j], r2), dw[j]);
-          dw[4 + j] = f2_fma(xb[j], f2_mul(yb[j], r2), dw[4 + j]);
+          if (mine) {                      // (a group without a head has what was there before)
+            dw[j] = f2_fma(xa[j], f2_mul(ya[j], r2), dw[j]);
+            dw[4 + j] = f2_fma(xb[j], f2_mul(yb[j], r2), dw[4 + j]);
+          }
           xa[j] = f2_mul(r2, f2_fma(ya[j], back2, wga[j]));
           xb[j] = f2_mul(r2, f2_fma(yb[j], back2, wgb[j]));
         }
         ga = rows_of(xa);
         gb = rows_of(xb);
       }
-      const int h = hb + g;
-      uint8_t* const to = dst + h * y_sh;
-      if (l.has_a && h < h1) *reinterpret_cast<uint4*>(to + l.pa * 16) = ga;
-      if (l.has_b && h < h1) *reinterpret_cast<uint4*>(to + l.pb * 16) = gb;
-      ga = nga; gb = ngb; za = nza; zb = nzb;
+      if (mine) {
+        if (l.has_a) *reinterpret_cast<uint4*>(to) = ga;
+        if (l.has_b) *reinterpret_cast<uint4*>(to + rows.to_b) = gb;
+      }
     }
   }
   if (!a.dw) return;                       // (the same for all of a block)
+  batch_wait<0>();                         // (nothing is on its way into the ring)
+  __syncthreads();
+  float* const sums_s = reinterpret_cast<float*>(ring_s);   // [warps][256]
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     float s[2];
@@ -286,14 +346,14 @@ rotary_norm_bwd_kernel(const RotaryParams p) {
     for (int e = 0; e < 2; ++e) {
 #pragma unroll
       for (int m = L; m < 32; m <<= 1) s[e] += __shfl_xor_sync(kAll, s[e], m);
-      if (g == 0 && (j < 4 ? l.has_a : l.has_b)) sums_s[warp][8 * (j < 4 ? l.pa : l.pb) + j % 4 * 2 + e] = s[e];
+      if (g == 0 && (j < 4 ? l.has_a : l.has_b)) sums_s[warp * 256 + 8 * (j < 4 ? l.pa : l.pb) + j % 4 * 2 + e] = s[e];
     }
   }
   __syncthreads();
   if ((int)threadIdx.x < p.rule.d) {
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kRotaryWarps; ++w) sum += sums_s[w][threadIdx.x];
+    for (int w = 0; w < kRotaryWarps; ++w) sum += sums_s[w * 256 + threadIdx.x];
     p.partial[(size_t)blockIdx.x * p.rule.d + threadIdx.x] = sum;
   }
 }
@@ -379,9 +439,9 @@ static void set_items(RotaryParams* p, int tensors, int sms) {
 template <int L, int kPairs, bool kNorm, bool kPages>
 static int launch_rotary_as(const RotaryParams& p, int sms, cudaStream_t stream) {
   const long long items = (long long)p.t[0].items + p.t[1].items + (kPages ? p.t[2].items : 0);
-  const long long blocks = (items + kRotaryWarps - 1) / kRotaryWarps, most = 4ll * sms;
+  const long long blocks = (items + kRotaryWarps - 1) / kRotaryWarps, most = (kNorm || kPairs == kHalvesOdd ? 2ll : 3ll) * sms;
   if (blocks == 0) return MALA_OK;
-  rotary_kernel<L, kPairs, kNorm, kPages><<<(unsigned)(blocks < most ? blocks : most), kRotaryThreads, 0, stream>>>(p);
+  rotary_kernel<L, kPairs, kNorm, kPages><<<(unsigned)(blocks < most ? blocks : most), kRotaryThreads, kRingBytes, stream>>>(p);
   return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 template <int L, bool kNorm, bool kPages>
@@ -402,16 +462,26 @@ static int launch_rotary(const RotaryParams& p, int interleaved, int sms, cudaSt
 template <int L>
 static int launch_norm_bwd_by(const RotaryParams& p, int interleaved, int blocks, cudaStream_t stream) {
   switch (pairs_kind(p.rule.rotary, interleaved)) {
-    case kHalves: rotary_norm_bwd_kernel<L, kHalves><<<blocks, kRotaryThreads, 0, stream>>>(p); break;
-    case kHalvesOdd: rotary_norm_bwd_kernel<L, kHalvesOdd><<<blocks, kRotaryThreads, 0, stream>>>(p); break;
-    default: rotary_norm_bwd_kernel<L, kNeighbours><<<blocks, kRotaryThreads, 0, stream>>>(p);
+    case kHalves: rotary_norm_bwd_kernel<L, kHalves><<<blocks, kRotaryThreads, kRingBytes, stream>>>(p); break;
+    case kHalvesOdd: rotary_norm_bwd_kernel<L, kHalvesOdd><<<blocks, kRotaryThreads, kRingBytes, stream>>>(p); break;
+    default: rotary_norm_bwd_kernel<L, kNeighbours><<<blocks, kRotaryThreads, kRingBytes, stream>>>(p);
   }
   return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
+template <int L, int kPairs>
+static bool set_attributes_of() {
+  auto ok = [](auto* kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes) == cudaSuccess; };
+  return ok(rotary_kernel<L, kPairs, true, true>) && ok(rotary_kernel<L, kPairs, true, false>) && ok(rotary_kernel<L, kPairs, false, true>) &&
+         ok(rotary_kernel<L, kPairs, false, false>) && ok(rotary_norm_bwd_kernel<L, kPairs>);
+}
+template <int L>
+static bool set_attributes_by() { return set_attributes_of<L, kHalves>() && set_attributes_of<L, kHalvesOdd>() && set_attributes_of<L, kNeighbours>(); }
+bool rotary_set_attributes() { return set_attributes_by<4>() && set_attributes_by<8>() && set_attributes_by<16>(); }
+
 static int launch_norm_bwd(RotaryParams& p, int interleaved, float* dwq, float* dwk, int sms, cudaStream_t stream) {
   const long long nq = (p.t[0].items + kRotaryWarps - 1) / kRotaryWarps, nk = (p.t[1].items + kRotaryWarps - 1) / kRotaryWarps;
-  const long long most = 4ll * sms < kNormBlocks ? 4ll * sms : kNormBlocks;
+  const long long most = 2ll * sms < kNormBlocks ? 2ll * sms : kNormBlocks;
   // the blocks in the share of the tensors' rows and heads
   const double loads_q = (double)p.t[0].rows * p.t[0].H, loads_k = (double)p.t[1].rows * p.t[1].H;
   long long gq = nq, gk = nk;

@@ -71,39 +71,43 @@ __device__ __forceinline__ float weight_at(const void* w, int fp32, int c) {
   return fp32 ? __ldg((const float*)w + c) : __bfloat162float(__ldg((const __nv_bfloat16*)w + c));
 }
 
-// A row of d columns in L lanes, two pieces of eight columns each: pieces whose columns are paired (halves), so that a pair lies in one lane, or
-// neighbouring pieces.
-template <int kPairs>
+// A row of d columns in L lanes, two pieces of eight columns each: pieces whose columns are paired (halves), so that a pair lies in one lane, else any two;
+// either way the first pieces of neighbouring lanes are neighbours, and so are the second ones.
+template <int L, int kPairs>
 struct LanePieces {
   int pa, pb;               // the pieces
   bool has_a, has_b, pair;  // whether the row has them; whether a's columns are paired with b's (halves)
-  int turns;                // neighbours: whether all eight pairs of columns are rotated (2), some (1) or none (0)
+  int turns;                // neighbours, kHalvesOdd: whether all of the lane's columns are rotated (2), some (1) or none (0)
   __device__ __forceinline__ void set(const RotaryRule& r, int c) {
-    const int turned = r.rotary / 16;
-    pair = kPairs == kHalves && c < turned;
-    pa = pair ? c : 2 * c;
-    pb = pair ? c + turned : 2 * c + 1;
-    has_a = 8 * pa < r.d;
-    has_b = 8 * pb < r.d;
-    turns = 16 * c + 16 <= r.rotary ? 2 : 16 * c < r.rotary ? 1 : 0;
+    const int turned = kPairs == kHalves ? r.rotary / 16 : 0, pieces = r.d / 8;
+    pair = c < turned;
+    const int rest = pieces - 2 * turned, near = kPairs == kHalves ? (rest + 1) / 2 : L;   // (without pairs: a whole number of lanes)
+    pa = pair ? c : turned + c;
+    pb = pair ? c + turned : turned + c + near;
+    has_a = pair || (c - turned < near && pa < pieces);
+    has_b = pair || (c - turned < near && pb < pieces);
+    turns = 8 * pa + 8 <= r.rotary && (8 * pb + 8 <= r.rotary || !has_b) ? 2 : 8 * pa < r.rotary ? 1 : 0;
   }
+  // column of the lane's e-th place of 16
+  __device__ __forceinline__ int col(int e) const { return e < 8 ? 8 * pa + e : 8 * pb + e - 8; }
 };
 
-// cos and sin (with magnitude and sense) of the angles of lane c of a row at one position: kAngles of them, of the pairs 8 c + e, or (kHalvesOdd) of the
-// columns 16 c + e; where nothing is rotated 1 and 0.  All 32 / L rows of the warp are at this position, so each lane works out its share of the angles and gets
+// cos and sin (with magnitude and sense) of a lane's angles at one position: halves, of the pairs 8 pa + e; neighbours, of four pairs of either piece; kHalvesOdd, of its
+// 16 columns; where nothing is rotated 1 and 0.  All 32 / L rows of the warp are at this position, so each lane works out its share of the angles and gets
 // the others by shuffles.
 template <int kPairs>
 constexpr int kAngles = kPairs == kHalvesOdd ? 16 : 8;
 template <int L, int kPairs>
-__device__ __forceinline__ void angles_at(const RotaryRule& r, const uint64_t* turns, int c, int g, int pos, float (&C)[kAngles<kPairs>], float (&S)[kAngles<kPairs>]) {
+__device__ __forceinline__ void angles_at(const RotaryRule& r, const uint64_t* turns, const LanePieces<L, kPairs>& l, int c, int g, int pos, float (&C)[kAngles<kPairs>], float (&S)[kAngles<kPairs>]) {
   constexpr int kShare = kAngles<kPairs> * L / 32;
   static_assert(kShare >= 1, "a lane has an angle at least");
   const int half = r.rotary / 2;
   float cs[kShare], sn[kShare];
 #pragma unroll
   for (int j = 0; j < kShare; ++j) {
-    const int x = kAngles<kPairs> * c + g * kShare + j;
-    const bool on = x < (kPairs == kHalvesOdd ? r.rotary : half);
+    const int e = g * kShare + j;
+    const int x = kPairs == kHalvesOdd ? l.col(e) : kPairs == kNeighbours ? (e < 4 ? 4 * l.pa + e : 4 * l.pb + e - 4) : 8 * l.pa + e;
+    const bool on = kPairs == kHalvesOdd ? x < r.rotary : kPairs == kNeighbours ? x < half : l.pair;
     cos_sin(turns[!on ? 0 : kPairs == kHalvesOdd && x >= half ? x - half : x], pos, cs[j], sn[j]);
     cs[j] = on ? cs[j] * r.magnitude : 1.f;
     sn[j] = on ? sn[j] * (kPairs == kHalvesOdd && x < half ? -r.turned : r.turned) : 0.f;
@@ -118,16 +122,16 @@ __device__ __forceinline__ void angles_at(const RotaryRule& r, const uint64_t* t
 
 // What a lane multiplies with, two columns at a time: halves  a <- a C - b S', b <- b C' + a S  (C, C' and S, S' differ by a norm's weights only); neighbours
 // pair by pair  x <- x C - y S', y <- y C' + x S;  kHalvesOdd: column by column  x <- x C + partner S.
-template <int kPairs>
+template <int L, int kPairs>
 struct LaneFactors {
   uint64_t ca[4], cb[4], sa[4], sb[4];     // C, C', S, -S'  (kHalvesOdd: C of a and b, S of a and b)
   template <bool kNorm>
-  __device__ __forceinline__ void set(const RotaryRule& r, int c, const LanePieces<kPairs>& l, const float (&C)[kAngles<kPairs>], const float (&S)[kAngles<kPairs>],
+  __device__ __forceinline__ void set(const RotaryRule& r, const LanePieces<L, kPairs>& l, const float (&C)[kAngles<kPairs>], const float (&S)[kAngles<kPairs>],
                                       const void* weight, int fp32) {
     float w[16], v[16];                    // weights of the lane's columns and (kHalvesOdd) of their partners
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int col = kNorm ? min(8 * (e < 8 ? l.pa : l.pb) + e % 8, r.d - 1) : 0;
+      const int col = kNorm ? min(l.col(e), r.d - 1) : 0;
       w[e] = kNorm ? weight_at(weight, fp32, col) : 1.f;
       v[e] = kNorm && kPairs == kHalvesOdd ? weight_at(weight, fp32, partner_of<kPairs>(col, r.rotary)) : 1.f;
     }
@@ -160,10 +164,14 @@ __device__ __forceinline__ uint64_t crossed(uint64_t x) {
   return f2(b, a);
 }
 
-// A lane's two pieces rotated (and multiplied by the norm's weights).  kHalvesOdd: the row lies in shared memory at `row`, its columns in order.  What is not rotated is
+template <int L>
+__device__ __forceinline__ int staged(int col) { return (col / 8 < L ? col / 8 : col / 8 - L + 32) * 8 + col % 8; }
+
+// A lane's two pieces rotated (and multiplied by the norm's weights).  kHalvesOdd: the row lies in shared memory at `row`, its first L pieces side by side
+// and the others 512 bytes behind them.  What is not rotated is
 // multiplied by its weight alone, whatever stands beside it.
-template <int kPairs, bool kNorm>
-__device__ __forceinline__ void rotate_pieces(const RotaryRule& r, int c, const LanePieces<kPairs>& l, const LaneFactors<kPairs>& f, const __nv_bfloat16* row, uint64_t (&a)[4],
+template <int L, int kPairs, bool kNorm>
+__device__ __forceinline__ void rotate_pieces(const RotaryRule& r, const LanePieces<L, kPairs>& l, const LaneFactors<L, kPairs>& f, const __nv_bfloat16* row, uint64_t (&a)[4],
                                               uint64_t (&b)[4]) {
   if constexpr (kPairs == kHalves) {
     if (l.pair) {
@@ -188,8 +196,8 @@ __device__ __forceinline__ void rotate_pieces(const RotaryRule& r, int c, const 
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint64_t x = f2_mul(a[j], f.ca[j]), y = f2_mul(b[j], f.cb[j]);
-        a[j] = 16 * c + 2 * j < r.rotary ? f2_fma(crossed(a[j]), f.sa[j], x) : x;
-        b[j] = 16 * c + 8 + 2 * j < r.rotary ? f2_fma(crossed(b[j]), f.sb[j], y) : y;
+        a[j] = 8 * l.pa + 2 * j < r.rotary ? f2_fma(crossed(a[j]), f.sa[j], x) : x;
+        b[j] = 8 * l.pb + 2 * j < r.rotary ? f2_fma(crossed(b[j]), f.sb[j], y) : y;
       }
       return;
     }
@@ -197,14 +205,14 @@ __device__ __forceinline__ void rotate_pieces(const RotaryRule& r, int c, const 
     if (l.turns > 0) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int col = 16 * c + e;
+        const int col = l.col(e);
         uint64_t& x2 = e < 8 ? a[e / 2] : b[e / 2 - 4];
         float x[2], k[2], s[2];
         f2_get(x2, x[0], x[1]);
         f2_get(e < 8 ? f.ca[e / 2] : f.cb[e / 2 - 4], k[0], k[1]);
         f2_get(e < 8 ? f.sa[e / 2] : f.sb[e / 2 - 4], s[0], s[1]);
         x[e % 2] *= k[e % 2];
-        if (col < r.rotary) x[e % 2] = fmaf(__bfloat162float(row[partner_of<kPairs>(col, r.rotary)]), s[e % 2], x[e % 2]);
+        if (col < r.rotary) x[e % 2] = fmaf(__bfloat162float(row[staged<L>(partner_of<kPairs>(col, r.rotary))]), s[e % 2], x[e % 2]);
         x2 = f2(x[0], x[1]);
       }
       return;

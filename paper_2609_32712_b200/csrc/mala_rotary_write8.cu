@@ -48,11 +48,11 @@ rotary_write8_kernel(const RotaryWriteParams p) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int lanes = p.lanes, c = tid & (lanes - 1), r0 = tid / lanes, step = kWriteThreads / lanes, window = min(kWriteRows, kPer * step);
   const int t0 = blockIdx.x * p.chunk, t1 = min(t0 + p.chunk, p.rows), h0 = blockIdx.y * p.heads, h1 = min(h0 + p.heads, p.Hkv);
-  // this thread's pieces: columns 8 pa .. and 8 pb ..
-  const int pieces = p.d / 8, turned = p.rule.rotary / 16;          // (halves: lanes whose pieces are partners)
-  const bool pair = kPairs == kHalves && c < turned;
-  const int pa = pair ? c : 2 * c, pb = pair ? c + turned : 2 * c + 1;
-  const bool mine = 2 * c < pieces;
+  // this thread's pieces: columns 8 pa .. and 8 pb .., and partners (halves) or any two, neighbouring threads' side by side
+  const int pieces = p.d / 8, turned = kPairs == kHalves ? p.rule.rotary / 16 : 0;
+  const bool pair = c < turned, mine = 2 * c < pieces;
+  const int pa = pair ? c : turned + c, pb = pair ? c + turned : pa + (pieces - 2 * turned) / 2;
+  auto col_of = [&](int e) -> int { return e < 8 ? 8 * pa + e : 8 * pb + e - 8; };
   const uint8_t* const src = (is_v ? p.v : p.k);
   const int64_t s_sn = is_v ? p.v_sn : p.k_sn, s_sh = is_v ? p.v_sh : p.k_sh;
   uint8_t* const pages = is_v ? p.vp : p.kp;
@@ -159,8 +159,8 @@ rotary_write8_kernel(const RotaryWriteParams p) {
       for (int i = 0; i < kPer; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int x = 8 * c + e;
-          const bool on = x < p.rule.rotary / 2;
+          const int x = kPairs == kHalves ? 8 * c + e : e < 4 ? 4 * pa + e : 4 * pb + e - 4;
+          const bool on = mine && x < p.rule.rotary / 2;
           cos_sin(turns_s[on ? x : 0], (int)pos[i], C[i][e], S[i][e]);
           C[i][e] = on ? C[i][e] * p.rule.magnitude : 1.f;
           S[i][e] = on ? S[i][e] * p.rule.turned : 0.f;
@@ -202,20 +202,23 @@ rotary_write8_kernel(const RotaryWriteParams p) {
           odd_s[2 * tid] = ra[i];
           odd_s[2 * tid + 1] = rb[i];
           __syncwarp();
-          const __nv_bfloat16* row = reinterpret_cast<const __nv_bfloat16*>(odd_s + 2 * (tid - c));
+          auto staged = [&](int x) -> float {
+            const int q = x / 8, of = q < pieces / 2 ? 2 * q : 2 * q - pieces + 1;
+            return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(odd_s + 2 * (tid - c) + of)[x % 8]);
+          };
           float sum = f2_sum(f2_fma(a[i][0], a[i][0], f2_fma(a[i][1], a[i][1], f2_fma(a[i][2], a[i][2], f2_mul(a[i][3], a[i][3]))))) +
                       f2_sum(f2_fma(b[i][0], b[i][0], f2_fma(b[i][1], b[i][1], f2_fma(b[i][2], b[i][2], f2_mul(b[i][3], b[i][3])))));
           for (int m = lanes / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(kAll, sum, m);
           const float r = p.normed ? rsqrtf(fmaf(sum, p.inv_d, p.eps)) : 1.f;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int col = mine ? 16 * c + e : 0, half = p.rule.rotary / 2;
-            float x = __bfloat162float(row[col]) * r * weight_s[col];
+            const int col = mine ? col_of(e) : 0, half = p.rule.rotary / 2;
+            float x = staged(col) * r * weight_s[col];
             if (col < p.rule.rotary) {
               const int other = partner_of<kHalvesOdd>(col, p.rule.rotary);
               float cs, sn;
               cos_sin(turns_s[col < half ? col : col - half], (int)pos[i], cs, sn);
-              const float y = __bfloat162float(row[other]) * r * weight_s[other];
+              const float y = staged(other) * r * weight_s[other];
               x = fmaf(y, (col < half ? -sn : sn) * p.rule.turned, x * (cs * p.rule.magnitude));
             }
             x = mine ? x : 0.f;
@@ -255,7 +258,7 @@ rotary_write8_kernel(const RotaryWriteParams p) {
                 b[i][j] = f2_fma(x, sn, f2_mul(b[i][j], cs));
               }
             }
-          } else {                         // pairs 8 c .. 8 c + 3 in a, the next four in b
+          } else {                         // four pairs in a, four in b
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               uint64_t& x = e < 4 ? a[i][e] : b[i][e - 4];
