@@ -31,6 +31,7 @@ struct RotaryParams {
   const int* positions; int pos_n;         // [B, pos_n], or null: a row's own index
   const int* cu_q; const int* cu_k; int B; // packed sequences
   const int64_t* slots; int64_t limit; int page_size; FastDiv by_page;   // into pages
+  int tensors, joint;                      // joint: an item is a row of all tensors (whose rows are the same tokens)
   int weights_fp32; float eps, inv_d;
   float* partial;                          // the norm's backward: [blocks, d] sums
   int q_blocks;
@@ -39,34 +40,47 @@ struct RotaryParams {
 // Positions of the rows of one tensor after another
 struct Positions {
   int which = -1, from = 0, to = 0, shift = 0;   // packed: the rows of the sequence found last, and what a row's position has more than its number
-  // position of row t (n of batch entry b) of tensor w; false: no sequence has it
-  __device__ __forceinline__ bool of(const RotaryParams& p, const RotaryTensor& a, int w, int t, int b, int n, int& pos) {
+  // position of row t (n of batch entry b) of tensor w; false: no sequence has it.  cu_q, cu_k: the offsets, in shared memory where they fit
+  __device__ __forceinline__ bool of(const RotaryParams& p, const int* cu_q, const int* cu_k, int w, int t, int b, int n, int& pos) {
     if (p.cu_q) {
       if (w != which || t < from || t >= to) {
-        const int* own = w == 0 ? p.cu_q : p.cu_k;
-        if (t < __ldg(own) || t >= __ldg(own + p.B)) return false;
+        const int* own = w == 0 ? cu_q : cu_k;
+        if (t < own[0] || t >= own[p.B]) return false;
         int lo = 0, hi = p.B;
         while (hi - lo > 1) {              // the last sequence that begins at or before t
           const int mid = (lo + hi) >> 1;
-          if (__ldg(own + mid) <= t) lo = mid;
+          if (own[mid] <= t) lo = mid;
           else hi = mid;
         }
         which = w;
-        from = __ldg(own + lo);
-        to = __ldg(own + lo + 1);
+        from = own[lo];
+        to = own[lo + 1];
         shift = -from;
-        if (w == 0) shift += (__ldg(p.cu_k + lo + 1) - __ldg(p.cu_k + lo)) - (to - from);
+        if (w == 0) shift += (cu_k[lo + 1] - cu_k[lo]) - (to - from);
       }
       pos = t + shift;
       return true;
     }
-    pos = n + a.first;
+    pos = n + p.t[w].first;
     if (p.positions) pos = __ldg(p.positions + (int64_t)b * p.pos_n + pos);
     return true;
   }
 };
 
-// A row's address, heads and place among a tensor's, item by item: a row and `span` of its heads
+constexpr int kCuShared = 512;             // offsets of packed sequences that fit into shared memory
+__device__ __forceinline__ void load_offsets(const RotaryParams& p, int* to, const int*& cu_q, const int*& cu_k) {
+  cu_q = p.cu_q;
+  cu_k = p.cu_k;
+  if (!p.cu_q || p.B >= kCuShared) return;
+  for (int x = threadIdx.x; x <= p.B; x += kRotaryThreads) {
+    to[x] = __ldg(p.cu_q + x);
+    to[kCuShared + x] = __ldg(p.cu_k + x);
+  }
+  cu_q = to;
+  cu_k = to + kCuShared;
+}
+
+// A row's address, heads and place among a tensor's, item by item: a row and `span` of its heads, or (joint) a row of all tensors, of which this is the first
 struct Item {
   int which, t, b, n, h0, h1;
   __device__ __forceinline__ void at(const RotaryParams& p, uint32_t nq, uint32_t nk, uint32_t item) {
@@ -78,6 +92,12 @@ struct Item {
     h1 = min(h0 + a.span, a.H);
     b = (int)a.by_n.div((uint32_t)t);
     n = t - b * a.N;
+  }
+  // joint: the same row of the next tensor; false: there is none
+  __device__ __forceinline__ bool more(const RotaryParams& p) {
+    if (!p.joint || which + 1 == p.tensors) return false;
+    h1 = p.t[++which].H;
+    return true;
   }
 };
 
@@ -103,13 +123,15 @@ struct Rows {
   const uint8_t *x, *g;     // this lane's first piece of the next batch
   int64_t x_step, g_step;
   int to_b;                 // from a lane's first piece to its second one
+  Item it;
   __device__ __forceinline__ void item(const RotaryParams& p, const LanePieces<L, kPairs>& l, int group) {
-    batches = 0;
-    left = 0;
-    if (next >= end) return;
-    Item it;
-    it.at(p, nq, nk, (uint32_t)next);
-    next += stride;
+    if (!it.more(p)) {
+      batches = 0;
+      left = 0;
+      if (next >= end) return;
+      it.at(p, nq, nk, (uint32_t)next);
+      next += stride;
+    }
     const RotaryTensor& a = p.t[it.which];
     x = a.x + it.b * a.x_sb + it.n * a.x_sn + (it.h0 + group) * a.x_sh + l.pa * 16;
     x_step = P * a.x_sh;
@@ -144,6 +166,7 @@ struct Rows {
     next = first; end = end_; stride = stride_; nq = nq_; nk = nk_;
     x = g = nullptr; x_step = g_step = 0;
     to_b = (l.pb - l.pa) * 16;
+    it.which = p.tensors - 1;                            // (an item's last)
 #pragma unroll
     for (int i = 0; i < kDepth; ++i) {
       if (!l.has_a) ring[i * kPlace] = make_uint4(0u, 0u, 0u, 0u);
@@ -174,6 +197,8 @@ rotary_kernel(const RotaryParams p) {
   constexpr int P = 32 / L;
   extern __shared__ uint4 ring_s[];
   __shared__ uint64_t turns_s[kMaxPairs];
+  __shared__ int cu_s[2 * kCuShared];
+  __shared__ __align__(16) float weight_s[kNorm ? 512 : 4];   // q's, k's
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, c = lane % L;
   LanePieces<L, kPairs> l;
   l.set(p.rule, c);
@@ -181,63 +206,76 @@ rotary_kernel(const RotaryParams p) {
   const uint32_t stride = gridDim.x * kRotaryWarps, first = blockIdx.x * kRotaryWarps + warp;
   Rows<L, kPairs, false> rows;
   rows.begin(p, l, g, ring_s + warp * 512 + lane, first, all, stride, nq, nk);
+  const int *cu_q, *cu_k;
   load_turns(p.rule, turns_s);
+  load_offsets(p, cu_s, cu_q, cu_k);
+  if constexpr (kNorm)
+    for (int x = threadIdx.x; x < p.rule.d; x += kRotaryThreads) {
+      weight_s[x] = weight_at(p.t[0].weight, p.weights_fp32, x);
+      weight_s[256 + x] = weight_at(p.t[1].weight, p.weights_fp32, x);
+    }
   __syncthreads();
   Positions positions;
   for (uint64_t x = first; x < all; x += stride) {
     Item it;
     it.at(p, nq, nk, (uint32_t)x);
-    const RotaryTensor& a = p.t[it.which];
-    uint8_t* dst = a.y;
-    bool place = true;
-    if (kPages && it.which > 0) {
-      const int64_t slot = __ldg(p.slots + it.t);
-      place = slot >= 0 && slot < p.limit;
-      const int64_t page = p.limit <= 0xffffffffll ? (int64_t)p.by_page.div((uint32_t)slot) : slot / p.page_size;
-      dst += page * a.y_sb + (slot - page * p.page_size) * a.y_sn;
-    } else {
-      dst += it.b * a.y_sb + it.n * a.y_sn;
-    }
-    int pos = 0;
-    const bool turn = it.which < 2 && positions.of(p, a, it.which, it.t, it.b, it.n, pos);
+    bool place = true, turn = false;
+    float C[kAngles<kPairs>], S[kAngles<kPairs>];
     LaneFactors<L, kPairs> f;
-    if (turn) {
-      float C[kAngles<kPairs>], S[kAngles<kPairs>];
-      angles_at<L, kPairs>(p.rule, turns_s, l, c, g, pos, C, S);
-      f.template set<kNorm>(p.rule, l, C, S, a.weight, p.weights_fp32);
+    if (it.which < 2) {
+      int pos = 0;
+      turn = positions.of(p, cu_q, cu_k, it.which, it.t, it.b, it.n, pos);   // (else: a row that no sequence has)
+      if (turn) {
+        angles_at<L, kPairs>(p.rule, turns_s, l, c, g, pos, C, S);
+        if constexpr (!kNorm) f.template set<false>(p.rule, l, C, S, nullptr);   // (with a norm: for each tensor, with its weights)
+      }
     }
-    uint8_t* to = dst + (it.h0 + g) * a.y_sh + l.pa * 16;
-    const int64_t y_step = P * a.y_sh;
-    for (int h = it.h0 + g, hb = it.h0; hb < it.h1; hb += P, h += P, to += y_step) {
-      const uint4* const at = rows.take(p, l, g);
-      uint4 wa = at[0], wb = at[32];
-      if (turn) {                          // (not: values, and rows that no sequence has)
-        uint64_t xa[4], xb[4];
-        pairs_of(wa, xa);
-        pairs_of(wb, xb);
-        float sum = 0.f;
-        if constexpr (kNorm) {
-          sum = squares(xa, xb);
+    do {
+      const RotaryTensor& a = p.t[it.which];
+      uint8_t* to = a.y + (it.h0 + g) * a.y_sh + l.pa * 16;
+      if (kPages && it.which > 0) {
+        const int64_t slot = __ldg(p.slots + it.t);
+        place = slot >= 0 && slot < p.limit;
+        const int64_t page = p.limit <= 0xffffffffll ? (int64_t)p.by_page.div((uint32_t)slot) : slot / p.page_size;
+        to += page * a.y_sb + (slot - page * p.page_size) * a.y_sn;
+      } else {
+        to += it.b * a.y_sb + it.n * a.y_sn;
+      }
+      const bool turn_this = turn && it.which < 2;         // (not: values)
+      if constexpr (kNorm)
+        if (turn_this) f.template set<true>(p.rule, l, C, S, weight_s + it.which * 256);
+      const int64_t y_step = P * a.y_sh;
+      for (int h = it.h0 + g, hb = it.h0; hb < it.h1; hb += P, h += P, to += y_step) {
+        const uint4* const at = rows.take(p, l, g);
+        uint4 wa = at[0], wb = at[32];
+        if (turn_this) {
+          uint64_t xa[4], xb[4];
+          pairs_of(wa, xa);
+          pairs_of(wb, xb);
+          float sum = 0.f;
+          if constexpr (kNorm) {
+            sum = squares(xa, xb);
 #pragma unroll
-          for (int m = L / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-        }
-        rotate_pieces<L, kPairs, kNorm>(p.rule, l, f, reinterpret_cast<const __nv_bfloat16*>(at - c), xa, xb);
-        if constexpr (kNorm) {
-          const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            xa[j] = f2_mul(xa[j], f2(r, r));
-            xb[j] = f2_mul(xb[j], f2(r, r));
+            for (int m = L / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
           }
+          rotate_pieces<L, kPairs, kNorm>(p.rule, l, f, reinterpret_cast<const __nv_bfloat16*>(at - c), xa, xb);
+          if constexpr (kNorm) {
+            const float r = rsqrtf(fmaf(sum, p.inv_d, p.eps));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              xa[j] = f2_mul(xa[j], f2(r, r));
+              xb[j] = f2_mul(xb[j], f2(r, r));
+            }
+          }
+          wa = rows_of(xa);
+          wb = rows_of(xb);
         }
-        wa = rows_of(xa);
-        wb = rows_of(xb);
+        if (h < it.h1 && place) {
+          if (l.has_a) *reinterpret_cast<uint4*>(to) = wa;
+          if (l.has_b) *reinterpret_cast<uint4*>(to + rows.to_b) = wb;
+        }
       }
-      if (h < it.h1 && place) {
-        if (l.has_a) *reinterpret_cast<uint4*>(to) = wa;
-        if (l.has_b) *reinterpret_cast<uint4*>(to + rows.to_b) = wb;
-      }
-    }
+    } while (it.more(p));
   }
 }
 
@@ -251,6 +289,7 @@ rotary_norm_bwd_kernel(const RotaryParams p) {
   constexpr uint32_t kAll = 0xffffffffu;
   extern __shared__ uint4 ring_s[];
   __shared__ uint64_t turns_s[kMaxPairs];
+  __shared__ int cu_s[2 * kCuShared];
   __shared__ __align__(16) float weight_s[256];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, c = lane % L;
   const int which = (int)blockIdx.x < p.q_blocks ? 0 : 1, block = blockIdx.x - (which ? p.q_blocks : 0);
@@ -261,7 +300,9 @@ rotary_norm_bwd_kernel(const RotaryParams p) {
   const uint32_t nq = p.t[0].items, before = which ? nq : 0, stride = blocks * kRotaryWarps, first = before + block * kRotaryWarps + warp, end = before + a.items;
   Rows<L, kPairs, true> rows;
   rows.begin(p, l, g, ring_s + warp * 512 + lane, first, end, stride, nq, p.t[1].items);
+  const int *cu_q, *cu_k;
   load_turns(p.rule, turns_s);
+  load_offsets(p, cu_s, cu_q, cu_k);
   for (int x = threadIdx.x; x < p.rule.d; x += kRotaryThreads) weight_s[x] = weight_at(a.weight, p.weights_fp32, x);
   __syncthreads();
   uint64_t dw[8] = {0, 0, 0, 0, 0, 0, 0, 0};   // of the columns of a, and of b
@@ -273,12 +314,12 @@ rotary_norm_bwd_kernel(const RotaryParams p) {
     it.at(p, nq, p.t[1].items, (uint32_t)x);
     uint8_t* const dst = a.y + it.b * a.y_sb + it.n * a.y_sn;
     int pos = 0;
-    const bool turn = positions.of(p, a, which, it.t, it.b, it.n, pos);
+    const bool turn = positions.of(p, cu_q, cu_k, which, it.t, it.b, it.n, pos);
     LaneFactors<L, kPairs> f;
     if (turn) {
       float C[kAngles<kPairs>], S[kAngles<kPairs>];
       angles_at<L, kPairs>(p.rule, turns_s, l, c, g, pos, C, S);
-      f.template set<false>(p.rule, l, C, S, nullptr, 0);
+      f.template set<false>(p.rule, l, C, S, nullptr);
     }
     uint8_t* to = dst + (it.h0 + g) * a.y_sh + l.pa * 16;
     const int64_t y_step = P * a.y_sh;
@@ -420,8 +461,12 @@ static void set_tensor(RotaryTensor* t, mala_tin x, mala_tout y, int B, int N, i
 
 static int lanes_of(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
 
-// Heads per item: all of a row's while that leaves every SM 32 warps, fewer where there are few rows (one load of a warp at least)
-static void set_items(RotaryParams* p, int tensors, int sms) {
+// Heads per item: all of a row's while that leaves every SM 32 warps, fewer where there are few rows (one load of a warp at least).  Where every row
+// is whole and the tensors' rows are the same tokens, an item is a row of all of them, so that the angles are worked out once (`same`; the
+// backward pass with a norm keeps q and k apart).
+static void set_items(RotaryParams* p, int tensors, int sms, bool same) {
+  p->tensors = tensors;
+  p->joint = same ? 1 : 0;
   const int per = 32 / lanes_of(p->rule.d);
   long long loads = 0;
   for (int x = 0; x < tensors; ++x) loads += (long long)p->t[x].rows * ((p->t[x].H + per - 1) / per);
@@ -433,7 +478,9 @@ static void set_items(RotaryParams* p, int tensors, int sms) {
     const int spans = t.H > 0 ? (t.H + t.span - 1) / t.span : 1;
     t.by_spans.set((uint32_t)spans);
     t.items = t.rows * spans;
+    if (spans > 1) p->joint = 0;
   }
+  for (int x = 1; x < tensors && p->joint; ++x) p->t[x].items = 0;
 }
 
 template <int L, int kPairs, bool kNorm, bool kPages>
@@ -536,7 +583,8 @@ static int rotate(const RotaryCall& c, mala_tin q, mala_tin k, mala_tout qo, mal
   if (with_k) set_tensor(&p.t[1], k, ko, c.B, c.Nk, c.Hkv, 0);
   p.positions = c.positions; p.pos_n = c.Nk;
   p.cu_q = c.cu_q; p.cu_k = c.cu_k; p.B = c.sequences;
-  set_items(&p, with_k ? 2 : 1, sm_count(dev));
+  // (offsets given once for both: the same rows of q and k)
+  set_items(&p, with_k ? 2 : 1, sm_count(dev), with_k && c.Nq == c.Nk && c.cu_q == c.cu_k);
   return norm ? launch_rotary<true, false>(p, r->interleaved, sm_count(dev), stream) : launch_rotary<false, false>(p, r->interleaved, sm_count(dev), stream);
 }
 
@@ -580,7 +628,7 @@ static int rotate_back(const RotaryCall& c, mala_tin dq, mala_tin dk, mala_tin q
   p.positions = c.positions; p.pos_n = c.Nk;
   p.cu_q = c.cu_q; p.cu_k = c.cu_k; p.B = c.sequences;
   p.partial = (float*)ws;
-  set_items(&p, with_k ? 2 : 1, sm_count(dev));
+  set_items(&p, with_k ? 2 : 1, sm_count(dev), false);
   return launch_norm_bwd(p, r->interleaved, dwq, dwk, sm_count(dev), stream);
 }
 
@@ -666,7 +714,7 @@ int mala_rotary_write(mala_tin q, mala_tin k, mala_tin v, const int32_t* positio
   set_tensor(&p.t[2], v, vpages, 1, rows, Hkv, 0);
   p.slots = slots; p.limit = (int64_t)num_pages * page_size; p.page_size = page_size; p.by_page.set((uint32_t)page_size);
   p.positions = positions; p.pos_n = rows;
-  set_items(&p, 3, sm_count(dev));
+  set_items(&p, 3, sm_count(dev), true);
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   return scope.finish(norm ? launch_rotary<true, true>(p, rotary->interleaved, sm_count(dev), stream)
                            : launch_rotary<false, true>(p, rotary->interleaved, sm_count(dev), stream));

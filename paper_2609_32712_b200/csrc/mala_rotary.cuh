@@ -125,15 +125,24 @@ __device__ __forceinline__ void angles_at(const RotaryRule& r, const uint64_t* t
 template <int L, int kPairs>
 struct LaneFactors {
   uint64_t ca[4], cb[4], sa[4], sb[4];     // C, C', S, -S'  (kHalvesOdd: C of a and b, S of a and b)
+  // weights: of the row's columns, in shared memory
   template <bool kNorm>
   __device__ __forceinline__ void set(const RotaryRule& r, const LanePieces<L, kPairs>& l, const float (&C)[kAngles<kPairs>], const float (&S)[kAngles<kPairs>],
-                                      const void* weight, int fp32) {
+                                      const float* weights) {
     float w[16], v[16];                    // weights of the lane's columns and (kHalvesOdd) of their partners
+    if constexpr (kNorm) {
+      const float4* const wa = reinterpret_cast<const float4*>(weights + (l.has_a ? 8 * l.pa : 0));
+      const float4* const wb = reinterpret_cast<const float4*>(weights + (l.has_b ? 8 * l.pb : 0));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 x = j < 2 ? wa[j] : wb[j - 2];
+        w[4 * j] = x.x; w[4 * j + 1] = x.y; w[4 * j + 2] = x.z; w[4 * j + 3] = x.w;
+      }
+    }
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int col = kNorm ? min(l.col(e), r.d - 1) : 0;
-      w[e] = kNorm ? weight_at(weight, fp32, col) : 1.f;
-      v[e] = kNorm && kPairs == kHalvesOdd ? weight_at(weight, fp32, partner_of<kPairs>(col, r.rotary)) : 1.f;
+      if constexpr (!kNorm) w[e] = 1.f;
+      v[e] = kNorm && kPairs == kHalvesOdd ? weights[partner_of<kPairs>(min(l.col(e), r.d - 1), r.rotary)] : 1.f;
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
