@@ -192,7 +192,7 @@ constexpr int kRingBytes = kRotaryWarps * 8192;
 // Rotations.  A row lies in the registers of L lanes, and a warp works on 32 / L heads of a token at a time: the angles of a token are worked out once for
 // all heads that a warp takes, and a warp's tokens are neighbours.
 template <int L, int kPairs, bool kNorm, bool kPages>
-__global__ void __launch_bounds__(kRotaryThreads, kNorm || kPairs == kHalvesOdd ? 2 : 3)
+__global__ void __launch_bounds__(kRotaryThreads, 2)
 rotary_kernel(const RotaryParams p) {
   constexpr int P = 32 / L;
   extern __shared__ uint4 ring_s[];
@@ -486,7 +486,7 @@ static void set_items(RotaryParams* p, int tensors, int sms, bool same) {
 template <int L, int kPairs, bool kNorm, bool kPages>
 static int launch_rotary_as(const RotaryParams& p, int sms, cudaStream_t stream) {
   const long long items = (long long)p.t[0].items + p.t[1].items + (kPages ? p.t[2].items : 0);
-  const long long blocks = (items + kRotaryWarps - 1) / kRotaryWarps, most = (kNorm || kPairs == kHalvesOdd ? 2ll : 3ll) * sms;
+  const long long blocks = (items + kRotaryWarps - 1) / kRotaryWarps, most = 2ll * sms;
   if (blocks == 0) return MALA_OK;
   rotary_kernel<L, kPairs, kNorm, kPages><<<(unsigned)(blocks < most ? blocks : most), kRotaryThreads, kRingBytes, stream>>>(p);
   return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;

@@ -12,7 +12,7 @@
 
 namespace mala {
 
-constexpr int kWriteThreads = 512, kWriteRows = 128;   // threads of a block; most rows that it has at once (a unit's)
+constexpr int kWriteRows = 128;            // most rows that a block has at once (a unit's)
 
 struct RotaryWriteParams {
   const uint8_t* k; const uint8_t* v;      // [rows, Hkv, d] bf16
@@ -35,18 +35,19 @@ struct RotaryWriteParams {
 // them, and the next head's rows are on their way meanwhile.  A row's lanes have two pieces of eight columns each: columns and their
 // partners (halves), or neighbouring pieces.  Between maxima and codes of a head the block meets once; the units' maxima
 // change places among three buffers, so that one is emptied while two are in use.
-template <int kPairs, int kPer>            // kPer: rows of a thread
-__global__ void __launch_bounds__(kWriteThreads, 1)
+template <int kPairs, int kPer, int kThreads>   // kPer: rows of a thread
+__global__ void __launch_bounds__(kThreads, 512 / kThreads)
 rotary_write8_kernel(const RotaryWriteParams p) {
   constexpr uint32_t kAll = 0xffffffffu;
   __shared__ uint64_t turns_s[kMaxPairs];
   __shared__ int64_t slot_s[kWriteRows];
-  __shared__ uint32_t ends_s[kWriteRows / 32], valid_s[kWriteRows / 32];
+  constexpr int kWords = kWriteRows / 32;
+  __shared__ uint32_t ends_s[kWords], valid_s[kWords], taken_s[kWords], stop_s[kWords], held_s[kWords], grown_s[kWords];   // a bit per row of the window
   __shared__ float max_s[3][kWriteRows], old_s[2][kWriteRows], weight_s[128];
-  __shared__ uint4 odd_s[kPairs == kHalvesOdd ? kWriteThreads * 2 : 1];
+  __shared__ uint4 odd_s[kPairs == kHalvesOdd ? kThreads * 2 : 1];
   const bool is_v = blockIdx.z != 0;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int lanes = p.lanes, c = tid & (lanes - 1), r0 = tid / lanes, step = kWriteThreads / lanes, window = min(kWriteRows, kPer * step);
+  const int lanes = p.lanes, c = tid & (lanes - 1), r0 = tid / lanes, step = kThreads / lanes, window = min(kWriteRows, kPer * step);
   const int t0 = blockIdx.x * p.chunk, t1 = min(t0 + p.chunk, p.rows), h0 = blockIdx.y * p.heads, h1 = min(h0 + p.heads, p.Hkv);
   // this thread's pieces: columns 8 pa .. and 8 pb .., and partners (halves) or any two, neighbouring threads' side by side
   const int pieces = p.d / 8, turned = kPairs == kHalves ? p.rule.rotary / 16 : 0;
@@ -60,7 +61,7 @@ rotary_write8_kernel(const RotaryWriteParams p) {
   float* const scales = is_v ? p.vscale : p.kscale;
   if (!is_v) {
     load_turns(p.rule, turns_s);
-    for (int x = tid; x < p.d; x += kWriteThreads) weight_s[x] = p.weighted ? weight_at(p.weight, p.weights_fp32, x) : 1.f;
+    for (int x = tid; x < p.d; x += kThreads) weight_s[x] = p.weighted ? weight_at(p.weight, p.weights_fp32, x) : 1.f;
   }
   auto page_of = [&](int64_t slot, int64_t& at) -> int64_t {
     const int64_t page = p.limit <= 0xffffffffll ? (int64_t)p.by_page.div((uint32_t)slot) : slot / p.page_size;
@@ -85,31 +86,29 @@ rotary_write8_kernel(const RotaryWriteParams p) {
     }
     __syncthreads();
     const int words = window / 32;
-    // first row at or behind j with a bit (window: none)
-    auto next_end = [&](int j) -> int {
+    auto first_of = [&](const uint32_t* bits, int j) -> int {   // first row at or behind j with a bit (window: none)
       for (int w = j >> 5; w < words; ++w) {
-        const uint32_t bits = w == j >> 5 ? ends_s[w] >> (j & 31) << (j & 31) : ends_s[w];
-        if (bits) return w * 32 + __ffs(bits) - 1;
+        const uint32_t x = w == j >> 5 ? bits[w] >> (j & 31) << (j & 31) : bits[w];
+        if (x) return w * 32 + __ffs(x) - 1;
       }
       return window;
     };
-    // a unit that begins at row j of the window belongs to this round: to this block, and all of it is in the window
-    auto taken = [&](int j) -> bool {
-      if (!((valid_s[j >> 5] & ends_s[j >> 5]) >> (j & 31) & 1u) || s + j >= t1) return false;
-      return min(next_end(j + 1), j + p.unit - (int)(slot_s[j] & (p.unit - 1))) < window || j + p.unit - (int)(slot_s[j] & (p.unit - 1)) <= window;
-    };
-    // a round begins with a unit of this block
-    int begin = next_end(0);
-    while (begin < window && !((valid_s[begin >> 5] >> (begin & 31)) & 1u)) begin = next_end(begin + 1);
-    if (begin >= window || s + begin >= t1) {
-      if (begin < window || s + window >= t1) break;
-      s += window;                         // (nothing but rows without a place, or another block's)
+    if (tid < window) {
+      // a unit that begins at a row of the window belongs to this round where it is this block's and all of it is in the window
+      const int off = (int)(slot_s[tid] & (p.unit - 1));
+      const bool mine_ = ((valid_s[tid >> 5] & ends_s[tid >> 5]) >> lane & 1u) && s + tid < t1;
+      const bool whole = tid + p.unit - off <= window || s + window >= p.rows || (tid + 1 < window && first_of(ends_s, tid + 1) < window);
+      const uint32_t taken = __ballot_sync(kAll, mine_ && whole), stop = __ballot_sync(kAll, mine_ && !whole), held = __ballot_sync(kAll, mine_ && whole && off > 0);
+      if (lane == 0) { taken_s[warp] = taken; stop_s[warp] = stop; held_s[warp] = held; }
+    }
+    __syncthreads();
+    const int begin = first_of(taken_s, 0), stop = first_of(stop_s, 0);
+    if (begin == window) {                 // (a round takes a unit at its front always, so the first one may begin behind it)
+      if (stop == window && s + window >= t1) break;
+      s += stop < window ? stop : window;
       continue;
     }
-    if (begin > 0) {
-      s += begin;
-      continue;
-    }
+    const bool held = first_of(held_s, 0) < window;    // whether a unit of the round holds keys already
     // this thread's rows: the row their unit begins at (-1: none), and where they go
     int unit_at[kPer];
     int64_t to[kPer];
@@ -121,14 +120,13 @@ rotary_write8_kernel(const RotaryWriteParams p) {
       to[i] = 0;
       pos[i] = 0;
       if (j < window && ((valid_s[j >> 5] >> (j & 31)) & 1u)) {
-        int b = j;                         // the last row at or before j with a bit
-        for (int w = j >> 5; w >= 0; --w) {
+        int b = -1;                        // the last row at or before j with which something begins
+        for (int w = j >> 5; w >= 0 && b < 0; --w) {
           const uint32_t bits = w == j >> 5 ? ends_s[w] << (31 - (j & 31)) >> (31 - (j & 31)) : ends_s[w];
-          if (bits) { b = w * 32 + 31 - __clz((int)bits); break; }
-          b = -1;
+          if (bits) b = w * 32 + 31 - __clz((int)bits);
         }
         // (a unit cut off at the window's front begins in another block, or was this one's before)
-        if (b >= 0 && taken(b)) {
+        if (b >= 0 && ((taken_s[b >> 5] >> (b & 31)) & 1u)) {
           int64_t at;
           const int64_t page = page_of(slot_s[j], at);
           unit_at[i] = b;
@@ -137,16 +135,9 @@ rotary_write8_kernel(const RotaryWriteParams p) {
         }
       }
     }
-    // where the next round begins: the first unit of this block that is not taken
-    int next = t1;
-    bool held = false;                     // whether a unit of the round holds keys already
-    for (int j = 0; j < window && s + j < t1; j = next_end(j + 1)) {
-      if (!((valid_s[j >> 5] >> (j & 31)) & 1u)) continue;
-      if (!taken(j)) { next = s + j; break; }
-      held = held || (slot_s[j] & (p.unit - 1)) != 0;
-    }
+    const int next = stop < window ? s + stop : t1;    // where the next round begins: at the first unit of this block that is not taken
     // this thread's unit, if it keeps one: row tid begins it
-    const bool keeper = tid < window && taken(tid);
+    const bool keeper = tid < window && ((taken_s[tid >> 5] >> lane) & 1u);
     float* scale = scales;
     if (keeper) {
       int64_t at;
@@ -311,13 +302,23 @@ rotary_write8_kernel(const RotaryWriteParams p) {
           *reinterpret_cast<uint2*>(at + 8 * pb) = make_uint2(by.four(b[i][0], b[i][1]), by.four(b[i][2], b[i][3]));
         }
       }
-      if (keeper) scale[(int64_t)h * p.per_page] = scale_of(tid);
+      if (tid < window) {
+        bool grows = false;
+        if (keeper) {
+          const float now = scale_of(tid);
+          scale[(int64_t)h * p.per_page] = now;
+          grows = (slot_s[tid] & (p.unit - 1)) != 0 && now > old_s[par][tid];
+        }
+        if (held) {
+          const uint32_t bits = __ballot_sync(kAll, grows);
+          if (lane == 0) grown_s[warp] = bits;
+        }
+      }
+      if (held) __syncthreads();
       // units that hold keys already, and whose scale grows: these keys' codes on the new scale, by the whole block
-      for (int j = 0; held && j < window && s + j < t1; j = next_end(j + 1)) {
+      for (int j = held ? first_of(grown_s, 0) : window; j < window; j = j + 1 < window ? first_of(grown_s, j + 1) : window) {
         const int off = (int)(slot_s[j] & (p.unit - 1));
-        if (off == 0 || !taken(j)) continue;
         const float was = old_s[par][j], now = scale_of(j);
-        if (!(now > was)) continue;
         const Quotients by(now);
         int64_t at;
         const int64_t page = page_of(slot_s[j], at);
@@ -340,9 +341,10 @@ rotary_write8_kernel(const RotaryWriteParams p) {
 }
 
 template <int kPairs>
-static int launch_write8(const RotaryWriteParams& p, bool two, dim3 grid, cudaStream_t stream) {
-  if (two) rotary_write8_kernel<kPairs, 2><<<grid, kWriteThreads, 0, stream>>>(p);
-  else rotary_write8_kernel<kPairs, 1><<<grid, kWriteThreads, 0, stream>>>(p);
+static int launch_write8(const RotaryWriteParams& p, int per, int threads, dim3 grid, cudaStream_t stream) {
+  if (threads == 512) rotary_write8_kernel<kPairs, 2, 512><<<grid, 512, 0, stream>>>(p);
+  else if (per == 2) rotary_write8_kernel<kPairs, 2, 256><<<grid, 256, 0, stream>>>(p);
+  else rotary_write8_kernel<kPairs, 1, 256><<<grid, 256, 0, stream>>>(p);
   return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
@@ -381,21 +383,21 @@ extern "C" int mala_rotary_write_fp8(mala_tin q, mala_tin k, mala_tin v, const i
   p.eps = norm ? norm->eps : 0.f; p.inv_d = 1.f / (float)d;
   p.lanes = 1;
   while (16 * p.lanes < d) p.lanes *= 2;
-  // A thread has two rows where a unit's rows need that; else one, and more registers for rows on their way
-  const int step = kWriteThreads / p.lanes;
-  const bool two = p.unit > step;
-  const int window = two ? kWriteRows : step < kWriteRows ? step : kWriteRows;
-  // Rows of a block: as few as leave every SM a block (a decode step: each unit's latency counts), at most the window; then heads of a block:
-  // as many as leave every SM four blocks
+  // Blocks of 256 threads, two per SM (while one meets, the other works), with one row per thread, or two where a unit's rows need that; of 512 where they
+  // need four
+  const int beside = 256 / p.lanes, most = p.unit < rows ? p.unit : rows, threads = most > 2 * beside ? 512 : 256, per = most > beside ? 2 : 1;
+  const int window = per * threads / p.lanes < kWriteRows ? per * threads / p.lanes : kWriteRows;
+  // Rows of a block: as few as let all blocks run at once (a decode step: each unit's latency counts), at most the window; then heads of a block: as many as
+  // leave every SM eight blocks
   const long long sms = sm_count(dev);
   p.chunk = 1; p.heads = 1;
   auto blocks = [&]() { return ((long long)rows + p.chunk - 1) / p.chunk * ((Hkv + p.heads - 1) / p.heads) * 2; };
-  while (p.chunk < window && blocks() > sms) p.chunk *= 2;
+  while (p.chunk < window && blocks() > 512 / threads * sms) p.chunk *= 2;
   while (p.heads < Hkv && blocks() > 8 * sms) p.heads *= 2;
   const dim3 grid((unsigned)((rows + p.chunk - 1) / p.chunk), (unsigned)((Hkv + p.heads - 1) / p.heads), 2);
   switch (pairs_kind(rotary->rotary, rotary->interleaved)) {
-    case kHalves: return scope.finish(launch_write8<kHalves>(p, two, grid, stream));
-    case kHalvesOdd: return scope.finish(launch_write8<kHalvesOdd>(p, two, grid, stream));
-    default: return scope.finish(launch_write8<kNeighbours>(p, two, grid, stream));
+    case kHalves: return scope.finish(launch_write8<kHalves>(p, per, threads, grid, stream));
+    case kHalvesOdd: return scope.finish(launch_write8<kHalvesOdd>(p, per, threads, grid, stream));
+    default: return scope.finish(launch_write8<kNeighbours>(p, per, threads, grid, stream));
   }
 }
