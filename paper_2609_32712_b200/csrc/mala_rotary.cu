@@ -15,6 +15,9 @@ constexpr int kMaxRows = 1 << 30;
 constexpr int kRotaryThreads = 256, kRotaryWarps = kRotaryThreads / 32;
 constexpr int kNormBlocks = 1024;          // most blocks of the norm's backward (each leaves a sum per column)
 
+// Items first .. end - 1 for `blocks` blocks: interleaved warp by warp, or (chunk > 0) 8 * chunk neighbours to a block
+struct WorkRange { int blocks; uint32_t first, end; int chunk; };
+
 // One of a call's tensors: x is read and y written, rows x heads of d columns; strides in bytes
 struct RotaryTensor {
   const uint8_t* x; const uint8_t* g; uint8_t* y;          // (g: the incoming gradient in the norm's backward)
@@ -31,10 +34,11 @@ struct RotaryParams {
   const int* positions; int pos_n;         // [B, pos_n], or null: a row's own index
   const int* cu_q; const int* cu_k; int B; // packed sequences
   const int64_t* slots; int64_t limit; int page_size; FastDiv by_page;   // into pages
+  long long batches;                       // of all items (host)
+  WorkRange ranges[4];
   int tensors, joint;                      // joint: an item is a row of all tensors (whose rows are the same tokens)
   int weights_fp32; float eps, inv_d;
   float* partial;                          // the norm's backward: [blocks, d] sums
-  int q_blocks;
 };
 
 // Positions of the rows of one tensor after another
@@ -64,6 +68,23 @@ struct Positions {
     pos = n + p.t[w].first;
     if (p.positions) pos = __ldg(p.positions + (int64_t)b * p.pos_n + pos);
     return true;
+  }
+};
+
+// This warp's items: `first`, and every `stride`th up to `end`; the range that the block belongs to
+struct WarpItems {
+  uint32_t first, end, stride;
+  int range;
+  __device__ __forceinline__ explicit WarpItems(const RotaryParams& p) {
+    int b = blockIdx.x;
+    range = 0;
+    while (range < 3 && b >= p.ranges[range].blocks) b -= p.ranges[range++].blocks;
+    const WorkRange& r = p.ranges[range];
+    const int warp = threadIdx.x >> 5;
+    const uint64_t per = r.chunk > 0 ? (uint64_t)r.chunk * kRotaryWarps : 0;
+    first = (uint32_t)(r.chunk > 0 ? r.first + b * per + warp : (uint64_t)r.first + b * kRotaryWarps + warp);
+    end = r.chunk > 0 ? (uint32_t)min((uint64_t)r.end, r.first + (b + 1) * per) : r.end;
+    stride = r.chunk > 0 ? kRotaryWarps : r.blocks * kRotaryWarps;
   }
 };
 
@@ -202,10 +223,10 @@ rotary_kernel(const RotaryParams p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, c = lane % L;
   LanePieces<L, kPairs> l;
   l.set(p.rule, c);
-  const uint32_t nq = p.t[0].items, nk = p.t[1].items, all = nq + nk + (kPages ? p.t[2].items : 0);   // (at most 3 * 2^30)
-  const uint32_t stride = gridDim.x * kRotaryWarps, first = blockIdx.x * kRotaryWarps + warp;
+  const uint32_t nq = p.t[0].items, nk = p.t[1].items;     // (at most 2^30 each)
+  const WarpItems items(p);
   Rows<L, kPairs, false> rows;
-  rows.begin(p, l, g, ring_s + warp * 512 + lane, first, all, stride, nq, nk);
+  rows.begin(p, l, g, ring_s + warp * 512 + lane, items.first, items.end, items.stride, nq, nk);
   const int *cu_q, *cu_k;
   load_turns(p.rule, turns_s);
   load_offsets(p, cu_s, cu_q, cu_k);
@@ -216,7 +237,7 @@ rotary_kernel(const RotaryParams p) {
     }
   __syncthreads();
   Positions positions;
-  for (uint64_t x = first; x < all; x += stride) {
+  for (uint64_t x = items.first; x < items.end; x += items.stride) {
     Item it;
     it.at(p, nq, nk, (uint32_t)x);
     bool place = true, turn = false;
@@ -292,14 +313,14 @@ rotary_norm_bwd_kernel(const RotaryParams p) {
   __shared__ int cu_s[2 * kCuShared];
   __shared__ __align__(16) float weight_s[256];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, c = lane % L;
-  const int which = (int)blockIdx.x < p.q_blocks ? 0 : 1, block = blockIdx.x - (which ? p.q_blocks : 0);
-  const int blocks = which ? gridDim.x - p.q_blocks : p.q_blocks;
+  const WarpItems items(p);                // (ranges 0 and 2 are q's, 1 and 3 k's)
+  const int which = items.range & 1;
   const RotaryTensor& a = p.t[which];
   LanePieces<L, kPairs> l;
   l.set(p.rule, c);
-  const uint32_t nq = p.t[0].items, before = which ? nq : 0, stride = blocks * kRotaryWarps, first = before + block * kRotaryWarps + warp, end = before + a.items;
+  const uint32_t nq = p.t[0].items;
   Rows<L, kPairs, true> rows;
-  rows.begin(p, l, g, ring_s + warp * 512 + lane, first, end, stride, nq, p.t[1].items);
+  rows.begin(p, l, g, ring_s + warp * 512 + lane, items.first, items.end, items.stride, nq, p.t[1].items);
   const int *cu_q, *cu_k;
   load_turns(p.rule, turns_s);
   load_offsets(p, cu_s, cu_q, cu_k);
@@ -309,7 +330,7 @@ rotary_norm_bwd_kernel(const RotaryParams p) {
   const float4* const weights_a = reinterpret_cast<const float4*>(weight_s) + (l.has_a ? 2 * l.pa : 0);
   const float4* const weights_b = reinterpret_cast<const float4*>(weight_s) + (l.has_b ? 2 * l.pb : 0);
   Positions positions;
-  for (uint64_t x = first; x < end; x += stride) {
+  for (uint64_t x = items.first; x < items.end; x += items.stride) {
     Item it;
     it.at(p, nq, p.t[1].items, (uint32_t)x);
     uint8_t* const dst = a.y + it.b * a.y_sb + it.n * a.y_sn;
@@ -399,16 +420,18 @@ rotary_norm_bwd_kernel(const RotaryParams p) {
   }
 }
 
-// dw from the blocks' sums, 32 columns by a block, in a fixed order
+// dw from the blocks' sums, 32 columns by a block, in a fixed order: b0, b1, b2, b3 blocks of q, k, q, k
 __global__ void __launch_bounds__(1024)
-rotary_norm_sum_kernel(const float* partial, float* dwq, float* dwk, int d, int q_blocks, int blocks) {
+rotary_norm_sum_kernel(const float* partial, float* dwq, float* dwk, int d, int b0, int b1, int b2, int b3) {
   __shared__ float sums_s[32][33];
   wait_for_primary();
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
   float* const out = blockIdx.y ? dwk : dwq;
   float sum = 0.f;
-  if (out && c < d)
-    for (int x = (blockIdx.y ? q_blocks : 0) + w; x < (blockIdx.y ? blocks : q_blocks); x += 32) sum += partial[(size_t)x * d + c];
+  if (out && c < d) {
+    const int near = blockIdx.y ? b1 : b0, all = near + (blockIdx.y ? b3 : b2), at = blockIdx.y ? b0 : 0, far = at + b1 + (blockIdx.y ? b2 : b0) - near;
+    for (int x = w; x < all; x += 32) sum += partial[(size_t)(x < near ? at + x : far + x) * d + c];
+  }
   sums_s[w][threadIdx.x & 31] = sum;
   __syncthreads();
   sum = sums_s[threadIdx.x & 31][w];       // (warp w: column w, a lane per share)
@@ -470,6 +493,7 @@ static void set_items(RotaryParams* p, int tensors, int sms, bool same) {
   const int per = 32 / lanes_of(p->rule.d);
   long long loads = 0;
   for (int x = 0; x < tensors; ++x) loads += (long long)p->t[x].rows * ((p->t[x].H + per - 1) / per);
+  p->batches = loads;
   const long long want = loads / (32ll * sms);
   for (int x = 0; x < tensors; ++x) {
     RotaryTensor& t = p->t[x];
@@ -483,12 +507,28 @@ static void set_items(RotaryParams* p, int tensors, int sms, bool same) {
   for (int x = 1; x < tensors && p->joint; ++x) p->t[x].items = 0;
 }
 
+// Items first .. first + items - 1, whose batches (of a head for each group of a warp) are `batches` in all, for `blocks` blocks at once.  One round of blocks for all of them would
+// leave the SMs that memory serves sooner idle at the end (32K tokens, 32 + 8 heads: 126 us), and many short blocks begin too often (frequencies, weights, the
+// ring's first rows: some 2 us; six rounds 106 us, but 35 thousand rows of a step 145 instead of 135).  So seven tenths go to one round,
+// and the rest to blocks of `of_warp` batches a warp, which go to the SMs that are through (110 and 138; the backward pass with the norm 163 instead of 186).
+constexpr int kWarpBatches = 24, kWarpBatchesBwd = 16;
+static void set_ranges(WorkRange* one, WorkRange* rest, uint32_t first, long long items, long long batches, int blocks, int of_warp) {
+  *rest = WorkRange{0, 0, 0, 0};
+  const long long most = (items + kRotaryWarps - 1) / kRotaryWarps;
+  if (items == 0 || most <= blocks || batches <= 2ll * of_warp * kRotaryWarps * blocks) {
+    *one = WorkRange{(int)(most < blocks ? most : blocks), first, first + (uint32_t)items, 0};
+    return;
+  }
+  const long long near = items * 7 / 10, chunk = (of_warp * items + batches - 1) / batches;
+  *one = WorkRange{blocks, first, first + (uint32_t)near, 0};
+  *rest = WorkRange{(int)((items - near + chunk * kRotaryWarps - 1) / (chunk * kRotaryWarps)), first + (uint32_t)near, first + (uint32_t)items, (int)chunk};
+}
+
 template <int L, int kPairs, bool kNorm, bool kPages>
-static int launch_rotary_as(const RotaryParams& p, int sms, cudaStream_t stream) {
-  const long long items = (long long)p.t[0].items + p.t[1].items + (kPages ? p.t[2].items : 0);
-  const long long blocks = (items + kRotaryWarps - 1) / kRotaryWarps, most = 2ll * sms;
-  if (blocks == 0) return MALA_OK;
-  rotary_kernel<L, kPairs, kNorm, kPages><<<(unsigned)(blocks < most ? blocks : most), kRotaryThreads, kRingBytes, stream>>>(p);
+static int launch_rotary_as(const RotaryParams& p0, int sms, cudaStream_t stream) {
+  RotaryParams p = p0;
+  set_ranges(&p.ranges[0], &p.ranges[1], 0, (long long)p.t[0].items + p.t[1].items + (kPages ? p.t[2].items : 0), p.batches, 2 * sms, kWarpBatches);
+  rotary_kernel<L, kPairs, kNorm, kPages><<<p.ranges[0].blocks + p.ranges[1].blocks, kRotaryThreads, kRingBytes, stream>>>(p);
   return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 template <int L, bool kNorm, bool kPages>
@@ -527,25 +567,24 @@ static bool set_attributes_by() { return set_attributes_of<L, kHalves>() && set_
 bool rotary_set_attributes() { return set_attributes_by<4>() && set_attributes_by<8>() && set_attributes_by<16>(); }
 
 static int launch_norm_bwd(RotaryParams& p, int interleaved, float* dwq, float* dwk, int sms, cudaStream_t stream) {
-  const long long nq = (p.t[0].items + kRotaryWarps - 1) / kRotaryWarps, nk = (p.t[1].items + kRotaryWarps - 1) / kRotaryWarps;
-  const long long most = 2ll * sms < kNormBlocks ? 2ll * sms : kNormBlocks;
-  // the blocks in the share of the tensors' rows and heads
-  const double loads_q = (double)p.t[0].rows * p.t[0].H, loads_k = (double)p.t[1].rows * p.t[1].H;
-  long long gq = nq, gk = nk;
-  if (gq + gk > most) {
-    gq = (long long)(most * (loads_q / (loads_q + loads_k)) + 0.5);
-    gq = gq < 1 ? 1 : gq > most - (nk > 0) ? most - (nk > 0) : gq;
-    gk = nk > 0 ? most - gq : 0;
-    gq = gq > nq ? nq : gq;
-    gk = gk > nk ? nk : gk;
-  }
-  p.q_blocks = (int)gq;
-  const int blocks = (int)(gq + gk), L = lanes_of(p.rule.d);
+  // the blocks that run at once, in the share of the tensors' rows and heads
+  const double loads_q = (double)p.t[0].rows * p.t[0].H, loads_k = (double)p.t[1].rows * p.t[1].H, part = loads_q / (loads_q + loads_k);
+  int gq = (int)(2 * sms * part + 0.5);
+  gq = gq < 1 ? 1 : gq > 2 * sms - (loads_k > 0) ? 2 * sms - (loads_k > 0) : gq;
+  set_ranges(&p.ranges[0], &p.ranges[2], 0, p.t[0].items, (long long)(p.batches * part), gq, kWarpBatchesBwd);
+  set_ranges(&p.ranges[1], &p.ranges[3], p.t[0].items, p.t[1].items, (long long)(p.batches * (1 - part)), 2 * sms - gq, kWarpBatchesBwd);
+  // (short blocks, as far as the workspace has room for their sums)
+  for (int x = 2; x < 4; ++x)
+    while (p.ranges[x].blocks > (kNormBlocks - 2 * sms) / 2) {
+      p.ranges[x].chunk *= 2;
+      p.ranges[x].blocks = (p.ranges[x].blocks + 1) / 2;
+    }
+  const int blocks = p.ranges[0].blocks + p.ranges[1].blocks + p.ranges[2].blocks + p.ranges[3].blocks, L = lanes_of(p.rule.d);
   MALA_TRY(L == 4 ? launch_norm_bwd_by<4>(p, interleaved, blocks, stream)
                   : L == 8 ? launch_norm_bwd_by<8>(p, interleaved, blocks, stream) : launch_norm_bwd_by<16>(p, interleaved, blocks, stream));
   if (!dwq && !dwk) return MALA_OK;
   return launch_dependent(rotary_norm_sum_kernel, dim3((p.rule.d + 31) / 32, 2), dim3(1024), stream, (const float*)p.partial, dwq, dwk, p.rule.d,
-                          p.q_blocks, blocks) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+                          p.ranges[0].blocks, p.ranges[1].blocks, p.ranges[2].blocks, p.ranges[3].blocks) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
 // What the calls have in common: q [B,Nq,Hq,d], k [B,Nk,Hkv,d] (or none), the queries being the last Nq of Nk positions; cu: packed

@@ -955,7 +955,9 @@ class Rotary:
         assert inv_freq.dim() == 1 and inv_freq.numel() >= 1 and inv_freq.is_floating_point(), "expects a frequency per pair of columns"
         if device is None and not inv_freq.is_cuda:
             device = "cuda"
-        self.inv_freq = inv_freq.detach().to(device=device, dtype=torch.float64).contiguous()
+        if device is not None or inv_freq.dtype is not torch.float64 or inv_freq.requires_grad or not inv_freq.is_contiguous():
+            inv_freq = inv_freq.detach().to(device=device, dtype=torch.float64).contiguous()
+        self.inv_freq = inv_freq
         self.rotary, self.interleaved, self.magnitude = 2 * inv_freq.numel(), bool(interleaved), float(magnitude)
         self.c = _Rotary(self.inv_freq.data_ptr(), self.rotary, int(self.interleaved), self.magnitude)
 
@@ -988,9 +990,9 @@ _NO_IN, _NO_OUT = _TIn(None, 0, 0, 0), _TOut(None, 0, 0, 0)
 
 
 def _like(x, out):
-    """A new tensor for rotated rows (contiguous, whatever wider tensor x is a part of), or the given one."""
+    """A new tensor for rotated rows (dense, whatever wider tensor x is a part of), or the given one."""
     if out is None:
-        return x.new_empty(x.shape)
+        return torch.empty_like(x)
     assert out.shape == x.shape
     return out
 
