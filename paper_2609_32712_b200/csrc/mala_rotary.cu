@@ -36,6 +36,7 @@ struct RotaryParams {
   const int64_t* slots; int64_t limit; int page_size; FastDiv by_page;   // into pages
   long long batches;                       // of all items (host)
   WorkRange ranges[4];
+  int release;                             // whether the next kernel may start beside this one (it reads and writes nothing of this one's)
   int tensors, joint;                      // joint: an item is a row of all tensors (whose rows are the same tokens)
   int weights_fp32; float eps, inv_d;
   float* partial;                          // the norm's backward: [blocks, d] sums
@@ -223,6 +224,7 @@ rotary_kernel(const RotaryParams p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / L, c = lane % L;
   LanePieces<L, kPairs> l;
   l.set(p.rule, c);
+  if (p.release) release_dependents();
   const uint32_t nq = p.t[0].items, nk = p.t[1].items;     // (at most 2^30 each)
   const WarpItems items(p);
   Rows<L, kPairs, false> rows;
@@ -527,7 +529,10 @@ static void set_ranges(WorkRange* one, WorkRange* rest, uint32_t first, long lon
 template <int L, int kPairs, bool kNorm, bool kPages>
 static int launch_rotary_as(const RotaryParams& p0, int sms, cudaStream_t stream) {
   RotaryParams p = p0;
-  set_ranges(&p.ranges[0], &p.ranges[1], 0, (long long)p.t[0].items + p.t[1].items + (kPages ? p.t[2].items : 0), p.batches, 2 * sms, kWarpBatches);
+  const long long items = (long long)p.t[0].items + p.t[1].items + (kPages ? p.t[2].items : 0), most = (items + kRotaryWarps - 1) / kRotaryWarps;
+  // (beside another kernel: one block per SM, which leaves it room)
+  if (p.release) p.ranges[0] = WorkRange{(int)(most < sms ? most : sms), 0, (uint32_t)items, 0};
+  else set_ranges(&p.ranges[0], &p.ranges[1], 0, items, p.batches, 2 * sms, kWarpBatches);
   rotary_kernel<L, kPairs, kNorm, kPages><<<p.ranges[0].blocks + p.ranges[1].blocks, kRotaryThreads, kRingBytes, stream>>>(p);
   return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
@@ -603,7 +608,7 @@ static int check_call(const RotaryCall& c, bool with_k) {
 
 // Forward; or, back: the same rotation in the other sense, from gradients to gradients (no norm)
 static int rotate(const RotaryCall& c, mala_tin q, mala_tin k, mala_tout qo, mala_tout ko, const mala_rotary* r, const mala_head_norm* norm, bool back,
-                  cudaStream_t stream) {
+                  cudaStream_t stream, bool release = false) {
   const bool with_k = k.p != nullptr || ko.p != nullptr;
   MALA_TRY(check_call(c, with_k));
   MALA_TRY(check_rule(r, norm, c.d));
@@ -618,6 +623,7 @@ static int rotate(const RotaryCall& c, mala_tin q, mala_tin k, mala_tout qo, mal
   MALA_TRY(device_setup(dev, &status));
   RotaryParams p = {};
   set_rule(&p, r, norm, c.d, back);
+  p.release = release ? 1 : 0;
   set_tensor(&p.t[0], q, qo, c.B, c.Nq, c.Hq, c.Nk - c.Nq);
   if (with_k) set_tensor(&p.t[1], k, ko, c.B, c.Nk, c.Hkv, 0);
   p.positions = c.positions; p.pos_n = c.Nk;
@@ -677,11 +683,11 @@ static int packed_call(RotaryCall* c, const int32_t* cu_q, const int32_t* cu_k, 
   return MALA_OK;
 }
 
-// Rows of q alone at their positions (in front of the e4m3 write)
+// Rows of q alone at their positions, beside the e4m3 write that is launched behind it as a dependent
 int rotate_queries(mala_tin q, const int32_t* positions, mala_tout qo, const mala_rotary* r, const mala_head_norm* norm, int rows, int Hq, int d,
                    cudaStream_t stream) {
   return rotate(RotaryCall{1, rows, rows, Hq, 0, d, positions, nullptr, nullptr, 0}, q, mala_tin{nullptr, 0, 0, 0}, qo, mala_tout{nullptr, 0, 0, 0}, r, norm, false,
-                stream);
+                stream, true);
 }
 
 int check_rotary_step(mala_tin q, const int32_t* positions, mala_tout qo, const mala_rotary* r, const mala_head_norm* norm, int rows, int Hq, int d) {

@@ -338,14 +338,13 @@ rotary_write8_kernel(const RotaryWriteParams p) {
     }
     s = next;
   }
+  wait_for_primary();                      // (the queries' rotation, which runs beside this: not over before that is)
 }
 
 template <int kPairs>
 static int launch_write8(const RotaryWriteParams& p, int per, int threads, dim3 grid, cudaStream_t stream) {
-  if (threads == 512) rotary_write8_kernel<kPairs, 2, 512><<<grid, 512, 0, stream>>>(p);
-  else if (per == 2) rotary_write8_kernel<kPairs, 2, 256><<<grid, 256, 0, stream>>>(p);
-  else rotary_write8_kernel<kPairs, 1, 256><<<grid, 256, 0, stream>>>(p);
-  return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
+  auto* const kernel = threads == 512 ? rotary_write8_kernel<kPairs, 2, 512> : per == 2 ? rotary_write8_kernel<kPairs, 2, 256> : rotary_write8_kernel<kPairs, 1, 256>;
+  return launch_dependent(kernel, grid, dim3(threads), stream, p) == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 
 }  // namespace mala
