@@ -24,28 +24,43 @@ __device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
   return __half22float2(*reinterpret_cast<__half2*>(&h));
 }
 
-// x / s for a unit's scale s, as mala_cache_write_fp8 rounds it: the quotient correctly rounded (Markstein's correction; the comment at cache_write8_kernel has the
-// steps), then to e4m3; the codes take the sign of x.
+// Codes e4m3(x / s) for a unit's scale s, the quotient correctly rounded as mala_cache_write_fp8 rounds it (Markstein's correction; the comment at
+// cache_write8_kernel has the steps), from n = -x: with q = n (-y), r = q s + n and q + r (-y) a zero keeps its sign without further work.
 struct Quotients {
-  uint64_t move2, y2, minus_s2;
+  uint64_t minus_y2, s2, move2;
+  bool far;                 // x and s are moved by a power of two first
   __device__ __forceinline__ explicit Quotients(float s) {
-    const float move = s < 1e-20f ? 0x1p64f : s > 1e20f ? 0x1p-64f : 1.f, s_ = s * move, y = __fdiv_rn(1.f, s_);
+    const float move = s < 1e-20f ? 0x1p64f : s > 1e20f ? 0x1p-64f : 1.f, s_ = s * move, y = -__fdiv_rn(1.f, s_);
+    far = move != 1.f;
     move2 = f2(move, move);
-    y2 = f2(y, y);
-    minus_s2 = f2(-s_, -s_);
+    minus_y2 = f2(y, y);
+    s2 = f2(s_, s_);
   }
-  __device__ __forceinline__ uint32_t two(uint64_t v) const {   // without signs of zeros
-    const uint64_t x = f2_mul(v, move2), q = f2_mul(x, y2);
+  __device__ __forceinline__ uint32_t two(uint64_t n) const {
+    const uint64_t q = f2_mul(n, minus_y2);
     float a, b;
-    f2_get(f2_fma(f2_fma(q, minus_s2, x), y2, q), a, b);
+    f2_get(f2_fma(f2_fma(q, s2, n), minus_y2, q), a, b);
     return e4m3x2(a, b);
   }
-  __device__ __forceinline__ uint32_t four(uint64_t lo, uint64_t hi) const {
-    float x0, x1, x2, x3;
-    f2_get(lo, x0, x1);
-    f2_get(hi, x2, x3);
-    const uint32_t high = __byte_perm(__byte_perm(__float_as_uint(x0), __float_as_uint(x1), 0x0073), __byte_perm(__float_as_uint(x2), __float_as_uint(x3), 0x0073), 0x5410);
-    return ((two(lo) | (two(hi) << 16)) & 0x7f7f7f7fu) | (high & 0x80808080u);
+  // eight codes of pairs n
+  __device__ __forceinline__ uint2 eight(const uint64_t (&n)[4]) const {
+    if (far) {
+      uint64_t m[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m[j] = f2_mul(n[j], move2);
+      return make_uint2(two(m[0]) | (two(m[1]) << 16), two(m[2]) | (two(m[3]) << 16));
+    }
+    return make_uint2(two(n[0]) | (two(n[1]) << 16), two(n[2]) | (two(n[3]) << 16));
+  }
+  // four codes on another scale: -was times what they stand for
+  __device__ __forceinline__ uint32_t again(uint32_t codes, float minus_was) const {
+    const float2 x = from_e4m3x2((uint16_t)codes), y = from_e4m3x2((uint16_t)(codes >> 16));
+    uint64_t a = f2_mul(f2(x.x, x.y), f2(minus_was, minus_was)), b = f2_mul(f2(y.x, y.y), f2(minus_was, minus_was));
+    if (far) {
+      a = f2_mul(a, move2);
+      b = f2_mul(b, move2);
+    }
+    return two(a) | (two(b) << 16);
   }
 };
 

@@ -529,10 +529,7 @@ static void set_ranges(WorkRange* one, WorkRange* rest, uint32_t first, long lon
 template <int L, int kPairs, bool kNorm, bool kPages>
 static int launch_rotary_as(const RotaryParams& p0, int sms, cudaStream_t stream) {
   RotaryParams p = p0;
-  const long long items = (long long)p.t[0].items + p.t[1].items + (kPages ? p.t[2].items : 0), most = (items + kRotaryWarps - 1) / kRotaryWarps;
-  // (beside another kernel: one block per SM, which leaves it room)
-  if (p.release) p.ranges[0] = WorkRange{(int)(most < sms ? most : sms), 0, (uint32_t)items, 0};
-  else set_ranges(&p.ranges[0], &p.ranges[1], 0, items, p.batches, 2 * sms, kWarpBatches);
+  set_ranges(&p.ranges[0], &p.ranges[1], 0, (long long)p.t[0].items + p.t[1].items + (kPages ? p.t[2].items : 0), p.batches, 2 * sms, kWarpBatches);
   rotary_kernel<L, kPairs, kNorm, kPages><<<p.ranges[0].blocks + p.ranges[1].blocks, kRotaryThreads, kRingBytes, stream>>>(p);
   return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }

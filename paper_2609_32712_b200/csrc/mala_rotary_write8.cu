@@ -29,6 +29,10 @@ struct RotaryWriteParams {
   float eps, inv_d;
 };
 
+__device__ __forceinline__ uint4 negated(const uint4& w) {
+  return make_uint4(w.x ^ 0x80008000u, w.y ^ 0x80008000u, w.z ^ 0x80008000u, w.w ^ 0x80008000u);
+}
+
 // A unit's scale follows from all of its rows, behind their rotation, so a block holds a unit's rows in registers, in fp32, between its
 // maximum and its codes: they are read once and rotated once.  The block takes the units that begin among `chunk` rows of the call, up to
 // kWriteRows rows of them at a time, and `heads` heads one after the other: a row's angles are worked out once for all of
@@ -180,11 +184,11 @@ rotary_write8_kernel(const RotaryWriteParams p) {
     load(h0);
     int buf = 0;
     for (int h = h0; h < h1; ++h, buf = buf == 2 ? 0 : buf + 1) {
-      uint64_t a[kPer][4], b[kPer][4];     // the rows in fp32
+      uint64_t a[kPer][4], b[kPer][4];     // the rows in fp32, negated: as the quotients below want them
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        pairs_of(ra[i], a[i]);
-        pairs_of(rb[i], b[i]);
+        pairs_of(negated(ra[i]), a[i]);
+        pairs_of(negated(rb[i]), b[i]);
       }
       if (kPairs == kHalvesOdd && !is_v) { // (rare: partners out of shared memory, angles column by column, one row of the thread after the other)
 #pragma unroll
@@ -212,7 +216,7 @@ rotary_write8_kernel(const RotaryWriteParams p) {
               const float y = staged(other) * r * weight_s[other];
               x = fmaf(y, (col < half ? -sn : sn) * p.rule.turned, x * (cs * p.rule.magnitude));
             }
-            x = mine ? x : 0.f;
+            x = mine ? -x : 0.f;
             uint64_t& to2 = e < 8 ? a[i][e / 2] : b[i][(e - 8) / 2];
             float lo, hi;
             f2_get(to2, lo, hi);
@@ -243,10 +247,12 @@ rotary_write8_kernel(const RotaryWriteParams p) {
             if (pair) {                    // (a, b) -> (a cos - b sin, b cos + a sin)
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                const uint64_t cs = f2(C[i][2 * j], C[i][2 * j + 1]), sn = f2(S[i][2 * j], S[i][2 * j + 1]), minus = f2(-S[i][2 * j], -S[i][2 * j + 1]);
-                const uint64_t x = a[i][j];
-                a[i][j] = f2_fma(b[i][j], minus, f2_mul(x, cs));
-                b[i][j] = f2_fma(x, sn, f2_mul(b[i][j], cs));
+                const uint64_t cs = f2(C[i][2 * j], C[i][2 * j + 1]), x = f2_mul(a[i][j], cs);
+                float x0, x1, b0, b1;
+                f2_get(x, x0, x1);
+                f2_get(b[i][j], b0, b1);
+                b[i][j] = f2_fma(a[i][j], f2(S[i][2 * j], S[i][2 * j + 1]), f2_mul(b[i][j], cs));
+                a[i][j] = f2(fmaf(-b0, S[i][2 * j], x0), fmaf(-b1, S[i][2 * j + 1], x1));
               }
             }
           } else {                         // four pairs in a, four in b
@@ -255,7 +261,7 @@ rotary_write8_kernel(const RotaryWriteParams p) {
               uint64_t& x = e < 4 ? a[i][e] : b[i][e - 4];
               float lo, hi;
               f2_get(x, lo, hi);
-              x = f2_fma(f2(hi, lo), f2(-S[i][e], S[i][e]), f2_mul(x, f2(C[i][e], C[i][e])));
+              x = f2(fmaf(-hi, S[i][e], lo * C[i][e]), fmaf(lo, S[i][e], hi * C[i][e]));
             }
           }
         }
@@ -292,15 +298,20 @@ rotary_write8_kernel(const RotaryWriteParams p) {
         const float x = (slot_s[u] & (p.unit - 1)) == 0 ? want : fmaxf(old_s[par][u], want);
         return x > 0.f ? x : 1.f;          // (nothing but zeros)
       };
+      auto put = [&](int i, const Quotients& by) {
+        uint8_t* const at = pages + to[i] + h * d_sh;
+        *reinterpret_cast<uint2*>(at + 8 * pa) = by.eight(a[i]);
+        *reinterpret_cast<uint2*>(at + 8 * pb) = by.eight(b[i]);
+      };
+      if (one >= 0) {
+        const Quotients by(scale_of(one));
+        if (mine)
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if (unit_at[i] < 0) continue;
-        const Quotients by(scale_of(unit_at[i]));
-        if (mine) {
-          uint8_t* at = pages + to[i] + h * d_sh;
-          *reinterpret_cast<uint2*>(at + 8 * pa) = make_uint2(by.four(a[i][0], a[i][1]), by.four(a[i][2], a[i][3]));
-          *reinterpret_cast<uint2*>(at + 8 * pb) = make_uint2(by.four(b[i][0], b[i][1]), by.four(b[i][2], b[i][3]));
-        }
+          for (int i = 0; i < kPer; ++i) put(i, by);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (unit_at[i] >= 0 && mine) put(i, Quotients(scale_of(unit_at[i])));
       }
       if (tid < window) {
         bool grows = false;
@@ -325,12 +336,8 @@ rotary_write8_kernel(const RotaryWriteParams p) {
         uint8_t* first = pages + page * d_sb + (at - off) * d_sn + h * d_sh + 16 * c;
         if (mine)
           for (int r = r0; r < off; r += step) {
-            uint4 o = *reinterpret_cast<const uint4*>(first + r * d_sn);
-            auto four = [&](uint32_t u) -> uint32_t {
-              const float2 x = from_e4m3x2((uint16_t)u), y = from_e4m3x2((uint16_t)(u >> 16));
-              return ((by.two(f2(x.x * was, x.y * was)) | (by.two(f2(y.x * was, y.y * was)) << 16)) & 0x7f7f7f7fu) | (u & 0x80808080u);
-            };
-            *reinterpret_cast<uint4*>(first + r * d_sn) = make_uint4(four(o.x), four(o.y), four(o.z), four(o.w));
+            const uint4 o = *reinterpret_cast<const uint4*>(first + r * d_sn);
+            *reinterpret_cast<uint4*>(first + r * d_sn) = make_uint4(by.again(o.x, -was), by.again(o.y, -was), by.again(o.z, -was), by.again(o.w, -was));
           }
       }
       // the buffer of the head behind the next one (last read before this head's meeting)
