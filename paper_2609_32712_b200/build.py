@@ -1,27 +1,52 @@
-"""Builds ``libmala.so`` in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Builds ``libmala.so`` in-tree with nvcc for sm_100a (cross-compiles without a GPU), and beside it ``_native.so``, the marshalling
+of the rotary calls and the cache reads, with g++ against torch."""
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
+import sysconfig
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRCS = [os.path.join(HERE, "csrc", n) for n in ("mala_api.cu", "mala_bias.cu", "mala_cache.cu", "mala_rotary.cu", "mala_rotary_write8.cu",
                                                 "mala_scaled.cu")]
 LIB = os.path.join(HERE, "libmala.so")
+NATIVE_SRC = os.path.join(HERE, "csrc", "mala_native.cpp")
+NATIVE = os.path.join(HERE, "_native.so")
+INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 
-def _newest_source_mtime() -> float:
-    t = 0.0
-    for root in (os.path.join(HERE, "csrc"), os.path.join(os.path.dirname(HERE), "include")):
-        for f in os.listdir(root):
-            t = max(t, os.path.getmtime(os.path.join(root, f)))
-    return t
+def _up_to_date(built: str, sources) -> bool:
+    return os.path.exists(built) and os.path.getmtime(built) >= max(map(os.path.getmtime, sources))
+
+
+def _sources():
+    files = [os.path.join(root, f) for root in (os.path.join(HERE, "csrc"), INCLUDE) for f in os.listdir(root)]
+    return [f for f in files if f != NATIVE_SRC]
+
+
+def _native_command():
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc")))
+    include = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+               os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    libs = os.path.join(home, "lib")
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
+            [f"-I{p}" for p in include] + [NATIVE_SRC, "-o", NATIVE, f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10",
+                                           f"-Wl,-rpath,{libs}", f"-L{HERE}", "-l:libmala.so", "-Wl,-rpath,$ORIGIN"])
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source_mtime():
-        return LIB
+    if force or not _up_to_date(LIB, _sources()):
+        _build_library(verbose)
+    if force or not _up_to_date(NATIVE, [NATIVE_SRC, os.path.join(INCLUDE, "mala.h")]):
+        subprocess.check_call(_native_command())
+    return LIB
+
+
+def _build_library(verbose: bool) -> None:
     # (one nvcc per source, side by side; the objects go to a folder that does not outlive the call)
     nvcc = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC"]
     if verbose:
@@ -33,7 +58,6 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if any(codes):
             raise RuntimeError(f"nvcc failed: {[os.path.basename(s) for s, c in zip(SRCS, codes) if c]}")
         subprocess.check_call(nvcc[:3] + ["-shared", "-o", LIB] + objs + ["-ldl"])
-    return LIB
 
 
 if __name__ == "__main__":

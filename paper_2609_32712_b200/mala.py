@@ -164,6 +164,29 @@ def lib():
     return _lib
 
 
+_native_module = None
+
+
+def _native():
+    """The extension that marshals the rotary calls and the cache reads (built beside libmala.so; fails loudly if absent)."""
+    global _native_module
+    if _native_module is None:
+        lib()                # (the library that it is linked with)
+        try:
+            from . import _native as module
+        except ImportError as e:
+            raise ImportError(f"{os.path.join(_HERE, '_native.so')}: run `python -m paper_2609_32712_b200.build` (needs g++)") from e
+        _native_module = module
+    return _native_module
+
+
+def _done(r, what: str):
+    """What a call of the extension gave: its outputs, or the code with which the library refused it."""
+    if type(r) is int:
+        raise MalaError(r, what)
+    return r
+
+
 # A decode step over a short cache takes about 10 us on the device, so what these helpers cost is what such a step waits
 # for: strides read once, the stream's raw handle and new_empty took a step over 2000 keys from 24 to 16 us.
 _BF16 = torch.bfloat16
@@ -860,34 +883,14 @@ def cache_read(kpages, vpages, block_table, seqlens, rows: int):
     """mala_cache_read: keys and values of the requests of block_table int32 [B, max_pages_per_seq] with seqlens int32 [B] tokens
     out of bf16 pages [num_pages, page_size, Hkv, d], packed.  rows: how many rows to make room for (at least the sum of the lengths for all
     of them).  Returns (k, v [1,rows,Hkv,d] bf16, cu_seqlens int32 [B+1]), as ``fwd_varlen_prefix`` takes them."""
-    return _cache_read(kpages, vpages, None, None, block_table, seqlens, rows)
+    return _done(_native().cache_read(kpages, vpages, None, None, block_table, seqlens, rows), "mala_cache_read")
 
 
 def cache_read_fp8(kpages8, vpages8, kscale, vscale, block_table, seqlens, rows: int):
     """mala_cache_read_fp8: the same out of e4m3 pages (uint8 or float8_e4m3fn) with their scales fp32
     [num_pages, Hkv, max(1, page_size/128)]."""
-    return _cache_read(kpages8, vpages8, kscale, vscale, block_table, seqlens, rows)
-
-
-def _cache_read(kp, vp, ks, vs, block_table, seqlens, rows):
-    _ints(block_table, seqlens)
-    num_pages, page_size, Hkv, d = kp.shape
-    B, max_pages = block_table.shape
-    assert seqlens.shape == (B,) and kp.shape == vp.shape
-    if ks is not None:
-        _scales(ks, vs, num_pages, Hkv, page_size)
-    k, v = (kp.new_empty((1, rows, Hkv, d), dtype=_BF16) for _ in range(2))
-    cu = seqlens.new_empty(B + 1)
-    stream = _here(kp, vp, ks, vs, block_table, seqlens)
-    tail = (block_table.data_ptr(), seqlens.data_ptr(), _view(k, _TOut), _view(v, _TOut), cu.data_ptr(), B, Hkv, num_pages, page_size,
-            max_pages, rows, d, stream)
-    if ks is None:
-        rc, name = lib().mala_cache_read(_view(kp, _TIn), _view(vp, _TIn), *tail), "mala_cache_read"
-    else:
-        rc, name = lib().mala_cache_read_fp8(_view8(kp), _view8(vp), ks.data_ptr(), vs.data_ptr(), *tail), "mala_cache_read_fp8"
-    if rc != 0:
-        raise MalaError(rc, name)
-    return k, v, cu
+    assert kscale is not None and vscale is not None, "expects scales of keys and of values"
+    return _done(_native().cache_read(kpages8, vpages8, kscale, vscale, block_table, seqlens, rows), "mala_cache_read_fp8")
 
 
 def fwd_paged_fp8(q, kpages8, vpages8, kscale, vscale, cu_seqlens_q, block_table, seqlens_k, max_seqlen_q: int, total_k: int,
@@ -959,7 +962,6 @@ class Rotary:
             inv_freq = inv_freq.detach().to(device=device, dtype=torch.float64).contiguous()
         self.inv_freq = inv_freq
         self.rotary, self.interleaved, self.magnitude = 2 * inv_freq.numel(), bool(interleaved), float(magnitude)
-        self.c = _Rotary(self.inv_freq.data_ptr(), self.rotary, int(self.interleaved), self.magnitude)
 
 
 class HeadNorm:
@@ -972,67 +974,18 @@ class HeadNorm:
             assert w.dim() == 1 and w.is_contiguous() and w.dtype in (_BF16, _F32) and w.dtype == both[0].dtype and w.shape == both[0].shape, \
                 "expects contiguous weights [d] of one type, bf16 or fp32"
         self.q_weight, self.k_weight, self.eps = q_weight, k_weight, float(eps)
-        self.fp32 = int(bool(both) and both[0].dtype is _F32)
-
-    def _for(self, d: int):
-        for w in (self.q_weight, self.k_weight):
-            assert w is None or w.shape == (d,), "a weight per column of a head"
-        q, k = (None if w is None else w.data_ptr() for w in (self.q_weight, self.k_weight))
-        self.c = _HeadNorm(q, k, self.fp32, self.eps)
-        return ctypes.byref(self.c)
 
 
-def _norm_of(norm: Optional[HeadNorm], d: int):
-    return (None, None, None) if norm is None else (norm._for(d), norm.q_weight, norm.k_weight)
-
-
-_NO_IN, _NO_OUT = _TIn(None, 0, 0, 0), _TOut(None, 0, 0, 0)
-
-
-def _like(x, out):
-    """A new tensor for rotated rows (dense, whatever wider tensor x is a part of), or the given one."""
-    if out is None:
-        return torch.empty_like(x)
-    assert out.shape == x.shape
-    return out
-
-
-def _positions(positions, B: int, Nq: int, Nk: int):
-    if positions is None:
-        return None
-    _ints(positions)
-    assert positions.shape == (B, Nk) and Nk >= Nq, "expects a position per row of k (or of q, without keys)"
-    return positions.data_ptr()
+def _rule(rot: Rotary, norm: Optional[HeadNorm]):
+    if norm is None:
+        return rot.inv_freq, rot.interleaved, rot.magnitude, None, None, None
+    return rot.inv_freq, rot.interleaved, rot.magnitude, norm.eps, norm.q_weight, norm.k_weight
 
 
 def rotary(q, k, rot: Rotary, positions=None, norm: Optional[HeadNorm] = None, q_out=None, k_out=None):
     """mala_rotary_fwd: rotary positions of q [B,Nq,Hq,d] and k [B,Nk,Hkv,d] (or None), bf16.  The queries are the last Nq of the Nk
     positions; positions int32 [B,Nk] (default 0 .. Nk - 1).  q_out, k_out may be q and k themselves.  Returns (q', k')."""
-    B, Nq, Hq, d = q.shape
-    Nk, Hkv = (Nq, 0) if k is None else k.shape[1:3]
-    assert k is None or (k.shape[0] == B and k.shape[3] == d)
-    qo, ko = _like(q, q_out), None if k is None else _like(k, k_out)
-    n, wq, wk = _norm_of(norm, d)
-    rc = lib().mala_rotary_fwd(_view(q, _TIn), _NO_IN if k is None else _view(k, _TIn), _positions(positions, B, Nq, Nk),
-                               ctypes.byref(rot.c), n, _view(qo, _TOut), _NO_OUT if k is None else _view(ko, _TOut), B, Nq, Nk, Hq,
-                               Hkv, d, _here(q, k, positions, rot.inv_freq, qo, ko, wq, wk))
-    if rc != 0:
-        raise MalaError(rc, "mala_rotary_fwd")
-    return qo, ko
-
-
-def _rotary_grads(norm, d: int, with_k: bool, weights: bool, q):
-    """(dq_weight, dk_weight, ws) of a backward call: where there is a weight."""
-    if norm is None or not weights:
-        return None, None, None
-    dwq = q.new_empty(d, dtype=_F32) if norm.q_weight is not None else None
-    dwk = q.new_empty(d, dtype=_F32) if norm.k_weight is not None and with_k else None
-    ws = _ws(int(lib().mala_rotary_workspace_bytes(d)), q.device) if dwq is not None or dwk is not None else None
-    return dwq, dwk, ws
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+    return _done(_native().rotary(q, k, *_rule(rot, norm), positions, None, None, q_out, k_out), "mala_rotary_fwd")
 
 
 def rotary_bwd(dq, dk, rot: Rotary, positions=None, norm: Optional[HeadNorm] = None, q=None, k=None, dq_out=None, dk_out=None,
@@ -1040,114 +993,30 @@ def rotary_bwd(dq, dk, rot: Rotary, positions=None, norm: Optional[HeadNorm] = N
     """mala_rotary_bwd: the gradients of q and k from those of rotary's outputs, dq and dk (or None); with a norm q and k as they went into it.
     dq_out, dk_out may be dq and dk themselves.  Returns (dq, dk, dq_weight, dk_weight), the weights' fp32 [d], None where there is
     none (or with weights false)."""
-    B, Nq, Hq, d = dq.shape
-    Nk, Hkv = (Nq, 0) if dk is None else dk.shape[1:3]
-    assert dk is None or (dk.shape[0] == B and dk.shape[3] == d)
-    if norm is not None:
-        assert q is not None and q.shape == dq.shape and (dk is None or (k is not None and k.shape == dk.shape)), "with a norm: q and k"
-    else:
-        q = k = None
-    if dk is None:
-        k = None
-    qo, ko = _like(dq, dq_out), None if dk is None else _like(dk, dk_out)
-    n, wq, wk = _norm_of(norm, d)
-    dwq, dwk, ws = _rotary_grads(norm, d, dk is not None, weights, dq)
-    rc = lib().mala_rotary_bwd(_view(dq, _TIn), _NO_IN if dk is None else _view(dk, _TIn), _NO_IN if q is None else _view(q, _TIn),
-                               _NO_IN if k is None else _view(k, _TIn), _positions(positions, B, Nq, Nk), ctypes.byref(rot.c), n,
-                               _view(qo, _TOut), _NO_OUT if dk is None else _view(ko, _TOut), _ptr(dwq), _ptr(dwk), B, Nq, Nk, Hq, Hkv,
-                               d, _ptr(ws), 0 if ws is None else ws.numel(), _here(dq, dk, q, k, positions, rot.inv_freq, qo, ko, wq, wk))
-    if rc != 0:
-        raise MalaError(rc, "mala_rotary_bwd")
-    return qo, ko, dwq, dwk
-
-
-def _packed(cu_q, cu_k, q, k):
-    _ints(cu_q, cu_k)
-    assert cu_q.shape == cu_k.shape and cu_q.dim() == 1 and q.shape[0] == 1
-    assert k is None or (k.shape[0] == 1 and k.shape[3] == q.shape[3])
-    return cu_q.numel() - 1
+    return _done(_native().rotary_bwd(dq, dk, *_rule(rot, norm), positions, None, None, q, k, dq_out, dk_out, weights), "mala_rotary_bwd")
 
 
 def rotary_varlen(q, k, cu_seqlens_q, cu_seqlens_k, rot: Rotary, norm: Optional[HeadNorm] = None, q_out=None, k_out=None):
     """mala_rotary_fwd_varlen: rotary on packed sequences, q [1,total_q,Hq,d], k [1,total_k,Hkv,d] (or None) with offsets int32 [B+1] on
     the device (the same tensor twice for self attention); positions count within a sequence's keys.  Returns (q', k')."""
-    one, total_q, Hq, d = q.shape
-    B = _packed(cu_seqlens_q, cu_seqlens_k, q, k)
-    total_k, Hkv = (total_q, 0) if k is None else k.shape[1:3]
-    qo, ko = _like(q, q_out), None if k is None else _like(k, k_out)
-    n, wq, wk = _norm_of(norm, d)
-    rc = lib().mala_rotary_fwd_varlen(_view(q, _TIn), _NO_IN if k is None else _view(k, _TIn), cu_seqlens_q.data_ptr(),
-                                      cu_seqlens_k.data_ptr(), ctypes.byref(rot.c), n, _view(qo, _TOut),
-                                      _NO_OUT if k is None else _view(ko, _TOut), B, Hq, Hkv, total_q, total_k, d,
-                                      _here(q, k, cu_seqlens_q, cu_seqlens_k, rot.inv_freq, qo, ko, wq, wk))
-    if rc != 0:
-        raise MalaError(rc, "mala_rotary_fwd_varlen")
-    return qo, ko
+    return _done(_native().rotary(q, k, *_rule(rot, norm), None, cu_seqlens_q, cu_seqlens_k, q_out, k_out), "mala_rotary_fwd_varlen")
 
 
 def rotary_varlen_bwd(dq, dk, cu_seqlens_q, cu_seqlens_k, rot: Rotary, norm: Optional[HeadNorm] = None, q=None, k=None, dq_out=None,
                       dk_out=None, weights: bool = True):
     """mala_rotary_bwd_varlen: as rotary_bwd, on packed sequences."""
-    one, total_q, Hq, d = dq.shape
-    B = _packed(cu_seqlens_q, cu_seqlens_k, dq, dk)
-    total_k, Hkv = (total_q, 0) if dk is None else dk.shape[1:3]
-    if norm is not None:
-        assert q is not None and q.shape == dq.shape and (dk is None or (k is not None and k.shape == dk.shape)), "with a norm: q and k"
-    else:
-        q = k = None
-    if dk is None:
-        k = None
-    qo, ko = _like(dq, dq_out), None if dk is None else _like(dk, dk_out)
-    n, wq, wk = _norm_of(norm, d)
-    dwq, dwk, ws = _rotary_grads(norm, d, dk is not None, weights, dq)
-    rc = lib().mala_rotary_bwd_varlen(_view(dq, _TIn), _NO_IN if dk is None else _view(dk, _TIn), _NO_IN if q is None else _view(q, _TIn),
-                                      _NO_IN if k is None else _view(k, _TIn), cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(),
-                                      ctypes.byref(rot.c), n, _view(qo, _TOut), _NO_OUT if dk is None else _view(ko, _TOut), _ptr(dwq),
-                                      _ptr(dwk), B, Hq, Hkv, total_q, total_k, d, _ptr(ws), 0 if ws is None else ws.numel(),
-                                      _here(dq, dk, q, k, cu_seqlens_q, cu_seqlens_k, rot.inv_freq, qo, ko, wq, wk))
-    if rc != 0:
-        raise MalaError(rc, "mala_rotary_bwd_varlen")
-    return qo, ko, dwq, dwk
-
-
-def _step(q, k, v, positions, slots, kpages, vpages, out, rot, norm):
-    """What the calls of a serving step check alike; (q_out, rows, Hq, Hkv, num_pages, page_size, d, norm, stream)."""
-    rows, Hq, d = q.shape
-    Hkv = k.shape[1]
-    assert k.shape == v.shape == (rows, Hkv, d) and slots.dtype is torch.int64 and slots.is_contiguous() and slots.shape == (rows,)
-    _ints(positions)
-    assert positions.shape == (rows,) and kpages.shape == vpages.shape and kpages.shape[2:] == (Hkv, d)
-    qo = _like(q, out)
-    n, wq, wk = _norm_of(norm, d)
-    return qo, rows, Hq, Hkv, kpages.shape[0], kpages.shape[1], d, n, _here(q, k, v, positions, slots, kpages, vpages, qo, rot.inv_freq, wq, wk)
-
-
-def _rows_out(t: torch.Tensor):
-    x = _rows(t)
-    return _TOut(x.p, 0, x.sn, x.sh)
+    return _done(_native().rotary_bwd(dq, dk, *_rule(rot, norm), None, cu_seqlens_q, cu_seqlens_k, q, k, dq_out, dk_out, weights),
+                 "mala_rotary_bwd_varlen")
 
 
 def rotary_write(q, k, v, positions, slots, kpages, vpages, rot: Rotary, norm: Optional[HeadNorm] = None, q_out=None):
     """mala_rotary_write: a serving step's rows q [rows,Hq,d], k, v [rows,Hkv,d] at positions int32 [rows]: k rotated into its slots
     (int64 [rows], negative: nowhere) of the bf16 pages [num_pages, page_size, Hkv, d], v into its own.  Returns q' (q_out may be q)."""
-    qo, rows, Hq, Hkv, num_pages, page_size, d, n, stream = _step(q, k, v, positions, slots, kpages, vpages, q_out, rot, norm)
-    rc = lib().mala_rotary_write(_rows(q), _rows(k), _rows(v), positions.data_ptr(), slots.data_ptr(), ctypes.byref(rot.c), n,
-                                 _rows_out(qo), _view(kpages, _TOut), _view(vpages, _TOut), rows, Hq, Hkv, num_pages, page_size, d, stream)
-    if rc != 0:
-        raise MalaError(rc, "mala_rotary_write")
-    return qo
+    return _done(_native().rotary_write(q, k, v, positions, slots, kpages, vpages, None, None, *_rule(rot, norm), q_out), "mala_rotary_write")
 
 
 def rotary_write_fp8(q, k, v, positions, slots, kpages8, vpages8, kscale, vscale, rot: Rotary, norm: Optional[HeadNorm] = None,
                      q_out=None):
     """mala_rotary_write_fp8: the same into e4m3 pages (uint8 or float8_e4m3fn) with their scales (see ``cache_write_fp8``)."""
-    qo, rows, Hq, Hkv, num_pages, page_size, d, n, _ = _step(q, k, v, positions, slots, kpages8, vpages8, q_out, rot, norm)
-    _scales(kscale, vscale, num_pages, Hkv, page_size)
-    kp, vp = _view8(kpages8), _view8(vpages8)
-    rc = lib().mala_rotary_write_fp8(_rows(q), _rows(k), _rows(v), positions.data_ptr(), slots.data_ptr(), ctypes.byref(rot.c), n,
-                                     _rows_out(qo), _TOut(kp.p, kp.sb, kp.sn, kp.sh), _TOut(vp.p, vp.sb, vp.sn, vp.sh),
-                                     kscale.data_ptr(), vscale.data_ptr(), rows, Hq, Hkv, num_pages, page_size, d,
-                                     _here(kscale, vscale))
-    if rc != 0:
-        raise MalaError(rc, "mala_rotary_write_fp8")
-    return qo
+    assert kscale is not None and vscale is not None, "expects scales of keys and of values"
+    return _done(_native().rotary_write(q, k, v, positions, slots, kpages8, vpages8, kscale, vscale, *_rule(rot, norm), q_out), "mala_rotary_write_fp8")
