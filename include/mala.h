@@ -421,6 +421,18 @@ int mala_fwd_paged_fp8(mala_tin q, mala_tin kpages8, mala_tin vpages8, const flo
 /* 0 for unsupported arguments */
 size_t mala_paged_fp8_workspace_bytes(int B, int Hkv, int total_k, int d);
 
+/* mala_fwd_paged_fp8 with the keys of every sequence cut into num_splits ranges of ceil(ceil(seqlen_k/128)/num_splits) blocks that run on
+ * different SMs, for few and short prompts behind long prefixes; test, merge and telemetry as in mala_fwd_chunk_split.
+ * Workspace: mala_paged_fp8_split_workspace_bytes.  B * num_splits <= 65535.  num_splits = 1 is mala_fwd_paged_fp8; the suggested count
+ * takes the lengths that the host knows, max_seqlen_k = min(max_pages_per_seq * page_size, total_k) (sm_count 0: the current device's). */
+int mala_fwd_paged_fp8_split(mala_tin q, mala_tin kpages8, mala_tin vpages8, const float* kscale, const float* vscale,
+                             const int32_t* cu_seqlens_q, const int32_t* block_table, const int32_t* seqlens_k, mala_tout o,
+                             float* lse, const mala_stats* st, int B, int Hq, int Hkv, int total_q, int max_seqlen_q, int total_k,
+                             int num_pages, int page_size, int max_pages_per_seq, int d, int causal, float scale, float tau,
+                             int num_splits, void* ws, size_t ws_bytes, void* cuda_stream);
+size_t mala_paged_fp8_split_workspace_bytes(int B, int Hq, int Hkv, int max_seqlen_q, int total_k, int d, int num_splits);
+int mala_paged_fp8_suggest_splits(int B, int Hq, int max_seqlen_q, int max_seqlen_k, int total_k, int sm_count);
+
 /* ---- Rotary positions ---------------------------------------------------------------------------------------------
  * The first `rotary` columns of a head's row (even, 2 .. d) are rotated in pairs by the angle position * inv_freq[i]: pair i is
  * the columns i and i + rotary / 2, or, interleaved != 0, 2 i and 2 i + 1:

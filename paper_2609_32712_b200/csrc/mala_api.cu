@@ -332,7 +332,7 @@ static int fwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse,
                     int scale_tiles = 0) {
   if (num_splits < 1) return MALA_ERR_INVALID_ARG;
   if (num_splits > 1) {
-    if (cu || num_splits > 65535 || (long long)B * num_splits > 65535) return MALA_ERR_UNSUPPORTED;
+    if ((cu && !kv_scales) || num_splits > 65535 || (long long)B * num_splits > 65535) return MALA_ERR_UNSUPPORTED;
     if (!ws) return MALA_ERR_INVALID_ARG;
     if ((((uintptr_t)ws) & 255) != 0) return MALA_ERR_MISALIGNED;
     if (B > 0 && Hq > 0 && N > 0 && head_size_ok(d, 256) &&
@@ -422,7 +422,12 @@ static int fwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse,
   }
   if (kv_scales) {
     p.kv_scales = kv_scales; p.scale_tiles = scale_tiles;
-    return scaled_launch_fwd(D, dense, one, tq, tk, tv, p, stream);
+    MALA_TRY(scaled_launch_fwd(D, dense, one, tq, tk, tv, p, stream));
+    if (num_splits == 1) return MALA_OK;
+    auto merge = D == 128 ? fwd_merge_splits_kernel<128, true> : fwd_merge_splits_kernel<64, true>;
+    return launch_dependent(merge, dim3((unsigned)((long long)((N + 7) / 8) * B * Hq)), dim3(256), stream, p.o_part, p.lse_part, p.o, p.o_sb, p.o_sn, p.o_sh,
+                            lse, Hq, N, num_splits, 0, 0, 0, 0, p.causal, d, cu, cu_k, total) == cudaSuccess
+               ? MALA_OK : MALA_ERR_CUDA;
   }
   if (D == 256) rc = launch_fwd<256>(dense, one, tq, tk, tv, p, stream);
   else if (D == 128) rc = launch_fwd<128>(dense, one, tq, tk, tv, p, stream);
@@ -431,7 +436,7 @@ static int fwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse,
   auto merge = D == 256 ? fwd_merge_splits_kernel<256> : D == 128 ? fwd_merge_splits_kernel<128> : fwd_merge_splits_kernel<64>;
   // (all rows in the grid's first coordinate: the others end at 65535, and B * Hq does not)
   return launch_dependent(merge, dim3((unsigned)((long long)((N + 7) / 8) * B * Hq)), dim3(256), stream, p.o_part, p.lse_part, p.o, p.o_sb, p.o_sn, p.o_sh,
-                          lse, Hq, N, num_splits, p.tps, p.Tk, p.koff, p.qshift, p.causal, d) == cudaSuccess
+                          lse, Hq, N, num_splits, p.tps, p.Tk, p.koff, p.qshift, p.causal, d, (const int*)nullptr, (const int*)nullptr, 0) == cudaSuccess
              ? MALA_OK : MALA_ERR_CUDA;
 }
 
@@ -585,11 +590,55 @@ size_t mala_paged_fp8_workspace_bytes(int B, int Hkv, int total_k, int d) {
   return 2 * up256((size_t)total_k * Hkv * d * 2) + up256((size_t)scale_tiles_of(B, total_k) * Hkv * 24 * sizeof(float)) + up256(((size_t)B + 1) * sizeof(int));
 }
 
+size_t mala_paged_fp8_split_workspace_bytes(int B, int Hq, int Hkv, int max_seqlen_q, int total_k, int d, int num_splits) {
+  const size_t keys = mala_paged_fp8_workspace_bytes(B, Hkv, total_k, d);
+  if (keys == 0 || Hq <= 0 || max_seqlen_q <= 0 || num_splits <= 0) return 0;
+  return keys + (num_splits > 1 ? fwd_split_workspace_bytes(B, Hq, max_seqlen_q, padded_head_size(d), num_splits) : 0);
+}
+
+// The count whose estimate is the lowest, if it is a tenth below that of one range.  Counted in key blocks of the kernel with two query blocks
+// per CTA (2 us), whose CTAs take as many plus three; the kernel with one walks them in 0.63 of that and takes the calls with no more blocks than
+// SMs.  A call takes as long as its longest range, or as its rounds of CTAs of average length; the merge 6 us, and its partials
+// come and go at 3.5 TB/s.  20 queries of 8 heads of 128 columns behind 8000 keys: 89 us in one range, 27 in eight; 500 of 32 heads behind 8000: 148, and 129 in
+// three; 2000 of 8 heads behind 30,000: 309, and 273 in two; 2048 of 32 heads behind 30,000: 1056 in one range, 1113 in two.
+int mala_paged_fp8_suggest_splits(int B, int Hq, int max_seqlen_q, int max_seqlen_k, int total_k, int sm_count) {
+  if (B <= 0 || Hq <= 0 || max_seqlen_q <= 0 || max_seqlen_k <= 0 || total_k <= 0) return MALA_ERR_INVALID_ARG;
+  if (sm_count <= 0) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sm_count <= 0)
+      return MALA_ERR_CUDA;
+  }
+  const double longest = (max_seqlen_k + 127ll) / 128, all = (total_k + 127ll) / 128;
+  const double pairs = (max_seqlen_q + 127ll + 255) / 256, blocks = (max_seqlen_q + 254ll) / 128, heads = (double)B * Hq;
+  auto estimate = [&](int S) {
+    const double merge = S > 1 ? 3 + heads * max_seqlen_q * S / 7000 : 0;
+    const double range = longest / S + 3;
+    if (blocks * heads * S <= sm_count) return 0.63 * range + merge;
+    const double rounds = ceil(pairs * heads * S / sm_count) * (all / B / S + 3);
+    return (rounds > range ? rounds : range) + merge;
+  };
+  int best = 1;
+  for (int S = 2; S <= 32 && S <= longest && (long long)B * S <= 65535; ++S)
+    if (estimate(S) < estimate(best)) best = S;
+  return estimate(best) < 0.9 * estimate(1) ? best : 1;
+}
+
 int mala_fwd_paged_fp8(mala_tin q, mala_tin kpages8, mala_tin vpages8, const float* kscale, const float* vscale, const int32_t* cu_seqlens_q,
                        const int32_t* block_table, const int32_t* seqlens_k, mala_tout o, float* lse, const mala_stats* st, int B, int Hq, int Hkv,
                        int total_q, int max_seqlen_q, int total_k, int num_pages, int page_size, int max_pages_per_seq, int d, int causal,
                        float scale, float tau, void* ws, size_t ws_bytes, void* cuda_stream) {
+  return mala_fwd_paged_fp8_split(q, kpages8, vpages8, kscale, vscale, cu_seqlens_q, block_table, seqlens_k, o, lse, st, B, Hq, Hkv, total_q,
+                                  max_seqlen_q, total_k, num_pages, page_size, max_pages_per_seq, d, causal, scale, tau, 1, ws, ws_bytes,
+                                  cuda_stream);
+}
+
+int mala_fwd_paged_fp8_split(mala_tin q, mala_tin kpages8, mala_tin vpages8, const float* kscale, const float* vscale, const int32_t* cu_seqlens_q,
+                             const int32_t* block_table, const int32_t* seqlens_k, mala_tout o, float* lse, const mala_stats* st, int B, int Hq, int Hkv,
+                             int total_q, int max_seqlen_q, int total_k, int num_pages, int page_size, int max_pages_per_seq, int d, int causal,
+                             float scale, float tau, int num_splits, void* ws, size_t ws_bytes, void* cuda_stream) {
   ApiScope scope("mala_fwd_paged_fp8", cuda_stream);
+  if (num_splits <= 0) return MALA_ERR_INVALID_ARG;
   MALA_TRY(check_packed(cu_seqlens_q, B, total_q, max_seqlen_q));
   if (!block_table || !seqlens_k || num_pages <= 0 || page_size <= 0 || max_pages_per_seq <= 0 || total_k <= 0) return MALA_ERR_INVALID_ARG;
   if ((long long)max_pages_per_seq * page_size > 0x7fffffffLL) return MALA_ERR_UNSUPPORTED;
@@ -601,8 +650,9 @@ int mala_fwd_paged_fp8(mala_tin q, mala_tin kpages8, mala_tin vpages8, const flo
   if (!lse || !ws) return MALA_ERR_INVALID_ARG;
   MALA_TRY(check_view(q.p, q.sb, q.sn, q.sh, 1, total_q, Hq));
   MALA_TRY(check_view(o.p, o.sb, o.sn, o.sh, 1, total_q, Hq));
-  const size_t bytes = mala_paged_fp8_workspace_bytes(B, Hkv, total_k, d);
-  if (bytes == 0) return MALA_ERR_UNSUPPORTED;
+  const size_t keys = mala_paged_fp8_workspace_bytes(B, Hkv, total_k, d);
+  const size_t bytes = mala_paged_fp8_split_workspace_bytes(B, Hq, Hkv, max_seqlen_q, total_k, d, num_splits);
+  if (keys == 0 || num_splits > 65535 || (long long)B * num_splits > 65535) return MALA_ERR_UNSUPPORTED;
   if ((((uintptr_t)ws) & 255) != 0) return MALA_ERR_MISALIGNED;
   if (ws_bytes < bytes) return MALA_ERR_WORKSPACE_TOO_SMALL;
   const size_t part = up256((size_t)total_k * Hkv * d * 2);
@@ -616,8 +666,8 @@ int mala_fwd_paged_fp8(mala_tin q, mala_tin kpages8, mala_tin vpages8, const flo
   MALA_TRY(cache_read_checked(kpages8, vpages8, kscale, vscale, block_table, seqlens_k, k, v, cu_k, B, Hkv, num_pages, page_size, max_pages_per_seq,
                               total_k, d, true, &cs, (cudaStream_t)cuda_stream));
   const mala_tin ki = {k.p, 0, k.sn, k.sh}, vi = {v.p, 0, v.sn, v.sh};
-  return scope.finish(fwd_impl(q, ki, vi, o, lse, st, B, Hq, Hkv, max_seqlen_q, max_k, d, causal, scale, tau, cuda_stream, cu_seqlens_q, total_q, 1, nullptr,
-                               0, cu_k, total_k, nullptr, nullptr, cs.out, cs.tiles));
+  return scope.finish(fwd_impl(q, ki, vi, o, lse, st, B, Hq, Hkv, max_seqlen_q, max_k, d, causal, scale, tau, cuda_stream, cu_seqlens_q, total_q, num_splits,
+                               (uint8_t*)ws + keys, ws_bytes - keys, cu_k, total_k, nullptr, nullptr, cs.out, cs.tiles));
 }
 
 int mala_bwd_varlen(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dout, const float* lse,

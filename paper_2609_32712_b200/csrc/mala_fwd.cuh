@@ -114,6 +114,9 @@ struct FwdCfg {
   static constexpr uint32_t kTmemCols = 512;
 };
 
+// Key blocks of one range of a packed sequence that is cut into num_splits ones
+__device__ __forceinline__ int range_of(int Tk, int num_splits) { return (Tk + num_splits - 1) / num_splits; }
+
 // kSmall: the keys and values lie in pages smaller than a tile (a kernel of its own, so that the copy loop with its
 // table lookups costs the other layouts nothing).  kBias: the scores carry a relative position bias (mala_bias.cuh): 282 us for 8192
 // tokens, causal, 16 heads on 4 KV heads of 128 columns, 64 buckets up to 2048 (275 GFLOP at 976 TFLOP/s; 238 without a bias), bound by
@@ -157,6 +160,9 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                                   : (p.cu_k ? __ldg(p.cu_k + b + 1) - krow0 : (p.cu ? Nq : p.Nk));
   // (with a bias the kernel is a dependent of the one that lays it out: the softmax warps wait for that, and blocks without work)
   auto settle = [&]() { if constexpr (kBias) wait_for_primary(); };
+  if constexpr (kScaled) {
+    if (Nq > p.N) return;                             // (longer than the partials' rows)
+  }
   if (own_keys && (Nkeys <= 0 || (p.causal && Nkeys < Nq))) {   // (not defined: no keys, more queries than keys)
     settle();
     if constexpr (kBias) empty_rows(p, b, h, row0, Nq, place.x * 256, 256);
@@ -197,8 +203,9 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   const int dB = p.causal ? iB + koff : Tk - 1;
   int jlo = 0, jhi = Tk - 1;                         // key blocks of this CTA
   if (p.num_splits > 1) {
-    jlo = sp * p.tps;
-    jhi = min(Tk, jlo + p.tps) - 1;
+    const int tps = kScaled ? range_of(Tk, p.num_splits) : p.tps;
+    jlo = sp * tps;
+    jhi = min(Tk, jlo + tps) - 1;
     if (jlo > dA) {                                  // the range holds no legal key of block A
       if (!hasB || jlo > dB) return;                 // ... nor of block B: nothing to do (the merge knows)
       iA = iB; dA = dB; hasB = false;                // only B's diagonal block: run B alone
@@ -874,16 +881,27 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
 // One warp per (b, head, row), eight rows per block: a partial is one or two 16-byte loads per lane, four ranges in
 // flight.  Bound by HBM and L2 (4 D bytes per row and range).  1000 x 16 rows of 256 columns in four ranges:
 // 44 us less per call than with a block per row and a thread per column, whose merge took 56 us.
-template <int D>
+// kPacked: sequences of cu_q, cu_k (N: rows of the longest), each cut into ranges of its own length.
+template <int D, bool kPacked = false>
 __global__ void __launch_bounds__(256)
 fwd_merge_splits_kernel(const float* __restrict__ o_part, const float* __restrict__ lse_part,
                         __nv_bfloat16* __restrict__ o, int64_t o_sb, int64_t o_sn, int64_t o_sh,
                         float* __restrict__ lse, int Hq, int N, int num_splits, int tps, int Tk, int koff, int qshift,
-                        int causal, int d) {
+                        int causal, int d, const int* __restrict__ cu_q, const int* __restrict__ cu_k, int total) {
   constexpr int L4 = D / 4, V = L4 > 32 ? L4 / 32 : 1;   // float4 per partial; per lane
   const int per = (N + 7) / 8, bh = blockIdx.x / per, h = bh % Hq, b = bh / Hq;   // blocks of eight rows per (b, head)
   const int lane = threadIdx.x & 31, row = (blockIdx.x - bh * per) * 8 + (threadIdx.x >> 5);
   if (row >= N) return;
+  if constexpr (kPacked) {
+    const int row0 = __ldg(cu_q + b), Nq = __ldg(cu_q + b + 1) - row0, Nkeys = __ldg(cu_k + b + 1) - __ldg(cu_k + b);
+    if (row >= Nq || Nq > N || Nkeys <= 0 || (causal && Nkeys < Nq)) return;   // (what the ranges leave out)
+    Tk = (Nkeys + 127) / 128;
+    tps = range_of(Tk, num_splits);
+    koff = (Nkeys - Nq) / 128;
+    qshift = (Nkeys - Nq) % 128;
+    o += (int64_t)row0 * o_sn - b * o_sb;
+    lse += (int64_t)h * total + row0 - (int64_t)bh * N;
+  }
   const int newest = causal ? (row + qshift) / 128 + koff : Tk - 1;
   const int ns = min(num_splits, newest / tps + 1);
   const size_t base = (size_t)bh * num_splits;

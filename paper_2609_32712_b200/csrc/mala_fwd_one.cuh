@@ -114,6 +114,9 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                                   : (p.cu_k ? __ldg(p.cu_k + b + 1) - krow0 : (p.cu ? Nq : p.Nk));
   // (with a bias the kernel is a dependent of the one that lays it out: the softmax warps wait for that, and blocks without work)
   auto settle = [&]() { if constexpr (kBias) wait_for_primary(); };
+  if constexpr (kScaled) {
+    if (Nq > p.N) return;
+  }
   if (own_keys && (Nkeys <= 0 || (p.causal && Nkeys < Nq))) {
     settle();
     if constexpr (kBias) empty_rows(p, b, h, row0, Nq, place.x * 128, 128);
@@ -130,8 +133,9 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   const int dI = p.causal ? i + koff : Tk - 1;       // newest key block with a legal key
   int jlo = 0, jhi = Tk - 1;                         // key blocks of this CTA
   if (p.num_splits > 1) {
-    jlo = sp * p.tps;
-    jhi = min(Tk, jlo + p.tps) - 1;
+    const int tps = kScaled ? range_of(Tk, p.num_splits) : p.tps;
+    jlo = sp * tps;
+    jhi = min(Tk, jlo + tps) - 1;
     if (jlo > dI) return;                            // no legal key in the range (the merge knows)
   }
   const int j0 = min(dI, jhi);                       // step u = 0 .. U-1 visits key block j0 - u

@@ -10,8 +10,9 @@ namespace mala {
 
 template <int D, bool kDense>
 static int launch_scaled_as(bool one, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const FwdParams& p, cudaStream_t stream) {
-  if (one) mala_fwd_one_kernel<D, kDense, false, false, true><<<dim3(p.Tr, p.Hq, p.B), FwdOneCfg<D>::kThreads, FwdOneCfg<D>::kSmemBytes, stream>>>(tq, tk, tv, p);
-  else mala_fwd_kernel<D, kDense, false, false, true><<<dim3((p.Tr + 1) / 2, p.Hq, p.B), FwdCfg<D, kDense>::kThreads, FwdCfg<D, kDense>::kSmemBytes, stream>>>(tq, tk, tv, p);
+  const int ranges = p.B * p.num_splits;
+  if (one) mala_fwd_one_kernel<D, kDense, false, false, true><<<dim3(p.Tr, p.Hq, ranges), FwdOneCfg<D>::kThreads, FwdOneCfg<D>::kSmemBytes, stream>>>(tq, tk, tv, p);
+  else mala_fwd_kernel<D, kDense, false, false, true><<<dim3((p.Tr + 1) / 2, p.Hq, ranges), FwdCfg<D, kDense>::kThreads, FwdCfg<D, kDense>::kSmemBytes, stream>>>(tq, tk, tv, p);
   return cudaGetLastError() == cudaSuccess ? MALA_OK : MALA_ERR_CUDA;
 }
 

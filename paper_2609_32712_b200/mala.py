@@ -133,7 +133,10 @@ def lib():
         L.mala_cache_read_fp8.argtypes = [_TIn, _TIn, vp, vp, vp, vp, _TOut, _TOut, vp] + [i] * 7 + [vp]
         L.mala_fwd_paged_fp8.argtypes = [_TIn, _TIn, _TIn, vp, vp, vp, vp, vp, _TOut, vp, ctypes.POINTER(_Stats)] + [i] * 11 + \
             [f, f, vp, sz, vp]
+        L.mala_fwd_paged_fp8_split.argtypes = L.mala_fwd_paged_fp8.argtypes[:24] + [i] + L.mala_fwd_paged_fp8.argtypes[24:]
         L.mala_paged_fp8_workspace_bytes.argtypes = [i] * 4
+        L.mala_paged_fp8_split_workspace_bytes.argtypes = [i] * 7
+        L.mala_paged_fp8_suggest_splits.argtypes, L.mala_paged_fp8_suggest_splits.restype = [i] * 6, i
         rp, np_ = ctypes.POINTER(_Rotary), ctypes.POINTER(_HeadNorm)
         L.mala_rotary_fwd.argtypes = [_TIn, _TIn, vp, rp, np_, _TOut, _TOut] + [i] * 6 + [vp]
         L.mala_rotary_bwd.argtypes = [_TIn, _TIn, _TIn, _TIn, vp, rp, np_, _TOut, _TOut, vp, vp] + [i] * 6 + [vp, sz, vp]
@@ -142,9 +145,9 @@ def lib():
         L.mala_rotary_write.argtypes = [_TIn, _TIn, _TIn, vp, vp, rp, np_, _TOut, _TOut, _TOut] + [i] * 6 + [vp]
         L.mala_rotary_write_fp8.argtypes = [_TIn, _TIn, _TIn, vp, vp, rp, np_, _TOut, _TOut, _TOut, vp, vp] + [i] * 6 + [vp]
         L.mala_rotary_workspace_bytes.argtypes = [i]
-        for n in ("mala_paged_fp8_workspace_bytes", "mala_rotary_workspace_bytes"):
+        for n in ("mala_paged_fp8_workspace_bytes", "mala_paged_fp8_split_workspace_bytes", "mala_rotary_workspace_bytes"):
             getattr(L, n).restype = sz
-        for n in ("mala_page_tables_positions", "mala_cache_read", "mala_cache_read_fp8", "mala_fwd_paged_fp8", "mala_rotary_fwd",
+        for n in ("mala_page_tables_positions", "mala_cache_read", "mala_cache_read_fp8", "mala_fwd_paged_fp8", "mala_fwd_paged_fp8_split", "mala_rotary_fwd",
                   "mala_rotary_bwd", "mala_rotary_fwd_varlen", "mala_rotary_bwd_varlen", "mala_rotary_write", "mala_rotary_write_fp8"):
             getattr(L, n).restype = i
         L.mala_test_expire_wait.argtypes = [ctypes.c_longlong, vp]
@@ -893,10 +896,15 @@ def cache_read_fp8(kpages8, vpages8, kscale, vscale, block_table, seqlens, rows:
     return _done(_native().cache_read(kpages8, vpages8, kscale, vscale, block_table, seqlens, rows), "mala_cache_read_fp8")
 
 
+def _suggested_splits(*lengths) -> int:
+    return max(1, lib().mala_paged_fp8_suggest_splits(*lengths, 0))     # (of lengths that the call refuses: 1)
+
+
 def fwd_paged_fp8(q, kpages8, vpages8, kscale, vscale, cu_seqlens_q, block_table, seqlens_k, max_seqlen_q: int, total_k: int,
-                  scale: float, tau: float, causal: bool = True, stats: bool = False, ws=None):
-    """mala_fwd_paged_fp8: ``fwd_paged`` over e4m3 pages with their scales; total_k: at least the sum of seqlens_k (room in the
-    workspace).  Returns (o, lse [Hq,total_q], Stats or None)."""
+                  scale: float, tau: float, causal: bool = True, stats: bool = False, ws=None, num_splits: Optional[int] = None):
+    """mala_fwd_paged_fp8(_split): ``fwd_paged`` over e4m3 pages with their scales; total_k: at least the sum of seqlens_k (room in the
+    workspace).  num_splits: ranges that a sequence's keys are cut into, each with a skip test of its own (None: with tau 0, where that
+    gives the same, and no ws of the caller's as many as the library suggests, else 1).  Returns (o, lse [Hq,total_q], Stats or None)."""
     one, total_q, Hq, d = q.shape
     num_pages, page_size, Hkv = kpages8.shape[0], kpages8.shape[1], kpages8.shape[2]
     B, max_pages = block_table.shape
@@ -908,11 +916,13 @@ def fwd_paged_fp8(q, kpages8, vpages8, kscale, vscale, cu_seqlens_q, block_table
     lse = q.new_empty((Hq, total_q), dtype=_F32)
     Tq, Tk = -(-(max_seqlen_q + 127) // 128), -(-min(max_pages * page_size, total_k) // 128)
     st = Stats((B, Hq, Tq), -(-Tk // 32), q.device) if stats else None
-    ws = _ws(int(lib().mala_paged_fp8_workspace_bytes(B, Hkv, total_k, d)), q.device) if ws is None else ws
-    rc = lib().mala_fwd_paged_fp8(_view(q, _TIn), _view8(kpages8), _view8(vpages8), kscale.data_ptr(), vscale.data_ptr(),
+    if num_splits is None:
+        num_splits = 1 if tau != 0.0 or ws is not None else _suggested_splits(B, Hq, max_seqlen_q, min(max_pages * page_size, total_k), total_k)
+    ws = _ws(int(lib().mala_paged_fp8_split_workspace_bytes(B, Hq, Hkv, max_seqlen_q, total_k, d, num_splits)), q.device) if ws is None else ws
+    rc = lib().mala_fwd_paged_fp8_split(_view(q, _TIn), _view8(kpages8), _view8(vpages8), kscale.data_ptr(), vscale.data_ptr(),
                                   cu_seqlens_q.data_ptr(), block_table.data_ptr(), seqlens_k.data_ptr(), _view(o, _TOut),
                                   lse.data_ptr(), ctypes.byref(st.c) if st else None, B, Hq, Hkv, total_q, max_seqlen_q, total_k,
-                                  num_pages, page_size, max_pages, d, int(causal), scale, tau, ws.data_ptr(), ws.numel(),
+                                  num_pages, page_size, max_pages, d, int(causal), scale, tau, num_splits, ws.data_ptr(), ws.numel(),
                                   _here(q, kpages8, vpages8, kscale, vscale, cu_seqlens_q, block_table, seqlens_k, ws))
     if rc != 0:
         raise MalaError(rc, "mala_fwd_paged_fp8")

@@ -253,6 +253,72 @@ def test_prompts_that_skip(mala, ps, Hq, Hkv, d, new):
     assert ((o.double() - o2.double()).norm() <= 2.0 ** -8 * 2 * o2.double().norm()) and ((lse - lse2).abs() <= 2.0 ** -20 * (1 + lse2.abs())).all()
 
 
+@pytest.mark.parametrize("splits", [2, 5, 33])
+@pytest.mark.parametrize("lens,new", PROMPTS)
+@pytest.mark.parametrize("ps,Hq,Hkv,d", [(64, 4, 2, 64), (128, 8, 2, 128), (16, 2, 2, 96)])
+def test_prompts_in_ranges(mala, lens, new, ps, Hq, Hkv, d, splits):
+    """Keys cut into ranges: the tolerances of test_prompts (the merge adds a few roundings in fp32), rows that belong to no sequence
+    left as they were, and nothing read that this call did not write."""
+    (kp, vp), (ks, vs), table = _cache(11, True, lens, ps, Hkv, d)
+    cu = [sum(new[:b]) for b in range(len(new) + 1)]
+    q = _randn(4, 1, cu[-1], Hq, d)
+    scale, total = 1 / math.sqrt(d), sum(lens)
+    ws = torch.full((int(mala.lib().mala_paged_fp8_split_workspace_bytes(len(lens), Hq, Hkv, max(new), total, d, splits)),), 0xff, dtype=torch.uint8, device="cuda")
+    o, lse, st = mala.fwd_paged_fp8(q, kp, vp, ks, vs, _i32(cu), table, _i32(lens), max(new), total, scale, 0.0, stats=True, ws=ws, num_splits=splits)
+    whole = mala.fwd_paged_fp8(q, kp, vp, ks, vs, _i32(cu), table, _i32(lens), max(new), total, scale, 0.0, stats=True, num_splits=1)[2]
+    assert mala.device_status() == 0 and torch.equal(st.totals, whole.totals) and torch.equal(st.bitmask, whole.bitmask) and torch.equal(st.retained, whole.retained)
+    for b, (k, v) in enumerate(_keys(kp, vp, ks, vs, table, lens, ps)[:6]):
+        for h in range(Hq if new[b] else 0):
+            qd = q[0, cu[b]:cu[b + 1], h].double()
+            w, z, a = R.attention(qd, k[:, h // (Hq // Hkv)], v[:, h // (Hq // Hkv)], scale)
+            parity.check_output(o[0, cu[b]:cu[b + 1], h].double().cpu().numpy(), w.cpu().numpy(), a_ref=a.cpu().numpy())
+            most = (qd.abs() @ k[:, h // (Hq // Hkv)].abs().T).amax(1) * scale
+            err = (lse[h, cu[b]:cu[b + 1]].double() - z).abs()
+            assert (err <= (d + 4) * 2.0 ** -24 * most + 2.0 ** -20 * (1 + z.abs())).all(), err.max().item()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("ps,Hq,Hkv,d,new,splits", [(64, 4, 2, 64, 300, 3), (128, 8, 2, 128, 1500, 4), (16, 2, 2, 96, 40, 7)])
+def test_prompts_in_ranges_that_skip(mala, ps, Hq, Hkv, d, new, splits, causal):
+    """Every range has a skip test of its own: the tiles that mala_fwd_chunk_split skips over the same values."""
+    lens, scale, tau = [2500], 1.0, 1e-3
+    (kp, vp), (ks, vs), table = _cache(17, True, lens, ps, Hkv, d)
+    ks, vs = torch.full_like(ks, 2.0 ** -7), torch.full_like(vs, 2.0 ** -8)
+    k, v, _ = mala.cache_read_fp8(kp, vp, ks, vs, table, _i32(lens), 2500)
+    q = k[:, 2500 - new:].repeat_interleave(Hq // Hkv, 2).contiguous()
+    o, lse, st = mala.fwd_paged_fp8(q, kp, vp, ks, vs, _i32([0, new]), table, _i32(lens), new, 2500, scale, tau, causal=causal, stats=True, num_splits=splits)
+    o2, lse2, st2 = mala.fwd_chunk_split(q, k, v, scale, tau, splits, causal=causal, stats=True)
+    T, Q = min(st.bitmask.shape[-1], st2.bitmask.shape[-1]), min(st.bitmask.shape[-2], st2.bitmask.shape[-2])
+    assert torch.equal(st.bitmask[..., :Q, :T], st2.bitmask[..., :Q, :T]) and torch.equal(st.totals, st2.totals)
+    assert int(st.totals[0]) < int(st.totals[1])
+    assert ((o.double() - o2.double()).norm() <= 2.0 ** -8 * 2 * o2.double().norm()) and ((lse - lse2[0]).abs() <= 2.0 ** -20 * (1 + lse2[0].abs())).all()
+
+
+def test_ranges_leave_rows_and_refuse(mala):
+    """Sequences without keys and with more queries than keys keep their rows; counts that the call refuses, and workspaces too small for them."""
+    lens, new, ps, Hq, Hkv, d = [0, 500, 30, 257], [5, 40, 31, 257], 64, 4, 2, 64
+    (kp, vp), (ks, vs), table = _cache(11, True, lens, ps, Hkv, d)
+    cu = _i32([0, 5, 45, 76, 333])
+    q = _randn(4, 1, 340, Hq, d)
+    L, need = mala.lib(), int(mala.lib().mala_paged_fp8_split_workspace_bytes(4, Hq, Hkv, 257, 787, d, 3))
+    o, lse, ws = torch.full_like(q, 7.0), torch.full((Hq, 340), 7.0, device="cuda"), torch.full((need,), 0xff, dtype=torch.uint8, device="cuda")
+
+    def call(splits=3, bytes_=need, B=4):
+        return L.mala_fwd_paged_fp8_split(mala._view(q, mala._TIn), mala._view8(kp), mala._view8(vp), ks.data_ptr(), vs.data_ptr(), cu.data_ptr(), table.data_ptr(),
+                                          _i32(lens).data_ptr(), mala._view(o, mala._TOut), lse.data_ptr(), None, B, Hq, Hkv, 340, 257, 787, kp.shape[0], ps,
+                                          table.shape[1], d, 1, 0.1, 0.0, splits, ws.data_ptr(), bytes_, torch.cuda.current_stream().cuda_stream)
+    for kw, code in ((dict(splits=0), -1), (dict(splits=-1), -1), (dict(splits=20000), -2), (dict(bytes_=need - 1), -4), (dict(splits=4), -4)):
+        assert call(**kw) == code, kw
+    assert (o == 7).all() and (lse == 7).all()
+    assert call() == 0 and mala.device_status() == 0
+    for a, b in ((0, 5), (45, 76), (333, 340)):
+        assert (o[:, a:b] == 7).all() and (lse[:, a:b] == 7).all()
+    ref = mala.fwd_paged_fp8(q, kp, vp, ks, vs, cu, table, _i32(lens), 257, 787, 0.1, 0.0, num_splits=1)
+    for a, b in ((5, 45), (76, 333)):
+        assert ((o[:, a:b].double() - ref[0][:, a:b].double()).norm() <= 2.0 ** -8 * 2 * ref[0][:, a:b].double().norm())
+        assert ((lse[:, a:b] - ref[1][:, a:b]).abs() <= 2.0 ** -20 * (1 + ref[1][:, a:b].abs())).all()
+
+
 @pytest.mark.parametrize("which", ["k", "v"])
 @pytest.mark.parametrize("value", [0.0, -0.01, 1e-30, 1e25, 2.0 ** -61, 2.0 ** -60])
 def test_prompts_with_far_scales(mala, which, value):

@@ -238,3 +238,18 @@ def test_autograd_entry_points_refuse(mala):
               lambda: A.rotary_packed(q, q, None, None, r, q_weight=w), lambda: A.mala_attention_rotary_packed(q, q, q, None, None, 4, 4, r, 0.0, q_weight=w)):
         with pytest.raises(AssertionError):
             f()
+
+
+def test_suggested_ranges(mala):
+    f = mala.lib().mala_paged_fp8_suggest_splits
+    for bad in ((0, 8, 1, 1, 1), (1, 0, 1, 1, 1), (1, 8, 0, 1, 1), (1, 8, 1, 0, 1), (1, 8, 1, 1, 0)):
+        assert f(*bad, 148) == -1
+    assert f(1, 32, 2048, 30000, 30000, 148) == 1                                # as many CTAs as fill the SMs
+    assert f(1, 8, 20, 8000, 8000, 148) == 9                                     # 16 blocks of queries
+    assert f(1, 8, 20, 100, 100, 148) == 1                                       # one key block
+    assert 2 <= f(1, 1, 1, 2 ** 31 - 1, 2 ** 31 - 1, 148) <= 32
+    assert f(65535, 8, 1, 8000, 8000, 148) == 1                                  # (the grid's third coordinate)
+    need, split = mala.lib().mala_paged_fp8_workspace_bytes, mala.lib().mala_paged_fp8_split_workspace_bytes
+    assert split(2, 4, 2, 40, 64, 128, 1) == need(2, 2, 64, 128)
+    assert split(2, 4, 2, 40, 64, 100, 3) == 0 and split(2, 4, 2, 0, 64, 128, 3) == 0 and split(2, 4, 2, 40, 64, 128, 0) == 0
+    assert split(2, 4, 2, 40, 64, 96, 3) == need(2, 2, 64, 96) + 2 * 4 * 3 * 40 * (128 + 1) * 4
