@@ -107,25 +107,25 @@ def _weight_grads(dwq, dwk, q_weight, k_weight):
 
 
 class _RotaryPositions(torch.autograd.Function):
-    """q and k rotated; packed: (cu_q, cu_k), else positions or None."""
+    """q and k rotated; packed: (cu_q, cu_k), else positions or None (saved like the other tensors, so that a change in place is noticed)."""
 
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, rot, positions, packed, eps):
         norm = _head_norm(eps, q_weight, k_weight)
         qo, ko = mala.rotary_varlen(q, k, *packed, rot, norm) if packed else mala.rotary(q, k, rot, positions, norm)
-        ctx.save_for_backward(*((q, k) if norm else (None, None)), q_weight, k_weight)
-        ctx.args = (rot, positions, packed, eps)
+        ctx.save_for_backward(*((q, k) if norm else (None, None)), q_weight, k_weight, positions, *(packed or (None, None)), rot.inv_freq)
+        ctx.args = (rot, eps)
         return qo, ko
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dq, dk):
-        q, k, q_weight, k_weight = ctx.saved_tensors
-        rot, positions, packed, eps = ctx.args
+        q, k, q_weight, k_weight, positions, cu_q, cu_k, _ = ctx.saved_tensors
+        rot, eps = ctx.args
         norm, weights = _head_norm(eps, q_weight, k_weight), any(ctx.needs_input_grad[2:4])
         dq, dk = _incoming(dq), _incoming(dk)
-        if packed:
-            dq, dk, dwq, dwk = mala.rotary_varlen_bwd(dq, dk, *packed, rot, norm, q, k, weights=weights)
+        if cu_q is not None:
+            dq, dk, dwq, dwk = mala.rotary_varlen_bwd(dq, dk, cu_q, cu_k, rot, norm, q, k, weights=weights)
         else:
             dq, dk, dwq, dwk = mala.rotary_bwd(dq, dk, rot, positions, norm, q, k, weights=weights)
         return (dq, dk, *_weight_grads(dwq, dwk, q_weight, k_weight), None, None, None, None)
@@ -143,20 +143,21 @@ class _MalaAttentionRotary(torch.autograd.Function):
         else:
             qr, kr = mala.rotary(q, k, rot, positions, norm)
             o, lse, _ = mala.fwd_chunk(qr, kr, v, scale, tau, causal=causal)
-        ctx.save_for_backward(qr, kr, v, o, lse, *((q, k) if norm else (None, None)), q_weight, k_weight)
-        ctx.args = (rot, positions, packed, eps, tau, scale, causal)
+        ctx.save_for_backward(qr, kr, v, o, lse, *((q, k) if norm else (None, None)), q_weight, k_weight, positions, *(packed[:2] if packed else (None, None)),
+                              rot.inv_freq)
+        ctx.args = (rot, packed and packed[2:], eps, tau, scale, causal)
         return o
 
     @staticmethod
     @once_differentiable
     def backward(ctx, do):
-        qr, kr, v, o, lse, q, k, q_weight, k_weight = ctx.saved_tensors
-        rot, positions, packed, eps, tau, scale, causal = ctx.args
+        qr, kr, v, o, lse, q, k, q_weight, k_weight, positions, cu_q, cu_k, _ = ctx.saved_tensors
+        rot, most, eps, tau, scale, causal = ctx.args
         norm, weights = _head_norm(eps, q_weight, k_weight), any(ctx.needs_input_grad[3:5])
         do = _incoming(do)
-        if packed:
-            dq, dk, dv, _ = mala.bwd_varlen_prefix(qr, kr, v, o, do, lse, *packed, scale, tau, causal=causal)
-            dq, dk, dwq, dwk = mala.rotary_varlen_bwd(dq, dk, *packed[:2], rot, norm, q, k, dq_out=dq, dk_out=dk, weights=weights)
+        if cu_q is not None:
+            dq, dk, dv, _ = mala.bwd_varlen_prefix(qr, kr, v, o, do, lse, cu_q, cu_k, *most, scale, tau, causal=causal)
+            dq, dk, dwq, dwk = mala.rotary_varlen_bwd(dq, dk, cu_q, cu_k, rot, norm, q, k, dq_out=dq, dk_out=dk, weights=weights)
         else:
             dq, dk, dv, _ = mala.bwd_chunk(qr, kr, v, o, do, lse, scale, tau, causal=causal)
             dq, dk, dwq, dwk = mala.rotary_bwd(dq, dk, rot, positions, norm, q, k, dq_out=dq, dk_out=dk, weights=weights)

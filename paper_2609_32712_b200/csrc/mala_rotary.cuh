@@ -56,7 +56,6 @@ __device__ __forceinline__ int partner_of(int c, int rotary) {
 
 // bf16 pairs as fp32 side by side, and back
 __device__ __forceinline__ uint64_t pair_of(uint32_t w) { return f2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-__device__ __forceinline__ uint64_t crossed_pair_of(uint32_t w) { return f2(__uint_as_float(w & 0xffff0000u), __uint_as_float(w << 16)); }
 __device__ __forceinline__ void pairs_of(const uint4& w, uint64_t (&x)[4]) { x[0] = pair_of(w.x); x[1] = pair_of(w.y); x[2] = pair_of(w.z); x[3] = pair_of(w.w); }
 __device__ __forceinline__ uint4 rows_of(const uint64_t (&x)[4]) { return make_uint4(f2_bf16(x[0]), f2_bf16(x[1]), f2_bf16(x[2]), f2_bf16(x[3])); }
 __device__ __forceinline__ float f2_sum(uint64_t x) {

@@ -426,3 +426,62 @@ def test_a_serving_run_at_rotary_positions(mala, fp8):
                     assert err <= (2 * 2.0 ** -4 if fp8 else 4 * 2.0 ** -8), (step, b, h, err.item())
             at += n
     assert mala.device_status() == 0
+
+
+def test_a_captured_serving_step(mala):
+    """Tables, rotated write and prompts over the e4m3 cache, and the read back, captured once and replayed step by step while the same step runs
+    eagerly on another stream: bit for bit the same tables, pages, scales and outputs."""
+    ps, Hq, Hkv, d, B, width, pool, rows = 64, 8, 2, 128, 3, 30, 90, 6
+    rot = mala.Rotary(mala.rotary_frequencies(128)[0])
+    norm = mala.HeadNorm(_randn(1, d) * 0.2 + 1, _randn(2, d) * 0.2 + 1, 1e-5)
+
+    def state():
+        return dict(table=torch.full((B, width), -1, dtype=torch.int32, device="cuda"), free=torch.arange(pool, dtype=torch.int32, device="cuda"), count=_i32([pool]),
+                    lens=_i32([0] * B), pages=[torch.zeros((pool, ps, Hkv, d), dtype=torch.uint8, device="cuda") for _ in range(2)],
+                    scales=[torch.ones((pool, Hkv, 1), device="cuda") for _ in range(2)])
+
+    def step(s, new, x, rows, most, total):
+        cu, lens, slots, count, pos = mala.page_tables(s["lens"], new, s["table"], s["free"], s["count"], ps, rows, positions=True)
+        q, k, v = x.split([Hq, Hkv, Hkv], 1)
+        qr = mala.rotary_write_fp8(q, k, v, pos, slots, *s["pages"], *s["scales"], rot, norm=norm)
+        o, lse, _ = mala.fwd_paged_fp8(qr[None], *s["pages"], *s["scales"], cu, s["table"], lens, most, total, 0.1, 0.0)
+        read = mala.cache_read_fp8(*s["pages"], *s["scales"], s["table"], lens, total)
+        s["lens"].copy_(lens)
+        s["count"].copy_(count)
+        return qr, o, lse, pos, slots, read[2], read[0][:, :total - 128], read[1][:, :total - 128]
+    total = 2200
+    first = _randn(5, 2000, Hq + 2 * Hkv, d)
+    a, b = state(), state()
+    for s in (a, b):
+        step(s, _i32([1500, 100, 400]), first, 2000, 1500, 2400)
+    for t, u in zip([a["table"], a["lens"], *a["pages"], *a["scales"]], [b["table"], b["lens"], *b["pages"], *b["scales"]]):
+        assert torch.equal(t, u)
+    x, new = _randn(6, rows, Hq + 2 * Hkv, d), _i32([2, 1, 3])
+    side, other, graph = torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    held = {n: [t.clone() for t in (v if isinstance(v, list) else [v])] for n, v in a.items()}
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(a, new, x, rows, 4, total)
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            out = step(a, new, x, rows, 4, total)
+    for n, v in a.items():                 # (back to where the other one is)
+        for t, u in zip(v if isinstance(v, list) else [v], held[n]):
+            t.copy_(u)
+    for i, counts in enumerate([[2, 1, 3], [1, 4, 1], [0, 3, 3], [4, 0, 2]]):
+        x.copy_(_randn(20 + i, rows, Hq + 2 * Hkv, d))
+        new.copy_(_i32(counts))
+        mine, mine_new = x.clone(), new.clone()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            want = step(b, mine_new, mine, rows, 4, total)
+        graph.replay()
+        torch.cuda.synchronize()
+        held_rows = int(a["lens"].sum())
+        for j, (t, u) in enumerate(zip(out, want)):
+            if j >= 6:                     # (rows behind the last sequence are not written)
+                t, u = t[:, :held_rows], u[:, :held_rows]
+            assert torch.equal(t, u), (i, j)
+        for t, u in zip([a["table"], a["lens"], *a["pages"], *a["scales"]], [b["table"], b["lens"], *b["pages"], *b["scales"]]):
+            assert torch.equal(t, u)
+    assert mala.device_status() == 0

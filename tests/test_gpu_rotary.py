@@ -92,7 +92,7 @@ def test_forward_and_backward(mala, d, rotary, interleaved, normed):
 
 
 @pytest.mark.parametrize("B,N,Hq,Hkv,d", [(1, 1, 1, 1, 128), (1, 1, 32, 8, 128), (3, 700, 5, 1, 64), (1, 6001, 33, 8, 128), (70000, 1, 2, 1, 16), (1, 9, 300, 17, 256),
-                                          (2, 20000, 3, 2, 32)])
+                                          (2, 20000, 3, 2, 32), (1, 12000, 16, 4, 256)])    # (the last one: more than a round of blocks)
 @pytest.mark.parametrize("normed", [False, True])
 def test_sizes(mala, B, N, Hq, Hkv, d, normed):
     rot, norm = _rule(mala, d), _norm(mala, d, 3) if normed else None
@@ -222,7 +222,7 @@ def test_rows_of_zeros(mala):
 # ---- packed sequences
 
 @pytest.mark.parametrize("lens_q,lens_k,behind", [([3, 1, 0, 40, 7], None, 0), ([3, 1, 0, 40, 7], [10, 1, 5, 200, 7], 6), ([1], None, 3), ([0, 0, 2], [4, 0, 2], 1),
-                                                  ([5] * 300, [9] * 300, 0)])
+                                                  ([5] * 300, [9] * 300, 0), ([2, 0, 5] * 220, None, 2), ([2, 0, 5] * 220, [4, 1, 5] * 220, 0)])
 @pytest.mark.parametrize("normed", [False, True])
 def test_packed(mala, lens_q, lens_k, behind, normed):
     """Bit for bit the single calls; rows behind the last sequence as they are, and without a part in the weights' gradients."""
@@ -396,6 +396,24 @@ def test_wrapper_refuses(mala):
     for f in (lambda: mala.rotary(q, q[:, :4], rot), lambda: mala.rotary(q, None, _rule(mala, 66)), lambda: mala.rotary(q.expand(1, 8, 2, 64)[:, :1].expand(1, 8, 2, 64), None, rot)):
         with pytest.raises(mala.MalaError):
             f()
+
+
+@pytest.mark.parametrize("attention", [False, True])
+def test_changes_before_the_backward_pass_are_noticed(mala, attention):
+    """Positions, offsets and frequencies belong to the gradient: changed in place before it is asked for, they raise."""
+    from paper_2609_32712_b200 import autograd as A
+    for packed in (False, True):
+        for which in (0, 1):
+            rot = _rule(mala, 64)
+            q, k, v = (_randn(x, 1, 40, 2, 64).requires_grad_(True) for x in range(3))
+            pos, cu = torch.arange(40, dtype=torch.int32, device="cuda")[None].contiguous(), _i32([0, 15, 40])
+            if attention:
+                o = A.mala_attention_rotary_packed(q, k, v, cu, cu, 25, 25, rot, 0.0) if packed else A.mala_attention_rotary(q, k, v, rot, 0.0, pos)
+            else:
+                o = A.rotary_packed(q, k, cu, cu, rot)[0] if packed else A.rotary(q, k, rot, pos)[0]
+            (rot.inv_freq if which else cu if packed else pos).add_(1)
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                o.sum().backward()
 
 
 # ---- a serving step
