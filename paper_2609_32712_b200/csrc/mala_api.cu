@@ -329,7 +329,7 @@ static int fwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse,
                     const int32_t* cu = nullptr, int total = 0, int num_splits = 1, void* ws = nullptr,
                     size_t ws_bytes = 0, const int32_t* cu_k = nullptr, int total_k = 0,
                     const FwdPaging* pg = nullptr, const mala_rel_bias* bias = nullptr, const float* kv_scales = nullptr,
-                    int scale_tiles = 0) {
+                    int scale_tiles = 0, bool whole_scales = false) {
   if (num_splits < 1) return MALA_ERR_INVALID_ARG;
   if (num_splits > 1) {
     if ((cu && !kv_scales) || num_splits > 65535 || (long long)B * num_splits > 65535) return MALA_ERR_UNSUPPORTED;
@@ -422,7 +422,7 @@ static int fwd_impl(mala_tin q, mala_tin k, mala_tin v, mala_tout o, float* lse,
   }
   if (kv_scales) {
     p.kv_scales = kv_scales; p.scale_tiles = scale_tiles;
-    MALA_TRY(scaled_launch_fwd(D, dense, one, tq, tk, tv, p, stream));
+    MALA_TRY(scaled_launch_fwd(D, dense, one, whole_scales, tq, tk, tv, p, stream));
     if (num_splits == 1) return MALA_OK;
     auto merge = D == 128 ? fwd_merge_splits_kernel<128, true> : fwd_merge_splits_kernel<64, true>;
     return launch_dependent(merge, dim3((unsigned)((long long)((N + 7) / 8) * B * Hq)), dim3(256), stream, p.o_part, p.lse_part, p.o, p.o_sb, p.o_sn, p.o_sh,
@@ -667,7 +667,7 @@ int mala_fwd_paged_fp8_split(mala_tin q, mala_tin kpages8, mala_tin vpages8, con
                               total_k, d, true, &cs, (cudaStream_t)cuda_stream));
   const mala_tin ki = {k.p, 0, k.sn, k.sh}, vi = {v.p, 0, v.sn, v.sh};
   return scope.finish(fwd_impl(q, ki, vi, o, lse, st, B, Hq, Hkv, max_seqlen_q, max_k, d, causal, scale, tau, cuda_stream, cu_seqlens_q, total_q, num_splits,
-                               (uint8_t*)ws + keys, ws_bytes - keys, cu_k, total_k, nullptr, nullptr, cs.out, cs.tiles));
+                               (uint8_t*)ws + keys, ws_bytes - keys, cu_k, total_k, nullptr, nullptr, cs.out, cs.tiles, page_size >= 128));
 }
 
 int mala_bwd_varlen(mala_tin q, mala_tin k, mala_tin v, mala_tin o, mala_tin dout, const float* lse,

@@ -76,6 +76,12 @@ __device__ __forceinline__ float kv_scales_of(const FwdParams& p, int hkv, int b
   const float s = __ldg(p.kv_scales + ((size_t)hkv * p.scale_tiles + krow0 / 128 + b + j) * 24 + lane);
   return lane < 8 ? s * c2 : s;
 }
+// A key block of one scale: the keys' (times c2), log2 of the values', and its inverse
+__device__ __forceinline__ void whole_scales(float sc, float& key, float& value, float& back) {
+  key = __shfl_sync(0xffffffffu, sc, 0);
+  value = __shfl_sync(0xffffffffu, sc, 8);
+  back = __shfl_sync(0xffffffffu, sc, 16);
+}
 // Largest of 32 scores, two groups of 16 with scales of their own (lanes g and g + 1 of sc)
 __device__ __forceinline__ float scaled_max(const uint32_t (&s)[32], float sc, int g) {
   float m[2];
@@ -124,8 +130,9 @@ __device__ __forceinline__ int range_of(int Tk, int num_splits) { return (Tk + n
 //
 // kScaled: keys and values are codes of a cache, whole numbers of their scales, and the scales (one per 16 keys) come in here: a key's is the
 // factor of its score in the maximum and in the exponential's argument; a value's is a summand there, P then carries it, and
-// the row's sum takes it out again.  So nothing is rounded that a cache of wider values would not round.
-template <int D, bool kDense, bool kSmall = false, bool kBias = false, bool kScaled = false>
+// the row's sum takes it out again.  So nothing is rounded that a cache of wider values would not round.  1: scales of 16 keys each; 2: one per key
+// block (pages of whole ones), then a factor, a summand and an inverse per tile in place of eight each.
+template <int D, bool kDense, bool kSmall = false, bool kBias = false, int kScaled = 0>
 __global__ void __launch_bounds__(384, 1)
 mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const FwdParams p) {
@@ -523,9 +530,11 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     for (int t = 0; t < T; ++t) {
       const int j = j0 - first - t;
       float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
+      [[maybe_unused]] float back = 1.f;                 // takes the values' scale out of the row's sum
       if constexpr (kScaled) {
         sc = sc_next;
         if (t + 1 < T) sc_next = kv_scales_of(p, hkv, b, krow0, j - 1, lane, c2);
+        if constexpr (kScaled == 2) whole_scales(sc, cs, bs, back);
       }
       // what kind of tile this is, and the next one: beside the wait for the scores, and from votes, because to the compiler no other
       // value is the same in all lanes (a vote where the branch stands is on the chain of the tile)
@@ -591,7 +600,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       }
       // row maximum of the 128 scores: four chains of three-input maxima (half the instructions of pairwise maxima)
       float mt;
-      if constexpr (kScaled) {
+      if constexpr (kScaled == 1) {
         mt = fmaxf(fmaxf(scaled_max(s0, sc, 0), scaled_max(s1, sc, 2)), fmaxf(scaled_max(s2, sc, 4), scaled_max(s3, sc, 6)));
       } else {
       float mx[4];
@@ -605,7 +614,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       }
       // row maximum of the scaled scores, log2 domain
       const float top_ = fmaxf(max3(mx[0], mx[1], __uint_as_float(s0[31])), max3(mx[2], mx[3], fmaxf(fmaxf(__uint_as_float(s1[31]), __uint_as_float(s2[31])), __uint_as_float(s3[31]))));
-      mt = kBias ? fmaxf(top_ * cs + bs, kBiasFloor) : top_ * c2;
+      mt = kBias ? fmaxf(top_ * cs + bs, kBiasFloor) : kScaled == 2 ? top_ * cs : top_ * c2;
       }
       bool retain = true;
       if (!kDense) {
@@ -693,7 +702,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         if (!ok) break;
       }
       // P = exp2(s * c2 - m_ref), row sum in fp32 before the bf16 cast, P written over S
-      const float nm = kBias ? bs - m_ref : -m_ref;
+      const float nm = kBias || kScaled == 2 ? bs - m_ref : -m_ref;
       [[maybe_unused]] const uint64_t cs2 = f2(cs, cs), nm2 = f2(nm, nm);   // (two scores at a time with a bias)
       [[maybe_unused]] uint64_t sums0 = 0, sums1 = 0;
       [[maybe_unused]] auto take_sums = [&](float& a, float& b, float& c, float& d) {
@@ -717,7 +726,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
 #define MALA_P_CHUNK(SRC, COL)                                                         \
       {                                                                                \
         _Pragma("unroll") for (int e = 0; e < 8; ++e) {                                \
-          if constexpr (kScaled) {                                                     \
+          if constexpr (kScaled == 1) {                                                \
             const int g = (COL) / 8 + e / 4;                                           \
             if (e % 4 == 0) scaled_group(g);                                           \
             float a0, a1, a2, a3;                                                      \
@@ -730,12 +739,12 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             if (e % 4 == 3) scaled_sum(g);                                             \
             continue;                                                                  \
           }                                                                            \
-          if constexpr (kBias) {                                                       \
+          if constexpr (kBias || kScaled == 2) {                                       \
             float a0, a1, a2, a3;                                                      \
             f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e]), __uint_as_float(SRC[4 * e + 1])), cs2, nm2), a0, a1);     \
             f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e + 2]), __uint_as_float(SRC[4 * e + 3])), cs2, nm2), a2, a3); \
             uint64_t x0 = f2(fast_exp2(a0), fast_exp2(a1)), x1 = f2(fast_exp2(a2), fast_exp2(a3));                  \
-            if (kFactors) {                                                            \
+            if constexpr (kBias && kFactors) {                                         \
               const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(bp + (COL) / 2 + e); \
               x0 = f2_mul(x0, f.x); x1 = f2_mul(x1, f.y);                              \
             }                                                                          \
@@ -760,8 +769,8 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         constexpr bool kFactors = FACTORS;                                             \
         MALA_P_CHUNK(s0, 0)                                                            \
         MALA_P_CHUNK(s1, 16)                                                           \
-        if constexpr (kBias) take_sums(sum0, sum1, sum2, sum3);                        \
-        l0 += (sum0 + sum1) + (sum2 + sum3);                                           \
+        if constexpr (kBias || kScaled == 2) take_sums(sum0, sum1, sum2, sum3);                        \
+        l0 += ((sum0 + sum1) + (sum2 + sum3)) * (kScaled == 2 ? back : 1.f);           \
         sum0 = sum1 = sum2 = sum3 = 0.f;                                               \
         tmem_wait_st();                                                                \
         tc_fence_before();                                                             \
@@ -787,8 +796,8 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       }
 #undef MALA_P_PHASE
 #undef MALA_P_CHUNK
-      if constexpr (kBias) take_sums(sum0, sum1, sum2, sum3);
-      l1 += (sum0 + sum1) + (sum2 + sum3);
+      if constexpr (kBias || kScaled == 2) take_sums(sum0, sum1, sum2, sum3);
+      l1 += ((sum0 + sum1) + (sum2 + sum3)) * (kScaled == 2 ? back : 1.f);
       if constexpr (!kDense && D != 64) lg = m_ref + __log2f(l0 + l1);
       tmem_wait_st();
       tc_fence_before();

@@ -79,7 +79,7 @@ struct FwdOneCtl {
   int flag[4], v_tile[2], early_exit;
 };
 
-template <int D, bool kDense, bool kSmall = false, bool kBias = false, bool kScaled = false>
+template <int D, bool kDense, bool kSmall = false, bool kBias = false, int kScaled = 0>
 __global__ void __launch_bounds__(384, 1)
 mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const FwdParams p) {
@@ -400,9 +400,11 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     for (int t = 0; t < U; ++t) {
       const int x = t & 1, j = j0 - t;
       float cs = c2, bs = 0.f;         // the tile's scores in the log2 domain are s * cs + bs
+      [[maybe_unused]] float back = 1.f;                 // takes the values' scale out of the row's sum
       if constexpr (kScaled) {
         sc = sc_next;
         if (t + 1 < U) sc_next = kv_scales_of(p, hkv, b, krow0, j - 1, lane, c2);
+        if constexpr (kScaled == 2) whole_scales(sc, cs, bs, back);
       }
       // what kind of tile this is, and the next one: beside the wait for the scores, and from votes, because to the compiler no other
       // value is the same in all lanes (a vote where the branch stands is on the chain of the tile)
@@ -454,7 +456,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         }
       }
       float mt;
-      if constexpr (kScaled) {
+      if constexpr (kScaled == 1) {
         mt = fmaxf(scaled_max(s0, sc, half * 4), scaled_max(s1, sc, half * 4 + 2));
       } else {
       float mx[4];
@@ -553,7 +555,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         }
       }
       // P = exp2(s * c2 - m_ref), row sum in fp32 before the bf16 cast, P over this thread's own scores
-      const float nm = kBias ? bs - m_ref : -m_ref;
+      const float nm = kBias || kScaled == 2 ? bs - m_ref : -m_ref;
       [[maybe_unused]] const uint64_t cs2 = f2(cs, cs), nm2 = f2(nm, nm);   // (two scores at a time with a bias)
       [[maybe_unused]] uint64_t sums0 = 0, sums1 = 0;
       [[maybe_unused]] auto take_sums = [&](float& a, float& b, float& c, float& d) {
@@ -577,7 +579,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       {                                                                                \
         uint32_t pk[16];                                                               \
         _Pragma("unroll") for (int e = 0; e < 8; ++e) {                                \
-          if constexpr (kScaled) {                                                     \
+          if constexpr (kScaled == 1) {                                                \
             const int g = half * 4 + (PIECE) * 2 + e / 4;                              \
             if (e % 4 == 0) scaled_group(g);                                           \
             float a0, a1, a2, a3;                                                      \
@@ -590,12 +592,12 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             if (e % 4 == 3) scaled_sum(g);                                             \
             continue;                                                                  \
           }                                                                            \
-          if constexpr (kBias) {                                                       \
+          if constexpr (kBias || kScaled == 2) {                                       \
             float a0, a1, a2, a3;                                                      \
             f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e]), __uint_as_float(SRC[4 * e + 1])), cs2, nm2), a0, a1);     \
             f2_get(f2_fma(f2(__uint_as_float(SRC[4 * e + 2]), __uint_as_float(SRC[4 * e + 3])), cs2, nm2), a2, a3); \
             uint64_t x0 = f2(fast_exp2(a0), fast_exp2(a1)), x1 = f2(fast_exp2(a2), fast_exp2(a3));                  \
-            if (kFactors) {                                                            \
+            if constexpr (kBias && kFactors) {                                         \
               const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(bp + (PIECE) * 8 + e); \
               x0 = f2_mul(x0, f.x); x1 = f2_mul(x1, f.y);                              \
             }                                                                          \
@@ -635,8 +637,8 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       } else {
         exponentials(BiasBool<false>{});
       }
-      if constexpr (kBias) take_sums(sum0, sum1, sum2, sum3);
-      l += (sum0 + sum1) + (sum2 + sum3);
+      if constexpr (kBias || kScaled == 2) take_sums(sum0, sum1, sum2, sum3);
+      l += ((sum0 + sum1) + (sum2 + sum3)) * (kScaled == 2 ? back : 1.f);
       fresh = true;
       if constexpr (kBias) {
         if (near) ++nears;

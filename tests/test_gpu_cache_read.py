@@ -183,7 +183,7 @@ def _keys(kp, vp, ks, vs, table, lens, ps):
 
 
 @pytest.mark.parametrize("lens,new", PROMPTS)
-@pytest.mark.parametrize("ps,Hq,Hkv,d", [(64, 4, 2, 64), (128, 8, 2, 128), (16, 2, 2, 96), (256, 6, 1, 128), (32, 4, 4, 16)])
+@pytest.mark.parametrize("ps,Hq,Hkv,d", [(64, 4, 2, 64), (128, 8, 2, 128), (16, 2, 2, 96), (256, 6, 1, 128), (32, 4, 4, 16), (128, 4, 2, 64), (256, 2, 2, 48)])
 def test_prompts(mala, lens, new, ps, Hq, Hkv, d):
     """Attention over scale * code in 64 bits: o within the kernels' roundings of P and o to bf16, lse within those of fp32 -- keys and values are not
     rounded on their way."""
@@ -216,7 +216,7 @@ def _dequantised(kp, vp, ks, vs, pow2):
 
 
 @pytest.mark.parametrize("lens,new", PROMPTS)
-@pytest.mark.parametrize("ps,Hq,Hkv,d", [(64, 4, 2, 64), (128, 8, 2, 128), (16, 2, 2, 96)])
+@pytest.mark.parametrize("ps,Hq,Hkv,d", [(64, 4, 2, 64), (128, 8, 2, 128), (16, 2, 2, 96), (128, 4, 2, 64)])
 @pytest.mark.parametrize("tau", [0.0, 1e-3, 0.05])
 def test_prompts_against_bf16_pages(mala, lens, new, ps, Hq, Hkv, d, tau):
     """Scales that are powers of two: the same values lie in bf16 pages, and mala_fwd_paged decides alike, tile by tile."""
@@ -236,7 +236,7 @@ def test_prompts_against_bf16_pages(mala, lens, new, ps, Hq, Hkv, d, tau):
     assert ((a - b).norm() <= 2.0 ** -8 * 2 * b.norm()) and ((c - e).abs() <= 2.0 ** -20 * (1 + e.abs())).all()
 
 
-@pytest.mark.parametrize("ps,Hq,Hkv,d,new", [(64, 4, 2, 64, 300), (128, 8, 2, 128, 1500), (16, 2, 2, 96, 40)])
+@pytest.mark.parametrize("ps,Hq,Hkv,d,new", [(64, 4, 2, 64, 300), (128, 8, 2, 128, 1500), (16, 2, 2, 96, 40), (128, 4, 2, 64, 300), (256, 4, 2, 64, 2100)])
 def test_prompts_that_skip(mala, ps, Hq, Hkv, d, new):
     """Queries that look for their own key: tiles are skipped, the same ones as over bf16 pages of the same values."""
     lens, scale, tau = [2500], 1.0, 1e-3
@@ -255,7 +255,7 @@ def test_prompts_that_skip(mala, ps, Hq, Hkv, d, new):
 
 @pytest.mark.parametrize("splits", [2, 5, 33])
 @pytest.mark.parametrize("lens,new", PROMPTS)
-@pytest.mark.parametrize("ps,Hq,Hkv,d", [(64, 4, 2, 64), (128, 8, 2, 128), (16, 2, 2, 96)])
+@pytest.mark.parametrize("ps,Hq,Hkv,d", [(64, 4, 2, 64), (128, 8, 2, 128), (16, 2, 2, 96), (128, 4, 2, 64)])
 def test_prompts_in_ranges(mala, lens, new, ps, Hq, Hkv, d, splits):
     """Keys cut into ranges: the tolerances of test_prompts (the merge adds a few roundings in fp32), rows that belong to no sequence
     left as they were, and nothing read that this call did not write."""
@@ -278,7 +278,7 @@ def test_prompts_in_ranges(mala, lens, new, ps, Hq, Hkv, d, splits):
 
 
 @pytest.mark.parametrize("causal", [True, False])
-@pytest.mark.parametrize("ps,Hq,Hkv,d,new,splits", [(64, 4, 2, 64, 300, 3), (128, 8, 2, 128, 1500, 4), (16, 2, 2, 96, 40, 7)])
+@pytest.mark.parametrize("ps,Hq,Hkv,d,new,splits", [(64, 4, 2, 64, 300, 3), (128, 8, 2, 128, 1500, 4), (16, 2, 2, 96, 40, 7), (128, 4, 2, 64, 300, 3)])
 def test_prompts_in_ranges_that_skip(mala, ps, Hq, Hkv, d, new, splits, causal):
     """Every range has a skip test of its own: the tiles that mala_fwd_chunk_split skips over the same values."""
     lens, scale, tau = [2500], 1.0, 1e-3
@@ -320,12 +320,13 @@ def test_ranges_leave_rows_and_refuse(mala):
 
 
 @pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("ps", [64, 128])
 @pytest.mark.parametrize("value", [0.0, -0.01, 1e-30, 1e25, 2.0 ** -61, 2.0 ** -60])
-def test_prompts_with_far_scales(mala, which, value):
+def test_prompts_with_far_scales(mala, which, value, ps):
     """Scales that no cache write gives (0, below 0, near the ends of fp32) in some units: bf16(scale * code) there."""
-    lens, new, ps, Hq, Hkv, d = [700], [130], 64, 4, 2, 64
+    lens, new, Hq, Hkv, d = [700], [130], 4, 2, 64
     (kp, vp), (ks, vs), table = _cache(13, True, lens, ps, Hkv, d)
-    used = table[0, [2, 5]].long()
+    used = table[0, [2, 4 if ps == 128 else 5]].long()
     (ks if which == "k" else vs)[used, 1] = value
     if which == "k" and value > 1:
         for x in used.tolist():            # (finite scores: one key of small codes)
