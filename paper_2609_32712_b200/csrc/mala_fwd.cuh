@@ -131,7 +131,8 @@ __device__ __forceinline__ int range_of(int Tk, int num_splits) { return (Tk + n
 // kScaled: keys and values are codes of a cache, whole numbers of their scales, and the scales (one per 16 keys) come in here: a key's is the
 // factor of its score in the maximum and in the exponential's argument; a value's is a summand there, P then carries it, and
 // the row's sum takes it out again.  So nothing is rounded that a cache of wider values would not round.  1: scales of 16 keys each; 2: one per key
-// block (pages of whole ones), then a factor, a summand and an inverse per tile in place of eight each.
+// block (pages of whole ones), then a factor, a summand and an inverse per tile in place of eight each.  2048 queries of 32 heads of 128 columns behind 30,000 keys
+// (1041 GFLOP): 970 us, over keys and values in bf16 915; under the power cap the eight per tile weigh little.
 template <int D, bool kDense, bool kSmall = false, bool kBias = false, int kScaled = 0>
 __global__ void __launch_bounds__(384, 1)
 mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,

@@ -1,5 +1,5 @@
 // Argument marshalling of the rotary calls and the cache reads as a CPython extension: checks, output tensors and the call of the C ABI in one step.  A decode
-// step's device work takes 4 us, and the same marshalling through ctypes 15; here it takes 6.  Raises AssertionError for what the wrappers check, and
+// step's device work takes 4 us, and a call through ctypes with the same checks 18; here it takes 7.  Raises AssertionError for what the wrappers check, and
 // returns the library's code (a negative int) where a call is refused.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>

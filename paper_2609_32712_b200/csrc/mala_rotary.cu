@@ -212,7 +212,9 @@ struct Rows {
 constexpr int kRingBytes = kRotaryWarps * 8192;
 
 // Rotations.  A row lies in the registers of L lanes, and a warp works on 32 / L heads of a token at a time: the angles of a token are worked out once for
-// all heads that a warp takes, and a warp's tokens are neighbours.
+// all heads that a warp takes (a lane has a share of them).  Bound by HBM where there are many rows: 4 bytes per element.  32K tokens, 32 + 8 heads of 128 columns:
+// 108 us (6.2 TB/s), with the norm 110; 8 x 4096 tokens, 16 + 4 heads, 64 of 128 columns as neighbours 61 us (5.5 TB/s).  10 thousand packed tokens,
+// 16 + 4 heads with the norm 25 us (4.1 TB/s): half of the issue slots, and some 6 us of beginning and end.  1024 tokens, 2 + 2 heads of 64: 4 us.
 template <int L, int kPairs, bool kNorm, bool kPages>
 __global__ void __launch_bounds__(kRotaryThreads, 2)
 rotary_kernel(const RotaryParams p) {
@@ -304,7 +306,8 @@ rotary_kernel(const RotaryParams p) {
 
 // The norm's backward, n = x r, r = (mean(x^2) + eps)^(-1/2):  with g the gradient behind the norm and its weight, rotated back,
 //   dx = r (g w - n mean(g w n)),   dw = sum over rows and heads of g n.
-// A block works on q or on k alone, keeps its sums per column in registers and leaves them in the workspace.
+// A block works on q or on k alone, keeps its sums per column in registers and leaves them in the workspace.  Bound by HBM, 6 bytes per element: 32K tokens, 32 + 8
+// heads of 128 columns 161 us (6.2 TB/s) and 6 for the sums behind it; 10 thousand tokens, 16 + 4 heads 44 us (3.5 TB/s) and 3, at 58 % of the issue slots.
 template <int L, int kPairs>
 __global__ void __launch_bounds__(kRotaryThreads, 2)
 rotary_norm_bwd_kernel(const RotaryParams p) {
@@ -513,6 +516,7 @@ static void set_items(RotaryParams* p, int tensors, int sms, bool same) {
 // leave the SMs that memory serves sooner idle at the end (32K tokens, 32 + 8 heads: 126 us), and many short blocks begin too often (frequencies, weights, the
 // ring's first rows: some 2 us; six rounds 106 us, but 35 thousand rows of a step 145 instead of 135).  So seven tenths go to one round,
 // and the rest to blocks of `of_warp` batches a warp, which go to the SMs that are through (110 and 138; the backward pass with the norm 163 instead of 186).
+// Below two such blocks' work for every block of the one round that does not pay (10 thousand tokens, 16 + 4 heads: forward 34 us instead of 25).
 constexpr int kWarpBatches = 24, kWarpBatchesBwd = 16;
 static void set_ranges(WorkRange* one, WorkRange* rest, uint32_t first, long long items, long long batches, int blocks, int of_warp) {
   *rest = WorkRange{0, 0, 0, 0};
