@@ -1,5 +1,5 @@
 """Builds ``libmala.so`` in-tree with nvcc for sm_100a (cross-compiles without a GPU), and beside it ``_native.so``, the marshalling
-of the rotary calls and the cache reads, with g++ against torch."""
+of the calls that serving steps wait for, with g++ against torch."""
 from __future__ import annotations
 
 import os

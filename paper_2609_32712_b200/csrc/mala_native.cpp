@@ -1,4 +1,4 @@
-// Argument marshalling of the rotary calls and the cache reads as a CPython extension: checks, output tensors and the call of the C ABI in one step.  A decode
+// Argument marshalling of the rotary calls, the cache reads and prompts over an e4m3 cache as a CPython extension: checks, output tensors and the call of the C ABI in one step.  A decode
 // step's device work takes 4 us, and a call through ctypes with the same checks 18; here it takes 7.  Raises AssertionError for what the wrappers check, and
 // returns the library's code (a negative int) where a call is refused.
 #define PY_SSIZE_T_CLEAN
@@ -8,10 +8,10 @@
 #include <ATen/ops/empty_like.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
-#include <string>
 
 #include "../../include/mala.h"
 
@@ -200,8 +200,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   } catch (const Refused& e) {
     PyErr_SetString(PyExc_AssertionError, e.what());
   } catch (const PythonError&) {
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (...) {                          // (torch's own: no memory left, ...)
+    torch::translate_exception_to_python(std::current_exception());
   }
   return nullptr;
 }
@@ -321,12 +321,58 @@ PyObject* cache_read(PyObject* const* a) {
   return rc != MALA_OK ? code(rc) : tuple(out);
 }
 
+// q, kpages8, vpages8, kscale, vscale, cu_seqlens_q, block_table, seqlens_k, max_seqlen_q, total_k, scale, tau, causal, num_splits (None: see the wrapper), ws, and the
+// telemetry's three tensors (None: no telemetry)
+PyObject* fwd_paged_fp8(PyObject* const* a) {
+  const Here here;
+  const at::Tensor &q = tensor(a[0]), &kp = tensor(a[1]), &vp = tensor(a[2]), &ks = tensor(a[3]), &vs = tensor(a[4]), &cu = tensor(a[5]), &table = tensor(a[6]), &lens = tensor(a[7]);
+  const int max_q = whole(a[8]), total_k = whole(a[9]), causal = PyObject_IsTrue(a[12]);
+  const float scale = (float)number(a[10]), tau = (float)number(a[11]);
+  const Arg ws_given(a[14]), retained(a[15]), bitmask(a[16]), totals(a[17]);
+  require(q.dim() == 4 && q.size(0) == 1 && kp.dim() == 4 && table.dim() == 2, "expects q [1,total_q,Hq,d], pages [num_pages, page_size, Hkv, d] and a block table");
+  const int total_q = size(q, 1), Hq = size(q, 2), d = size(q, 3), num_pages = size(kp, 0), page_size = size(kp, 1), Hkv = size(kp, 2), B = size(table, 0), width = size(table, 1);
+  ints(cu);
+  ints(table);
+  ints(lens);
+  require(cu.dim() == 1 && cu.size(0) == B + 1 && lens.dim() == 1 && lens.size(0) == B, "expects offsets and lengths of the block table's sequences");
+  require(kp.sizes() == vp.sizes() && kp.size(3) == d, "expects pages of q's head size");
+  check_scales(ks, num_pages, Hkv, page_size);
+  check_scales(vs, num_pages, Hkv, page_size);
+  for (const at::Tensor* t : {&q, &kp, &vp, &ks, &vs, &cu, &table, &lens}) here.on(*t);
+  here.on(ws_given);
+  require(!ws_given || (ws_given->scalar_type() == at::kByte && ws_given->is_contiguous()), "expects a workspace of bytes");
+  int splits = 1;
+  if (a[13] != Py_None) {
+    splits = whole(a[13]);
+  } else if (tau == 0.f && !ws_given) {
+    const int64_t room = (int64_t)width * page_size;
+    splits = mala_paged_fp8_suggest_splits(B, Hq, max_q, (int)(room < total_k ? room : total_k), total_k, 0);
+    if (splits < 1) splits = 1;            // (lengths that the call refuses)
+  }
+  const mala_tin qi = in4(q), ki = in4(kp, true), vi = in4(vp, true);
+  const at::Tensor o = at::empty_like(q), lse = at::empty({Hq, total_q}, q.options().dtype(at::kFloat));
+  at::Tensor ws;
+  if (!ws_given) {
+    const size_t need = mala_paged_fp8_split_workspace_bytes(B, Hq, Hkv, max_q, total_k, d, splits);
+    ws = at::empty({(int64_t)(need < 256 ? 256 : need)}, q.options().dtype(at::kByte));
+  } else {
+    ws = *ws_given;
+  }
+  const mala_stats st = {(uint32_t*)retained.data(), (uint32_t*)bitmask.data(), (uint64_t*)totals.data()};
+  const int rc = mala_fwd_paged_fp8_split(qi, ki, vi, ks.data_ptr<float>(), vs.data_ptr<float>(), cu.data_ptr<int32_t>(), table.data_ptr<int32_t>(), lens.data_ptr<int32_t>(), out4(o),
+                                          lse.data_ptr<float>(), totals ? &st : nullptr, B, Hq, Hkv, total_q, max_q, total_k, num_pages, page_size, width, d, causal, scale, tau, splits,
+                                          ws.data_ptr(), (size_t)ws.numel(), here.stream());
+  const at::Tensor out[2] = {o, lse};
+  return rc != MALA_OK ? code(rc) : tuple(out);
+}
+
 PyMethodDef methods[] = {{"rotary", (PyCFunction)(void*)entry<rotary, 13>, METH_FASTCALL, nullptr},
                          {"rotary_bwd", (PyCFunction)(void*)entry<rotary_bwd, 16>, METH_FASTCALL, nullptr},
                          {"rotary_write", (PyCFunction)(void*)entry<rotary_write, 16>, METH_FASTCALL, nullptr},
                          {"cache_read", (PyCFunction)(void*)entry<cache_read, 7>, METH_FASTCALL, nullptr},
+                         {"fwd_paged_fp8", (PyCFunction)(void*)entry<fwd_paged_fp8, 18>, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of the rotary calls and the cache reads.", -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of the rotary calls, the cache reads and prompts over an e4m3 cache.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

@@ -100,7 +100,7 @@ rotary_write8_kernel(const RotaryWriteParams p) {
       return window;
     };
     if (tid < window) {
-      // a unit that begins at a row of the window belongs to this round where it is this block's and all of it is in the window
+      // a unit that begins at a row of the window is taken now where it is this block's and all of it is in the window
       const int off = (int)(slot_s[tid] & (p.unit - 1));
       const bool mine_ = ((valid_s[tid >> 5] & ends_s[tid >> 5]) >> lane & 1u) && s + tid < t1;
       const bool whole = tid + p.unit - off <= window || s + window >= p.rows || (tid + 1 < window && first_of(ends_s, tid + 1) < window);

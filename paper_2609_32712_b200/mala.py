@@ -171,7 +171,7 @@ _native_module = None
 
 
 def _native():
-    """The extension that marshals the rotary calls and the cache reads (built beside libmala.so; fails loudly if absent)."""
+    """The extension that marshals the rotary calls, the cache reads and prompts over an e4m3 cache (beside libmala.so; fails loudly if absent)."""
     global _native_module
     if _native_module is None:
         lib()                # (the library that it is linked with)
@@ -877,11 +877,6 @@ def cache_write_fp8(k, v, slots, kpages8, vpages8, kscale, vscale) -> None:
         raise MalaError(rc, "mala_cache_write_fp8")
 
 
-def _scales(kscale, vscale, num_pages: int, Hkv: int, page_size: int):
-    for t in (kscale, vscale):
-        assert t.dtype is _F32 and t.is_contiguous() and tuple(t.shape) == (num_pages, Hkv, max(1, page_size // 128))
-
-
 def cache_read(kpages, vpages, block_table, seqlens, rows: int):
     """mala_cache_read: keys and values of the requests of block_table int32 [B, max_pages_per_seq] with seqlens int32 [B] tokens
     out of bf16 pages [num_pages, page_size, Hkv, d], packed.  rows: how many rows to make room for (at least the sum of the lengths for all
@@ -896,36 +891,19 @@ def cache_read_fp8(kpages8, vpages8, kscale, vscale, block_table, seqlens, rows:
     return _done(_native().cache_read(kpages8, vpages8, kscale, vscale, block_table, seqlens, rows), "mala_cache_read_fp8")
 
 
-def _suggested_splits(*lengths) -> int:
-    return max(1, lib().mala_paged_fp8_suggest_splits(*lengths, 0))     # (of lengths that the call refuses: 1)
-
-
 def fwd_paged_fp8(q, kpages8, vpages8, kscale, vscale, cu_seqlens_q, block_table, seqlens_k, max_seqlen_q: int, total_k: int,
                   scale: float, tau: float, causal: bool = True, stats: bool = False, ws=None, num_splits: Optional[int] = None):
     """mala_fwd_paged_fp8(_split): ``fwd_paged`` over e4m3 pages with their scales; total_k: at least the sum of seqlens_k (room in the
     workspace).  num_splits: ranges that a sequence's keys are cut into, each with a skip test of its own (None: with tau 0, where that
     gives the same, and no ws of the caller's as many as the library suggests, else 1).  Returns (o, lse [Hq,total_q], Stats or None)."""
-    one, total_q, Hq, d = q.shape
-    num_pages, page_size, Hkv = kpages8.shape[0], kpages8.shape[1], kpages8.shape[2]
-    B, max_pages = block_table.shape
-    _ints(cu_seqlens_q, block_table, seqlens_k)
-    assert one == 1 and cu_seqlens_q.shape == (B + 1,) and seqlens_k.shape == (B,)
-    assert kpages8.shape == vpages8.shape and kpages8.shape[3] == d
-    _scales(kscale, vscale, num_pages, Hkv, page_size)
-    o = torch.empty_like(q)
-    lse = q.new_empty((Hq, total_q), dtype=_F32)
-    Tq, Tk = -(-(max_seqlen_q + 127) // 128), -(-min(max_pages * page_size, total_k) // 128)
-    st = Stats((B, Hq, Tq), -(-Tk // 32), q.device) if stats else None
-    if num_splits is None:
-        num_splits = 1 if tau != 0.0 or ws is not None else _suggested_splits(B, Hq, max_seqlen_q, min(max_pages * page_size, total_k), total_k)
-    ws = _ws(int(lib().mala_paged_fp8_split_workspace_bytes(B, Hq, Hkv, max_seqlen_q, total_k, d, num_splits)), q.device) if ws is None else ws
-    rc = lib().mala_fwd_paged_fp8_split(_view(q, _TIn), _view8(kpages8), _view8(vpages8), kscale.data_ptr(), vscale.data_ptr(),
-                                  cu_seqlens_q.data_ptr(), block_table.data_ptr(), seqlens_k.data_ptr(), _view(o, _TOut),
-                                  lse.data_ptr(), ctypes.byref(st.c) if st else None, B, Hq, Hkv, total_q, max_seqlen_q, total_k,
-                                  num_pages, page_size, max_pages, d, int(causal), scale, tau, num_splits, ws.data_ptr(), ws.numel(),
-                                  _here(q, kpages8, vpages8, kscale, vscale, cu_seqlens_q, block_table, seqlens_k, ws))
-    if rc != 0:
-        raise MalaError(rc, "mala_fwd_paged_fp8")
+    st = None
+    if stats:
+        B, max_pages = block_table.shape
+        Tk = -(-min(max_pages * kpages8.shape[1], total_k) // 128)
+        st = Stats((B, q.shape[2], -(-(max_seqlen_q + 127) // 128)), -(-Tk // 32), q.device)
+    o, lse = _done(_native().fwd_paged_fp8(q, kpages8, vpages8, kscale, vscale, cu_seqlens_q, block_table, seqlens_k, max_seqlen_q, total_k, scale, tau,
+                                           causal, num_splits, ws, *((st.retained, st.bitmask, st.totals) if stats else (None, None, None))),
+                   "mala_fwd_paged_fp8")
     return o, lse, st
 
 
