@@ -70,6 +70,10 @@ __device__ __forceinline__ float weight_at(const void* w, int fp32, int c) {
   return fp32 ? __ldg((const float*)w + c) : __bfloat162float(__ldg((const __nv_bfloat16*)w + c));
 }
 
+// Where a column of a row lies in shared memory: the row's first L pieces are side by side and the others 512 bytes behind them
+template <int L>
+__device__ __forceinline__ int staged(int col) { return (col / 8 < L ? col / 8 : col / 8 - L + 32) * 8 + col % 8; }
+
 // A row of d columns in L lanes, two pieces of eight columns each: pieces whose columns are paired (halves), so that a pair lies in one lane, else any two;
 // either way the first pieces of neighbouring lanes are neighbours, and so are the second ones.
 template <int L, int kPairs>
@@ -77,6 +81,9 @@ struct LanePieces {
   int pa, pb;               // the pieces
   bool has_a, has_b, pair;  // whether the row has them; whether a's columns are paired with b's (halves)
   int turns;                // neighbours, kHalvesOdd: whether all of the lane's columns are rotated (2), some (1) or none (0)
+  // kHalvesOdd, half of the rotated columns even: where the partners of the lane's columns 2 j and 2 j + 1 of 16 lie (two numbers of 16 bits each), and a bit
+  // for each of these eight that is rotated (else 0)
+  uint32_t partners[4], turned_twos;
   __device__ __forceinline__ void set(const RotaryRule& r, int c) {
     const int turned = kPairs == kHalves ? r.rotary / 16 : 0, pieces = r.d / 8;
     pair = c < turned;
@@ -86,6 +93,15 @@ struct LanePieces {
     has_a = pair || (c - turned < near && pa < pieces);
     has_b = pair || (c - turned < near && pb < pieces);
     turns = 8 * pa + 8 <= r.rotary && (8 * pb + 8 <= r.rotary || !has_b) ? 2 : 8 * pa < r.rotary ? 1 : 0;
+    if constexpr (kPairs == kHalvesOdd) {
+      turned_twos = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int x = col(2 * j), at = staged<L>(partner_of<kPairs>(x, r.rotary));
+        partners[j / 2] = j % 2 ? partners[j / 2] | (uint32_t)at << 16 : (uint32_t)at;
+        if (x < r.rotary && r.rotary % 4 == 0) turned_twos |= 1u << j;
+      }
+    }
   }
   // column of the lane's e-th place of 16
   __device__ __forceinline__ int col(int e) const { return e < 8 ? 8 * pa + e : 8 * pb + e - 8; }
@@ -172,12 +188,8 @@ __device__ __forceinline__ uint64_t crossed(uint64_t x) {
   return f2(b, a);
 }
 
-template <int L>
-__device__ __forceinline__ int staged(int col) { return (col / 8 < L ? col / 8 : col / 8 - L + 32) * 8 + col % 8; }
-
-// A lane's two pieces rotated (and multiplied by the norm's weights).  kHalvesOdd: the row lies in shared memory at `row`, its first L pieces side by side
-// and the others 512 bytes behind them.  What is not rotated is
-// multiplied by its weight alone, whatever stands beside it.
+// A lane's two pieces rotated (and multiplied by the norm's weights).  kHalvesOdd: the row lies in shared memory at `row` (see staged), two columns of a partner at
+// a time where half of the rotated ones is even.  What is not rotated is multiplied by its weight alone, whatever stands beside it.
 template <int L, int kPairs, bool kNorm>
 __device__ __forceinline__ void rotate_pieces(const RotaryRule& r, const LanePieces<L, kPairs>& l, const LaneFactors<L, kPairs>& f, const __nv_bfloat16* row, uint64_t (&a)[4],
                                               uint64_t (&b)[4]) {
@@ -210,6 +222,16 @@ __device__ __forceinline__ void rotate_pieces(const RotaryRule& r, const LanePie
       return;
     }
   } else {
+    if (l.turned_twos != 0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint64_t& x = j < 4 ? a[j % 4] : b[j % 4];
+        const uint32_t y = *reinterpret_cast<const uint32_t*>(row + (j % 2 ? l.partners[j / 2] >> 16 : l.partners[j / 2] & 0xffffu));
+        const uint64_t own = f2_mul(x, j < 4 ? f.ca[j % 4] : f.cb[j % 4]);
+        x = (l.turned_twos >> j) & 1u ? f2_fma(pair_of(y), j < 4 ? f.sa[j % 4] : f.sb[j % 4], own) : own;
+      }
+      return;
+    }
     if (l.turns > 0) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
