@@ -767,7 +767,7 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       // (the same phase with factors and without: warp-uniform)
 #define MALA_P_PHASE(FACTORS)                                                          \
       {                                                                                \
-        constexpr bool kFactors = FACTORS;                                             \
+        [[maybe_unused]] constexpr bool kFactors = FACTORS;                            \
         MALA_P_CHUNK(s0, 0)                                                            \
         MALA_P_CHUNK(s1, 16)                                                           \
         if constexpr (kBias || kScaled == 2) take_sums(sum0, sum1, sum2, sum3);                        \

@@ -621,7 +621,7 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         if (lane == 0) mbar_arrive(&p_full[x][PIECE]);                                 \
       }
       auto exponentials = [&](auto with_factors) {   // (warp-uniform)
-        constexpr bool kFactors = decltype(with_factors)::value;
+        [[maybe_unused]] constexpr bool kFactors = decltype(with_factors)::value;
         MALA_P_PIECE(s0, 0)
         MALA_P_PIECE(s1, 1)
       };
