@@ -411,6 +411,7 @@ int mala_cache_read_fp8(mala_tin kpages8, mala_tin vpages8, const float* kscale,
 /* mala_fwd_paged over an e4m3 cache: keys and values are scale * code, not rounded on their way (the codes are multiplied, the scales come in
  * at the softmax; beyond 2^-60 .. 2^60, or not positive, bf16(scale * code)).  total_k: room for keys in the workspace, at least the sum of
  * seqlens_k (see mala_cache_read_fp8 for what lies beyond it: the sequences that reach beyond have no meaningful result).
+ * A sequence's result is the same whatever the other sequences' keys and values are, infinities and NaNs among them.
  * Workspace: mala_paged_fp8_workspace_bytes.  d a multiple of 16 up to 128, page_size not 8; everything else as
  * mala_fwd_paged; telemetry laid out for max_seqlen_k = min(max_pages_per_seq * page_size, total_k). */
 int mala_fwd_paged_fp8(mala_tin q, mala_tin kpages8, mala_tin vpages8, const float* kscale, const float* vscale,

@@ -95,6 +95,18 @@ __device__ __forceinline__ float scaled_max(const uint32_t (&s)[32], float sc, i
   return fmaxf(m[0], m[1]);
 }
 
+// Zeros in the rows from `rows` on of a tile of 128 values in shared memory (panels of 64 columns, 128 bytes a row; the swizzle stays within a
+// row), by a warp, in front of the product that reads them.  Behind a sequence's last key come the next one's rows: P is 0 there, but 0 times
+// its infinities and NaNs is not.  Once per CTA that has the sequence's last block, while the softmax works on that block's scores.
+template <int kPanels>
+__device__ __forceinline__ void clear_rows(uint8_t* tile, int rows, int lane) {
+#pragma unroll
+  for (int pn = 0; pn < kPanels; ++pn)
+    for (int x = rows * 8 + lane; x < 128 * 8; x += 32) *reinterpret_cast<uint4*>(tile + pn * 16384 + x * 16) = make_uint4(0u, 0u, 0u, 0u);
+  fence_proxy_async_smem();
+  __syncwarp();
+}
+
 // Rows first .. first + count - 1 of a packed sequence whose queries see no key: o = 0, lse = -inf (all threads of the block)
 __device__ __forceinline__ void empty_rows(const FwdParams& p, int b, int h, int row0, int Nq, int first, int count) {
   const int per = p.d / 8;
@@ -224,6 +236,8 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   const int j0 = hasB ? hB : hA;
   const int U = j0 - jlo + 1;
   const int firstA = hasB ? hB - hA : 0;             // 1 when B's diagonal key block, not legal for A, is in the range
+  // keys of the first block visited (128: all of its rows are this sequence's)
+  [[maybe_unused]] const int last_rows = kScaled && j0 == Tk - 1 ? Nkeys - j0 * 128 : 128;
   int* status = p.status;
 
   if (tid == 0) {
@@ -428,6 +442,8 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           // P arrives in two halves of 64 keys: the first four k-steps of O += P V run while the second half
           // of the exponentials is still being computed
           ok = mbar_wait_warp(&v_full[vs], vpar, status);
+          if constexpr (kScaled)       // (in the shared stage by the issuers of both blocks, each in front of its own product)
+            if (ok && u == 0 && last_rows < 128) clear_rows<PAN>(sV + vs * Cfg::kTileBytes, last_rows, lane);
           if (ok) ok = mbar_wait_warp(&p_full[x][0], r & 1, status);
           if (!ok) break;
           tc_fence_after();
@@ -669,7 +685,8 @@ mala_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       // The scores of this tile were produced after every earlier PV of this block (same tensor pipe,
       // program order), so O may be touched here without a further wait.
       // (warp votes stay out of conditional code: there the compiler has to re-converge the warp around each of them)
-      const bool need_any = __any_sync(0xffffffffu, r > 0 && mt > m_ref + 8.f);
+      // (kScaled: whatever the rows of the block that are not this request's have seen of its neighbour's keys)
+      const bool need_any = __any_sync(0xffffffffu, r > 0 && (!kScaled || valid) && mt > m_ref + 8.f);
       if (r == 0) {
         m_ref = mt;
       } else {

@@ -140,6 +140,8 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   }
   const int j0 = min(dI, jhi);                       // step u = 0 .. U-1 visits key block j0 - u
   const int U = j0 - jlo + 1;
+  // keys of the first block visited (128: all of its rows are this sequence's)
+  [[maybe_unused]] const int last_rows = kScaled && j0 == Tk - 1 ? Nkeys - j0 * 128 : 128;
   int* status = p.status;
 
   // One slot of key block jt: columns sub * 128 .. of its 128 rows.  All lanes of the warp call this; pages smaller than a
@@ -296,6 +298,14 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         }
       }
       if (retain) {
+        if constexpr (kScaled) {
+          static_assert(!kScaled || SUB == 1, "a tile's values lie in one slot");
+          if (u == 0 && last_rows < 128) {
+            ok = mbar_wait_warp(&v_full[vs], vpar, status);
+            if (!ok) break;
+            clear_rows<PAN>(sV + vs * SLOT, last_rows, lane);
+          }
+        }
         // P arrives in two pieces, the first 32 keys of either half of the tile before the others (the MMAs keep the order of the
         // keys, in which mala_fwd_kernel adds them too)
 #pragma unroll
@@ -533,7 +543,8 @@ mala_fwd_one_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       }
       // Lazy rescaling: the reference maximum only moves when the row maximum grew by more than 2^8.  The PV before may
       // still be running then: it has to be over first.
-      const bool need_any = __any_sync(0xffffffffu, r > 0 && mt > m_ref + 8.f);
+      // (kScaled: whatever the rows of the block that are not this request's have seen of its neighbour's keys)
+      const bool need_any = __any_sync(0xffffffffu, r > 0 && (!kScaled || valid) && mt > m_ref + 8.f);
       if (r == 0) {
         m_ref = mt;
       } else if (need_any) {

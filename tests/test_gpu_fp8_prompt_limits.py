@@ -1,0 +1,70 @@
+"""Prompts over an e4m3 cache at their limits: requests whose cache holds infinities and NaNs beside others."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+PS, SHAPES = "ps,Hq,Hkv,d", [(64, 4, 2, 64), (128, 4, 2, 64), (128, 8, 2, 128), (16, 32, 8, 96), (128, 32, 8, 64), (256, 32, 4, 128)]   # 32 heads: two blocks of queries per CTA
+
+
+@pytest.fixture(scope="module")
+def mala():
+    from paper_2609_32712_b200 import mala as m
+    m.lib()
+    return m
+
+
+def _randn(seed, *shape):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _cache(seed, lens, ps, Hkv, d):
+    per = [-(-n // ps) for n in lens]
+    table = torch.full((len(lens), max(per)), -1, dtype=torch.int32)
+    order = torch.randperm(sum(per), generator=torch.Generator().manual_seed(seed)).tolist()
+    for b, n in enumerate(per):
+        table[b, :n] = torch.tensor([order.pop() for _ in range(n)], dtype=torch.int32)
+    pages = [(_randn(seed + x, sum(per), ps, Hkv, d).float() * 100).clamp(-448, 448).to(torch.float8_e4m3fn) for x in range(2)]
+    scales = [_randn(seed + 2 + x, sum(per), Hkv, max(1, ps // 128)).float().abs() * 0.01 + 0.005 for x in range(2)]
+    return pages, scales, table.cuda()
+
+
+@pytest.mark.parametrize(PS, SHAPES)
+@pytest.mark.parametrize("what", ["value codes", "value scales", "key codes"])
+@pytest.mark.parametrize("tau,splits,causal", [(0.0, 1, True), (0.0, 3, True), (0.0, 1, False), (1e-3, 1, True), (1e-3, 2, False)])
+def test_requests_do_not_reach_one_another(mala, ps, Hq, Hkv, d, what, tau, splits, causal):
+    """NaN codes, and values that are infinite (448 * 1e36), at the front of a request's cache: the requests beside it, whose last blocks are not
+    whole, get the results that they have beside a clean one, bit by bit, and the request itself NaNs in the columns that hold them."""
+    lens, new, col = [200, 300, 77, 129], [40, 300, 1, 129], 5
+    (kp, vp), (ks, vs), table = _cache(3, lens, ps, Hkv, d)
+    q, cu = _randn(9, 1, sum(new), Hq, d), [0, 40, 340, 341, 470]
+
+    def call():
+        return mala.fwd_paged_fp8(q, kp, vp, ks, vs, _i32(cu), table, _i32(lens), max(new), sum(lens), 1 / math.sqrt(d), tau, causal=causal, num_splits=splits)[:2]
+    clean = call()
+    if what == "value codes":
+        for x in range(0, 300, 7):
+            vp.view(torch.uint8)[table[1, x // ps], x % ps, :, col] = 0x7f
+    elif what == "value scales":
+        vp.view(torch.uint8)[table[1, 0], :, :, col] = 0x7e                  # 448
+        vs[table[1, 0].long(), :, 0] = 1e36
+    else:
+        kp.view(torch.uint8)[table[1, 0], :, :, col] = 0xff
+    got = call()
+    assert mala.device_status() == 0
+    for b in (0, 2, 3):
+        rows = slice(cu[b], cu[b + 1])
+        assert torch.isfinite(clean[0][:, rows]).all() and torch.equal(got[0][:, rows], clean[0][:, rows]) and torch.equal(got[1][:, rows], clean[1][:, rows]), b
+    if tau == 0 and what == "value codes":
+        mine = got[0][:, cu[1]:cu[2]]
+        assert torch.isnan(mine[..., col]).all() and torch.equal(got[1], clean[1])
+        rest = [c for c in range(d) if c != col]
+        assert torch.equal(mine[..., rest], clean[0][:, cu[1]:cu[2]][..., rest])
