@@ -19,6 +19,8 @@
 //   warps 4-7    softmax group of block A, warps 8-11 of block B (one thread per query row)
 // All synchronisation is by mbarriers with bounded waits.
 #pragma once
+#include <float.h>
+
 #include "mala_bias.cuh"
 #include "sm100_ptx.cuh"
 
@@ -70,11 +72,12 @@ struct FwdParams {
   int scale_tiles;               // sequence b 24 floats at 24 * (h * scale_tiles + cu_k[b] / 128 + b + j), see kv_scales_of
 };
 
-// The scales of a key block, a lane's share of them: keys' (times c2) in lanes 0-7, log2 of the values' in 8-15 and their inverses in 16-23
+// The scales of a key block, a lane's share of them: keys' (times c2) in lanes 0-7, log2 of the values' in 8-15 and their inverses in 16-23.
+// (A factor below fp32's numbers, or above them, would make NaNs of masked scores, -inf, and of scores of 0.)
 __device__ __forceinline__ float kv_scales_of(const FwdParams& p, int hkv, int b, int krow0, int j, int lane, float c2) {
   if (lane >= 24) return 0.f;
   const float s = __ldg(p.kv_scales + ((size_t)hkv * p.scale_tiles + krow0 / 128 + b + j) * 24 + lane);
-  return lane < 8 ? s * c2 : s;
+  return lane < 8 ? fminf(fmaxf(s * c2, FLT_MIN), FLT_MAX) : s;
 }
 // A key block of one scale: the keys' (times c2), log2 of the values', and its inverse
 __device__ __forceinline__ void whole_scales(float sc, float& key, float& value, float& back) {

@@ -1,8 +1,11 @@
-"""Prompts over an e4m3 cache at their limits: requests whose cache holds infinities and NaNs beside others."""
+"""Prompts over an e4m3 cache at their limits: requests whose cache holds infinities and NaNs beside others, and scores whose factors leave fp32."""
 import math
 
 import pytest
 import torch
+
+from tests import parity
+from tests import rotary_reference as R
 
 pytestmark = pytest.mark.gpu
 
@@ -68,3 +71,36 @@ def test_requests_do_not_reach_one_another(mala, ps, Hq, Hkv, d, what, tau, spli
         assert torch.isnan(mine[..., col]).all() and torch.equal(got[1], clean[1])
         rest = [c for c in range(d) if c != col]
         assert torch.equal(mine[..., rest], clean[0][:, cu[1]:cu[2]][..., rest])
+
+
+UP = 2.0 ** 60
+
+
+@pytest.mark.parametrize("ps,d", [(64, 64), (128, 64), (128, 128)])
+@pytest.mark.parametrize("splits", [1, 2])
+def test_scores_whose_factor_is_below_fp32(mala, ps, d, splits):
+    """scale * key scale below the least number of fp32: all scores are 0, and masked keys stay masked."""
+    n, new, Hq, Hkv = 300, 70, 4, 2
+    (kp, vp), (ks, vs), table = _cache(5, [n], ps, Hkv, d)
+    ks = torch.full_like(ks, 1 / UP)
+    q = _randn(4, 1, new, Hq, d)
+    o, lse, _ = mala.fwd_paged_fp8(q, kp, vp, ks, vs, _i32([0, new]), table, _i32([n]), new, n, 1e-30, 0.0, num_splits=splits)
+    x = torch.arange(n, device="cuda")
+    page, at = table[0][x // ps].long(), x % ps
+    v = vp[page, at].double() * vs[page, :, at // 128].double()[..., None]
+    for h in range(Hq):
+        w, z, a = R.attention(q[0, :, h].double() * 0, v[:, h // 2] * 0, v[:, h // 2], 1.0)
+        parity.check_output(o[0, :, h].double().cpu().numpy(), w.cpu().numpy(), a_ref=a.cpu().numpy())
+        assert ((lse[h].double() - z).abs() <= 2.0 ** -20 * (1 + z.abs())).all()
+
+
+@pytest.mark.parametrize("ps,d", [(64, 64), (128, 64), (128, 128)])
+def test_scores_of_zero_whose_factor_is_above_fp32(mala, ps, d):
+    """scale * key scale above the largest number of fp32, queries of 0: all scores are 0."""
+    n, new, Hq, Hkv = 300, 70, 4, 2
+    (kp, vp), (ks, vs), table = _cache(5, [n], ps, Hkv, d)
+    ks = torch.full_like(ks, UP)
+    q = torch.zeros((1, new, Hq, d), dtype=torch.bfloat16, device="cuda")
+    o, lse, _ = mala.fwd_paged_fp8(q, kp, vp, ks, vs, _i32([0, new]), table, _i32([n]), new, n, 1e30, 0.0)
+    visible = torch.arange(n - new + 1, n + 1, device="cuda").double()
+    assert torch.isfinite(o).all() and ((lse.double() - visible.log()).abs() <= 2.0 ** -20 * (1 + visible.log())).all()
