@@ -19,11 +19,14 @@ struct RotaryRule {
   float magnitude, turned;  // factor on the rotated columns; the same with the sense of the rotation as its sign
 };
 
-// Angles.  A frequency becomes turns per position in units of 2^-64, so that pos * f modulo a turn is a 64-bit product of whole numbers,
-// exact however far the position lies; its upper 32 bits are the phase.  (In fp32 an angle of 10^6 radians would be off by 0.06.)
+// Angles.  A frequency becomes turns per position in whole units of 2^-64, so that pos * f modulo a turn is a 64-bit product of whole numbers; its upper 32 bits are
+// the phase.  What is lost is a unit times the position, 2^-33 of a turn at 2^31, and the phase's last bit: below 2^-31 of a turn wherever the position lies.  For that
+// 1 / (2 pi) comes in two doubles and the product's rounding is kept (left out it is 2^-24.7 of a turn at 2^31).  (In fp32 an angle of 10^6 radians would be off by 0.06.)
 __device__ __forceinline__ uint64_t turns_of(double radians) {
-  const double t = radians * 0.15915494309189533577;     // 1 / (2 pi)
-  return (uint64_t)__double2ll_rn((t - rint(t)) * 18446744073709551616.0);
+  constexpr double hi = 0.15915494309189535, lo = -9.839338337591243e-18;
+  const double t = __dmul_rn(radians, hi), rest = fma(radians, lo, fma(radians, hi, -t));   // (__dmul_rn: t is not to be one of a sum's fma)
+  const double units = 18446744073709551616.0;
+  return (uint64_t)__double2ll_rn((t - rint(t)) * units) + (uint64_t)__double2ll_rn((rest - rint(rest)) * units);
 }
 // cos and sin of pos * f: the nearest quarter of a turn by the phase's upper bits, the rest (at most pi / 4) by Taylor's series,
 // whose first terms left out are 1.8e-9 (sin) and 2.5e-8 (cos).
