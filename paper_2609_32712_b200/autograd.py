@@ -123,7 +123,7 @@ class _RotaryPositions(torch.autograd.Function):
         q, k, q_weight, k_weight, positions, cu_q, cu_k, _ = ctx.saved_tensors
         rot, eps = ctx.args
         norm, weights = _head_norm(eps, q_weight, k_weight), any(ctx.needs_input_grad[2:4])
-        dq, dk = _incoming(dq), _incoming(dk)
+        dq, dk = _incoming(dq), (None if dk is None else _incoming(dk))   # (without keys there is no gradient of them)
         if cu_q is not None:
             dq, dk, dwq, dwk = mala.rotary_varlen_bwd(dq, dk, cu_q, cu_k, rot, norm, q, k, weights=weights)
         else:
@@ -212,8 +212,9 @@ def mala_attention_bias_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor
 
 def rotary(q: torch.Tensor, k: torch.Tensor, rot: mala.Rotary, positions: Optional[torch.Tensor] = None,
            q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: Optional[float] = None):
-    """Rotary positions of bf16 q [B,Nq,Hq,d] and k [B,Nk,Hkv,d] (``mala.rotary``), differentiable once with respect to q and k; with
-    eps each head's row goes through a root-mean-square norm first, differentiable in its weights [d] too (None: 1).  Returns (q', k')."""
+    """Rotary positions of bf16 q [B,Nq,Hq,d] and k [B,Nk,Hkv,d] or None (``mala.rotary``), differentiable once with respect to q and k; with
+    eps each head's row goes through a root-mean-square norm first, differentiable in its weights [d] too (None: 1).  Returns (q', k'),
+    k' None without keys."""
     assert eps is not None or (q_weight is None and k_weight is None), "weights belong to a norm: give its eps"
     return _RotaryPositions.apply(q, k, q_weight, k_weight, rot, positions, None, eps)
 

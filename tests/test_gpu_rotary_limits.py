@@ -1,10 +1,12 @@
-"""Rotary positions at their limits: the phase of far positions, where a column shows it to its last bits."""
+"""Rotary positions at their limits: the phase of far positions, where a column shows it to its last bits, and the differentiable calls without keys."""
 import math
 from fractions import Fraction
 
 import numpy as np
 import pytest
 import torch
+
+from tests import rotary_reference as R
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +66,31 @@ def test_far_phases(mala, end, step, pair, interleaved):
             # 2^-31 turns; fp32's roundings of phase and series (2^-21 of a sine this small); half a step of bf16
             assert abs(y[second].item() - want) <= 2 * math.pi * 2.0 ** -31 + abs(want) * (2.0 ** -8 + 2.0 ** -21), (phase, y[second].item() / want)
             assert y[first].item() == 1.0
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("normed", [False, True])
+def test_gradients_without_keys(mala, packed, normed):
+    from paper_2609_32712_b200 import autograd as A
+    d, total = 64, 9
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q = torch.randn((1, total, 3, d), generator=g, device="cuda").to(torch.bfloat16).requires_grad_()
+    w = (torch.randn(d, generator=g, device="cuda") * 0.3 + 1).requires_grad_() if normed else None
+    rot, eps = mala.Rotary(mala.rotary_frequencies(48)[0]), 1e-5 if normed else None
+    cu = _i32([0, 4, 9])
+    if packed:
+        out, keys = A.rotary_packed(q, None, cu, cu, rot, q_weight=w, eps=eps)
+        pos = torch.tensor([0, 1, 2, 3, 0, 1, 2, 3, 4], device="cuda")[None]
+    else:
+        out, keys = A.rotary(q, None, rot, q_weight=w, eps=eps)
+        pos = torch.arange(total, device="cuda")[None]
+    assert keys is None
+    dy = torch.randn(q.shape, generator=g, device="cuda").to(torch.bfloat16)
+    out.backward(dy)
+    a = (pos, rot.inv_freq, False, 1.0, eps, w.detach() if normed else None)
+    dx, dw, total_w = R.backward(dy, q.detach(), *a)
+    size = R.backward_size(dy, q.detach(), *a)
+    # (tolerances of the calls with keys: half a step of bf16, 2^-19 of the terms before it; fp32 sums of 27 terms)
+    assert ((q.grad.double() - dx).abs() <= 2.0 ** -8 * dx.abs() + 2.0 ** -19 * size).all()
+    if normed:
+        assert ((w.grad.double() - dw).abs() <= total_w * (2.0 ** -19 + 40 * 2.0 ** -24)).all()
