@@ -6,6 +6,7 @@ derivative of the forward's output; at tau = 0 it is the exact FullAttn gradient
 """
 from __future__ import annotations
 
+import copy
 import math
 from typing import Optional
 
@@ -114,7 +115,7 @@ class _RotaryPositions(torch.autograd.Function):
         norm = _head_norm(eps, q_weight, k_weight)
         qo, ko = mala.rotary_varlen(q, k, *packed, rot, norm) if packed else mala.rotary(q, k, rot, positions, norm)
         ctx.save_for_backward(*((q, k) if norm else (None, None)), q_weight, k_weight, positions, *(packed or (None, None)), rot.inv_freq)
-        ctx.args = (rot, eps)
+        ctx.args = (copy.copy(rot), eps)     # (the caller's may get other frequencies before the backward pass)
         return qo, ko
 
     @staticmethod
@@ -145,7 +146,7 @@ class _MalaAttentionRotary(torch.autograd.Function):
             o, lse, _ = mala.fwd_chunk(qr, kr, v, scale, tau, causal=causal)
         ctx.save_for_backward(qr, kr, v, o, lse, *((q, k) if norm else (None, None)), q_weight, k_weight, positions, *(packed[:2] if packed else (None, None)),
                               rot.inv_freq)
-        ctx.args = (rot, packed and packed[2:], eps, tau, scale, causal)
+        ctx.args = (copy.copy(rot), packed and packed[2:], eps, tau, scale, causal)
         return o
 
     @staticmethod

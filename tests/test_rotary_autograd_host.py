@@ -55,3 +55,28 @@ def test_without_keys(A, packed, normed):
     pos = torch.tensor([0, 1, 2, 0, 1, 2, 3] if packed else range(7))[None]
     dx, dw, _ = R.backward(dy, q.detach(), pos, rot.inv_freq, False, 1.0, eps, None if w is None else w.detach())
     assert torch.equal(q.grad, dx.to(torch.bfloat16)) and (w is None or torch.equal(w.grad, dw.float()))
+
+
+@pytest.mark.parametrize("change", [dict(inv_freq=lambda r: r.inv_freq / 4), dict(magnitude=lambda r: 2.0), dict(interleaved=lambda r: True)])
+def test_rule_of_the_forward_pass(A, change):
+    """A Rotary whose frequencies are replaced behind a forward pass (a context that grows over its length): its gradients are those of that pass."""
+    from paper_2609_32712_b200 import mala
+    q, dy, _ = _inputs(False)
+    rot = mala.Rotary(0.3 ** torch.arange(6).double(), device="cpu")
+    A.rotary(q, q.detach(), rot)[0].backward(dy)
+    want, q.grad = q.grad, None
+    out = A.rotary(q, q.detach(), rot)[0]
+    for name, value in change.items():
+        setattr(rot, name, value(rot))
+    out.backward(dy)
+    assert torch.equal(q.grad, want)
+
+
+def test_frequencies_changed_in_place_are_noticed(A):
+    from paper_2609_32712_b200 import mala
+    q, dy, _ = _inputs(False)
+    rot = mala.Rotary(0.3 ** torch.arange(6).double(), device="cpu")
+    out = A.rotary(q, None, rot)[0]
+    rot.inv_freq.mul_(0.5)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.backward(dy)
