@@ -51,6 +51,11 @@ double number(PyObject* o) {
   if (x == -1.0 && PyErr_Occurred()) throw PythonError();
   return x;
 }
+bool truth(PyObject* o) {
+  const int x = PyObject_IsTrue(o);
+  if (x < 0) throw PythonError();
+  return x != 0;
+}
 int whole(PyObject* o) {
   const long x = PyLong_AsLong(o);
   if (x == -1 && PyErr_Occurred()) throw PythonError();
@@ -122,7 +127,7 @@ struct Rule {
     require(f.scalar_type() == at::kDouble && f.dim() == 1 && f.is_contiguous(), "expects frequencies in fp64");
     require(!q_weight || !k_weight || q_weight->scalar_type() == k_weight->scalar_type(), "expects weights of one type");
     here.on(f);
-    rotary = {f.data_ptr<double>(), 2 * size(f, 0), PyObject_IsTrue(a[1]), (float)number(a[2])};
+    rotary = {f.data_ptr<double>(), 2 * size(f, 0), truth(a[1]), (float)number(a[2])};
     norm = {};
     if (!normed) return;
     for (const Arg* w : {&q_weight, &k_weight}) {
@@ -229,7 +234,7 @@ PyObject* rotary_bwd(PyObject* const* a) {
   const Here here;
   const at::Tensor& dq = tensor(a[0]);
   const Arg dk(a[1]), q(a[11]), k(a[12]), dq_out(a[13]), dk_out(a[14]);
-  const bool weights = PyObject_IsTrue(a[15]);
+  const bool weights = truth(a[15]);
   const Call c(dq, dk, a[8], a[9], a[10], here);
   const Rule r(a + 2, c.d, here);
   if (r.normed) {
@@ -326,7 +331,7 @@ PyObject* cache_read(PyObject* const* a) {
 PyObject* fwd_paged_fp8(PyObject* const* a) {
   const Here here;
   const at::Tensor &q = tensor(a[0]), &kp = tensor(a[1]), &vp = tensor(a[2]), &ks = tensor(a[3]), &vs = tensor(a[4]), &cu = tensor(a[5]), &table = tensor(a[6]), &lens = tensor(a[7]);
-  const int max_q = whole(a[8]), total_k = whole(a[9]), causal = PyObject_IsTrue(a[12]);
+  const int max_q = whole(a[8]), total_k = whole(a[9]), causal = truth(a[12]);
   const float scale = (float)number(a[10]), tau = (float)number(a[11]);
   const Arg ws_given(a[14]), retained(a[15]), bitmask(a[16]), totals(a[17]);
   require(q.dim() == 4 && q.size(0) == 1 && kp.dim() == 4 && table.dim() == 2, "expects q [1,total_q,Hq,d], pages [num_pages, page_size, Hkv, d] and a block table");
