@@ -987,12 +987,14 @@ def rotary_bwd(dq, dk, rot: Rotary, positions=None, norm: Optional[HeadNorm] = N
 def rotary_varlen(q, k, cu_seqlens_q, cu_seqlens_k, rot: Rotary, norm: Optional[HeadNorm] = None, q_out=None, k_out=None):
     """mala_rotary_fwd_varlen: rotary on packed sequences, q [1,total_q,Hq,d], k [1,total_k,Hkv,d] (or None) with offsets int32 [B+1] on
     the device (the same tensor twice for self attention); positions count within a sequence's keys.  Returns (q', k')."""
+    assert cu_seqlens_q is not None and cu_seqlens_k is not None, "expects the offsets of both"
     return _done(_native().rotary(q, k, *_rule(rot, norm), None, cu_seqlens_q, cu_seqlens_k, q_out, k_out), "mala_rotary_fwd_varlen")
 
 
 def rotary_varlen_bwd(dq, dk, cu_seqlens_q, cu_seqlens_k, rot: Rotary, norm: Optional[HeadNorm] = None, q=None, k=None, dq_out=None,
                       dk_out=None, weights: bool = True):
     """mala_rotary_bwd_varlen: as rotary_bwd, on packed sequences."""
+    assert cu_seqlens_q is not None and cu_seqlens_k is not None, "expects the offsets of both"
     return _done(_native().rotary_bwd(dq, dk, *_rule(rot, norm), None, cu_seqlens_q, cu_seqlens_k, q, k, dq_out, dk_out, weights),
                  "mala_rotary_bwd_varlen")
 

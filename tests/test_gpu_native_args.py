@@ -30,3 +30,15 @@ def test_flags_without_a_truth_value(mala):
         mala.rotary(q, None, rot)
     torch.cuda.synchronize()
     assert mala.device_status() == 0
+
+
+def test_packed_calls_without_offsets(mala):
+    """No offsets, or those of one side only, are not the call for sequences of one length."""
+    q = torch.zeros((1, 4, 2, 16), dtype=torch.bfloat16, device="cuda")
+    rot, cu = mala.Rotary(torch.ones(8, dtype=torch.float64)), torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    from paper_2609_32712_b200 import autograd as A
+    for a, b in ((None, None), (cu, None), (None, cu)):
+        for call in (lambda: mala.rotary_varlen(q, q, a, b, rot), lambda: mala.rotary_varlen_bwd(q, q, a, b, rot), lambda: A.rotary_packed(q, q, a, b, rot)):  # noqa: B023
+            with pytest.raises(AssertionError):
+                call()
+    assert torch.equal(mala.rotary_varlen(q, q, cu, cu, rot)[0], q)
