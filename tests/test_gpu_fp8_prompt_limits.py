@@ -1,4 +1,5 @@
-"""Prompts over an e4m3 cache at their limits: requests whose cache holds infinities and NaNs beside others, and scores whose factors leave fp32."""
+"""Prompts over an e4m3 cache at their limits: requests whose cache holds infinities and NaNs beside others, scores whose factors leave fp32, and scales at
+the ends of the range that comes in at the softmax and beyond it, against attention in 64 bits."""
 import math
 
 import pytest
@@ -74,6 +75,38 @@ def test_requests_do_not_reach_one_another(mala, ps, Hq, Hkv, d, what, tau, spli
 
 
 UP = 2.0 ** 60
+
+
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("value", [UP, UP * (1 + 2.0 ** -23), 2 * UP, 1e25, 1 / UP, (1 - 2.0 ** -24) / UP, 0.5 / UP])
+@pytest.mark.parametrize("ps,splits", [(64, 1), (128, 1), (64, 3), (256, 3)])
+def test_scales_at_the_ends(mala, which, value, ps, splits):
+    """Scales of 2^-60 and 2^60, which come in at the softmax, and beyond, where values are bf16(scale * code), in some units of a KV head, against
+    attention over these values in 64 bits.  Queries are scaled down where keys are large, so that scores stay at a few units."""
+    n, new, Hq, Hkv, d = 700, 130, 4, 2, 64
+    (kp, vp), (ks, vs), table = _cache(13, [n], ps, Hkv, d)
+    (ks if which == "k" else vs)[table[0, [0, 2]].long(), 1] = value
+    q = _randn(4, 1, new, Hq, d)
+    if which == "k" and value > 1:
+        q = (q.float() * 2.0 ** -(round(math.log2(value)) + 7)).to(torch.bfloat16)          # (exact)
+    o, lse, _ = mala.fwd_paged_fp8(q, kp, vp, ks, vs, _i32([0, new]), table, _i32([n]), new, n, 1 / 8, 0.0, num_splits=splits)
+    x = torch.arange(n, device="cuda")
+    page, at = table[0][x // ps].long(), x % ps
+    keys = []
+    for t, s in ((kp, ks), (vp, vs)):
+        code, by = t[page, at].float(), s[page, :, at // 128][..., None]
+        apart = (by >= 1 / UP) & (by <= UP)
+        keys.append(torch.where(apart, code.double() * by.double(), (code * by).to(torch.bfloat16).double()))
+    for h in range(Hq):
+        qd, k, v = q[0, :, h].double(), keys[0][:, h // 2], keys[1][:, h // 2]
+        w, z, a = R.attention(qd, k, v, 1 / 8)
+        assert z.abs().max() < 100                          # (scores of a few units: what the tolerances below are for)
+        parity.check_output(o[0, :, h].double().cpu().numpy(), w.cpu().numpy(), a_ref=a.cpu().numpy())
+        # as for scales in the middle: fp32 sums of d products, off by at most (d + 4) 2^-24 of the sum of their magnitudes; exp2 and the sums by a few 2^-23 more
+        most = (qd.abs() @ k.abs().T).amax(1) / 8
+        err = (lse[h].double() - z).abs()
+        assert (err <= (d + 4) * 2.0 ** -24 * most + 2.0 ** -20 * (1 + z.abs())).all(), err.max().item()
+    assert mala.device_status() == 0
 
 
 @pytest.mark.parametrize("ps,d", [(64, 64), (128, 64), (128, 128)])
