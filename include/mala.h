@@ -396,7 +396,7 @@ int mala_page_tables_positions(const int32_t* seqlens, const int32_t* new_tokens
  * what its row of the table can map.  rows: room in the outputs, at least the sum of the lengths; of a sequence that reaches
  * beyond it only what fits is there, in cu_seqlens too.  A key whose page is not one of the pool's is 0.  The first 128 rows behind the last
  * sequence (as far as there are) are set to 0, so that the tiles of the packed calls may cover them; the others stay as they were.
- * d a multiple of 8 up to 256. */
+ * d a multiple of 8 up to 256; B <= 16384 and at most 2^30 rows. */
 int mala_cache_read(mala_tin kpages, mala_tin vpages, const int32_t* block_table, const int32_t* seqlens, mala_tout k_out,
                     mala_tout v_out, int32_t* cu_seqlens, int B, int Hkv, int num_pages, int page_size,
                     int max_pages_per_seq, int rows, int d, void* cuda_stream);
@@ -412,7 +412,7 @@ int mala_cache_read_fp8(mala_tin kpages8, mala_tin vpages8, const float* kscale,
  * at the softmax; beyond 2^-60 .. 2^60, or not positive, bf16(scale * code)).  total_k: room for keys in the workspace, at least the sum of
  * seqlens_k (see mala_cache_read_fp8 for what lies beyond it: the sequences that reach beyond have no meaningful result).
  * A sequence's result is the same whatever the other sequences' keys and values are, infinities and NaNs among them.
- * Workspace: mala_paged_fp8_workspace_bytes.  d a multiple of 16 up to 128, page_size not 8; everything else as
+ * Workspace: mala_paged_fp8_workspace_bytes.  d a multiple of 16 up to 128, page_size not 8, B <= 16384, total_k <= 2^30; everything else as
  * mala_fwd_paged; telemetry laid out for max_seqlen_k = min(max_pages_per_seq * page_size, total_k). */
 int mala_fwd_paged_fp8(mala_tin q, mala_tin kpages8, mala_tin vpages8, const float* kscale, const float* vscale,
                        const int32_t* cu_seqlens_q, const int32_t* block_table, const int32_t* seqlens_k, mala_tout o,
@@ -439,7 +439,7 @@ int mala_paged_fp8_suggest_splits(int B, int Hq, int max_seqlen_q, int max_seqle
  * the columns i and i + rotary / 2, or, interleaved != 0, 2 i and 2 i + 1:
  *     (y1, y2) -> magnitude * (y1 cos - y2 sin, y2 cos + y1 sin);   columns from rotary on stay as they are.
  * inv_freq: DEVICE pointer, doubles [rotary / 2], radians per position (scaled for long contexts or not); the struct itself is read during the
- * call.  Angles are exact to about 2^-31 of a turn wherever the position lies.
+ * call.  Angles are exact to 2^-31 of a turn wherever the position lies, their cosines and sines to 2^-23.
  * norm (may be NULL): before its rotation each head's row is normed, y = x / sqrt(mean(x^2) + eps) * weight, over all d columns;
  * weights [d] on the device, bf16 or (weights_fp32 != 0) fp32, NULL: 1.  All arithmetic is fp32, rounded once to bf16.
  * d a multiple of 8 up to 256; at most 2^30 rows per tensor. */

@@ -40,7 +40,8 @@ __device__ __forceinline__ uint4 negated(const uint4& w) {
 // partners (halves), or neighbouring pieces.  Between maxima and codes of a head the block meets once; the units' maxima
 // change places among three buffers, so that one is emptied while two are in use.  35 thousand rows, 32 + 8 heads of 128 columns, pages of 64: 89 us alone, and 168
 // with the queries' rotation beside it, whose 87 are bound by HBM; half of the issue slots go to quotients, rotation and maxima, the rest waits at the
-// meetings.  A decode step of 64 rows, 8.6 us with the queries' rotation: the chain slots -> rows -> maximum -> scale -> codes.
+// meetings.  A decode step of 64 rows, 8.6 us with the queries' rotation: the chain slots -> rows -> maximum -> scale -> codes,
+// on which the angles stand that all threads work out, those without a row too (some 400 of 1100 instructions per warp).
 template <int kPairs, int kPer, int kThreads>   // kPer: rows of a thread
 __global__ void __launch_bounds__(kThreads, 512 / kThreads)
 rotary_write8_kernel(const RotaryWriteParams p) {
